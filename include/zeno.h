@@ -306,6 +306,97 @@ zeno_status zeno_score_lsq_static(int32_t device, const float *x, const float *V
                                   int32_t m, const float *A, const float *y, int32_t n_r, float gamma,
                                   float rho, float *scores, float *losses, float *norms, void *stream);
 
+/* ---- Operators of language models, on activations and logits that the caller's own model computes ----------------------
+ *
+ * A worker of Algorithm 1 that trains a language model, and a server that evaluates m + 1 of them (Definition 2), run most of
+ * the model in a framework of their own.  These calls are the parts that belong next to the candidates: norm layers and
+ * dense layers whose weight gradients go to every worker's own row of V (not summed over the workers), activations kept in
+ * 8 bits for the backward pass, and the loss over a large vocabulary with its gradient.
+ *
+ * Conventions besides those at the top of this file: no handle; `device` is the CUDA device of all pointers.  Activations
+ * are m groups (workers, or models) of n rows (tokens) each, described by zeno_rows.  m or n may be zero: nothing is read,
+ * per-token outputs are left alone and weight gradients become zero.  `type` is the storage type of activations and logits,
+ * `param_type` that of weights and weight gradients; sums, statistics and products are kept in binary32, and results are
+ * rounded once, when they are stored.  No output may overlap an input or another output unless the call says so.
+ * Scratch is the caller's (`workspace`, 16-byte aligned, as many bytes as the call's _workspace function says, contents
+ * irrelevant): calls that may overlap on the GPU need workspaces of their own.  Results do not depend on the order in which
+ * blocks run.  The first call on a device makes the CUDA runtime load the library's code: make it before a stream capture.
+ * INVALID_ARG: a NULL pointer where one is required, a type outside zeno_dtype, a negative size, a stride smaller than the
+ * row, a NaN or infinite scalar, a workspace that is too small.  UNSUPPORTED: more than 65535 groups, more than 2^31 - 1 rows,
+ * or rows of more than 2^30 entries. */
+typedef struct {
+    void *data;
+    int64_t row;   /* elements from one row of a group to the next */
+    int64_t group; /* elements from one group's first row to the next group's; 0 in an input: the same rows for all groups */
+} zeno_rows;
+
+/* Columns that share a scale in activations kept in 8 bits. */
+#define ZENO_SAVED_BLOCK 128
+/* Most alternatives zeno_token_logprobs lists. */
+#define ZENO_MAX_TOP 32
+
+/* Layer norm of every row:  y_j = (x_j - mean) rstd w_j + b_j,  mean and variance over the row's cols entries,
+ * rstd = (variance + eps)^(-1/2); the variance is the mean square of the centred entries.  w, b: cols entries, ldw elements
+ * from one group's to the next (0: shared by all groups); b may be NULL.  mean, rstd: float[m][n] or NULL.
+ * y may be x itself (same pointer and strides).  INVALID_ARG also: cols < 1, eps < 0. */
+zeno_status zeno_layer_norm(int32_t device, int32_t type, int32_t param_type, const zeno_rows *x, int32_t m, int64_t n,
+                            int64_t cols, const void *w, const void *b, int64_t ldw, float eps, const zeno_rows *y,
+                            float *mean, float *rstd, void *stream);
+
+/* The backward pass of zeno_layer_norm from dy, the gradient at y: with h = (x - mean) rstd and g = dy w,
+ *   dx = rstd (g - avg(g) - h avg(g h))      (averages over the row),
+ *   dw[i] = sum over group i's rows of dy h,  db[i] = sum over group i's rows of dy.
+ * The layer's input is x, or (x NULL) what zeno_pack_activations kept of it: codes and scales.  mean and rstd are those of
+ * the forward pass.  dx or NULL; it may be dy itself.  dw, db: group i's gradient starts ldg elements after group i - 1's, as in
+ * a slice of V; either may be NULL, and w then too if dx is NULL. */
+int64_t zeno_layer_norm_gradient_workspace(int32_t m, int64_t n, int64_t cols);
+zeno_status zeno_layer_norm_gradient(int32_t device, int32_t type, int32_t param_type, const zeno_rows *dy, const zeno_rows *x,
+                                     const zeno_rows *codes, const zeno_rows *scales, int32_t m, int64_t n, int64_t cols,
+                                     const void *w, int64_t ldw, const float *mean, const float *rstd, const zeno_rows *dx,
+                                     void *dw, void *db, int64_t ldg, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Activations in 8 bits.  A row is cut into blocks of ZENO_SAVED_BLOCK columns (the last one may be shorter).  A block's
+ * scale is the smallest power of two 2^k, k in [-117, 119], with max |x_j| <= 448 * 2^k (1 for a block of zeros), its codes are
+ * x_j / 2^k rounded to nearest even in e4m3 (four exponent bits, three of mantissa, no infinity); the value kept, code * scale,
+ * is exact in bfloat16 and in binary32 and off by at most 2^-4 of |x_j|, or 2^(k-10) if that is more.  Entries beyond 448 * 2^119
+ * are kept as that.  An infinity or NaN is kept as NaN and does not count for the maximum.
+ * codes: bytes; scales: float, ceil(cols / ZENO_SAVED_BLOCK) to a row. */
+zeno_status zeno_pack_activations(int32_t device, int32_t type, const zeno_rows *x, int32_t m, int64_t n, int64_t cols,
+                                  const zeno_rows *codes, const zeno_rows *scales, void *stream);
+
+/* A dense layer's weight gradient for every group, from the gradient dy at its output and its input as
+ * zeno_pack_activations kept it:  dw[i][o][k] = sum over group i's rows of dy_o x_k,  db[i][o] = sum of dy_o.
+ * dw: per group outputs x inputs entries, row-major, ldw elements after the previous group's; db (or NULL) likewise with ldb:
+ * slices of V in the layout of the parameter vector.  The products are exact and summed in binary32.
+ * Aligned bfloat16 dy (rows and groups of multiples of 16 bytes) goes to the tensor cores. */
+int64_t zeno_dense_gradient_workspace(int32_t m, int64_t n, int64_t inputs, int64_t outputs);
+zeno_status zeno_dense_gradient(int32_t device, int32_t type, int32_t param_type, const zeno_rows *dy, const zeno_rows *codes,
+                                const zeno_rows *scales, int32_t m, int64_t n, int64_t inputs, int64_t outputs, void *dw,
+                                int64_t ldw, void *db, int64_t ldb, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Log probabilities of given tokens.  For every row z of vocab logits:
+ *   lse = log sum_j exp(z_j),  logprob = z_target - lse,  entropy = -sum_j p_j log p_j with p_j = exp(z_j - lse),
+ *   the `top` largest logits' indices in order (equal ones: lower index first; a NaN ranks with minus infinity) and their
+ *   log probabilities.
+ * targets: int32[m][n]; one outside [0, vocab) means that the row has none: logprob 0.  logprobs (needs targets), entropy, lse:
+ * float[m][n], top_idx: int32[m][n][top], top_logprobs: float[m][n][top]; each may be NULL.
+ * A logit of minus infinity has probability zero.  A row of nothing else has lse and log probabilities of minus infinity and
+ * entropy 0.  A row with a NaN or plus infinity gives NaN.
+ * INVALID_ARG also: vocab < 1, top < 0 or > vocab.  UNSUPPORTED: top > ZENO_MAX_TOP. */
+zeno_status zeno_token_logprobs(int32_t device, int32_t type, const zeno_rows *logits, int32_t m, int64_t n, int64_t vocab,
+                                const int32_t *targets, int32_t top, float *logprobs, float *entropy, float *lse,
+                                int32_t *top_idx, float *top_logprobs, void *stream);
+
+/* The gradient at the logits of  sum over rows of g_logprob logprob + g_entropy entropy:
+ *   dz_j = g_logprob ([j = target] - p_j) - g_entropy p_j (log p_j + entropy),
+ * from zeno_token_logprobs's lse and entropy.  (The mean loss of n tokens has g_logprob = -1 / n.)  lse, g_logprob: float[m][n];
+ * g_entropy: float[m][n], or NULL for none, and entropy then too.  A row without a target has no first term, and if g_entropy
+ * is NULL its gradient is zero whatever its logits; so is that of a row whose logits are all minus infinity.
+ * grad: in the type of the logits; it may be the logits themselves. */
+zeno_status zeno_token_gradient(int32_t device, int32_t type, const zeno_rows *logits, int32_t m, int64_t n, int64_t vocab,
+                                const int32_t *targets, const float *lse, const float *entropy, const float *g_logprob,
+                                const float *g_entropy, const zeno_rows *grad, void *stream);
+
 /* Synchronises `stream` and reports whether any kernel enqueued through this handle gave up on a
  * bounded device-side wait (its outputs are then undefined): ZENO_ERR_TIMEOUT if so, else
  * ZENO_OK.  The condition is sticky for the life of the handle. */

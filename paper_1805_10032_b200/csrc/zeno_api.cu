@@ -5,11 +5,12 @@
 #include <stdlib.h>
 #include <string.h>
 
-#include <nvtx3/nvToolsExt.h>
-
+#include "zeno_guard.h"
 #include "zeno_internal.h"
 
 using zeno::Context;
+using zeno::DeviceGuard;
+using zeno::Range;
 
 struct zeno_context : public Context {};
 
@@ -54,29 +55,6 @@ size_t feature_count(const zeno_model_desc &d) {
 }
 
 bool is_aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-// A named range around an entry point, visible on a profiler's timeline (a no-op without one attached).
-struct Range {
-    explicit Range(const char *name) { nvtxRangePushA(name); }
-    ~Range() { nvtxRangePop(); }
-};
-
-// Switches to the handle's device for the duration of a call and back afterwards.
-struct DeviceGuard {
-    int prev = -1;
-    bool switched = false;
-    cudaError_t err = cudaSuccess;
-    explicit DeviceGuard(int dev) {
-        err = cudaGetDevice(&prev);
-        if (err == cudaSuccess && prev != dev) {
-            err = cudaSetDevice(dev);
-            switched = err == cudaSuccess;
-        }
-    }
-    ~DeviceGuard() {
-        if (switched) cudaSetDevice(prev);
-    }
-};
 
 // Per-kernel timing: a call starts a fresh list of events and closes it after its last kernel.
 void profile_begin(Context *c) { c->profiled = 0; }

@@ -1,0 +1,108 @@
+// Internal declarations of the language model operators (zeno_norm.cu, zeno_saved.cu, zeno_tokens.cu): arguments checked, the
+// device current, at least one row unless noted.
+#pragma once
+
+#include "zeno_internal.h"
+
+namespace zeno {
+
+// Rows of m groups of n: row r is row r % n of group r / n.  Strides in elements.
+struct Rows {
+    void *data;
+    int64_t row, group;
+    int64_t n;
+#ifdef __CUDACC__
+    __device__ __forceinline__ int64_t at(int64_t r) const {
+        const uint32_t g = (uint32_t)r / (uint32_t)n;          // rows are counted in 31 bits
+        return (int64_t)g * group + (int64_t)((uint32_t)r - g * (uint32_t)n) * row;
+    }
+#endif
+};
+
+struct NormArgs {
+    Rows x, y;
+    int m;
+    int64_t n, cols;
+    const void *w, *b;
+    int64_t ldw;
+    float eps;
+    float *mean, *rstd;
+};
+cudaError_t launch_layer_norm(int type, int param_type, const NormArgs &a, cudaStream_t s);
+
+struct NormGradArgs {
+    Rows dy, x, codes, scales, dx;      // x.data NULL: codes and scales; dx.data NULL: not wanted
+    int m;
+    int64_t n, cols;
+    const void *w;
+    int64_t ldw;
+    const float *mean, *rstd;
+    void *dw, *db;                      // either may be NULL
+    int64_t ldg;
+    float *workspace;
+};
+int64_t norm_gradient_workspace(int m, int64_t n, int64_t cols);
+cudaError_t launch_layer_norm_gradient(int type, int param_type, const NormGradArgs &a, cudaStream_t s);   // n may be 0
+
+struct PackArgs {
+    Rows x, codes, scales;
+    int m;
+    int64_t n, cols;
+};
+cudaError_t launch_pack(int type, const PackArgs &a, cudaStream_t s);
+
+struct DenseGradArgs {
+    Rows dy, codes, scales;
+    int m;
+    int64_t n, inputs, outputs;
+    void *dw, *db;                      // db may be NULL
+    int64_t ldw, ldb;
+    float *workspace;
+};
+int64_t dense_gradient_workspace(int m, int64_t n, int64_t inputs, int64_t outputs);
+cudaError_t launch_dense_gradient(int type, int param_type, const DenseGradArgs &a, cudaStream_t s);       // n may be 0
+
+struct LogprobArgs {
+    Rows logits;
+    int m;
+    int64_t n, vocab;
+    const int32_t *targets;
+    int top;
+    float *logprobs, *entropy, *lse;
+    int32_t *top_idx;
+    float *top_logprobs;
+};
+cudaError_t launch_token_logprobs(int type, const LogprobArgs &a, cudaStream_t s);
+
+struct TokenGradArgs {
+    Rows logits, grad;
+    int m;
+    int64_t n, vocab;
+    const int32_t *targets;
+    const float *lse, *entropy, *g_logprob, *g_entropy;
+};
+cudaError_t launch_token_gradient(int type, const TokenGradArgs &a, cudaStream_t s);
+
+#ifdef __CUDACC__
+
+// An element as it lies in memory; without the read-only path, since an output may lie in its input's place.
+__device__ __forceinline__ float value_of(const float *p) { return *p; }
+__device__ __forceinline__ float value_of(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void put(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+
+// Sum over the block in every thread; `scratch` holds a float for each warp and may be used again after the next barrier.
+template <int THREADS>
+__device__ __forceinline__ float block_sum(float v, float *scratch) {
+    v = warp_sum(v);
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) s += scratch[i];
+    return s;
+}
+
+#endif
+
+}  // namespace zeno

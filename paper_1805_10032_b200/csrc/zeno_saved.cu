@@ -1,0 +1,141 @@
+// Activations kept in 8 bits for the backward pass, and the dense layers' weight gradients that are taken from them.
+#include "zeno_saved.cuh"
+
+namespace zeno {
+
+namespace {
+
+constexpr int kBlock = ZENO_SAVED_BLOCK;
+constexpr int kMinExp = -117, kMaxExp = 119;
+
+// bits of |v| if it is finite, else 0: non-finite entries do not count for a block's maximum
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+    const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
+    return u < 0x7f800000u ? u : 0u;
+}
+
+// k of a block's scale 2^k: amax = f 2^e with 1 <= f < 2 is at most 448 2^k = 1.75 2^(k+8) from k = e - 8 on if f <= 1.75, else
+// from e - 7 on.  Subnormal maxima are far below the smallest k.
+__device__ __forceinline__ int scale_exponent(uint32_t amax) {
+    const int k = (int)(amax >> 23) - 127 - 8 + ((amax & 0x7fffffu) > 0x600000u);
+    return min(max(k, kMinExp), kMaxExp);
+}
+
+// one code: to nearest even; the conversion saturates, and infinities are made NaN like NaN itself
+__device__ __forceinline__ uint8_t code_of(float v, float inv_scale) {
+    const float q = fabsf(v) < INFINITY ? v * inv_scale : NAN;
+    return (uint8_t)__nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
+}
+
+// A warp takes a block of one row.
+template <typename T>
+__global__ void __launch_bounds__(256) pack_any_kernel(PackArgs a, int64_t blocks_per_row, int64_t blocks) {
+    const int lane = threadIdx.x & 31;
+    for (int64_t q = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); q < blocks; q += (int64_t)gridDim.x * 8) {
+        const int64_t r = q / blocks_per_row, blk = q - r * blocks_per_row;
+        const T *x = static_cast<const T *>(a.x.data) + a.x.at(r) + blk * kBlock;
+        uint8_t *codes = static_cast<uint8_t *>(a.codes.data) + a.codes.at(r) + blk * kBlock;
+        const int count = (int)min((int64_t)kBlock, a.cols - blk * kBlock);
+        float v[kBlock / 32];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < kBlock / 32; ++i) {
+            v[i] = lane + 32 * i < count ? value_of(x + lane + 32 * i) : 0.f;
+            amax = max(amax, finite_bits(v[i]));
+        }
+        amax = __reduce_max_sync(0xffffffffu, amax);
+        const int k = amax ? scale_exponent(amax) : 0;
+        const float inv = __uint_as_float((uint32_t)(127 - k) << 23);
+#pragma unroll
+        for (int i = 0; i < kBlock / 32; ++i)
+            if (lane + 32 * i < count) codes[lane + 32 * i] = code_of(v[i], inv);
+        if (lane == 0) (static_cast<float *>(a.scales.data) + a.scales.at(r))[blk] = __uint_as_float((uint32_t)(127 + k) << 23);
+    }
+}
+
+// dW of a tile of 64 outputs by 64 inputs of one group in a block: 16 rows at a time through shared memory, 4 x 4 sums a thread.
+template <typename T, typename P>
+__global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
+    constexpr int kTile = 64, kRows = 16;
+    __shared__ float sd[kRows][kTile], sx[kRows][kTile];
+    const int64_t o0 = (int64_t)blockIdx.y * kTile, k0 = (int64_t)blockIdx.x * kTile;
+    const int i = blockIdx.z, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    float acc[4][4] = {};
+    for (int64_t t0 = 0; t0 < a.n; t0 += kRows) {
+        for (int e = threadIdx.x; e < kRows * kTile; e += 256) {
+            const int t = e / kTile, c = e % kTile;
+            float d = 0.f, x = 0.f;
+            if (t0 + t < a.n) {
+                const int64_t r = i * a.n + t0 + t;
+                if (o0 + c < a.outputs) d = value_of(static_cast<const T *>(a.dy.data) + a.dy.at(r) + o0 + c);
+                if (k0 + c < a.inputs)
+                    x = saved_value((static_cast<const uint8_t *>(a.codes.data) + a.codes.at(r))[k0 + c],
+                                    (static_cast<const float *>(a.scales.data) + a.scales.at(r))[(k0 + c) / kBlock]);
+            }
+            sd[t][c] = d;
+            sx[t][c] = x;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kRows; ++t)
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(sd[t][ty + 16 * p], sx[t][tx + 16 * q], acc[p][q]);
+        __syncthreads();
+    }
+    P *dw = static_cast<P *>(a.dw) + i * a.ldw;
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t o = o0 + ty + 16 * p, k = k0 + tx + 16 * q;
+            if (o < a.outputs && k < a.inputs) put(dw + o * a.inputs + k, acc[p][q]);
+        }
+}
+
+// db: a block takes 32 outputs of a group, its warps the rows in turn
+template <typename T, typename P>
+__global__ void __launch_bounds__(256) dense_bias_kernel(DenseGradArgs a) {
+    __shared__ float sums[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.y;
+    const int64_t o = (int64_t)blockIdx.x * 32 + lane;
+    float s = 0.f;
+    if (o < a.outputs)
+        for (int64_t t = warp; t < a.n; t += 8) s += value_of(static_cast<const T *>(a.dy.data) + a.dy.at(i * a.n + t) + o);
+    sums[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && o < a.outputs) {
+#pragma unroll
+        for (int q = 1; q < 8; ++q) s += sums[q][lane];
+        put(static_cast<P *>(a.db) + i * a.ldb + o, s);
+    }
+}
+
+template <typename T, typename P>
+cudaError_t dense_gradient(const DenseGradArgs &a, cudaStream_t s) {
+    const dim3 grid((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m);
+    cudaError_t e = launch_chained(dense_any_kernel<T, P>, grid, dim3(256), 0, s, false, a);
+    if (e == cudaSuccess && a.db)
+        e = launch_chained(dense_bias_kernel<T, P>, dim3((unsigned)((a.outputs + 31) / 32), a.m), dim3(256), 0, s, false, a);
+    return e;
+}
+
+}  // namespace
+
+cudaError_t launch_pack(int type, const PackArgs &a, cudaStream_t s) {
+    const int64_t per_row = (a.cols + kBlock - 1) / kBlock, blocks = per_row * a.m * a.n;
+    const unsigned grid = (unsigned)min((blocks + 7) / 8, (int64_t)148 * 8);
+    return launch_chained(type == ZENO_BF16 ? pack_any_kernel<__nv_bfloat16> : pack_any_kernel<float>, dim3(grid), dim3(256), 0, s, false, a,
+                          per_row, blocks);
+}
+
+int64_t dense_gradient_workspace(int m, int64_t n, int64_t inputs, int64_t outputs) { return 0; }
+
+cudaError_t launch_dense_gradient(int type, int param_type, const DenseGradArgs &a, cudaStream_t s) {
+    if (type == ZENO_BF16)
+        return param_type == ZENO_BF16 ? dense_gradient<__nv_bfloat16, __nv_bfloat16>(a, s) : dense_gradient<__nv_bfloat16, float>(a, s);
+    return param_type == ZENO_BF16 ? dense_gradient<float, __nv_bfloat16>(a, s) : dense_gradient<float, float>(a, s);
+}
+
+}  // namespace zeno

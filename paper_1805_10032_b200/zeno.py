@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence, Union
 
 import torch
 
@@ -31,6 +31,8 @@ EXPORTS = (
     "zeno_profile", "zeno_profile_read",
     "zeno_last_launch_count",
     "zeno_last_cuda_error", "zeno_last_wait_code", "zeno_status_string",
+    "zeno_layer_norm", "zeno_layer_norm_gradient", "zeno_layer_norm_gradient_workspace", "zeno_pack_activations",
+    "zeno_dense_gradient", "zeno_dense_gradient_workspace", "zeno_token_logprobs", "zeno_token_gradient",
 )
 
 
@@ -43,6 +45,11 @@ class ModelDesc(ctypes.Structure):
 class Batch(ctypes.Structure):
     _fields_ = [("features", ctypes.c_void_p), ("targets", ctypes.c_void_p),
                 ("n_r", ctypes.c_int32)]
+
+
+class RowsDesc(ctypes.Structure):
+    """zeno_rows: where the rows of m groups of activations lie (strides in elements)."""
+    _fields_ = [("data", ctypes.c_void_p), ("row", ctypes.c_int64), ("group", ctypes.c_int64)]
 
 
 class ZenoError(RuntimeError):
@@ -115,6 +122,24 @@ def load_library() -> ctypes.CDLL:
     lib.zeno_last_wait_code.argtypes = [vp]
     lib.zeno_status_string.restype = ctypes.c_char_p
     lib.zeno_status_string.argtypes = [i32]
+    rows = ctypes.POINTER(RowsDesc)
+    lib.zeno_layer_norm.restype = i32
+    lib.zeno_layer_norm.argtypes = [i32, i32, i32, rows, i32, i64, i64, vp, vp, i64, f32, rows, vp, vp, vp]
+    lib.zeno_layer_norm_gradient.restype = i32
+    lib.zeno_layer_norm_gradient.argtypes = [i32, i32, i32, rows, rows, rows, rows, i32, i64, i64, vp, i64, vp, vp, rows, vp, vp,
+                                             i64, vp, i64, vp]
+    lib.zeno_layer_norm_gradient_workspace.restype = i64
+    lib.zeno_layer_norm_gradient_workspace.argtypes = [i32, i64, i64]
+    lib.zeno_pack_activations.restype = i32
+    lib.zeno_pack_activations.argtypes = [i32, i32, rows, i32, i64, i64, rows, rows, vp]
+    lib.zeno_dense_gradient.restype = i32
+    lib.zeno_dense_gradient.argtypes = [i32, i32, i32, rows, rows, rows, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.zeno_dense_gradient_workspace.restype = i64
+    lib.zeno_dense_gradient_workspace.argtypes = [i32, i64, i64, i64]
+    lib.zeno_token_logprobs.restype = i32
+    lib.zeno_token_logprobs.argtypes = [i32, i32, rows, i32, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.zeno_token_gradient.restype = i32
+    lib.zeno_token_gradient.argtypes = [i32, i32, rows, i32, i64, i64, vp, vp, vp, vp, vp, rows, vp]
     _lib = lib
     return lib
 
@@ -425,6 +450,234 @@ def score_lsq_static(x, V, A, y, gamma, rho, scores, losses=None, norms=None, m=
     if st != OK:
         raise ZenoError(st, "zeno_score_lsq_static")
     return scores
+
+
+# -- operators of language models -----------------------------------------------------------------------------------------
+# No handle: the device is the tensors', the stream its current one unless one is given, and what a call allocates (outputs
+# that are not passed in, scratch) belongs to that stream.  Activations are [m, n, columns] -- n tokens of each of m workers or
+# models -- or [n, columns]; any strides whose last one is 1, and inputs may be expanded over the groups.  Arguments that do
+# not fit raise ValueError, what the library refuses raises ZenoError.
+
+SAVED_BLOCK = 128
+MAX_TOP = 32
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+class Saved(NamedTuple):
+    """Activations kept in 8 bits: codes (float8_e4m3fn, shaped like the activations; rows start at multiples of 16 bytes)
+    and the scales of every 128 columns (float32 [.., ceil(columns / 128)]).  The values are codes * scales."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+class TokenLogprobs(NamedTuple):
+    logprobs: torch.Tensor
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_idx: Optional[torch.Tensor]
+    top_logprobs: Optional[torch.Tensor]
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _type(t: torch.Tensor, name: str) -> int:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{name}: float32 or bfloat16 is needed, not {t.dtype}")
+    return kind
+
+
+def _rows(t: torch.Tensor, name: str) -> RowsDesc:
+    _need(t.dim() in (2, 3), f"{name}: [m, n, columns] or [n, columns] is needed, not {tuple(t.shape)}")
+    _need(t.stride(-1) == 1 or t.shape[-1] <= 1, f"{name}: the last stride has to be 1")
+    return RowsDesc(t.data_ptr(), t.stride(-2), t.stride(0) if t.dim() == 3 else 0)
+
+
+def _sizes(t: torch.Tensor):
+    return (t.shape[0] if t.dim() == 3 else 1), t.shape[-2], t.shape[-1]
+
+
+def _cuda(dev: torch.device, **tensors):
+    _need(dev.type == "cuda", "CUDA tensors are needed")
+    for name, t in tensors.items():
+        _need(t is None or t.device == dev, f"{name}: on another device than the rest")
+
+
+def _per_token(t: Optional[torch.Tensor], like: torch.Tensor, dtype, name: str):
+    if t is not None:
+        _need(t.dtype == dtype and t.shape == like.shape[:-1] and t.is_contiguous(), f"{name}: contiguous {dtype} {tuple(like.shape[:-1])} is needed")
+
+
+def _current(dev: torch.device, stream) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream(dev).cuda_stream
+    return _raw_stream(dev.index)
+
+
+def _empty(stream, shape, dtype, dev):
+    """An output or scratch: memory of the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _scratch(stream, nbytes: int, dev):
+    return _empty(stream, nbytes, torch.uint8, dev) if nbytes else None
+
+
+def _done(st: int, what: str):
+    if st != OK:
+        raise ZenoError(st, what)
+
+
+def _norm_weight(w: Optional[torch.Tensor], x: torch.Tensor, name: str) -> int:
+    """Elements between the groups' weights: 0 if they share them."""
+    if w is None:
+        return 0
+    m, _, cols = _sizes(x)
+    _need(w.shape[-1] == cols and (w.dim() == 1 or (w.dim() == 2 and w.shape[0] == m)) and (w.stride(-1) == 1 or cols <= 1),
+          f"{name}: [{cols}] or [{m}, {cols}] with a last stride of 1 is needed")
+    return w.stride(0) if w.dim() == 2 and m > 1 else 0
+
+
+def layer_norm(x, weight, bias=None, eps=1e-5, out=None, want_stats=True, stream=None):
+    """zeno_layer_norm: returns (y, mean or None, rstd or None).  weight, bias: [columns], or [m, columns] where every model has its own (of one
+    stride: slices of the models' parameter vectors).  out may be x."""
+    lib = load_library()
+    m, n, cols = _sizes(x)
+    _cuda(x.device, weight=weight, bias=bias, out=out)
+    ldw = _norm_weight(weight, x, "weight")
+    if bias is not None:
+        _need(bias.dtype == weight.dtype and bias.dim() == weight.dim() and _norm_weight(bias, x, "bias") == ldw,
+              "bias: the type and layout of the weight is needed")
+    y = _empty(stream, x.shape, x.dtype, x.device) if out is None else out
+    _need(y.shape == x.shape and y.dtype == x.dtype, "out: the shape and type of x is needed")
+    mean = _empty(stream, x.shape[:-1], torch.float32, x.device) if want_stats else None
+    rstd = _empty(stream, x.shape[:-1], torch.float32, x.device) if want_stats else None
+    _done(lib.zeno_layer_norm(x.device.index, _type(x, "x"), _type(weight, "weight"), _rows(x, "x"), m, n, cols, _ptr(weight),
+                              _ptr(bias), ldw, eps, _rows(y, "out"), _ptr(mean), _ptr(rstd), _current(x.device, stream)), "zeno_layer_norm")
+    return y, mean, rstd
+
+
+def _saved_rows(saved, like, cols: int):
+    codes, scales = saved
+    lead = tuple(like.shape[:-1])
+    _need(codes.dtype in (torch.float8_e4m3fn, torch.uint8) and tuple(codes.shape) == lead + (cols,), f"codes: float8_e4m3fn {lead + (cols,)} is needed")
+    _need(scales.dtype == torch.float32 and tuple(scales.shape) == lead + (-(-cols // SAVED_BLOCK),),
+          f"scales: float32 {lead + (-(-cols // SAVED_BLOCK),)} is needed")
+    return _rows(codes, "codes"), _rows(scales, "scales")
+
+
+def _gradient_row(t: Optional[torch.Tensor], m: int, cols: int, like, name: str) -> int:
+    if t is None:
+        return 0
+    _need(t.dtype == like.dtype and tuple(t.shape) in ((m, cols),) + (((cols,),) if m == 1 else ()) and (t.stride(-1) == 1 or cols <= 1),
+          f"{name}: {like.dtype} [{m}, {cols}] with a last stride of 1 is needed")
+    return t.stride(0) if t.dim() == 2 else cols
+
+
+def layer_norm_gradient(dy, x: Union[torch.Tensor, Saved], weight, mean, rstd, dweight=None, dbias=None, dx=None, want_dx=True,
+                        stream=None):
+    """zeno_layer_norm_gradient: writes dweight and dbias ([m, columns], for instance V[:, at:at + columns], of one stride) and
+    returns dx (None if not wanted).  x: the layer's input, or what pack_activations kept of it.  dx may be dy."""
+    lib = load_library()
+    m, n, cols = _sizes(dy)
+    saved = isinstance(x, tuple)
+    _cuda(dy.device, x=x[0] if saved else x, scales=x[1] if saved else None, weight=weight, mean=mean, rstd=rstd, dweight=dweight, dbias=dbias, dx=dx)
+    codes, scales = _saved_rows(x, dy, cols) if saved else (None, None)
+    if not saved:
+        _need(x.shape == dy.shape and x.dtype == dy.dtype, "x: the shape and type of dy is needed")
+    _per_token(mean, dy, torch.float32, "mean")
+    _per_token(rstd, dy, torch.float32, "rstd")
+    ldw = _norm_weight(weight, dy, "weight")
+    ldg = _gradient_row(dweight, m, cols, weight, "dweight")
+    if dbias is not None:
+        ldb = _gradient_row(dbias, m, cols, weight, "dbias")
+        _need(dweight is None or ldb == ldg or m == 1, "dbias: the stride of dweight is needed")
+        ldg = ldb if dweight is None else ldg
+    if dx is None and want_dx:
+        dx = _empty(stream, dy.shape, dy.dtype, dy.device)
+    _need(dx is None or (dx.shape == dy.shape and dx.dtype == dy.dtype), "dx: the shape and type of dy is needed")
+    nbytes = lib.zeno_layer_norm_gradient_workspace(m, n, cols)
+    ws = _scratch(stream, nbytes, dy.device)
+    _done(lib.zeno_layer_norm_gradient(dy.device.index, _type(dy, "dy"), _type(weight, "weight"), _rows(dy, "dy"),
+                                       None if saved else _rows(x, "x"), codes, scales, m, n, cols, _ptr(weight), ldw, _ptr(mean),
+                                       _ptr(rstd), None if dx is None else _rows(dx, "dx"), _ptr(dweight), _ptr(dbias), ldg, _ptr(ws), nbytes,
+                                       _current(dy.device, stream)), "zeno_layer_norm_gradient")
+    return dx
+
+
+def pack_activations(x, stream=None) -> Saved:
+    """zeno_pack_activations: x in 8 bits, for layer_norm_gradient and dense_gradient."""
+    lib = load_library()
+    m, n, cols = _sizes(x)
+    _cuda(x.device)
+    codes = _empty(stream, tuple(x.shape[:-1]) + (-(-cols // 16) * 16,), torch.float8_e4m3fn, x.device)[..., :cols]
+    scales = _empty(stream, tuple(x.shape[:-1]) + (-(-cols // SAVED_BLOCK),), torch.float32, x.device)
+    _done(lib.zeno_pack_activations(x.device.index, _type(x, "x"), _rows(x, "x"), m, n, cols, _rows(codes, "codes"), _rows(scales, "scales"),
+                                    _current(x.device, stream)), "zeno_pack_activations")
+    return Saved(codes, scales)
+
+
+def dense_gradient(dy, saved: Saved, dweight, dbias=None, stream=None):
+    """zeno_dense_gradient: the weight gradient of a dense layer, dy^T x for every group, from x as pack_activations kept it.
+    dweight: [m, outputs, inputs] (or without m), contiguous per group, for instance
+    V[:, at:at + outputs * inputs].unflatten(1, (outputs, inputs)); dbias: [m, outputs]."""
+    lib = load_library()
+    m, n, outputs = _sizes(dy)
+    inputs = saved[0].shape[-1]
+    _cuda(dy.device, codes=saved[0], scales=saved[1], dweight=dweight, dbias=dbias)
+    codes, scales = _saved_rows(saved, dy, inputs)
+    _need(tuple(dweight.shape) in ((m, outputs, inputs),) + (((outputs, inputs),) if m == 1 else ()), f"dweight: [{m}, {outputs}, {inputs}] is needed")
+    _need((inputs <= 1 or dweight.stride(-1) == 1) and (outputs <= 1 or dweight.stride(-2) == inputs), "dweight: contiguous for every group is needed")
+    ldb = _gradient_row(dbias, m, outputs, dweight, "dbias")
+    nbytes = lib.zeno_dense_gradient_workspace(m, n, inputs, outputs)
+    ws = _scratch(stream, nbytes, dy.device)
+    _done(lib.zeno_dense_gradient(dy.device.index, _type(dy, "dy"), _type(dweight, "dweight"), _rows(dy, "dy"), codes, scales, m, n, inputs,
+                                  outputs, _ptr(dweight), dweight.stride(0) if dweight.dim() == 3 else inputs * outputs, _ptr(dbias), ldb,
+                                  _ptr(ws), nbytes, _current(dy.device, stream)), "zeno_dense_gradient")
+    return dweight
+
+
+def token_logprobs(logits, targets=None, top=0, stream=None) -> TokenLogprobs:
+    """zeno_token_logprobs: (logprobs or None without targets, entropy, lse, top_idx, top_logprobs (None if top is 0)) of logits [m, n, vocab] or
+    [n, vocab]; targets: int32, one outside the vocabulary means none."""
+    lib = load_library()
+    m, n, vocab = _sizes(logits)
+    dev, lead = logits.device, tuple(logits.shape[:-1])
+    _cuda(dev, targets=targets)
+    _per_token(targets, logits, torch.int32, "targets")
+    lp = _empty(stream, lead, torch.float32, dev) if targets is not None else None
+    entropy, lse = _empty(stream, lead, torch.float32, dev), _empty(stream, lead, torch.float32, dev)
+    idx = _empty(stream, lead + (top,), torch.int32, dev) if top > 0 else None
+    top_lp = _empty(stream, lead + (top,), torch.float32, dev) if top > 0 else None
+    _done(lib.zeno_token_logprobs(dev.index, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, _ptr(targets), top, _ptr(lp),
+                                  _ptr(entropy), _ptr(lse), _ptr(idx), _ptr(top_lp), _current(dev, stream)), "zeno_token_logprobs")
+    return TokenLogprobs(lp, entropy, lse, idx, top_lp)
+
+
+def token_gradient(logits, targets, lse, g_logprob, entropy=None, g_entropy=None, out=None, stream=None):
+    """zeno_token_gradient: the gradient at the logits from the gradients at token_logprobs's logprobs and (g_entropy) entropy.
+    out may be the logits."""
+    lib = load_library()
+    m, n, vocab = _sizes(logits)
+    _cuda(logits.device, targets=targets, lse=lse, g_logprob=g_logprob, entropy=entropy, g_entropy=g_entropy, out=out)
+    _need(g_entropy is None or entropy is not None, "entropy: needed with g_entropy")
+    _per_token(targets, logits, torch.int32, "targets")
+    for name, t in (("lse", lse), ("g_logprob", g_logprob), ("entropy", entropy), ("g_entropy", g_entropy)):
+        _per_token(t, logits, torch.float32, name)
+    grad = _empty(stream, logits.shape, logits.dtype, logits.device) if out is None else out
+    _need(grad.shape == logits.shape and grad.dtype == logits.dtype, "out: the shape and type of the logits is needed")
+    _done(lib.zeno_token_gradient(logits.device.index, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, _ptr(targets),
+                                  _ptr(lse), _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _rows(grad, "out"),
+                                  _current(logits.device, stream)), "zeno_token_gradient")
+    return grad
 
 
 def from_workload(w, m_max=None, n_r_max=None, device=0) -> "Zeno":
