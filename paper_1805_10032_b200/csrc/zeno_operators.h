@@ -19,6 +19,11 @@ struct Rows {
 #endif
 };
 
+// Whether every row starts at a multiple of `to` bytes.
+inline bool aligned_to(const Rows &v, int m, int64_t n, size_t elem, size_t to) {
+    return reinterpret_cast<uintptr_t>(v.data) % to == 0 && (n <= 1 || v.row * elem % to == 0) && (m <= 1 || v.group * elem % to == 0);
+}
+
 struct NormArgs {
     Rows x, y;
     int m;

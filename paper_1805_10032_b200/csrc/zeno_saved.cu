@@ -53,6 +53,78 @@ __global__ void __launch_bounds__(256) pack_any_kernel(PackArgs a, int64_t block
     }
 }
 
+// Rows of whole vectors: 16 lanes take a block, eight columns each; a half-warp takes kStrip blocks of a row one behind the
+// other, with all their loads ahead of the first maximum.
+constexpr int kStrip = 4;
+
+__device__ __forceinline__ void load_eight(const float *p, float (&f)[8]) {
+    const float4 u = reinterpret_cast<const float4 *>(p)[0], v = reinterpret_cast<const float4 *>(p)[1];
+    f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; f[4] = v.x; f[5] = v.y; f[6] = v.z; f[7] = v.w;
+}
+__device__ __forceinline__ void load_eight(const __nv_bfloat16 *p, float (&f)[8]) {
+    const uint4 u = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_per_row, int64_t strips) {
+    const int lane = threadIdx.x & 15;
+    const int64_t q = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const bool on = q < strips;                            // the warp's other half may still have work
+    const int64_t r = on ? q / strips_per_row : 0;
+    const int64_t blk = (on ? q - r * strips_per_row : 0) * kStrip, col = blk * kBlock + lane * 8;
+    const T *x = static_cast<const T *>(a.x.data) + a.x.at(r) + col;
+    uint8_t *codes = static_cast<uint8_t *>(a.codes.data) + a.codes.at(r) + col;
+    float *scales = static_cast<float *>(a.scales.data) + a.scales.at(r) + blk;
+    float f[kStrip][8];
+#pragma unroll
+    for (int i = 0; i < kStrip; ++i) {
+        if (on && col + i * kBlock < a.cols) load_eight(x + i * kBlock, f[i]);
+        else
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[i][k] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kStrip; ++i) {
+        uint32_t amax = 0;
+        float all = 0.f;                                   // NaN if one of the lane's entries is not finite
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            amax = max(amax, __float_as_uint(f[i][k]) & 0x7fffffffu);
+            all = fmaf(f[i][k], 0.f, all);
+        }
+        if (all != all) {
+            amax = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) amax = max(amax, finite_bits(f[i][k]));
+        }
+#pragma unroll
+        for (int s = 8; s >= 1; s >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, s));
+        const int k = amax ? scale_exponent(amax) : 0;
+        const float inv = __uint_as_float((uint32_t)(127 - k) << 23);
+        if (on && col + i * kBlock < a.cols) {
+            uint32_t w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float2 lo = make_float2(f[i][4 * h] * inv, f[i][4 * h + 1] * inv), hi = make_float2(f[i][4 * h + 2] * inv, f[i][4 * h + 3] * inv);
+                w[h] = __nv_cvt_float2_to_fp8x2(lo, __NV_SATFINITE, __NV_E4M3) | (uint32_t)__nv_cvt_float2_to_fp8x2(hi, __NV_SATFINITE, __NV_E4M3) << 16;
+            }
+            if (all != all) {                              // infinities saturate in the conversion; they are kept as NaN
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (!(fabsf(f[i][c]) < INFINITY)) w[c / 4] |= 0x7fu << (8 * (c % 4));
+            }
+            *reinterpret_cast<uint2 *>(codes + i * kBlock) = make_uint2(w[0], w[1]);
+            if (lane == 0) scales[i] = __uint_as_float((uint32_t)(127 + k) << 23);
+        }
+    }
+}
+
 // dW of a tile of 64 outputs by 64 inputs of one group in a block: 16 rows at a time through shared memory, 4 x 4 sums a thread.
 template <typename T, typename P>
 __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
@@ -124,9 +196,15 @@ cudaError_t dense_gradient(const DenseGradArgs &a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_pack(int type, const PackArgs &a, cudaStream_t s) {
-    const int64_t per_row = (a.cols + kBlock - 1) / kBlock, blocks = per_row * a.m * a.n;
-    const unsigned grid = (unsigned)min((blocks + 7) / 8, (int64_t)148 * 8);
-    return launch_chained(type == ZENO_BF16 ? pack_any_kernel<__nv_bfloat16> : pack_any_kernel<float>, dim3(grid), dim3(256), 0, s, false, a,
+    const int64_t per_row = (a.cols + kBlock - 1) / kBlock;
+    const bool aligned = a.cols % 8 == 0 && aligned_to(a.x, a.m, a.n, type == ZENO_BF16 ? 2 : 4, 16) && aligned_to(a.codes, a.m, a.n, 1, 8);
+    const int64_t strips_per_row = (per_row + kStrip - 1) / kStrip, strips = strips_per_row * a.m * a.n, grid = (strips + 15) / 16;
+    if (aligned && grid <= 0x7fffffff)
+        return launch_chained(type == ZENO_BF16 ? pack_kernel<__nv_bfloat16> : pack_kernel<float>, dim3((unsigned)grid), dim3(256), 0, s, false, a,
+                              (uint32_t)strips_per_row, strips);
+    const int64_t blocks = per_row * a.m * a.n;
+    const unsigned any_grid = (unsigned)min((blocks + 7) / 8, (int64_t)148 * 8);
+    return launch_chained(type == ZENO_BF16 ? pack_any_kernel<__nv_bfloat16> : pack_any_kernel<float>, dim3(any_grid), dim3(256), 0, s, false, a,
                           per_row, blocks);
 }
 

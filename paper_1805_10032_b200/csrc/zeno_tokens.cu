@@ -1,108 +1,475 @@
 // Log probabilities of given tokens with entropy and top alternatives, and their gradient at the logits.
+//
+// Both directions are bound by the logits' bytes.  Forward: one pass with a running reference instead of the maximum, in
+// powers of two: with t_j = z_j log2 e - M, S = sum 2^t_j and E = sum 2^t_j t_j for any M near the largest z log2 e,
+//   lse = (M + log2 S) ln 2,   log p_j = (t_j - log2 S) ln 2,   entropy = (log2 S - E / S) ln 2;
+// M moves by d: S' = 2^-d S, E' = 2^-d (E - d S).  No subtraction of nearly equal numbers besides those of the definition.
 #include "zeno_operators.h"
 
 namespace zeno {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // exp is zero in binary32 below this: a logarithm under it may be taken as it, so that zero times it is zero
 constexpr float kLogOfNothing = -200.f;
+// Logits between -kFar and kFar go by powers of two, whose products with log2 e stay finite; rows whose largest logit is
+// outside (masked by the type's lowest value throughout, or not finite) are summed by the definition.
+constexpr float kFar = 1e38f;
+constexpr float kUnset = -kFar * kLog2e;      // the reference of nothing
+constexpr float kSlack = 4.f;      // how far (in logits) the reference may fall behind the largest logit before it moves
+constexpr int kMaxTop = ZENO_MAX_TOP;
+constexpr unsigned kAll = 0xffffffffu;
 
-template <typename V, typename F>
-__device__ __forceinline__ V block_reduce(V v, V *scratch, F op) {
-#pragma unroll
-    for (int s = 16; s >= 1; s >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, s));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = scratch[0];
-#pragma unroll
-    for (int i = 1; i < kThreads / 32; ++i) v = op(v, scratch[i]);
-    return v;
+__device__ __forceinline__ float exp2_fast(float t) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    return r;
 }
 
-// What a row's statistics say of a logit: with the largest logit m and S = sum exp(z - m),
-// log p = (z - m) - log S.  A row of minus infinities has m = 0 here, S = 0.
-__device__ __forceinline__ float log_prob(float z, float m, float log_s) { return log_s == -INFINITY ? -INFINITY : (z - m) - log_s; }
+// 16 bytes of logits
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int N = 4;
+    static constexpr uint32_t kFill = 0xff800000u;      // minus infinity
+    // largest entry; a NaN counts only among nothing else
+    static __device__ __forceinline__ float most(uint4 v) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
+    // entries, at least -kFar each (a NaN stays)
+    static __device__ __forceinline__ void entries(uint4 v, float (&o)[N]) {
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %1, %2;" : "=f"(o[i]) : "f"(__uint_as_float(u[i])), "f"(-kFar));
+    }
+};
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int N = 8;
+    static constexpr uint32_t kFill = 0xff80ff80u;
+    static __device__ __forceinline__ __nv_bfloat162 pair(uint32_t u) { return *reinterpret_cast<__nv_bfloat162 *>(&u); }
+    static __device__ __forceinline__ float most(uint4 v) {
+        const __nv_bfloat162 m = __hmax2(__hmax2(pair(v.x), pair(v.y)), __hmax2(pair(v.z), pair(v.w)));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    static __device__ __forceinline__ void entries(uint4 v, float (&o)[N]) {
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+        const __nv_bfloat162 low = __float2bfloat162_rn(-kFar);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 m = __hmax2_nan(pair(u[i]), low);
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(&m);
+            o[2 * i] = __uint_as_float(w << 16);
+            o[2 * i + 1] = __uint_as_float(w & 0xffff0000u);
+        }
+    }
+};
 
-// A block takes a row: its maximum, then the sums, then one maximum after another in the order of their keys.
+// Entries before the first 16-byte boundary of a row (all of a short one)
 template <typename T>
-__global__ void __launch_bounds__(kThreads) logprobs_any_kernel(LogprobArgs a) {
-    __shared__ float scratch[kThreads / 32];
-    __shared__ unsigned long long keys[kThreads / 32];
-    const int64_t r = blockIdx.x;
-    const T *z = static_cast<const T *>(a.logits.data) + a.logits.at(r);
-    float m = -INFINITY;
-    for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads) m = fmaxf(m, value_of(z + j));
-    m = block_reduce(m, scratch, [](float p, float q) { return fmaxf(p, q); });
+__device__ __forceinline__ int64_t head_of(const T *p, int64_t count) {
+    const int64_t h = (int64_t)((16u - (unsigned)(reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / (int64_t)sizeof(T);
+    return h < count ? h : count;
+}
+
+struct Sums {
+    float M, s, e;
+    // to the reference `to`, not below M unless nothing has been added
+    __device__ __forceinline__ void move(float to) {
+        const float d = to - M, f = s == 0.f ? 0.f : exp2_fast(-d);
+        e = f == 0.f ? 0.f : f * (e - d * s);
+        s *= f;
+        M = to;
+    }
+    __device__ __forceinline__ void add(float z) {
+        const float t = fmaf(z, kLog2e, -M), p = exp2_fast(t);
+        s += p;
+        e = fmaf(p, t, e);
+    }
+};
+
+// The unsigned half of rank_key: the order of the values, NaN with minus infinity
+__device__ __forceinline__ uint32_t order_of(float z) { return (uint32_t)(rank_key(z, 0) >> 32); }
+__device__ __forceinline__ float value_of_order(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+
+// A warp's list of the largest keys, the k-th one in lane k - 1 (zero: none yet), and the value that a candidate has to reach.
+struct TopList {
+    unsigned long long mine = 0;
+    uint32_t need = 0;
+    // every candidate of the warp that is better than the last of `top`
+    __device__ __forceinline__ void offer(unsigned long long key, int top, int lane) {
+        unsigned todo = __ballot_sync(kAll, key > __shfl_sync(kAll, mine, top - 1));
+        while (todo) {
+            const int from = __ffs(todo) - 1;
+            todo &= todo - 1;
+            const unsigned long long k = __shfl_sync(kAll, key, from);
+            const unsigned long long before = __shfl_up_sync(kAll, mine, 1);
+            const bool later = k > mine;                              // this lane's entry moves back by one
+            const bool first = lane == 0 || !(k > before);            // the new one's place, if it is before this entry
+            if (later) mine = first ? k : before;
+        }
+        need = max(need, (uint32_t)(__shfl_sync(kAll, mine, top - 1) >> 32));
+    }
+};
+
+// the k-th largest of the lanes' values
+__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t v, int k, int lane) {
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+        for (int s = size >> 1; s >= 1; s >>= 1) {
+            const uint32_t w = __shfl_xor_sync(kAll, v, s);
+            const bool keep_max = ((lane & s) == 0) == ((lane & size) == 0);      // descending; the last merge has no set bit `size`
+            v = keep_max ? max(v, w) : min(v, w);
+        }
+    return __shfl_sync(kAll, v, k - 1);
+}
+
+// The row's sums by the definition, for a block: m (the largest entry, 0 for a row of minus infinities), sum exp(z - m) and the
+// sum of those times z - m.
+template <typename T, int THREADS>
+__device__ __noinline__ void sums_by_definition(const T *z, int64_t vocab, float *scratch, float &m, float &s, float &e) {
+    m = -INFINITY;
+    for (int64_t j = threadIdx.x; j < vocab; j += THREADS) m = fmaxf(m, value_of(z + j));
+#pragma unroll
+    for (int k = 16; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, k));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = m;
+    __syncthreads();
+    for (int k = 0; k < THREADS / 32; ++k) m = fmaxf(m, scratch[k]);
     if (m == -INFINITY) m = 0.f;
-    float s = 0.f, e = 0.f;
-    for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads) {
+    s = e = 0.f;
+    for (int64_t j = threadIdx.x; j < vocab; j += THREADS) {
         const float d = value_of(z + j) - m, p = exp2f(d * kLog2e);
         s += p;
         e = fmaf(p, fmaxf(d, kLogOfNothing), e);
     }
-    auto add = [](float p, float q) { return p + q; };
-    s = block_reduce(s, scratch, add);
-    e = block_reduce(e, scratch, add);
-    const float log_s = logf(s);
-    if (threadIdx.x == 0) {
-        if (a.lse) a.lse[r] = m + log_s;
-        if (a.entropy) a.entropy[r] = s == 0.f ? 0.f : log_s - e / s;
-        if (a.logprobs) {
-            const int t = a.targets[r];
-            a.logprobs[r] = t >= 0 && t < a.vocab ? log_prob(value_of(z + t), m, log_s) : 0.f;
+    __syncthreads();
+    s = block_sum<THREADS>(s, scratch);
+    __syncthreads();
+    e = block_sum<THREADS>(e, scratch);
+}
+
+// A row goes to a block, or (few rows) to a cluster of `parts` blocks that join through distributed shared memory.  A warp takes 32
+// x kBatch vectors at a time, all loads ahead of their use.  The best `top` are kept per warp: a batch whose largest entry does
+// not reach the k-th best that any warp of the block has (nearly all of them, in rows that are in no order) costs one comparison.
+template <typename T, int THREADS, bool TOP>
+__global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobArgs a, int parts) {
+    using V = Vec<T>;
+    constexpr int kWarps = THREADS / 32, kBatch = 32 / V::N, kMaxParts = 8;
+    __shared__ float scratch[kWarps];
+    __shared__ float warp_sums[kWarps][3];
+    __shared__ float part_sums[4];
+    __shared__ unsigned long long keys[TOP ? (kWarps > kMaxParts ? kWarps : kMaxParts) * kMaxTop : 1];
+    __shared__ unsigned long long best[TOP ? kMaxTop : 1];
+    __shared__ uint32_t block_need;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t r = (int)(blockIdx.x / (unsigned)parts);
+    const int part = (int)(blockIdx.x - (unsigned)r * (unsigned)parts);
+    const T *z = static_cast<const T *>(a.logits.data) + a.logits.at(r);
+    const int top = a.top;
+
+    float zt = 0.f;
+    bool given = false;
+    if (threadIdx.x == 0 && part == 0 && a.logprobs) {
+        const int t = a.targets[r];
+        given = t >= 0 && t < a.vocab;
+        if (given) zt = value_of(z + t);
+    }
+    if (TOP && THREADS > 32) {
+        if (threadIdx.x == 0) block_need = 0;
+        __syncthreads();
+    }
+    const int64_t head = head_of(z, a.vocab), vecs = (a.vocab - head) / V::N;
+    const int64_t v_end = vecs * (part + 1) / parts;
+    const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
+    // Until an entry is above -kFar the reference is 0, where all others (kept at least -kFar) add nothing.
+    Sums q = {0.f, 0.f, 0.f};
+    float limit = -kFar;                              // the reference moves for entries beyond this
+    TopList list;
+    bool fresh = true;
+
+    for (int64_t base = vecs * part / parts + warp * 32 * kBatch; base < v_end; base += THREADS * kBatch) {
+        uint4 raw[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int64_t v = base + i * 32 + lane;
+            raw[i] = v < v_end ? __ldcs(zv + v) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
+        }
+        float most = V::most(raw[0]);
+#pragma unroll
+        for (int i = 1; i < kBatch; ++i) most = fmaxf(most, V::most(raw[i]));
+        if (most > limit) {
+            q.move(most * kLog2e);
+            limit = most + kSlack;
+        }
+        // two chains of sums
+        Sums q1 = {q.M, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            float f[V::N];
+            V::entries(raw[i], f);
+#pragma unroll
+            for (int k = 0; k < V::N; k += 2) {
+                q.add(f[k]);
+                q1.add(f[k + 1]);
+            }
+        }
+        q.s += q1.s;
+        q.e += q1.e;
+        if (TOP) {
+            const uint32_t u = order_of(most);
+            if (THREADS > 32) list.need = max(list.need, *(volatile uint32_t *)&block_need);
+            if (fresh) list.need = max(list.need, kth_of_lanes(u, top, lane));    // as many lanes have an entry that is no less
+            fresh = false;
+            unsigned todo = __ballot_sync(kAll, u >= list.need);
+            if (todo) {
+                do {      // a lane's 32 entries (or as many as it has) in the warp's lanes
+                    const int from = __ffs(todo) - 1;
+                    todo &= todo - 1;
+                    const int64_t v = base + lane / V::N * 32 + from;
+                    const int64_t j = head + v * V::N + lane % V::N;
+                    unsigned long long key = 0;
+                    if (v < v_end) key = rank_key(value_of(z + j), (int)j);
+                    list.offer(key, top, lane);
+                } while (todo);
+                if (THREADS > 32 && lane == 0) atomicMax(&block_need, list.need);
+            }
         }
     }
-    unsigned long long below = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-        unsigned long long best = 0;
-        for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads) {
-            const unsigned long long key = rank_key(value_of(z + j), (int)j);
-            if (key < below && key > best) best = key;
+    // what lies before the first vector and behind the last: fewer than 2 N entries
+    const int64_t rest = a.vocab - vecs * V::N;
+    if (part == 0 && warp == 0) {
+        const bool valid = lane < rest;
+        const int64_t j = lane < head ? lane : vecs * V::N + lane;
+        const float v = valid ? value_of(z + j) : -INFINITY;
+        if (v > limit) {
+            q.move(v * kLog2e);
+            limit = v;
         }
-        below = block_reduce(best, keys, [](unsigned long long p, unsigned long long q) { return p > q ? p : q; });
+        if (valid) q.add(v < -kFar ? -kFar : v);
+        if (TOP) list.offer(valid ? rank_key(v, (int)j) : 0, top, lane);
+    }
+
+    // the warp's sums, the block's, the cluster's
+    if (limit == -kFar) q.M = kUnset;
+    float M = q.M;
+#pragma unroll
+    for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
+    q.move(M);
+    q.s = warp_sum(q.s);
+    q.e = warp_sum(q.e);
+    if (THREADS > 32) {
+        if (lane == 0) {
+            warp_sums[warp][0] = q.M;
+            warp_sums[warp][1] = q.s;
+            warp_sums[warp][2] = q.e;
+        }
+        if (TOP && lane < top) keys[warp * top + lane] = list.mine;
+        __syncthreads();
+        if (warp == 0) {
+            Sums w = {lane < kWarps ? warp_sums[lane][0] : kUnset, lane < kWarps ? warp_sums[lane][1] : 0.f,
+                      lane < kWarps ? warp_sums[lane][2] : 0.f};
+            M = w.M;
+#pragma unroll
+            for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
+            w.move(M);
+            q = {M, warp_sum(w.s), warp_sum(w.e)};
+        }
+        if (TOP) {      // an entry's place is the number of better ones; keys differ
+            for (int i = threadIdx.x; i < kWarps * top; i += THREADS) {
+                const unsigned long long k = keys[i];
+                int place = 0;
+                for (int c = 0; c < kWarps * top; ++c) place += keys[c] > k;
+                if (k && place < top) best[place] = k;
+            }
+            if (parts > 1 && threadIdx.x == 0) {          // a short part may have fewer
+                int have = 0;
+                for (int c = 0; c < kWarps * top; ++c) have += keys[c] != 0;
+                for (; have < top; ++have) best[have] = 0;
+            }
+            __syncthreads();
+        }
+    }
+    if (parts > 1) {
         if (threadIdx.x == 0) {
-            const int j = (int)(0xffffffffu - (uint32_t)below);
-            if (a.top_idx) a.top_idx[r * a.top + k] = j;
-            if (a.top_logprobs) a.top_logprobs[r * a.top + k] = log_prob(value_of(z + j), m, log_s);
+            part_sums[0] = q.M;
+            part_sums[1] = q.s;
+            part_sums[2] = q.e;
         }
+        cluster_barrier();
+        if (part == 0) {
+            if (warp == 0) {
+                Sums w = {kUnset, 0.f, 0.f};
+                if (lane < parts) {
+                    w.M = cluster_load(cluster_addr(&part_sums[0], lane));
+                    w.s = cluster_load(cluster_addr(&part_sums[1], lane));
+                    w.e = cluster_load(cluster_addr(&part_sums[2], lane));
+                }
+                M = w.M;
+#pragma unroll
+                for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
+                w.move(M);
+                q = {M, warp_sum(w.s), warp_sum(w.e)};
+            }
+            if (TOP) {
+                for (int i = threadIdx.x; i < parts * top; i += THREADS) keys[i] = cluster_load64(cluster_addr(&best[i % top], i / top));
+                __syncthreads();
+                for (int i = threadIdx.x; i < parts * top; i += THREADS) {
+                    const unsigned long long k = keys[i];
+                    int place = 0;
+                    for (int c = 0; c < parts * top; ++c) place += keys[c] > k;
+                    if (k && place < top) best[place] = k;
+                }
+            }
+        }
+        cluster_barrier();
+        if (part != 0) return;
+    }
+    if (THREADS > 32) {
+        if (threadIdx.x == 0) {
+            part_sums[0] = q.M;
+            part_sums[1] = q.s;
+            part_sums[2] = q.e;
+        }
+        __syncthreads();
+        q = {part_sums[0], part_sums[1], part_sums[2]};
+    }
+
+    const bool plain = !(fabsf(q.M) <= 0.99f * kFar * kLog2e);
+    float m, log_s, mean_t;
+    if (plain) {
+        float s, e;
+        sums_by_definition<T, THREADS>(z, a.vocab, scratch, m, s, e);
+        log_s = logf(s);
+        mean_t = s == 0.f ? log_s : e / s;                // a row of nothing: entropy 0
+    } else {
+        m = q.M;
+        log_s = log2f(q.s);
+        mean_t = q.e / q.s;
+    }
+    auto log_prob = [&](float v) {
+        if (plain) return log_s == -INFINITY ? -INFINITY : (v - m) - log_s;
+        if (v < -kFar) return v - (m + log_s) * kLn2;     // its product with log2 e may be beyond binary32
+        const float lp = (fmaf(v, kLog2e, -m) - log_s) * kLn2;
+        return lp > 0.f ? 0.f : lp;                       // a rounding above the definition's bound
+    };
+    if (threadIdx.x == 0) {
+        if (a.lse) a.lse[r] = plain ? m + log_s : (m + log_s) * kLn2;
+        if (a.entropy) a.entropy[r] = log_s == -INFINITY ? 0.f : (log_s - mean_t) * (plain ? 1.f : kLn2);
+        if (a.logprobs) a.logprobs[r] = given ? log_prob(zt) : 0.f;
+    }
+    if (TOP && (int)threadIdx.x < top) {
+        const unsigned long long key = THREADS > 32 ? best[threadIdx.x] : list.mine;
+        if (a.top_idx) a.top_idx[r * top + threadIdx.x] = (int)(0xffffffffu - (uint32_t)key);
+        if (a.top_logprobs) a.top_logprobs[r * top + threadIdx.x] = log_prob(value_of_order((uint32_t)(key >> 32)));
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) token_gradient_any_kernel(TokenGradArgs a) {
-    const int64_t r = blockIdx.x;
+// Elements in a block of the gradient's kernel: two rounds of four vectors a thread, so that a block has 64 KB in flight.
+constexpr int kGradThreads = 256, kGradBatch = 4;
+
+// One element: what the row's sums say and the upstream gradients ask for; the target's own term is added apart.
+template <bool ENTROPY>
+__device__ __forceinline__ float token_slope(float z, float lse, float g, float h, float entropy) {
+    const float lp = z - lse, p = exp2_fast(lp * kLog2e);
+    return -p * (ENTROPY ? fmaf(h, fmaxf(lp, kLogOfNothing) + entropy, g) : g);
+}
+
+// A block takes `chunk` entries of a row.  VECTORS: logits and gradient start at the same offset from a 16-byte boundary.
+template <typename T, bool ENTROPY, bool VECTORS>
+__global__ void __launch_bounds__(kGradThreads) token_gradient_kernel(TokenGradArgs a, unsigned chunks, int64_t chunk) {
+    using V = Vec<T>;
+    const int64_t r = (int)(blockIdx.x / chunks);
+    const int64_t first = (int64_t)(blockIdx.x - (unsigned)r * chunks) * chunk;
     const T *z = static_cast<const T *>(a.logits.data) + a.logits.at(r);
     T *out = static_cast<T *>(a.grad.data) + a.grad.at(r);
     const int t = a.targets[r];
     const bool given = t >= 0 && t < a.vocab;
-    const float lse = a.lse[r], g = given ? a.g_logprob[r] : 0.f, h = a.g_entropy ? a.g_entropy[r] : 0.f;
-    const float entropy = a.g_entropy ? a.entropy[r] : 0.f;
-    if ((!given && !a.g_entropy) || lse == -INFINITY) {
-        for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads) put(out + j, 0.f);
+    const float lse = a.lse[r], g = given ? a.g_logprob[r] : 0.f, h = ENTROPY ? a.g_entropy[r] : 0.f, entropy = ENTROPY ? a.entropy[r] : 0.f;
+    const bool zero = (!given && !ENTROPY) || lse == -INFINITY;
+    auto one = [&](int64_t j) {
+        float v = 0.f;
+        if (!zero) v = token_slope<ENTROPY>(value_of(z + j), lse, g, h, entropy) + (j == t && given ? g : 0.f);
+        put(out + j, v);
+    };
+    if (!VECTORS) {
+        const int64_t end = min(first + chunk, a.vocab);
+        for (int64_t j = first + threadIdx.x; j < end; j += kGradThreads) one(j);
         return;
     }
-    for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads) {
-        const float lp = value_of(z + j) - lse, p = exp2f(lp * kLog2e);
-        // p (g + h (log p + H)), whose second factor stays finite where p is zero
-        const float v = (j == t && given ? g : 0.f) - p * fmaf(h, fmaxf(lp, kLogOfNothing) + entropy, g);
-        put(out + j, v);
+    const int64_t head = head_of(z, a.vocab), vecs = (a.vocab - head) / V::N;
+    if (first == 0 && threadIdx.x < a.vocab - vecs * V::N) one(threadIdx.x < head ? threadIdx.x : vecs * V::N + threadIdx.x);
+    const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
+    uint4 *ov = reinterpret_cast<uint4 *>(out + head);
+    const int64_t end = min((first + chunk) / V::N, vecs);
+    for (int64_t base = first / V::N + threadIdx.x; base < end; base += kGradThreads * kGradBatch) {
+        uint4 raw[kGradBatch];
+        if (!zero)
+#pragma unroll
+            for (int i = 0; i < kGradBatch; ++i)
+                if (base + i * kGradThreads < end) raw[i] = zv[base + i * kGradThreads];
+#pragma unroll
+        for (int i = 0; i < kGradBatch; ++i) {
+            const int64_t v = base + i * kGradThreads;
+            if (v >= end) break;
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            if (!zero) {
+                T e[V::N], o[V::N];
+                *reinterpret_cast<uint4 *>(e) = raw[i];
+                const int64_t at = (int64_t)t - (head + v * V::N);
+#pragma unroll
+                for (int k = 0; k < V::N; ++k) {
+                    float s = token_slope<ENTROPY>(value_of(e + k), lse, g, h, entropy);
+                    if (at == k) s += g;                       // g is 0 without a target
+                    put(o + k, s);
+                }
+                w = *reinterpret_cast<uint4 *>(o);
+            }
+            ov[v] = w;
+        }
     }
+}
+
+template <typename T, int THREADS>
+cudaError_t launch_logprobs(const LogprobArgs &a, int parts, cudaStream_t s) {
+    auto *kernel = a.top ? logprobs_kernel<T, THREADS, true> : logprobs_kernel<T, THREADS, false>;
+    const dim3 grid((unsigned)(a.m * a.n * parts));
+    return parts > 1 ? launch_clustered(kernel, parts, grid, dim3(THREADS), 0, s, false, a, parts) : launch_chained(kernel, grid, dim3(THREADS), 0, s, false, a, parts);
+}
+
+template <typename T>
+cudaError_t token_logprobs(const LogprobArgs &a, cudaStream_t s) {
+    const int64_t rows = a.m * a.n;
+    if (a.vocab <= 2048) return launch_logprobs<T, 32>(a, 1, s);
+    if (a.vocab <= 16384 && rows >= 148) return launch_logprobs<T, 128>(a, 1, s);
+    int parts = 8;
+    while (parts > 1 && (rows * parts > 296 || a.vocab < parts * 2048)) parts /= 2;
+    return launch_logprobs<T, 512>(a, parts, s);
+}
+
+template <typename T>
+cudaError_t token_gradient(const TokenGradArgs &a, cudaStream_t s) {
+    const int64_t rows = a.m * a.n;
+    int64_t chunk = 2 * kGradBatch * kGradThreads * Vec<T>::N;
+    while (rows * ((a.vocab + chunk - 1) / chunk) > 0x7fffffff) chunk *= 2;
+    const unsigned chunks = (unsigned)((a.vocab + chunk - 1) / chunk);
+    // every row of both at the same offset from a 16-byte boundary
+    const bool vectors = ((reinterpret_cast<uintptr_t>(a.logits.data) - reinterpret_cast<uintptr_t>(a.grad.data)) & 15) == 0 &&
+                         (a.n <= 1 || (a.logits.row - a.grad.row) * (int64_t)sizeof(T) % 16 == 0) &&
+                         (a.m <= 1 || (a.logits.group - a.grad.group) * (int64_t)sizeof(T) % 16 == 0);
+    auto *kernel = a.g_entropy ? (vectors ? token_gradient_kernel<T, true, true> : token_gradient_kernel<T, true, false>)
+                               : (vectors ? token_gradient_kernel<T, false, true> : token_gradient_kernel<T, false, false>);
+    return launch_chained(kernel, dim3((unsigned)(rows * chunks)), dim3(kGradThreads), 0, s, false, a, chunks, chunk);
 }
 
 }  // namespace
 
 cudaError_t launch_token_logprobs(int type, const LogprobArgs &a, cudaStream_t s) {
-    return launch_chained(type == ZENO_BF16 ? logprobs_any_kernel<__nv_bfloat16> : logprobs_any_kernel<float>, dim3((unsigned)(a.m * a.n)),
-                          dim3(kThreads), 0, s, false, a);
+    return type == ZENO_BF16 ? token_logprobs<__nv_bfloat16>(a, s) : token_logprobs<float>(a, s);
 }
 
 cudaError_t launch_token_gradient(int type, const TokenGradArgs &a, cudaStream_t s) {
-    return launch_chained(type == ZENO_BF16 ? token_gradient_any_kernel<__nv_bfloat16> : token_gradient_any_kernel<float>, dim3((unsigned)(a.m * a.n)),
-                          dim3(kThreads), 0, s, false, a);
+    return type == ZENO_BF16 ? token_gradient<__nv_bfloat16>(a, s) : token_gradient<float>(a, s);
 }
 
 }  // namespace zeno
