@@ -3,7 +3,7 @@
 // Bound by the activations' bytes: forward x in, y out; backward dy and x in, dx out, each once.  Forward: a row's entries stay in
 // the registers of the 32 to 1024 threads that share it, between the sum, the centred squares and the result.  Backward: a
 // thread owns columns, not rows: it goes down a stretch of a group's rows with the sums of its columns' weight gradients in
-// registers, and the loads of the rows ahead are in flight while a row's two averages are formed across the block.
+// registers, and copies of the rows ahead are in flight while a row's two averages are formed across the block.
 #include "zeno_operators.h"
 #include "zeno_saved.cuh"
 
@@ -74,34 +74,6 @@ __global__ void __launch_bounds__(kThreads) norm_dx_any_kernel(NormGradArgs a) {
     for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
         const float g = value_of(dy + j) * value_of(w + j), h = (x(j) - mean) * rstd;
         put(dx + j, rstd * (g - c1 - h * c2));
-    }
-}
-
-// Weight gradients: a block takes 32 columns of a group, its warps the group's rows in turn.
-template <typename T, typename P>
-__global__ void __launch_bounds__(kThreads) norm_weights_any_kernel(NormGradArgs a) {
-    constexpr int kWarps = kThreads / 32;
-    __shared__ float sums[2][kWarps][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t j = (int64_t)blockIdx.x * 32 + lane;
-    const int i = blockIdx.y;
-    float sw = 0.f, sb = 0.f;
-    if (j < a.cols)
-        for (int64_t t = warp; t < a.n; t += kWarps) {
-            const int64_t r = i * a.n + t;
-            const float d = value_of(static_cast<const T *>(a.dy.data) + a.dy.at(r) + j);
-            sw = fmaf(d, (InputRow<T>(a, r)(j) - a.mean[r]) * a.rstd[r], sw);
-            sb += d;
-        }
-    sums[0][warp][lane] = sw;
-    sums[1][warp][lane] = sb;
-    __syncthreads();
-    if (warp < 2 && j < a.cols) {
-        float s = 0.f;
-#pragma unroll
-        for (int q = 0; q < kWarps; ++q) s += sums[warp][q][lane];
-        void *out = warp == 0 ? a.dw : a.db;
-        if (out) put(static_cast<P *>(out) + i * a.ldg + j, s);
     }
 }
 
@@ -221,137 +193,312 @@ __global__ void __launch_bounds__(TPR == 32 ? kRowBlock : TPR) norm_row_kernel(N
 
 // ---- backward, by columns
 
-// The layer's input, N entries at a time: as it was, or codes and their block's scale
-template <typename T, int N, bool SAVED> struct InputPack;
-template <typename T, int N> struct InputPack<T, N, false> {
-    Pack<T, N> x;
-    __device__ __forceinline__ void load(const NormGradArgs &a, int64_t r, int j) { x = load_pack<T, N>(static_cast<const T *>(a.x.data) + a.x.at(r) + j); }
-    __device__ __forceinline__ void get(float (&f)[N]) const { values(x, f); }
-};
-template <typename T, int N> struct InputPack<T, N, true> {
-    Pack<uint8_t, N> codes;
-    float scale;
-    __device__ __forceinline__ void load(const NormGradArgs &a, int64_t r, int j) {
-        codes = load_pack<uint8_t, N>(static_cast<const uint8_t *>(a.codes.data) + a.codes.at(r) + j);
-        scale = (static_cast<const float *>(a.scales.data) + a.scales.at(r))[j / ZENO_SAVED_BLOCK];
-    }
-    __device__ __forceinline__ void get(float (&f)[N]) const {
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = saved_value(codes.v[i], scale);
-    }
-};
+// Two binary32 numbers that one instruction takes
+struct Two { float x, y; };
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two d;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ Two both(float v) { return Two{v, v}; }
 
-// A block: ROWS rows side by side, TPR threads each, N columns a thread, down the rows [first, last) of group blockIdx.y.  Then
-// the sums of the ROWS rows' threads are joined, and go to the group's gradients, or (several blocks to a group) to `part`
-// [group][block][dw, db][cols].
-template <typename T, typename P, int N, int TPR, int ROWS, bool SAVED, bool DX>
-__global__ void __launch_bounds__(TPR *ROWS) norm_columns_kernel(NormGradArgs a, float *part) {
-    constexpr int kWarps = TPR / 32;
-    constexpr int kAhead = TPR * N >= 8192 ? 1 : 2;      // rows whose loads are in flight ahead of the one at work: 64 registers a thread
-    __shared__ float2 scratch[2][kWarps];
-    __shared__ float joined[ROWS > 1 ? 2 : 1][ROWS > 1 ? (ROWS - 1) * TPR * N : 1];
-    const int sub = ROWS > 1 ? threadIdx.x / TPR : 0, t = ROWS > 1 ? threadIdx.x % TPR : threadIdx.x;
-    const int cols = (int)a.cols, j = t * N, chunks = gridDim.x, i = blockIdx.y;
-    const bool mine = j < cols;
-    const int64_t first = a.n * blockIdx.x / chunks, last = a.n * (blockIdx.x + 1) / chunks;
-    const float inv = 1.f / (float)cols;
-    float w[N], sw[N], sb[N];
+// 16 bytes of activations as pairs
+__device__ __forceinline__ void pairs(uint4 u, Two (&f)[2], float) {
+    f[0] = Two{__uint_as_float(u.x), __uint_as_float(u.y)};
+    f[1] = Two{__uint_as_float(u.z), __uint_as_float(u.w)};
+}
+__device__ __forceinline__ void pairs(uint4 u, Two (&f)[4], __nv_bfloat16) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        w[k] = DX && mine ? value_of(static_cast<const P *>(a.w) + i * a.ldw + j + k) : 0.f;
-        sw[k] = sb[k] = 0.f;
+    for (int i = 0; i < 4; ++i) f[i] = Two{__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)};
+}
+__device__ __forceinline__ uint4 from_pairs(const Two (&f)[2], float) {
+    return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+}
+__device__ __forceinline__ uint32_t bf16_pair(Two f) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint4 from_pairs(const Two (&f)[4], __nv_bfloat16) { return make_uint4(bf16_pair(f[0]), bf16_pair(f[1]), bf16_pair(f[2]), bf16_pair(f[3])); }
+
+// Rows of whole vectors.  A block: ROWS rows side by side, TPR threads each with NV = 2 vectors of columns, down the rows [first, last) of
+// group blockIdx.y.  A thread stages its own columns of the rows ahead in shared memory by asynchronous copies that nobody
+// else reads, so they need no registers and no barrier; the one barrier a row is that of its two averages.  Then the sums of the
+// ROWS rows' threads are joined, and go to the group's gradients, or (several blocks to a group) to `part` [group][block][dw, db][cols].
+constexpr int kNV = 2;
+template <typename T, bool SAVED> constexpr int kSlotBytes = 16 + (SAVED ? 16 / (int)sizeof(T) : 16);     // a vector of dy, and of x or its codes
+
+template <typename T, typename P, int TPR, int ROWS, int STAGES, bool SAVED, bool DX>
+__global__ void __launch_bounds__(TPR *ROWS, TPR *ROWS <= 256 ? 2 : 1) norm_columns_kernel(NormGradArgs a, float *part) {
+    constexpr int N = 16 / sizeof(T), H = N / 2, kWarps = TPR / 32, kThreadsHere = TPR * ROWS;
+    constexpr int kXBytes = SAVED ? N : 16;
+    extern __shared__ __align__(16) uint8_t ring[];            // [STAGES][NV][threads] vectors of dy, then the same of x, then (SAVED) of scales
+    __shared__ __align__(16) float2 scratch[2][ROWS][kWarps];
+    uint8_t *ring_x = ring + STAGES * kNV * kThreadsHere * 16;
+    float *ring_s = reinterpret_cast<float *>(ring_x + STAGES * kNV * kThreadsHere * kXBytes);
+    const int tid = threadIdx.x, sub = tid / TPR, t = tid % TPR;
+    const int cols = (int)a.cols, chunks = gridDim.x, i = blockIdx.y;
+    const int64_t first = a.n * blockIdx.x / chunks + sub, last = a.n * (blockIdx.x + 1) / chunks;
+    const float inv = 1.f / (float)cols;
+    const T *dy = static_cast<const T *>(a.dy.data) + i * a.dy.group;
+    const T *x = SAVED ? nullptr : static_cast<const T *>(a.x.data) + i * a.x.group;
+    const uint8_t *codes = SAVED ? static_cast<const uint8_t *>(a.codes.data) + i * a.codes.group : nullptr;
+    const float *scales = SAVED ? static_cast<const float *>(a.scales.data) + i * a.scales.group : nullptr;
+    T *dx = DX ? static_cast<T *>(a.dx.data) + i * a.dx.group : nullptr;
+    int at[kNV];
+    bool mine[kNV];
+    Two w[kNV][H], sw[kNV][H], sb[kNV][H];
+#pragma unroll
+    for (int v = 0; v < kNV; ++v) {
+        at[v] = (v * TPR + t) * N;
+        mine[v] = at[v] < cols;
+#pragma unroll
+        for (int k = 0; k < H; ++k) {
+            const P *from = static_cast<const P *>(a.w) + i * a.ldw + at[v] + 2 * k;
+            w[v][k] = DX && mine[v] ? Two{value_of(from), value_of(from + 1)} : both(0.f);
+            sw[v][k] = sb[v][k] = both(0.f);
+        }
     }
-    Pack<T, N> dy[kAhead];
-    InputPack<T, N, SAVED> x[kAhead];
-    float mean[kAhead], rstd[kAhead];
-    auto fetch = [&](int slot, int64_t row) {
-        if (row >= last) return;
-        const int64_t r = i * a.n + row;
-        mean[slot] = a.mean[r];
-        rstd[slot] = a.rstd[r];
-        if (!mine) return;
-        dy[slot] = load_pack<T, N>(static_cast<const T *>(a.dy.data) + a.dy.at(r) + j);
-        x[slot].load(a, r, j);
+    auto slot = [&](int stage, int v) { return (stage * kNV + v) * kThreadsHere + tid; };
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring), ring_x_at = (uint32_t)__cvta_generic_to_shared(ring_x),
+                   ring_s_at = (uint32_t)__cvta_generic_to_shared(ring_s);
+    auto fetch = [&](int stage, int64_t row) {
+        if (row < last)
+#pragma unroll
+            for (int v = 0; v < kNV; ++v)
+                if (mine[v]) {
+                    cp_async<16>(ring_at + slot(stage, v) * 16, dy + row * a.dy.row + at[v]);
+                    if (SAVED) {
+                        cp_async<kXBytes>(ring_x_at + slot(stage, v) * kXBytes, codes + row * a.codes.row + at[v]);
+                        cp_async<4>(ring_s_at + slot(stage, v) * 4, scales + row * a.scales.row + at[v] / ZENO_SAVED_BLOCK);
+                    } else {
+                        cp_async<16>(ring_x_at + slot(stage, v) * 16, x + row * a.x.row + at[v]);
+                    }
+                }
+        cp_async_commit();
     };
 #pragma unroll
-    for (int q = 0; q < kAhead; ++q) fetch(q, first + sub + q * ROWS);
-    int turn = 0;
-    for (int64_t row0 = first; row0 < last; row0 += kAhead * ROWS)
+    for (int q = 0; q < STAGES - 1; ++q) fetch(q, first + q * ROWS);
+    int stage = 0, turn = 0;
+    float mean = 0.f, rstd = 0.f;
+    if (first < last) {
+        mean = a.mean[i * a.n + first];
+        rstd = a.rstd[i * a.n + first];
+    }
+    for (int64_t row = first; row - sub < last; row += ROWS) {
+        float next_mean = 0.f, next_rstd = 0.f;
+        if (row + ROWS < last) {
+            next_mean = a.mean[i * a.n + row + ROWS];
+            next_rstd = a.rstd[i * a.n + row + ROWS];
+        }
+        fetch(stage == 0 ? STAGES - 1 : stage - 1, row + (STAGES - 1) * ROWS);
+        cp_async_wait<STAGES - 1>();
+        const bool on = row < last;
+        Two h[kNV][H], g[kNV][H], c1 = both(0.f), c2 = both(0.f);
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            const int64_t row = row0 + q * ROWS + sub;
-            if (row0 + q * ROWS >= last) break;           // the whole block's
-            const bool on = row < last && mine;
-            float g[N], h[N], d[N], c1 = 0.f, c2 = 0.f;
-            const float rs = row < last ? rstd[q] : 0.f, mu = row < last ? mean[q] : 0.f;
-            if (on) {
-                values(dy[q], d);
-                x[q].get(h);
+        for (int v = 0; v < kNV; ++v) {
+            Two d[H];
+            pairs(reinterpret_cast<const uint4 *>(ring)[slot(stage, v)], d, T());
+            if constexpr (SAVED) {
+                const float scale = ring_s[slot(stage, v)];
+                const uint32_t *c = reinterpret_cast<const uint32_t *>(ring_x + slot(stage, v) * kXBytes);
 #pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    h[k] = (h[k] - mu) * rs;
-                    sw[k] = fmaf(d[k], h[k], sw[k]);
-                    sb[k] += d[k];
-                    g[k] = d[k] * w[k];
-                    c1 += g[k];
-                    c2 = fmaf(g[k], h[k], c2);
+                for (int k = 0; k < H; ++k) {
+                    const __half2_raw e = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c[k / 2] >> (16 * (k & 1))), __NV_E4M3);
+                    const float2 f = __half22float2(__half2(e));
+                    h[v][k] = mul2(Two{f.x, f.y}, both(scale));
                 }
+            } else {
+                pairs(reinterpret_cast<const uint4 *>(ring_x)[slot(stage, v)], h[v], T());
             }
-            fetch(q, row + kAhead * ROWS);
-            if (!DX) continue;
-            c1 = warp_sum(c1);
-            c2 = warp_sum(c2);
-            if constexpr (kWarps > 1) {                   // ROWS is 1 then
-                if ((t & 31) == 0) scratch[turn][t >> 5] = make_float2(c1, c2);
-                __syncthreads();
-                c1 = c2 = 0.f;
+            if (!on || !mine[v])
 #pragma unroll
-                for (int k = 0; k < kWarps; ++k) {
-                    const float2 v = scratch[turn][k];
-                    c1 += v.x;
-                    c2 += v.y;
+                for (int k = 0; k < H; ++k) d[k] = h[v][k] = both(0.f);         // nothing was copied for this row
+#pragma unroll
+            for (int k = 0; k < H; ++k) {
+                h[v][k] = mul2(add2(h[v][k], both(-mean)), both(rstd));
+                sw[v][k] = fma2(d[k], h[v][k], sw[v][k]);
+                sb[v][k] = add2(sb[v][k], d[k]);
+                g[v][k] = mul2(d[k], w[v][k]);
+                c1 = add2(c1, g[v][k]);
+                c2 = fma2(g[v][k], h[v][k], c2);
+            }
+        }
+        if (DX) {
+            Two c = {warp_sum(c1.x + c1.y), warp_sum(c2.x + c2.y)};
+            if constexpr (kWarps > 1) {
+                if ((t & 31) == 0) scratch[turn][sub][t >> 5] = make_float2(c.x, c.y);
+                __syncthreads();
+                const float4 *s = reinterpret_cast<const float4 *>(scratch[turn][sub]);
+                c = both(0.f);
+#pragma unroll
+                for (int k = 0; k < kWarps / 2; ++k) {
+                    const float4 v = s[k];
+                    c = add2(c, add2(Two{v.x, v.y}, Two{v.z, v.w}));
                 }
                 turn ^= 1;
             }
-            if (on) {
-                c1 *= inv;
-                c2 *= inv;
+            // rstd (g - c1 - h c2)
+            const Two m1 = both(-rstd * c.x * inv), m2 = both(-rstd * c.y * inv), rs = both(rstd);
 #pragma unroll
-                for (int k = 0; k < N; ++k) g[k] = rs * (g[k] - c1 - h[k] * c2);
-                store_pack<T, N>(static_cast<T *>(a.dx.data) + a.dx.at(i * a.n + row) + j, g);
-            }
+            for (int v = 0; v < kNV; ++v)
+                if (on && mine[v]) {
+                    Two o[H];
+#pragma unroll
+                    for (int k = 0; k < H; ++k) o[k] = fma2(h[v][k], m2, fma2(g[v][k], rs, m1));
+                    *reinterpret_cast<uint4 *>(dx + row * a.dx.row + at[v]) = from_pairs(o, T());
+                }
         }
+        mean = next_mean;
+        rstd = next_rstd;
+        if (++stage == STAGES) stage = 0;
+    }
     if (!a.dw && !a.db) return;
+    cp_async_wait<0>();
     if constexpr (ROWS > 1) {
+        float *joined = reinterpret_cast<float *>(ring);          // [ROWS - 1][2][NV][N][TPR]
+        auto place = [&](int q, int which, int v, int k) { return joined + ((((q * 2 + which) * kNV + v) * N + k) * TPR) + t; };
+        __syncthreads();
         if (sub > 0)
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                joined[0][((sub - 1) * TPR + t) * N + k] = sw[k];
-                joined[1][((sub - 1) * TPR + t) * N + k] = sb[k];
-            }
+            for (int v = 0; v < kNV; ++v)
+#pragma unroll
+                for (int k = 0; k < H; ++k) {
+                    *place(sub - 1, 0, v, 2 * k) = sw[v][k].x;
+                    *place(sub - 1, 0, v, 2 * k + 1) = sw[v][k].y;
+                    *place(sub - 1, 1, v, 2 * k) = sb[v][k].x;
+                    *place(sub - 1, 1, v, 2 * k + 1) = sb[v][k].y;
+                }
         __syncthreads();
         if (sub > 0) return;
         for (int q = 0; q < ROWS - 1; ++q)
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                sw[k] += joined[0][(q * TPR + t) * N + k];
-                sb[k] += joined[1][(q * TPR + t) * N + k];
+            for (int v = 0; v < kNV; ++v)
+#pragma unroll
+                for (int k = 0; k < H; ++k) {
+                    sw[v][k].x += *place(q, 0, v, 2 * k);
+                    sw[v][k].y += *place(q, 0, v, 2 * k + 1);
+                    sb[v][k].x += *place(q, 1, v, 2 * k);
+                    sb[v][k].y += *place(q, 1, v, 2 * k + 1);
+                }
+    }
+#pragma unroll
+    for (int v = 0; v < kNV; ++v) {
+        if (!mine[v]) continue;
+        if (part) {
+            float *to = part + ((int64_t)i * chunks + blockIdx.x) * 2 * cols + at[v];       // cols is a multiple of N
+#pragma unroll
+            for (int k = 0; k < H; k += 2) {
+                *reinterpret_cast<float4 *>(to + 2 * k) = make_float4(sw[v][k].x, sw[v][k].y, sw[v][k + 1].x, sw[v][k + 1].y);
+                *reinterpret_cast<float4 *>(to + cols + 2 * k) = make_float4(sb[v][k].x, sb[v][k].y, sb[v][k + 1].x, sb[v][k + 1].y);
             }
-    }
-    if (!mine) return;
-    if (part) {
-        float *to = part + ((int64_t)i * chunks + blockIdx.x) * 2 * cols + j;
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            to[k] = sw[k];
-            to[cols + k] = sb[k];
+            continue;
         }
-        return;
-    }
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        if (a.dw) put(static_cast<P *>(a.dw) + i * a.ldg + j + k, sw[k]);
-        if (a.db) put(static_cast<P *>(a.db) + i * a.ldg + j + k, sb[k]);
+        for (int k = 0; k < H; ++k) {
+            const int64_t to = i * a.ldg + at[v] + 2 * k;
+            if (a.dw) {
+                put(static_cast<P *>(a.dw) + to, sw[v][k].x);
+                put(static_cast<P *>(a.dw) + to + 1, sw[v][k].y);
+            }
+            if (a.db) {
+                put(static_cast<P *>(a.db) + to, sb[v][k].x);
+                put(static_cast<P *>(a.db) + to + 1, sb[v][k].y);
+            }
+        }
+    }
+}
+
+// Rows of any alignment, and what is too long for the above: the columns blockIdx.x * TPR .. of chunk blockIdx.z of a group's rows.  With DX
+// the block has the whole row (gridDim.x is 1).
+template <typename T, typename P, int TPR, int NV, bool DX>
+__global__ void __launch_bounds__(TPR) norm_entries_kernel(NormGradArgs a, float *part) {
+    constexpr int kWarps = TPR / 32;
+    __shared__ __align__(16) float2 scratch[2][kWarps];
+    const int t = threadIdx.x, cols = (int)a.cols, chunks = gridDim.z, i = blockIdx.y;
+    const int j0 = blockIdx.x * TPR * NV + t;
+    const int64_t first = a.n * blockIdx.z / chunks, last = a.n * (blockIdx.z + 1) / chunks;
+    const float inv = 1.f / (float)cols;
+    float w[NV], sw[NV], sb[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        w[v] = DX && j0 + v * TPR < cols ? value_of(static_cast<const P *>(a.w) + i * a.ldw + j0 + v * TPR) : 0.f;
+        sw[v] = sb[v] = 0.f;
+    }
+    float d[NV], h[NV], mean = 0.f, rstd = 0.f;
+    auto fetch = [&](int64_t row) {
+        if (row >= last) return;
+        const int64_t r = i * a.n + row;
+        const T *dy = static_cast<const T *>(a.dy.data) + a.dy.at(r);
+        const InputRow<T> x(a, r);
+        mean = a.mean[r];
+        rstd = a.rstd[r];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int j = j0 + v * TPR;
+            d[v] = j < cols ? value_of(dy + j) : 0.f;
+            h[v] = j < cols ? x(j) : 0.f;
+        }
+    };
+    fetch(first);
+    int turn = 0;
+    for (int64_t row = first; row < last; ++row) {
+        float g[NV], hh[NV], c1 = 0.f, c2 = 0.f;
+        const float rs = rstd;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            hh[v] = j0 + v * TPR < cols ? (h[v] - mean) * rs : 0.f;
+            sw[v] = fmaf(d[v], hh[v], sw[v]);
+            sb[v] += d[v];
+            g[v] = d[v] * w[v];
+            c1 += g[v];
+            c2 = fmaf(g[v], hh[v], c2);
+        }
+        fetch(row + 1);
+        if (!DX) continue;
+        c1 = warp_sum(c1);
+        c2 = warp_sum(c2);
+        if ((t & 31) == 0) scratch[turn][t >> 5] = make_float2(c1, c2);
+        __syncthreads();
+        c1 = c2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) {
+            const float2 v = scratch[turn][k];
+            c1 += v.x;
+            c2 += v.y;
+        }
+        turn ^= 1;
+        T *dx = static_cast<T *>(a.dx.data) + a.dx.at(i * a.n + row);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (j0 + v * TPR < cols) put(dx + j0 + v * TPR, rs * (g[v] - c1 * inv - hh[v] * (c2 * inv)));
+    }
+    if (!a.dw && !a.db) return;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int j = j0 + v * TPR;
+        if (j >= cols) continue;
+        if (part) {
+            float *to = part + ((int64_t)i * chunks + blockIdx.z) * 2 * cols + j;
+            to[0] = sw[v];
+            to[cols] = sb[v];
+        } else {
+            if (a.dw) put(static_cast<P *>(a.dw) + i * a.ldg + j, sw[v]);
+            if (a.db) put(static_cast<P *>(a.db) + i * a.ldg + j, sb[v]);
+        }
     }
 }
 
@@ -362,14 +509,14 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(const float *part, 
     __shared__ float sums[kWarps][32];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.y;
-    const int at = blockIdx.x * 32 + lane;           // of the 2 cols sums
+    const int64_t at = (int64_t)blockIdx.x * 32 + lane, all = 2 * (int64_t)cols;
     float s = 0.f;
-    if (at < 2 * cols)
+    if (at < all)
 #pragma unroll 4
-        for (int c = warp; c < chunks; c += kWarps) s += part[((int64_t)i * chunks + c) * 2 * cols + at];
+        for (int c = warp; c < chunks; c += kWarps) s += part[((int64_t)i * chunks + c) * all + at];
     sums[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && at < 2 * cols) {
+    if (warp == 0 && at < all) {
 #pragma unroll
         for (int q = 1; q < kWarps; ++q) s += sums[q][lane];
         P *out = at < cols ? dw : db;
@@ -409,52 +556,80 @@ cudaError_t layer_norm(const NormArgs &a, cudaStream_t s) {
     return launch_chained(norm_any_kernel<T, P>, dim3((unsigned)(a.m * a.n)), dim3(kThreads), 0, s, false, a);
 }
 
-// Blocks that a group's rows are cut into.  About four times as many blocks as SMs (two at a time, so two rounds), each with at least
-// 16 rows for every row of threads.
+// Blocks that a group's rows are cut into: all groups' make two rounds of two blocks an SM, each block with at least 32 rows, beside
+// which its sums' way through memory is small.
 constexpr int kNormBlocks = 592;
 int norm_chunks(int m, int64_t n) {
     int64_t c = m > 0 ? kNormBlocks / m : 1;
-    if (c > n / 16) c = n / 16;
+    if (c > n / 32) c = n / 32;
     return c < 1 ? 1 : (int)c;
 }
 
-template <typename T, typename P, int N, int TPR, int ROWS>
-cudaError_t norm_columns(const NormGradArgs &a, cudaStream_t s) {
-    const bool weights = a.dw || a.db, saved = !a.x.data;
-    const int chunks = norm_chunks(a.m, a.n);
-    auto *kernel = a.dx.data ? (saved ? norm_columns_kernel<T, P, N, TPR, ROWS, true, true> : norm_columns_kernel<T, P, N, TPR, ROWS, false, true>)
-                             : (saved ? norm_columns_kernel<T, P, N, TPR, ROWS, true, false> : norm_columns_kernel<T, P, N, TPR, ROWS, false, false>);
-    const bool join = weights && chunks > 1;
-    cudaError_t e = launch_chained(kernel, dim3(chunks, a.m), dim3(TPR * ROWS), 0, s, false, a, join ? a.workspace : nullptr);
-    if (e == cudaSuccess && join)
-        e = launch_chained(norm_join_kernel<P>, dim3((unsigned)((2 * a.cols + 31) / 32), a.m), dim3(kThreads), 0, s, true, a.workspace, chunks,
-                           (int)a.cols, static_cast<P *>(a.dw), static_cast<P *>(a.db), a.ldg);
-    return e;
+template <typename P>
+cudaError_t norm_join(const NormGradArgs &a, int chunks, cudaStream_t s) {
+    return launch_chained(norm_join_kernel<P>, dim3((unsigned)((2 * a.cols + 31) / 32), a.m), dim3(kThreads), 0, s, true, a.workspace, chunks,
+                          (int)a.cols, static_cast<P *>(a.dw), static_cast<P *>(a.db), a.ldg);
 }
 
-template <typename T, typename P, int N>
+template <typename T, typename P, int TPR, bool SAVED, bool DX>
+cudaError_t norm_columns(const NormGradArgs &a, cudaStream_t s) {
+    constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kStages = TPR <= 256 ? 4 : 3;
+    constexpr int kSmem = kStages * kNV * TPR * kRows * (kSlotBytes<T, SAVED> + (SAVED ? 4 : 0));
+    auto *kernel = norm_columns_kernel<T, P, TPR, kRows, kStages, SAVED, DX>;
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    static PerDeviceOnce attr_set;
+    if (e == cudaSuccess && attr_set.need(device)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e == cudaSuccess) attr_set.mark(device);
+    }
+    if (e != cudaSuccess) return e;
+    const int chunks = norm_chunks(a.m, a.n);
+    const bool join = (a.dw || a.db) && chunks > 1;
+    e = launch_chained(kernel, dim3(chunks, a.m), dim3(TPR * kRows), kSmem, s, false, a, join ? a.workspace : nullptr);
+    return e == cudaSuccess && join ? norm_join<P>(a, chunks, s) : e;
+}
+
+template <typename T, typename P, bool SAVED, bool DX>
 cudaError_t norm_columns_any(const NormGradArgs &a, cudaStream_t s) {
-    const int64_t packs = a.cols / N;
-    if (packs <= 32) return norm_columns<T, P, N, 32, 8>(a, s);
-    if (packs <= 64) return norm_columns<T, P, N, 64, 1>(a, s);
-    if (packs <= 128) return norm_columns<T, P, N, 128, 1>(a, s);
-    if (packs <= 256) return norm_columns<T, P, N, 256, 1>(a, s);
-    if (packs <= 512) return norm_columns<T, P, N, 512, 1>(a, s);
-    return norm_columns<T, P, N, 1024, 1>(a, s);
+    const int64_t packs = a.cols / (16 / sizeof(T));
+    if (packs <= 64) return norm_columns<T, P, 32, SAVED, DX>(a, s);
+    if (packs <= 128) return norm_columns<T, P, 64, SAVED, DX>(a, s);
+    if (packs <= 256) return norm_columns<T, P, 128, SAVED, DX>(a, s);
+    if (packs <= 512) return norm_columns<T, P, 256, SAVED, DX>(a, s);
+    return norm_columns<T, P, 512, SAVED, DX>(a, s);
+}
+
+template <typename T, typename P, int TPR, int NV, bool DX>
+cudaError_t norm_entries(const NormGradArgs &a, cudaStream_t s) {
+    const int64_t tiles = DX ? 1 : (a.cols + TPR * NV - 1) / (TPR * NV);
+    const int chunks = norm_chunks(a.m, a.n);
+    const bool join = (a.dw || a.db) && chunks > 1;
+    const cudaError_t e = launch_chained(norm_entries_kernel<T, P, TPR, NV, DX>, dim3((unsigned)tiles, a.m, chunks), dim3(TPR), 0, s, false, a,
+                                         join ? a.workspace : nullptr);
+    return e == cudaSuccess && join ? norm_join<P>(a, chunks, s) : e;
 }
 
 template <typename T, typename P>
 cudaError_t layer_norm_gradient(const NormGradArgs &a, cudaStream_t s) {
     constexpr int N = 16 / sizeof(T);
+    const bool dx = a.dx.data && a.n > 0, weights = a.dw || a.db;
     const bool aligned = a.cols % N == 0 && aligned_to(a.dy, a.m, a.n, sizeof(T), 16) && aligned_to(a.dx, a.m, a.n, sizeof(T), 16) &&
                          (a.x.data ? aligned_to(a.x, a.m, a.n, sizeof(T), 16) : aligned_to(a.codes, a.m, a.n, 1, N));
-    if (a.n > 0 && aligned && a.cols <= 1024 * N) return norm_columns_any<T, P, N>(a, s);
-    if (a.n > 0 && a.cols <= 1024) return norm_columns_any<T, P, 1>(a, s);
+    if (!dx && !weights) return cudaSuccess;
+    if (a.n > 0 && aligned && a.cols <= 1024 * N) {
+        if (a.x.data) return dx ? norm_columns_any<T, P, false, true>(a, s) : norm_columns_any<T, P, false, false>(a, s);
+        return dx ? norm_columns_any<T, P, true, true>(a, s) : norm_columns_any<T, P, true, false>(a, s);
+    }
+    if (dx && weights) {
+        if (a.cols <= 512) return norm_entries<T, P, 128, 4, true>(a, s);
+        if (a.cols <= 2048) return norm_entries<T, P, 512, 4, true>(a, s);
+        if (a.cols <= 4096) return norm_entries<T, P, 1024, 4, true>(a, s);
+    }
     cudaError_t e = cudaSuccess;
-    if (a.dw || a.db) e = launch_chained(norm_weights_any_kernel<T, P>, dim3((unsigned)((a.cols + 31) / 32), a.m), dim3(kThreads), 0, s, false, a);
+    if (weights) e = norm_entries<T, P, 256, 2, false>(a, s);
     // last, since dx may lie in dy's place
-    if (e == cudaSuccess && a.dx.data && a.n > 0)
-        e = launch_chained(norm_dx_any_kernel<T, P>, dim3((unsigned)(a.m * a.n)), dim3(kThreads), 0, s, false, a);
+    if (e == cudaSuccess && dx) e = launch_chained(norm_dx_any_kernel<T, P>, dim3((unsigned)(a.m * a.n)), dim3(kThreads), 0, s, false, a);
     return e;
 }
 

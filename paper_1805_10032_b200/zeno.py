@@ -478,37 +478,52 @@ class TokenLogprobs(NamedTuple):
     top_logprobs: Optional[torch.Tensor]
 
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+# Calls of a few tokens are over on the GPU in a few microseconds, so here too what the binding spends on a call shows: messages are built only for
+# a refusal, shapes and strides are read once, empty_like is preferred.
+def _refuse(what: str):
+    raise ValueError(what)
 
 
 def _type(t: torch.Tensor, name: str) -> int:
     kind = _TYPES.get(t.dtype)
     if kind is None:
-        raise ValueError(f"{name}: float32 or bfloat16 is needed, not {t.dtype}")
+        _refuse(f"{name}: float32 or bfloat16 is needed, not {t.dtype}")
     return kind
 
 
 def _rows(t: torch.Tensor, name: str) -> RowsDesc:
-    _need(t.dim() in (2, 3), f"{name}: [m, n, columns] or [n, columns] is needed, not {tuple(t.shape)}")
-    _need(t.stride(-1) == 1 or t.shape[-1] <= 1, f"{name}: the last stride has to be 1")
-    return RowsDesc(t.data_ptr(), t.stride(-2), t.stride(0) if t.dim() == 3 else 0)
+    strides = t.stride()
+    if len(strides) == 3:
+        group, row, last = strides
+    elif len(strides) == 2:
+        group, (row, last) = 0, strides
+    else:
+        _refuse(f"{name}: [m, n, columns] or [n, columns] is needed, not {tuple(t.shape)}")
+    if last != 1 and t.shape[-1] > 1:
+        _refuse(f"{name}: the last stride has to be 1")
+    return RowsDesc(t.data_ptr(), row, group)
 
 
 def _sizes(t: torch.Tensor):
-    return (t.shape[0] if t.dim() == 3 else 1), t.shape[-2], t.shape[-1]
+    shape = t.shape
+    if len(shape) == 3:
+        return shape
+    if len(shape) != 2:
+        _refuse(f"[m, n, columns] or [n, columns] is needed, not {tuple(shape)}")
+    return 1, shape[0], shape[1]
 
 
-def _cuda(dev: torch.device, **tensors):
-    _need(dev.type == "cuda", "CUDA tensors are needed")
-    for name, t in tensors.items():
-        _need(t is None or t.device == dev, f"{name}: on another device than the rest")
+def _cuda(dev: torch.device, *tensors):
+    if dev.type != "cuda":
+        _refuse("CUDA tensors are needed")
+    for t in tensors:
+        if t is not None and t.device != dev:
+            _refuse(f"CUDA tensors on one device are needed, not {dev} and {t.device}")
 
 
-def _per_token(t: Optional[torch.Tensor], like: torch.Tensor, dtype, name: str):
-    if t is not None:
-        _need(t.dtype == dtype and t.shape == like.shape[:-1] and t.is_contiguous(), f"{name}: contiguous {dtype} {tuple(like.shape[:-1])} is needed")
+def _per_token(t: Optional[torch.Tensor], lead, dtype, name: str):
+    if t is not None and (t.dtype != dtype or t.shape != lead or not t.is_contiguous()):
+        _refuse(f"{name}: contiguous {dtype} {tuple(lead)} is needed")
 
 
 def _current(dev: torch.device, stream) -> int:
@@ -519,7 +534,7 @@ def _current(dev: torch.device, stream) -> int:
     return _raw_stream(dev.index)
 
 
-def _empty(stream, shape, dtype, dev):
+def _empty(stream, dev: torch.device, shape, dtype) -> torch.Tensor:
     """An output or scratch: memory of the stream that the call runs on."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=dev)
@@ -527,8 +542,16 @@ def _empty(stream, shape, dtype, dev):
         return torch.empty(shape, dtype=dtype, device=dev)
 
 
-def _scratch(stream, nbytes: int, dev):
-    return _empty(stream, nbytes, torch.uint8, dev) if nbytes else None
+def _empty_like(stream, t: torch.Tensor, dtype=None) -> torch.Tensor:
+    """The same in the shape of t (and its order of dimensions), at less than half the cost."""
+    if stream is None:
+        return torch.empty_like(t, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t, dtype=dtype)
+
+
+def _scratch(stream, nbytes: int, dev: torch.device):
+    return _empty(stream, dev, nbytes, torch.uint8) if nbytes else None
 
 
 def _done(st: int, what: str):
@@ -536,50 +559,58 @@ def _done(st: int, what: str):
         raise ZenoError(st, what)
 
 
-def _norm_weight(w: Optional[torch.Tensor], x: torch.Tensor, name: str) -> int:
+def _norm_weight(w: torch.Tensor, m: int, cols: int, name: str) -> int:
     """Elements between the groups' weights: 0 if they share them."""
-    if w is None:
-        return 0
-    m, _, cols = _sizes(x)
-    _need(w.shape[-1] == cols and (w.dim() == 1 or (w.dim() == 2 and w.shape[0] == m)) and (w.stride(-1) == 1 or cols <= 1),
-          f"{name}: [{cols}] or [{m}, {cols}] with a last stride of 1 is needed")
-    return w.stride(0) if w.dim() == 2 and m > 1 else 0
+    shape = w.shape
+    if shape[-1] != cols or not (len(shape) == 1 or (len(shape) == 2 and shape[0] == m)) or (cols > 1 and w.stride(-1) != 1):
+        _refuse(f"{name}: [{cols}] or [{m}, {cols}] with a last stride of 1 is needed")
+    return w.stride(0) if len(shape) == 2 and m > 1 else 0
+
+
+def _alike(t: torch.Tensor, like: torch.Tensor, name: str):
+    if t.shape != like.shape or t.dtype != like.dtype:
+        _refuse(f"{name}: {like.dtype} {tuple(like.shape)} is needed")
 
 
 def layer_norm(x, weight, bias=None, eps=1e-5, out=None, want_stats=True, stream=None):
     """zeno_layer_norm: returns (y, mean or None, rstd or None).  weight, bias: [columns], or [m, columns] where every model has its own (of one
     stride: slices of the models' parameter vectors).  out may be x."""
     lib = load_library()
+    dev = x.device
     m, n, cols = _sizes(x)
-    _cuda(x.device, weight=weight, bias=bias, out=out)
-    ldw = _norm_weight(weight, x, "weight")
-    if bias is not None:
-        _need(bias.dtype == weight.dtype and bias.dim() == weight.dim() and _norm_weight(bias, x, "bias") == ldw,
-              "bias: the type and layout of the weight is needed")
-    y = _empty(stream, x.shape, x.dtype, x.device) if out is None else out
-    _need(y.shape == x.shape and y.dtype == x.dtype, "out: the shape and type of x is needed")
-    mean = _empty(stream, x.shape[:-1], torch.float32, x.device) if want_stats else None
-    rstd = _empty(stream, x.shape[:-1], torch.float32, x.device) if want_stats else None
-    _done(lib.zeno_layer_norm(x.device.index, _type(x, "x"), _type(weight, "weight"), _rows(x, "x"), m, n, cols, _ptr(weight),
-                              _ptr(bias), ldw, eps, _rows(y, "out"), _ptr(mean), _ptr(rstd), _current(x.device, stream)), "zeno_layer_norm")
-    return y, mean, rstd
+    _cuda(dev, weight, bias, out)
+    ldw = _norm_weight(weight, m, cols, "weight")
+    if bias is not None and (bias.dtype != weight.dtype or bias.shape != weight.shape or _norm_weight(bias, m, cols, "bias") != ldw):
+        _refuse("bias: the type and layout of the weight is needed")
+    if out is None:
+        out = _empty_like(stream, x)
+    else:
+        _alike(out, x, "out")
+    mean = rstd = None
+    if want_stats:
+        mean = _empty(stream, dev, x.shape[:-1], torch.float32)
+        rstd = _empty_like(stream, mean)
+    _done(lib.zeno_layer_norm(dev.index, _type(x, "x"), _type(weight, "weight"), _rows(x, "x"), m, n, cols, weight.data_ptr(),
+                              _ptr(bias), ldw, eps, _rows(out, "out"), _ptr(mean), _ptr(rstd), _current(dev, stream)), "zeno_layer_norm")
+    return out, mean, rstd
 
 
-def _saved_rows(saved, like, cols: int):
+def _saved_rows(saved, lead, cols: int):
     codes, scales = saved
-    lead = tuple(like.shape[:-1])
-    _need(codes.dtype in (torch.float8_e4m3fn, torch.uint8) and tuple(codes.shape) == lead + (cols,), f"codes: float8_e4m3fn {lead + (cols,)} is needed")
-    _need(scales.dtype == torch.float32 and tuple(scales.shape) == lead + (-(-cols // SAVED_BLOCK),),
-          f"scales: float32 {lead + (-(-cols // SAVED_BLOCK),)} is needed")
+    if codes.dtype not in (torch.float8_e4m3fn, torch.uint8) or codes.shape != (*lead, cols):
+        _refuse(f"codes: float8_e4m3fn {(*lead, cols)} is needed")
+    if scales.dtype != torch.float32 or scales.shape != (*lead, -(-cols // SAVED_BLOCK)):
+        _refuse(f"scales: float32 {(*lead, -(-cols // SAVED_BLOCK))} is needed")
     return _rows(codes, "codes"), _rows(scales, "scales")
 
 
-def _gradient_row(t: Optional[torch.Tensor], m: int, cols: int, like, name: str) -> int:
+def _gradient_row(t: Optional[torch.Tensor], m: int, cols: int, dtype, name: str) -> int:
     if t is None:
         return 0
-    _need(t.dtype == like.dtype and tuple(t.shape) in ((m, cols),) + (((cols,),) if m == 1 else ()) and (t.stride(-1) == 1 or cols <= 1),
-          f"{name}: {like.dtype} [{m}, {cols}] with a last stride of 1 is needed")
-    return t.stride(0) if t.dim() == 2 else cols
+    shape = t.shape
+    if t.dtype != dtype or not (shape == (m, cols) or (m == 1 and shape == (cols,))) or (cols > 1 and t.stride(-1) != 1):
+        _refuse(f"{name}: {dtype} [{m}, {cols}] with a last stride of 1 is needed")
+    return t.stride(0) if len(shape) == 2 else cols
 
 
 def layer_norm_gradient(dy, x: Union[torch.Tensor, Saved], weight, mean, rstd, dweight=None, dbias=None, dx=None, want_dx=True,
@@ -587,41 +618,50 @@ def layer_norm_gradient(dy, x: Union[torch.Tensor, Saved], weight, mean, rstd, d
     """zeno_layer_norm_gradient: writes dweight and dbias ([m, columns], for instance V[:, at:at + columns], of one stride) and
     returns dx (None if not wanted).  x: the layer's input, or what pack_activations kept of it.  dx may be dy."""
     lib = load_library()
+    dev, lead = dy.device, dy.shape[:-1]
     m, n, cols = _sizes(dy)
-    saved = isinstance(x, tuple)
-    _cuda(dy.device, x=x[0] if saved else x, scales=x[1] if saved else None, weight=weight, mean=mean, rstd=rstd, dweight=dweight, dbias=dbias, dx=dx)
-    codes, scales = _saved_rows(x, dy, cols) if saved else (None, None)
-    if not saved:
-        _need(x.shape == dy.shape and x.dtype == dy.dtype, "x: the shape and type of dy is needed")
-    _per_token(mean, dy, torch.float32, "mean")
-    _per_token(rstd, dy, torch.float32, "rstd")
-    ldw = _norm_weight(weight, dy, "weight")
-    ldg = _gradient_row(dweight, m, cols, weight, "dweight")
+    x_rows = codes = scales = None
+    if isinstance(x, tuple):
+        _cuda(dev, x[0], x[1], weight, mean, rstd, dweight, dbias, dx)
+        codes, scales = _saved_rows(x, lead, cols)
+    else:
+        _cuda(dev, x, weight, mean, rstd, dweight, dbias, dx)
+        _alike(x, dy, "x")
+        x_rows = _rows(x, "x")
+    _per_token(mean, lead, torch.float32, "mean")
+    _per_token(rstd, lead, torch.float32, "rstd")
+    ldw = _norm_weight(weight, m, cols, "weight")
+    ldg = _gradient_row(dweight, m, cols, weight.dtype, "dweight")
     if dbias is not None:
-        ldb = _gradient_row(dbias, m, cols, weight, "dbias")
-        _need(dweight is None or ldb == ldg or m == 1, "dbias: the stride of dweight is needed")
-        ldg = ldb if dweight is None else ldg
-    if dx is None and want_dx:
-        dx = _empty(stream, dy.shape, dy.dtype, dy.device)
-    _need(dx is None or (dx.shape == dy.shape and dx.dtype == dy.dtype), "dx: the shape and type of dy is needed")
+        ldb = _gradient_row(dbias, m, cols, weight.dtype, "dbias")
+        if dweight is None:
+            ldg = ldb
+        elif ldb != ldg and m > 1:
+            _refuse("dbias: the stride of dweight is needed")
+    if dx is not None:
+        _alike(dx, dy, "dx")
+    elif want_dx:
+        dx = _empty_like(stream, dy)
     nbytes = lib.zeno_layer_norm_gradient_workspace(m, n, cols)
-    ws = _scratch(stream, nbytes, dy.device)
-    _done(lib.zeno_layer_norm_gradient(dy.device.index, _type(dy, "dy"), _type(weight, "weight"), _rows(dy, "dy"),
-                                       None if saved else _rows(x, "x"), codes, scales, m, n, cols, _ptr(weight), ldw, _ptr(mean),
-                                       _ptr(rstd), None if dx is None else _rows(dx, "dx"), _ptr(dweight), _ptr(dbias), ldg, _ptr(ws), nbytes,
-                                       _current(dy.device, stream)), "zeno_layer_norm_gradient")
+    ws = _scratch(stream, nbytes, dev)
+    _done(lib.zeno_layer_norm_gradient(dev.index, _type(dy, "dy"), _type(weight, "weight"), _rows(dy, "dy"), x_rows, codes, scales, m, n, cols,
+                                       weight.data_ptr(), ldw, mean.data_ptr(), rstd.data_ptr(), None if dx is None else _rows(dx, "dx"),
+                                       _ptr(dweight), _ptr(dbias), ldg, _ptr(ws), nbytes, _current(dev, stream)), "zeno_layer_norm_gradient")
     return dx
 
 
 def pack_activations(x, stream=None) -> Saved:
     """zeno_pack_activations: x in 8 bits, for layer_norm_gradient and dense_gradient."""
     lib = load_library()
+    dev, lead = x.device, x.shape[:-1]
     m, n, cols = _sizes(x)
-    _cuda(x.device)
-    codes = _empty(stream, tuple(x.shape[:-1]) + (-(-cols // 16) * 16,), torch.float8_e4m3fn, x.device)[..., :cols]
-    scales = _empty(stream, tuple(x.shape[:-1]) + (-(-cols // SAVED_BLOCK),), torch.float32, x.device)
-    _done(lib.zeno_pack_activations(x.device.index, _type(x, "x"), _rows(x, "x"), m, n, cols, _rows(codes, "codes"), _rows(scales, "scales"),
-                                    _current(x.device, stream)), "zeno_pack_activations")
+    _cuda(dev)
+    codes = _empty(stream, dev, (*lead, -(-cols // 16) * 16), torch.float8_e4m3fn)
+    if cols % 16:
+        codes = codes[..., :cols]
+    scales = _empty(stream, dev, (*lead, -(-cols // SAVED_BLOCK)), torch.float32)
+    _done(lib.zeno_pack_activations(dev.index, _type(x, "x"), _rows(x, "x"), m, n, cols, _rows(codes, "codes"), _rows(scales, "scales"),
+                                    _current(dev, stream)), "zeno_pack_activations")
     return Saved(codes, scales)
 
 
@@ -630,18 +670,22 @@ def dense_gradient(dy, saved: Saved, dweight, dbias=None, stream=None):
     dweight: [m, outputs, inputs] (or without m), contiguous per group, for instance
     V[:, at:at + outputs * inputs].unflatten(1, (outputs, inputs)); dbias: [m, outputs]."""
     lib = load_library()
+    dev = dy.device
     m, n, outputs = _sizes(dy)
     inputs = saved[0].shape[-1]
-    _cuda(dy.device, codes=saved[0], scales=saved[1], dweight=dweight, dbias=dbias)
-    codes, scales = _saved_rows(saved, dy, inputs)
-    _need(tuple(dweight.shape) in ((m, outputs, inputs),) + (((outputs, inputs),) if m == 1 else ()), f"dweight: [{m}, {outputs}, {inputs}] is needed")
-    _need((inputs <= 1 or dweight.stride(-1) == 1) and (outputs <= 1 or dweight.stride(-2) == inputs), "dweight: contiguous for every group is needed")
-    ldb = _gradient_row(dbias, m, outputs, dweight, "dbias")
+    _cuda(dev, saved[0], saved[1], dweight, dbias)
+    codes, scales = _saved_rows(saved, dy.shape[:-1], inputs)
+    shape, strides = dweight.shape, dweight.stride()
+    if not (shape == (m, outputs, inputs) or (m == 1 and shape == (outputs, inputs))):
+        _refuse(f"dweight: [{m}, {outputs}, {inputs}] is needed")
+    if (inputs > 1 and strides[-1] != 1) or (outputs > 1 and strides[-2] != inputs):
+        _refuse("dweight: contiguous for every group is needed")
+    ldb = _gradient_row(dbias, m, outputs, dweight.dtype, "dbias")
     nbytes = lib.zeno_dense_gradient_workspace(m, n, inputs, outputs)
-    ws = _scratch(stream, nbytes, dy.device)
-    _done(lib.zeno_dense_gradient(dy.device.index, _type(dy, "dy"), _type(dweight, "dweight"), _rows(dy, "dy"), codes, scales, m, n, inputs,
-                                  outputs, _ptr(dweight), dweight.stride(0) if dweight.dim() == 3 else inputs * outputs, _ptr(dbias), ldb,
-                                  _ptr(ws), nbytes, _current(dy.device, stream)), "zeno_dense_gradient")
+    ws = _scratch(stream, nbytes, dev)
+    _done(lib.zeno_dense_gradient(dev.index, _type(dy, "dy"), _type(dweight, "dweight"), _rows(dy, "dy"), codes, scales, m, n, inputs,
+                                  outputs, dweight.data_ptr(), strides[0] if len(shape) == 3 else inputs * outputs, _ptr(dbias), ldb,
+                                  _ptr(ws), nbytes, _current(dev, stream)), "zeno_dense_gradient")
     return dweight
 
 
@@ -650,15 +694,18 @@ def token_logprobs(logits, targets=None, top=0, stream=None) -> TokenLogprobs:
     [n, vocab]; targets: int32, one outside the vocabulary means none."""
     lib = load_library()
     m, n, vocab = _sizes(logits)
-    dev, lead = logits.device, tuple(logits.shape[:-1])
-    _cuda(dev, targets=targets)
-    _per_token(targets, logits, torch.int32, "targets")
-    lp = _empty(stream, lead, torch.float32, dev) if targets is not None else None
-    entropy, lse = _empty(stream, lead, torch.float32, dev), _empty(stream, lead, torch.float32, dev)
-    idx = _empty(stream, lead + (top,), torch.int32, dev) if top > 0 else None
-    top_lp = _empty(stream, lead + (top,), torch.float32, dev) if top > 0 else None
+    dev, lead = logits.device, logits.shape[:-1]
+    _cuda(dev, targets)
+    _per_token(targets, lead, torch.int32, "targets")
+    entropy = _empty(stream, dev, lead, torch.float32)
+    lse = _empty_like(stream, entropy)
+    lp = None if targets is None else _empty_like(stream, entropy)
+    idx = top_lp = None
+    if top > 0:
+        idx = _empty(stream, dev, (*lead, top), torch.int32)
+        top_lp = _empty_like(stream, idx, torch.float32)
     _done(lib.zeno_token_logprobs(dev.index, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, _ptr(targets), top, _ptr(lp),
-                                  _ptr(entropy), _ptr(lse), _ptr(idx), _ptr(top_lp), _current(dev, stream)), "zeno_token_logprobs")
+                                  entropy.data_ptr(), lse.data_ptr(), _ptr(idx), _ptr(top_lp), _current(dev, stream)), "zeno_token_logprobs")
     return TokenLogprobs(lp, entropy, lse, idx, top_lp)
 
 
@@ -666,18 +713,25 @@ def token_gradient(logits, targets, lse, g_logprob, entropy=None, g_entropy=None
     """zeno_token_gradient: the gradient at the logits from the gradients at token_logprobs's logprobs and (g_entropy) entropy.
     out may be the logits."""
     lib = load_library()
+    dev, lead = logits.device, logits.shape[:-1]
     m, n, vocab = _sizes(logits)
-    _cuda(logits.device, targets=targets, lse=lse, g_logprob=g_logprob, entropy=entropy, g_entropy=g_entropy, out=out)
-    _need(g_entropy is None or entropy is not None, "entropy: needed with g_entropy")
-    _per_token(targets, logits, torch.int32, "targets")
-    for name, t in (("lse", lse), ("g_logprob", g_logprob), ("entropy", entropy), ("g_entropy", g_entropy)):
-        _per_token(t, logits, torch.float32, name)
-    grad = _empty(stream, logits.shape, logits.dtype, logits.device) if out is None else out
-    _need(grad.shape == logits.shape and grad.dtype == logits.dtype, "out: the shape and type of the logits is needed")
-    _done(lib.zeno_token_gradient(logits.device.index, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, _ptr(targets),
-                                  _ptr(lse), _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _rows(grad, "out"),
-                                  _current(logits.device, stream)), "zeno_token_gradient")
-    return grad
+    _cuda(dev, targets, lse, g_logprob, entropy, g_entropy, out)
+    _per_token(targets, lead, torch.int32, "targets")
+    _per_token(lse, lead, torch.float32, "lse")
+    _per_token(g_logprob, lead, torch.float32, "g_logprob")
+    if g_entropy is not None:
+        if entropy is None:
+            _refuse("entropy: needed with g_entropy")
+        _per_token(entropy, lead, torch.float32, "entropy")
+        _per_token(g_entropy, lead, torch.float32, "g_entropy")
+    if out is None:
+        out = _empty_like(stream, logits)
+    else:
+        _alike(out, logits, "out")
+    _done(lib.zeno_token_gradient(dev.index, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, targets.data_ptr(), lse.data_ptr(),
+                                  _ptr(entropy), g_logprob.data_ptr(), _ptr(g_entropy), _rows(out, "out"), _current(dev, stream)),
+          "zeno_token_gradient")
+    return out
 
 
 def from_workload(w, m_max=None, n_r_max=None, device=0) -> "Zeno":
