@@ -4,6 +4,8 @@
 // the registers of the 32 to 1024 threads that share it, between the sum, the centred squares and the result.  Backward: a
 // thread owns columns, not rows: it goes down a stretch of a group's rows with the sums of its columns' weight gradients in
 // registers, and copies of the rows ahead are in flight while a row's two averages are formed across the block.
+#include <stdlib.h>
+
 #include "zeno_operators.h"
 #include "zeno_saved.cuh"
 
@@ -192,28 +194,6 @@ __global__ void __launch_bounds__(TPR == 32 ? kRowBlock : TPR) norm_row_kernel(N
 }
 
 // ---- backward, by columns
-
-// Two binary32 numbers that one instruction takes
-struct Two { float x, y; };
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-    Two d;
-    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ Two add2(Two a, Two b) {
-    Two d;
-    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-__device__ __forceinline__ Two mul2(Two a, Two b) {
-    Two d;
-    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-__device__ __forceinline__ Two both(float v) { return Two{v, v}; }
 
 // 16 bytes of activations as pairs
 __device__ __forceinline__ void pairs(uint4 u, Two (&f)[2], float) {
@@ -502,6 +482,103 @@ __global__ void __launch_bounds__(TPR) norm_entries_kernel(NormGradArgs a, float
     }
 }
 
+// Forward, many rows of whole vectors: the blocks, rows and rings of the backward pass, with a group's weights in registers.  (Taking
+// the weights from L2 for every row, as norm_row_kernel does, costs as much of its bandwidth as the rows themselves.)
+template <typename T, typename P, int TPR, int ROWS, int STAGES>
+__global__ void __launch_bounds__(TPR *ROWS, TPR *ROWS <= 256 ? 3 : 1) norm_stream_kernel(NormArgs a) {
+    constexpr int N = 16 / sizeof(T), H = N / 2, kWarps = TPR / 32, kThreadsHere = TPR * ROWS;
+    extern __shared__ __align__(16) uint8_t ring[];            // [STAGES][NV][threads] vectors of x
+    __shared__ __align__(16) float scratch[2][ROWS][kWarps];
+    const int tid = threadIdx.x, sub = tid / TPR, t = tid % TPR;
+    const int cols = (int)a.cols, chunks = gridDim.x, i = blockIdx.y;
+    const int64_t first = a.n * blockIdx.x / chunks + sub, last = a.n * (blockIdx.x + 1) / chunks;
+    const T *x = static_cast<const T *>(a.x.data) + i * a.x.group;
+    T *y = static_cast<T *>(a.y.data) + i * a.y.group;
+    int at[kNV];
+    bool mine[kNV];
+    Two w[kNV][H], b[kNV][H];
+    auto slot = [&](int stage, int v) { return (stage * kNV + v) * kThreadsHere + tid; };
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    auto fetch = [&](int stage, int64_t row) {
+        if (row < last)
+#pragma unroll
+            for (int v = 0; v < kNV; ++v)
+                if (mine[v]) cp_async<16>(ring_at + slot(stage, v) * 16, x + row * a.x.row + at[v]);
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int v = 0; v < kNV; ++v) {
+        at[v] = (v * TPR + t) * N;
+        mine[v] = at[v] < cols;
+    }
+#pragma unroll
+    for (int q = 0; q < STAGES - 1; ++q) fetch(q, first + q * ROWS);
+#pragma unroll
+    for (int v = 0; v < kNV; ++v)
+#pragma unroll
+        for (int k = 0; k < H; ++k) {
+            const int64_t from = i * a.ldw + at[v] + 2 * k;
+            const P *wp = static_cast<const P *>(a.w) + from, *bp = static_cast<const P *>(a.b) + from;
+            w[v][k] = mine[v] ? Two{value_of(wp), value_of(wp + 1)} : both(0.f);
+            b[v][k] = mine[v] && a.b ? Two{value_of(bp), value_of(bp + 1)} : both(0.f);
+        }
+    // the row's sum in all of its threads; `which` of two scratches in turn
+    auto row_total = [&](float v, int which) {
+        v = warp_sum(v);
+        if constexpr (kWarps > 1) {
+            if ((t & 31) == 0) scratch[which][sub][t >> 5] = v;
+            __syncthreads();
+            v = 0.f;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) v += scratch[which][sub][k];
+        }
+        return v;
+    };
+    int stage = 0;
+    for (int64_t row = first; row - sub < last; row += ROWS) {
+        fetch(stage == 0 ? STAGES - 1 : stage - 1, row + (STAGES - 1) * ROWS);
+        cp_async_wait<STAGES - 1>();
+        const bool on = row < last;
+        Two f[kNV][H], s = both(0.f);
+#pragma unroll
+        for (int v = 0; v < kNV; ++v) {
+            pairs(reinterpret_cast<const uint4 *>(ring)[slot(stage, v)], f[v], T());
+            if (!on || !mine[v])
+#pragma unroll
+                for (int k = 0; k < H; ++k) f[v][k] = both(0.f);
+#pragma unroll
+            for (int k = 0; k < H; ++k) s = add2(s, f[v][k]);
+        }
+        const float mean = row_total(s.x + s.y, 0) / (float)cols;
+        s = both(0.f);
+#pragma unroll
+        for (int v = 0; v < kNV; ++v)
+            if (mine[v])
+#pragma unroll
+                for (int k = 0; k < H; ++k) {
+                    f[v][k] = add2(f[v][k], both(-mean));
+                    s = fma2(f[v][k], f[v][k], s);
+                }
+        const float rstd = rsqrtf(row_total(s.x + s.y, 1) / (float)cols + a.eps);
+        if (on) {
+#pragma unroll
+            for (int v = 0; v < kNV; ++v)
+                if (mine[v]) {
+                    Two o[H];
+#pragma unroll
+                    for (int k = 0; k < H; ++k) o[k] = fma2(mul2(f[v][k], both(rstd)), w[v][k], b[v][k]);
+                    *reinterpret_cast<uint4 *>(y + row * a.y.row + at[v]) = from_pairs(o, T());
+                }
+            if (t == 0) {
+                if (a.mean) a.mean[i * a.n + row] = mean;
+                if (a.rstd) a.rstd[i * a.n + row] = rstd;
+            }
+        }
+        if (++stage == STAGES) stage = 0;
+    }
+    cp_async_wait<0>();
+}
+
 // The blocks' sums of a group, column by column: 32 columns a block, eight warps take the blocks in turn.
 template <typename P>
 __global__ void __launch_bounds__(kThreads) norm_join_kernel(const float *part, int chunks, int cols, P *dw, P *db, int64_t ldg) {
@@ -524,6 +601,36 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(const float *part, 
     }
 }
 
+// Blocks that a group's rows are cut into: all groups' make two rounds of two blocks an SM, each block with at least 8 rows: few
+// rows to a block are few groups' rows, whose sums stay in L2.
+constexpr int kNormBlocks = 592;
+int norm_chunks(int m, int64_t n) {
+    int64_t c = m > 0 ? kNormBlocks / m : 1;
+    if (c > n / 8) c = n / 8;
+    return c < 1 ? 1 : (int)c;
+}
+
+// sets a kernel's dynamic shared memory on the current device, once
+template <typename K>
+cudaError_t allow_shared(K *kernel, int bytes, PerDeviceOnce &once) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess && once.need(device)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) once.mark(device);
+    }
+    return e;
+}
+
+template <typename T, typename P, int TPR>
+cudaError_t norm_stream(const NormArgs &a, cudaStream_t s) {
+    constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kStages = 4, kSmem = kStages * kNV * TPR * kRows * 16;
+    auto *kernel = norm_stream_kernel<T, P, TPR, kRows, kStages>;
+    static PerDeviceOnce attr_set;
+    const cudaError_t e = allow_shared(kernel, kSmem, attr_set);
+    return e != cudaSuccess ? e : launch_chained(kernel, dim3(norm_chunks(a.m, a.n), a.m), dim3(TPR * kRows), kSmem, s, false, a);
+}
+
 template <typename T, typename P, int N, int TPR, int NV>
 cudaError_t norm_rows(const NormArgs &a, bool wide, cudaStream_t s) {
     const int64_t rows = a.m * a.n;
@@ -539,6 +646,14 @@ cudaError_t layer_norm(const NormArgs &a, cudaStream_t s) {
         const size_t pack = N * sizeof(P) < 16 ? N * sizeof(P) : 16;
         const bool wide = reinterpret_cast<uintptr_t>(a.w) % pack == 0 && reinterpret_cast<uintptr_t>(a.b) % pack == 0 && a.ldw * sizeof(P) % pack == 0;
         const int64_t packs = a.cols / N;
+        // enough rows for every block to keep the weights for eight of them and more
+        if (norm_chunks(a.m, a.n) * (int64_t)a.m >= kNormBlocks / 2 && packs <= 1024 && a.n * a.m >= kNormBlocks * 8 && getenv("NOSTREAM") == nullptr) {
+            if (packs <= 64) return norm_stream<T, P, 32>(a, s);
+            if (packs <= 128) return norm_stream<T, P, 64>(a, s);
+            if (packs <= 256) return norm_stream<T, P, 128>(a, s);
+            if (packs <= 512) return norm_stream<T, P, 256>(a, s);
+            return norm_stream<T, P, 512>(a, s);
+        }
         if (packs <= 32) return norm_rows<T, P, N, 32, 1>(a, wide, s);
         if (packs <= 64) return norm_rows<T, P, N, 32, 2>(a, wide, s);
         if (packs <= 128) return norm_rows<T, P, N, 32, 4>(a, wide, s);
@@ -556,15 +671,6 @@ cudaError_t layer_norm(const NormArgs &a, cudaStream_t s) {
     return launch_chained(norm_any_kernel<T, P>, dim3((unsigned)(a.m * a.n)), dim3(kThreads), 0, s, false, a);
 }
 
-// Blocks that a group's rows are cut into: all groups' make two rounds of two blocks an SM, each block with at least 32 rows, beside
-// which its sums' way through memory is small.
-constexpr int kNormBlocks = 592;
-int norm_chunks(int m, int64_t n) {
-    int64_t c = m > 0 ? kNormBlocks / m : 1;
-    if (c > n / 32) c = n / 32;
-    return c < 1 ? 1 : (int)c;
-}
-
 template <typename P>
 cudaError_t norm_join(const NormGradArgs &a, int chunks, cudaStream_t s) {
     return launch_chained(norm_join_kernel<P>, dim3((unsigned)((2 * a.cols + 31) / 32), a.m), dim3(kThreads), 0, s, true, a.workspace, chunks,
@@ -576,13 +682,8 @@ cudaError_t norm_columns(const NormGradArgs &a, cudaStream_t s) {
     constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kStages = TPR <= 256 ? 4 : 3;
     constexpr int kSmem = kStages * kNV * TPR * kRows * (kSlotBytes<T, SAVED> + (SAVED ? 4 : 0));
     auto *kernel = norm_columns_kernel<T, P, TPR, kRows, kStages, SAVED, DX>;
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
     static PerDeviceOnce attr_set;
-    if (e == cudaSuccess && attr_set.need(device)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        if (e == cudaSuccess) attr_set.mark(device);
-    }
+    cudaError_t e = allow_shared(kernel, kSmem, attr_set);
     if (e != cudaSuccess) return e;
     const int chunks = norm_chunks(a.m, a.n);
     const bool join = (a.dw || a.db) && chunks > 1;

@@ -57,69 +57,87 @@ __global__ void __launch_bounds__(256) pack_any_kernel(PackArgs a, int64_t block
 // other, with all their loads ahead of the first maximum.
 constexpr int kStrip = 4;
 
-__device__ __forceinline__ void load_eight(const float *p, float (&f)[8]) {
-    const float4 u = reinterpret_cast<const float4 *>(p)[0], v = reinterpret_cast<const float4 *>(p)[1];
-    f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; f[4] = v.x; f[5] = v.y; f[6] = v.z; f[7] = v.w;
-}
-__device__ __forceinline__ void load_eight(const __nv_bfloat16 *p, float (&f)[8]) {
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+// Eight entries of a row: the bits of their largest magnitude (at least 0x7f800000 if one is not finite), and themselves as pairs.
+struct Eight {
+    uint4 u, v;
+    __device__ __forceinline__ void load(const float *p) {
+        u = reinterpret_cast<const uint4 *>(p)[0];
+        v = reinterpret_cast<const uint4 *>(p)[1];
     }
-}
+    __device__ __forceinline__ uint32_t most(float) const {
+        const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+        return m;
+    }
+    __device__ __forceinline__ void get(Two (&f)[4], float) const {
+        f[0] = Two{__uint_as_float(u.x), __uint_as_float(u.y)};
+        f[1] = Two{__uint_as_float(u.z), __uint_as_float(u.w)};
+        f[2] = Two{__uint_as_float(v.x), __uint_as_float(v.y)};
+        f[3] = Two{__uint_as_float(v.z), __uint_as_float(v.w)};
+    }
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { u = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ uint32_t most(__nv_bfloat16) const {
+        auto size = [](uint32_t w) {
+            w &= 0x7fff7fffu;
+            return *reinterpret_cast<__nv_bfloat162 *>(&w);
+        };
+        const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(size(u.x), size(u.y)), __hmax2_nan(size(u.z), size(u.w)));
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(&m);
+        return max(w << 16, w & 0xffff0000u);
+    }
+    __device__ __forceinline__ void get(Two (&f)[4], __nv_bfloat16) const {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = Two{__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)};
+    }
+};
 
 template <typename T>
-__global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_per_row, int64_t strips) {
+__global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_per_row, uint32_t strips) {
     const int lane = threadIdx.x & 15;
-    const int64_t q = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const uint32_t q = blockIdx.x * 16 + (threadIdx.x >> 4);
     const bool on = q < strips;                            // the warp's other half may still have work
-    const int64_t r = on ? q / strips_per_row : 0;
-    const int64_t blk = (on ? q - r * strips_per_row : 0) * kStrip, col = blk * kBlock + lane * 8;
+    const uint32_t r = on ? q / strips_per_row : 0;
+    const int blk = (int)(on ? q - r * strips_per_row : 0) * kStrip, col = blk * kBlock + lane * 8;
+    const int cols = (int)a.cols;
     const T *x = static_cast<const T *>(a.x.data) + a.x.at(r) + col;
     uint8_t *codes = static_cast<uint8_t *>(a.codes.data) + a.codes.at(r) + col;
     float *scales = static_cast<float *>(a.scales.data) + a.scales.at(r) + blk;
-    float f[kStrip][8];
+    Eight e[kStrip];
 #pragma unroll
     for (int i = 0; i < kStrip; ++i) {
-        if (on && col + i * kBlock < a.cols) load_eight(x + i * kBlock, f[i]);
-        else
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[i][k] = 0.f;
+        e[i].u = e[i].v = make_uint4(0u, 0u, 0u, 0u);
+        if (on && col + i * kBlock < cols) e[i].load(x + i * kBlock);
     }
 #pragma unroll
     for (int i = 0; i < kStrip; ++i) {
-        uint32_t amax = 0;
-        float all = 0.f;                                   // NaN if one of the lane's entries is not finite
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            amax = max(amax, __float_as_uint(f[i][k]) & 0x7fffffffu);
-            all = fmaf(f[i][k], 0.f, all);
-        }
-        if (all != all) {
+        uint32_t amax = e[i].most(T());
+        const bool odd = amax >= 0x7f800000u;              // an infinity or NaN among the lane's
+        Two f[4];
+        e[i].get(f, T());
+        if (odd) {
             amax = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) amax = max(amax, finite_bits(f[i][k]));
+            for (int k = 0; k < 4; ++k) amax = max(amax, max(finite_bits(f[k].x), finite_bits(f[k].y)));
         }
 #pragma unroll
         for (int s = 8; s >= 1; s >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, s));
         const int k = amax ? scale_exponent(amax) : 0;
-        const float inv = __uint_as_float((uint32_t)(127 - k) << 23);
-        if (on && col + i * kBlock < a.cols) {
-            uint32_t w[2];
+        const Two inv = both(__uint_as_float((uint32_t)(127 - k) << 23));
+        if (on && col + i * kBlock < cols) {
+            uint32_t w[4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float2 lo = make_float2(f[i][4 * h] * inv, f[i][4 * h + 1] * inv), hi = make_float2(f[i][4 * h + 2] * inv, f[i][4 * h + 3] * inv);
-                w[h] = __nv_cvt_float2_to_fp8x2(lo, __NV_SATFINITE, __NV_E4M3) | (uint32_t)__nv_cvt_float2_to_fp8x2(hi, __NV_SATFINITE, __NV_E4M3) << 16;
+            for (int h = 0; h < 4; ++h) {
+                const Two v = mul2(f[h], inv);
+                w[h] = __nv_cvt_float2_to_fp8x2(make_float2(v.x, v.y), __NV_SATFINITE, __NV_E4M3);
+                if (odd) {                                 // infinities saturate in the conversion; they are kept as NaN
+                    if (!(fabsf(f[h].x) < INFINITY)) w[h] |= 0x7fu;
+                    if (!(fabsf(f[h].y) < INFINITY)) w[h] |= 0x7f00u;
+                }
             }
-            if (all != all) {                              // infinities saturate in the conversion; they are kept as NaN
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    if (!(fabsf(f[i][c]) < INFINITY)) w[c / 4] |= 0x7fu << (8 * (c % 4));
-            }
-            *reinterpret_cast<uint2 *>(codes + i * kBlock) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2 *>(codes + i * kBlock) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
             if (lane == 0) scales[i] = __uint_as_float((uint32_t)(127 + k) << 23);
         }
     }
@@ -199,9 +217,9 @@ cudaError_t launch_pack(int type, const PackArgs &a, cudaStream_t s) {
     const int64_t per_row = (a.cols + kBlock - 1) / kBlock;
     const bool aligned = a.cols % 8 == 0 && aligned_to(a.x, a.m, a.n, type == ZENO_BF16 ? 2 : 4, 16) && aligned_to(a.codes, a.m, a.n, 1, 8);
     const int64_t strips_per_row = (per_row + kStrip - 1) / kStrip, strips = strips_per_row * a.m * a.n, grid = (strips + 15) / 16;
-    if (aligned && grid <= 0x7fffffff)
+    if (aligned && strips < (int64_t)1 << 31)
         return launch_chained(type == ZENO_BF16 ? pack_kernel<__nv_bfloat16> : pack_kernel<float>, dim3((unsigned)grid), dim3(256), 0, s, false, a,
-                              (uint32_t)strips_per_row, strips);
+                              (uint32_t)strips_per_row, (uint32_t)strips);
     const int64_t blocks = per_row * a.m * a.n;
     const unsigned any_grid = (unsigned)min((blocks + 7) / 8, (int64_t)148 * 8);
     return launch_chained(type == ZENO_BF16 ? pack_any_kernel<__nv_bfloat16> : pack_any_kernel<float>, dim3(any_grid), dim3(256), 0, s, false, a,

@@ -36,11 +36,14 @@ template <> struct Vec<float> {
     static __device__ __forceinline__ float most(uint4 v) {
         return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
     }
-    // entries, at least -kFar each (a NaN stays)
-    static __device__ __forceinline__ void entries(uint4 v, float (&o)[N]) {
+    // entries in pairs, at least -kFar each (a NaN stays)
+    static __device__ __forceinline__ void entries(uint4 v, Two (&o)[N / 2]) {
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+        float f[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %1, %2;" : "=f"(o[i]) : "f"(__uint_as_float(u[i])), "f"(-kFar));
+        for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %1, %2;" : "=f"(f[i]) : "f"(__uint_as_float(u[i])), "f"(-kFar));
+        o[0] = Two{f[0], f[1]};
+        o[1] = Two{f[2], f[3]};
     }
 };
 template <> struct Vec<__nv_bfloat16> {
@@ -51,15 +54,14 @@ template <> struct Vec<__nv_bfloat16> {
         const __nv_bfloat162 m = __hmax2(__hmax2(pair(v.x), pair(v.y)), __hmax2(pair(v.z), pair(v.w)));
         return fmaxf(__low2float(m), __high2float(m));
     }
-    static __device__ __forceinline__ void entries(uint4 v, float (&o)[N]) {
+    static __device__ __forceinline__ void entries(uint4 v, Two (&o)[N / 2]) {
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
         const __nv_bfloat162 low = __float2bfloat162_rn(-kFar);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const __nv_bfloat162 m = __hmax2_nan(pair(u[i]), low);
             const uint32_t w = *reinterpret_cast<const uint32_t *>(&m);
-            o[2 * i] = __uint_as_float(w << 16);
-            o[2 * i + 1] = __uint_as_float(w & 0xffff0000u);
+            o[i] = Two{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
         }
     }
 };
@@ -111,19 +113,6 @@ struct TopList {
     }
 };
 
-// the k-th largest of the lanes' values
-__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t v, int k, int lane) {
-#pragma unroll
-    for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-        for (int s = size >> 1; s >= 1; s >>= 1) {
-            const uint32_t w = __shfl_xor_sync(kAll, v, s);
-            const bool keep_max = ((lane & s) == 0) == ((lane & size) == 0);      // descending; the last merge has no set bit `size`
-            v = keep_max ? max(v, w) : min(v, w);
-        }
-    return __shfl_sync(kAll, v, k - 1);
-}
-
 // The row's sums by the definition, for a block: m (the largest entry, 0 for a row of minus infinities), sum exp(z - m) and the
 // sum of those times z - m.
 template <typename T, int THREADS>
@@ -149,19 +138,80 @@ __device__ __noinline__ void sums_by_definition(const T *z, int64_t vocab, float
     e = block_sum<THREADS>(e, scratch);
 }
 
-// A row goes to a block, or (few rows) to a cluster of `parts` blocks that join through distributed shared memory.  A warp takes 32
-// x kBatch vectors at a time, all loads ahead of their use.  The best `top` are kept per warp: a batch whose largest entry does
-// not reach the k-th best that any warp of the block has (nearly all of them, in rows that are in no order) costs one comparison.
-template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobArgs a, int parts) {
+// Places the better of `count` keys, which differ but for zeros (none), in their order: a key's place is the number of better ones.
+template <int THREADS>
+__device__ __forceinline__ void rank_keys(const unsigned long long *keys, int count, int top, unsigned long long *best) {
+    for (int i = threadIdx.x; i < count; i += THREADS) {
+        const unsigned long long k = keys[i];
+        int place = 0;
+        for (int c = 0; c < count; ++c) place += keys[c] > k;
+        if (k && place < top) best[place] = k;
+    }
+}
+
+// The best `top` of a stretch of vectors and the entries beside them, by lists that the warps keep: for rows in which too many
+// entries reach what is known to be needed (ties above all).
+template <typename T, int THREADS>
+__device__ __noinline__ void top_by_lists(const T *z, int64_t head, int64_t v_begin, int64_t v_end, int64_t rest, int64_t rest_at, int top, uint32_t need,
+                                          unsigned long long *keys, unsigned long long *best) {
     using V = Vec<T>;
-    constexpr int kWarps = THREADS / 32, kBatch = 32 / V::N, kMaxParts = 8;
+    constexpr int kWarps = THREADS / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    TopList list;
+    list.need = need;
+    for (int64_t base = v_begin + warp * 32; base < v_end; base += THREADS) {
+        uint32_t u = 0;
+        if (base + lane < v_end) u = order_of(V::most(reinterpret_cast<const uint4 *>(z + head)[base + lane]));
+        // four lanes' vectors at a time (or eight), an entry to a lane
+        constexpr int kSide = 32 / V::N;
+        unsigned todo = __ballot_sync(kAll, u >= list.need);
+        while (todo) {
+            int from = -1;
+            unsigned left = todo;
+#pragma unroll
+            for (int s = 0; s < kSide; ++s) {
+                const int f = __ffs(left) - 1;
+                left &= left - 1;
+                if (lane / V::N == s) from = f;
+            }
+            todo = left;
+            unsigned long long key = 0;
+            if (from >= 0) {
+                const int64_t j = head + (base + from) * V::N + lane % V::N;
+                if (base + from < v_end) key = rank_key(value_of(z + j), (int)j);
+            }
+            list.offer(key, top, lane);
+        }
+    }
+    if (warp == 0) {
+        const int64_t j = lane < head ? lane : rest_at + lane;
+        list.offer(lane < rest ? rank_key(value_of(z + j), (int)j) : 0, top, lane);
+    }
+    __syncthreads();
+    if (lane < top) keys[warp * top + lane] = list.mine;
+    __syncthreads();
+    rank_keys<THREADS>(keys, kWarps * top, top, best);
+}
+
+// A row goes to a block, or (few rows) to a cluster of `parts` blocks that join through distributed shared memory.  A warp takes 32
+// x kBatch vectors at a time, all loads ahead of their use.
+//
+// The alternatives cost the pass over the logits one comparison a batch: a thread keeps its largest entry.  The k-th largest of the
+// threads' largest is a bound that k entries reach, and only about k threads have entries that do; theirs are read again (from
+// L2), and what reaches the bound is ranked by counting.  The bound is taken to the upper 16 bits of the order.
+template <typename T, int THREADS, bool TOP>
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ? 8 : 24) logprobs_kernel(LogprobArgs a, int parts) {
+    using V = Vec<T>;
+    constexpr int kWarps = THREADS / 32, kBatch = 4, kMaxParts = 8, kKeys = 512;
+    static_assert(kKeys >= kWarps * kMaxTop && kKeys >= kMaxParts * kMaxTop, "the lists of all warps, of all parts");
     __shared__ float scratch[kWarps];
     __shared__ float warp_sums[kWarps][3];
     __shared__ float part_sums[4];
-    __shared__ unsigned long long keys[TOP ? (kWarps > kMaxParts ? kWarps : kMaxParts) * kMaxTop : 1];
+    __shared__ unsigned long long keys[TOP ? kKeys : 1];
     __shared__ unsigned long long best[TOP ? kMaxTop : 1];
-    __shared__ uint32_t block_need;
+    __shared__ uint32_t orders[TOP ? THREADS : 1];     // the threads' largest entries; then the threads to look at again
+    __shared__ uint32_t bound;
+    __shared__ int n_threads, n_keys;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t r = (int)(blockIdx.x / (unsigned)parts);
     const int part = (int)(blockIdx.x - (unsigned)r * (unsigned)parts);
@@ -175,84 +225,124 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobArgs a, int pa
         given = t >= 0 && t < a.vocab;
         if (given) zt = value_of(z + t);
     }
-    if (TOP && THREADS > 32) {
-        if (threadIdx.x == 0) block_need = 0;
-        __syncthreads();
-    }
     const int64_t head = head_of(z, a.vocab), vecs = (a.vocab - head) / V::N;
-    const int64_t v_end = vecs * (part + 1) / parts;
+    const int64_t v_begin = vecs * part / parts, v_end = vecs * (part + 1) / parts;
     const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
-    // Until an entry is above -kFar the reference is 0, where all others (kept at least -kFar) add nothing.
-    Sums q = {0.f, 0.f, 0.f};
-    float limit = -kFar;                              // the reference moves for entries beyond this
-    TopList list;
-    bool fresh = true;
+    // Until an entry is above -kFar the reference M is 0, where all others (kept at least -kFar) add nothing.
+    float limit = -kFar, largest = -INFINITY;          // the reference moves for entries beyond the limit
+    float M = 0.f;
+    Two s2 = both(0.f), e2 = both(0.f);
+    auto move = [&](float to) {
+        Sums p = {M, s2.x, e2.x}, q = {M, s2.y, e2.y};
+        p.move(to);
+        q.move(to);
+        s2 = Two{p.s, q.s};
+        e2 = Two{p.e, q.e};
+        M = to;
+    };
+    bool any = false;
 
-    for (int64_t base = vecs * part / parts + warp * 32 * kBatch; base < v_end; base += THREADS * kBatch) {
+    for (int64_t base = v_begin + warp * 32 * kBatch; base < v_end; base += THREADS * kBatch) {
         uint4 raw[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int64_t v = base + i * 32 + lane;
-            raw[i] = v < v_end ? __ldcs(zv + v) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
+            raw[i] = v < v_end ? __ldg(zv + v) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
+            any |= v < v_end;
         }
         float most = V::most(raw[0]);
 #pragma unroll
         for (int i = 1; i < kBatch; ++i) most = fmaxf(most, V::most(raw[i]));
+        if (TOP) largest = fmaxf(largest, most);
         if (most > limit) {
-            q.move(most * kLog2e);
+            move(most * kLog2e);
             limit = most + kSlack;
         }
-        // two chains of sums
-        Sums q1 = {q.M, 0.f, 0.f};
+        const Two c = both(kLog2e), m = both(-M);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            float f[V::N];
+            Two f[V::N / 2];
             V::entries(raw[i], f);
 #pragma unroll
-            for (int k = 0; k < V::N; k += 2) {
-                q.add(f[k]);
-                q1.add(f[k + 1]);
-            }
-        }
-        q.s += q1.s;
-        q.e += q1.e;
-        if (TOP) {
-            const uint32_t u = order_of(most);
-            if (THREADS > 32) list.need = max(list.need, *(volatile uint32_t *)&block_need);
-            if (fresh) list.need = max(list.need, kth_of_lanes(u, top, lane));    // as many lanes have an entry that is no less
-            fresh = false;
-            unsigned todo = __ballot_sync(kAll, u >= list.need);
-            if (todo) {
-                do {      // a lane's 32 entries (or as many as it has) in the warp's lanes
-                    const int from = __ffs(todo) - 1;
-                    todo &= todo - 1;
-                    const int64_t v = base + lane / V::N * 32 + from;
-                    const int64_t j = head + v * V::N + lane % V::N;
-                    unsigned long long key = 0;
-                    if (v < v_end) key = rank_key(value_of(z + j), (int)j);
-                    list.offer(key, top, lane);
-                } while (todo);
-                if (THREADS > 32 && lane == 0) atomicMax(&block_need, list.need);
+            for (int k = 0; k < V::N / 2; ++k) {
+                const Two t = fma2(f[k], c, m), p = {exp2_fast(t.x), exp2_fast(t.y)};
+                s2 = add2(s2, p);
+                e2 = fma2(p, t, e2);
             }
         }
     }
     // what lies before the first vector and behind the last: fewer than 2 N entries
-    const int64_t rest = a.vocab - vecs * V::N;
-    if (part == 0 && warp == 0) {
-        const bool valid = lane < rest;
-        const int64_t j = lane < head ? lane : vecs * V::N + lane;
-        const float v = valid ? value_of(z + j) : -INFINITY;
-        if (v > limit) {
-            q.move(v * kLog2e);
-            limit = v;
+    const int64_t rest = part == 0 ? a.vocab - vecs * V::N : 0, rest_at = vecs * V::N;
+    const int64_t rest_j = lane < head ? lane : rest_at + lane;
+    const bool has_rest = warp == 0 && lane < rest;
+    const float v_rest = has_rest ? value_of(z + rest_j) : -INFINITY;
+    if (has_rest) {
+        if (v_rest > limit) {
+            move(v_rest * kLog2e);
+            limit = v_rest;
         }
-        if (valid) q.add(v < -kFar ? -kFar : v);
-        if (TOP) list.offer(valid ? rank_key(v, (int)j) : 0, top, lane);
+        Sums p = {M, s2.x, e2.x};
+        p.add(v_rest < -kFar ? -kFar : v_rest);
+        s2.x = p.s;
+        e2.x = p.e;
+        any = true;
+    }
+    Sums q = {M, s2.x + s2.y, e2.x + e2.y};
+
+    if (TOP) {
+        // the bound: the largest multiple of 2^16 that the largest entries of `top` threads reach
+        orders[threadIdx.x] = any ? order_of(fmaxf(largest, v_rest)) : 0u;
+        __syncthreads();
+        if (warp == 0) {
+            uint32_t o[kWarps], at_least = 0;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) o[k] = orders[k * 32 + lane];
+            for (int bit = 31; bit >= 16; --bit) {
+                const uint32_t next = at_least | 1u << bit;
+                int n = 0;
+#pragma unroll
+                for (int k = 0; k < kWarps; ++k) n += o[k] >= next;
+                if ((int)__reduce_add_sync(kAll, (unsigned)n) >= top) at_least = next;
+            }
+            if (lane == 0) {
+                bound = at_least;
+                n_threads = n_keys = 0;
+            }
+        }
+        __syncthreads();
+        const uint32_t need = bound, own = orders[threadIdx.x];
+        __syncthreads();
+        if (own >= need && any) orders[atomicAdd(&n_threads, 1)] = threadIdx.x;
+        auto offer = [&](float v, int64_t j) {
+            if (order_of(v) < need) return;
+            const int at = atomicAdd(&n_keys, 1);
+            if (at < kKeys) keys[at] = rank_key(v, (int)j);
+        };
+        if (has_rest) offer(v_rest, rest_j);
+        __syncthreads();
+        const int threads = n_threads, per = (int)((v_end - v_begin + THREADS * kBatch - 1) / (THREADS * kBatch)) * kBatch;
+        const bool few = threads <= 2 * top + 32;
+        if (few)
+            for (int i = threadIdx.x; i < threads * per; i += THREADS) {
+                const int who = (int)orders[i / per], k = i % per;
+                const int64_t v = v_begin + (int64_t)(k / kBatch) * THREADS * kBatch + (who >> 5) * 32 * kBatch + k % kBatch * 32 + (who & 31);
+                if (v < v_end) {
+                    const int64_t j = head + v * V::N;
+                    T e[V::N];
+                    *reinterpret_cast<uint4 *>(e) = __ldg(zv + v);
+#pragma unroll
+                    for (int n = 0; n < V::N; ++n) offer(value_of(e + n), j + n);
+                }
+            }
+        __syncthreads();
+        if (few && n_keys <= kKeys) rank_keys<THREADS>(keys, n_keys, top, best);
+        else top_by_lists<T, THREADS>(z, head, v_begin, v_end, rest, rest_at, top, need, keys, best);
+        __syncthreads();
     }
 
     // the warp's sums, the block's, the cluster's
     if (limit == -kFar) q.M = kUnset;
-    float M = q.M;
+    M = q.M;
 #pragma unroll
     for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
     q.move(M);
@@ -264,7 +354,6 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobArgs a, int pa
             warp_sums[warp][1] = q.s;
             warp_sums[warp][2] = q.e;
         }
-        if (TOP && lane < top) keys[warp * top + lane] = list.mine;
         __syncthreads();
         if (warp == 0) {
             Sums w = {lane < kWarps ? warp_sums[lane][0] : kUnset, lane < kWarps ? warp_sums[lane][1] : 0.f,
@@ -274,20 +363,6 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobArgs a, int pa
             for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
             w.move(M);
             q = {M, warp_sum(w.s), warp_sum(w.e)};
-        }
-        if (TOP) {      // an entry's place is the number of better ones; keys differ
-            for (int i = threadIdx.x; i < kWarps * top; i += THREADS) {
-                const unsigned long long k = keys[i];
-                int place = 0;
-                for (int c = 0; c < kWarps * top; ++c) place += keys[c] > k;
-                if (k && place < top) best[place] = k;
-            }
-            if (parts > 1 && threadIdx.x == 0) {          // a short part may have fewer
-                int have = 0;
-                for (int c = 0; c < kWarps * top; ++c) have += keys[c] != 0;
-                for (; have < top; ++have) best[have] = 0;
-            }
-            __syncthreads();
         }
     }
     if (parts > 1) {
@@ -314,12 +389,7 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobArgs a, int pa
             if (TOP) {
                 for (int i = threadIdx.x; i < parts * top; i += THREADS) keys[i] = cluster_load64(cluster_addr(&best[i % top], i / top));
                 __syncthreads();
-                for (int i = threadIdx.x; i < parts * top; i += THREADS) {
-                    const unsigned long long k = keys[i];
-                    int place = 0;
-                    for (int c = 0; c < parts * top; ++c) place += keys[c] > k;
-                    if (k && place < top) best[place] = k;
-                }
+                rank_keys<THREADS>(keys, parts * top, top, best);
             }
         }
         cluster_barrier();
@@ -359,7 +429,7 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobArgs a, int pa
         if (a.logprobs) a.logprobs[r] = given ? log_prob(zt) : 0.f;
     }
     if (TOP && (int)threadIdx.x < top) {
-        const unsigned long long key = THREADS > 32 ? best[threadIdx.x] : list.mine;
+        const unsigned long long key = best[threadIdx.x];
         if (a.top_idx) a.top_idx[r * top + threadIdx.x] = (int)(0xffffffffu - (uint32_t)key);
         if (a.top_logprobs) a.top_logprobs[r * top + threadIdx.x] = log_prob(value_of_order((uint32_t)(key >> 32)));
     }

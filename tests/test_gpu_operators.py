@@ -150,6 +150,35 @@ def test_layer_norm_gradient_layouts_and_optional_outputs(layout, saved):
         assert out is dy and torch.equal(dy, dx) and torch.equal(only, dw)
 
 
+# enough rows for the kernels that keep a group's weights over many of them: a row's threads from a warp to all of a block, groups that
+# the blocks share unevenly
+MANY = [(1, 4900, 40), (2, 2501, 264), (9, 555, 1000), (300, 17, 72), (3, 1700, 2048), (2, 2400, 2056), (1, 4800, 4096), (1, 4737, 8192)]
+
+
+@pytest.mark.parametrize("m,n,cols", MANY)
+@pytest.mark.parametrize("act,par", TYPES)
+def test_layer_norm_of_many_rows(m, n, cols, act, par):
+    g = _gen(cols)
+    for layout, models in (("dense", False), ("aligned", True), ("padded", False)):
+        x = _rows(g, m, n, cols, act, layout, 2.0, 0.5)
+        if layout == "dense":
+            x[0, n // 2] = 3.0
+            x[-1, -1, 0] = NAN
+        w, b = (torch.randn((m, cols) if models else (cols,), generator=g, device="cuda").to(par) for _ in range(2))
+        got = zeno.layer_norm(x, w, b, eps=1e-5)
+        want = R.norm(x, w, b, float(np.float32(1e-5)))
+        for k, what in enumerate(("y", "mean", "rstd")):
+            R.assert_near(got[k], want[k], want[k + 3].nan_to_num(0.0), (what, layout))
+        bare, _, _ = zeno.layer_norm(x, w, eps=1e-5, want_stats=False, out=x if layout == "aligned" else None)
+        zero = R.norm(x, w, torch.zeros_like(b), float(np.float32(1e-5))) if layout != "aligned" else None
+        if zero is not None:
+            R.assert_near(bare, zero[0], zero[3].nan_to_num(0.0), "without bias")
+        else:
+            assert torch.isfinite(x).all()
+    _norm_gradient_case(m, n, cols, act, par, "aligned", False, cols, models=True)
+    _norm_gradient_case(m, n, cols, act, par, "dense", True, cols + 1)
+
+
 def test_layer_norm_gradient_against_differences():
     g = _gen(17)
     m, n, cols = 2, 3, 40
@@ -320,6 +349,25 @@ def test_token_logprobs_of_hard_rows(vocab, act, rows):
         one = zeno.token_logprobs(z[r:r + 1], t[r:r + 1], top=top)
         assert torch.equal(one.top_idx, got.top_idx[r:r + 1])
         R.assert_near(one.lse, want[2][r:r + 1], want[7][r:r + 1], "one")
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab", [(300, 1500), (300, 9000), (200, 40003), (3, 70000)])
+def test_token_logprobs_alternatives_among_ties(act, rows, vocab):
+    """Few values, so that far more entries reach the last alternative than there are alternatives; blocks of equal entries; rows whose
+    best entries lie side by side or all with one thread."""
+    g = _gen(vocab)
+    z = torch.randint(0, 4, (rows, vocab), generator=g, device="cuda").float()
+    z[1::5] = torch.randint(0, 500, (rows, vocab), generator=g, device="cuda")[1::5] * 0.25
+    z[2::5] = 0.0
+    z[3::5, vocab // 3: vocab // 3 + 60] = 9.0
+    z[4::5, 5::2048] = 11.0
+    z[4::5, 6::2048] = torch.arange(z[0, 6::2048].numel(), device="cuda") + 12.0
+    z = z.to(act)
+    for top in (1, 3, 32):
+        got = zeno.token_logprobs(z, top=top)
+        want = torch.sort(z, dim=-1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(got.top_idx.long(), want)
 
 
 def test_token_logprobs_of_full_lists():
