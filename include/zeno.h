@@ -368,11 +368,18 @@ zeno_status zeno_pack_activations(int32_t device, int32_t type, const zeno_rows 
  * zeno_pack_activations kept it:  dw[i][o][k] = sum over group i's rows of dy_o x_k,  db[i][o] = sum of dy_o.
  * dw: per group outputs x inputs entries, row-major, ldw elements after the previous group's; db (or NULL) likewise with ldb:
  * slices of V in the layout of the parameter vector.  The products are exact and summed in binary32.
- * Aligned bfloat16 dy (rows and groups of multiples of 16 bytes) goes to the tensor cores. */
+ * The scales have to be powers of two, as zeno_pack_activations writes them.  bfloat16 dy in rows and groups of multiples of
+ * 16 bytes (codes likewise), one group behind the other, goes to the tensor cores. */
 int64_t zeno_dense_gradient_workspace(int32_t m, int64_t n, int64_t inputs, int64_t outputs);
 zeno_status zeno_dense_gradient(int32_t device, int32_t type, int32_t param_type, const zeno_rows *dy, const zeno_rows *codes,
                                 const zeno_rows *scales, int32_t m, int64_t n, int64_t inputs, int64_t outputs, void *dw,
                                 int64_t ldw, void *db, int64_t ldb, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Synchronises `stream` and reports whether a kernel of these calls on `device` gave up on a bounded device-side wait since the
+ * last such report (its outputs are then undefined): ZENO_ERR_TIMEOUT if so, else ZENO_OK.
+ * zeno_debug_set_operator_wait_limit: test hook, as zeno_debug_set_wait_limit, for later calls of this process (default 2^22). */
+zeno_status zeno_operator_status(int32_t device, void *stream);
+zeno_status zeno_debug_set_operator_wait_limit(uint32_t polls);
 
 /* Log probabilities of given tokens.  For every row z of vocab logits:
  *   lse = log sum_j exp(z_j),  logprob = z_target - lse,  entropy = -sum_j p_j log p_j with p_j = exp(z_j - lse),

@@ -1,0 +1,457 @@
+// A dense layer's weight gradient dW = dY^T X for every group on the tensor cores, X kept in 8 bits.
+//
+// A pair of blocks (a cluster of two SMs) takes a tile of 256 outputs by 256 inputs.  dY and X lie token by token, so both operands are read with
+// the token as the contraction index and the output or input index contiguous ("MN-major"), in the 128-byte swizzled layout that
+// the tensor copies write.  Each block holds 128 of the outputs' rows of dY^T and 128 of the inputs of X, and the pair's instruction
+// (cta_group::2, M = 256, N = 256) reads both halves: a code is turned into bfloat16 once for 256 outputs.  code * scale is
+// exact in bfloat16, products of bfloat16 are exact, and the sums stay binary32 in TMEM.
+//   warp 0: copies of the codes;  warp 2: copies of dY;  warp 1 of the pair's first block: the instructions;
+//   warps 4 - 11: codes to bfloat16;  warps 12 - 15: a finished tile from TMEM to dW while the next one is summed.
+#include "zeno_saved.cuh"
+#include "zeno_tc.cuh"
+
+namespace zeno {
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kTokens = 64;                   // tokens (the contraction index) of a stage
+constexpr int kHalf = 128;                    // outputs, and inputs, of a block
+constexpr int kPairTile = 2 * kHalf;
+constexpr int kSubBytes = kTokens * 128;      // 64 tokens of 64 bfloat16 (or 128 codes) in 128-byte rows
+constexpr int kABytes = 2 * kSubBytes, kBBytes = 2 * kSubBytes, kCodeBytes = kSubBytes;
+constexpr int kStages = 5, kCodeStages = 6;
+constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * kCodeBytes + 1024;
+constexpr int kConvWarps = 8, kEpiWarps = 4;
+constexpr int kTmemCols = 512;                // two sets of 256 sums
+constexpr int kKernelId = 5;
+
+__device__ int g_status;                      // raised by a block whose bounded wait gave up, cleared by who reads it
+
+struct DenseTcArgs {
+    DenseGradArgs d;
+    int out_tiles, in_tiles, shared_dy, shared_codes;
+    int64_t items;
+    int vector_stores;
+    uint32_t spin_limit;
+};
+
+// ---- waits for what the other block of the pair signals
+
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+    if (mbar_try_wait_cluster(bar, parity)) return true;
+    if (!mbar_wait_poll(bar, parity, abort_flag)) return false;
+    return mbar_try_wait_cluster(bar, parity);          // the phase has ended: once more, for what it orders
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+// the pair's commit: an arrival on the barrier at this place in both blocks
+__device__ __forceinline__ void pair_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// MN-major operand in the 128-byte swizzled layout: rows of 64 contiguous entries, one for each value of the contraction index;
+// eight of them, 1024 bytes, make a group (stride-dimension offset); the next 64 entries lie kSubBytes on (leading-dimension offset).
+__device__ __forceinline__ uint64_t mn_desc(uint32_t addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((addr & 0x3ffffu) >> 4);
+    d |= (uint64_t)(kSubBytes >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+// Two codes (in the upper byte of each half) times 2^120 and the scale.  The sign keeps its place, exponent and mantissa move to where
+// bfloat16 has them; its exponent counts from 127, that of the code from 7, and both steps to the code's value times its scale
+// are exact.
+__device__ __forceinline__ uint32_t two_values(uint32_t high_bytes, __nv_bfloat162 up, __nv_bfloat162 scale) {
+    const uint32_t bits = (high_bytes & 0x80008000u) | ((high_bytes >> 4) & 0x07f007f0u);
+    const __nv_bfloat162 v = __hmul2(__hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&bits), up), scale);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+// 16 codes to two vectors of eight bfloat16
+__device__ __forceinline__ void sixteen_values(uint4 codes, float scale, uint4 (&out)[2]) {
+    const __nv_bfloat162 up = __float2bfloat162_rn(__uint_as_float((127u + 120u) << 23)), s = __float2bfloat162_rn(scale);
+    const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w};
+    uint32_t o[8];
+    uint32_t nan = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        nan |= (c[i] & 0x7f7f7f7fu) + 0x01010101u;                            // a byte's top bit: all seven bits were set, NaN
+        o[2 * i] = two_values(__byte_perm(c[i], 0u, 0x1404), up, s);
+        o[2 * i + 1] = two_values(__byte_perm(c[i], 0u, 0x3424), up, s);
+    }
+    if (nan & 0x80808080u) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (((c[i / 4] >> (8 * (i % 4))) & 0x7fu) == 0x7fu) o[i / 2] |= 0x7fffu << (16 * (i % 2));
+    }
+    out[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    out[1] = make_uint4(o[4], o[5], o[6], o[7]);
+}
+
+template <typename P>
+__global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes,
+                                                               DenseTcArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    // cfull, cempty [kCodeStages]; afull, abempty, bready [kStages]; dfull, dempty [2]
+    constexpr int kBars = 2 * kCodeStages + 3 * kStages + 4;
+    __shared__ __align__(8) uint64_t bars[kBars];
+    __shared__ __align__(8) uint64_t drain_bar, never_bar;
+    __shared__ uint32_t tmem_base_slot;
+    __shared__ int abort_state[kAbortWords];
+    __shared__ int issued[kCodeStages + kStages];            // last round a copy was issued into a stage, plus one
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = (int)cluster_rank();
+    uint8_t *a_ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *b_ring = a_ring + kStages * kABytes, *code_ring = b_ring + kStages * kBBytes;
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    auto cfull = [&](int s) { return bar(s); };
+    auto cempty = [&](int s) { return bar(kCodeStages + s); };
+    auto afull = [&](int s) { return bar(2 * kCodeStages + s); };
+    auto abempty = [&](int s) { return bar(2 * kCodeStages + kStages + s); };
+    auto bready = [&](int s) { return bar(2 * kCodeStages + 2 * kStages + s); };
+    auto dfull = [&](int q) { return bar(2 * kCodeStages + 3 * kStages + q); };
+    auto dempty = [&](int q) { return bar(2 * kCodeStages + 3 * kStages + 2 + q); };
+    const int64_t n = a.d.n;
+    const int nkb = (int)((n + kTokens - 1) / kTokens);
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    // item li of this pair -> (group, output tile, input tile); neighbouring pairs share dY's tile in L2
+    auto get_item = [&](int li, int &group, int &ot, int &it) {
+        const int64_t item = pair + (int64_t)li * pairs;
+        group = (int)(item / ((int64_t)a.out_tiles * a.in_tiles));
+        const int in_group = (int)(item - (int64_t)group * a.out_tiles * a.in_tiles);
+        ot = in_group / a.in_tiles;
+        it = in_group - ot * a.in_tiles;
+        return item < a.items;
+    };
+
+    if (tid == 0) {
+        abort_state[0] = 0;
+        abort_state[1] = (int)a.spin_limit;
+        for (int s = 0; s < kCodeStages; ++s) {
+            mbar_init(cfull(s), 1);
+            mbar_init(cempty(s), kConvWarps);
+        }
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(afull(s), 1);
+            mbar_init(abempty(s), 1);
+            mbar_init(bready(s), 2 * kConvWarps);
+        }
+        for (int q = 0; q < 2; ++q) {
+            mbar_init(dfull(q), 1);
+            mbar_init(dempty(q), 2 * kEpiWarps);
+        }
+        for (int s = 0; s < kCodeStages + kStages; ++s) issued[s] = 0;
+        mbar_init(smem_u32(&drain_bar), 1);
+        mbar_init(smem_u32(&never_bar), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();                        // the other block's barriers are there
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_slot;
+    volatile int *abortp = &abort_state[0];
+    int group, ot, it;
+
+    if (warp == 0) wait_for_nothing(smem_u32(&never_bar), abortp);
+    if (warp == 0 || warp == 2) {
+        // ------------------------------------------------------------------ copies: codes (warp 0), dY (warp 2)
+        const bool is_codes = warp == 0;
+        const int stages = is_codes ? kCodeStages : kStages;
+        int s = 0;
+        uint32_t round = 0;
+        bool ok = true;
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li)
+            for (int kb = 0; kb < nkb; ++kb) {
+                ok = __all_sync(0xffffffffu, mbar_wait(is_codes ? cempty(s) : abempty(s), (round & 1) ^ 1, abortp));
+                if (!ok) break;
+                if (elect_one()) {
+                    if (is_codes) {
+                        mbar_expect_tx(cfull(s), kCodeBytes);
+                        issued[s] = (int)round + 1;
+                        tma_load_3d(smem_u32(code_ring + s * kCodeBytes), &map_codes, it * kPairTile + rank * kHalf, kb * kTokens, a.shared_codes ? 0 : group, cfull(s));
+                    } else {
+                        mbar_expect_tx(afull(s), kABytes);
+                        issued[kCodeStages + s] = (int)round + 1;
+#pragma unroll 1
+                        for (int h = 0; h < 2; ++h)
+                            tma_load_3d(smem_u32(a_ring + s * kABytes + h * kSubBytes), &map_dy, ot * kPairTile + rank * kHalf + h * 64, kb * kTokens,
+                                        a.shared_dy ? 0 : group, afull(s));
+                    }
+                }
+                __syncwarp();
+                if (++s == stages) {
+                    s = 0;
+                    ++round;
+                }
+            }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ instructions, by the first block for both
+        // descriptor: sums binary32, operands bfloat16, both MN-major
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(kPairTile >> 3) << 17) | ((uint32_t)(kPairTile >> 4) << 24);
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = rank == 0;
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
+            const int set = li & 1;
+            ok = __all_sync(0xffffffffu, mbar_wait_cluster(dempty(set), ((uint32_t)(li >> 1) & 1) ^ 1, abortp));
+            if (!ok) break;
+            tc_fence_after();
+            for (int kb = 0; kb < nkb; ++kb) {
+                ok = mbar_wait_cluster(bready(s), ph, abortp) && mbar_wait(afull(s), ph, abortp);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t ab = smem_u32(a_ring + s * kABytes), bb = smem_u32(b_ring + s * kBBytes);
+#pragma unroll
+                    for (int k = 0; k < kTokens / 16; ++k)        // 16 tokens: two groups of eight rows
+                        pair_mma(tmem + set * 256, mn_desc(ab + k * 2048), mn_desc(bb + k * 2048), idesc, (uint32_t)(kb | k));
+                    pair_commit(abempty(s));
+                    if (kb + 1 == nkb) pair_commit(dfull(set));
+                }
+                __syncwarp();
+                if (++s == kStages) {
+                    s = 0;
+                    ph ^= 1;
+                }
+            }
+        }
+    } else if (warp >= 4 && warp < 4 + kConvWarps) {
+        // ------------------------------------------------------------------ codes to bfloat16
+        // Eight lanes take a pair of rows (even and odd token), four of the eight 16-code groups of each, the other four in the other half
+        // (`flip`): their 16-byte accesses then meet all banks once, reading and writing, in the swizzled layouts of both.
+        const int w = warp - 4, l = lane & 7, flip = (lane >> 3) & 1, odd = l >> 2;
+        const int g = (l & 3) + 4 * (odd ^ flip);
+        const uint32_t remote_bready = rank == 0 ? 0u : cluster_addr(&bars[2 * kCodeStages + 2 * kStages], 0);
+        int s = 0, sc = 0;
+        uint32_t ph = 0, phc = 0;
+        bool ok = true;
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
+            const int64_t block = (int64_t)it * 2 + rank;                   // of 128 columns
+            const bool in_range = block * kHalf < a.d.inputs;
+            const float *scales = static_cast<const float *>(a.d.scales.data) + group * a.d.scales.group + block;
+            auto token = [&](int kb, int j) { return (int64_t)kb * kTokens + 2 * (j * 16 + w * 2 + (lane >> 4)) + odd; };
+            float next[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) next[j] = in_range && token(0, j) < n ? __ldg(scales + token(0, j) * a.d.scales.row) : 0.f;
+            for (int kb = 0; kb < nkb; ++kb) {
+                float scale[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    scale[j] = next[j];
+                    next[j] = in_range && token(kb + 1, j) < n ? __ldg(scales + token(kb + 1, j) * a.d.scales.row) : 0.f;
+                }
+                ok = mbar_wait(cfull(sc), phc, abortp) && mbar_wait(abempty(s), ph ^ 1, abortp);
+                // the second block vouches for its part of dY with its part of X
+                if (ok && rank != 0) ok = mbar_wait(afull(s), ph, abortp);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint8_t *codes = code_ring + sc * kCodeBytes;
+                uint8_t *to = b_ring + s * kBBytes + (g >> 2) * kSubBytes;
+                uint4 c[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int row = 2 * (j * 16 + w * 2 + (lane >> 4)) + odd;
+                    c[j] = *reinterpret_cast<const uint4 *>(codes + row * 128 + ((g ^ (row & 7)) << 4));
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int row = 2 * (j * 16 + w * 2 + (lane >> 4)) + odd;
+                    uint4 v[2];
+                    sixteen_values(c[j], scale[j], v);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4 *>(to + row * 128 + (((2 * (g & 3) + h) ^ (row & 7)) << 4)) = v[h];
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(cempty(sc));
+                    if (rank == 0) mbar_arrive(bready(s));
+                    else mbar_arrive_cluster(remote_bready + s * 8);
+                }
+                if (++s == kStages) {
+                    s = 0;
+                    ph ^= 1;
+                }
+                if (++sc == kCodeStages) {
+                    sc = 0;
+                    phc ^= 1;
+                }
+            }
+        }
+    } else if (warp >= 12) {
+        // ------------------------------------------------------------------ finished tiles to dW
+        const int quad = warp & 3;                                 // TMEM lanes this warp may access
+        const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[2 * kCodeStages + 3 * kStages + 2], 0);
+        for (int li = 0; __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
+            const int set = li & 1;
+            if (!__all_sync(0xffffffffu, mbar_wait(dfull(set), (uint32_t)(li >> 1) & 1, abortp))) break;
+            tc_fence_after();
+            const int64_t o = (int64_t)ot * kPairTile + rank * kHalf + quad * 32 + lane, k0 = (int64_t)it * kPairTile;
+            P *dw = static_cast<P *>(a.d.dw) + group * a.d.ldw + o * a.d.inputs + k0;
+            const bool mine = o < a.d.outputs;
+            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + set * 256;
+#pragma unroll 1
+            for (int c0 = 0; c0 < kPairTile; c0 += 32) {
+                uint32_t v[2][16];
+                __syncwarp();
+                tc_ld16(from + c0, v[0]);
+                tc_ld16(from + c0 + 16, v[1]);
+                tc_wait_ld();
+                if (c0 + 32 == kPairTile) {                         // the sums are in registers: the set may be overwritten
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (rank == 0) mbar_arrive(dempty(set));
+                        else mbar_arrive_cluster(remote_dempty + set * 8);
+                    }
+                }
+                if (!mine) continue;
+                if (a.vector_stores) {
+                    constexpr int kPer = 16 / sizeof(P);
+#pragma unroll
+                    for (int q = 0; q < 32 / kPer; ++q) {
+                        alignas(16) P e[kPer];
+#pragma unroll
+                        for (int k = 0; k < kPer; ++k) put(e + k, __uint_as_float(v[(q * kPer + k) / 16][(q * kPer + k) % 16]));
+                        if (k0 + c0 + q * kPer < a.d.inputs) *reinterpret_cast<uint4 *>(dw + c0 + q * kPer) = *reinterpret_cast<const uint4 *>(e);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (k0 + c0 + k < a.d.inputs) put(dw + c0 + k, __uint_as_float(v[k / 16][k % 16]));
+                }
+            }
+        }
+    }
+
+    // ---------------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1 && rank == 0 && abort_state[0]) {                 // instructions may still be running
+        if (elect_one()) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&drain_bar)) : "memory");
+        __syncwarp();
+        for (uint32_t i = 0; i < kSpinLimit; ++i) {
+            if (mbar_try_wait(smem_u32(&drain_bar), 0)) break;
+            __nanosleep(64);
+        }
+        __syncwarp();
+    }
+    if (tid == 0 && abort_state[0]) {
+        // copies still in flight must land before the block exits
+        for (int s = 0; s < kCodeStages + kStages; ++s)
+            if (issued[s] > 0) {
+                const uint32_t b = s < kCodeStages ? cfull(s) : afull(s - kCodeStages);
+                for (uint32_t i = 0; i < kSpinLimit; ++i) {
+                    if (mbar_try_wait(b, (uint32_t)(issued[s] - 1) & 1)) break;
+                    __nanosleep(64);
+                }
+            }
+        atomicCAS(&g_status, 0, wait_code(kKernelId, abort_state[0], smem_u32(bars)));
+    }
+    __syncthreads();
+    cluster_barrier();                        // the other block's instructions, arrivals and reads have ended too
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+uint32_t spin_limit = kSpinLimit;
+
+bool encode(CUtensorMap *map, CUtensorMapDataType type, const Rows &v, int elem, int m, int64_t n, int64_t cols, int box_cols) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return false;
+    const bool shared = m > 1 && v.group == 0;
+    const cuuint64_t row = (cuuint64_t)(n > 1 ? v.row : (cols * elem + 15) / 16 * 16 / elem) * elem;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)n, (cuuint64_t)(shared ? 1 : m)};
+    const cuuint64_t strides[2] = {row, m > 1 && !shared ? (cuuint64_t)v.group * elem : row * (cuuint64_t)n};
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)kTokens, 1}, ones[3] = {1, 1, 1};
+    return enc(map, type, 3, v.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// groups behind one another (or one for all), rows that a tensor map can step through
+bool mappable(const Rows &v, int elem, int m, int64_t n, int64_t cols) {
+    const int64_t limit = (int64_t)1 << 39;
+    if (!aligned_to(v, m, n, elem, 16)) return false;
+    if (n > 1 && v.row * elem >= limit) return false;
+    return m <= 1 || v.group == 0 || (v.group >= (n > 1 ? n * v.row : cols) && v.group * elem < limit);
+}
+
+}  // namespace
+
+bool dense_tc_usable(const DenseGradArgs &a) {
+    return a.n > 0 && mappable(a.dy, 2, a.m, a.n, a.outputs) && mappable(a.codes, 1, a.m, a.n, a.inputs) && a.n < ((int64_t)1 << 31) - kTokens;
+}
+
+cudaError_t launch_dense_tc(int param_type, const DenseGradArgs &d, cudaStream_t s) {
+    CUtensorMap map_dy, map_codes;
+    if (!encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d.dy, 2, d.m, d.n, d.outputs, 64) ||
+        !encode(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, d.codes, 1, d.m, d.n, d.inputs, 128))
+        return cudaErrorNotSupported;
+    DenseTcArgs a;
+    a.d = d;
+    a.out_tiles = (int)((d.outputs + kPairTile - 1) / kPairTile);
+    a.in_tiles = (int)((d.inputs + kPairTile - 1) / kPairTile);
+    a.shared_dy = d.m > 1 && d.dy.group == 0;
+    a.shared_codes = d.m > 1 && d.codes.group == 0;
+    a.items = (int64_t)d.m * a.out_tiles * a.in_tiles;
+    const size_t elem = param_type == ZENO_BF16 ? 2 : 4;
+    a.vector_stores = reinterpret_cast<uintptr_t>(d.dw) % 16 == 0 && d.inputs * elem % 16 == 0 && (d.m <= 1 || d.ldw * elem % 16 == 0);
+    a.spin_limit = spin_limit;
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return e;
+    auto *kernel = param_type == ZENO_BF16 ? dense_tc_kernel<__nv_bfloat16> : dense_tc_kernel<float>;
+    static PerDeviceOnce attr_set[2];
+    if (attr_set[param_type == ZENO_BF16].need(device)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        attr_set[param_type == ZENO_BF16].mark(device);
+    }
+    // equal shares: the fewest pairs that make as many rounds as all would
+    const int64_t most = sms / 2, rounds = (a.items + most - 1) / most, pairs = (a.items + rounds - 1) / rounds;
+    return launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), kSmem, s, false, map_dy, map_codes, a);
+}
+
+void set_operator_wait_limit(uint32_t polls) { spin_limit = polls; }
+
+// reads and clears what a block that gave up left
+cudaError_t read_operator_status(cudaStream_t s, int *status) {
+    void *at = nullptr;
+    cudaError_t e = cudaGetSymbolAddress(&at, g_status);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(status, at, sizeof(int), cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess && *status) {
+        e = cudaMemsetAsync(at, 0, sizeof(int), s);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    }
+    return e;
+}
+
+}  // namespace zeno

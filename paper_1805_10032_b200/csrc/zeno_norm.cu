@@ -4,8 +4,6 @@
 // the registers of the 32 to 1024 threads that share it, between the sum, the centred squares and the result.  Backward: a
 // thread owns columns, not rows: it goes down a stretch of a group's rows with the sums of its columns' weight gradients in
 // registers, and copies of the rows ahead are in flight while a row's two averages are formed across the block.
-#include <stdlib.h>
-
 #include "zeno_operators.h"
 #include "zeno_saved.cuh"
 
@@ -482,101 +480,129 @@ __global__ void __launch_bounds__(TPR) norm_entries_kernel(NormGradArgs a, float
     }
 }
 
-// Forward, many rows of whole vectors: the blocks, rows and rings of the backward pass, with a group's weights in registers.  (Taking
-// the weights from L2 for every row, as norm_row_kernel does, costs as much of its bandwidth as the rows themselves.)
-template <typename T, typename P, int TPR, int ROWS, int STAGES>
-__global__ void __launch_bounds__(TPR *ROWS, TPR *ROWS <= 256 ? 3 : 1) norm_stream_kernel(NormArgs a) {
-    constexpr int N = 16 / sizeof(T), H = N / 2, kWarps = TPR / 32, kThreadsHere = TPR * ROWS;
-    extern __shared__ __align__(16) uint8_t ring[];            // [STAGES][NV][threads] vectors of x
-    __shared__ __align__(16) float scratch[2][ROWS][kWarps];
-    const int tid = threadIdx.x, sub = tid / TPR, t = tid % TPR;
-    const int cols = (int)a.cols, chunks = gridDim.x, i = blockIdx.y;
-    const int64_t first = a.n * blockIdx.x / chunks + sub, last = a.n * (blockIdx.x + 1) / chunks;
+// Forward, many rows of up to 1024 vectors: TPR threads take R rows at a time, NV vectors of each in a thread's registers, with a group's
+// weights in shared memory for all rows of the block.  (Taken from L2 for every row, as norm_row_kernel does, they cost as much of its
+// bandwidth as the rows.)  Up to a warp's threads a row meets no barrier; two or four warps have one of their own.  A vector's
+// register takes the next rows' vector as soon as its result is stored.
+constexpr int kGroupThreads = 256;
+template <typename T, typename P, int TPR, int NV, int R>
+__global__ void __launch_bounds__(kGroupThreads, 2) norm_group_kernel(NormArgs a) {
+    constexpr int N = 16 / sizeof(T), H = N / 2, kSide = kGroupThreads / TPR;        // rows side by side
+    extern __shared__ __align__(16) float weights_at[];        // w, then b
+    __shared__ float scratch[2][kGroupThreads / 32][R];
+    const int t = threadIdx.x % TPR, side = threadIdx.x / TPR, cols = (int)a.cols, packs = cols / N, chunks = gridDim.x, i = blockIdx.y;
+    const int64_t last = a.n * (blockIdx.x + 1) / chunks;
+    int64_t row = a.n * blockIdx.x / chunks + side * R;
     const T *x = static_cast<const T *>(a.x.data) + i * a.x.group;
     T *y = static_cast<T *>(a.y.data) + i * a.y.group;
-    int at[kNV];
-    bool mine[kNV];
-    Two w[kNV][H], b[kNV][H];
-    auto slot = [&](int stage, int v) { return (stage * kNV + v) * kThreadsHere + tid; };
-    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-    auto fetch = [&](int stage, int64_t row) {
-        if (row < last)
-#pragma unroll
-            for (int v = 0; v < kNV; ++v)
-                if (mine[v]) cp_async<16>(ring_at + slot(stage, v) * 16, x + row * a.x.row + at[v]);
-        cp_async_commit();
+    uint4 raw[R][NV];
+    auto fetch = [&](int q, int v, int64_t r) {
+        const int at = v * TPR + t;
+        raw[q][v] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < last && at < packs) raw[q][v] = reinterpret_cast<const uint4 *>(x + r * a.x.row)[at];
     };
 #pragma unroll
-    for (int v = 0; v < kNV; ++v) {
-        at[v] = (v * TPR + t) * N;
-        mine[v] = at[v] < cols;
+    for (int q = 0; q < R; ++q)
+#pragma unroll
+        for (int v = 0; v < NV; ++v) fetch(q, v, row + q);
+    // four weights of a thread beside the next one's, so that a warp's loads of 16 bytes meet all banks
+    float *biases_at = weights_at + NV * TPR * N;
+    for (int j = threadIdx.x; j < cols; j += kGroupThreads) {
+        const int at = j / N, to = ((at / TPR * (N / 4) + j % N / 4) * TPR + at % TPR) * 4 + j % 4;
+        weights_at[to] = value_of(static_cast<const P *>(a.w) + i * a.ldw + j);
+        biases_at[to] = a.b ? value_of(static_cast<const P *>(a.b) + i * a.ldw + j) : 0.f;
     }
+    __syncthreads();
+    // the rows' averages in all of their threads
+    auto averages = [&](float (&s)[R], int which) {
 #pragma unroll
-    for (int q = 0; q < STAGES - 1; ++q) fetch(q, first + q * ROWS);
+        for (int q = 0; q < R; ++q)
 #pragma unroll
-    for (int v = 0; v < kNV; ++v)
+            for (int d = (TPR < 32 ? TPR : 32) / 2; d >= 1; d >>= 1) s[q] += __shfl_xor_sync(0xffffffffu, s[q], d);
+        if constexpr (TPR > 32) {
+            const int warp = threadIdx.x >> 5;
+            if ((t & 31) == 0)
 #pragma unroll
-        for (int k = 0; k < H; ++k) {
-            const int64_t from = i * a.ldw + at[v] + 2 * k;
-            const P *wp = static_cast<const P *>(a.w) + from, *bp = static_cast<const P *>(a.b) + from;
-            w[v][k] = mine[v] ? Two{value_of(wp), value_of(wp + 1)} : both(0.f);
-            b[v][k] = mine[v] && a.b ? Two{value_of(bp), value_of(bp + 1)} : both(0.f);
-        }
-    // the row's sum in all of its threads; `which` of two scratches in turn
-    auto row_total = [&](float v, int which) {
-        v = warp_sum(v);
-        if constexpr (kWarps > 1) {
-            if ((t & 31) == 0) scratch[which][sub][t >> 5] = v;
-            __syncthreads();
-            v = 0.f;
+                for (int q = 0; q < R; ++q) scratch[which][warp][q] = s[q];
+            asm volatile("bar.sync %0, %1;" ::"r"(side + 1), "n"(TPR) : "memory");
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) v += scratch[which][sub][k];
-        }
-        return v;
-    };
-    int stage = 0;
-    for (int64_t row = first; row - sub < last; row += ROWS) {
-        fetch(stage == 0 ? STAGES - 1 : stage - 1, row + (STAGES - 1) * ROWS);
-        cp_async_wait<STAGES - 1>();
-        const bool on = row < last;
-        Two f[kNV][H], s = both(0.f);
+            for (int q = 0; q < R; ++q) {
+                s[q] = 0.f;
 #pragma unroll
-        for (int v = 0; v < kNV; ++v) {
-            pairs(reinterpret_cast<const uint4 *>(ring)[slot(stage, v)], f[v], T());
-            if (!on || !mine[v])
-#pragma unroll
-                for (int k = 0; k < H; ++k) f[v][k] = both(0.f);
-#pragma unroll
-            for (int k = 0; k < H; ++k) s = add2(s, f[v][k]);
-        }
-        const float mean = row_total(s.x + s.y, 0) / (float)cols;
-        s = both(0.f);
-#pragma unroll
-        for (int v = 0; v < kNV; ++v)
-            if (mine[v])
-#pragma unroll
-                for (int k = 0; k < H; ++k) {
-                    f[v][k] = add2(f[v][k], both(-mean));
-                    s = fma2(f[v][k], f[v][k], s);
-                }
-        const float rstd = rsqrtf(row_total(s.x + s.y, 1) / (float)cols + a.eps);
-        if (on) {
-#pragma unroll
-            for (int v = 0; v < kNV; ++v)
-                if (mine[v]) {
-                    Two o[H];
-#pragma unroll
-                    for (int k = 0; k < H; ++k) o[k] = fma2(mul2(f[v][k], both(rstd)), w[v][k], b[v][k]);
-                    *reinterpret_cast<uint4 *>(y + row * a.y.row + at[v]) = from_pairs(o, T());
-                }
-            if (t == 0) {
-                if (a.mean) a.mean[i * a.n + row] = mean;
-                if (a.rstd) a.rstd[i * a.n + row] = rstd;
+                for (int k = 0; k < TPR / 32; ++k) s[q] += scratch[which][side * (TPR / 32) + k][q];
             }
         }
-        if (++stage == STAGES) stage = 0;
+#pragma unroll
+        for (int q = 0; q < R; ++q) s[q] /= (float)cols;
+    };
+    // a warp's threads go on together: up to where the first of their rows ends
+    for (const int64_t behind = TPR < 32 ? (side % (32 / TPR)) * R : 0; row - behind < last; row += kSide * R) {
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            Two s = both(0.f);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                Two f[H];
+                pairs(raw[q][v], f, T());
+#pragma unroll
+                for (int k = 0; k < H; ++k) s = add2(s, f[k]);
+            }
+            mean[q] = s.x + s.y;
+        }
+        averages(mean, 0);
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            Two s = both(0.f);
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                if (v * TPR + t < packs) {
+                    Two f[H];
+                    pairs(raw[q][v], f, T());
+#pragma unroll
+                    for (int k = 0; k < H; ++k) {
+                        f[k] = add2(f[k], both(-mean[q]));
+                        s = fma2(f[k], f[k], s);
+                    }
+                }
+            rstd[q] = s.x + s.y;
+        }
+        averages(rstd, 1);
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            rstd[q] = rsqrtf(rstd[q] + a.eps);
+            if (t == 0 && row + q < last) {
+                if (a.mean) a.mean[i * a.n + row + q] = mean[q];
+                if (a.rstd) a.rstd[i * a.n + row + q] = rstd[q];
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int at = v * TPR + t;
+            Two w[H], b[H];
+            if (at < packs)
+#pragma unroll
+                for (int k = 0; k < H; k += 2) {
+                    const int from = ((v * (N / 4) + k / 2) * TPR + t) * 4;
+                    const float4 wf = *reinterpret_cast<const float4 *>(weights_at + from), bf = *reinterpret_cast<const float4 *>(biases_at + from);
+                    w[k] = Two{wf.x, wf.y};
+                    w[k + 1] = Two{wf.z, wf.w};
+                    b[k] = Two{bf.x, bf.y};
+                    b[k + 1] = Two{bf.z, bf.w};
+                }
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                if (at < packs && row + q < last) {
+                    Two f[H];
+                    pairs(raw[q][v], f, T());
+#pragma unroll
+                    for (int k = 0; k < H; ++k) f[k] = fma2(mul2(add2(f[k], both(-mean[q])), both(rstd[q])), w[k], b[k]);
+                    reinterpret_cast<uint4 *>(y + (row + q) * a.y.row)[at] = from_pairs(f, T());
+                }
+                fetch(q, v, row + q + kSide * R);
+            }
+        }
     }
-    cp_async_wait<0>();
 }
 
 // The blocks' sums of a group, column by column: 32 columns a block, eight warps take the blocks in turn.
@@ -622,13 +648,13 @@ cudaError_t allow_shared(K *kernel, int bytes, PerDeviceOnce &once) {
     return e;
 }
 
-template <typename T, typename P, int TPR>
-cudaError_t norm_stream(const NormArgs &a, cudaStream_t s) {
-    constexpr int kRows = TPR < 256 ? 256 / TPR : 1, kStages = 4, kSmem = kStages * kNV * TPR * kRows * 16;
-    auto *kernel = norm_stream_kernel<T, P, TPR, kRows, kStages>;
+template <typename T, typename P, int TPR, int NV, int R>
+cudaError_t norm_groups(const NormArgs &a, cudaStream_t s) {
+    constexpr int kSmem = 2 * NV * TPR * (16 / (int)sizeof(T)) * (int)sizeof(float);
+    auto *kernel = norm_group_kernel<T, P, TPR, NV, R>;
     static PerDeviceOnce attr_set;
     const cudaError_t e = allow_shared(kernel, kSmem, attr_set);
-    return e != cudaSuccess ? e : launch_chained(kernel, dim3(norm_chunks(a.m, a.n), a.m), dim3(TPR * kRows), kSmem, s, false, a);
+    return e != cudaSuccess ? e : launch_chained(kernel, dim3(norm_chunks(a.m, a.n), a.m), dim3(kGroupThreads), kSmem, s, false, a);
 }
 
 template <typename T, typename P, int N, int TPR, int NV>
@@ -646,13 +672,18 @@ cudaError_t layer_norm(const NormArgs &a, cudaStream_t s) {
         const size_t pack = N * sizeof(P) < 16 ? N * sizeof(P) : 16;
         const bool wide = reinterpret_cast<uintptr_t>(a.w) % pack == 0 && reinterpret_cast<uintptr_t>(a.b) % pack == 0 && a.ldw * sizeof(P) % pack == 0;
         const int64_t packs = a.cols / N;
-        // enough rows for every block to keep the weights for eight of them and more
-        if (norm_chunks(a.m, a.n) * (int64_t)a.m >= kNormBlocks / 2 && packs <= 1024 && a.n * a.m >= kNormBlocks * 8 && getenv("NOSTREAM") == nullptr) {
-            if (packs <= 64) return norm_stream<T, P, 32>(a, s);
-            if (packs <= 128) return norm_stream<T, P, 64>(a, s);
-            if (packs <= 256) return norm_stream<T, P, 128>(a, s);
-            if (packs <= 512) return norm_stream<T, P, 256>(a, s);
-            return norm_stream<T, P, 512>(a, s);
+        // Enough rows for two blocks an SM with eight rows each and more (21 x 2048 x 4096 bfloat16: 123 us, 157 by norm_row_kernel; 86,016 rows of
+        // 128: 18 against 35).  Eight vectors a thread in bfloat16, whose weights take twice their bytes of shared memory; four in binary32
+        // (43,008 rows of 4096: 227 us, with eight 258).
+        if (norm_chunks(a.m, a.n) * (int64_t)a.m >= kNormBlocks / 2 && a.n * a.m >= kNormBlocks * 8 && packs <= 1024) {
+            constexpr int kMany = sizeof(T) == 2 ? 8 : 4;
+            if (packs <= 16) return norm_groups<T, P, 4, 4, 2>(a, s);
+            if (packs <= 32) return norm_groups<T, P, 8, 4, 2>(a, s);
+            if (packs <= 64) return norm_groups<T, P, 16, 4, 2>(a, s);
+            if (packs <= 128) return norm_groups<T, P, 32, 4, 2>(a, s);
+            if (packs <= 256) return norm_groups<T, P, 256 / kMany, kMany, 1>(a, s);
+            if (packs <= 512) return norm_groups<T, P, 512 / kMany, kMany, 1>(a, s);
+            return norm_groups<T, P, 1024 / kMany, kMany, 1>(a, s);
         }
         if (packs <= 32) return norm_rows<T, P, N, 32, 1>(a, wide, s);
         if (packs <= 64) return norm_rows<T, P, N, 32, 2>(a, wide, s);

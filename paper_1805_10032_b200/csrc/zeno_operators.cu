@@ -127,6 +127,18 @@ zeno_status zeno_dense_gradient(int32_t device, int32_t type, int32_t param_type
     return on_device(device, [&] { return zeno::launch_dense_gradient(type, param_type, a, static_cast<cudaStream_t>(stream)); });
 }
 
+zeno_status zeno_operator_status(int32_t device, void *stream) {
+    DeviceGuard guard(device);
+    int status = 0;
+    if (guard.err != cudaSuccess || zeno::read_operator_status(static_cast<cudaStream_t>(stream), &status) != cudaSuccess) return ZENO_ERR_CUDA;
+    return status ? ZENO_ERR_TIMEOUT : ZENO_OK;
+}
+
+zeno_status zeno_debug_set_operator_wait_limit(uint32_t polls) {
+    zeno::set_operator_wait_limit(polls);
+    return ZENO_OK;
+}
+
 zeno_status zeno_token_logprobs(int32_t device, int32_t type, const zeno_rows *logits, int32_t m, int64_t n, int64_t vocab,
                                 const int32_t *targets, int32_t top, float *logprobs, float *entropy, float *lse,
                                 int32_t *top_idx, float *top_logprobs, void *stream) {

@@ -204,8 +204,10 @@ __global__ void __launch_bounds__(256) dense_bias_kernel(DenseGradArgs a) {
 
 template <typename T, typename P>
 cudaError_t dense_gradient(const DenseGradArgs &a, cudaStream_t s) {
-    const dim3 grid((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m);
-    cudaError_t e = launch_chained(dense_any_kernel<T, P>, grid, dim3(256), 0, s, false, a);
+    cudaError_t e = cudaErrorNotSupported;
+    if (is_bf16<T>::value && dense_tc_usable(a)) e = launch_dense_tc(is_bf16<P>::value ? ZENO_BF16 : ZENO_F32, a, s);
+    if (e == cudaErrorNotSupported)
+        e = launch_chained(dense_any_kernel<T, P>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
     if (e == cudaSuccess && a.db)
         e = launch_chained(dense_bias_kernel<T, P>, dim3((unsigned)((a.outputs + 31) / 32), a.m), dim3(256), 0, s, false, a);
     return e;

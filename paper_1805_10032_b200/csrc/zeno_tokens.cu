@@ -198,7 +198,7 @@ __device__ __noinline__ void top_by_lists(const T *z, int64_t head, int64_t v_be
 //
 // The alternatives cost the pass over the logits one comparison a batch: a thread keeps its largest entry.  The k-th largest of the
 // threads' largest is a bound that k entries reach, and only about k threads have entries that do; theirs are read again (from
-// L2), and what reaches the bound is ranked by counting.  The bound is taken to the upper 16 bits of the order.
+// L2), and what reaches the bound is ranked by counting.
 template <typename T, int THREADS, bool TOP>
 __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ? 8 : 24) logprobs_kernel(LogprobArgs a, int parts) {
     using V = Vec<T>;
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int64_t v = base + i * 32 + lane;
-            raw[i] = v < v_end ? __ldg(zv + v) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
+            raw[i] = v < v_end ? (TOP ? __ldg(zv + v) : __ldcs(zv + v)) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
             any |= v < v_end;
         }
         float most = V::most(raw[0]);
@@ -290,19 +290,34 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
     Sums q = {M, s2.x + s2.y, e2.x + e2.y};
 
     if (TOP) {
-        // the bound: the largest multiple of 2^16 that the largest entries of `top` threads reach
+        // the bound: what the largest entries of `top` threads and few more reach
         orders[threadIdx.x] = any ? order_of(fmaxf(largest, v_rest)) : 0u;
         __syncthreads();
         if (warp == 0) {
             uint32_t o[kWarps], at_least = 0;
 #pragma unroll
             for (int k = 0; k < kWarps; ++k) o[k] = orders[k * 32 + lane];
-            for (int bit = 31; bit >= 16; --bit) {
-                const uint32_t next = at_least | 1u << bit;
-                int n = 0;
+            uint32_t lowest = ~0u, highest = 0;
 #pragma unroll
-                for (int k = 0; k < kWarps; ++k) n += o[k] >= next;
-                if ((int)__reduce_add_sync(kAll, (unsigned)n) >= top) at_least = next;
+            for (int k = 0; k < kWarps; ++k) {
+                lowest = min(lowest, o[k]);
+                highest = max(highest, o[k]);
+            }
+            // `top` threads and more reach at_least, fewer than `top` reach beyond; a few more than wanted will do
+            at_least = __reduce_min_sync(kAll, lowest);
+            uint32_t beyond = __reduce_max_sync(kAll, highest);
+            if (at_least < beyond) {
+                ++beyond;
+                while (beyond - at_least > 1) {
+                    const uint32_t next = at_least + (beyond - at_least) / 2;
+                    int n = 0;
+#pragma unroll
+                    for (int k = 0; k < kWarps; ++k) n += o[k] >= next;
+                    n = (int)__reduce_add_sync(kAll, (unsigned)n);
+                    if (n < top) beyond = next;
+                    else at_least = next;
+                    if (n >= top && n <= top + 8) break;
+                }
             }
             if (lane == 0) {
                 bound = at_least;

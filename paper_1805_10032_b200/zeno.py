@@ -33,6 +33,7 @@ EXPORTS = (
     "zeno_last_cuda_error", "zeno_last_wait_code", "zeno_status_string",
     "zeno_layer_norm", "zeno_layer_norm_gradient", "zeno_layer_norm_gradient_workspace", "zeno_pack_activations",
     "zeno_dense_gradient", "zeno_dense_gradient_workspace", "zeno_token_logprobs", "zeno_token_gradient",
+    "zeno_operator_status", "zeno_debug_set_operator_wait_limit",
 )
 
 
@@ -136,6 +137,10 @@ def load_library() -> ctypes.CDLL:
     lib.zeno_dense_gradient.argtypes = [i32, i32, i32, rows, rows, rows, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp]
     lib.zeno_dense_gradient_workspace.restype = i64
     lib.zeno_dense_gradient_workspace.argtypes = [i32, i64, i64, i64]
+    lib.zeno_operator_status.restype = i32
+    lib.zeno_operator_status.argtypes = [i32, vp]
+    lib.zeno_debug_set_operator_wait_limit.restype = i32
+    lib.zeno_debug_set_operator_wait_limit.argtypes = [ctypes.c_uint32]
     lib.zeno_token_logprobs.restype = i32
     lib.zeno_token_logprobs.argtypes = [i32, i32, rows, i32, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.zeno_token_gradient.restype = i32
@@ -732,6 +737,16 @@ def token_gradient(logits, targets, lse, g_logprob, entropy=None, g_entropy=None
                                   _ptr(entropy), g_logprob.data_ptr(), _ptr(g_entropy), _rows(out, "out"), _current(dev, stream)),
           "zeno_token_gradient")
     return out
+
+
+def check_operator_status(device: int = 0, stream=None):
+    """Synchronises and raises if a kernel of the operators above gave up on a bounded device-side wait (dense_gradient on the tensor cores has them)."""
+    _done(load_library().zeno_operator_status(device, _current(torch.device("cuda", device), stream)), "zeno_operator_status")
+
+
+def debug_set_operator_wait_limit(polls: int):
+    """Test hook: polls a bounded device-side wait of the operators may take before it gives up (see zeno.h)."""
+    load_library().zeno_debug_set_operator_wait_limit(polls)
 
 
 def from_workload(w, m_max=None, n_r_max=None, device=0) -> "Zeno":

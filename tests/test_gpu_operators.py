@@ -265,6 +265,58 @@ def test_dense_gradient(m, n, inputs, outputs, act, par):
         R.assert_near(only, want[0], want[2], "no bias")
 
 
+@pytest.mark.parametrize("m,n,inputs,outputs", [(3, 300, 2048, 2048), (40, 129, 640, 768), (2, 2100, 1040, 4112), (1, 5000, 2064, 1296)])
+def test_dense_gradient_of_many_tiles(m, n, inputs, outputs):
+    """More tiles than the device takes at a time, with edges, and long sums."""
+    g = _gen(n)
+    saved = zeno.pack_activations(_rows(g, m, n, inputs, BF16, "aligned"))
+    dy = _rows(g, m, n, outputs, BF16, "aligned", 0.1)
+    for par in (F32, BF16):
+        dw, db = torch.full((m, outputs, inputs), NAN, device="cuda", dtype=par), torch.full((m, outputs), NAN, device="cuda", dtype=par)
+        zeno.dense_gradient(dy, saved, dw, db)
+        zeno.check_operator_status()
+        for i in range(m):
+            want = R.dense_gradient(dy[i], R.unpack(saved.codes[i], saved.scales[i]))
+            R.assert_near(dw[i], want[0], want[2], "dw")
+            R.assert_near(db[i], want[1], want[3], "db")
+
+
+def test_dense_gradient_of_every_code_and_scale():
+    """All 255 codes of a number and NaN, under the smallest and largest scales."""
+    codes = torch.arange(256, device="cuda").to(torch.uint8).reshape(1, 1, 256).repeat(1, 64, 1)
+    k = torch.linspace(-117, 119, 64, device="cuda").round()
+    scales = torch.exp2(k.double()).float().reshape(1, 64, 1).repeat(1, 1, 2)
+    dy = torch.eye(64, device="cuda", dtype=BF16).unsqueeze(0)
+    dw = torch.empty(1, 64, 256, device="cuda")
+    zeno.dense_gradient(dy, zeno.Saved(codes, scales), dw)
+    value = codes.view(torch.float8_e4m3fn).double() * scales.double().repeat_interleave(128, -1)
+    bad = torch.isnan(value[0, 0])
+    assert int(bad.sum()) == 2
+    assert torch.isnan(dw[..., bad]).all()                       # zero times NaN, too
+    assert torch.equal(dw[..., ~bad].double(), value[..., ~bad])
+
+
+def test_a_wait_that_runs_out_is_reported_and_leaves_the_device_usable():
+    g = _gen(1)
+    saved = zeno.pack_activations(_rows(g, 2, 200, 512, BF16))
+    dy = _rows(g, 2, 200, 768, BF16, "dense", 0.1)
+    dw, want = torch.empty(2, 768, 512, device="cuda"), torch.empty(2, 768, 512, device="cuda")
+    zeno.dense_gradient(dy, saved, want)
+    zeno.check_operator_status()
+    zeno.debug_set_operator_wait_limit(0)
+    try:
+        zeno.dense_gradient(dy, saved, dw)
+        with pytest.raises(zeno.ZenoError) as e:
+            zeno.check_operator_status()
+        assert e.value.status == zeno.ERR_TIMEOUT
+    finally:
+        zeno.debug_set_operator_wait_limit(1 << 22)
+    zeno.check_operator_status()                                 # the report was the last one's
+    zeno.dense_gradient(dy, saved, dw)
+    zeno.check_operator_status()
+    assert torch.equal(dw, want)
+
+
 def test_dense_gradient_layouts_and_values_that_are_not_finite():
     g = _gen(5)
     m, n, inputs, outputs = 3, 70, 256, 128
