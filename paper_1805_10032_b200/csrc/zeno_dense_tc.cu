@@ -5,7 +5,7 @@
 // the tensor copies write.  Each block holds 128 of the outputs' rows of dY^T and 128 of the inputs of X, and the pair's instruction
 // (cta_group::2, M = 256, N = 256) reads both halves: a code is turned into bfloat16 once for 256 outputs.  code * scale is
 // exact in bfloat16, products of bfloat16 are exact, and the sums stay binary32 in TMEM.
-//   warp 0: copies of the codes;  warp 2: copies of dY;  warp 1 of the pair's first block: the instructions;
+//   warp 0: copies of the codes;  warp 3: of their scales;  warp 2: of dY;  warp 1 of the pair's first block: the instructions;
 //   warps 4 - 11: codes to bfloat16;  warps 12 - 15: a finished tile from TMEM to dW while the next one is summed.
 #include "zeno_saved.cuh"
 #include "zeno_tc.cuh"
@@ -19,10 +19,12 @@ constexpr int kTokens = 64;                   // tokens (the contraction index) 
 constexpr int kHalf = 128;                    // outputs, and inputs, of a block
 constexpr int kPairTile = 2 * kHalf;
 constexpr int kSubBytes = kTokens * 128;      // 64 tokens of 64 bfloat16 (or 128 codes) in 128-byte rows
-constexpr int kABytes = 2 * kSubBytes, kBBytes = 2 * kSubBytes, kCodeBytes = kSubBytes;
+constexpr int kABytes = 2 * kSubBytes, kBBytes = 2 * kSubBytes, kCodeBytes = kSubBytes, kScaleBytes = kTokens * 4;
 constexpr int kStages = 5, kCodeStages = 6;
-constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * kCodeBytes + 1024;
-constexpr int kConvWarps = 8, kEpiWarps = 4;
+constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * (kCodeBytes + kScaleBytes) + 1024;
+// The warps that convert come in sets, which take the stages in turn: a stage is a chain of waits, loads, arithmetic, stores and an
+// arrival that one set alone would follow from end to end (8 x 2048 tokens, 4096 x 4096: one set 691 us, two 589, four 562).
+constexpr int kConvWarps = 8, kSets = 4, kSetWarps = kConvWarps / kSets, kEpiWarps = 4;
 constexpr int kTmemCols = 512;                // two sets of 256 sums
 constexpr int kKernelId = 5;
 
@@ -36,24 +38,11 @@ struct DenseTcArgs {
     uint32_t spin_limit;
 };
 
-// ---- waits for what the other block of the pair signals
-
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-        "selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
-    if (mbar_try_wait_cluster(bar, parity)) return true;
-    if (!mbar_wait_poll(bar, parity, abort_flag)) return false;
-    return mbar_try_wait_cluster(bar, parity);          // the phase has ended: once more, for what it orders
-}
+// An arrival at a barrier of the pair's other block.  What it vouches for are this warp's writes to its own shared memory, already
+// ordered before the tensor cores' reads of them (fence.proxy.async): with the semantics of a release to the whole cluster every one
+// of these arrivals also waited for whatever its lanes had on the way.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 // the pair's commit: an arrival on the barrier at this place in both blocks
 __device__ __forceinline__ void pair_commit(uint32_t bar) {
@@ -122,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)cluster_rank();
     uint8_t *a_ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t *b_ring = a_ring + kStages * kABytes, *code_ring = b_ring + kStages * kBBytes;
+    uint8_t *b_ring = a_ring + kStages * kABytes, *code_ring = b_ring + kStages * kBBytes, *scale_ring = code_ring + kCodeStages * kCodeBytes;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     auto cfull = [&](int s) { return bar(s); };
     auto cempty = [&](int s) { return bar(kCodeStages + s); };
@@ -148,13 +137,13 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         abort_state[0] = 0;
         abort_state[1] = (int)a.spin_limit;
         for (int s = 0; s < kCodeStages; ++s) {
-            mbar_init(cfull(s), 1);
-            mbar_init(cempty(s), kConvWarps);
+            mbar_init(cfull(s), 1 + 32);       // the codes' copy, and the lanes that copy the scales
+            mbar_init(cempty(s), kSetWarps);
         }
         for (int s = 0; s < kStages; ++s) {
             mbar_init(afull(s), 1);
             mbar_init(abempty(s), 1);
-            mbar_init(bready(s), 2 * kConvWarps);
+            mbar_init(bready(s), 2 * kSetWarps);
         }
         for (int q = 0; q < 2; ++q) {
             mbar_init(dfull(q), 1);
@@ -209,6 +198,33 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                     ++round;
                 }
             }
+    } else if (warp == 3) {
+        // ------------------------------------------------------------------ scales: two tokens a lane
+        int s = 0;
+        uint32_t round = 0;
+        bool ok = true;
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
+            const int64_t block = (int64_t)it * 2 + rank;                   // of 128 columns
+            const bool in_range = block * kHalf < a.d.inputs;
+            const float *scales = static_cast<const float *>(a.d.scales.data) + group * a.d.scales.group + (in_range ? block : 0);
+            for (int kb = 0; kb < nkb; ++kb) {
+                ok = __all_sync(0xffffffffu, mbar_wait(cempty(s), (round & 1) ^ 1, abortp));
+                if (!ok) break;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int64_t t = (int64_t)kb * kTokens + j * 32 + lane;
+                    const bool valid = in_range && t < n;
+                    cp_async<4>(smem_u32(scale_ring + s * kScaleBytes + (j * 32 + lane) * 4), scales + (valid ? t * a.d.scales.row : 0), valid);
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(cfull(s)) : "memory");
+                if (++s == kCodeStages) {
+                    s = 0;
+                    ++round;
+                }
+            }
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
     } else if (warp == 1) {
         // ------------------------------------------------------------------ instructions, by the first block for both
         // descriptor: sums binary32, operands bfloat16, both MN-major
@@ -218,11 +234,11 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         bool ok = rank == 0;
         for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
             const int set = li & 1;
-            ok = __all_sync(0xffffffffu, mbar_wait_cluster(dempty(set), ((uint32_t)(li >> 1) & 1) ^ 1, abortp));
+            ok = __all_sync(0xffffffffu, mbar_wait(dempty(set), ((uint32_t)(li >> 1) & 1) ^ 1, abortp));
             if (!ok) break;
             tc_fence_after();
             for (int kb = 0; kb < nkb; ++kb) {
-                ok = mbar_wait_cluster(bready(s), ph, abortp) && mbar_wait(afull(s), ph, abortp);
+                ok = mbar_wait(bready(s), ph, abortp) && mbar_wait(afull(s), ph, abortp);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -245,43 +261,38 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         // ------------------------------------------------------------------ codes to bfloat16
         // Eight lanes take a pair of rows (even and odd token), four of the eight 16-code groups of each, the other four in the other half
         // (`flip`): their 16-byte accesses then meet all banks once, reading and writing, in the swizzled layouts of both.
-        const int w = warp - 4, l = lane & 7, flip = (lane >> 3) & 1, odd = l >> 2;
+        const int set = (warp - 4) / kSetWarps, w = (warp - 4) % kSetWarps, l = lane & 7, flip = (lane >> 3) & 1, odd = l >> 2;
         const int g = (l & 3) + 4 * (odd ^ flip);
         const uint32_t remote_bready = rank == 0 ? 0u : cluster_addr(&bars[2 * kCodeStages + 2 * kStages], 0);
-        int s = 0, sc = 0;
-        uint32_t ph = 0, phc = 0;
+        constexpr int kRows = kTokens / (4 * kSetWarps);                    // of a lane
+        auto row_of = [&](int j) { return 2 * ((j * kSetWarps + w) * 2 + (lane >> 4)) + odd; };
+        uint32_t stage = 0;                                                 // stages so far, all sets'
         bool ok = true;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
-            const int64_t block = (int64_t)it * 2 + rank;                   // of 128 columns
-            const bool in_range = block * kHalf < a.d.inputs;
-            const float *scales = static_cast<const float *>(a.d.scales.data) + group * a.d.scales.group + block;
-            auto token = [&](int kb, int j) { return (int64_t)kb * kTokens + 2 * (j * 16 + w * 2 + (lane >> 4)) + odd; };
-            float next[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) next[j] = in_range && token(0, j) < n ? __ldg(scales + token(0, j) * a.d.scales.row) : 0.f;
-            for (int kb = 0; kb < nkb; ++kb) {
-                float scale[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    scale[j] = next[j];
-                    next[j] = in_range && token(kb + 1, j) < n ? __ldg(scales + token(kb + 1, j) * a.d.scales.row) : 0.f;
-                }
-                ok = mbar_wait(cfull(sc), phc, abortp) && mbar_wait(abempty(s), ph ^ 1, abortp);
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li, stage += nkb)
+            for (int kb = (int)((set - stage) & (kSets - 1)); kb < nkb; kb += kSets) {
+                const uint32_t at = stage + kb, round = at / kStages, code_round = at / kCodeStages;
+                const int s = (int)(at - round * kStages), sc = (int)(at - code_round * kCodeStages);
+                // First the place for the result: that it is free says that all instructions up to kStages stages ago have ended, and so that
+                // neither barrier is more than one phase behind (a set does not see every use of a stage, and phases are told by parity).
+                ok = mbar_wait(abempty(s), (round & 1) ^ 1, abortp) && mbar_wait(cfull(sc), code_round & 1, abortp);
                 // the second block vouches for its part of dY with its part of X
-                if (ok && rank != 0) ok = mbar_wait(afull(s), ph, abortp);
+                if (ok && rank != 0) ok = mbar_wait(afull(s), round & 1, abortp);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const uint8_t *codes = code_ring + sc * kCodeBytes;
+                const float *scales = reinterpret_cast<const float *>(scale_ring + sc * kScaleBytes);
                 uint8_t *to = b_ring + s * kBBytes + (g >> 2) * kSubBytes;
-                uint4 c[2];
+                uint4 c[kRows];
+                float scale[kRows];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int row = 2 * (j * 16 + w * 2 + (lane >> 4)) + odd;
+                for (int j = 0; j < kRows; ++j) {
+                    const int row = row_of(j);
                     c[j] = *reinterpret_cast<const uint4 *>(codes + row * 128 + ((g ^ (row & 7)) << 4));
+                    scale[j] = scales[row];
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int row = 2 * (j * 16 + w * 2 + (lane >> 4)) + odd;
+                for (int j = 0; j < kRows; ++j) {
+                    const int row = row_of(j);
                     uint4 v[2];
                     sixteen_values(c[j], scale[j], v);
 #pragma unroll
@@ -290,20 +301,12 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
+                    // Not before the stores: they need what the loads bring.  An arrival right behind the loads let the next codes overtake them.
                     mbar_arrive(cempty(sc));
                     if (rank == 0) mbar_arrive(bready(s));
                     else mbar_arrive_cluster(remote_bready + s * 8);
                 }
-                if (++s == kStages) {
-                    s = 0;
-                    ph ^= 1;
-                }
-                if (++sc == kCodeStages) {
-                    sc = 0;
-                    phc ^= 1;
-                }
             }
-        }
     } else if (warp >= 12) {
         // ------------------------------------------------------------------ finished tiles to dW
         const int quad = warp & 3;                                 // TMEM lanes this warp may access

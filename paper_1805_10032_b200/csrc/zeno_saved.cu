@@ -184,22 +184,56 @@ __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
         }
 }
 
-// db: a block takes 32 outputs of a group, its warps the rows in turn
-template <typename T, typename P>
-__global__ void __launch_bounds__(256) dense_bias_kernel(DenseGradArgs a) {
-    __shared__ float sums[8][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.y;
-    const int64_t o = (int64_t)blockIdx.x * 32 + lane;
-    float s = 0.f;
-    if (o < a.outputs)
-        for (int64_t t = warp; t < a.n; t += 8) s += value_of(static_cast<const T *>(a.dy.data) + a.dy.at(i * a.n + t) + o);
-    sums[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0 && o < a.outputs) {
+// db: a cluster takes 32 N outputs of a group, its blocks and their warps the rows in turn, a lane N neighbouring outputs; the warps' sums are
+// joined in shared memory, the blocks' through the cluster's.
+constexpr int kBiasWarps = 8;
+template <typename T, typename P, int N>
+__global__ void __launch_bounds__(kBiasWarps * 32) dense_bias_kernel(DenseGradArgs a, int cluster) {
+    __shared__ float sums[kBiasWarps][32 * N + 1];
+    __shared__ float total[32 * N];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.z, rank = cluster > 1 ? (int)cluster_rank() : 0;
+    const int64_t o0 = (int64_t)blockIdx.y * 32 * N, o = o0 + lane * N;
+    const T *dy = static_cast<const T *>(a.dy.data) + i * a.dy.group + o;
+    float s[N];
 #pragma unroll
-        for (int q = 1; q < 8; ++q) s += sums[q][lane];
-        put(static_cast<P *>(a.db) + i * a.ldb + o, s);
+    for (int k = 0; k < N; ++k) s[k] = 0.f;
+    if (o < a.outputs) {
+#pragma unroll 8
+        for (int64_t t = rank * kBiasWarps + warp; t < a.n; t += cluster * kBiasWarps) {
+            alignas(16) T e[N];
+            if constexpr (N * sizeof(T) == 16) *reinterpret_cast<uint4 *>(e) = __ldg(reinterpret_cast<const uint4 *>(dy + t * a.dy.row));
+            else e[0] = dy[t * a.dy.row];
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[k] += value_of(e + k);
+        }
     }
+#pragma unroll
+    for (int k = 0; k < N; ++k) sums[warp][k * 32 + lane] = s[k];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 32 * N; c += kBiasWarps * 32) {
+        float v = 0.f;
+#pragma unroll
+        for (int q = 0; q < kBiasWarps; ++q) v += sums[q][c];
+        total[c] = v;
+    }
+    if (cluster > 1) cluster_barrier();
+    if (rank == 0)
+        for (int c = threadIdx.x; c < 32 * N; c += kBiasWarps * 32) {
+            float v = total[c];
+            for (int q = 1; q < cluster; ++q) v += cluster_load(cluster_addr(&total[c], q));
+            const int64_t to = o0 + (c & 31) * N + c / 32;
+            if (to < a.outputs) put(static_cast<P *>(a.db) + i * a.ldb + to, v);
+        }
+    if (cluster > 1) cluster_barrier();
+}
+
+template <typename T, typename P, int N>
+cudaError_t dense_bias(const DenseGradArgs &a, cudaStream_t s) {
+    int cluster = 1;
+    while (cluster < 8 && a.n > cluster * 64) cluster *= 2;          // eight rows a warp and more
+    const dim3 grid(cluster, (unsigned)((a.outputs + 32 * N - 1) / (32 * N)), a.m);
+    if (cluster == 1) return launch_chained(dense_bias_kernel<T, P, N>, grid, dim3(kBiasWarps * 32), 0, s, false, a, cluster);
+    return launch_clustered(dense_bias_kernel<T, P, N>, cluster, grid, dim3(kBiasWarps * 32), 0, s, false, a, cluster);
 }
 
 template <typename T, typename P>
@@ -208,8 +242,10 @@ cudaError_t dense_gradient(const DenseGradArgs &a, cudaStream_t s) {
     if (is_bf16<T>::value && dense_tc_usable(a)) e = launch_dense_tc(is_bf16<P>::value ? ZENO_BF16 : ZENO_F32, a, s);
     if (e == cudaErrorNotSupported)
         e = launch_chained(dense_any_kernel<T, P>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
-    if (e == cudaSuccess && a.db)
-        e = launch_chained(dense_bias_kernel<T, P>, dim3((unsigned)((a.outputs + 31) / 32), a.m), dim3(256), 0, s, false, a);
+    if (e == cudaSuccess && a.db) {
+        constexpr int N = 16 / sizeof(T);
+        e = a.outputs % N == 0 && aligned_to(a.dy, a.m, a.n, sizeof(T), 16) ? dense_bias<T, P, N>(a, s) : dense_bias<T, P, 1>(a, s);
+    }
     return e;
 }
 
