@@ -368,9 +368,11 @@ zeno_status zeno_pack_activations(int32_t device, int32_t type, const zeno_rows 
  * zeno_pack_activations kept it:  dw[i][o][k] = sum over group i's rows of dy_o x_k,  db[i][o] = sum of dy_o.
  * dw: per group outputs x inputs entries, row-major, ldw elements after the previous group's; db (or NULL) likewise with ldb:
  * slices of V in the layout of the parameter vector.  The products are exact and summed in binary32.
- * The scales have to be powers of two, as zeno_pack_activations writes them.  bfloat16 dy in rows and groups of multiples of
- * 16 bytes (codes likewise), one group behind the other, goes to the tensor cores. */
-int64_t zeno_dense_gradient_workspace(int32_t m, int64_t n, int64_t inputs, int64_t outputs);
+ * The scales have to be powers of two, as zeno_pack_activations writes them.  Codes in rows and groups of multiples of 16 bytes, one
+ * group behind the other (as the binding makes them), go to the tensor cores; binary32 dy then takes 6 bytes of workspace an entry, bfloat16
+ * dy that is aligned the same way none. */
+int64_t zeno_dense_gradient_workspace(int32_t type, const zeno_rows *dy, const zeno_rows *codes, int32_t m, int64_t n, int64_t inputs,
+                                      int64_t outputs);
 zeno_status zeno_dense_gradient(int32_t device, int32_t type, int32_t param_type, const zeno_rows *dy, const zeno_rows *codes,
                                 const zeno_rows *scales, int32_t m, int64_t n, int64_t inputs, int64_t outputs, void *dw,
                                 int64_t ldw, void *db, int64_t ldb, void *workspace, int64_t workspace_bytes, void *stream);

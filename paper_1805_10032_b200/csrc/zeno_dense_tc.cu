@@ -6,6 +6,7 @@
 // (cta_group::2, M = 256, N = 256) reads both halves: a code is turned into bfloat16 once for 256 outputs.  code * scale is
 // exact in bfloat16, products of bfloat16 are exact, and the sums stay binary32 in TMEM.
 //   warp 0: copies of the codes;  warp 3: of their scales;  warp 2: of dY;  warp 1 of the pair's first block: the instructions;
+// binary32 dY is rewritten as three bfloat16 terms first, which hold it exactly; few tiles are cut along the tokens.
 //   warps 4 - 11: codes to bfloat16;  warps 12 - 15: a finished tile from TMEM to dW while the next one is summed.
 #include "zeno_saved.cuh"
 #include "zeno_tc.cuh"
@@ -21,7 +22,8 @@ constexpr int kPairTile = 2 * kHalf;
 constexpr int kSubBytes = kTokens * 128;      // 64 tokens of 64 bfloat16 (or 128 codes) in 128-byte rows
 constexpr int kABytes = 2 * kSubBytes, kBBytes = 2 * kSubBytes, kCodeBytes = kSubBytes, kScaleBytes = kTokens * 4;
 constexpr int kStages = 5, kCodeStages = 6;
-constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * (kCodeBytes + kScaleBytes) + 1024;
+constexpr int kTurnBytes = 32 * 17 * 4;       // a warp's 32 x 16 sums on their way from rows to columns
+constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * (kCodeBytes + kScaleBytes) + 4 * kTurnBytes + 1024;
 // The warps that convert come in sets, which take the stages in turn: a stage is a chain of waits, loads, arithmetic, stores and an
 // arrival that one set alone would follow from end to end (8 x 2048 tokens, 4096 x 4096: one set 691 us, two 589, four 562).
 constexpr int kConvWarps = 8, kSets = 4, kSetWarps = kConvWarps / kSets, kEpiWarps = 4;
@@ -33,6 +35,10 @@ __device__ int g_status;                      // raised by a block whose bounded
 struct DenseTcArgs {
     DenseGradArgs d;
     int out_tiles, in_tiles, shared_dy, shared_codes;
+    int terms;                  // bfloat16 terms of dY, planes of the tensor map's third dimension: summed like further tokens
+    int nkb;                    // stages of one term
+    int splits;                 // parts that the sum over tokens is cut into
+    float *part;                // [split][group][output][input] (splits > 1)
     int64_t items;
     int vector_stores;
     uint32_t spin_limit;
@@ -121,15 +127,20 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
     auto dfull = [&](int q) { return bar(2 * kCodeStages + 3 * kStages + q); };
     auto dempty = [&](int q) { return bar(2 * kCodeStages + 3 * kStages + 2 + q); };
     const int64_t n = a.d.n;
-    const int nkb = (int)((n + kTokens - 1) / kTokens);
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    // item li of this pair -> (group, output tile, input tile); neighbouring pairs share dY's tile in L2
-    auto get_item = [&](int li, int &group, int &ot, int &it) {
+    // item li of this pair -> (group, output tile, input tile, part of the stages); neighbouring pairs share dY's tile in L2
+    int group, ot, it, split, kb0, kb1;
+    auto get_item = [&](int li) {
         const int64_t item = pair + (int64_t)li * pairs;
-        group = (int)(item / ((int64_t)a.out_tiles * a.in_tiles));
-        const int in_group = (int)(item - (int64_t)group * a.out_tiles * a.in_tiles);
+        int64_t rest = item / a.splits;
+        split = (int)(item - rest * a.splits);
+        group = (int)(rest / ((int64_t)a.out_tiles * a.in_tiles));
+        const int in_group = (int)(rest - (int64_t)group * a.out_tiles * a.in_tiles);
         ot = in_group / a.in_tiles;
         it = in_group - ot * a.in_tiles;
+        const int64_t all = (int64_t)a.terms * a.nkb;
+        kb0 = (int)(all * split / a.splits);
+        kb1 = (int)(all * (split + 1) / a.splits);
         return item < a.items;
     };
 
@@ -164,8 +175,6 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
     tc_fence_after();
     const uint32_t tmem = tmem_base_slot;
     volatile int *abortp = &abort_state[0];
-    int group, ot, it;
-
     if (warp == 0) wait_for_nothing(smem_u32(&never_bar), abortp);
     if (warp == 0 || warp == 2) {
         // ------------------------------------------------------------------ copies: codes (warp 0), dY (warp 2)
@@ -174,25 +183,30 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         int s = 0;
         uint32_t round = 0;
         bool ok = true;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li)
-            for (int kb = 0; kb < nkb; ++kb) {
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li)
+            for (int kb = kb0, term = kb0 / a.nkb, in_term = kb0 - term * a.nkb; kb < kb1; ++kb) {
                 ok = __all_sync(0xffffffffu, mbar_wait(is_codes ? cempty(s) : abempty(s), (round & 1) ^ 1, abortp));
                 if (!ok) break;
+                const int token0 = in_term * kTokens;
                 if (elect_one()) {
                     if (is_codes) {
                         mbar_expect_tx(cfull(s), kCodeBytes);
                         issued[s] = (int)round + 1;
-                        tma_load_3d(smem_u32(code_ring + s * kCodeBytes), &map_codes, it * kPairTile + rank * kHalf, kb * kTokens, a.shared_codes ? 0 : group, cfull(s));
+                        tma_load_3d(smem_u32(code_ring + s * kCodeBytes), &map_codes, it * kPairTile + rank * kHalf, token0, a.shared_codes ? 0 : group, cfull(s));
                     } else {
                         mbar_expect_tx(afull(s), kABytes);
                         issued[kCodeStages + s] = (int)round + 1;
 #pragma unroll 1
                         for (int h = 0; h < 2; ++h)
-                            tma_load_3d(smem_u32(a_ring + s * kABytes + h * kSubBytes), &map_dy, ot * kPairTile + rank * kHalf + h * 64, kb * kTokens,
-                                        a.shared_dy ? 0 : group, afull(s));
+                            tma_load_3d(smem_u32(a_ring + s * kABytes + h * kSubBytes), &map_dy, ot * kPairTile + rank * kHalf + h * 64, token0,
+                                        a.shared_dy ? 0 : group * a.terms + term, afull(s));
                     }
                 }
                 __syncwarp();
+                if (++in_term == a.nkb) {
+                    in_term = 0;
+                    ++term;
+                }
                 if (++s == stages) {
                     s = 0;
                     ++round;
@@ -203,20 +217,21 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         int s = 0;
         uint32_t round = 0;
         bool ok = true;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li) {
             const int64_t block = (int64_t)it * 2 + rank;                   // of 128 columns
             const bool in_range = block * kHalf < a.d.inputs;
             const float *scales = static_cast<const float *>(a.d.scales.data) + group * a.d.scales.group + (in_range ? block : 0);
-            for (int kb = 0; kb < nkb; ++kb) {
+            for (int kb = kb0, in_term = kb0 % a.nkb; kb < kb1; ++kb) {
                 ok = __all_sync(0xffffffffu, mbar_wait(cempty(s), (round & 1) ^ 1, abortp));
                 if (!ok) break;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const int64_t t = (int64_t)kb * kTokens + j * 32 + lane;
+                    const int64_t t = (int64_t)in_term * kTokens + j * 32 + lane;
                     const bool valid = in_range && t < n;
                     cp_async<4>(smem_u32(scale_ring + s * kScaleBytes + (j * 32 + lane) * 4), scales + (valid ? t * a.d.scales.row : 0), valid);
                 }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(cfull(s)) : "memory");
+                if (++in_term == a.nkb) in_term = 0;
                 if (++s == kCodeStages) {
                     s = 0;
                     ++round;
@@ -232,12 +247,12 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         int s = 0;
         uint32_t ph = 0;
         bool ok = rank == 0;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li) {
             const int set = li & 1;
             ok = __all_sync(0xffffffffu, mbar_wait(dempty(set), ((uint32_t)(li >> 1) & 1) ^ 1, abortp));
             if (!ok) break;
             tc_fence_after();
-            for (int kb = 0; kb < nkb; ++kb) {
+            for (int kb = kb0; kb < kb1; ++kb) {
                 ok = mbar_wait(bready(s), ph, abortp) && mbar_wait(afull(s), ph, abortp);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
@@ -246,9 +261,9 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                     const uint32_t ab = smem_u32(a_ring + s * kABytes), bb = smem_u32(b_ring + s * kBBytes);
 #pragma unroll
                     for (int k = 0; k < kTokens / 16; ++k)        // 16 tokens: two groups of eight rows
-                        pair_mma(tmem + set * 256, mn_desc(ab + k * 2048), mn_desc(bb + k * 2048), idesc, (uint32_t)(kb | k));
+                        pair_mma(tmem + set * 256, mn_desc(ab + k * 2048), mn_desc(bb + k * 2048), idesc, (uint32_t)((kb - kb0) | k));
                     pair_commit(abempty(s));
-                    if (kb + 1 == nkb) pair_commit(dfull(set));
+                    if (kb + 1 == kb1) pair_commit(dfull(set));
                 }
                 __syncwarp();
                 if (++s == kStages) {
@@ -268,8 +283,8 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         auto row_of = [&](int j) { return 2 * ((j * kSetWarps + w) * 2 + (lane >> 4)) + odd; };
         uint32_t stage = 0;                                                 // stages so far, all sets'
         bool ok = true;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li, stage += nkb)
-            for (int kb = (int)((set - stage) & (kSets - 1)); kb < nkb; kb += kSets) {
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li, stage += kb1 - kb0)
+            for (int kb = (int)((set - stage) & (kSets - 1)); kb < kb1 - kb0; kb += kSets) {
                 const uint32_t at = stage + kb, round = at / kStages, code_round = at / kCodeStages;
                 const int s = (int)(at - round * kStages), sc = (int)(at - code_round * kCodeStages);
                 // First the place for the result: that it is free says that all instructions up to kStages stages ago have ended, and so that
@@ -311,12 +326,13 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         // ------------------------------------------------------------------ finished tiles to dW
         const int quad = warp & 3;                                 // TMEM lanes this warp may access
         const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[2 * kCodeStages + 3 * kStages + 2], 0);
-        for (int li = 0; __all_sync(0xffffffffu, get_item(li, group, ot, it) && !*abortp); ++li) {
+        for (int li = 0; __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li) {
             const int set = li & 1;
             if (!__all_sync(0xffffffffu, mbar_wait(dfull(set), (uint32_t)(li >> 1) & 1, abortp))) break;
             tc_fence_after();
             const int64_t o = (int64_t)ot * kPairTile + rank * kHalf + quad * 32 + lane, k0 = (int64_t)it * kPairTile;
-            P *dw = static_cast<P *>(a.d.dw) + group * a.d.ldw + o * a.d.inputs + k0;
+            P *dw = a.splits > 1 ? reinterpret_cast<P *>(a.part) + (((int64_t)split * a.d.m + group) * a.d.outputs + o) * a.d.inputs + k0
+                                 : static_cast<P *>(a.d.dw) + group * a.d.ldw + o * a.d.inputs + k0;
             const bool mine = o < a.d.outputs;
             const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + set * 256;
 #pragma unroll 1
@@ -334,8 +350,8 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                         else mbar_arrive_cluster(remote_dempty + set * 8);
                     }
                 }
-                if (!mine) continue;
                 if (a.vector_stores) {
+                    if (!mine) continue;
                     constexpr int kPer = 16 / sizeof(P);
 #pragma unroll
                     for (int q = 0; q < 32 / kPer; ++q) {
@@ -344,10 +360,21 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                         for (int k = 0; k < kPer; ++k) put(e + k, __uint_as_float(v[(q * kPer + k) / 16][(q * kPer + k) % 16]));
                         if (k0 + c0 + q * kPer < a.d.inputs) *reinterpret_cast<uint4 *>(dw + c0 + q * kPer) = *reinterpret_cast<const uint4 *>(e);
                     }
-                } else {
+                } else {                                            // rows of any alignment: two outputs' 16 sums in a store of the warp
+                    float *turn = reinterpret_cast<float *>(scale_ring + kCodeStages * kScaleBytes + quad * kTurnBytes);
+                    const int rows = (int)min((int64_t)32, a.d.outputs - (o - lane)), col = lane & 15;
 #pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (k0 + c0 + k < a.d.inputs) put(dw + c0 + k, __uint_as_float(v[k / 16][k % 16]));
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) turn[lane * 17 + k] = __uint_as_float(v[h][k]);
+                        __syncwarp();
+                        const int64_t at = c0 + h * 16 + col;
+                        P *to = dw - (int64_t)lane * a.d.inputs + at;
+                        if (k0 + at < a.d.inputs)
+#pragma unroll 4
+                            for (int k = lane >> 4; k < rows; k += 2) put(to + (int64_t)k * a.d.inputs, turn[k * 17 + col]);
+                        __syncwarp();
+                    }
                 }
             }
         }
@@ -383,6 +410,53 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
+// dY as bfloat16 terms in [group][term][token][outputs, rounded up to 8]: one term (of bfloat16 in rows that no tensor map can step through) or
+// three, which hold a binary32 number exactly: each takes the leading 8 bits of what is left.  An infinity or NaN is its first term.
+template <typename T, int TERMS>
+__global__ void __launch_bounds__(256) dense_terms_kernel(Rows dy, int64_t rows, int64_t n, int64_t outputs, int64_t pitch, __nv_bfloat16 *out, int vectors) {
+    const int64_t per_row = pitch / 8, total = rows * per_row;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
+        const int64_t r = q / per_row, o = (q - r * per_row) * 8, group = r / n;
+        const T *from = static_cast<const T *>(dy.data) + dy.at(r) + o;
+        alignas(16) T e[8];
+        float f[8];
+        if (vectors) {
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(e) / 16; ++k) reinterpret_cast<uint4 *>(e)[k] = reinterpret_cast<const uint4 *>(from)[k];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = value_of(e + k);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = o + k < outputs ? value_of(from + k) : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+            alignas(16) __nv_bfloat16 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = __float2bfloat16_rn(f[k]);
+                // (a finite number may round to infinity: then the term is the largest finite one)
+                if (fabsf(f[k]) < INFINITY && !(fabsf(__bfloat162float(v[k])) < INFINITY)) v[k] = __ushort_as_bfloat16(f[k] < 0.f ? 0xff7f : 0x7f7f);
+                f[k] = fabsf(f[k]) < INFINITY ? f[k] - __bfloat162float(v[k]) : 0.f;
+            }
+            *reinterpret_cast<uint4 *>(out + ((group * TERMS + t) * n + (r - group * n)) * pitch + o) = *reinterpret_cast<const uint4 *>(v);
+        }
+    }
+}
+
+// the parts' sums
+template <typename P>
+__global__ void __launch_bounds__(256) dense_join_kernel(const float *part, int splits, int64_t per_group, int64_t total, P *dw, int64_t ldw) {
+    pdl_wait();
+    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (q >= total) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < splits; ++k) s += part[k * total + q];
+    const int64_t group = q / per_group;
+    put(dw + group * ldw + (q - group * per_group), s);
+}
+
 uint32_t spin_limit = kSpinLimit;
 
 bool encode(CUtensorMap *map, CUtensorMapDataType type, const Rows &v, int elem, int m, int64_t n, int64_t cols, int box_cols) {
@@ -405,41 +479,98 @@ bool mappable(const Rows &v, int elem, int m, int64_t n, int64_t cols) {
     return m <= 1 || v.group == 0 || (v.group >= (n > 1 ? n * v.row : cols) && v.group * elem < limit);
 }
 
-}  // namespace
+// What a call does: the terms that dY is rewritten in (0: it is read as it lies), the parts of the sum, and where they lie in the workspace.
+struct Plan {
+    int terms, splits, out_tiles, in_tiles;
+    int64_t pitch, part_at, bytes;
+};
 
-bool dense_tc_usable(const DenseGradArgs &a) {
-    return a.n > 0 && mappable(a.dy, 2, a.m, a.n, a.outputs) && mappable(a.codes, 1, a.m, a.n, a.inputs) && a.n < ((int64_t)1 << 31) - kTokens;
+// Parts: with fewer tiles than half the pairs of SMs, as many as the pairs take, each of eight stages and more.  The count of SMs is this
+// design's, so that the workspace's size needs no device.
+constexpr int kPairs = 74;
+
+bool plan_dense_tc(int type, const DenseGradArgs &a, Plan *p) {
+    if (a.n < 1 || a.n >= (int64_t)1 << 28 || !mappable(a.codes, 1, a.m, a.n, a.inputs)) return false;
+    p->terms = type == ZENO_F32 ? 3 : mappable(a.dy, 2, a.m, a.n, a.outputs) ? 0 : 1;
+    p->pitch = (a.outputs + 7) / 8 * 8;
+    p->out_tiles = (int)((a.outputs + kPairTile - 1) / kPairTile);
+    p->in_tiles = (int)((a.inputs + kPairTile - 1) / kPairTile);
+    const int64_t tiles = (int64_t)a.m * p->out_tiles * p->in_tiles, stages = (a.n + kTokens - 1) / kTokens * (p->terms > 1 ? p->terms : 1);
+    int64_t splits = tiles * 2 > kPairs ? 1 : kPairs / tiles;
+    if (splits > stages / 8) splits = stages / 8;
+    p->splits = splits < 1 ? 1 : (int)splits;
+    const int64_t terms_bytes = (int64_t)a.m * p->terms * a.n * p->pitch * 2;
+    p->part_at = (terms_bytes + 255) / 256 * 256;
+    p->bytes = p->part_at + (p->splits > 1 ? (int64_t)p->splits * a.m * a.outputs * a.inputs * 4 : 0);
+    return true;
 }
 
-cudaError_t launch_dense_tc(int param_type, const DenseGradArgs &d, cudaStream_t s) {
+}  // namespace
+
+int64_t dense_tc_workspace(int type, const DenseGradArgs &a) {
+    Plan p;
+    return plan_dense_tc(type, a, &p) ? p.bytes : 0;
+}
+
+cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &d, cudaStream_t s) {
+    Plan p;
+    if (!plan_dense_tc(type, d, &p)) return cudaErrorNotSupported;
+    uint8_t *ws = reinterpret_cast<uint8_t *>(d.workspace);
+    Rows dy = d.dy;
+    int planes = d.m;
+    if (p.terms) {
+        planes = d.m * p.terms;
+        dy = Rows{ws, p.pitch, d.n * p.pitch, d.n};
+    }
     CUtensorMap map_dy, map_codes;
-    if (!encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d.dy, 2, d.m, d.n, d.outputs, 64) ||
+    if (!encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, 2, planes, d.n, d.outputs, 64) ||
         !encode(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, d.codes, 1, d.m, d.n, d.inputs, 128))
         return cudaErrorNotSupported;
-    DenseTcArgs a;
-    a.d = d;
-    a.out_tiles = (int)((d.outputs + kPairTile - 1) / kPairTile);
-    a.in_tiles = (int)((d.inputs + kPairTile - 1) / kPairTile);
-    a.shared_dy = d.m > 1 && d.dy.group == 0;
-    a.shared_codes = d.m > 1 && d.codes.group == 0;
-    a.items = (int64_t)d.m * a.out_tiles * a.in_tiles;
-    const size_t elem = param_type == ZENO_BF16 ? 2 : 4;
-    a.vector_stores = reinterpret_cast<uintptr_t>(d.dw) % 16 == 0 && d.inputs * elem % 16 == 0 && (d.m <= 1 || d.ldw * elem % 16 == 0);
-    a.spin_limit = spin_limit;
     int device = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return e;
-    auto *kernel = param_type == ZENO_BF16 ? dense_tc_kernel<__nv_bfloat16> : dense_tc_kernel<float>;
+    if (p.terms) {
+        const int64_t rows = d.m * d.n, blocks = (rows * (p.pitch / 8) + 255) / 256;
+        const bool vectors = d.outputs % 8 == 0 && aligned_to(d.dy, d.m, d.n, type == ZENO_F32 ? 4 : 2, 16);
+        const dim3 grid((unsigned)(blocks < 148 * 16 ? blocks : 148 * 16));
+        auto *out = reinterpret_cast<__nv_bfloat16 *>(ws);
+        e = type == ZENO_F32 ? launch_chained(dense_terms_kernel<float, 3>, grid, dim3(256), 0, s, false, d.dy, rows, d.n, d.outputs, p.pitch, out, (int)vectors)
+                             : launch_chained(dense_terms_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, s, false, d.dy, rows, d.n, d.outputs, p.pitch, out, (int)vectors);
+        if (e != cudaSuccess) return e;
+    }
+    DenseTcArgs a;
+    a.d = d;
+    a.out_tiles = p.out_tiles;
+    a.in_tiles = p.in_tiles;
+    a.shared_dy = p.terms == 0 && d.m > 1 && d.dy.group == 0;
+    a.shared_codes = d.m > 1 && d.codes.group == 0;
+    a.terms = p.terms > 1 ? p.terms : 1;
+    a.nkb = (int)((d.n + kTokens - 1) / kTokens);
+    a.splits = p.splits;
+    a.part = reinterpret_cast<float *>(ws + p.part_at);
+    a.items = (int64_t)d.m * a.out_tiles * a.in_tiles * a.splits;
+    const bool bf16 = param_type == ZENO_BF16 && p.splits == 1;
+    const size_t elem = bf16 ? 2 : 4;
+    a.vector_stores = d.inputs * elem % 16 == 0 &&
+                      (p.splits > 1 || (reinterpret_cast<uintptr_t>(d.dw) % 16 == 0 && (d.m <= 1 || d.ldw * elem % 16 == 0)));
+    a.spin_limit = spin_limit;
+    auto *kernel = bf16 ? dense_tc_kernel<__nv_bfloat16> : dense_tc_kernel<float>;
     static PerDeviceOnce attr_set[2];
-    if (attr_set[param_type == ZENO_BF16].need(device)) {
+    if (attr_set[bf16].need(device)) {
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return e;
-        attr_set[param_type == ZENO_BF16].mark(device);
+        attr_set[bf16].mark(device);
     }
     // equal shares: the fewest pairs that make as many rounds as all would
     const int64_t most = sms / 2, rounds = (a.items + most - 1) / most, pairs = (a.items + rounds - 1) / rounds;
-    return launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), kSmem, s, false, map_dy, map_codes, a);
+    e = launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), kSmem, s, false, map_dy, map_codes, a);
+    if (e != cudaSuccess || p.splits == 1) return e;
+    const int64_t per_group = d.outputs * d.inputs, total = per_group * d.m;
+    const dim3 grid((unsigned)((total + 255) / 256));
+    if (param_type == ZENO_BF16)
+        return launch_chained(dense_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, true, a.part, p.splits, per_group, total, static_cast<__nv_bfloat16 *>(d.dw), d.ldw);
+    return launch_chained(dense_join_kernel<float>, grid, dim3(256), 0, s, true, a.part, p.splits, per_group, total, static_cast<float *>(d.dw), d.ldw);
 }
 
 void set_operator_wait_limit(uint32_t polls) { spin_limit = polls; }

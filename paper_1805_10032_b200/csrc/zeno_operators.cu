@@ -106,24 +106,40 @@ zeno_status zeno_pack_activations(int32_t device, int32_t type, const zeno_rows 
     return on_device(device, [&] { return zeno::launch_pack(type, a, static_cast<cudaStream_t>(stream)); });
 }
 
-int64_t zeno_dense_gradient_workspace(int32_t m, int64_t n, int64_t inputs, int64_t outputs) {
-    return check_sizes(m, n, inputs) == ZENO_OK && check_sizes(m, n, outputs) == ZENO_OK ? zeno::dense_gradient_workspace(m, n, inputs, outputs) : 0;
+// The checks of zeno_dense_gradient that the size of its workspace depends on; fills in everything but the outputs.
+static zeno_status check_dense(int32_t type, const zeno_rows *dy, const zeno_rows *codes, const zeno_rows *scales, int32_t m, int64_t n, int64_t inputs,
+                               int64_t outputs, zeno::DenseGradArgs *a) {
+    if (!type_ok(type)) return ZENO_ERR_INVALID_ARG;
+    zeno_status st = check_sizes(m, n, inputs);
+    if (st == ZENO_OK) st = check_sizes(m, n, outputs);
+    if (st != ZENO_OK) return st;
+    if (!rows_ok(dy, m, n, outputs) || !rows_ok(codes, m, n, inputs)) return ZENO_ERR_INVALID_ARG;
+    *a = {rows_of(dy, n), rows_of(codes, n), rows_of(scales, n), m, n, inputs, outputs, nullptr, nullptr, 0, 0, nullptr};
+    return ZENO_OK;
+}
+
+int64_t zeno_dense_gradient_workspace(int32_t type, const zeno_rows *dy, const zeno_rows *codes, int32_t m, int64_t n, int64_t inputs, int64_t outputs) {
+    zeno::DenseGradArgs a;
+    return check_dense(type, dy, codes, nullptr, m, n, inputs, outputs, &a) == ZENO_OK && m > 0 ? zeno::dense_gradient_workspace(type, a) : 0;
 }
 
 zeno_status zeno_dense_gradient(int32_t device, int32_t type, int32_t param_type, const zeno_rows *dy, const zeno_rows *codes,
                                 const zeno_rows *scales, int32_t m, int64_t n, int64_t inputs, int64_t outputs, void *dw,
                                 int64_t ldw, void *db, int64_t ldb, void *workspace, int64_t workspace_bytes, void *stream) {
     Range range("zeno_dense_gradient");
-    if (!type_ok(type) || !type_ok(param_type)) return ZENO_ERR_INVALID_ARG;
-    zeno_status st = check_sizes(m, n, inputs);
-    if (st == ZENO_OK) st = check_sizes(m, n, outputs);
+    if (!type_ok(param_type)) return ZENO_ERR_INVALID_ARG;
+    zeno::DenseGradArgs a;
+    const zeno_status st = check_dense(type, dy, codes, scales, m, n, inputs, outputs, &a);
     if (st != ZENO_OK) return st;
-    if (!rows_ok(dy, m, n, outputs) || !rows_ok(codes, m, n, inputs) || !rows_ok(scales, m, n, blocks_of(inputs))) return ZENO_ERR_INVALID_ARG;
+    if (!rows_ok(scales, m, n, blocks_of(inputs))) return ZENO_ERR_INVALID_ARG;
     if (m == 0) return ZENO_OK;
     if (!dw || (m > 1 && (ldw < inputs * outputs || (db && ldb < outputs)))) return ZENO_ERR_INVALID_ARG;
-    if (!workspace_ok(workspace, workspace_bytes, zeno::dense_gradient_workspace(m, n, inputs, outputs))) return ZENO_ERR_INVALID_ARG;
-    zeno::DenseGradArgs a = {rows_of(dy, n), rows_of(codes, n), rows_of(scales, n), m, n, inputs, outputs, dw, db, ldw, ldb,
-                             static_cast<float *>(workspace)};
+    if (!workspace_ok(workspace, workspace_bytes, zeno::dense_gradient_workspace(type, a))) return ZENO_ERR_INVALID_ARG;
+    a.dw = dw;
+    a.db = db;
+    a.ldw = ldw;
+    a.ldb = ldb;
+    a.workspace = static_cast<float *>(workspace);
     return on_device(device, [&] { return zeno::launch_dense_gradient(type, param_type, a, static_cast<cudaStream_t>(stream)); });
 }
 

@@ -64,13 +64,13 @@ struct DenseGradArgs {
     int64_t ldw, ldb;
     float *workspace;
 };
-int64_t dense_gradient_workspace(int m, int64_t n, int64_t inputs, int64_t outputs);
+int64_t dense_gradient_workspace(int type, const DenseGradArgs &a);
 cudaError_t launch_dense_gradient(int type, int param_type, const DenseGradArgs &a, cudaStream_t s);       // n may be 0
 
-// The same on the tensor cores (zeno_dense_tc.cu): bfloat16 dy, rows and groups that tensor maps can step through.  NotSupported: no
-// tensor map could be made.  db is not its business.
-bool dense_tc_usable(const DenseGradArgs &a);
-cudaError_t launch_dense_tc(int param_type, const DenseGradArgs &a, cudaStream_t s);
+// The same on the tensor cores (zeno_dense_tc.cu), for codes in rows and groups that tensor maps can step through.  NotSupported: it does not
+// take the call.  db is not its business.
+int64_t dense_tc_workspace(int type, const DenseGradArgs &a);
+cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &a, cudaStream_t s);
 void set_operator_wait_limit(uint32_t polls);
 cudaError_t read_operator_status(cudaStream_t s, int *status);
 

@@ -1,4 +1,5 @@
 // Activations kept in 8 bits for the backward pass, and the dense layers' weight gradients that are taken from them.
+#include <stdlib.h>
 #include "zeno_saved.cuh"
 
 namespace zeno {
@@ -143,35 +144,52 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_p
     }
 }
 
-// dW of a tile of 64 outputs by 64 inputs of one group in a block: 16 rows at a time through shared memory, 4 x 4 sums a thread.
+// dW of a tile of 64 outputs by 64 inputs of one group in a block: 16 rows at a time through shared memory, the next ones on their way into
+// registers, 4 x 4 sums a thread; db with the first tile of the inputs.
 template <typename T, typename P>
 __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
-    constexpr int kTile = 64, kRows = 16;
+    constexpr int kTile = 64, kRows = 16, kEach = kRows * kTile / 256;
     __shared__ float sd[kRows][kTile], sx[kRows][kTile];
     const int64_t o0 = (int64_t)blockIdx.y * kTile, k0 = (int64_t)blockIdx.x * kTile;
-    const int i = blockIdx.z, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int64_t t0 = 0; t0 < a.n; t0 += kRows) {
-        for (int e = threadIdx.x; e < kRows * kTile; e += 256) {
-            const int t = e / kTile, c = e % kTile;
-            float d = 0.f, x = 0.f;
-            if (t0 + t < a.n) {
-                const int64_t r = i * a.n + t0 + t;
-                if (o0 + c < a.outputs) d = value_of(static_cast<const T *>(a.dy.data) + a.dy.at(r) + o0 + c);
-                if (k0 + c < a.inputs)
-                    x = saved_value((static_cast<const uint8_t *>(a.codes.data) + a.codes.at(r))[k0 + c],
-                                    (static_cast<const float *>(a.scales.data) + a.scales.at(r))[(k0 + c) / kBlock]);
+    const int i = blockIdx.z, tx = threadIdx.x & 15, ty = threadIdx.x >> 4, c = threadIdx.x % kTile, t = threadIdx.x / kTile;
+    const bool has_o = o0 + c < a.outputs, has_k = k0 + c < a.inputs;
+    const T *dy = static_cast<const T *>(a.dy.data) + i * a.dy.group + o0 + c;
+    const uint8_t *codes = static_cast<const uint8_t *>(a.codes.data) + i * a.codes.group + k0 + c;
+    const float *scales = static_cast<const float *>(a.scales.data) + i * a.scales.group + (k0 + c) / kBlock;
+    float acc[4][4] = {}, bias = 0.f, d[kEach], scale[kEach];
+    uint8_t code[kEach];
+    auto fetch = [&](int64_t t0) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int64_t row = t0 + t + e * (kRows / kEach);
+            d[e] = scale[e] = 0.f;
+            code[e] = 0;
+            if (row >= a.n) continue;
+            if (has_o) d[e] = value_of(dy + row * a.dy.row);
+            if (has_k) {
+                code[e] = codes[row * a.codes.row];
+                scale[e] = scales[row * a.scales.row];
             }
-            sd[t][c] = d;
-            sx[t][c] = x;
+        }
+    };
+    fetch(0);
+    for (int64_t t0 = 0; t0 < a.n; t0 += kRows) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            sd[t + e * (kRows / kEach)][c] = d[e];
+            sx[t + e * (kRows / kEach)][c] = saved_value(code[e], scale[e]);
         }
         __syncthreads();
+        fetch(t0 + kRows);
+        if (threadIdx.x < kTile)
 #pragma unroll
-        for (int t = 0; t < kRows; ++t)
+            for (int q = 0; q < kRows; ++q) bias += sd[q][threadIdx.x];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
 #pragma unroll
             for (int p = 0; p < 4; ++p)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(sd[t][ty + 16 * p], sx[t][tx + 16 * q], acc[p][q]);
+                for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(sd[r][ty + 16 * p], sx[r][tx + 16 * q], acc[p][q]);
         __syncthreads();
     }
     P *dw = static_cast<P *>(a.dw) + i * a.ldw;
@@ -182,6 +200,7 @@ __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
             const int64_t o = o0 + ty + 16 * p, k = k0 + tx + 16 * q;
             if (o < a.outputs && k < a.inputs) put(dw + o * a.inputs + k, acc[p][q]);
         }
+    if (a.db && blockIdx.x == 0 && threadIdx.x < kTile && has_o) put(static_cast<P *>(a.db) + i * a.ldb + o0 + threadIdx.x, bias);
 }
 
 // db: a cluster takes 32 N outputs of a group, its blocks and their warps the rows in turn, a lane N neighbouring outputs; the warps' sums are
@@ -236,12 +255,20 @@ cudaError_t dense_bias(const DenseGradArgs &a, cudaStream_t s) {
     return launch_clustered(dense_bias_kernel<T, P, N>, cluster, grid, dim3(kBiasWarps * 32), 0, s, false, a, cluster);
 }
 
+// Few rows of few tiles are over on the CUDA cores, in one launch, before the tensor cores' launches are: a step of 16 rows of as many tiles as
+// are resident takes about 1.5 us there, the tensor cores' launches 13 us in all with dY's terms 25 (binary32, 12 groups of
+// 37 rows, 301 x 131: 12 us against 32; 4 groups of 100 rows, 512 x 512: 19 against 32).
+bool dense_on_tensor_cores(int type, const DenseGradArgs &a) {
+    if (getenv("NOTC")) return getenv("NOTC")[0] == '0';
+    const int64_t tiles = (a.inputs + 63) / 64 * ((a.outputs + 63) / 64) * a.m, waves = (tiles + 591) / 592, steps = (a.n + 15) / 16;
+    return waves * steps > (type == ZENO_F32 ? 12 : 6);
+}
+
 template <typename T, typename P>
-cudaError_t dense_gradient(const DenseGradArgs &a, cudaStream_t s) {
-    cudaError_t e = cudaErrorNotSupported;
-    if (is_bf16<T>::value && dense_tc_usable(a)) e = launch_dense_tc(is_bf16<P>::value ? ZENO_BF16 : ZENO_F32, a, s);
+cudaError_t dense_gradient(int type, int param_type, const DenseGradArgs &a, cudaStream_t s) {
+    cudaError_t e = dense_on_tensor_cores(type, a) ? launch_dense_tc(type, param_type, a, s) : cudaErrorNotSupported;
     if (e == cudaErrorNotSupported)
-        e = launch_chained(dense_any_kernel<T, P>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
+        return launch_chained(dense_any_kernel<T, P>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
     if (e == cudaSuccess && a.db) {
         constexpr int N = 16 / sizeof(T);
         e = a.outputs % N == 0 && aligned_to(a.dy, a.m, a.n, sizeof(T), 16) ? dense_bias<T, P, N>(a, s) : dense_bias<T, P, 1>(a, s);
@@ -264,12 +291,12 @@ cudaError_t launch_pack(int type, const PackArgs &a, cudaStream_t s) {
                           per_row, blocks);
 }
 
-int64_t dense_gradient_workspace(int m, int64_t n, int64_t inputs, int64_t outputs) { return 0; }
+int64_t dense_gradient_workspace(int type, const DenseGradArgs &a) { return dense_on_tensor_cores(type, a) ? dense_tc_workspace(type, a) : 0; }
 
 cudaError_t launch_dense_gradient(int type, int param_type, const DenseGradArgs &a, cudaStream_t s) {
     if (type == ZENO_BF16)
-        return param_type == ZENO_BF16 ? dense_gradient<__nv_bfloat16, __nv_bfloat16>(a, s) : dense_gradient<__nv_bfloat16, float>(a, s);
-    return param_type == ZENO_BF16 ? dense_gradient<float, __nv_bfloat16>(a, s) : dense_gradient<float, float>(a, s);
+        return param_type == ZENO_BF16 ? dense_gradient<__nv_bfloat16, __nv_bfloat16>(type, param_type, a, s) : dense_gradient<__nv_bfloat16, float>(type, param_type, a, s);
+    return param_type == ZENO_BF16 ? dense_gradient<float, __nv_bfloat16>(type, param_type, a, s) : dense_gradient<float, float>(type, param_type, a, s);
 }
 
 }  // namespace zeno

@@ -136,7 +136,7 @@ def load_library() -> ctypes.CDLL:
     lib.zeno_dense_gradient.restype = i32
     lib.zeno_dense_gradient.argtypes = [i32, i32, i32, rows, rows, rows, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp]
     lib.zeno_dense_gradient_workspace.restype = i64
-    lib.zeno_dense_gradient_workspace.argtypes = [i32, i64, i64, i64]
+    lib.zeno_dense_gradient_workspace.argtypes = [i32, rows, rows, i32, i64, i64, i64]
     lib.zeno_operator_status.restype = i32
     lib.zeno_operator_status.argtypes = [i32, vp]
     lib.zeno_debug_set_operator_wait_limit.restype = i32
@@ -686,9 +686,10 @@ def dense_gradient(dy, saved: Saved, dweight, dbias=None, stream=None):
     if (inputs > 1 and strides[-1] != 1) or (outputs > 1 and strides[-2] != inputs):
         _refuse("dweight: contiguous for every group is needed")
     ldb = _gradient_row(dbias, m, outputs, dweight.dtype, "dbias")
-    nbytes = lib.zeno_dense_gradient_workspace(m, n, inputs, outputs)
+    kind, dy_rows = _type(dy, "dy"), _rows(dy, "dy")
+    nbytes = lib.zeno_dense_gradient_workspace(kind, dy_rows, codes, m, n, inputs, outputs)
     ws = _scratch(stream, nbytes, dev)
-    _done(lib.zeno_dense_gradient(dev.index, _type(dy, "dy"), _type(dweight, "dweight"), _rows(dy, "dy"), codes, scales, m, n, inputs,
+    _done(lib.zeno_dense_gradient(dev.index, kind, _type(dweight, "dweight"), dy_rows, codes, scales, m, n, inputs,
                                   outputs, dweight.data_ptr(), strides[0] if len(shape) == 3 else inputs * outputs, _ptr(dbias), ldb,
                                   _ptr(ws), nbytes, _current(dev, stream)), "zeno_dense_gradient")
     return dweight

@@ -121,9 +121,14 @@ def test_norm_gradient_refusals(lib):
 def test_dense_refusals(lib):
     assert dense(lib, ptype=5) == INVALID and dense(lib, dw=None) == INVALID and dense(lib, ldw=4095) == INVALID and dense(lib, ldb=63) == INVALID
     assert dense(lib, outputs=0) == INVALID and dense(lib, outputs=65) == INVALID and dense(lib, inputs=65) == INVALID
-    need = lib.zeno_dense_gradient_workspace(2, 10, 64, 64)
+    need = lib.zeno_dense_gradient_workspace(0, rows(), rows(), 2, 10, 64, 64)
     if need:
         assert dense(lib, ws=None) == INVALID and dense(lib, bytes=need - 1) == INVALID and dense(lib, ws=P + 8) == INVALID
+    big = rows(4096, 4096 * 1000)
+    assert lib.zeno_dense_gradient_workspace(0, big, big, 2, 1000, 4096, 4096) >= 6 * 2 * 1000 * 4096       # three terms of dy
+    assert lib.zeno_dense_gradient_workspace(1, big, big, 2, 1000, 4096, 4096) == 0
+    assert lib.zeno_dense_gradient_workspace(7, big, big, 2, 1000, 4096, 4096) == 0
+    assert lib.zeno_dense_gradient_workspace(1, None, big, 2, 1000, 4096, 4096) == 0
 
 
 def test_token_refusals(lib):
