@@ -1,5 +1,4 @@
 // Activations kept in 8 bits for the backward pass, and the dense layers' weight gradients that are taken from them.
-#include <stdlib.h>
 #include "zeno_saved.cuh"
 
 namespace zeno {
@@ -259,7 +258,6 @@ cudaError_t dense_bias(const DenseGradArgs &a, cudaStream_t s) {
 // are resident takes about 1.5 us there, the tensor cores' launches 13 us in all with dY's terms 25 (binary32, 12 groups of
 // 37 rows, 301 x 131: 12 us against 32; 4 groups of 100 rows, 512 x 512: 19 against 32).
 bool dense_on_tensor_cores(int type, const DenseGradArgs &a) {
-    if (getenv("NOTC")) return getenv("NOTC")[0] == '0';
     const int64_t tiles = (a.inputs + 63) / 64 * ((a.outputs + 63) / 64) * a.m, waves = (tiles + 591) / 592, steps = (a.n + 15) / 16;
     return waves * steps > (type == ZENO_F32 ? 12 : 6);
 }
