@@ -484,7 +484,12 @@ class TokenLogprobs(NamedTuple):
 
 
 # Calls of a few tokens are over on the GPU in a few microseconds, so here too what the binding spends on a call shows: messages are built only for
-# a refusal, shapes and strides are read once, empty_like is preferred.
+# a refusal, shapes and strides are read once, devices are compared by their index, empty_like (half as dear) is preferred.
+_DEVICES = [torch.device("cuda", i) for i in range(64)]
+_EMPTY, _EMPTY_LIKE = torch.empty, torch.empty_like
+_ROWS = RowsDesc
+
+
 def _refuse(what: str):
     raise ValueError(what)
 
@@ -506,11 +511,10 @@ def _rows(t: torch.Tensor, name: str) -> RowsDesc:
         _refuse(f"{name}: [m, n, columns] or [n, columns] is needed, not {tuple(t.shape)}")
     if last != 1 and t.shape[-1] > 1:
         _refuse(f"{name}: the last stride has to be 1")
-    return RowsDesc(t.data_ptr(), row, group)
+    return _ROWS(t.data_ptr(), row, group)
 
 
-def _sizes(t: torch.Tensor):
-    shape = t.shape
+def _sizes(shape):
     if len(shape) == 3:
         return shape
     if len(shape) != 2:
@@ -518,58 +522,61 @@ def _sizes(t: torch.Tensor):
     return 1, shape[0], shape[1]
 
 
-def _cuda(dev: torch.device, *tensors):
-    if dev.type != "cuda":
+def _device(t: torch.Tensor, *others) -> int:
+    """The index of the device that all of the tensors (or None) are on."""
+    index = t.get_device()
+    if index < 0:
         _refuse("CUDA tensors are needed")
-    for t in tensors:
-        if t is not None and t.device != dev:
-            _refuse(f"CUDA tensors on one device are needed, not {dev} and {t.device}")
+    for o in others:
+        if o is not None and o.get_device() != index:
+            _refuse(f"CUDA tensors on one device are needed, not {t.device} and {o.device}")
+    return index
 
 
-def _per_token(t: Optional[torch.Tensor], lead, dtype, name: str):
-    if t is not None and (t.dtype != dtype or t.shape != lead or not t.is_contiguous()):
+def _per_token(t: torch.Tensor, lead, dtype, name: str):
+    if t.dtype != dtype or t.shape != lead or not t.is_contiguous():
         _refuse(f"{name}: contiguous {dtype} {tuple(lead)} is needed")
 
 
-def _current(dev: torch.device, stream) -> int:
+def _current(index: int, stream) -> int:
     if stream is not None:
         return stream.cuda_stream
     if _raw_stream is None:
-        return torch.cuda.current_stream(dev).cuda_stream
-    return _raw_stream(dev.index)
+        return torch.cuda.current_stream(index).cuda_stream
+    return _raw_stream(index)
 
 
-def _empty(stream, dev: torch.device, shape, dtype) -> torch.Tensor:
+def _empty(stream, index: int, shape, dtype) -> torch.Tensor:
     """An output or scratch: memory of the stream that the call runs on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return _EMPTY(shape, dtype=dtype, device=_DEVICES[index])
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return _EMPTY(shape, dtype=dtype, device=_DEVICES[index])
 
 
 def _empty_like(stream, t: torch.Tensor, dtype=None) -> torch.Tensor:
-    """The same in the shape of t (and its order of dimensions), at less than half the cost."""
+    """The same in the shape of t (and its order of dimensions)."""
     if stream is None:
-        return torch.empty_like(t, dtype=dtype)
+        return _EMPTY_LIKE(t, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty_like(t, dtype=dtype)
-
-
-def _scratch(stream, nbytes: int, dev: torch.device):
-    return _empty(stream, dev, nbytes, torch.uint8) if nbytes else None
+        return _EMPTY_LIKE(t, dtype=dtype)
 
 
 def _done(st: int, what: str):
-    if st != OK:
-        raise ZenoError(st, what)
+    raise ZenoError(st, what)
 
 
-def _norm_weight(w: torch.Tensor, m: int, cols: int, name: str) -> int:
+def _norm_weight(w: torch.Tensor, m: int, cols: int) -> int:
     """Elements between the groups' weights: 0 if they share them."""
     shape = w.shape
-    if shape[-1] != cols or not (len(shape) == 1 or (len(shape) == 2 and shape[0] == m)) or (cols > 1 and w.stride(-1) != 1):
-        _refuse(f"{name}: [{cols}] or [{m}, {cols}] with a last stride of 1 is needed")
-    return w.stride(0) if len(shape) == 2 and m > 1 else 0
+    if len(shape) == 1:
+        if shape[0] == cols and (cols == 1 or w.stride(0) == 1):
+            return 0
+    elif len(shape) == 2 and shape[0] == m and shape[1] == cols:
+        row, last = w.stride()
+        if last == 1 or cols == 1:
+            return row if m > 1 else 0
+    _refuse(f"weight and bias: [{cols}] or [{m}, {cols}] with a last stride of 1 is needed")
 
 
 def _alike(t: torch.Tensor, like: torch.Tensor, name: str):
@@ -581,11 +588,11 @@ def layer_norm(x, weight, bias=None, eps=1e-5, out=None, want_stats=True, stream
     """zeno_layer_norm: returns (y, mean or None, rstd or None).  weight, bias: [columns], or [m, columns] where every model has its own (of one
     stride: slices of the models' parameter vectors).  out may be x."""
     lib = load_library()
-    dev = x.device
-    m, n, cols = _sizes(x)
-    _cuda(dev, weight, bias, out)
-    ldw = _norm_weight(weight, m, cols, "weight")
-    if bias is not None and (bias.dtype != weight.dtype or bias.shape != weight.shape or _norm_weight(bias, m, cols, "bias") != ldw):
+    shape = x.shape
+    m, n, cols = _sizes(shape)
+    dev = _device(x, weight, bias, out)
+    ldw = _norm_weight(weight, m, cols)
+    if bias is not None and (bias.dtype != weight.dtype or bias.shape != weight.shape or _norm_weight(bias, m, cols) != ldw):
         _refuse("bias: the type and layout of the weight is needed")
     if out is None:
         out = _empty_like(stream, x)
@@ -593,11 +600,11 @@ def layer_norm(x, weight, bias=None, eps=1e-5, out=None, want_stats=True, stream
         _alike(out, x, "out")
     mean = rstd = None
     if want_stats:
-        mean = _empty(stream, dev, x.shape[:-1], torch.float32)
+        mean = _empty(stream, dev, shape[:-1], torch.float32)
         rstd = _empty_like(stream, mean)
-    _done(lib.zeno_layer_norm(dev.index, _type(x, "x"), _type(weight, "weight"), _rows(x, "x"), m, n, cols, weight.data_ptr(),
-                              _ptr(bias), ldw, eps, _rows(out, "out"), _ptr(mean), _ptr(rstd), _current(dev, stream)), "zeno_layer_norm")
-    return out, mean, rstd
+    st = lib.zeno_layer_norm(dev, _type(x, "x"), _type(weight, "weight"), _rows(x, "x"), m, n, cols, weight.data_ptr(), _ptr(bias), ldw, eps,
+                             _rows(out, "out"), _ptr(mean), _ptr(rstd), _current(dev, stream))
+    return (out, mean, rstd) if st == OK else _done(st, "zeno_layer_norm")
 
 
 def _saved_rows(saved, lead, cols: int):
@@ -609,13 +616,17 @@ def _saved_rows(saved, lead, cols: int):
     return _rows(codes, "codes"), _rows(scales, "scales")
 
 
-def _gradient_row(t: Optional[torch.Tensor], m: int, cols: int, dtype, name: str) -> int:
-    if t is None:
-        return 0
+def _gradient_row(t: torch.Tensor, m: int, cols: int, dtype, name: str) -> int:
+    """Elements between the groups' gradients."""
     shape = t.shape
-    if t.dtype != dtype or not (shape == (m, cols) or (m == 1 and shape == (cols,))) or (cols > 1 and t.stride(-1) != 1):
-        _refuse(f"{name}: {dtype} [{m}, {cols}] with a last stride of 1 is needed")
-    return t.stride(0) if len(shape) == 2 else cols
+    if t.dtype == dtype:
+        if len(shape) == 2 and shape[0] == m and shape[1] == cols:
+            row, last = t.stride()
+            if last == 1 or cols == 1:
+                return row
+        elif m == 1 and len(shape) == 1 and shape[0] == cols and (cols == 1 or t.stride(0) == 1):
+            return cols
+    _refuse(f"{name}: {dtype} [{m}, {cols}] with a last stride of 1 is needed")
 
 
 def layer_norm_gradient(dy, x: Union[torch.Tensor, Saved], weight, mean, rstd, dweight=None, dbias=None, dx=None, want_dx=True,
@@ -623,20 +634,23 @@ def layer_norm_gradient(dy, x: Union[torch.Tensor, Saved], weight, mean, rstd, d
     """zeno_layer_norm_gradient: writes dweight and dbias ([m, columns], for instance V[:, at:at + columns], of one stride) and
     returns dx (None if not wanted).  x: the layer's input, or what pack_activations kept of it.  dx may be dy."""
     lib = load_library()
-    dev, lead = dy.device, dy.shape[:-1]
-    m, n, cols = _sizes(dy)
+    shape = dy.shape
+    lead = shape[:-1]
+    m, n, cols = _sizes(shape)
     x_rows = codes = scales = None
     if isinstance(x, tuple):
-        _cuda(dev, x[0], x[1], weight, mean, rstd, dweight, dbias, dx)
+        dev = _device(dy, x[0], x[1], weight, mean, rstd, dweight, dbias, dx)
         codes, scales = _saved_rows(x, lead, cols)
     else:
-        _cuda(dev, x, weight, mean, rstd, dweight, dbias, dx)
+        dev = _device(dy, x, weight, mean, rstd, dweight, dbias, dx)
         _alike(x, dy, "x")
         x_rows = _rows(x, "x")
     _per_token(mean, lead, torch.float32, "mean")
     _per_token(rstd, lead, torch.float32, "rstd")
-    ldw = _norm_weight(weight, m, cols, "weight")
-    ldg = _gradient_row(dweight, m, cols, weight.dtype, "dweight")
+    ldw = _norm_weight(weight, m, cols)
+    ldg = 0
+    if dweight is not None:
+        ldg = _gradient_row(dweight, m, cols, weight.dtype, "dweight")
     if dbias is not None:
         ldb = _gradient_row(dbias, m, cols, weight.dtype, "dbias")
         if dweight is None:
@@ -648,26 +662,26 @@ def layer_norm_gradient(dy, x: Union[torch.Tensor, Saved], weight, mean, rstd, d
     elif want_dx:
         dx = _empty_like(stream, dy)
     nbytes = lib.zeno_layer_norm_gradient_workspace(m, n, cols)
-    ws = _scratch(stream, nbytes, dev)
-    _done(lib.zeno_layer_norm_gradient(dev.index, _type(dy, "dy"), _type(weight, "weight"), _rows(dy, "dy"), x_rows, codes, scales, m, n, cols,
-                                       weight.data_ptr(), ldw, mean.data_ptr(), rstd.data_ptr(), None if dx is None else _rows(dx, "dx"),
-                                       _ptr(dweight), _ptr(dbias), ldg, _ptr(ws), nbytes, _current(dev, stream)), "zeno_layer_norm_gradient")
-    return dx
+    ws = _empty(stream, dev, nbytes, torch.uint8) if nbytes else None
+    st = lib.zeno_layer_norm_gradient(dev, _type(dy, "dy"), _type(weight, "weight"), _rows(dy, "dy"), x_rows, codes, scales, m, n, cols,
+                                      weight.data_ptr(), ldw, mean.data_ptr(), rstd.data_ptr(), None if dx is None else _rows(dx, "dx"),
+                                      _ptr(dweight), _ptr(dbias), ldg, _ptr(ws), nbytes, _current(dev, stream))
+    return dx if st == OK else _done(st, "zeno_layer_norm_gradient")
 
 
 def pack_activations(x, stream=None) -> Saved:
     """zeno_pack_activations: x in 8 bits, for layer_norm_gradient and dense_gradient."""
     lib = load_library()
-    dev, lead = x.device, x.shape[:-1]
-    m, n, cols = _sizes(x)
-    _cuda(dev)
+    shape = x.shape
+    lead = shape[:-1]
+    m, n, cols = _sizes(shape)
+    dev = _device(x)
     codes = _empty(stream, dev, (*lead, -(-cols // 16) * 16), torch.float8_e4m3fn)
     if cols % 16:
         codes = codes[..., :cols]
     scales = _empty(stream, dev, (*lead, -(-cols // SAVED_BLOCK)), torch.float32)
-    _done(lib.zeno_pack_activations(dev.index, _type(x, "x"), _rows(x, "x"), m, n, cols, _rows(codes, "codes"), _rows(scales, "scales"),
-                                    _current(dev, stream)), "zeno_pack_activations")
-    return Saved(codes, scales)
+    st = lib.zeno_pack_activations(dev, _type(x, "x"), _rows(x, "x"), m, n, cols, _rows(codes, "codes"), _rows(scales, "scales"), _current(dev, stream))
+    return Saved(codes, scales) if st == OK else _done(st, "zeno_pack_activations")
 
 
 def dense_gradient(dy, saved: Saved, dweight, dbias=None, stream=None):
@@ -675,34 +689,35 @@ def dense_gradient(dy, saved: Saved, dweight, dbias=None, stream=None):
     dweight: [m, outputs, inputs] (or without m), contiguous per group, for instance
     V[:, at:at + outputs * inputs].unflatten(1, (outputs, inputs)); dbias: [m, outputs]."""
     lib = load_library()
-    dev = dy.device
-    m, n, outputs = _sizes(dy)
+    dy_shape = dy.shape
+    m, n, outputs = _sizes(dy_shape)
     inputs = saved[0].shape[-1]
-    _cuda(dev, saved[0], saved[1], dweight, dbias)
-    codes, scales = _saved_rows(saved, dy.shape[:-1], inputs)
+    dev = _device(dy, saved[0], saved[1], dweight, dbias)
+    codes, scales = _saved_rows(saved, dy_shape[:-1], inputs)
     shape, strides = dweight.shape, dweight.stride()
     if not (shape == (m, outputs, inputs) or (m == 1 and shape == (outputs, inputs))):
         _refuse(f"dweight: [{m}, {outputs}, {inputs}] is needed")
     if (inputs > 1 and strides[-1] != 1) or (outputs > 1 and strides[-2] != inputs):
         _refuse("dweight: contiguous for every group is needed")
-    ldb = _gradient_row(dbias, m, outputs, dweight.dtype, "dbias")
+    ldb = 0 if dbias is None else _gradient_row(dbias, m, outputs, dweight.dtype, "dbias")
     kind, dy_rows = _type(dy, "dy"), _rows(dy, "dy")
     nbytes = lib.zeno_dense_gradient_workspace(kind, dy_rows, codes, m, n, inputs, outputs)
-    ws = _scratch(stream, nbytes, dev)
-    _done(lib.zeno_dense_gradient(dev.index, kind, _type(dweight, "dweight"), dy_rows, codes, scales, m, n, inputs,
-                                  outputs, dweight.data_ptr(), strides[0] if len(shape) == 3 else inputs * outputs, _ptr(dbias), ldb,
-                                  _ptr(ws), nbytes, _current(dev, stream)), "zeno_dense_gradient")
-    return dweight
+    ws = _empty(stream, dev, nbytes, torch.uint8) if nbytes else None
+    st = lib.zeno_dense_gradient(dev, kind, _type(dweight, "dweight"), dy_rows, codes, scales, m, n, inputs, outputs, dweight.data_ptr(),
+                                 strides[0] if len(shape) == 3 else inputs * outputs, _ptr(dbias), ldb, _ptr(ws), nbytes, _current(dev, stream))
+    return dweight if st == OK else _done(st, "zeno_dense_gradient")
 
 
 def token_logprobs(logits, targets=None, top=0, stream=None) -> TokenLogprobs:
     """zeno_token_logprobs: (logprobs or None without targets, entropy, lse, top_idx, top_logprobs (None if top is 0)) of logits [m, n, vocab] or
     [n, vocab]; targets: int32, one outside the vocabulary means none."""
     lib = load_library()
-    m, n, vocab = _sizes(logits)
-    dev, lead = logits.device, logits.shape[:-1]
-    _cuda(dev, targets)
-    _per_token(targets, lead, torch.int32, "targets")
+    shape = logits.shape
+    lead = shape[:-1]
+    m, n, vocab = _sizes(shape)
+    dev = _device(logits, targets)
+    if targets is not None:
+        _per_token(targets, lead, torch.int32, "targets")
     entropy = _empty(stream, dev, lead, torch.float32)
     lse = _empty_like(stream, entropy)
     lp = None if targets is None else _empty_like(stream, entropy)
@@ -710,18 +725,19 @@ def token_logprobs(logits, targets=None, top=0, stream=None) -> TokenLogprobs:
     if top > 0:
         idx = _empty(stream, dev, (*lead, top), torch.int32)
         top_lp = _empty_like(stream, idx, torch.float32)
-    _done(lib.zeno_token_logprobs(dev.index, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, _ptr(targets), top, _ptr(lp),
-                                  entropy.data_ptr(), lse.data_ptr(), _ptr(idx), _ptr(top_lp), _current(dev, stream)), "zeno_token_logprobs")
-    return TokenLogprobs(lp, entropy, lse, idx, top_lp)
+    st = lib.zeno_token_logprobs(dev, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, _ptr(targets), top, _ptr(lp),
+                                 entropy.data_ptr(), lse.data_ptr(), _ptr(idx), _ptr(top_lp), _current(dev, stream))
+    return TokenLogprobs(lp, entropy, lse, idx, top_lp) if st == OK else _done(st, "zeno_token_logprobs")
 
 
 def token_gradient(logits, targets, lse, g_logprob, entropy=None, g_entropy=None, out=None, stream=None):
     """zeno_token_gradient: the gradient at the logits from the gradients at token_logprobs's logprobs and (g_entropy) entropy.
     out may be the logits."""
     lib = load_library()
-    dev, lead = logits.device, logits.shape[:-1]
-    m, n, vocab = _sizes(logits)
-    _cuda(dev, targets, lse, g_logprob, entropy, g_entropy, out)
+    shape = logits.shape
+    lead = shape[:-1]
+    m, n, vocab = _sizes(shape)
+    dev = _device(logits, targets, lse, g_logprob, entropy, g_entropy, out)
     _per_token(targets, lead, torch.int32, "targets")
     _per_token(lse, lead, torch.float32, "lse")
     _per_token(g_logprob, lead, torch.float32, "g_logprob")
@@ -734,15 +750,16 @@ def token_gradient(logits, targets, lse, g_logprob, entropy=None, g_entropy=None
         out = _empty_like(stream, logits)
     else:
         _alike(out, logits, "out")
-    _done(lib.zeno_token_gradient(dev.index, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, targets.data_ptr(), lse.data_ptr(),
-                                  _ptr(entropy), g_logprob.data_ptr(), _ptr(g_entropy), _rows(out, "out"), _current(dev, stream)),
-          "zeno_token_gradient")
-    return out
+    st = lib.zeno_token_gradient(dev, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, targets.data_ptr(), lse.data_ptr(),
+                                 _ptr(entropy), g_logprob.data_ptr(), _ptr(g_entropy), _rows(out, "out"), _current(dev, stream))
+    return out if st == OK else _done(st, "zeno_token_gradient")
 
 
 def check_operator_status(device: int = 0, stream=None):
     """Synchronises and raises if a kernel of the operators above gave up on a bounded device-side wait (dense_gradient on the tensor cores has them)."""
-    _done(load_library().zeno_operator_status(device, _current(torch.device("cuda", device), stream)), "zeno_operator_status")
+    st = load_library().zeno_operator_status(device, _current(device, stream))
+    if st != OK:
+        _done(st, "zeno_operator_status")
 
 
 def debug_set_operator_wait_limit(polls: int):

@@ -151,7 +151,7 @@ def test_binding_refuses_what_does_not_fit(lib):
 
 def test_binding_checks_shapes_types_and_layouts(lib, monkeypatch):
     """With the check of the device out of the way: nothing here reaches the library."""
-    monkeypatch.setattr(zeno, "_cuda", lambda *a, **k: None)
+    monkeypatch.setattr(zeno, "_device", lambda *a: 0)
     monkeypatch.setattr(zeno, "load_library", lambda: ctypes.CDLL(None))
     x = torch.zeros(2, 3, 8)
     w, s, t = torch.zeros(8), torch.zeros(2, 3), torch.zeros(2, 3, dtype=torch.int32)
@@ -180,7 +180,7 @@ def test_binding_checks_shapes_types_and_layouts(lib, monkeypatch):
 
 
 def test_operators_say_what_type_or_layout_they_need(monkeypatch, lib):
-    monkeypatch.setattr(zeno, "_cuda", lambda *a, **k: None)
+    monkeypatch.setattr(zeno, "_device", lambda *a: 0)
     with pytest.raises(ValueError, match="bfloat16"):
         zeno._type(torch.zeros(2, dtype=torch.float16), "x")
     for t in (torch.zeros(4), torch.zeros(2, 2, 2, 2), torch.zeros(2, 3, 8)[..., ::2], torch.zeros(8, 3).T):
