@@ -7,7 +7,7 @@
 // exact in bfloat16, products of bfloat16 are exact, and the sums stay binary32 in TMEM.
 //   warp 0: copies of the codes;  warp 3: of their scales;  warp 2: of dY;  warp 1 of the pair's first block: the instructions;
 // binary32 dY is rewritten as three bfloat16 terms first, which hold it exactly; few tiles are cut along the tokens.
-//   warps 4 - 11: codes to bfloat16;  warps 12 - 15: a finished tile from TMEM to dW while the next one is summed.
+//   warps 4 - 19: codes to bfloat16;  warps 20 - 23: a finished tile from TMEM to dW while the next one is summed.
 #include "zeno_saved.cuh"
 #include "zeno_tc.cuh"
 
@@ -15,7 +15,6 @@ namespace zeno {
 
 namespace {
 
-constexpr int kThreads = 512;
 constexpr int kTokens = 64;                   // tokens (the contraction index) of a stage
 constexpr int kHalf = 128;                    // outputs, and inputs, of a block
 constexpr int kPairTile = 2 * kHalf;
@@ -25,8 +24,10 @@ constexpr int kStages = 5, kCodeStages = 6;
 constexpr int kTurnBytes = 32 * 17 * 4;       // a warp's 32 x 16 sums on their way from rows to columns
 constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * (kCodeBytes + kScaleBytes) + 4 * kTurnBytes + 1024;
 // The warps that convert come in sets, which take the stages in turn: a stage is a chain of waits, loads, arithmetic, stores and an
-// arrival that one set alone would follow from end to end (8 x 2048 tokens, 4096 x 4096: one set 691 us, two 589, four 562).
-constexpr int kConvWarps = 8, kSets = 4, kSetWarps = kConvWarps / kSets, kEpiWarps = 4;
+// arrival that one set alone would follow from end to end (8 x 2048 tokens, 4096 x 4096, with
+// the bias: one set of eight warps 691 us, two of four 589, four of two 562 (536 by now); four of four 515).
+constexpr int kConvWarps = 16, kSets = 4, kSetWarps = kConvWarps / kSets, kEpiWarps = 4;
+constexpr int kThreads = 32 * (4 + kConvWarps + kEpiWarps);
 constexpr int kTmemCols = 512;                // two sets of 256 sums
 constexpr int kKernelId = 5;
 
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                     else mbar_arrive_cluster(remote_bready + s * 8);
                 }
             }
-    } else if (warp >= 12) {
+    } else if (warp >= 4 + kConvWarps) {
         // ------------------------------------------------------------------ finished tiles to dW
         const int quad = warp & 3;                                 // TMEM lanes this warp may access
         const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[2 * kCodeStages + 3 * kStages + 2], 0);

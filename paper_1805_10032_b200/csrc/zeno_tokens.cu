@@ -89,6 +89,21 @@ struct Sums {
     }
 };
 
+// the sums of the first COUNT lanes (a power of two), in those
+template <int COUNT>
+__device__ __forceinline__ Sums join_first(Sums w) {
+    float M = w.M;
+#pragma unroll
+    for (int k = COUNT / 2; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
+    w.move(M);
+#pragma unroll
+    for (int k = COUNT / 2; k >= 1; k >>= 1) {
+        w.s += __shfl_xor_sync(kAll, w.s, k);
+        w.e += __shfl_xor_sync(kAll, w.e, k);
+    }
+    return w;
+}
+
 // The unsigned half of rank_key: the order of the values, NaN with minus infinity
 __device__ __forceinline__ uint32_t order_of(float z) { return (uint32_t)(rank_key(z, 0) >> 32); }
 __device__ __forceinline__ float value_of_order(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
@@ -200,7 +215,7 @@ __device__ __noinline__ void top_by_lists(const T *z, int64_t head, int64_t v_be
 // threads' largest is a bound that k entries reach, and only about k threads have entries that do; theirs are read again (from
 // L2), and what reaches the bound is ranked by counting.
 template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ? 8 : 24) logprobs_kernel(LogprobArgs a, int parts) {
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ? 12 : 32) logprobs_kernel(LogprobArgs a, int parts) {
     using V = Vec<T>;
     constexpr int kWarps = THREADS / 32, kBatch = 4, kMaxParts = 8, kKeys = 512;
     static_assert(kKeys >= kWarps * kMaxTop && kKeys >= kMaxParts * kMaxTop, "the lists of all warps, of all parts");
@@ -218,13 +233,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
     const T *z = static_cast<const T *>(a.logits.data) + a.logits.at(r);
     const int top = a.top;
 
-    float zt = 0.f;
-    bool given = false;
-    if (threadIdx.x == 0 && part == 0 && a.logprobs) {
-        const int t = a.targets[r];
-        given = t >= 0 && t < a.vocab;
-        if (given) zt = value_of(z + t);
-    }
+    const int target = a.logprobs && threadIdx.x == 0 && part == 0 ? a.targets[r] : -1;     // its logit is asked for when this has come
     const int64_t head = head_of(z, a.vocab), vecs = (a.vocab - head) / V::N;
     const int64_t v_begin = vecs * part / parts, v_end = vecs * (part + 1) / parts;
     const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
@@ -247,7 +256,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int64_t v = base + i * 32 + lane;
-            raw[i] = v < v_end ? (TOP ? __ldg(zv + v) : __ldcs(zv + v)) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
+            raw[i] = v < v_end ? (TOP ? __ldcg(zv + v) : __ldcs(zv + v)) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
             any |= v < v_end;
         }
         float most = V::most(raw[0]);
@@ -271,6 +280,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
             }
         }
     }
+    const bool given = target >= 0 && target < a.vocab;
+    const float zt = given ? value_of(z + target) : 0.f;
     // what lies before the first vector and behind the last: fewer than 2 N entries
     const int64_t rest = part == 0 ? a.vocab - vecs * V::N : 0, rest_at = vecs * V::N;
     const int64_t rest_j = lane < head ? lane : rest_at + lane;
@@ -337,18 +348,31 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
         __syncthreads();
         const int threads = n_threads, per = (int)((v_end - v_begin + THREADS * kBatch - 1) / (THREADS * kBatch)) * kBatch;
         const bool few = threads <= 2 * top + 32;
-        if (few)
-            for (int i = threadIdx.x; i < threads * per; i += THREADS) {
-                const int who = (int)orders[i / per], k = i % per;
-                const int64_t v = v_begin + (int64_t)(k / kBatch) * THREADS * kBatch + (who >> 5) * 32 * kBatch + k % kBatch * 32 + (who & 31);
-                if (v < v_end) {
-                    const int64_t j = head + v * V::N;
-                    T e[V::N];
-                    *reinterpret_cast<uint4 *>(e) = __ldg(zv + v);
+        if (few) {
+            constexpr int kAtOnce = 4;                // loads in flight
+            for (int i0 = threadIdx.x; i0 < threads * per; i0 += THREADS * kAtOnce) {
+                uint4 raw[kAtOnce];
+                int64_t at[kAtOnce];
 #pragma unroll
-                    for (int n = 0; n < V::N; ++n) offer(value_of(e + n), j + n);
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const int i = i0 + u * THREADS;
+                    at[u] = v_end;
+                    if (i < threads * per) {
+                        const int who = (int)orders[i / per], k = i % per;
+                        at[u] = v_begin + (int64_t)(k / kBatch) * THREADS * kBatch + (who >> 5) * 32 * kBatch + k % kBatch * 32 + (who & 31);
+                    }
+                    if (at[u] < v_end) raw[u] = __ldcg(zv + at[u]);
                 }
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+                    if (at[u] < v_end && order_of(V::most(raw[u])) >= need) {
+                        T e[V::N];
+                        *reinterpret_cast<uint4 *>(e) = raw[u];
+#pragma unroll
+                        for (int n = 0; n < V::N; ++n) offer(value_of(e + n), head + at[u] * V::N + n);
+                    }
             }
+        }
         __syncthreads();
         if (few && n_keys <= kKeys) rank_keys<THREADS>(keys, n_keys, top, best);
         else top_by_lists<T, THREADS>(z, head, v_begin, v_end, rest, rest_at, top, need, keys, best);
@@ -357,12 +381,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
 
     // the warp's sums, the block's, the cluster's
     if (limit == -kFar) q.M = kUnset;
-    M = q.M;
-#pragma unroll
-    for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
-    q.move(M);
-    q.s = warp_sum(q.s);
-    q.e = warp_sum(q.e);
+    q = join_first<32>(q);
     if (THREADS > 32) {
         if (lane == 0) {
             warp_sums[warp][0] = q.M;
@@ -373,11 +392,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
         if (warp == 0) {
             Sums w = {lane < kWarps ? warp_sums[lane][0] : kUnset, lane < kWarps ? warp_sums[lane][1] : 0.f,
                       lane < kWarps ? warp_sums[lane][2] : 0.f};
-            M = w.M;
-#pragma unroll
-            for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
-            w.move(M);
-            q = {M, warp_sum(w.s), warp_sum(w.e)};
+            q = join_first<kWarps>(w);
         }
     }
     if (parts > 1) {
@@ -395,11 +410,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : THREADS == 128 ?
                     w.s = cluster_load(cluster_addr(&part_sums[1], lane));
                     w.e = cluster_load(cluster_addr(&part_sums[2], lane));
                 }
-                M = w.M;
-#pragma unroll
-                for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, k));
-                w.move(M);
-                q = {M, warp_sum(w.s), warp_sum(w.e)};
+                q = join_first<kMaxParts>(w);
             }
             if (TOP) {
                 for (int i = threadIdx.x; i < parts * top; i += THREADS) keys[i] = cluster_load64(cluster_addr(&best[i % top], i / top));
@@ -525,11 +536,11 @@ cudaError_t launch_logprobs(const LogprobArgs &a, int parts, cudaStream_t s) {
 template <typename T>
 cudaError_t token_logprobs(const LogprobArgs &a, cudaStream_t s) {
     const int64_t rows = a.m * a.n;
-    if (a.vocab <= 2048) return launch_logprobs<T, 32>(a, 1, s);
+    if (a.vocab <= 2048 || (a.vocab <= 4096 && rows >= 16 * 148)) return launch_logprobs<T, 32>(a, 1, s);
     if (a.vocab <= 16384 && rows >= 148) return launch_logprobs<T, 128>(a, 1, s);
     int parts = 8;
     while (parts > 1 && (rows * parts > 296 || a.vocab < parts * 2048)) parts /= 2;
-    return launch_logprobs<T, 512>(a, parts, s);
+    return launch_logprobs<T, 256>(a, parts, s);
 }
 
 template <typename T>
