@@ -191,6 +191,73 @@ __global__ void __launch_bounds__(TPR == 32 ? kRowBlock : TPR) norm_row_kernel(N
     }
 }
 
+// The layer's input, N entries at a time: as it was, or codes and their block's scale
+template <typename T, int N, bool SAVED> struct InputPack {
+    Pack<T, N> x;
+    __device__ __forceinline__ void load(const NormGradArgs &a, int64_t r, int j) { x = load_pack<T, N>(static_cast<const T *>(a.x.data) + a.x.at(r) + j); }
+    __device__ __forceinline__ void get(float (&f)[N]) const { values(x, f); }
+};
+template <typename T, int N> struct InputPack<T, N, true> {
+    Pack<uint8_t, N> codes;
+    float scale;
+    __device__ __forceinline__ void load(const NormGradArgs &a, int64_t r, int j) {
+        codes = load_pack<uint8_t, N>(static_cast<const uint8_t *>(a.codes.data) + a.codes.at(r) + j);
+        scale = (static_cast<const float *>(a.scales.data) + a.scales.at(r))[j / ZENO_SAVED_BLOCK];
+    }
+    __device__ __forceinline__ void get(float (&f)[N]) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = saved_value(codes.v[i], scale);
+    }
+};
+
+// dx of a row in TPR threads' registers: rows too long for the kernels by columns below, which give both gradients from one reading.
+template <typename T, typename P, int N, int TPR, int NV, bool SAVED, bool WV>
+__global__ void __launch_bounds__(TPR, TPR <= 512 ? 2 : 1) norm_dx_row_kernel(NormGradArgs a) {
+    __shared__ float scratch[2][32];
+    const int64_t r = blockIdx.x;
+    const int t = threadIdx.x, cols = (int)a.cols, packs = cols / N;
+    const T *dy = static_cast<const T *>(a.dy.data) + a.dy.at(r);
+    T *dx = static_cast<T *>(a.dx.data) + a.dx.at(r);
+    const P *w = static_cast<const P *>(a.w) + (a.ldw ? r / a.n * a.ldw : 0);
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    Pack<T, N> d[NV];
+    InputPack<T, N, SAVED> x[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (t + i * TPR < packs) {
+            d[i] = load_pack<T, N>(dy + (int64_t)(t + i * TPR) * N);
+            x[i].load(a, r, (t + i * TPR) * N);
+        }
+    float c1 = 0.f, c2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (t + i * TPR < packs) {
+            float g[N], h[N], wf[N];
+            values(d[i], g);
+            x[i].get(h);
+            weights<WV>(w + (t + i * TPR) * N, wf);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                g[k] *= wf[k];
+                c1 += g[k];
+                c2 = fmaf(g[k], (h[k] - mean) * rstd, c2);
+            }
+        }
+    c1 = block_sum<TPR>(c1, scratch[0]) / (float)cols;
+    c2 = block_sum<TPR>(c2, scratch[1]) / (float)cols;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (t + i * TPR < packs) {
+            float g[N], h[N], wf[N];
+            values(d[i], g);
+            x[i].get(h);
+            weights<WV>(w + (t + i * TPR) * N, wf);
+#pragma unroll
+            for (int k = 0; k < N; ++k) g[k] = rstd * (g[k] * wf[k] - c1 - (h[k] - mean) * rstd * c2);
+            store_pack<T, N>(dx + (int64_t)(t + i * TPR) * N, g);
+        }
+}
+
 // ---- backward, by columns
 
 // 16 bytes of activations as pairs
@@ -241,7 +308,7 @@ __global__ void __launch_bounds__(TPR *ROWS, TPR *ROWS <= 256 ? 2 : 1) norm_colu
     Two w[kNV][H], sw[kNV][H], sb[kNV][H];
 #pragma unroll
     for (int v = 0; v < kNV; ++v) {
-        at[v] = (v * TPR + t) * N;
+        at[v] = ((DX ? 0 : (int)blockIdx.z * kNV * TPR) + v * TPR + t) * N;       // without dx the columns may be cut
         mine[v] = at[v] < cols;
 #pragma unroll
         for (int k = 0; k < H; ++k) {
@@ -400,69 +467,99 @@ __global__ void __launch_bounds__(TPR *ROWS, TPR *ROWS <= 256 ? 2 : 1) norm_colu
     }
 }
 
-// Rows of any alignment, and what is too long for the above: the columns blockIdx.x * TPR .. of chunk blockIdx.z of a group's rows.  With DX
-// the block has the whole row (gridDim.x is 1).
-template <typename T, typename P, int TPR, int NV, bool DX>
+// Rows of any alignment, and what is too long for the above: the columns blockIdx.x * TPR * NV .. of chunk blockIdx.z of a group's rows, R rows at
+// a time with the next R on their way, one barrier for them all.  With DX the block has the whole row (gridDim.x is 1).
+template <typename T, typename P, int TPR, int NV, int R, bool SAVED, bool DX>
 __global__ void __launch_bounds__(TPR) norm_entries_kernel(NormGradArgs a, float *part) {
     constexpr int kWarps = TPR / 32;
-    __shared__ __align__(16) float2 scratch[2][kWarps];
-    const int t = threadIdx.x, cols = (int)a.cols, chunks = gridDim.z, i = blockIdx.y;
+    __shared__ float scratch[2][kWarps][2 * R];
+    const int t = threadIdx.x, lane = t & 31, cols = (int)a.cols, chunks = gridDim.z, i = blockIdx.y;
     const int j0 = blockIdx.x * TPR * NV + t;
     const int64_t first = a.n * blockIdx.z / chunks, last = a.n * (blockIdx.z + 1) / chunks;
     const float inv = 1.f / (float)cols;
+    const T *dy = static_cast<const T *>(a.dy.data) + i * a.dy.group + j0;
+    const T *x = SAVED ? nullptr : static_cast<const T *>(a.x.data) + i * a.x.group + j0;
+    const uint8_t *codes = SAVED ? static_cast<const uint8_t *>(a.codes.data) + i * a.codes.group + j0 : nullptr;
+    const float *scales = SAVED ? static_cast<const float *>(a.scales.data) + i * a.scales.group : nullptr;
     float w[NV], sw[NV], sb[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         w[v] = DX && j0 + v * TPR < cols ? value_of(static_cast<const P *>(a.w) + i * a.ldw + j0 + v * TPR) : 0.f;
         sw[v] = sb[v] = 0.f;
     }
-    float d[NV], h[NV], mean = 0.f, rstd = 0.f;
-    auto fetch = [&](int64_t row) {
-        if (row >= last) return;
-        const int64_t r = i * a.n + row;
-        const T *dy = static_cast<const T *>(a.dy.data) + a.dy.at(r);
-        const InputRow<T> x(a, r);
-        mean = a.mean[r];
-        rstd = a.rstd[r];
+    // the next rows as they lie in memory: what is done to them waits until their turn
+    T next_d[R][NV], next_x[SAVED ? 1 : R][SAVED ? 1 : NV];
+    uint8_t next_c[SAVED ? R : 1][SAVED ? NV : 1];
+    float next_s[SAVED ? R : 1][SAVED ? NV : 1], next_mean[R], next_rstd[R];
+    auto fetch = [&](int64_t row0) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int j = j0 + v * TPR;
-            d[v] = j < cols ? value_of(dy + j) : 0.f;
-            h[v] = j < cols ? x(j) : 0.f;
+        for (int q = 0; q < R; ++q) {
+            const int64_t row = row0 + q;
+            if (row >= last) return;
+            next_mean[q] = a.mean[i * a.n + row];
+            next_rstd[q] = a.rstd[i * a.n + row];
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                if (j0 + v * TPR < cols) {
+                    next_d[q][v] = dy[row * a.dy.row + v * TPR];
+                    if constexpr (SAVED) {
+                        next_c[q][v] = codes[row * a.codes.row + v * TPR];
+                        next_s[q][v] = scales[row * a.scales.row + (j0 + v * TPR) / ZENO_SAVED_BLOCK];
+                    } else {
+                        next_x[q][v] = x[row * a.x.row + v * TPR];
+                    }
+                }
         }
     };
     fetch(first);
     int turn = 0;
-    for (int64_t row = first; row < last; ++row) {
-        float g[NV], hh[NV], c1 = 0.f, c2 = 0.f;
-        const float rs = rstd;
+    for (int64_t row = first; row < last; row += R) {
+        float g[R][NV], h[R][NV], rs[R], c[2 * R];
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            hh[v] = j0 + v * TPR < cols ? (h[v] - mean) * rs : 0.f;
-            sw[v] = fmaf(d[v], hh[v], sw[v]);
-            sb[v] += d[v];
-            g[v] = d[v] * w[v];
-            c1 += g[v];
-            c2 = fmaf(g[v], hh[v], c2);
+        for (int q = 0; q < R; ++q) {
+            const bool on = row + q < last;
+            rs[q] = on ? next_rstd[q] : 0.f;
+            c[2 * q] = c[2 * q + 1] = 0.f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                float d = 0.f;
+                h[q][v] = 0.f;
+                if (on && j0 + v * TPR < cols) {
+                    d = value_of(&next_d[q][v]);
+                    if constexpr (SAVED) h[q][v] = saved_value(next_c[q][v], next_s[q][v]);
+                    else h[q][v] = value_of(&next_x[q][v]);
+                    h[q][v] = (h[q][v] - next_mean[q]) * rs[q];
+                }
+                sw[v] = fmaf(d, h[q][v], sw[v]);
+                sb[v] += d;
+                g[q][v] = d * w[v];
+                c[2 * q] += g[q][v];
+                c[2 * q + 1] = fmaf(g[q][v], h[q][v], c[2 * q + 1]);
+            }
         }
-        fetch(row + 1);
+        fetch(row + R);
         if (!DX) continue;
-        c1 = warp_sum(c1);
-        c2 = warp_sum(c2);
-        if ((t & 31) == 0) scratch[turn][t >> 5] = make_float2(c1, c2);
+        // the rows' sums, two for each: first a lane has one of them for the warp, then, over the warps, for the block
+        float mine = warp_transpose_reduce<2 * R>(c, lane);
+        if (lane < 2 * R) scratch[turn][t >> 5][lane] = mine;
         __syncthreads();
-        c1 = c2 = 0.f;
+        mine = 0.f;
+        constexpr int kGroups = 32 / (2 * R);
 #pragma unroll
-        for (int k = 0; k < kWarps; ++k) {
-            const float2 v = scratch[turn][k];
-            c1 += v.x;
-            c2 += v.y;
-        }
+        for (int k = 0; k < kWarps; k += kGroups)
+            if (k + lane / (2 * R) < kWarps) mine += scratch[turn][k + lane / (2 * R)][lane % (2 * R)];
+#pragma unroll
+        for (int k = 2 * R; k < 32; k <<= 1) mine += __shfl_xor_sync(0xffffffffu, mine, k);
         turn ^= 1;
-        T *dx = static_cast<T *>(a.dx.data) + a.dx.at(i * a.n + row);
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
-            if (j0 + v * TPR < cols) put(dx + j0 + v * TPR, rs * (g[v] - c1 * inv - hh[v] * (c2 * inv)));
+        for (int q = 0; q < R; ++q) {
+            const float c1 = __shfl_sync(0xffffffffu, mine, 2 * q) * inv, c2 = __shfl_sync(0xffffffffu, mine, 2 * q + 1) * inv;
+            if (row + q >= last) continue;
+            T *dx = static_cast<T *>(a.dx.data) + i * a.dx.group + (row + q) * a.dx.row + j0;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                if (j0 + v * TPR < cols) put(dx + v * TPR, rs[q] * (g[q][v] - c1 - h[q][v] * c2));
+        }
     }
     if (!a.dw && !a.db) return;
 #pragma unroll
@@ -605,26 +702,42 @@ __global__ void __launch_bounds__(kGroupThreads, 2) norm_group_kernel(NormArgs a
     }
 }
 
-// The blocks' sums of a group, column by column: 32 columns a block, eight warps take the blocks in turn.
-template <typename P>
+// The blocks' sums of a group: 32 N columns a block, N a lane, eight warps take the blocks in turn.
+template <typename P, int N>
 __global__ void __launch_bounds__(kThreads) norm_join_kernel(const float *part, int chunks, int cols, P *dw, P *db, int64_t ldg) {
     constexpr int kWarps = kThreads / 32;
-    __shared__ float sums[kWarps][32];
+    __shared__ float sums[kWarps][N][32];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.y;
-    const int64_t at = (int64_t)blockIdx.x * 32 + lane, all = 2 * (int64_t)cols;
-    float s = 0.f;
+    const int64_t at = ((int64_t)blockIdx.x * 32 + lane) * N, all = 2 * (int64_t)cols;
+    float s[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[k] = 0.f;
     if (at < all)
 #pragma unroll 4
-        for (int c = warp; c < chunks; c += kWarps) s += part[((int64_t)i * chunks + c) * all + at];
-    sums[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0 && at < all) {
+        for (int c = warp; c < chunks; c += kWarps) {
+            const Pack<float, N> v = load_pack<float, N>(part + ((int64_t)i * chunks + c) * all + at);
 #pragma unroll
-        for (int q = 1; q < kWarps; ++q) s += sums[q][lane];
-        P *out = at < cols ? dw : db;
-        if (out) put(out + i * ldg + (at < cols ? at : at - cols), s);
+            for (int k = 0; k < N; ++k) s[k] += v.v[k];
+        }
+#pragma unroll
+    for (int k = 0; k < N; ++k) sums[warp][k][lane] = s[k];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 32 * N; c += kThreads) {
+        float v = 0.f;
+#pragma unroll
+        for (int q = 0; q < kWarps; ++q) v += sums[q][c % N][c / N];
+        const int64_t to = (int64_t)blockIdx.x * 32 * N + c;
+        P *out = to < cols ? dw : db;
+        if (to < all && out) put(out + i * ldg + (to < cols ? to : to - cols), v);
     }
+}
+
+// Whether N weights (and biases) can be loaded at a time for every group.
+template <typename P, int N>
+bool wide_weights(const void *w, const void *b, int64_t ldw) {
+    constexpr size_t kPack = N * sizeof(P) < 16 ? N * sizeof(P) : 16;
+    return reinterpret_cast<uintptr_t>(w) % kPack == 0 && reinterpret_cast<uintptr_t>(b) % kPack == 0 && ldw * sizeof(P) % kPack == 0;
 }
 
 // Blocks that a group's rows are cut into: all groups' make two rounds of two blocks an SM, each block with at least 8 rows: few
@@ -669,8 +782,7 @@ template <typename T, typename P>
 cudaError_t layer_norm(const NormArgs &a, cudaStream_t s) {
     constexpr int N = 16 / sizeof(T);
     if (a.cols % N == 0 && aligned_to(a.x, a.m, a.n, sizeof(T), 16) && aligned_to(a.y, a.m, a.n, sizeof(T), 16)) {
-        const size_t pack = N * sizeof(P) < 16 ? N * sizeof(P) : 16;
-        const bool wide = reinterpret_cast<uintptr_t>(a.w) % pack == 0 && reinterpret_cast<uintptr_t>(a.b) % pack == 0 && a.ldw * sizeof(P) % pack == 0;
+        const bool wide = wide_weights<P, N>(a.w, a.b, a.ldw);
         const int64_t packs = a.cols / N;
         // Enough rows for two blocks an SM with eight rows each and more (21 x 2048 x 4096 bfloat16: 123 us, 157 by norm_row_kernel; 86,016 rows of
         // 128: 18 against 35).  Eight vectors a thread in bfloat16, whose weights take twice their bytes of shared memory; four in binary32
@@ -704,8 +816,9 @@ cudaError_t layer_norm(const NormArgs &a, cudaStream_t s) {
 
 template <typename P>
 cudaError_t norm_join(const NormGradArgs &a, int chunks, cudaStream_t s) {
-    return launch_chained(norm_join_kernel<P>, dim3((unsigned)((2 * a.cols + 31) / 32), a.m), dim3(kThreads), 0, s, true, a.workspace, chunks,
-                          (int)a.cols, static_cast<P *>(a.dw), static_cast<P *>(a.db), a.ldg);
+    const int n = a.cols % 4 == 0 ? 4 : 1;
+    return launch_chained(n == 4 ? norm_join_kernel<P, 4> : norm_join_kernel<P, 1>, dim3((unsigned)((2 * a.cols + 32 * n - 1) / (32 * n)), a.m), dim3(kThreads),
+                          0, s, true, a.workspace, chunks, (int)a.cols, static_cast<P *>(a.dw), static_cast<P *>(a.db), a.ldg);
 }
 
 template <typename T, typename P, int TPR, bool SAVED, bool DX>
@@ -718,7 +831,8 @@ cudaError_t norm_columns(const NormGradArgs &a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     const int chunks = norm_chunks(a.m, a.n);
     const bool join = (a.dw || a.db) && chunks > 1;
-    e = launch_chained(kernel, dim3(chunks, a.m), dim3(TPR * kRows), kSmem, s, false, a, join ? a.workspace : nullptr);
+    const int64_t per_block = (int64_t)TPR * kNV * (16 / sizeof(T)), tiles = DX ? 1 : (a.cols + per_block - 1) / per_block;
+    e = launch_chained(kernel, dim3(chunks, a.m, (unsigned)tiles), dim3(TPR * kRows), kSmem, s, false, a, join ? a.workspace : nullptr);
     return e == cudaSuccess && join ? norm_join<P>(a, chunks, s) : e;
 }
 
@@ -732,14 +846,22 @@ cudaError_t norm_columns_any(const NormGradArgs &a, cudaStream_t s) {
     return norm_columns<T, P, 512, SAVED, DX>(a, s);
 }
 
-template <typename T, typename P, int TPR, int NV, bool DX>
+template <typename T, typename P, int TPR, int NV, int R, bool DX>
 cudaError_t norm_entries(const NormGradArgs &a, cudaStream_t s) {
     const int64_t tiles = DX ? 1 : (a.cols + TPR * NV - 1) / (TPR * NV);
     const int chunks = norm_chunks(a.m, a.n);
     const bool join = (a.dw || a.db) && chunks > 1;
-    const cudaError_t e = launch_chained(norm_entries_kernel<T, P, TPR, NV, DX>, dim3((unsigned)tiles, a.m, chunks), dim3(TPR), 0, s, false, a,
-                                         join ? a.workspace : nullptr);
+    auto *kernel = a.x.data || a.n == 0 ? norm_entries_kernel<T, P, TPR, NV, R, false, DX> : norm_entries_kernel<T, P, TPR, NV, R, true, DX>;
+    const cudaError_t e = launch_chained(kernel, dim3((unsigned)tiles, a.m, chunks), dim3(TPR), 0, s, false, a, join ? a.workspace : nullptr);
     return e == cudaSuccess && join ? norm_join<P>(a, chunks, s) : e;
+}
+
+template <typename T, typename P, int N, int TPR, int NV>
+cudaError_t norm_dx_row(const NormGradArgs &a, cudaStream_t s) {
+    const bool wide = N > 1 && wide_weights<P, N>(a.w, nullptr, a.ldw);
+    auto *kernel = a.x.data ? (wide ? norm_dx_row_kernel<T, P, N, TPR, NV, false, (N > 1)> : norm_dx_row_kernel<T, P, N, TPR, NV, false, false>)
+                            : (wide ? norm_dx_row_kernel<T, P, N, TPR, NV, true, (N > 1)> : norm_dx_row_kernel<T, P, N, TPR, NV, true, false>);
+    return launch_chained(kernel, dim3((unsigned)(a.m * a.n)), dim3(TPR), 0, s, false, a);
 }
 
 template <typename T, typename P>
@@ -754,15 +876,24 @@ cudaError_t layer_norm_gradient(const NormGradArgs &a, cudaStream_t s) {
         return dx ? norm_columns_any<T, P, true, true>(a, s) : norm_columns_any<T, P, true, false>(a, s);
     }
     if (dx && weights) {
-        if (a.cols <= 512) return norm_entries<T, P, 128, 4, true>(a, s);
-        if (a.cols <= 2048) return norm_entries<T, P, 512, 4, true>(a, s);
-        if (a.cols <= 4096) return norm_entries<T, P, 1024, 4, true>(a, s);
+        if (a.cols <= 256) return norm_entries<T, P, 64, 4, 4, true>(a, s);
+        if (a.cols <= 512) return norm_entries<T, P, 128, 4, 4, true>(a, s);
+        if (a.cols <= 1024) return norm_entries<T, P, 256, 4, 4, true>(a, s);
+        if (a.cols <= 2048) return norm_entries<T, P, 512, 4, 2, true>(a, s);
+        if (a.cols <= 4096) return norm_entries<T, P, 1024, 4, 1, true>(a, s);
     }
+    // long rows: the weight gradients, then dx, each from a reading of its own; dx last, since it may lie in dy's place
     cudaError_t e = cudaSuccess;
-    if (weights) e = norm_entries<T, P, 256, 2, false>(a, s);
-    // last, since dx may lie in dy's place
-    if (e == cudaSuccess && dx) e = launch_chained(norm_dx_any_kernel<T, P>, dim3((unsigned)(a.m * a.n)), dim3(kThreads), 0, s, false, a);
-    return e;
+    if (weights) {
+        if (a.n > 0 && aligned) e = a.x.data ? norm_columns<T, P, 256, false, false>(a, s) : norm_columns<T, P, 256, true, false>(a, s);
+        else e = norm_entries<T, P, 256, 2, 4, false>(a, s);
+    }
+    if (e != cudaSuccess || !dx) return e;
+    if (aligned && a.cols <= 2048 * N) return norm_dx_row<T, P, N, 512, 4>(a, s);
+    if (aligned && a.cols <= 4096 * N) return norm_dx_row<T, P, N, 1024, 4>(a, s);
+    if (a.cols <= 8192) return norm_dx_row<T, P, 1, 1024, 8>(a, s);
+    if (a.cols <= 16384) return norm_dx_row<T, P, 1, 1024, 16>(a, s);
+    return launch_chained(norm_dx_any_kernel<T, P>, dim3((unsigned)(a.m * a.n)), dim3(kThreads), 0, s, false, a);
 }
 
 }  // namespace

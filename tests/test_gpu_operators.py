@@ -49,7 +49,8 @@ def _rows(g, m, n, cols, dtype, layout="dense", scale=1.0, shift=0.0):
 
 
 SIZES = [(1, 1, 1), (1, 1, 4096), (2, 3, 5), (3, 7, 31), (2, 9, 32), (5, 4, 33), (3, 11, 128), (1, 70, 129), (4, 33, 256), (2, 5, 777), (3, 17, 1024),
-         (2, 13, 1029), (1, 6, 2048), (2, 4, 4100), (21, 1, 520), (2, 3, 8192), (1, 2, 11111), (1, 3, 16384), (1, 2, 40003), (70, 2, 64), (3, 300, 96)]
+         (2, 13, 1029), (1, 6, 2048), (2, 4, 4100), (21, 1, 520), (2, 3, 8192), (1, 2, 11111), (1, 3, 16384), (1, 2, 40003), (70, 2, 64), (3, 300, 96),
+         (3, 41, 2500), (2, 70, 6001), (1, 50, 12000), (1, 33, 32768), (1, 20, 20480)]
 TYPES = [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)]
 
 
