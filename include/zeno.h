@@ -322,8 +322,9 @@ zeno_status zeno_score_lsq_static(int32_t device, const float *x, const float *V
  * irrelevant): calls that may overlap on the GPU need workspaces of their own.  Results do not depend on the order in which
  * blocks run.  The first call on a device makes the CUDA runtime load the library's code: make it before a stream capture.
  * INVALID_ARG: a NULL pointer where one is required, a type outside zeno_dtype, a negative size, a stride smaller than the
- * row, a NaN or infinite scalar, a workspace that is too small.  UNSUPPORTED: more than 65535 groups, more than 2^31 - 1 rows,
- * or rows of more than 2^30 entries. */
+ * row, an address that is no multiple of its entries' size, a NaN or infinite scalar, a workspace that is too small.
+ * UNSUPPORTED: more than 65535 groups, more than 2^31 - 1 rows, rows of more than 2^30 entries (2^20 where weight gradients are
+ * formed). */
 typedef struct {
     void *data;
     int64_t row;   /* elements from one row of a group to the next */

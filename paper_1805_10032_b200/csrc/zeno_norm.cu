@@ -740,11 +740,12 @@ bool wide_weights(const void *w, const void *b, int64_t ldw) {
     return reinterpret_cast<uintptr_t>(w) % kPack == 0 && reinterpret_cast<uintptr_t>(b) % kPack == 0 && ldw * sizeof(P) % kPack == 0;
 }
 
-// Blocks that a group's rows are cut into: all groups' make two rounds of two blocks an SM, each block with at least 8 rows: few
-// rows to a block are few groups' rows, whose sums stay in L2.
+// Blocks that a group's rows are cut into: all groups' make two rounds of two blocks an SM, each block with at least 8 rows: few rows to a
+// block are few groups' rows, whose sums stay in L2.  Long rows are cut into blocks by their columns too.
 constexpr int kNormBlocks = 592;
-int norm_chunks(int m, int64_t n) {
-    int64_t c = m > 0 ? kNormBlocks / m : 1;
+int norm_chunks(int m, int64_t n, int64_t cols) {
+    const int64_t by_columns = cols > 4096 ? cols / 4096 : 1;
+    int64_t c = m > 0 ? kNormBlocks / (m * by_columns) : 1;
     if (c > n / 8) c = n / 8;
     return c < 1 ? 1 : (int)c;
 }
@@ -767,7 +768,7 @@ cudaError_t norm_groups(const NormArgs &a, cudaStream_t s) {
     auto *kernel = norm_group_kernel<T, P, TPR, NV, R>;
     static PerDeviceOnce attr_set;
     const cudaError_t e = allow_shared(kernel, kSmem, attr_set);
-    return e != cudaSuccess ? e : launch_chained(kernel, dim3(norm_chunks(a.m, a.n), a.m), dim3(kGroupThreads), kSmem, s, false, a);
+    return e != cudaSuccess ? e : launch_chained(kernel, dim3(norm_chunks(a.m, a.n, 1), a.m), dim3(kGroupThreads), kSmem, s, false, a);
 }
 
 template <typename T, typename P, int N, int TPR, int NV>
@@ -787,7 +788,7 @@ cudaError_t layer_norm(const NormArgs &a, cudaStream_t s) {
         // Enough rows for two blocks an SM with eight rows each and more (21 x 2048 x 4096 bfloat16: 123 us, 157 by norm_row_kernel; 86,016 rows of
         // 128: 18 against 35).  Eight vectors a thread in bfloat16, whose weights take twice their bytes of shared memory; four in binary32
         // (43,008 rows of 4096: 227 us, with eight 258).
-        if (norm_chunks(a.m, a.n) * (int64_t)a.m >= kNormBlocks / 2 && a.n * a.m >= kNormBlocks * 8 && packs <= 1024) {
+        if (norm_chunks(a.m, a.n, 1) * (int64_t)a.m >= kNormBlocks / 2 && a.n * a.m >= kNormBlocks * 8 && packs <= 1024) {
             constexpr int kMany = sizeof(T) == 2 ? 8 : 4;
             if (packs <= 16) return norm_groups<T, P, 4, 4, 2>(a, s);
             if (packs <= 32) return norm_groups<T, P, 8, 4, 2>(a, s);
@@ -829,7 +830,7 @@ cudaError_t norm_columns(const NormGradArgs &a, cudaStream_t s) {
     static PerDeviceOnce attr_set;
     cudaError_t e = allow_shared(kernel, kSmem, attr_set);
     if (e != cudaSuccess) return e;
-    const int chunks = norm_chunks(a.m, a.n);
+    const int chunks = norm_chunks(a.m, a.n, a.cols);
     const bool join = (a.dw || a.db) && chunks > 1;
     const int64_t per_block = (int64_t)TPR * kNV * (16 / sizeof(T)), tiles = DX ? 1 : (a.cols + per_block - 1) / per_block;
     e = launch_chained(kernel, dim3(chunks, a.m, (unsigned)tiles), dim3(TPR * kRows), kSmem, s, false, a, join ? a.workspace : nullptr);
@@ -849,7 +850,7 @@ cudaError_t norm_columns_any(const NormGradArgs &a, cudaStream_t s) {
 template <typename T, typename P, int TPR, int NV, int R, bool DX>
 cudaError_t norm_entries(const NormGradArgs &a, cudaStream_t s) {
     const int64_t tiles = DX ? 1 : (a.cols + TPR * NV - 1) / (TPR * NV);
-    const int chunks = norm_chunks(a.m, a.n);
+    const int chunks = norm_chunks(a.m, a.n, a.cols);
     const bool join = (a.dw || a.db) && chunks > 1;
     auto *kernel = a.x.data || a.n == 0 ? norm_entries_kernel<T, P, TPR, NV, R, false, DX> : norm_entries_kernel<T, P, TPR, NV, R, true, DX>;
     const cudaError_t e = launch_chained(kernel, dim3((unsigned)tiles, a.m, chunks), dim3(TPR), 0, s, false, a, join ? a.workspace : nullptr);
@@ -905,7 +906,7 @@ cudaError_t launch_layer_norm(int type, int param_type, const NormArgs &a, cudaS
 }
 
 int64_t norm_gradient_workspace(int m, int64_t n, int64_t cols) {
-    const int chunks = norm_chunks(m, n);
+    const int chunks = norm_chunks(m, n, cols);
     return chunks > 1 ? (int64_t)m * chunks * 2 * cols * (int64_t)sizeof(float) : 0;
 }
 

@@ -10,7 +10,7 @@ using zeno::Rows;
 
 namespace {
 
-constexpr int64_t kMaxRows = 0x7fffffff, kMaxCols = (int64_t)1 << 30, kMaxStride = (int64_t)1 << 44;
+constexpr int64_t kMaxRows = 0x7fffffff, kMaxCols = (int64_t)1 << 30, kMaxWeights = (int64_t)1 << 20, kMaxStride = (int64_t)1 << 44;
 constexpr int kMaxGroups = 65535;
 
 bool type_ok(int32_t type) { return type == ZENO_F32 || type == ZENO_BF16; }
@@ -22,11 +22,15 @@ zeno_status check_sizes(int32_t m, int64_t n, int64_t cols) {
     return ZENO_OK;
 }
 
-// Rows of `cols` elements that do not overlap (with no rows, anything goes).  Inputs may be one group for all (a stride of 0).
-bool rows_ok(const zeno_rows *v, int32_t m, int64_t n, int64_t cols, bool input = true) {
+int size_of(int32_t type) { return type == ZENO_BF16 ? 2 : 4; }
+
+bool placed(const void *p, int size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
+
+// Rows of `cols` elements of `size` bytes that do not overlap (with no rows, anything goes).  Inputs may be one group for all (a stride of 0).
+bool rows_ok(const zeno_rows *v, int size, int32_t m, int64_t n, int64_t cols, bool input = true) {
     if (!v) return false;
     if (m == 0 || n == 0) return true;
-    if (!v->data) return false;
+    if (!v->data || !placed(v->data, size)) return false;
     if (n > 1 && (v->row < cols || v->row > kMaxStride)) return false;
     if (m == 1 || (input && v->group == 0)) return true;
     if (v->group < cols || v->group > kMaxStride) return false;
@@ -64,14 +68,16 @@ zeno_status zeno_layer_norm(int32_t device, int32_t type, int32_t param_type, co
     if (!type_ok(type) || !type_ok(param_type) || !isfinite(eps) || eps < 0.f) return ZENO_ERR_INVALID_ARG;
     const zeno_status st = check_sizes(m, n, cols);
     if (st != ZENO_OK) return st;
-    if (!rows_ok(x, m, n, cols) || !rows_ok(y, m, n, cols, false) || !w || (ldw != 0 && ldw < cols)) return ZENO_ERR_INVALID_ARG;
+    const int size = size_of(type), wsize = size_of(param_type);
+    if (!rows_ok(x, size, m, n, cols) || !rows_ok(y, size, m, n, cols, false) || !w || (ldw != 0 && ldw < cols)) return ZENO_ERR_INVALID_ARG;
+    if (!placed(w, wsize) || !placed(b, wsize) || !placed(mean, 4) || !placed(rstd, 4)) return ZENO_ERR_INVALID_ARG;
     if (m == 0 || n == 0) return ZENO_OK;
     zeno::NormArgs a = {rows_of(x, n), rows_of(y, n), m, n, cols, w, b, ldw, eps, mean, rstd};
     return on_device(device, [&] { return zeno::launch_layer_norm(type, param_type, a, static_cast<cudaStream_t>(stream)); });
 }
 
 int64_t zeno_layer_norm_gradient_workspace(int32_t m, int64_t n, int64_t cols) {
-    return check_sizes(m, n, cols) == ZENO_OK ? zeno::norm_gradient_workspace(m, n, cols) : 0;
+    return check_sizes(m, n, cols) == ZENO_OK && cols <= kMaxWeights ? zeno::norm_gradient_workspace(m, n, cols) : 0;
 }
 
 zeno_status zeno_layer_norm_gradient(int32_t device, int32_t type, int32_t param_type, const zeno_rows *dy, const zeno_rows *x,
@@ -83,9 +89,12 @@ zeno_status zeno_layer_norm_gradient(int32_t device, int32_t type, int32_t param
     const zeno_status st = check_sizes(m, n, cols);
     if (st != ZENO_OK) return st;
     const bool rows = m > 0 && n > 0;
-    if (!rows_ok(dy, m, n, cols) || (x ? !rows_ok(x, m, n, cols) : !rows_ok(codes, m, n, cols) || !rows_ok(scales, m, n, blocks_of(cols))))
+    if (cols > kMaxWeights) return ZENO_ERR_UNSUPPORTED;
+    const int size = size_of(type), wsize = size_of(param_type);
+    if (!rows_ok(dy, size, m, n, cols) || (x ? !rows_ok(x, size, m, n, cols) : !rows_ok(codes, 1, m, n, cols) || !rows_ok(scales, 4, m, n, blocks_of(cols))))
         return ZENO_ERR_INVALID_ARG;
-    if ((rows && (!mean || !rstd)) || (dx && (!rows_ok(dx, m, n, cols, false) || !w || (ldw != 0 && ldw < cols)))) return ZENO_ERR_INVALID_ARG;
+    if (!placed(w, wsize) || !placed(dw, wsize) || !placed(db, wsize) || !placed(mean, 4) || !placed(rstd, 4)) return ZENO_ERR_INVALID_ARG;
+    if ((rows && (!mean || !rstd)) || (dx && (!rows_ok(dx, size, m, n, cols, false) || !w || (ldw != 0 && ldw < cols)))) return ZENO_ERR_INVALID_ARG;
     if ((dw || db) && m > 1 && ldg < cols) return ZENO_ERR_INVALID_ARG;
     if (!workspace_ok(workspace, workspace_bytes, zeno::norm_gradient_workspace(m, n, cols))) return ZENO_ERR_INVALID_ARG;
     if (m == 0) return ZENO_OK;
@@ -100,7 +109,7 @@ zeno_status zeno_pack_activations(int32_t device, int32_t type, const zeno_rows 
     if (!type_ok(type)) return ZENO_ERR_INVALID_ARG;
     const zeno_status st = check_sizes(m, n, cols);
     if (st != ZENO_OK) return st;
-    if (!rows_ok(x, m, n, cols) || !rows_ok(codes, m, n, cols, false) || !rows_ok(scales, m, n, blocks_of(cols), false)) return ZENO_ERR_INVALID_ARG;
+    if (!rows_ok(x, size_of(type), m, n, cols) || !rows_ok(codes, 1, m, n, cols, false) || !rows_ok(scales, 4, m, n, blocks_of(cols), false)) return ZENO_ERR_INVALID_ARG;
     if (m == 0 || n == 0) return ZENO_OK;
     zeno::PackArgs a = {rows_of(x, n), rows_of(codes, n), rows_of(scales, n), m, n, cols};
     return on_device(device, [&] { return zeno::launch_pack(type, a, static_cast<cudaStream_t>(stream)); });
@@ -113,7 +122,8 @@ static zeno_status check_dense(int32_t type, const zeno_rows *dy, const zeno_row
     zeno_status st = check_sizes(m, n, inputs);
     if (st == ZENO_OK) st = check_sizes(m, n, outputs);
     if (st != ZENO_OK) return st;
-    if (!rows_ok(dy, m, n, outputs) || !rows_ok(codes, m, n, inputs)) return ZENO_ERR_INVALID_ARG;
+    if (inputs > kMaxWeights || outputs > kMaxWeights) return ZENO_ERR_UNSUPPORTED;
+    if (!rows_ok(dy, size_of(type), m, n, outputs) || !rows_ok(codes, 1, m, n, inputs)) return ZENO_ERR_INVALID_ARG;
     *a = {rows_of(dy, n), rows_of(codes, n), rows_of(scales, n), m, n, inputs, outputs, nullptr, nullptr, 0, 0, nullptr};
     return ZENO_OK;
 }
@@ -131,7 +141,7 @@ zeno_status zeno_dense_gradient(int32_t device, int32_t type, int32_t param_type
     zeno::DenseGradArgs a;
     const zeno_status st = check_dense(type, dy, codes, scales, m, n, inputs, outputs, &a);
     if (st != ZENO_OK) return st;
-    if (!rows_ok(scales, m, n, blocks_of(inputs))) return ZENO_ERR_INVALID_ARG;
+    if (!rows_ok(scales, 4, m, n, blocks_of(inputs)) || !placed(dw, size_of(param_type)) || !placed(db, size_of(param_type))) return ZENO_ERR_INVALID_ARG;
     if (m == 0) return ZENO_OK;
     if (!dw || (m > 1 && (ldw < inputs * outputs || (db && ldb < outputs)))) return ZENO_ERR_INVALID_ARG;
     if (!workspace_ok(workspace, workspace_bytes, zeno::dense_gradient_workspace(type, a))) return ZENO_ERR_INVALID_ARG;
@@ -163,7 +173,8 @@ zeno_status zeno_token_logprobs(int32_t device, int32_t type, const zeno_rows *l
     if (top > ZENO_MAX_TOP) return ZENO_ERR_UNSUPPORTED;
     const zeno_status st = check_sizes(m, n, vocab);
     if (st != ZENO_OK) return st;
-    if (!rows_ok(logits, m, n, vocab)) return ZENO_ERR_INVALID_ARG;
+    if (!rows_ok(logits, size_of(type), m, n, vocab)) return ZENO_ERR_INVALID_ARG;
+    if (!placed(targets, 4) || !placed(logprobs, 4) || !placed(entropy, 4) || !placed(lse, 4) || !placed(top_idx, 4) || !placed(top_logprobs, 4)) return ZENO_ERR_INVALID_ARG;
     if (m == 0 || n == 0) return ZENO_OK;
     if (logprobs && !targets) return ZENO_ERR_INVALID_ARG;
     if (!top_idx && !top_logprobs) top = 0;
@@ -178,7 +189,8 @@ zeno_status zeno_token_gradient(int32_t device, int32_t type, const zeno_rows *l
     if (!type_ok(type)) return ZENO_ERR_INVALID_ARG;
     const zeno_status st = check_sizes(m, n, vocab);
     if (st != ZENO_OK) return st;
-    if (!rows_ok(logits, m, n, vocab) || !rows_ok(grad, m, n, vocab, false)) return ZENO_ERR_INVALID_ARG;
+    if (!rows_ok(logits, size_of(type), m, n, vocab) || !rows_ok(grad, size_of(type), m, n, vocab, false)) return ZENO_ERR_INVALID_ARG;
+    if (!placed(targets, 4) || !placed(lse, 4) || !placed(entropy, 4) || !placed(g_logprob, 4) || !placed(g_entropy, 4)) return ZENO_ERR_INVALID_ARG;
     if (m == 0 || n == 0) return ZENO_OK;
     if (!targets || !lse || !g_logprob || (g_entropy && !entropy)) return ZENO_ERR_INVALID_ARG;
     zeno::TokenGradArgs a = {rows_of(logits, n), rows_of(grad, n), m, n, vocab, targets, lse, entropy, g_logprob, g_entropy};

@@ -318,9 +318,10 @@ def test_a_wait_that_runs_out_is_reported_and_leaves_the_device_usable():
     assert torch.equal(dw, want)
 
 
-def test_dense_gradient_layouts_and_values_that_are_not_finite():
+@pytest.mark.parametrize("n", [70, 700])
+def test_dense_gradient_layouts_and_values_that_are_not_finite(n):
     g = _gen(5)
-    m, n, inputs, outputs = 3, 70, 256, 128
+    m, inputs, outputs = 3, 256, 128
     for act in (F32, BF16):
         x = _rows(g, m, n, inputs, act, "interleaved")
         dy = _rows(g, m, n, outputs, act, "interleaved")
@@ -331,6 +332,11 @@ def test_dense_gradient_layouts_and_values_that_are_not_finite():
             zeno.dense_gradient(dy, s, dw)
             want = R.dense_gradient(dy, R.unpack(s.codes, s.scales))
             R.assert_near(dw, want[0], want[2], "dw")
+        odd = zeno.Saved(torch.zeros(m, n, inputs + 5, device="cuda", dtype=torch.uint8)[..., 5:], saved.scales)      # codes that no tensor map can step through
+        odd.codes.copy_(saved.codes.view(torch.uint8))
+        zeno.dense_gradient(dy, odd, dw)
+        want = R.dense_gradient(dy, R.unpack(saved.codes, saved.scales))
+        R.assert_near(dw, want[0], want[2], "odd codes")
         x[1, 5, 77] = NAN
         dy[2, 69, 100] = INF
         zeno.dense_gradient(dy, zeno.pack_activations(x), dw)

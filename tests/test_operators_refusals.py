@@ -86,6 +86,9 @@ def test_sizes_types_and_rows(lib, name):
         assert call(lib, **{arg: rows(-64, 640)}) == INVALID, arg
         assert call(lib, **{arg: rows(width, 10 * width - 1)}) == INVALID, arg
         assert call(lib, **{arg: rows(1 << 60, 1 << 62)}) == INVALID, arg
+    for arg in ROWS[name]:                                 # no address of an entry
+        if arg != "codes":
+            assert call(lib, **{arg: rows(64, 640, P + 1)}) == INVALID, arg
     if name in OUT:                                        # an input may be shared by the groups, an output not
         assert call(lib, **{OUT[name]: rows(64, 0)}) == INVALID
 
@@ -96,6 +99,21 @@ def test_nothing_to_do_is_no_error(lib, name):
     assert CALLS[name](lib, m=0, **none) == zeno.OK
     if name not in ("norm_gradient", "dense"):             # those write zeros
         assert CALLS[name](lib, n=0, **none) == zeno.OK
+
+
+def test_misplaced_addresses(lib):
+    for call, names in ((norm, ("w", "b", "mean", "rstd")), (norm_gradient, ("w", "mean", "rstd", "dw", "db")), (dense, ("dw", "db")),
+                        (logprobs, ("t", "lp", "entropy", "lse", "idx", "top_lp")), (gradient, ("t", "lse", "entropy", "g", "gh"))):
+        for name in names:
+            assert call(lib, **{name: P + 1}) == INVALID, (call.__name__, name)
+
+
+def test_widths_of_weight_gradients(lib):
+    wide = (1 << 20) + 8
+    r = rows(wide, 10 * wide)
+    assert norm_gradient(lib, cols=wide, dy=r, x=r, dx=r, ldg=wide) == UNSUPPORTED
+    assert dense(lib, inputs=wide, codes=r) == UNSUPPORTED and dense(lib, outputs=wide, dy=r) == UNSUPPORTED
+    assert lib.zeno_layer_norm_gradient_workspace(1, 1000, wide) == 0
 
 
 def test_norm_refusals(lib):
