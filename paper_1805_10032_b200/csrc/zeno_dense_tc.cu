@@ -466,7 +466,7 @@ bool encode(CUtensorMap *map, CUtensorMapDataType type, const Rows &v, int elem,
     const bool shared = m > 1 && v.group == 0;
     const cuuint64_t row = (cuuint64_t)(n > 1 ? v.row : (cols * elem + 15) / 16 * 16 / elem) * elem;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)n, (cuuint64_t)(shared ? 1 : m)};
-    const cuuint64_t strides[2] = {row, m > 1 && !shared ? (cuuint64_t)v.group * elem : row * (cuuint64_t)n};
+    const cuuint64_t strides[2] = {row, m > 1 && !shared ? (cuuint64_t)v.group * elem : row};
     const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)kTokens, 1}, ones[3] = {1, 1, 1};
     return enc(map, type, 3, v.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

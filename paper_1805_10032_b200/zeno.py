@@ -461,7 +461,7 @@ def score_lsq_static(x, V, A, y, gamma, rho, scores, losses=None, norms=None, m=
 # No handle: the device is the tensors', the stream its current one unless one is given, and what a call allocates (outputs
 # that are not passed in, scratch) belongs to that stream.  Activations are [m, n, columns] -- n tokens of each of m workers or
 # models -- or [n, columns]; any strides whose last one is 1, and inputs may be expanded over the groups.  Arguments that do
-# not fit raise ValueError, what the library refuses raises ZenoError.
+# not fit raise ValueError, what the library refuses raises ZenoError.  They record nothing for autograd: a backward pass is a call.
 
 SAVED_BLOCK = 128
 MAX_TOP = 32
