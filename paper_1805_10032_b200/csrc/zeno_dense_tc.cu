@@ -174,6 +174,8 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
     __syncthreads();
     cluster_barrier();                        // the other block's barriers are there
     tc_fence_after();
+    pdl_launch_dependents();                  // those wait for this kernel's end before they touch what it writes
+    pdl_wait();                               // dY's terms
     const uint32_t tmem = tmem_base_slot;
     volatile int *abortp = &abort_state[0];
     if (warp == 0) wait_for_nothing(smem_u32(&never_bar), abortp);
@@ -416,6 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
 template <typename T, int TERMS>
 __global__ void __launch_bounds__(256) dense_terms_kernel(Rows dy, int64_t rows, int64_t n, int64_t outputs, int64_t pitch, __nv_bfloat16 *out, int vectors) {
     const int64_t per_row = pitch / 8, total = rows * per_row;
+    pdl_launch_dependents();
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
         const int64_t r = q / per_row, o = (q - r * per_row) * 8, group = r / n;
         const T *from = static_cast<const T *>(dy.data) + dy.at(r) + o;
@@ -445,17 +448,26 @@ __global__ void __launch_bounds__(256) dense_terms_kernel(Rows dy, int64_t rows,
     }
 }
 
-// the parts' sums
-template <typename P>
+// the parts' sums, N neighbouring entries a thread
+template <typename P, int N>
 __global__ void __launch_bounds__(256) dense_join_kernel(const float *part, int splits, int64_t per_group, int64_t total, P *dw, int64_t ldw) {
+    pdl_launch_dependents();
     pdl_wait();
-    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t q = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N;
     if (q >= total) return;
-    float s = 0.f;
+    float s[N] = {};
 #pragma unroll 8
-    for (int k = 0; k < splits; ++k) s += part[k * total + q];
+    for (int k = 0; k < splits; ++k) {
+        alignas(16) float v[N];
+        if constexpr (N == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(part + k * total + q);
+        else v[0] = part[k * total + q];
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] += v[j];
+    }
     const int64_t group = q / per_group;
-    put(dw + group * ldw + (q - group * per_group), s);
+    P *to = dw + group * ldw + (q - group * per_group);
+#pragma unroll
+    for (int j = 0; j < N; ++j) put(to + j, s[j]);
 }
 
 uint32_t spin_limit = kSpinLimit;
@@ -565,13 +577,16 @@ cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &d, cu
     }
     // equal shares: the fewest pairs that make as many rounds as all would
     const int64_t most = sms / 2, rounds = (a.items + most - 1) / most, pairs = (a.items + rounds - 1) / rounds;
-    e = launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), kSmem, s, false, map_dy, map_codes, a);
+    e = launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), kSmem, s, p.terms > 0, map_dy, map_codes, a);
     if (e != cudaSuccess || p.splits == 1) return e;
     const int64_t per_group = d.outputs * d.inputs, total = per_group * d.m;
-    const dim3 grid((unsigned)((total + 255) / 256));
+    const int n = per_group % 4 == 0 ? 4 : 1;
+    const dim3 grid((unsigned)((total / n + 255) / 256));
     if (param_type == ZENO_BF16)
-        return launch_chained(dense_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, true, a.part, p.splits, per_group, total, static_cast<__nv_bfloat16 *>(d.dw), d.ldw);
-    return launch_chained(dense_join_kernel<float>, grid, dim3(256), 0, s, true, a.part, p.splits, per_group, total, static_cast<float *>(d.dw), d.ldw);
+        return launch_chained(n == 4 ? dense_join_kernel<__nv_bfloat16, 4> : dense_join_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, s, true, a.part, p.splits,
+                              per_group, total, static_cast<__nv_bfloat16 *>(d.dw), d.ldw);
+    return launch_chained(n == 4 ? dense_join_kernel<float, 4> : dense_join_kernel<float, 1>, grid, dim3(256), 0, s, true, a.part, p.splits, per_group, total,
+                          static_cast<float *>(d.dw), d.ldw);
 }
 
 void set_operator_wait_limit(uint32_t polls) { spin_limit = polls; }

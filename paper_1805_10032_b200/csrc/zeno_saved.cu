@@ -143,28 +143,27 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_p
     }
 }
 
-// dW of a tile of 64 outputs by 64 inputs of one group in a block: 16 rows at a time through shared memory, the next ones on their way into
+// dW of a tile of 64 outputs by 64 inputs of one group in a block: ROWS rows at a time through shared memory, the next ones on their way into
 // registers, 4 x 4 sums a thread; db with the first tile of the inputs.
-template <typename T, typename P>
+template <typename T, typename P, int ROWS>
 __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
-    constexpr int kTile = 64, kRows = 16, kEach = kRows * kTile / 256;
-    __shared__ float sd[kRows][kTile], sx[kRows][kTile];
+    constexpr int kTile = 64, kEach = ROWS * kTile / 256, kApart = ROWS / kEach;
+    __shared__ __align__(16) float sd[ROWS][kTile], sx[ROWS][kTile];
     const int64_t o0 = (int64_t)blockIdx.y * kTile, k0 = (int64_t)blockIdx.x * kTile;
     const int i = blockIdx.z, tx = threadIdx.x & 15, ty = threadIdx.x >> 4, c = threadIdx.x % kTile, t = threadIdx.x / kTile;
     const bool has_o = o0 + c < a.outputs, has_k = k0 + c < a.inputs;
     const T *dy = static_cast<const T *>(a.dy.data) + i * a.dy.group + o0 + c;
     const uint8_t *codes = static_cast<const uint8_t *>(a.codes.data) + i * a.codes.group + k0 + c;
     const float *scales = static_cast<const float *>(a.scales.data) + i * a.scales.group + (k0 + c) / kBlock;
-    float acc[4][4] = {}, bias = 0.f, d[kEach], scale[kEach];
+    float acc[4][4] = {}, bias = 0.f, scale[kEach];
+    T d[kEach];
     uint8_t code[kEach];
     auto fetch = [&](int64_t t0) {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const int64_t row = t0 + t + e * (kRows / kEach);
-            d[e] = scale[e] = 0.f;
-            code[e] = 0;
-            if (row >= a.n) continue;
-            if (has_o) d[e] = value_of(dy + row * a.dy.row);
+            const int64_t row = t0 + t + e * kApart;
+            if (row >= a.n) break;
+            if (has_o) d[e] = dy[row * a.dy.row];
             if (has_k) {
                 code[e] = codes[row * a.codes.row];
                 scale[e] = scales[row * a.scales.row];
@@ -172,33 +171,46 @@ __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
         }
     };
     fetch(0);
-    for (int64_t t0 = 0; t0 < a.n; t0 += kRows) {
+    for (int64_t t0 = 0; t0 < a.n; t0 += ROWS) {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            sd[t + e * (kRows / kEach)][c] = d[e];
-            sx[t + e * (kRows / kEach)][c] = saved_value(code[e], scale[e]);
+            const bool on = t0 + t + e * kApart < a.n;
+            sd[t + e * kApart][c] = on && has_o ? value_of(&d[e]) : 0.f;
+            sx[t + e * kApart][c] = on && has_k ? saved_value(code[e], scale[e]) : 0.f;
         }
         __syncthreads();
-        fetch(t0 + kRows);
-        if (threadIdx.x < kTile)
+        fetch(t0 + ROWS);
+        if (a.db && blockIdx.x == 0 && threadIdx.x < kTile)
 #pragma unroll
-            for (int q = 0; q < kRows; ++q) bias += sd[q][threadIdx.x];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r)
+            for (int r = 0; r < ROWS; ++r) bias += sd[r][threadIdx.x];
+#pragma unroll 8
+        for (int r = 0; r < ROWS; ++r) {
+            const float4 dr = *reinterpret_cast<const float4 *>(&sd[r][4 * ty]), xr = *reinterpret_cast<const float4 *>(&sx[r][4 * tx]);
+            const float df[4] = {dr.x, dr.y, dr.z, dr.w}, xf[4] = {xr.x, xr.y, xr.z, xr.w};
 #pragma unroll
             for (int p = 0; p < 4; ++p)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(sd[r][ty + 16 * p], sx[r][tx + 16 * q], acc[p][q]);
+                for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(df[p], xf[q], acc[p][q]);
+        }
         __syncthreads();
     }
     P *dw = static_cast<P *>(a.dw) + i * a.ldw;
+    // through shared memory, ROWS outputs at a time, so that a warp writes a row's entries side by side
+    float (*out)[kTile] = sd;
 #pragma unroll
-    for (int p = 0; p < 4; ++p)
+    for (int part = 0; part < kTile / ROWS; ++part) {
+        if (ty / (ROWS / 4) == part)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int64_t o = o0 + ty + 16 * p, k = k0 + tx + 16 * q;
-            if (o < a.outputs && k < a.inputs) put(dw + o * a.inputs + k, acc[p][q]);
+            for (int p = 0; p < 4; ++p)
+                *reinterpret_cast<float4 *>(&out[4 * (ty % (ROWS / 4)) + p][4 * tx]) = make_float4(acc[p][0], acc[p][1], acc[p][2], acc[p][3]);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int64_t o = o0 + part * ROWS + t + e * kApart;
+            if (o < a.outputs && has_k) put(dw + o * a.inputs + k0 + c, out[t + e * kApart][c]);
         }
+        __syncthreads();
+    }
     if (a.db && blockIdx.x == 0 && threadIdx.x < kTile && has_o) put(static_cast<P *>(a.db) + i * a.ldb + o0 + threadIdx.x, bias);
 }
 
@@ -243,6 +255,7 @@ __global__ void __launch_bounds__(kBiasWarps * 32) dense_bias_kernel(DenseGradAr
             if (to < a.outputs) put(static_cast<P *>(a.db) + i * a.ldb + to, v);
         }
     if (cluster > 1) cluster_barrier();
+    pdl_wait();        // nothing here needs what went before; what comes after needs both
 }
 
 template <typename T, typename P, int N>
@@ -250,23 +263,24 @@ cudaError_t dense_bias(const DenseGradArgs &a, cudaStream_t s) {
     int cluster = 1;
     while (cluster < 8 && a.n > cluster * 64) cluster *= 2;          // eight rows a warp and more
     const dim3 grid(cluster, (unsigned)((a.outputs + 32 * N - 1) / (32 * N)), a.m);
-    if (cluster == 1) return launch_chained(dense_bias_kernel<T, P, N>, grid, dim3(kBiasWarps * 32), 0, s, false, a, cluster);
-    return launch_clustered(dense_bias_kernel<T, P, N>, cluster, grid, dim3(kBiasWarps * 32), 0, s, false, a, cluster);
+    if (cluster == 1) return launch_chained(dense_bias_kernel<T, P, N>, grid, dim3(kBiasWarps * 32), 0, s, true, a, cluster);
+    return launch_clustered(dense_bias_kernel<T, P, N>, cluster, grid, dim3(kBiasWarps * 32), 0, s, true, a, cluster);
 }
 
-// Few rows of few tiles are over on the CUDA cores, in one launch, before the tensor cores' launches are: a step of 16 rows of as many tiles as
-// are resident takes about 1.5 us there, the tensor cores' launches 13 us in all with dY's terms 25 (binary32, 12 groups of
-// 37 rows, 301 x 131: 12 us against 32; 4 groups of 100 rows, 512 x 512: 19 against 32).
+// Few rows of few tiles are over on the CUDA cores, in one launch, before the tensor cores' launches are.  Beside what any launch costs, as many tiles
+// as are resident take about 3 us there for every 32 rows (2 for the only 16); the tensor cores' kernel and the sums of dY 9 us, with dY's terms 13
+// and more (12 groups of 37 rows, 301 x 131: 6 us against 17 in binary32; 8 groups of 200 rows, 304 x 304: 22 against 19).
 bool dense_on_tensor_cores(int type, const DenseGradArgs &a) {
-    const int64_t tiles = (a.inputs + 63) / 64 * ((a.outputs + 63) / 64) * a.m, waves = (tiles + 591) / 592, steps = (a.n + 15) / 16;
-    return waves * steps > (type == ZENO_F32 ? 12 : 6);
+    const int64_t tiles = (a.inputs + 63) / 64 * ((a.outputs + 63) / 64) * a.m, waves = (tiles + 443) / 444;
+    const bool as_it_lies = type == ZENO_BF16 && aligned_to(a.dy, a.m, a.n, 2, 16);
+    return waves * (a.n <= 16 ? 2 : (a.n + 31) / 32 * 3) > (as_it_lies ? 8 : 12);
 }
 
 template <typename T, typename P>
 cudaError_t dense_gradient(int type, int param_type, const DenseGradArgs &a, cudaStream_t s) {
     cudaError_t e = dense_on_tensor_cores(type, a) ? launch_dense_tc(type, param_type, a, s) : cudaErrorNotSupported;
     if (e == cudaErrorNotSupported)
-        return launch_chained(dense_any_kernel<T, P>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
+        return launch_chained(a.n <= 16 ? dense_any_kernel<T, P, 16> : dense_any_kernel<T, P, 32>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
     if (e == cudaSuccess && a.db) {
         constexpr int N = 16 / sizeof(T);
         e = a.outputs % N == 0 && aligned_to(a.dy, a.m, a.n, sizeof(T), 16) ? dense_bias<T, P, N>(a, s) : dense_bias<T, P, 1>(a, s);
