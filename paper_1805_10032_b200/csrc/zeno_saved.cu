@@ -102,9 +102,11 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_p
     const uint32_t r = on ? q / strips_per_row : 0;
     const int blk = (int)(on ? q - r * strips_per_row : 0) * kStrip, col = blk * kBlock + lane * 8;
     const int cols = (int)a.cols;
-    const T *x = static_cast<const T *>(a.x.data) + a.x.at(r) + col;
-    uint8_t *codes = static_cast<uint8_t *>(a.codes.data) + a.codes.at(r) + col;
-    float *scales = static_cast<float *>(a.scales.data) + a.scales.at(r) + blk;
+    const uint32_t g = r / (uint32_t)a.n;
+    const int64_t group = g, row = r - g * (uint32_t)a.n;
+    const T *x = static_cast<const T *>(a.x.data) + group * a.x.group + row * a.x.row + col;
+    uint8_t *codes = static_cast<uint8_t *>(a.codes.data) + group * a.codes.group + row * a.codes.row + col;
+    float *scales = static_cast<float *>(a.scales.data) + group * a.scales.group + row * a.scales.row + blk;
     Eight e[kStrip];
 #pragma unroll
     for (int i = 0; i < kStrip; ++i) {
