@@ -230,13 +230,21 @@ __global__ void __launch_bounds__(kBiasWarps * 32) dense_bias_kernel(DenseGradAr
 #pragma unroll
     for (int k = 0; k < N; ++k) s[k] = 0.f;
     if (o < a.outputs) {
-#pragma unroll 8
-        for (int64_t t = rank * kBiasWarps + warp; t < a.n; t += cluster * kBiasWarps) {
-            alignas(16) T e[N];
-            if constexpr (N * sizeof(T) == 16) *reinterpret_cast<uint4 *>(e) = __ldg(reinterpret_cast<const uint4 *>(dy + t * a.dy.row));
-            else e[0] = dy[t * a.dy.row];
+        constexpr int kAtOnce = 8;                               // rows' loads in flight
+        const int64_t step = cluster * kBiasWarps;
+        for (int64_t t = rank * kBiasWarps + warp; t < a.n; t += kAtOnce * step) {
+            alignas(16) T e[kAtOnce][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) s[k] += value_of(e + k);
+            for (int u = 0; u < kAtOnce; ++u)
+                if (t + u * step < a.n) {
+                    if constexpr (N * sizeof(T) == 16) *reinterpret_cast<uint4 *>(e[u]) = __ldg(reinterpret_cast<const uint4 *>(dy + (t + u * step) * a.dy.row));
+                    else e[u][0] = dy[(t + u * step) * a.dy.row];
+                }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+                if (t + u * step < a.n)
+#pragma unroll
+                    for (int k = 0; k < N; ++k) s[k] += value_of(&e[u][k]);
         }
     }
 #pragma unroll
@@ -261,12 +269,20 @@ __global__ void __launch_bounds__(kBiasWarps * 32) dense_bias_kernel(DenseGradAr
 }
 
 template <typename T, typename P, int N>
-cudaError_t dense_bias(const DenseGradArgs &a, cudaStream_t s) {
-    int cluster = 1;
-    while (cluster < 8 && a.n > cluster * 64) cluster *= 2;          // eight rows a warp and more
+cudaError_t dense_bias(const DenseGradArgs &a, int cluster, cudaStream_t s) {
     const dim3 grid(cluster, (unsigned)((a.outputs + 32 * N - 1) / (32 * N)), a.m);
     if (cluster == 1) return launch_chained(dense_bias_kernel<T, P, N>, grid, dim3(kBiasWarps * 32), 0, s, true, a, cluster);
     return launch_clustered(dense_bias_kernel<T, P, N>, cluster, grid, dim3(kBiasWarps * 32), 0, s, true, a, cluster);
+}
+
+// 16 bytes of outputs a lane where that still gives every SM a block
+template <typename T, typename P>
+cudaError_t dense_bias(const DenseGradArgs &a, cudaStream_t s) {
+    constexpr int N = 16 / sizeof(T);
+    int cluster = 1;
+    while (cluster < 8 && a.n > cluster * 64) cluster *= 2;          // eight rows a warp and more
+    const bool many = (a.outputs + 32 * N - 1) / (32 * N) * a.m * cluster >= 148;
+    return many && a.outputs % N == 0 && aligned_to(a.dy, a.m, a.n, sizeof(T), 16) ? dense_bias<T, P, N>(a, cluster, s) : dense_bias<T, P, 1>(a, cluster, s);
 }
 
 // Few rows of few tiles are over on the CUDA cores, in one launch, before the tensor cores' launches are.  Beside what any launch costs, as many tiles
@@ -283,11 +299,7 @@ cudaError_t dense_gradient(int type, int param_type, const DenseGradArgs &a, cud
     cudaError_t e = dense_on_tensor_cores(type, a) ? launch_dense_tc(type, param_type, a, s) : cudaErrorNotSupported;
     if (e == cudaErrorNotSupported)
         return launch_chained(a.n <= 16 ? dense_any_kernel<T, P, 16> : dense_any_kernel<T, P, 32>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
-    if (e == cudaSuccess && a.db) {
-        constexpr int N = 16 / sizeof(T);
-        e = a.outputs % N == 0 && aligned_to(a.dy, a.m, a.n, sizeof(T), 16) ? dense_bias<T, P, N>(a, s) : dense_bias<T, P, 1>(a, s);
-    }
-    return e;
+    return e == cudaSuccess && a.db ? dense_bias<T, P>(a, s) : e;
 }
 
 }  // namespace
