@@ -13,9 +13,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // exp is zero in binary32 below this: a logarithm under it may be taken as it, so that zero times it is zero
 constexpr float kLogOfNothing = -200.f;
-// Logits between -kFar and kFar go by powers of two, whose products with log2 e stay finite; rows whose largest logit is
-// outside (masked by the type's lowest value throughout, or not finite) are summed by the definition.
-constexpr float kFar = 1e38f;
+// Rows whose largest logit is between -kFar and kFar go by powers of two: M, rounded, is there off the largest z log2 e by at most 8, so that
+// no 2^t overflows.  Entries below -kFar (masks) are kept at that, where they add nothing to such a row.  Other rows (masked
+// throughout, or not finite) are summed by the definition.
+constexpr float kFar = 134217728.f;
 constexpr float kUnset = -kFar * kLog2e;      // the reference of nothing
 constexpr float kSlack = 4.f;      // how far (in logits) the reference may fall behind the largest logit before it moves
 constexpr int kMaxTop = ZENO_MAX_TOP;
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
         for (int i = 1; i < kBatch; ++i) most = fmaxf(most, V::most(raw[i]));
         if (TOP) largest = fmaxf(largest, most);
         if (most > limit) {
-            move(most * kLog2e);
+            move(__fmul_rn(most, kLog2e));       // rounded before it is subtracted from anything
             limit = most + kSlack;
         }
         const Two c = both(kLog2e), m = both(-M);
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
     const float v_rest = has_rest ? value_of(z + rest_j) : -INFINITY;
     if (has_rest) {
         if (v_rest > limit) {
-            move(v_rest * kLog2e);
+            move(__fmul_rn(v_rest, kLog2e));
             limit = v_rest;
         }
         Sums p = {M, s2.x, e2.x};

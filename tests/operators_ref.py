@@ -112,10 +112,12 @@ def token_logprobs(z, targets, top):
     entropy = torch.where(empty, 0.0, log_s - (p * dd).sum(-1))
     given = (t >= 0) & (t < vocab)
     zt = z.gather(-1, torch.where(given, t, 0).unsqueeze(-1)).squeeze(-1)
-    lp = torch.where(given, torch.where(empty, -float("inf"), zt - lse), 0.0)
+    of = lambda v: torch.where(empty.reshape(empty.shape + (1,) * (v.dim() - empty.dim())), -float("inf"),  # noqa: E731
+                               (v - m.reshape(m.shape[:-1] + (1,) * (v.dim() - empty.dim()))) - log_s.reshape(empty.shape + (1,) * (v.dim() - empty.dim())))
+    lp = torch.where(given, of(zt), 0.0)
     order = torch.where(torch.isnan(z), -float("inf"), z)
     idx = torch.sort(order, dim=-1, descending=True, stable=True).indices[..., :top]
-    top_lp = torch.where(empty.unsqueeze(-1), -float("inf"), z.gather(-1, idx) - lse.unsqueeze(-1))
+    top_lp = of(z.gather(-1, idx))
     # an exponent t = d log2 e is off by 2 U |t| + U, so exp by (3 |d| + 4) U; S by that, weighted, and the chains
     k = (vocab / 32 + 32) * U
     depth = (p * dd.abs()).sum(-1).nan_to_num(0.0)
@@ -123,9 +125,10 @@ def token_logprobs(z, targets, top):
     lse_off = s_off + 4 * U * (m.squeeze(-1).abs() + lse.abs())
     fin = lambda v: torch.where(torch.isfinite(v), v, 0.0)  # noqa: E731
     lse_off = fin(lse_off)
-    h_off = fin((s_off + k) * (1 + depth + log_s.abs()) + U * (p * 8 * dd * dd).sum(-1))
-    return (lp, entropy, lse, idx.int(), top_lp, lse_off + 4 * U * fin(zt).abs() * given + 4 * U * fin(lp).abs(), h_off, lse_off,
-            lse_off.unsqueeze(-1) + 4 * U * (fin(z.gather(-1, idx)).abs() + fin(top_lp).abs()))
+    h_off = fin((s_off + k) * (17 + depth + log_s.abs()) + U * (p * 8 * dd * dd).sum(-1))
+    # a log probability comes from z - m and log S, whatever the size of m; m itself may stand 8 powers of two beside the largest entry
+    lp_off = fin(s_off + 4 * U * (log_s.abs() + 16))
+    return (lp, entropy, lse, idx.int(), top_lp, lp_off + 8 * U * fin(lp).abs(), h_off, lse_off, lp_off.unsqueeze(-1) + 8 * U * fin(top_lp).abs())
 
 
 def token_gradient(z, targets, lse, entropy, g, gh):

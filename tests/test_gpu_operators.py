@@ -411,6 +411,39 @@ def test_token_logprobs_of_hard_rows(vocab, act, rows):
 
 
 @pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("vocab", [7, 100, 3000, 30000])
+def test_token_logprobs_under_masks_and_offsets_of_any_size(act, vocab):
+    """Masks by large negative numbers of any size, over part of a row, over all that some threads read, over the whole row; logits far from zero."""
+    g = _gen(vocab)
+    masks = [-1e4, -1e6, -2.0 ** 27, -1.3e8, -1e9, -1e12, -1e20, -1e30, -1e38, float(torch.finfo(act).min), -INF]
+    rows = []
+    for mask in masks:
+        base = torch.randn(vocab, generator=g, device="cuda") * 3
+        part = base.clone()
+        part[vocab // 3:] = mask                            # all but the first third
+        sparse = torch.full((vocab,), mask, device="cuda")
+        sparse[vocab // 2] = 0.5
+        every = torch.full((vocab,), mask, device="cuda")
+        mixed = base.clone()
+        mixed[::2] = mask
+        rows += [part, sparse, every, mixed]
+    for offset in (1e3, 1e6, 1.2e8, 2.0 ** 27, 1.5e8, 1e9, 1e12, 1e30, 3e38):
+        for sign in (1.0, -1.0):
+            rows.append((torch.randn(vocab, generator=g, device="cuda") * 3).double().add(sign * offset).clamp(-3.3e38, 3.3e38).float())
+    z = torch.stack(rows).to(act)
+    z = z.repeat(-(-160 // len(rows)), 1) if vocab <= 3000 else z
+    t = torch.randint(0, vocab, (z.shape[0],), generator=g, device="cuda", dtype=torch.int32)
+    top = min(vocab, 6)
+    got = zeno.token_logprobs(z, t, top=top)
+    want = R.token_logprobs(z, t, top)
+    assert torch.equal(got.top_idx.cpu(), want[3])
+    for k, name, off in ((0, "logprobs", 5), (1, "entropy", 6), (2, "lse", 7), (4, "top_logprobs", 8)):
+        R.assert_near(got[k], want[k], want[off], name)
+    one = zeno.token_logprobs(z[5:6], t[5:6], top=top)     # a row of its own goes to several blocks
+    R.assert_near(one.lse, want[2][5:6], want[7][5:6], "one row")
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
 @pytest.mark.parametrize("rows,vocab", [(300, 1500), (300, 9000), (200, 40003), (3, 70000)])
 def test_token_logprobs_alternatives_among_ties(act, rows, vocab):
     """Few values, so that far more entries reach the last alternative than there are alternatives; blocks of equal entries; rows whose
