@@ -44,6 +44,7 @@ struct DenseTcArgs {
     float *part;                // [split][group][output][input] (splits > 1)
     int64_t items;
     int vector_stores;
+    int followed;               // another kernel of the same call comes after this one
     uint32_t spin_limit;
 };
 
@@ -176,8 +177,8 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
     __syncthreads();
     cluster_barrier();                        // the other block's barriers are there
     tc_fence_after();
-    pdl_launch_dependents();                  // those wait for this kernel's end before they touch what it writes
     pdl_wait();                               // dY's terms
+    if (a.followed) pdl_launch_dependents();  // by a kernel of this call, never by the next call's: that one may read V
     const uint32_t tmem = tmem_base_slot;
     volatile int *abortp = &abort_state[0];
     if (warp == 0) wait_for_nothing(smem_u32(&never_bar), abortp);
@@ -452,9 +453,9 @@ __global__ void __launch_bounds__(256) dense_terms_kernel(Rows dy, int64_t rows,
 
 // the parts' sums, N neighbouring entries a thread
 template <typename P, int N>
-__global__ void __launch_bounds__(256) dense_join_kernel(const float *part, int splits, int64_t per_group, int64_t total, P *dw, int64_t ldw) {
-    pdl_launch_dependents();
+__global__ void __launch_bounds__(256) dense_join_kernel(const float *part, int splits, int64_t per_group, int64_t total, P *dw, int64_t ldw, int followed) {
     pdl_wait();
+    if (followed) pdl_launch_dependents();
     const int64_t q = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N;
     if (q >= total) return;
     float s[N] = {};
@@ -569,6 +570,7 @@ cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &d, cu
     const size_t elem = bf16 ? 2 : 4;
     a.vector_stores = d.inputs * elem % 16 == 0 &&
                       (p.splits > 1 || (reinterpret_cast<uintptr_t>(d.dw) % 16 == 0 && (d.m <= 1 || d.ldw * elem % 16 == 0)));
+    a.followed = p.splits > 1 || d.db;
     a.spin_limit = spin_limit;
     auto *kernel = bf16 ? dense_tc_kernel<__nv_bfloat16> : dense_tc_kernel<float>;
     static PerDeviceOnce attr_set[2];
@@ -586,9 +588,9 @@ cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &d, cu
     const dim3 grid((unsigned)((total / n + 255) / 256));
     if (param_type == ZENO_BF16)
         return launch_chained(n == 4 ? dense_join_kernel<__nv_bfloat16, 4> : dense_join_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, s, true, a.part, p.splits,
-                              per_group, total, static_cast<__nv_bfloat16 *>(d.dw), d.ldw);
+                              per_group, total, static_cast<__nv_bfloat16 *>(d.dw), d.ldw, (int)(d.db != nullptr));
     return launch_chained(n == 4 ? dense_join_kernel<float, 4> : dense_join_kernel<float, 1>, grid, dim3(256), 0, s, true, a.part, p.splits, per_group, total,
-                          static_cast<float *>(d.dw), d.ldw);
+                          static_cast<float *>(d.dw), d.ldw, (int)(d.db != nullptr));
 }
 
 void set_operator_wait_limit(uint32_t polls) { spin_limit = polls; }

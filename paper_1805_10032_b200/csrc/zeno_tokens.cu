@@ -453,7 +453,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
     };
     if (threadIdx.x == 0) {
         if (a.lse) a.lse[r] = plain ? m + log_s : (m + log_s) * kLn2;
-        if (a.entropy) a.entropy[r] = log_s == -INFINITY ? 0.f : (log_s - mean_t) * (plain ? 1.f : kLn2);
+        if (a.entropy) {
+            const float h = log_s == -INFINITY ? 0.f : (log_s - mean_t) * (plain ? 1.f : kLn2);
+            a.entropy[r] = h < 0.f ? 0.f : h;             // a rounding under the definition's bound
+        }
         if (a.logprobs) a.logprobs[r] = given ? log_prob(zt) : 0.f;
     }
     if (TOP && (int)threadIdx.x < top) {

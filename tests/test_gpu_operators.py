@@ -627,6 +627,33 @@ def test_two_graphs_replayed_side_by_side():
         assert all(torch.equal(p, q) for p, q in zip(outs, want))
 
 
+@pytest.mark.parametrize("n,inputs,outputs,act", [(700, 512, 768, BF16), (700, 512, 768, F32), (3000, 256, 256, BF16), (10, 64, 32, F32)])
+def test_gradients_are_there_for_the_call_that_follows(n, inputs, outputs, act):
+    """The rules on the candidates right behind the kernels that write them, with nothing between the calls."""
+    m, d = 5, inputs * outputs
+    g = _gen(12)
+    dy = [_rows(g, m, n, outputs, act, "dense", 0.1) for _ in range(2)]
+    saved = zeno.pack_activations(_rows(g, m, n, inputs, act))
+    V = torch.zeros(m, d, device="cuda")
+    dw = V.unflatten(1, (outputs, inputs))
+    idx = torch.tensor([4, 0, 2], device="cuda", dtype=torch.int32)
+    with zeno.Zeno(zeno.LOSS_LEAST_SQUARES, zeno.F32, (d, 1), False, m_max=m, n_r_max=4) as z:
+        want = []
+        for t in dy:
+            zeno.dense_gradient(t, saved, dw)
+            torch.cuda.synchronize()
+            want.append((z.aggregate(V, idx).clone(), z.median(V).clone(), z.krum(V, 1)[2].clone()))
+            torch.cuda.synchronize()
+        assert not torch.equal(want[0][0], want[1][0])
+        for k in range(20):
+            zeno.dense_gradient(dy[k % 2], saved, dw)
+            got = [z.aggregate(V, idx), z.median(V), z.krum(V, 1)[2]][k % 3]
+            assert torch.equal(got, want[k % 2][k % 3]), k
+            zeno.dense_gradient(dy[1 - k % 2], saved, dw)
+            sums = z.krum(V, 1)[2]
+            assert torch.equal(sums, want[1 - k % 2][2]), k
+
+
 def test_offsets_beyond_32_bits():
     """Rows that start more than 2^32 bytes, and elements, behind the first."""
     cols = 1 << 20
