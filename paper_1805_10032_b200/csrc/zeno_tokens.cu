@@ -470,6 +470,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
 // Elements in a block of its kernel: two rounds of four vectors a thread, half of them in flight.
 constexpr int kGradThreads = 256, kGradBatch = 4;
 
+// From here on lse is rounded to sixteenths and worse (rows masked throughout by large numbers, above all): its row is summed again.
+constexpr float kFarLse = 1048576.f;
+
 // One element: what the row's sums say and the upstream gradients ask for; the target's own term is added apart.
 template <bool ENTROPY>
 __device__ __forceinline__ float token_slope(float z, float lse, float g, float h, float entropy) {
@@ -494,6 +497,17 @@ __global__ void __launch_bounds__(kGradThreads) token_gradient_kernel(TokenGradA
         if (!zero) v = token_slope<ENTROPY>(value_of(z + j), lse, g, h, entropy) + (j == t && given ? g : 0.f);
         put(out + j, v);
     };
+    if (!zero && fabsf(lse) >= kFarLse) {       // one block for the row, which it reads as a whole before it writes: the gradient may lie there
+        if (first != 0) return;
+        __shared__ float scratch[kGradThreads / 32];
+        float m, s, unused;
+        sums_by_definition<T, kGradThreads>(z, a.vocab, scratch, m, s, unused);
+        __syncthreads();
+        const float log_s = logf(s);
+        for (int64_t j = threadIdx.x; j < a.vocab; j += kGradThreads)
+            put(out + j, token_slope<ENTROPY>(value_of(z + j) - m, log_s, g, h, entropy) + (j == t && given ? g : 0.f));
+        return;
+    }
     if (!VECTORS) {
         const int64_t end = min(first + chunk, a.vocab);
         for (int64_t j = first + threadIdx.x; j < end; j += kGradThreads) one(j);

@@ -132,23 +132,32 @@ def token_logprobs(z, targets, top):
 
 
 def token_gradient(z, targets, lse, entropy, g, gh):
-    """(gradient, slack) with the lse and entropy that are given."""
+    """(gradient, slack) with the lse and entropy that are given; far from zero, where lse in binary32 says little, from the logits."""
     z, t, lse, g = z.double().cpu(), targets.long().cpu(), lse.double().cpu().unsqueeze(-1), g.double().cpu()
     vocab = z.shape[-1]
+    far = (lse.abs() >= 2.0 ** 20) & (lse != -float("inf"))
+    if far.any():
+        top = torch.where(far, z.amax(-1, keepdim=True), 0.0)
+        z = z - top
+        lse = torch.where(far, torch.log(torch.exp(z).sum(-1, keepdim=True)), lse)
     given = (t >= 0) & (t < vocab)
     g = torch.where(given, g, 0.0).unsqueeze(-1)
     logp = z - lse
     p = torch.exp(logp)
     hot = torch.zeros_like(z).scatter_(-1, torch.where(given, t, 0).unsqueeze(-1), 1.0) * given.unsqueeze(-1)
+    # where the row is summed again, p is off by its sum too, and log p by as much: chains of vocab / 32 terms, each exponential off by
+    # U (3 |d| + 4), as in token_logprobs
+    depth = torch.where(p > 0, p * logp, 0.0).sum(-1, keepdim=True).abs()
+    s_off = far * U * (vocab / 32 + 32 + 8 + 4 * depth)
     factor, factor_off = g, 4 * U * g.abs() + torch.zeros_like(z)
     size = torch.where(torch.isfinite(z), z.abs(), 0.0) + lse.abs()
     if gh is not None:
         gh, entropy = gh.double().cpu().unsqueeze(-1), entropy.double().cpu().unsqueeze(-1)
         safe = torch.where(p > 0, logp, 0.0)
         factor = g + gh * (safe + entropy)
-        factor_off = 4 * U * (g.abs() + gh.abs() * (size + entropy.abs()))
+        factor_off = 4 * U * (g.abs() + gh.abs() * (size + entropy.abs())) + gh.abs() * s_off
     # log p is off by U (|z| + |lse|) and its exponential by that and U (2 |log p| + 4)
-    rel = U * (4 + 4 * size)
+    rel = U * (4 + 4 * size) + s_off
     none = lse == -float("inf")
     if gh is None:
         none = none | ~given.unsqueeze(-1)

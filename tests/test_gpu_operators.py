@@ -441,6 +441,14 @@ def test_token_logprobs_under_masks_and_offsets_of_any_size(act, vocab):
         R.assert_near(got[k], want[k], want[off], name)
     one = zeno.token_logprobs(z[5:6], t[5:6], top=top)     # a row of its own goes to several blocks
     R.assert_near(one.lse, want[2][5:6], want[7][5:6], "one row")
+    gl, gh = (torch.randn(z.shape[0], generator=g, device="cuda") for _ in range(2))
+    for h in (None, gh):
+        grad, slack = R.token_gradient(z, t, got.lse, got.entropy, gl, h)
+        out = zeno.token_gradient(z, t, got.lse, gl, got.entropy, h)
+        R.assert_near(out, grad, slack, "gradient")
+        inside = z.clone()
+        zeno.token_gradient(inside, t, got.lse, gl, got.entropy, h, out=inside)
+        assert torch.equal(inside, out)
 
 
 @pytest.mark.parametrize("act", [F32, BF16])
