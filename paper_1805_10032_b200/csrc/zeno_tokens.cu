@@ -212,9 +212,9 @@ __device__ __noinline__ void top_by_lists(const T *z, int64_t head, int64_t v_be
 // A row goes to a block, or (few rows) to a cluster of `parts` blocks that join through distributed shared memory.  A warp takes 32
 // x kBatch vectors at a time, all loads ahead of their use.
 //
-// The alternatives cost the pass over the logits one comparison a batch: a thread keeps its largest entry.  The k-th largest of the
-// threads' largest is a bound that k entries reach, and only about k threads have entries that do; theirs are read again (from
-// L2), and what reaches the bound is ranked by counting.  (4096 x 131,072 bfloat16: 174 us without alternatives, 6.2 TB/s; 203 with four, 268 with 32;
+// The alternatives cost the pass over the logits a comparison or two a batch: a thread keeps its largest entry, the batch it was in, and the largest
+// of its other batches.  The k-th largest of the threads' largest is a bound that k entries reach, and only about k threads have
+// entries that do, nearly always in one batch; those are read again, and what reaches the bound is ranked by counting.  (4096 x 131,072 bfloat16: 174 us without alternatives, 6.2 TB/s; 203 with four, 268 with 32;
 // with lists kept by the warps during the pass 340 and 1,047.  8192 x 8000: 51 us, the row's end as long as the row.)
 template <typename T, int THREADS, bool TOP>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ? 12 : 32) logprobs_kernel(LogprobArgs a, int parts) {
@@ -223,12 +223,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
     static_assert(kKeys >= kWarps * kMaxTop && kKeys >= kMaxParts * kMaxTop, "the lists of all warps, of all parts");
     __shared__ float scratch[kWarps];
     __shared__ float warp_sums[kWarps][3];
-    __shared__ float part_sums[4];
+    __shared__ float sums[3];
     __shared__ unsigned long long keys[TOP ? kKeys : 1];
     __shared__ unsigned long long best[TOP ? kMaxTop : 1];
-    __shared__ uint32_t orders[TOP ? THREADS : 1];     // the threads' largest entries; then the threads to look at again
+    __shared__ uint32_t orders[TOP ? THREADS : 1];     // the threads' largest entries
+    __shared__ uint16_t hits[TOP ? THREADS : 1];       // the threads to look at again
     __shared__ uint32_t bound;
-    __shared__ int n_threads, n_keys;
+    __shared__ int hit_batch[TOP ? THREADS : 1];
+    __shared__ int n_single, n_whole, n_keys;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t r = (int)(blockIdx.x / (unsigned)parts);
     const int part = (int)(blockIdx.x - (unsigned)r * (unsigned)parts);
@@ -240,7 +242,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
     const int64_t v_begin = vecs * part / parts, v_end = vecs * (part + 1) / parts;
     const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
     // Until an entry is above -kFar the reference M is 0, where all others (kept at least -kFar) add nothing.
-    float limit = -kFar, largest = -INFINITY;          // the reference moves for entries beyond the limit
+    float limit = -kFar;                               // the reference moves for entries beyond this
+    float largest = -INFINITY, second = -INFINITY;     // of the batches' largest entries; and which batch's
+    int batch = 0, largest_batch = 0;
     float M = 0.f;
     Two s2 = both(0.f), e2 = both(0.f);
     auto move = [&](float to) {
@@ -264,7 +268,16 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
         float most = V::most(raw[0]);
 #pragma unroll
         for (int i = 1; i < kBatch; ++i) most = fmaxf(most, V::most(raw[i]));
-        if (TOP) largest = fmaxf(largest, most);
+        if (TOP) {
+            if (most > largest) {
+                second = largest;
+                largest = most;
+                largest_batch = batch;
+            } else {
+                second = fmaxf(second, most);
+            }
+            ++batch;
+        }
         if (most > limit) {
             move(__fmul_rn(most, kLog2e));       // rounded before it is subtracted from anything
             limit = most + kSlack;
@@ -300,47 +313,70 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
         e2.x = p.e;
         any = true;
     }
-    Sums q = {M, s2.x + s2.y, e2.x + e2.y};
-
+    // The warps' sums and the threads' largest entries; then one warp joins the sums, and another finds the bound: what the largest entries of
+    // `top` threads and few more reach.
+    Sums q = {limit == -kFar ? kUnset : M, s2.x + s2.y, e2.x + e2.y};
+    q = join_first<32>(q);
+    if (lane == 0) {
+        warp_sums[warp][0] = q.M;
+        warp_sums[warp][1] = q.s;
+        warp_sums[warp][2] = q.e;
+    }
     if (TOP) {
-        // the bound: what the largest entries of `top` threads and few more reach
         orders[threadIdx.x] = any ? order_of(fmaxf(largest, v_rest)) : 0u;
-        __syncthreads();
-        if (warp == 0) {
-            uint32_t o[kWarps], at_least = 0;
+        if (threadIdx.x == 0) n_single = n_whole = n_keys = 0;
+    }
+    __syncthreads();
+    if (warp == kWarps - 1) {
+        Sums w = {kUnset, 0.f, 0.f};
+        if (lane < kWarps) w = {warp_sums[lane][0], warp_sums[lane][1], warp_sums[lane][2]};
+        w = join_first<kWarps>(w);
+        if (lane == 0) {
+            sums[0] = w.M;
+            sums[1] = w.s;
+            sums[2] = w.e;
+        }
+    }
+    if (TOP && warp == 0) {
+        uint32_t o[kWarps], at_least = 0;
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) o[k] = orders[k * 32 + lane];
-            uint32_t lowest = ~0u, highest = 0;
+        for (int k = 0; k < kWarps; ++k) o[k] = orders[k * 32 + lane];
+        uint32_t lowest = ~0u, highest = 0;
 #pragma unroll
-            for (int k = 0; k < kWarps; ++k) {
-                lowest = min(lowest, o[k]);
-                highest = max(highest, o[k]);
-            }
-            // `top` threads and more reach at_least, fewer than `top` reach beyond; a few more than wanted will do
-            at_least = __reduce_min_sync(kAll, lowest);
-            uint32_t beyond = __reduce_max_sync(kAll, highest);
-            if (at_least < beyond) {
-                ++beyond;
-                while (beyond - at_least > 1) {
-                    const uint32_t next = at_least + (beyond - at_least) / 2;
-                    int n = 0;
+        for (int k = 0; k < kWarps; ++k) {
+            lowest = min(lowest, o[k]);
+            highest = max(highest, o[k]);
+        }
+        // `top` threads and more reach at_least, fewer than `top` reach beyond; a few more than wanted will do
+        at_least = __reduce_min_sync(kAll, lowest);
+        uint32_t beyond = __reduce_max_sync(kAll, highest);
+        if (at_least < beyond) {
+            ++beyond;
+            while (beyond - at_least > 1) {
+                const uint32_t next = at_least + (beyond - at_least) / 2;
+                int n = 0;
 #pragma unroll
-                    for (int k = 0; k < kWarps; ++k) n += o[k] >= next;
-                    n = (int)__reduce_add_sync(kAll, (unsigned)n);
-                    if (n < top) beyond = next;
-                    else at_least = next;
-                    if (n >= top && n <= top + 8) break;
-                }
-            }
-            if (lane == 0) {
-                bound = at_least;
-                n_threads = n_keys = 0;
+                for (int k = 0; k < kWarps; ++k) n += o[k] >= next;
+                n = (int)__reduce_add_sync(kAll, (unsigned)n);
+                if (n < top) beyond = next;
+                else at_least = next;
+                if (n >= top && n <= top + 8) break;
             }
         }
-        __syncthreads();
+        if (lane == 0) bound = at_least;
+    }
+    __syncthreads();
+    if (TOP) {
         const uint32_t need = bound, own = orders[threadIdx.x];
-        __syncthreads();
-        if (own >= need && any) orders[atomicAdd(&n_threads, 1)] = threadIdx.x;
+        if (own >= need && any) {         // from the front: one batch to read again; from the back: all of them
+            if (order_of(second) >= need) {
+                hits[THREADS - 1 - atomicAdd(&n_whole, 1)] = (uint16_t)threadIdx.x;
+            } else {
+                const int at = atomicAdd(&n_single, 1);
+                hits[at] = (uint16_t)threadIdx.x;
+                hit_batch[at] = largest_batch;
+            }
+        }
         auto offer = [&](float v, int64_t j) {
             if (order_of(v) < need) return;
             const int at = atomicAdd(&n_keys, 1);
@@ -348,19 +384,21 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
         };
         if (has_rest) offer(v_rest, rest_j);
         __syncthreads();
-        const int threads = n_threads, per = (int)((v_end - v_begin + THREADS * kBatch - 1) / (THREADS * kBatch)) * kBatch;
-        const bool few = threads <= 2 * top + 32;
+        const int per = (int)((v_end - v_begin + THREADS * kBatch - 1) / (THREADS * kBatch)) * kBatch;        // a thread's vectors
+        const int singles = n_single * kBatch, vectors = singles + n_whole * per;
+        const bool few = n_single + n_whole <= 2 * top + 32;
         if (few) {
             constexpr int kAtOnce = 4;                // loads in flight
-            for (int i0 = threadIdx.x; i0 < threads * per; i0 += THREADS * kAtOnce) {
+            for (int i0 = threadIdx.x; i0 < vectors; i0 += THREADS * kAtOnce) {
                 uint4 raw[kAtOnce];
                 int64_t at[kAtOnce];
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u) {
                     const int i = i0 + u * THREADS;
                     at[u] = v_end;
-                    if (i < threads * per) {
-                        const int who = (int)orders[i / per], k = i % per;
+                    if (i < vectors) {
+                        const int k = i < singles ? hit_batch[i / kBatch] * kBatch + i % kBatch : (i - singles) % per;
+                        const int who = hits[i < singles ? i / kBatch : THREADS - 1 - (i - singles) / per];
                         at[u] = v_begin + (int64_t)(k / kBatch) * THREADS * kBatch + (who >> 5) * 32 * kBatch + k % kBatch * 32 + (who & 31);
                     }
                     if (at[u] < v_end) raw[u] = __ldcg(zv + at[u]);
@@ -381,38 +419,23 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
         __syncthreads();
     }
 
-    // the warp's sums, the block's, the cluster's
-    if (limit == -kFar) q.M = kUnset;
-    q = join_first<32>(q);
-    if (THREADS > 32) {
-        if (lane == 0) {
-            warp_sums[warp][0] = q.M;
-            warp_sums[warp][1] = q.s;
-            warp_sums[warp][2] = q.e;
-        }
-        __syncthreads();
-        if (warp == 0) {
-            Sums w = {lane < kWarps ? warp_sums[lane][0] : kUnset, lane < kWarps ? warp_sums[lane][1] : 0.f,
-                      lane < kWarps ? warp_sums[lane][2] : 0.f};
-            q = join_first<kWarps>(w);
-        }
-    }
     if (parts > 1) {
-        if (threadIdx.x == 0) {
-            part_sums[0] = q.M;
-            part_sums[1] = q.s;
-            part_sums[2] = q.e;
-        }
         cluster_barrier();
         if (part == 0) {
             if (warp == 0) {
                 Sums w = {kUnset, 0.f, 0.f};
                 if (lane < parts) {
-                    w.M = cluster_load(cluster_addr(&part_sums[0], lane));
-                    w.s = cluster_load(cluster_addr(&part_sums[1], lane));
-                    w.e = cluster_load(cluster_addr(&part_sums[2], lane));
+                    w.M = cluster_load(cluster_addr(&sums[0], lane));
+                    w.s = cluster_load(cluster_addr(&sums[1], lane));
+                    w.e = cluster_load(cluster_addr(&sums[2], lane));
                 }
-                q = join_first<kMaxParts>(w);
+                w = join_first<kMaxParts>(w);
+                __syncwarp();                                  // lane 0's loads are from here too
+                if (lane == 0) {
+                    sums[0] = w.M;
+                    sums[1] = w.s;
+                    sums[2] = w.e;
+                }
             }
             if (TOP) {
                 for (int i = threadIdx.x; i < parts * top; i += THREADS) keys[i] = cluster_load64(cluster_addr(&best[i % top], i / top));
@@ -423,15 +446,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
         cluster_barrier();
         if (part != 0) return;
     }
-    if (THREADS > 32) {
-        if (threadIdx.x == 0) {
-            part_sums[0] = q.M;
-            part_sums[1] = q.s;
-            part_sums[2] = q.e;
-        }
-        __syncthreads();
-        q = {part_sums[0], part_sums[1], part_sums[2]};
-    }
+    q = {sums[0], sums[1], sums[2]};
 
     const bool plain = !(fabsf(q.M) <= 0.99f * kFar * kLog2e);
     float m, log_s, mean_t;
