@@ -214,8 +214,9 @@ __device__ __noinline__ void top_by_lists(const T *z, int64_t head, int64_t v_be
 //
 // The alternatives cost the pass over the logits a comparison or two a batch: a thread keeps its largest entry, the batch it was in, and the largest
 // of its other batches.  The k-th largest of the threads' largest is a bound that k entries reach, and only about k threads have
-// entries that do, nearly always in one batch; those are read again, and what reaches the bound is ranked by counting.  (4096 x 131,072 bfloat16: 174 us without alternatives, 6.2 TB/s; 203 with four, 268 with 32;
-// with lists kept by the warps during the pass 340 and 1,047.  8192 x 8000: 51 us, the row's end as long as the row.)
+// entries that do, nearly always in one batch; those are read again, and what reaches the bound is ranked by counting.  (4096 x 131,072 bfloat16:
+// 174 us without alternatives, 6.2 TB/s; 188 with four, 205 with 32; with lists kept by the warps during the pass 340 and 1,047, and with all of
+// those threads' entries read again, by then from memory, 203 and 281.  8192 x 8000: 51 us, the row's end as long as the row.)
 template <typename T, int THREADS, bool TOP>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ? 12 : 32) logprobs_kernel(LogprobArgs a, int parts) {
     using V = Vec<T>;
@@ -262,7 +263,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int64_t v = base + i * 32 + lane;
-            raw[i] = v < v_end ? (TOP ? __ldcg(zv + v) : __ldcs(zv + v)) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
+            raw[i] = v < v_end ? __ldcs(zv + v) : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
             any |= v < v_end;
         }
         float most = V::most(raw[0]);
