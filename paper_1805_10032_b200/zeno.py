@@ -484,9 +484,9 @@ class TokenLogprobs(NamedTuple):
 
 
 # Calls of a few tokens are over on the GPU in a few microseconds, so here too what the binding spends on a call shows: messages are built only for
-# a refusal, shapes and strides are read once, devices are compared by their index, empty_like (half as dear) is preferred.
+# a refusal, shapes and strides are read once, devices are compared by their index, empty_like and empty_strided (1.4 and 1.6 us) stand in for empty (2.4).
 _DEVICES = [torch.device("cuda", i) for i in range(64)]
-_EMPTY, _EMPTY_LIKE = torch.empty, torch.empty_like
+_EMPTY, _EMPTY_LIKE = torch.empty_strided, torch.empty_like
 _ROWS = RowsDesc
 
 
@@ -547,17 +547,21 @@ def _current(index: int, stream) -> int:
 
 
 def _empty(stream, index: int, shape, dtype) -> torch.Tensor:
-    """An output or scratch: memory of the stream that the call runs on."""
+    """An output or scratch of one to three dimensions, contiguous: memory of the stream that the call runs on."""
+    if len(shape) == 2:
+        strides = shape[1], 1
+    else:
+        strides = (1,) if len(shape) == 1 else (shape[1] * shape[2], shape[2], 1)
     if stream is None:
-        return _EMPTY(shape, dtype=dtype, device=_DEVICES[index])
+        return _EMPTY(shape, strides, dtype=dtype, device=_DEVICES[index])
     with torch.cuda.stream(stream):
-        return _EMPTY(shape, dtype=dtype, device=_DEVICES[index])
+        return _EMPTY(shape, strides, dtype=dtype, device=_DEVICES[index])
 
 
 def _empty_like(stream, t: torch.Tensor, dtype=None) -> torch.Tensor:
     """The same in the shape of t (and its order of dimensions)."""
     if stream is None:
-        return _EMPTY_LIKE(t, dtype=dtype)
+        return _EMPTY_LIKE(t) if dtype is None else _EMPTY_LIKE(t, dtype=dtype)
     with torch.cuda.stream(stream):
         return _EMPTY_LIKE(t, dtype=dtype)
 
@@ -662,7 +666,7 @@ def layer_norm_gradient(dy, x: Union[torch.Tensor, Saved], weight, mean, rstd, d
     elif want_dx:
         dx = _empty_like(stream, dy)
     nbytes = lib.zeno_layer_norm_gradient_workspace(m, n, cols)
-    ws = _empty(stream, dev, nbytes, torch.uint8) if nbytes else None
+    ws = _empty(stream, dev, (nbytes,), torch.uint8) if nbytes else None
     st = lib.zeno_layer_norm_gradient(dev, _type(dy, "dy"), _type(weight, "weight"), _rows(dy, "dy"), x_rows, codes, scales, m, n, cols,
                                       weight.data_ptr(), ldw, mean.data_ptr(), rstd.data_ptr(), None if dx is None else _rows(dx, "dx"),
                                       _ptr(dweight), _ptr(dbias), ldg, _ptr(ws), nbytes, _current(dev, stream))
@@ -702,7 +706,7 @@ def dense_gradient(dy, saved: Saved, dweight, dbias=None, stream=None):
     ldb = 0 if dbias is None else _gradient_row(dbias, m, outputs, dweight.dtype, "dbias")
     kind, dy_rows = _type(dy, "dy"), _rows(dy, "dy")
     nbytes = lib.zeno_dense_gradient_workspace(kind, dy_rows, codes, m, n, inputs, outputs)
-    ws = _empty(stream, dev, nbytes, torch.uint8) if nbytes else None
+    ws = _empty(stream, dev, (nbytes,), torch.uint8) if nbytes else None
     st = lib.zeno_dense_gradient(dev, kind, _type(dweight, "dweight"), dy_rows, codes, scales, m, n, inputs, outputs, dweight.data_ptr(),
                                  strides[0] if len(shape) == 3 else inputs * outputs, _ptr(dbias), ldb, _ptr(ws), nbytes, _current(dev, stream))
     return dweight if st == OK else _done(st, "zeno_dense_gradient")
