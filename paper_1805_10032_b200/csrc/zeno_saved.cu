@@ -27,7 +27,7 @@ __device__ __forceinline__ uint8_t code_of(float v, float inv_scale) {
     return (uint8_t)__nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
 }
 
-// Rows of any alignment: a warp takes a block of one row (3 x 57 x 1029: 3.4 us).
+// Codes of any alignment: a warp takes a block of one row.
 template <typename T>
 __global__ void __launch_bounds__(256) pack_any_kernel(PackArgs a, int64_t blocks_per_row, int64_t blocks) {
     const int lane = threadIdx.x & 31;
@@ -53,10 +53,14 @@ __global__ void __launch_bounds__(256) pack_any_kernel(PackArgs a, int64_t block
     }
 }
 
-// Rows of whole vectors: 16 lanes take a block, eight columns each; a half-warp takes kStrip blocks of a row one behind the
+// 16 lanes take a block, eight columns each; a half-warp takes kStrip blocks of a row one behind the
 // other, with all their loads ahead of the first maximum.  The maxima of four blocks go over the lanes together, and one lane in four works a block's
 // scale out: 9 shuffles instead of 16, a quarter of the scales' arithmetic.  Bound by bytes (20 x 2048 x 4096: bfloat16 84 us, 6.1 TB/s, 88 block by
 // block; binary32 127 us, 6.7 TB/s).
+//
+// Rows that start anywhere (WHOLE false) are read by the aligned 16 bytes that a lane's entries lie in, one more than there would be, and put
+// together by shifts, which are the same for all of a row; 20 x 512 x 4096 in rows of 4097: bfloat16 37 us,
+// binary32 70, either 100 by single entries.
 constexpr int kStrip = 4;
 
 // Eight entries of a row: the bits of their largest magnitude (at least 0x7f800000 if one is not finite), and themselves as pairs.
@@ -96,7 +100,69 @@ struct Eight {
     }
 };
 
-template <typename T>
+// Eight entries that start anywhere.  `from` and `to`: where the first and behind the last entry of the group's rows lie; what is in between may be
+// read, whosever it is.
+template <typename T> struct Shifted {
+    static constexpr int kWords = 2 * sizeof(T);                  // of eight entries
+    uint4 raw[kWords / 4 + 1];
+    unsigned off;
+    __device__ __forceinline__ void load(const T *p, int count, uintptr_t from, uintptr_t to) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p), first = at & ~(uintptr_t)15;
+        off = (unsigned)(at & 15);
+#pragma unroll
+        for (int i = 0; i <= kWords / 4; ++i) raw[i] = make_uint4(0u, 0u, 0u, 0u);
+        const uintptr_t end = at + count * sizeof(T);
+        if (count > 0 && first >= from && ((end + 15) & ~(uintptr_t)15) <= to) {
+#pragma unroll
+            for (int i = 0; i <= kWords / 4; ++i)
+                if (first + i * 16 < end) raw[i] = __ldcs(reinterpret_cast<const uint4 *>(first) + i);
+        } else {                                                  // at the ends of the group's rows
+            uint32_t w[kWords] = {};
+            constexpr int kPer = 4 / sizeof(T);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) {
+                    uint32_t bits;
+                    if constexpr (kPer == 1) bits = reinterpret_cast<const uint32_t *>(p)[i];
+                    else bits = reinterpret_cast<const uint16_t *>(p)[i];
+                    w[i / kPer] |= bits << (i % kPer * 16);
+                }
+            off = 0;
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) raw[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        }
+    }
+    // the entries, those from `count` on zero
+    __device__ __forceinline__ Eight get(int count) const {
+        uint32_t w[kWords + 4];
+#pragma unroll
+        for (int i = 0; i <= kWords / 4; ++i) w[4 * i] = raw[i].x, w[4 * i + 1] = raw[i].y, w[4 * i + 2] = raw[i].z, w[4 * i + 3] = raw[i].w;
+#pragma unroll
+        for (int i = 0; i < kWords + 2; ++i)
+            if (off & 8) w[i] = w[i + 2];
+#pragma unroll
+        for (int i = 0; i < kWords + 1; ++i)
+            if (off & 4) w[i] = w[i + 1];
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (off & 2) * 8);
+        }
+        if (count < 8) {
+            constexpr int kPer = 4 / sizeof(T);
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                if (i * kPer >= count) w[i] = 0u;
+                else if (kPer == 2 && i * kPer + 1 == count) w[i] &= 0xffffu;
+            }
+        }
+        Eight e;
+        e.u = make_uint4(w[0], w[1], w[2], w[3]);
+        if constexpr (kWords == 8) e.v = make_uint4(w[4], w[5], w[6], w[7]);
+        return e;
+    }
+};
+
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_per_row, uint32_t strips) {
     const int lane = threadIdx.x & 15;
     const uint32_t q = blockIdx.x * 16 + (threadIdx.x >> 4);
@@ -113,7 +179,16 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_p
 #pragma unroll
     for (int i = 0; i < kStrip; ++i) {
         e[i].u = e[i].v = make_uint4(0u, 0u, 0u, 0u);
-        if (on && col + i * kBlock < cols) e[i].load(x + i * kBlock);
+        if (WHOLE && on && col + i * kBlock < cols) e[i].load(x + i * kBlock);
+    }
+    if constexpr (!WHOLE) {
+        const T *group_x = static_cast<const T *>(a.x.data) + group * a.x.group;
+        const uintptr_t from = reinterpret_cast<uintptr_t>(group_x), to = reinterpret_cast<uintptr_t>(group_x + (a.n - 1) * a.x.row + cols);
+        Shifted<T> s[kStrip];
+#pragma unroll
+        for (int i = 0; i < kStrip; ++i) s[i].load(x + i * kBlock, on ? max(min(cols - col - i * kBlock, 8), 0) : 0, from, to);
+#pragma unroll
+        for (int i = 0; i < kStrip; ++i) e[i] = s[i].get(on ? max(min(cols - col - i * kBlock, 8), 0) : 0);
     }
     // The blocks' largest magnitudes over the 16 lanes: lanes give half of the blocks away at a time until each has one block left
     static_assert(kStrip == 4, "two steps halve the blocks");
@@ -156,7 +231,12 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_p
                     if (!(fabsf(f[h].y) < INFINITY)) w[h] |= 0x7f00u;
                 }
             }
-            *reinterpret_cast<uint2 *>(codes + i * kBlock) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+            const uint2 c = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+            if (WHOLE || col + i * kBlock + 8 <= cols) *reinterpret_cast<uint2 *>(codes + i * kBlock) = c;
+            else
+#pragma unroll
+                for (int h = 0; h < 7; ++h)
+                    if (col + i * kBlock + h < cols) codes[i * kBlock + h] = (uint8_t)((h < 4 ? c.x : c.y) >> (h % 4 * 8));
         }
     }
 }
@@ -323,11 +403,13 @@ cudaError_t dense_gradient(int type, int param_type, const DenseGradArgs &a, cud
 
 cudaError_t launch_pack(int type, const PackArgs &a, cudaStream_t s) {
     const int64_t per_row = (a.cols + kBlock - 1) / kBlock;
-    const bool aligned = a.cols % 8 == 0 && aligned_to(a.x, a.m, a.n, type == ZENO_BF16 ? 2 : 4, 16) && aligned_to(a.codes, a.m, a.n, 1, 8);
+    const bool whole = a.cols % 8 == 0 && aligned_to(a.x, a.m, a.n, type == ZENO_BF16 ? 2 : 4, 16);
     const int64_t strips_per_row = (per_row + kStrip - 1) / kStrip, strips = strips_per_row * a.m * a.n, grid = (strips + 15) / 16;
-    if (aligned && strips < (int64_t)1 << 31)
-        return launch_chained(type == ZENO_BF16 ? pack_kernel<__nv_bfloat16> : pack_kernel<float>, dim3((unsigned)grid), dim3(256), 0, s, false, a,
-                              (uint32_t)strips_per_row, (uint32_t)strips);
+    if (aligned_to(a.codes, a.m, a.n, 1, 8) && strips < (int64_t)1 << 31) {
+        auto *kernel = type == ZENO_BF16 ? (whole ? pack_kernel<__nv_bfloat16, true> : pack_kernel<__nv_bfloat16, false>)
+                                         : (whole ? pack_kernel<float, true> : pack_kernel<float, false>);
+        return launch_chained(kernel, dim3((unsigned)grid), dim3(256), 0, s, false, a, (uint32_t)strips_per_row, (uint32_t)strips);
+    }
     const int64_t blocks = per_row * a.m * a.n;
     const unsigned any_grid = (unsigned)min((blocks + 7) / 8, (int64_t)148 * 8);
     return launch_chained(type == ZENO_BF16 ? pack_any_kernel<__nv_bfloat16> : pack_any_kernel<float>, dim3(any_grid), dim3(256), 0, s, false, a,

@@ -68,6 +68,29 @@ def test_layer_norm_over_the_sizes(m, n, cols, act, par):
             R.assert_near(got, want[k], want[k + 3], what)
 
 
+@pytest.mark.parametrize("m,n,cols", [(1, 1201, 4093), (3, 450, 1), (5, 301, 33), (21, 60, 201), (7, 190, 256), (2, 700, 777), (150, 8, 1024), (4, 333, 1025),
+                                      (1, 1190, 4096)])
+@pytest.mark.parametrize("act,par", TYPES)
+def test_layer_norm_of_many_rows_that_start_anywhere(m, n, cols, act, par):
+    g = _gen(cols + m)
+    for layout in ("padded", "shared"):
+        x = _rows(g, m, n, cols, act, "padded", 2.0, 0.5)
+        if layout == "shared":
+            x = x[:1].expand(m, n, cols)
+        V = torch.randn(m, 5 + 2 * cols, generator=g, device="cuda").to(par)
+        w, b = V[:, 1:1 + cols], V[:, 3 + cols:3 + 2 * cols]
+        around = torch.full((m, n + 1, cols + 5), NAN, device="cuda", dtype=act)
+        y, mean, rstd = zeno.layer_norm(x, w, b, eps=1e-5, out=around[:, :n, 1:1 + cols])
+        want = R.norm(x, w, b, float(np.float32(1e-5)))
+        for got, k, what in ((y, 0, "y"), (mean, 1, "mean"), (rstd, 2, "rstd")):
+            R.assert_near(got, want[k], want[k + 3], what)
+        assert torch.isnan(around[:, n:]).all() and torch.isnan(around[:, :, 0]).all() and torch.isnan(around[:, :, 1 + cols:]).all()
+        if layout == "padded":                                   # in place, and without bias and statistics
+            kept = y.clone()
+            zeno.layer_norm(x, w, b, eps=1e-5, out=x, want_stats=False)
+            assert torch.equal(x, kept)
+
+
 @pytest.mark.parametrize("layout", ["aligned", "interleaved", "shared"])
 def test_layer_norm_layouts_and_what_lies_around(layout):
     m, n, cols = 3, 5, 264
@@ -218,6 +241,23 @@ def test_pack_activations(rows, cols, act, layout):
     assert torch.equal(value.to(BF16).double(), value)           # exact in bfloat16
     block = scales.double().repeat_interleave(128, -1)[..., :cols]
     assert ((value - x.double()).abs() <= torch.maximum(2.0 ** -4 * x.double().abs(), 2.0 ** -10 * block)).all()
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("cols,stride", [(1, 1), (5, 6), (131, 131), (512, 515), (1029, 1029), (777, 780), (4096, 4097)])
+def test_pack_activations_of_rows_that_start_anywhere(cols, stride, act):
+    """Every offset from a 16-byte boundary, the first and last entries of an allocation among the rows', NaN in all that lies between."""
+    m, n = 2, 9
+    for off in range(16 // act.itemsize):
+        base = torch.full((off + (m * n - 1) * stride + cols,), NAN, device="cuda", dtype=act)
+        x = base[off:].as_strided((m, n, cols), (n * stride, stride, 1))
+        x.copy_(torch.randn(m, n, cols, generator=_gen(cols + off), device="cuda") * 5)
+        codes, scales = zeno.pack_activations(x)
+        want, want_scales = R.pack(x)
+        assert torch.equal(scales.double().cpu(), want_scales) and torch.equal(codes.double().cpu(), want)
+        mixed = x.transpose(0, 1)                              # the groups' rows between one another
+        codes_mixed, scales_mixed = zeno.pack_activations(mixed)
+        assert torch.equal(codes_mixed.view(torch.uint8), codes.transpose(0, 1).view(torch.uint8)) and torch.equal(scales_mixed, scales.transpose(0, 1))
 
 
 def test_pack_activations_borders():
