@@ -706,6 +706,67 @@ __global__ void __launch_bounds__(kGroupThreads, 2) norm_group_kernel(NormArgs a
     }
 }
 
+// The same for rows that start anywhere, by single entries: TPR threads take a row, NV of its entries in a thread's registers, the next row's on their
+// way behind each result.  Every entry costs about a dozen instructions, four of them to memory of some kind.  (21 x 512 x 4096 in rows of 4097:
+// bfloat16 57 us, binary32 78; by norm_row_kernel, where every row fetches its weights, 131 and 141.)
+template <typename T, typename P, int TPR, int NV>
+__global__ void __launch_bounds__(kGroupThreads, 4) norm_single_kernel(NormArgs a) {
+    constexpr int kSide = kGroupThreads / TPR, kWarps = TPR / 32;
+    extern __shared__ __align__(16) float weights_at[];        // w, then b
+    __shared__ float scratch[2][kGroupThreads / 32];
+    const int t = threadIdx.x % TPR, side = threadIdx.x / TPR, cols = (int)a.cols, chunks = gridDim.x, i = blockIdx.y;
+    const int64_t last = a.n * (blockIdx.x + 1) / chunks;
+    int64_t row = a.n * blockIdx.x / chunks + side;
+    const T *x = static_cast<const T *>(a.x.data) + i * a.x.group + t;
+    T *y = static_cast<T *>(a.y.data) + i * a.y.group + t;
+    T raw[NV];
+    auto fetch = [&](int v, int64_t r) {
+        if (r < last && v * TPR + t < cols) raw[v] = x[r * a.x.row + v * TPR];
+    };
+#pragma unroll
+    for (int v = 0; v < NV; ++v) fetch(v, row);
+    float *biases_at = weights_at + cols;
+    for (int j = threadIdx.x; j < cols; j += kGroupThreads) {
+        weights_at[j] = value_of(static_cast<const P *>(a.w) + i * a.ldw + j);
+        biases_at[j] = a.b ? value_of(static_cast<const P *>(a.b) + i * a.ldw + j) : 0.f;
+    }
+    __syncthreads();
+    // the row's average in all of its threads
+    auto average = [&](float s, int which) {
+        s = warp_sum(s);
+        if constexpr (TPR > 32) {
+            if ((t & 31) == 0) scratch[which][threadIdx.x >> 5] = s;
+            asm volatile("bar.sync %0, %1;" ::"r"(side + 1), "n"(TPR) : "memory");
+            s = 0.f;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) s += scratch[which][side * kWarps + k];
+        }
+        return s / (float)cols;
+    };
+    for (; row < last; row += kSide) {
+        float s = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (v * TPR + t < cols) s += value_of(raw + v);
+        const float mean = average(s, 0);
+        s = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (v * TPR + t < cols) s = fmaf(value_of(raw + v) - mean, value_of(raw + v) - mean, s);
+        const float rstd = rsqrtf(average(s, 1) + a.eps);
+        if (t == 0) {
+            if (a.mean) a.mean[i * a.n + row] = mean;
+            if (a.rstd) a.rstd[i * a.n + row] = rstd;
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int j = v * TPR + t;
+            if (j < cols) put(y + row * a.y.row + v * TPR, fmaf((value_of(raw + v) - mean) * rstd, weights_at[j], biases_at[j]));
+            fetch(v, row + kSide);
+        }
+    }
+}
+
 // The blocks' sums of a group: 32 N columns a block, N a lane, eight warps take the blocks in turn.
 template <typename P, int N>
 __global__ void __launch_bounds__(kThreads) norm_join_kernel(const float *part, int chunks, int cols, P *dw, P *db, int64_t ldg) {
@@ -775,6 +836,12 @@ cudaError_t norm_groups(const NormArgs &a, cudaStream_t s) {
     return e != cudaSuccess ? e : launch_chained(kernel, dim3(norm_chunks(a.m, a.n, 1), a.m), dim3(kGroupThreads), kSmem, s, false, a);
 }
 
+template <typename T, typename P, int TPR, int NV>
+cudaError_t norm_singles(const NormArgs &a, cudaStream_t s) {
+    static_assert(TPR * NV * 2 * (int)sizeof(float) <= 48 * 1024, "no attribute needed");
+    return launch_chained(norm_single_kernel<T, P, TPR, NV>, dim3(norm_chunks(a.m, a.n, 1), a.m), dim3(kGroupThreads), 2 * (size_t)a.cols * sizeof(float), s, false, a);
+}
+
 template <typename T, typename P, int N, int TPR, int NV>
 cudaError_t norm_rows(const NormArgs &a, bool wide, cudaStream_t s) {
     const int64_t rows = a.m * a.n;
@@ -811,6 +878,12 @@ cudaError_t layer_norm(const NormArgs &a, cudaStream_t s) {
         if (packs <= 2048) return norm_rows<T, P, N, 512, 4>(a, wide, s);
         if (packs <= 4096) return norm_rows<T, P, N, 1024, 4>(a, wide, s);
     } else {
+        // A block an SM with eight rows each and more (1 x 1200 x 4095 bfloat16: 20 us, 22 by norm_row_kernel; 3 x 300 binary32: 26 and 22)
+        if (norm_chunks(a.m, a.n, 1) * (int64_t)a.m >= kNormBlocks / 4 && a.n * a.m >= kNormBlocks * 2) {
+            if (a.cols <= 256) return norm_singles<T, P, 32, 8>(a, s);
+            if (a.cols <= 1024) return norm_singles<T, P, 64, 16>(a, s);
+            if (a.cols <= 4096) return norm_singles<T, P, 256, 16>(a, s);
+        }
         if (a.cols <= 256) return norm_rows<T, P, 1, 32, 8>(a, false, s);
         if (a.cols <= 1024) return norm_rows<T, P, 1, 64, 16>(a, false, s);
         if (a.cols <= 4096) return norm_rows<T, P, 1, 256, 16>(a, false, s);
