@@ -24,6 +24,23 @@ inline bool aligned_to(const Rows &v, int m, int64_t n, size_t elem, size_t to) 
     return reinterpret_cast<uintptr_t>(v.data) % to == 0 && (n <= 1 || v.row * elem % to == 0) && (m <= 1 || v.group * elem % to == 0);
 }
 
+// The 16 bytes that start `off` bytes into a and end in b (off: 0 .. 14; a multiple of ALIGN, 2 or 4).
+template <int ALIGN>
+__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, unsigned off) {
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i)
+        if (off & 8) w[i] = w[i + 2];
+#pragma unroll
+    for (int i = 0; i < 5; ++i)
+        if (off & 4) w[i] = w[i + 1];
+    if constexpr (ALIGN == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (off & 2) * 8);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 struct NormArgs {
     Rows x, y;
     int m;

@@ -59,8 +59,8 @@ __global__ void __launch_bounds__(256) pack_any_kernel(PackArgs a, int64_t block
 // block; binary32 127 us, 6.7 TB/s).
 //
 // Rows that start anywhere (WHOLE false) are read by the aligned 16 bytes that a lane's entries lie in, one more than there would be, and put
-// together by shifts, which are the same for all of a row; 20 x 512 x 4096 in rows of 4097: bfloat16 37 us,
-// binary32 70, either 100 by single entries.
+// together by shifts, which are the same for all of a row; 20 x 512 x 4096 in rows of 4097: bfloat16 38 us,
+// binary32 58, either 100 by single entries.
 constexpr int kStrip = 4;
 
 // Eight entries of a row: the bits of their largest magnitude (at least 0x7f800000 if one is not finite), and themselves as pairs.
@@ -134,18 +134,12 @@ template <typename T> struct Shifted {
     }
     // the entries, those from `count` on zero
     __device__ __forceinline__ Eight get(int count) const {
-        uint32_t w[kWords + 4];
-#pragma unroll
-        for (int i = 0; i <= kWords / 4; ++i) w[4 * i] = raw[i].x, w[4 * i + 1] = raw[i].y, w[4 * i + 2] = raw[i].z, w[4 * i + 3] = raw[i].w;
-#pragma unroll
-        for (int i = 0; i < kWords + 2; ++i)
-            if (off & 8) w[i] = w[i + 2];
-#pragma unroll
-        for (int i = 0; i < kWords + 1; ++i)
-            if (off & 4) w[i] = w[i + 1];
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (off & 2) * 8);
+        Eight e;
+        e.u = shifted<sizeof(T)>(raw[0], raw[1], off);
+        uint32_t w[8] = {e.u.x, e.u.y, e.u.z, e.u.w};
+        if constexpr (kWords == 8) {
+            e.v = shifted<sizeof(T)>(raw[1], raw[2], off);
+            w[4] = e.v.x, w[5] = e.v.y, w[6] = e.v.z, w[7] = e.v.w;
         }
         if (count < 8) {
             constexpr int kPer = 4 / sizeof(T);
@@ -155,7 +149,6 @@ template <typename T> struct Shifted {
                 else if (kPer == 2 && i * kPer + 1 == count) w[i] &= 0xffffu;
             }
         }
-        Eight e;
         e.u = make_uint4(w[0], w[1], w[2], w[3]);
         if constexpr (kWords == 8) e.v = make_uint4(w[4], w[5], w[6], w[7]);
         return e;

@@ -555,6 +555,33 @@ def test_token_gradient(vocab, act, with_entropy):
         del kept
 
 
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("vocab", [1, 7, 8, 22, 24, 39, 131, 8192, 20011])
+def test_token_gradient_of_rows_that_start_anywhere(vocab, act):
+    """Logits and gradient at every offset from a 16-byte boundary, the first and last entries of an allocation among the rows': the bits of
+    the same rows side by side."""
+    g = _gen(vocab)
+    n, per = 3, 16 // act.itemsize
+    values = (torch.randn(n, vocab, generator=g, device="cuda") * 3).to(act)
+    t = torch.tensor([0, vocab - 1, -1], device="cuda", dtype=torch.int32)
+    s = zeno.token_logprobs(values, t)
+    gl, gh = torch.randn(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+    want = zeno.token_gradient(values, t, s.lse, gl, s.entropy, gh)
+    exact, slack = R.token_gradient(values, t, s.lse, s.entropy, gl, gh)
+    R.assert_near(want, exact, slack, "gradient")
+    for a in range(per):
+        for b in {0, (a + 1) % per, per - 1}:
+            stride, stride_out = vocab + a % 4, vocab + b % 3
+            z = torch.full((a + (n - 1) * stride + vocab,), NAN, device="cuda", dtype=act)[a:].as_strided((n, vocab), (stride, 1))
+            z.copy_(values)
+            base = torch.full((b + n * stride_out + 1,), NAN, device="cuda", dtype=act)
+            out = base[b:].as_strided((n, vocab), (stride_out, 1))
+            zeno.token_gradient(z, t, s.lse, gl, s.entropy, gh, out=out)
+            assert torch.equal(out, want)
+            out.fill_(NAN)                                       # and nothing else was written
+            assert torch.isnan(base).all()
+
+
 def test_token_gradient_against_differences():
     g = _gen(2)
     z = torch.randn(1, 4, 50, generator=g, device="cuda")
