@@ -23,7 +23,10 @@ constexpr int kPairTile = 2 * kHalf;
 constexpr int kSubBytes = kTokens * 128;      // 64 tokens of 64 bfloat16 (or 128 codes) in 128-byte rows
 constexpr int kABytes = 2 * kSubBytes, kBBytes = 2 * kSubBytes, kCodeBytes = kSubBytes, kScaleBytes = kTokens * 4;
 constexpr int kStages = 5, kCodeStages = 6;
-constexpr int kTurnBytes = 32 * 17 * 4;       // a warp's 32 x 16 sums on their way from rows to columns
+// A warp's sums of 32 rows on their way from a row a lane to 64 bytes of a row in four lanes' stores (or 16 sums in 16 lanes'): 80 bytes apart, so that
+// eight lanes' 16 bytes meet all banks.  By lanes that store along their own rows, 16 bytes of 32 rows at a time, a tile takes about twice as long, which
+// shows where tokens are few (30 x 45 tokens, 2320 x 3920 into binary32: 304 us against 577; 8 x 2048, 4096 x 4096 into bfloat16: 500 against 521).
+constexpr int kTurnPitch = 80, kTurnBytes = 32 * kTurnPitch;
 constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * (kCodeBytes + kScaleBytes) + 4 * kTurnBytes + 1024;
 // The warps that convert come in sets, which take the stages in turn: a stage is a chain of waits, loads, arithmetic, stores and an
 // arrival that one set alone would follow from end to end (8 x 2048 tokens, 4096 x 4096, with
@@ -339,7 +342,6 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
             const int64_t o = (int64_t)ot * kPairTile + rank * kHalf + quad * 32 + lane, k0 = (int64_t)it * kPairTile;
             P *dw = a.splits > 1 ? reinterpret_cast<P *>(a.part) + (((int64_t)split * a.d.m + group) * a.d.outputs + o) * a.d.inputs + k0
                                  : static_cast<P *>(a.d.dw) + group * a.d.ldw + o * a.d.inputs + k0;
-            const bool mine = o < a.d.outputs;
             const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + set * 256;
 #pragma unroll 1
             for (int c0 = 0; c0 < kPairTile; c0 += 32) {
@@ -356,29 +358,55 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                         else mbar_arrive_cluster(remote_dempty + set * 8);
                     }
                 }
+                uint8_t *turns = scale_ring + kCodeStages * kScaleBytes + quad * kTurnBytes;
+                const int rows = (int)min((int64_t)32, a.d.outputs - (o - lane));
+                const int pitch = (int)a.d.inputs;
+                P *corner = dw - lane * pitch + c0;
                 if (a.vector_stores) {
-                    if (!mine) continue;
-                    constexpr int kPer = 16 / sizeof(P);
+                    constexpr int kPer = 16 / sizeof(P), kAtOnce = 4 * kPer;
 #pragma unroll
-                    for (int q = 0; q < 32 / kPer; ++q) {
-                        alignas(16) P e[kPer];
+                    for (int h = 0; h < 32 / kAtOnce; ++h) {
 #pragma unroll
-                        for (int k = 0; k < kPer; ++k) put(e + k, __uint_as_float(v[(q * kPer + k) / 16][(q * kPer + k) % 16]));
-                        if (k0 + c0 + q * kPer < a.d.inputs) *reinterpret_cast<uint4 *>(dw + c0 + q * kPer) = *reinterpret_cast<const uint4 *>(e);
+                        for (int q = 0; q < 4; ++q) {
+                            alignas(16) P e[kPer];
+#pragma unroll
+                            for (int k = 0; k < kPer; ++k) {
+                                const int col = h * kAtOnce + q * kPer + k;
+                                put(e + k, __uint_as_float(v[col / 16][col % 16]));
+                            }
+                            *reinterpret_cast<uint4 *>(turns + lane * kTurnPitch + q * 16) = *reinterpret_cast<const uint4 *>(e);
+                        }
+                        __syncwarp();
+                        const int col = h * kAtOnce + (lane & 3) * kPer;
+                        uint4 piece[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) piece[k] = *reinterpret_cast<const uint4 *>(turns + (k * 8 + (lane >> 2)) * kTurnPitch + (lane & 3) * 16);
+                        __syncwarp();
+                        const int below = k0 + c0 + col < a.d.inputs ? rows - (lane >> 2) : 0;
+                        P *to = corner + (lane >> 2) * pitch + col;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (k * 8 < below) *reinterpret_cast<uint4 *>(to + k * 8 * pitch) = piece[k];
                     }
                 } else {                                            // rows of any alignment: two outputs' 16 sums in a store of the warp
-                    float *turn = reinterpret_cast<float *>(scale_ring + kCodeStages * kScaleBytes + quad * kTurnBytes);
-                    const int rows = (int)min((int64_t)32, a.d.outputs - (o - lane)), col = lane & 15;
+                    float *turn = reinterpret_cast<float *>(turns);
+                    const int col = lane & 15;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) turn[lane * 17 + k] = __uint_as_float(v[h][k]);
                         __syncwarp();
-                        const int64_t at = c0 + h * 16 + col;
-                        P *to = dw - (int64_t)lane * a.d.inputs + at;
-                        if (k0 + at < a.d.inputs)
-#pragma unroll 4
-                            for (int k = lane >> 4; k < rows; k += 2) put(to + (int64_t)k * a.d.inputs, turn[k * 17 + col]);
+                        const int at = h * 16 + col, below = k0 + c0 + at < a.d.inputs ? rows - (lane >> 4) : 0;
+                        P *to = corner + (lane >> 4) * pitch + at;
+#pragma unroll 1
+                        for (int k = 0; k < below; k += 8, to += 8 * pitch) {
+                            float f[4];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) f[u] = turn[(k + 2 * u + (lane >> 4)) * 17 + col];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                if (k + 2 * u < below) put(to + 2 * u * pitch, f[u]);
+                        }
                         __syncwarp();
                     }
                 }
