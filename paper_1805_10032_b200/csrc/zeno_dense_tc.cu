@@ -5,7 +5,7 @@
 // the tensor copies write.  Each block holds 128 of the outputs' rows of dY^T and 128 of the inputs of X, and the pair's instruction
 // (cta_group::2, M = 256, N = 256) reads both halves: a code is turned into bfloat16 once for 256 outputs.  code * scale is
 // exact in bfloat16, products of bfloat16 are exact, and the sums stay binary32 in TMEM.
-// 8 x 2048 tokens, 4096 x 4096: 480 us alone (1,145 TFLOP/s, 70 % of cuBLAS's burst rate), 515 with the bias; without the conversion's arithmetic 15 %
+// 8 x 2048 tokens, 4096 x 4096: 462 us alone (1,190 TFLOP/s, 73 % of cuBLAS's burst rate), 499 with the bias; without the conversion's arithmetic 15 %
 // less, without its stores too 24 % less.
 //   warp 0: copies of the codes;  warp 3: of their scales;  warp 2: of dY;  warp 1 of the pair's first block: the instructions;
 // binary32 dY is rewritten as three bfloat16 terms first, which hold it exactly; few tiles are cut along the tokens.
@@ -30,7 +30,7 @@ constexpr int kTurnPitch = 80, kTurnBytes = 32 * kTurnPitch;
 constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * (kCodeBytes + kScaleBytes) + 4 * kTurnBytes + 1024;
 // The warps that convert come in sets, which take the stages in turn: a stage is a chain of waits, loads, arithmetic, stores and an
 // arrival that one set alone would follow from end to end (8 x 2048 tokens, 4096 x 4096, with
-// the bias: one set of eight warps 691 us, two of four 589, four of two 562 (536 by now); four of four 515).
+// the bias: one set of eight warps 691 us, two of four 589, four of two 562 (536 by now); four of four 515, before the sums left by pieces).
 constexpr int kConvWarps = 16, kSets = 4, kSetWarps = kConvWarps / kSets, kEpiWarps = 4;
 constexpr int kThreads = 32 * (4 + kConvWarps + kEpiWarps);
 constexpr int kTmemCols = 512;                // two sets of 256 sums
