@@ -372,9 +372,10 @@ __global__ void __launch_bounds__(TPR *ROWS, TPR *ROWS <= 256 ? 2 : 1) norm_colu
             } else {
                 pairs(reinterpret_cast<const uint4 *>(ring_x)[slot(stage, v)], h[v], T());
             }
+            // Where nothing was copied, the entry is the mean: (0 - mean) rstd of finite numbers may be beyond binary32, and its product with 0 a NaN.
             if (!on || !mine[v])
 #pragma unroll
-                for (int k = 0; k < H; ++k) d[k] = h[v][k] = both(0.f);         // nothing was copied for this row
+                for (int k = 0; k < H; ++k) d[k] = both(0.f), h[v][k] = both(mean);
 #pragma unroll
             for (int k = 0; k < H; ++k) {
                 h[v][k] = mul2(add2(h[v][k], both(-mean)), both(rstd));
