@@ -4,7 +4,7 @@
 // the token as the contraction index and the output or input index contiguous ("MN-major"), in the 128-byte swizzled layout that
 // the tensor copies write.  Each block holds 128 of the outputs' rows of dY^T and 128 of the inputs of X, and the pair's instruction
 // (cta_group::2, M = 256, N = 256) reads both halves: a code is turned into bfloat16 once for 256 outputs.  code * scale is
-// exact in bfloat16, products of bfloat16 are exact, and the sums stay binary32 in TMEM.
+// exact in bfloat16, products of bfloat16 are exact, and the sums are binary32 in TMEM, for long ones stretch by stretch.
 // 8 x 2048 tokens, 4096 x 4096: 462 us alone (1,190 TFLOP/s, 73 % of cuBLAS's burst rate), 499 with the bias; without the conversion's arithmetic 15 %
 // less, without its stores too 24 % less.
 //   warp 0: copies of the codes;  warp 3: of their scales;  warp 2: of dY;  warp 1 of the pair's first block: the instructions;
@@ -38,13 +38,36 @@ constexpr int kKernelId = 5;
 
 __device__ int g_status;                      // raised by a block whose bounded wait gave up, cleared by who reads it
 
+// The tensor core adds with truncation towards zero, which takes about 1.4e-8 of a sum with every 16 tokens: of 2,048 tokens' all positive products
+// 1.8e-6, of 32,768 6.7e-5, and 1.2e-4 in three terms.  So no set of sums in TMEM takes more than a stretch of stages; between two stretches of a tile
+// the warps that write it keep its sums in binary32 in the workspace (L2), where they are added to nearest: 6.7e-7 for any number of tokens (the plain
+// product in binary32: 0.6 to 8e-7).  2 x 8192 tokens, 4096 x 4096, bfloat16 into binary32: 572 us, 482 in one stretch; 8 x 2048 in
+// three terms 1,582 and 1,478; stretches of 2,048 tokens are off by 1.8e-6.  A result in bfloat16, which is rounded by 2^-9 anyway, takes stretches of
+// 4,096 tokens (4e-6).  Of dY's terms the smaller ones come first: what they lose is 2^-8 of that and less, so that their stretches are 64 times as long.
+constexpr int kDrain = 16, kDrainBf16 = 64, kDrainSmall = 64;
+struct Stretches {
+    int first, last, small_end, early, late;          // stages; where the smaller terms end; stretches in those alone, and others
+    __host__ __device__ Stretches(int kb0, int kb1, int small, int drain) : first(kb0), last(kb1) {
+        small_end = small < kb0 ? kb0 : small < kb1 ? small : kb1;
+        early = (small_end - kb0) / (kDrainSmall * drain);
+        late = (kb1 - small_end + drain - 1) / drain;
+        if (late == 0 && first + early * kDrainSmall * drain < kb1) late = 1;
+    }
+    __host__ __device__ int count() const { return early + late; }
+    __host__ __device__ int at(int part, int drain) const {
+        return part <= early ? first + part * kDrainSmall * drain : small_end + (int)((int64_t)(last - small_end) * (part - early) / late);
+    }
+};
+
 struct DenseTcArgs {
     DenseGradArgs d;
     int out_tiles, in_tiles, shared_dy, shared_codes;
     int terms;                  // bfloat16 terms of dY, planes of the tensor map's third dimension: summed like further tokens
     int nkb;                    // stages of one term
     int splits;                 // parts that the sum over tokens is cut into
+    int drain;                  // stages of a stretch
     float *part;                // [split][group][output][input] (splits > 1)
+    float *kept;                // [block][64 times 4 columns][128 outputs] x 4: a block's sums between two stretches of a tile
     int64_t items;
     int vector_stores;
     int followed;               // another kernel of the same call comes after this one
@@ -109,7 +132,8 @@ __device__ __forceinline__ void sixteen_values(uint4 codes, float scale, uint4 (
     out[1] = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
-template <typename P>
+// LONG: some sums take more than one stretch.
+template <typename P, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes,
                                                                DenseTcArgs a) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -208,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
 #pragma unroll 1
                         for (int h = 0; h < 2; ++h)
                             tma_load_3d(smem_u32(a_ring + s * kABytes + h * kSubBytes), &map_dy, ot * kPairTile + rank * kHalf + h * 64, token0,
-                                        a.shared_dy ? 0 : group * a.terms + term, afull(s));
+                                        a.shared_dy ? 0 : group * a.terms + a.terms - 1 - term, afull(s));
                     }
                 }
                 __syncwarp();
@@ -254,33 +278,35 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         // descriptor: sums binary32, operands bfloat16, both MN-major
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(kPairTile >> 3) << 17) | ((uint32_t)(kPairTile >> 4) << 24);
         int s = 0;
-        uint32_t ph = 0;
+        uint32_t ph = 0, drain = 0;                                  // stretches so far
         bool ok = rank == 0;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li) {
-            const int set = li & 1;
-            ok = __all_sync(0xffffffffu, mbar_wait(dempty(set), ((uint32_t)(li >> 1) & 1) ^ 1, abortp));
-            if (!ok) break;
-            tc_fence_after();
-            for (int kb = kb0; kb < kb1; ++kb) {
-                ok = mbar_wait(bready(s), ph, abortp) && mbar_wait(afull(s), ph, abortp);
-                ok = __all_sync(0xffffffffu, ok);
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li)
+            for (int part = 0, parts = LONG ? Stretches(kb0, kb1, (a.terms - 1) * a.nkb, a.drain).count() : 1; ok && part < parts; ++part, ++drain) {
+                const Stretches stretches(kb0, kb1, (a.terms - 1) * a.nkb, a.drain);
+                const int set = (int)(drain & 1), from = LONG ? stretches.at(part, a.drain) : kb0, to = LONG ? stretches.at(part + 1, a.drain) : kb1;
+                ok = __all_sync(0xffffffffu, mbar_wait(dempty(set), ((drain >> 1) & 1) ^ 1, abortp));
                 if (!ok) break;
                 tc_fence_after();
-                if (elect_one()) {
-                    const uint32_t ab = smem_u32(a_ring + s * kABytes), bb = smem_u32(b_ring + s * kBBytes);
+                for (int kb = from; kb < to; ++kb) {
+                    ok = mbar_wait(bready(s), ph, abortp) && mbar_wait(afull(s), ph, abortp);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t ab = smem_u32(a_ring + s * kABytes), bb = smem_u32(b_ring + s * kBBytes);
 #pragma unroll
-                    for (int k = 0; k < kTokens / 16; ++k)        // 16 tokens: two groups of eight rows
-                        pair_mma(tmem + set * 256, mn_desc(ab + k * 2048), mn_desc(bb + k * 2048), idesc, (uint32_t)((kb - kb0) | k));
-                    pair_commit(abempty(s));
-                    if (kb + 1 == kb1) pair_commit(dfull(set));
-                }
-                __syncwarp();
-                if (++s == kStages) {
-                    s = 0;
-                    ph ^= 1;
+                        for (int k = 0; k < kTokens / 16; ++k)        // 16 tokens: two groups of eight rows
+                            pair_mma(tmem + set * 256, mn_desc(ab + k * 2048), mn_desc(bb + k * 2048), idesc, (uint32_t)((kb - from) | k));
+                        pair_commit(abempty(s));
+                        if (kb + 1 == to) pair_commit(dfull(set));
+                    }
+                    __syncwarp();
+                    if (++s == kStages) {
+                        s = 0;
+                        ph ^= 1;
+                    }
                 }
             }
-        }
     } else if (warp >= 4 && warp < 4 + kConvWarps) {
         // ------------------------------------------------------------------ codes to bfloat16
         // Eight lanes take a pair of rows (even and odd token), four of the eight 16-code groups of each, the other four in the other half
@@ -335,83 +361,118 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         // ------------------------------------------------------------------ finished tiles to dW
         const int quad = warp & 3;                                 // TMEM lanes this warp may access
         const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[2 * kCodeStages + 3 * kStages + 2], 0);
-        for (int li = 0; __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li) {
-            const int set = li & 1;
-            if (!__all_sync(0xffffffffu, mbar_wait(dfull(set), (uint32_t)(li >> 1) & 1, abortp))) break;
-            tc_fence_after();
-            const int64_t o = (int64_t)ot * kPairTile + rank * kHalf + quad * 32 + lane, k0 = (int64_t)it * kPairTile;
-            P *dw = a.splits > 1 ? reinterpret_cast<P *>(a.part) + (((int64_t)split * a.d.m + group) * a.d.outputs + o) * a.d.inputs + k0
-                                 : static_cast<P *>(a.d.dw) + group * a.d.ldw + o * a.d.inputs + k0;
-            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + set * 256;
-#pragma unroll 1
-            for (int c0 = 0; c0 < kPairTile; c0 += 32) {
-                uint32_t v[2][16];
-                __syncwarp();
-                tc_ld16(from + c0, v[0]);
-                tc_ld16(from + c0 + 16, v[1]);
-                tc_wait_ld();
-                if (c0 + 32 == kPairTile) {                         // the sums are in registers: the set may be overwritten
-                    tc_fence_before();
+        uint32_t drain = 0;
+        for (int li = 0; __all_sync(0xffffffffu, get_item(li) && !*abortp); ++li)      // a wait that gave up has raised the flag
+            for (int part = 0, parts = LONG ? Stretches(kb0, kb1, (a.terms - 1) * a.nkb, a.drain).count() : 1; part < parts; ++part, ++drain) {
+                const int set = (int)(drain & 1);
+                if (!__all_sync(0xffffffffu, mbar_wait(dfull(set), (drain >> 1) & 1, abortp))) break;
+                tc_fence_after();
+                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + set * 256;
+                // the sums of 32 columns; behind the last of them the set may be overwritten
+                auto take = [&](int c0, uint32_t (&v)[2][16]) {
                     __syncwarp();
-                    if (lane == 0) {
-                        if (rank == 0) mbar_arrive(dempty(set));
-                        else mbar_arrive_cluster(remote_dempty + set * 8);
-                    }
-                }
-                uint8_t *turns = scale_ring + kCodeStages * kScaleBytes + quad * kTurnBytes;
-                const int rows = (int)min((int64_t)32, a.d.outputs - (o - lane));
-                const int pitch = (int)a.d.inputs;
-                P *corner = dw - lane * pitch + c0;
-                if (a.vector_stores) {
-                    constexpr int kPer = 16 / sizeof(P), kAtOnce = 4 * kPer;
-#pragma unroll
-                    for (int h = 0; h < 32 / kAtOnce; ++h) {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            alignas(16) P e[kPer];
-#pragma unroll
-                            for (int k = 0; k < kPer; ++k) {
-                                const int col = h * kAtOnce + q * kPer + k;
-                                put(e + k, __uint_as_float(v[col / 16][col % 16]));
-                            }
-                            *reinterpret_cast<uint4 *>(turns + lane * kTurnPitch + q * 16) = *reinterpret_cast<const uint4 *>(e);
+                    tc_ld16(from + c0, v[0]);
+                    tc_ld16(from + c0 + 16, v[1]);
+                    tc_wait_ld();
+                    if (c0 + 32 == kPairTile) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (rank == 0) mbar_arrive(dempty(set));
+                            else mbar_arrive_cluster(remote_dempty + set * 8);
                         }
-                        __syncwarp();
-                        const int col = h * kAtOnce + (lane & 3) * kPer;
-                        uint4 piece[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) piece[k] = *reinterpret_cast<const uint4 *>(turns + (k * 8 + (lane >> 2)) * kTurnPitch + (lane & 3) * 16);
-                        __syncwarp();
-                        const int below = k0 + c0 + col < a.d.inputs ? rows - (lane >> 2) : 0;
-                        P *to = corner + (lane >> 2) * pitch + col;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (k * 8 < below) *reinterpret_cast<uint4 *>(to + k * 8 * pitch) = piece[k];
                     }
-                } else {                                            // rows of any alignment: two outputs' 16 sums in a store of the warp
-                    float *turn = reinterpret_cast<float *>(turns);
-                    const int col = lane & 15;
+                };
+                // what was kept of the tile's earlier stretches is added; a thread meets none but its own
+                auto kept = [&](int c0) { return reinterpret_cast<float4 *>(a.kept) + ((blockIdx.x * kPairTile + c0) / 4 * kHalf + quad * 32 + lane); };
+                auto add_kept = [&](int c0, uint32_t (&v)[2][16]) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) turn[lane * 17 + k] = __uint_as_float(v[h][k]);
-                        __syncwarp();
-                        const int at = h * 16 + col, below = k0 + c0 + at < a.d.inputs ? rows - (lane >> 4) : 0;
-                        P *to = corner + (lane >> 4) * pitch + at;
+                    for (int k = 0; k < 8; ++k) {
+                        const float4 f = __ldcg(kept(c0) + k * kHalf);
+                        uint32_t *u = v[k / 4] + k % 4 * 4;
+                        u[0] = __float_as_uint(__uint_as_float(u[0]) + f.x);
+                        u[1] = __float_as_uint(__uint_as_float(u[1]) + f.y);
+                        u[2] = __float_as_uint(__uint_as_float(u[2]) + f.z);
+                        u[3] = __float_as_uint(__uint_as_float(u[3]) + f.w);
+                    }
+                };
+                if (LONG && part + 1 < parts) {
 #pragma unroll 1
-                        for (int k = 0; k < below; k += 8, to += 8 * pitch) {
-                            float f[4];
+                    for (int c0 = 0; c0 < kPairTile; c0 += 32) {
+                        uint32_t v[2][16];
+                        take(c0, v);
+                        if (part > 0) add_kept(c0, v);
 #pragma unroll
-                            for (int u = 0; u < 4; ++u) f[u] = turn[(k + 2 * u + (lane >> 4)) * 17 + col];
-#pragma unroll
-                            for (int u = 0; u < 4; ++u)
-                                if (k + 2 * u < below) put(to + 2 * u * pitch, f[u]);
+                        for (int k = 0; k < 8; ++k) {
+                            const uint32_t *u = v[k / 4] + k % 4 * 4;
+                            __stcg(kept(c0) + k * kHalf, make_float4(__uint_as_float(u[0]), __uint_as_float(u[1]), __uint_as_float(u[2]), __uint_as_float(u[3])));
                         }
-                        __syncwarp();
+                    }
+                    continue;
+                }
+                const int64_t o = (int64_t)ot * kPairTile + rank * kHalf + quad * 32 + lane, k0 = (int64_t)it * kPairTile;
+                P *dw = a.splits > 1 ? reinterpret_cast<P *>(a.part) + (((int64_t)split * a.d.m + group) * a.d.outputs + o) * a.d.inputs + k0
+                                     : static_cast<P *>(a.d.dw) + group * a.d.ldw + o * a.d.inputs + k0;
+#pragma unroll 1
+                for (int c0 = 0; c0 < kPairTile; c0 += 32) {
+                    uint32_t v[2][16];
+                    take(c0, v);
+                    if constexpr (LONG)
+                        if (part > 0) add_kept(c0, v);
+                    uint8_t *turns = scale_ring + kCodeStages * kScaleBytes + quad * kTurnBytes;
+                    const int rows = (int)min((int64_t)32, a.d.outputs - (o - lane));
+                    const int pitch = (int)a.d.inputs;
+                    P *corner = dw - lane * pitch + c0;
+                    if (a.vector_stores) {
+                        constexpr int kPer = 16 / sizeof(P), kAtOnce = 4 * kPer;
+#pragma unroll
+                        for (int h = 0; h < 32 / kAtOnce; ++h) {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                alignas(16) P e[kPer];
+#pragma unroll
+                                for (int k = 0; k < kPer; ++k) {
+                                    const int col = h * kAtOnce + q * kPer + k;
+                                    put(e + k, __uint_as_float(v[col / 16][col % 16]));
+                                }
+                                *reinterpret_cast<uint4 *>(turns + lane * kTurnPitch + q * 16) = *reinterpret_cast<const uint4 *>(e);
+                            }
+                            __syncwarp();
+                            const int col = h * kAtOnce + (lane & 3) * kPer;
+                            uint4 piece[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) piece[k] = *reinterpret_cast<const uint4 *>(turns + (k * 8 + (lane >> 2)) * kTurnPitch + (lane & 3) * 16);
+                            __syncwarp();
+                            const int below = k0 + c0 + col < a.d.inputs ? rows - (lane >> 2) : 0;
+                            P *to = corner + (lane >> 2) * pitch + col;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (k * 8 < below) *reinterpret_cast<uint4 *>(to + k * 8 * pitch) = piece[k];
+                        }
+                    } else {                                            // rows of any alignment: two outputs' 16 sums in a store of the warp
+                        float *turn = reinterpret_cast<float *>(turns);
+                        const int col = lane & 15;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) turn[lane * 17 + k] = __uint_as_float(v[h][k]);
+                            __syncwarp();
+                            const int at = h * 16 + col, below = k0 + c0 + at < a.d.inputs ? rows - (lane >> 4) : 0;
+                            P *to = corner + (lane >> 4) * pitch + at;
+#pragma unroll 1
+                            for (int k = 0; k < below; k += 8, to += 8 * pitch) {
+                                float f[4];
+#pragma unroll
+                                for (int u = 0; u < 4; ++u) f[u] = turn[(k + 2 * u + (lane >> 4)) * 17 + col];
+#pragma unroll
+                                for (int u = 0; u < 4; ++u)
+                                    if (k + 2 * u < below) put(to + 2 * u * pitch, f[u]);
+                            }
+                            __syncwarp();
+                        }
                     }
                 }
             }
-        }
     }
 
     // ---------------------------------------------------------------------- teardown
@@ -526,12 +587,21 @@ bool mappable(const Rows &v, int elem, int m, int64_t n, int64_t cols) {
 // What a call does: the terms that dY is rewritten in (0: it is read as it lies), the parts of the sum, and where they lie in the workspace.
 struct Plan {
     int terms, splits, out_tiles, in_tiles;
-    int64_t pitch, part_at, bytes;
+    int64_t pitch, part_at, kept_at, bytes;
 };
 
 // Parts: with fewer tiles than half the pairs of SMs, as many as the pairs take, each of eight stages and more.  The count of SMs is this
 // design's, so that the workspace's size needs no device.
 constexpr int kPairs = 74;
+
+// Whether any part takes more than one stretch.
+bool long_sums(const Plan &p, const DenseGradArgs &a, int drain) {
+    const int terms = p.terms > 1 ? p.terms : 1, nkb = (int)((a.n + kTokens - 1) / kTokens);
+    const int64_t all = (int64_t)terms * nkb;
+    for (int s = 0; s < p.splits; ++s)
+        if (Stretches((int)(all * s / p.splits), (int)(all * (s + 1) / p.splits), (terms - 1) * nkb, drain).count() > 1) return true;
+    return false;
+}
 
 bool plan_dense_tc(int type, const DenseGradArgs &a, Plan *p) {
     if (a.n < 1 || a.n >= (int64_t)1 << 28 || !mappable(a.codes, 1, a.m, a.n, a.inputs)) return false;
@@ -545,7 +615,8 @@ bool plan_dense_tc(int type, const DenseGradArgs &a, Plan *p) {
     p->splits = splits < 1 ? 1 : (int)splits;
     const int64_t terms_bytes = (int64_t)a.m * p->terms * a.n * p->pitch * 2;
     p->part_at = (terms_bytes + 255) / 256 * 256;
-    p->bytes = p->part_at + (p->splits > 1 ? (int64_t)p->splits * a.m * a.outputs * a.inputs * 4 : 0);
+    p->kept_at = p->part_at + ((p->splits > 1 ? (int64_t)p->splits * a.m * a.outputs * a.inputs * 4 : 0) + 255) / 256 * 256;
+    p->bytes = p->kept_at + (long_sums(*p, a, kDrain) ? (int64_t)2 * kPairs * kHalf * kPairTile * 4 : 0);
     return true;
 }
 
@@ -592,7 +663,9 @@ cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &d, cu
     a.terms = p.terms > 1 ? p.terms : 1;
     a.nkb = (int)((d.n + kTokens - 1) / kTokens);
     a.splits = p.splits;
+    a.drain = param_type == ZENO_BF16 ? kDrainBf16 : kDrain;
     a.part = reinterpret_cast<float *>(ws + p.part_at);
+    a.kept = reinterpret_cast<float *>(ws + p.kept_at);
     a.items = (int64_t)d.m * a.out_tiles * a.in_tiles * a.splits;
     const bool bf16 = param_type == ZENO_BF16 && p.splits == 1;
     const size_t elem = bf16 ? 2 : 4;
@@ -600,15 +673,18 @@ cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &d, cu
                       (p.splits > 1 || (reinterpret_cast<uintptr_t>(d.dw) % 16 == 0 && (d.m <= 1 || d.ldw * elem % 16 == 0)));
     a.followed = p.splits > 1 || d.db;
     a.spin_limit = spin_limit;
-    auto *kernel = bf16 ? dense_tc_kernel<__nv_bfloat16> : dense_tc_kernel<float>;
-    static PerDeviceOnce attr_set[2];
-    if (attr_set[bf16].need(device)) {
+    const bool in_stretches = long_sums(p, d, a.drain);
+    auto *kernel = bf16 ? (in_stretches ? dense_tc_kernel<__nv_bfloat16, true> : dense_tc_kernel<__nv_bfloat16, false>)
+                        : (in_stretches ? dense_tc_kernel<float, true> : dense_tc_kernel<float, false>);
+    static PerDeviceOnce attr_set[4];
+    PerDeviceOnce &once = attr_set[2 * bf16 + in_stretches];
+    if (once.need(device)) {
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return e;
-        attr_set[bf16].mark(device);
+        once.mark(device);
     }
     // equal shares: the fewest pairs that make as many rounds as all would
-    const int64_t most = sms / 2, rounds = (a.items + most - 1) / most, pairs = (a.items + rounds - 1) / rounds;
+    const int64_t most = sms / 2 < kPairs ? sms / 2 : kPairs, rounds = (a.items + most - 1) / most, pairs = (a.items + rounds - 1) / rounds;
     e = launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), kSmem, s, p.terms > 0, map_dy, map_codes, a);
     if (e != cudaSuccess || p.splits == 1) return e;
     const int64_t per_group = d.outputs * d.inputs, total = per_group * d.m;

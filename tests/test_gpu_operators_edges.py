@@ -49,3 +49,39 @@ def test_layer_norm_gradient_of_large_constant_rows(cols, act, saved):
     R.assert_near(dx, want[0], (cols / 32 + 40) * R.U * size, "dx")
     assert torch.equal(dw, torch.zeros_like(dw))
     R.assert_near(db, want[2], want[5], "db")
+
+
+# 40 tiles and more, so that a tile's sum over the tokens is not cut into parts; binary32 dy in three terms, up to where the small ones fill stretches
+@pytest.mark.parametrize("n,act,par", [(2048, F32, F32), (8192, BF16, F32), (8192, F32, F32), (32768, BF16, F32), (70000, F32, F32), (8200, BF16, BF16),
+                                       (140000, F32, BF16)])
+def test_dense_gradient_of_many_tokens_is_summed_in_binary32(n, act, par):
+    """All products positive.  The tensor core adds 16 tokens at a time and truncates: off by less than a step of binary32, 2^-23 of the sum.  Its
+    sums go on after at most 1,024 tokens (64 additions; 4,096 and 256 into bfloat16, with up to 65,536 and 262,144 of the two small terms before, 2^-8
+    of the sum together: 2 * 16,384 * 2^-23 * 2^-8 at most), in n / 1,024 additions to nearest, of half a step each."""
+    g = _gen(n)
+    inputs, outputs = 2560, 1024
+    saved = zeno.pack_activations(torch.rand(1, n, inputs, generator=g, device="cuda").to(BF16))
+    dy = torch.rand(1, n, outputs, generator=g, device="cuda").to(act)
+    dw, db = torch.full((1, outputs, inputs), NAN, device="cuda", dtype=par), torch.full((1, outputs), NAN, device="cuda", dtype=par)
+    zeno.dense_gradient(dy, saved, dw, db)
+    zeno.check_operator_status()
+    want = torch.zeros(outputs, inputs, device="cuda", dtype=torch.float64)
+    for at in range(0, n, 8192):
+        want += dy[0, at:at + 8192].double().T @ R.unpack(saved.codes[0, at:at + 8192], saved.scales[0, at:at + 8192])
+    additions = 64 if par == F32 else 256
+    small = 0 if act == BF16 else min(2 * n / 16, 64 * additions) * 2.0 ** -31
+    R.assert_near(dw[0], want, want * (additions * 2.0 ** -23 + small + (n / 1024 + 1) * R.U), "dw")
+    R.assert_near(db, dy.double().sum(1), (n + 32) * R.U * dy.double().sum(1), "db")
+
+
+def test_dense_gradient_keeps_the_small_terms_of_few_tokens():
+    """Three terms of 160 tokens in one stretch: 10 truncating additions of the largest term, 2^-23 each, on what the small ones left (2^-8, and 20 more of
+    those), and the half step that the result is rounded by."""
+    g = _gen(4)
+    saved = zeno.pack_activations(torch.rand(8, 160, 512, generator=g, device="cuda").to(BF16))
+    dy = 1 + torch.rand(8, 160, 512, generator=g, device="cuda")
+    dw = torch.full((8, 512, 512), NAN, device="cuda")
+    zeno.dense_gradient(dy, saved, dw)
+    zeno.check_operator_status()
+    want = dy.double().transpose(1, 2) @ R.unpack(saved.codes, saved.scales)
+    R.assert_near(dw, want, want * (10 + 30 / 256) * 2.0 ** -23, "dw")
