@@ -2,7 +2,7 @@
 //
 // Both directions are bound by the logits' bytes.  Forward: one pass with a running reference instead of the maximum, in
 // powers of two: with t_j = z_j log2 e - M, S = sum 2^t_j and E = sum 2^t_j t_j for any M near the largest z log2 e,
-//   lse = (M + log2 S) ln 2,   log p_j = (t_j - log2 S) ln 2,   entropy = (log2 S - E / S) ln 2;
+//   lse = (M + log2 S) ln 2 (formed from M ln 2, rounded, and the remainder),   log p_j = (t_j - log2 S) ln 2,   entropy = (log2 S - E / S) ln 2;
 // M moves by d: S' = 2^-d S, E' = 2^-d (E - d S).  No subtraction of nearly equal numbers besides those of the definition.
 #include "zeno_operators.h"
 
@@ -468,7 +468,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
         return lp > 0.f ? 0.f : lp;                       // a rounding above the definition's bound
     };
     if (threadIdx.x == 0) {
-        if (a.lse) a.lse[r] = plain ? m + log_s : (m + log_s) * kLn2;
+        if (a.lse) {
+            // M / log2 e as a logit: what its rounding is off by joins log2 S, and only the last addition rounds at the size of lse
+            const float at = m * kLn2;
+            a.lse[r] = plain ? m + log_s : at + (log_s - fmaf(at, kLog2e, -m)) * kLn2;
+        }
         if (a.entropy) {
             const float h = log_s == -INFINITY ? 0.f : (log_s - mean_t) * (plain ? 1.f : kLn2);
             a.entropy[r] = h < 0.f ? 0.f : h;             // a rounding under the definition's bound

@@ -85,3 +85,20 @@ def test_dense_gradient_keeps_the_small_terms_of_few_tokens():
     zeno.check_operator_status()
     want = dy.double().transpose(1, 2) @ R.unpack(saved.codes, saved.scales)
     R.assert_near(dw, want, want * (10 + 30 / 256) * 2.0 ** -23, "dw")
+
+
+@pytest.mark.parametrize("vocab,rows", [(64, 3000), (3001, 500), (40000, 600), (140000, 20)])
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_lse_is_rounded_once_at_its_own_size(vocab, rows, act):
+    """Rows of 1, 2 or 4 equal entries and nothing else: lse = v + log k.  Besides the half step of lse there is only what is rounded at the size of log2 S and
+    of the remainder (a step of v at most): an exponential and a logarithm, 2^-22 each, and four roundings of at most 3."""
+    g = _gen(vocab)
+    v = ((torch.rand(rows, generator=g, device="cuda") * 230 + 20) * torch.where(torch.rand(rows, generator=g, device="cuda") < 0.5, -1.0, 1.0)).to(act)
+    z = torch.full((rows, vocab), -INF, device="cuda", dtype=act)
+    k = 2 ** (torch.arange(rows, device="cuda") % 3)
+    for r in range(rows):
+        z[r, torch.randperm(vocab, generator=g, device="cuda")[: int(k[r])]] = v[r]
+    got = zeno.token_logprobs(z, torch.zeros(rows, device="cuda", dtype=torch.int32), top=1)
+    want = v.double() + torch.log(k.double())
+    R.assert_near(got.lse, want, 2.0 ** -21 + 12 * R.U, "lse")
+    R.assert_near(got.top_logprobs[:, 0], -torch.log(k.double()), 2.0 ** -21 + 12 * R.U, "log probability")
