@@ -403,9 +403,9 @@ zeno_status zeno_token_logprobs(int32_t device, int32_t type, const zeno_rows *l
  *   dz_j = g_logprob ([j = target] - p_j) - g_entropy p_j (log p_j + entropy),
  * from zeno_token_logprobs's lse and entropy.  (The mean loss of n tokens has g_logprob = -1 / n.)  lse, g_logprob: float[m][n];
  * g_entropy: float[m][n], or NULL for none, and entropy then too.  A row without a target has no first term, and if g_entropy
- * is NULL its gradient is zero whatever its logits; so is that of a row whose logits are all minus infinity.  p_j is as
- * exact as lse in binary32 makes it; where |lse| is 2^20 or more (masked throughout by large numbers) it is taken from the
- * logits again.
+ * is NULL its gradient is zero whatever its logits; so is that of a row whose logits are all minus infinity.  lse, rounded to
+ * binary32, would put all of a row's p_j off by half a step of lse: where |lse| is 2^8 or more (2^12 in bfloat16) the row is summed again beside
+ * it, by one block.  p_j is off by 2^-16 of it at most (in bfloat16 by 2^-12, before the gradient is rounded).
  * grad: in the type of the logits; it may be the logits themselves. */
 zeno_status zeno_token_gradient(int32_t device, int32_t type, const zeno_rows *logits, int32_t m, int64_t n, int64_t vocab,
                                 const int32_t *targets, const float *lse, const float *entropy, const float *g_logprob,

@@ -490,13 +490,40 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
 // Elements in a block of its kernel: two rounds of four vectors a thread, half of them in flight.
 constexpr int kGradThreads = 256, kGradBatch = 4;
 
-// From here on lse is rounded to sixteenths and worse (rows masked throughout by large numbers, above all): its row is summed again.
-constexpr float kFarLse = 1048576.f;
+// An lse in binary32 is off by half a step, and so relative to them are all of a row's probabilities.  From 2^8 on (binary32, 2^-17 below; 2^12 and
+// 2^-13 for a gradient in bfloat16, whose own half step is 2^-9) that is more than the rest of the arithmetic: the row is summed again, by the block
+// that then does all of it, since the gradient may lie over the logits (4096 x 65,536 binary32: 501 us, 322 near zero; 61 x 50,001: 27 and 12).
+template <typename T> constexpr float kFarLse = sizeof(T) == 4 ? 256.f : 4096.f;
 
-// One element: what the row's sums say and the upstream gradients ask for; the target's own term is added apart.
+// Sum of exp(z - lse) over a row, for a block: what a rounded lse leaves to be taken off every log probability.  Near 1 as far as lse is right.
+template <typename T>
+__device__ __noinline__ float sum_beside(const T *z, int64_t vocab, float lse, float *scratch) {
+    using V = Vec<T>;
+    const int64_t head = head_of(z, vocab), vecs = (vocab - head) / V::N, rest = vocab - vecs * V::N;
+    const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
+    float s = 0.f;
+    if (threadIdx.x < rest) s = exp2_fast((value_of(z + (threadIdx.x < head ? threadIdx.x : vecs * V::N + threadIdx.x)) - lse) * kLog2e);
+    for (int64_t base = threadIdx.x; base < vecs; base += kGradThreads * kGradBatch) {
+        uint4 raw[kGradBatch];
+#pragma unroll
+        for (int i = 0; i < kGradBatch; ++i) raw[i] = base + i * kGradThreads < vecs ? zv[base + i * kGradThreads] : make_uint4(V::kFill, V::kFill, V::kFill, V::kFill);
+        float part = 0.f;
+#pragma unroll
+        for (int i = 0; i < kGradBatch; ++i) {
+            T e[V::N];
+            *reinterpret_cast<uint4 *>(e) = raw[i];
+#pragma unroll
+            for (int k = 0; k < V::N; ++k) part += exp2_fast((value_of(e + k) - lse) * kLog2e);
+        }
+        s += part;
+    }
+    return block_sum<kGradThreads>(s, scratch);
+}
+
+// One element: what the row's sums say and the upstream gradients ask for; the target's own term is added apart.  `beside`: log of the above.
 template <bool ENTROPY>
-__device__ __forceinline__ float token_slope(float z, float lse, float g, float h, float entropy) {
-    const float lp = z - lse, p = exp2_fast(lp * kLog2e);
+__device__ __forceinline__ float token_slope(float z, float lse, float beside, float g, float h, float entropy) {
+    const float lp = (z - lse) - beside, p = exp2_fast(lp * kLog2e);
     return -p * (ENTROPY ? fmaf(h, fmaxf(lp, kLogOfNothing) + entropy, g) : g);
 }
 
@@ -513,22 +540,19 @@ __global__ void __launch_bounds__(kGradThreads) token_gradient_kernel(TokenGradA
     const bool given = t >= 0 && t < a.vocab;
     const float lse = a.lse[r], g = given ? a.g_logprob[r] : 0.f, h = ENTROPY ? a.g_entropy[r] : 0.f, entropy = ENTROPY ? a.entropy[r] : 0.f;
     const bool zero = (!given && !ENTROPY) || lse == -INFINITY;
-    auto one = [&](int64_t j) {
-        float v = 0.f;
-        if (!zero) v = token_slope<ENTROPY>(value_of(z + j), lse, g, h, entropy) + (j == t && given ? g : 0.f);
-        put(out + j, v);
-    };
-    if (!zero && fabsf(lse) >= kFarLse) {       // one block for the row, which it reads as a whole before it writes: the gradient may lie there
+    float beside = 0.f;
+    int64_t last = first + chunk;
+    if (!zero && fabsf(lse) >= kFarLse<T>) {       // one block for the row, which it reads as a whole before it writes: the gradient may lie there
         if (first != 0) return;
         __shared__ float scratch[kGradThreads / 32];
-        float m, s, unused;
-        sums_by_definition<T, kGradThreads>(z, a.vocab, scratch, m, s, unused);
-        __syncthreads();
-        const float log_s = logf(s);
-        for (int64_t j = threadIdx.x; j < a.vocab; j += kGradThreads)
-            put(out + j, token_slope<ENTROPY>(value_of(z + j) - m, log_s, g, h, entropy) + (j == t && given ? g : 0.f));
-        return;
+        beside = logf(sum_beside(z, a.vocab, lse, scratch));
+        last = a.vocab;
     }
+    auto one = [&](int64_t j) {
+        float v = 0.f;
+        if (!zero) v = token_slope<ENTROPY>(value_of(z + j), lse, beside, g, h, entropy) + (j == t && given ? g : 0.f);
+        put(out + j, v);
+    };
     // the vectors from v_first to v_end; what lies before and behind, at most 4 N entries, by single ones.  Of the first and last vector of a row whose
     // logits lie otherwise one half would come from outside of it.
     const int64_t head = head_of(out, a.vocab), vecs = (a.vocab - head) / V::N;
@@ -539,7 +563,7 @@ __global__ void __launch_bounds__(kGradThreads) token_gradient_kernel(TokenGradA
     const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(z + head) & 15);
     const uint4 *zv = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(z + head) - off);
     uint4 *ov = reinterpret_cast<uint4 *>(out + head);
-    const int64_t end = min((first + chunk) / V::N, v_end);
+    const int64_t end = min((last + V::N - 1) / V::N, v_end);
     for (int64_t base = max(first / V::N, v_first) + threadIdx.x; base < end; base += kGradThreads * kGradBatch) {
         uint4 raw[kGradBatch], more[VECTORS ? 1 : kGradBatch];
         if (!zero)
@@ -560,7 +584,7 @@ __global__ void __launch_bounds__(kGradThreads) token_gradient_kernel(TokenGradA
                 const int64_t at = (int64_t)t - (head + v * V::N);
 #pragma unroll
                 for (int k = 0; k < V::N; ++k) {
-                    float s = token_slope<ENTROPY>(value_of(e + k), lse, g, h, entropy);
+                    float s = token_slope<ENTROPY>(value_of(e + k), lse, beside, g, h, entropy);
                     if (at == k) s += g;                       // g is 0 without a target
                     put(o + k, s);
                 }

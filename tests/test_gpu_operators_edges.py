@@ -102,3 +102,56 @@ def test_lse_is_rounded_once_at_its_own_size(vocab, rows, act):
     want = v.double() + torch.log(k.double())
     R.assert_near(got.lse, want, 2.0 ** -21 + 12 * R.U, "lse")
     R.assert_near(got.top_logprobs[:, 0], -torch.log(k.double()), 2.0 ** -21 + 12 * R.U, "log probability")
+
+
+def _gradient_from_logits(z, t, g, gh):
+    """The gradient by its definition, in 64 bits, from the logits alone; p and what multiplies it."""
+    z = z.double()
+    p = torch.softmax(z, -1)
+    logp = torch.log_softmax(z, -1)
+    h = -torch.where(p > 0, p * logp, 0.0).sum(-1, keepdim=True)
+    given = (t >= 0).unsqueeze(-1)
+    hot = torch.zeros_like(z).scatter_(-1, t.long().clamp(min=0).unsqueeze(-1), 1.0) * given
+    g = g.double().unsqueeze(-1) * given
+    factor = g if gh is None else g + gh.double().unsqueeze(-1) * torch.where(p > 0, logp + h, 0.0)
+    return g * hot - p * factor, p, factor
+
+
+@pytest.mark.parametrize("vocab", [1, 9, 1000, 20011, 140001])
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("with_entropy", [False, True])
+def test_token_gradient_of_logits_far_from_zero(vocab, act, with_entropy):
+    """Whatever the size of the logits, p is off by 2^-16 of itself at most in binary32: half a step of an lse under 2^8 (2^-17) and an eighth of that each for the
+    errors of lse, of the exponential and of a row's sum.  In bfloat16 half a step of an lse under 2^12 (2^-13), 2^-12 in all, beside the result's own.  With the entropy
+    log p + H is off by as much, absolutely, and H by 2^-16 of 1 + H.  The rows' gradients of the log probability sum to zero."""
+    g = _gen(vocab)
+    far = [0.0, 100.0, -250.0, 300.0, 1e3, 5e3, -1e4, 65504.0, 3e5, -5e5, 1e6, 5e6, -3e8]
+    n = len(far) + 3
+    z = torch.randn(n, vocab, generator=g, device="cuda") * 2
+    for r, off in enumerate(far):
+        z[r] += off
+    z[-3] = -3e38                                                 # masked throughout by the type's lowest, or nearly
+    z[-2] -= 1e4
+    z[-2, vocab // 2:] = -INF
+    z[-1] += 4e4
+    z[-1, 1::2] = -3e38
+    z = z.to(act)
+    t = torch.randint(0, (vocab + 1) // 2, (n,), generator=g, device="cuda", dtype=torch.int32)
+    if vocab == 1:
+        z[-2] = -1e4
+    t[5] = -1
+    gl = torch.randn(n, generator=g, device="cuda")
+    gh = torch.randn(n, generator=g, device="cuda") if with_entropy else None
+    s = zeno.token_logprobs(z, t)
+    want, p, factor = _gradient_from_logits(z, t, gl, gh)
+    off = 2.0 ** -16 if act == F32 else 2.0 ** -12
+    h = gh.double().abs().unsqueeze(-1) if with_entropy else 0.0
+    slack = p * off * (factor.abs() + h * (2 + s.entropy.double().unsqueeze(-1))) + 4 * R.U * (p * factor).abs() + 2.0 ** -120
+    base = torch.full((n, vocab + 3), NAN, device="cuda", dtype=act)
+    for out in (None, base[:, 3:], z):                            # lying otherwise, too; last over the logits
+        got = zeno.token_gradient(z, t, s.lse, gl, s.entropy, gh, out=out)
+        R.assert_near(got, want, slack, "gradient")
+        if act == F32 and not with_entropy:
+            total = got.double().sum(-1).abs()
+            assert (total <= gl.double().abs() * (off + 2 * R.U) + vocab * 2.0 ** -120).all(), total
+    assert torch.isnan(base[:, :3]).all()
