@@ -13,6 +13,19 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Sum over a row's entries j of a block's thread
+template <typename F>
+__device__ __forceinline__ float sum_of_row(int64_t cols, F term) {
+    LongSum s;
+    for (int64_t j = threadIdx.x; j < cols;) {
+        const int64_t end = min(cols, j + kShortSum * kThreads);
+        float part = 0.f;
+        for (; j < end; j += kThreads) part += term(j);
+        s.add(part);
+    }
+    return s.sum;
+}
+
 // Rows of any length and alignment, a block each: the sum, then the centred squares, then the result, reading the row three
 // times (twice of it from L1 or L2).
 template <typename T, typename P>
@@ -23,14 +36,12 @@ __global__ void __launch_bounds__(kThreads) norm_any_kernel(NormArgs a) {
     T *y = static_cast<T *>(a.y.data) + a.y.at(r);
     const P *w = static_cast<const P *>(a.w) + r / a.n * a.ldw;
     const P *b = a.b ? static_cast<const P *>(a.b) + r / a.n * a.ldw : nullptr;
-    float s = 0.f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) s += value_of(x + j);
+    float s = sum_of_row(a.cols, [&](int64_t j) { return value_of(x + j); });
     const float mean = block_sum<kThreads>(s, scratch[0]) / (float)a.cols;
-    s = 0.f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
+    s = sum_of_row(a.cols, [&](int64_t j) {
         const float d = value_of(x + j) - mean;
-        s = fmaf(d, d, s);
-    }
+        return d * d;
+    });
     const float rstd = rsqrtf(block_sum<kThreads>(s, scratch[1]) / (float)a.cols + a.eps);
     for (int64_t j = threadIdx.x; j < a.cols; j += kThreads)
         put(y + j, fmaf((value_of(x + j) - mean) * rstd, value_of(w + j), b ? value_of(b + j) : 0.f));
@@ -64,13 +75,20 @@ __global__ void __launch_bounds__(kThreads) norm_dx_any_kernel(NormGradArgs a) {
     const P *w = static_cast<const P *>(a.w) + r / a.n * a.ldw;
     const InputRow<T> x(a, r);
     const float mean = a.mean[r], rstd = a.rstd[r];
-    float s1 = 0.f, s2 = 0.f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-        const float g = value_of(dy + j) * value_of(w + j);
-        s1 += g;
-        s2 = fmaf(g, (x(j) - mean) * rstd, s2);
+    LongSum s1, s2;
+    for (int64_t j = threadIdx.x; j < a.cols;) {
+        const int64_t end = min(a.cols, j + kShortSum * kThreads);
+        float p1 = 0.f, p2 = 0.f;
+#pragma unroll 4
+        for (; j < end; j += kThreads) {
+            const float g = value_of(dy + j) * value_of(w + j);
+            p1 += g;
+            p2 = fmaf(g, (x(j) - mean) * rstd, p2);
+        }
+        s1.add(p1);
+        s2.add(p2);
     }
-    const float c1 = block_sum<kThreads>(s1, scratch[0]) / (float)a.cols, c2 = block_sum<kThreads>(s2, scratch[1]) / (float)a.cols;
+    const float c1 = block_sum<kThreads>(s1.sum, scratch[0]) / (float)a.cols, c2 = block_sum<kThreads>(s2.sum, scratch[1]) / (float)a.cols;
     for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
         const float g = value_of(dy + j) * value_of(w + j), h = (x(j) - mean) * rstd;
         put(dx + j, rstd * (g - c1 - h * c2));
@@ -776,18 +794,24 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(const float *part, 
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.y;
     const int64_t at = ((int64_t)blockIdx.x * 32 + lane) * N, all = 2 * (int64_t)cols;
-    float s[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) s[k] = 0.f;
+    LongSum total[N];
     if (at < all)
-#pragma unroll 4
-        for (int c = warp; c < chunks; c += kWarps) {
-            const Pack<float, N> v = load_pack<float, N>(part + ((int64_t)i * chunks + c) * all + at);
+        for (int c = warp; c < chunks;) {
+            const int end = min(chunks, c + 2 * kShortSum * kWarps);          // one stretch for kNormBlocks of them
+            float s[N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) s[k] += v.v[k];
+            for (int k = 0; k < N; ++k) s[k] = 0.f;
+#pragma unroll 4
+            for (; c < end; c += kWarps) {
+                const Pack<float, N> v = load_pack<float, N>(part + ((int64_t)i * chunks + c) * all + at);
+#pragma unroll
+                for (int k = 0; k < N; ++k) s[k] += v.v[k];
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) total[k].add(s[k]);
         }
 #pragma unroll
-    for (int k = 0; k < N; ++k) sums[warp][k][lane] = s[k];
+    for (int k = 0; k < N; ++k) sums[warp][k][lane] = total[k].sum;
     __syncthreads();
     for (int c = threadIdx.x; c < 32 * N; c += kThreads) {
         float v = 0.f;
@@ -814,6 +838,13 @@ int norm_chunks(int m, int64_t n, int64_t cols) {
     int64_t c = m > 0 ? kNormBlocks / (m * by_columns) : 1;
     if (c > n / 8) c = n / 8;
     return c < 1 ? 1 : (int)c;
+}
+
+// The same for the backward pass, with no more than 4,096 rows to a block (as far as a grid's third dimension goes): their sums are chains of additions.
+constexpr int64_t kChainRows = 4096;
+int gradient_chunks(int m, int64_t n, int64_t cols) {
+    const int64_t c = min((n + kChainRows - 1) / kChainRows, (int64_t)65535);
+    return (int)max((int64_t)norm_chunks(m, n, cols), c);
 }
 
 // sets a kernel's dynamic shared memory on the current device, once
@@ -908,7 +939,7 @@ cudaError_t norm_columns(const NormGradArgs &a, cudaStream_t s) {
     static PerDeviceOnce attr_set;
     cudaError_t e = allow_shared(kernel, kSmem, attr_set);
     if (e != cudaSuccess) return e;
-    const int chunks = norm_chunks(a.m, a.n, a.cols);
+    const int chunks = gradient_chunks(a.m, a.n, a.cols);
     const bool join = (a.dw || a.db) && chunks > 1;
     const int64_t per_block = (int64_t)TPR * kNV * (16 / sizeof(T)), tiles = DX ? 1 : (a.cols + per_block - 1) / per_block;
     e = launch_chained(kernel, dim3(chunks, a.m, (unsigned)tiles), dim3(TPR * kRows), kSmem, s, false, a, join ? a.workspace : nullptr);
@@ -928,7 +959,7 @@ cudaError_t norm_columns_any(const NormGradArgs &a, cudaStream_t s) {
 template <typename T, typename P, int TPR, int NV, int R, bool DX>
 cudaError_t norm_entries(const NormGradArgs &a, cudaStream_t s) {
     const int64_t tiles = DX ? 1 : (a.cols + TPR * NV - 1) / (TPR * NV);
-    const int chunks = norm_chunks(a.m, a.n, a.cols);
+    const int chunks = gradient_chunks(a.m, a.n, a.cols);
     const bool join = (a.dw || a.db) && chunks > 1;
     auto *kernel = a.x.data || a.n == 0 ? norm_entries_kernel<T, P, TPR, NV, R, false, DX> : norm_entries_kernel<T, P, TPR, NV, R, true, DX>;
     const cudaError_t e = launch_chained(kernel, dim3((unsigned)tiles, a.m, chunks), dim3(TPR), 0, s, false, a, join ? a.workspace : nullptr);
@@ -984,7 +1015,7 @@ cudaError_t launch_layer_norm(int type, int param_type, const NormArgs &a, cudaS
 }
 
 int64_t norm_gradient_workspace(int m, int64_t n, int64_t cols) {
-    const int chunks = norm_chunks(m, n, cols);
+    const int chunks = gradient_chunks(m, n, cols);
     return chunks > 1 ? (int64_t)m * chunks * 2 * cols * (int64_t)sizeof(float) : 0;
 }
 

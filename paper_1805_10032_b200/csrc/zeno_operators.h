@@ -100,6 +100,7 @@ struct LogprobArgs {
     float *logprobs, *entropy, *lse;
     int32_t *top_idx;
     float *top_logprobs;
+    int long_sums;                      // by the definition, whose sums may have any number of terms; the launch sets it
 };
 cudaError_t launch_token_logprobs(int type, const LogprobArgs &a, cudaStream_t s);
 
@@ -131,6 +132,20 @@ __device__ __forceinline__ float block_sum(float v, float *scratch) {
     for (int i = 0; i < THREADS / 32; ++i) s += scratch[i];
     return s;
 }
+
+// A sum of sums, each of kShortSum terms or a few more, with what its additions lose given back to the next term (Kahan, Further remarks on reducing
+// truncation errors, 1965): however many there are, it is off by little more than they are.  By one chain of additions 2^18 equal terms come out wrong
+// by up to a hundredth.
+constexpr int kShortSum = 64;
+struct LongSum {
+    float sum = 0.f, lost = 0.f;
+    __device__ __forceinline__ void add(float v) {
+        const float y = __fsub_rn(v, lost), t = __fadd_rn(sum, y);
+        lost = __fsub_rn(__fsub_rn(t, sum), y);
+        if (!(fabsf(lost) < INFINITY)) lost = 0.f;          // the sum is not finite
+        sum = t;
+    }
+};
 
 // Two binary32 numbers that one instruction takes
 struct Two { float x, y; };

@@ -237,7 +237,9 @@ __global__ void __launch_bounds__(256) pack_kernel(PackArgs a, uint32_t strips_p
 // dW of a tile of 64 outputs by 64 inputs of one group in a block: ROWS rows at a time through shared memory, the next ones on their way into
 // registers, 4 x 4 sums a thread; db with the first tile of the inputs.  For what is over before the tensor cores' kernels have started, and for
 // codes that no tensor map can step through (12 groups of 37 rows, 301 x 131: 6 us beside the launch; it reaches about 27 TFLOP/s).
-template <typename T, typename P, int ROWS>
+// LONG: sums of more than kChain rows.
+constexpr int kChain = 1024;
+template <typename T, typename P, int ROWS, bool LONG>
 __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
     constexpr int kTile = 64, kEach = ROWS * kTile / 256, kApart = ROWS / kEach;
     __shared__ __align__(16) float sd[ROWS][kTile], sx[ROWS][kTile];
@@ -262,8 +264,20 @@ __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
             }
         }
     };
+    LongSum long_acc[LONG ? 4 : 1][LONG ? 4 : 1], long_bias;
     fetch(0);
     for (int64_t t0 = 0; t0 < a.n; t0 += ROWS) {
+        if (LONG && t0 % kChain == 0) {
+            long_bias.add(bias);
+            bias = 0.f;
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    long_acc[LONG ? p : 0][LONG ? q : 0].add(acc[p][q]);
+                    acc[p][q] = 0.f;
+                }
+        }
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const bool on = t0 + t + e * kApart < a.n;
@@ -285,6 +299,17 @@ __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
                 for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(df[p], xf[q], acc[p][q]);
         }
         __syncthreads();
+    }
+    if constexpr (LONG) {
+        long_bias.add(bias);
+        bias = long_bias.sum;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                long_acc[p][q].add(acc[p][q]);
+                acc[p][q] = long_acc[p][q].sum;
+            }
     }
     P *dw = static_cast<P *>(a.dw) + i * a.ldw;
     // through shared memory, ROWS outputs at a time, so that a warp writes a row's entries side by side
@@ -309,7 +334,7 @@ __global__ void __launch_bounds__(256) dense_any_kernel(DenseGradArgs a) {
 // db: a cluster takes 32 N outputs of a group, its blocks and their warps the rows in turn, a lane N neighbouring outputs; the warps' sums are
 // joined in shared memory, the blocks' through the cluster's.
 constexpr int kBiasWarps = 8;
-template <typename T, typename P, int N>
+template <typename T, typename P, int N, bool LONG>
 __global__ void __launch_bounds__(kBiasWarps * 32) dense_bias_kernel(DenseGradArgs a, int cluster) {
     __shared__ float sums[kBiasWarps][32 * N + 1];
     __shared__ float total[32 * N];
@@ -317,12 +342,23 @@ __global__ void __launch_bounds__(kBiasWarps * 32) dense_bias_kernel(DenseGradAr
     const int64_t o0 = (int64_t)blockIdx.y * 32 * N, o = o0 + lane * N;
     const T *dy = static_cast<const T *>(a.dy.data) + i * a.dy.group + o;
     float s[N];
+    LongSum long_s[LONG ? N : 1];
 #pragma unroll
     for (int k = 0; k < N; ++k) s[k] = 0.f;
     if (o < a.outputs) {
         constexpr int kAtOnce = 8;                               // rows' loads in flight
         const int64_t step = cluster * kBiasWarps;
+        int terms = 0;
         for (int64_t t = rank * kBiasWarps + warp; t < a.n; t += kAtOnce * step) {
+            if (LONG && terms == kChain) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    long_s[LONG ? k : 0].add(s[k]);
+                    s[k] = 0.f;
+                }
+                terms = 0;
+            }
+            terms += kAtOnce;
             alignas(16) T e[kAtOnce][N];
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u)
@@ -338,7 +374,10 @@ __global__ void __launch_bounds__(kBiasWarps * 32) dense_bias_kernel(DenseGradAr
         }
     }
 #pragma unroll
-    for (int k = 0; k < N; ++k) sums[warp][k * 32 + lane] = s[k];
+    for (int k = 0; k < N; ++k) {
+        if (LONG) long_s[LONG ? k : 0].add(s[k]);
+        sums[warp][k * 32 + lane] = LONG ? long_s[LONG ? k : 0].sum : s[k];
+    }
     __syncthreads();
     for (int c = threadIdx.x; c < 32 * N; c += kBiasWarps * 32) {
         float v = 0.f;
@@ -361,8 +400,9 @@ __global__ void __launch_bounds__(kBiasWarps * 32) dense_bias_kernel(DenseGradAr
 template <typename T, typename P, int N>
 cudaError_t dense_bias(const DenseGradArgs &a, int cluster, cudaStream_t s) {
     const dim3 grid(cluster, (unsigned)((a.outputs + 32 * N - 1) / (32 * N)), a.m);
-    if (cluster == 1) return launch_chained(dense_bias_kernel<T, P, N>, grid, dim3(kBiasWarps * 32), 0, s, true, a, cluster);
-    return launch_clustered(dense_bias_kernel<T, P, N>, cluster, grid, dim3(kBiasWarps * 32), 0, s, true, a, cluster);
+    auto *kernel = a.n > (int64_t)kChain * kBiasWarps * cluster ? dense_bias_kernel<T, P, N, true> : dense_bias_kernel<T, P, N, false>;
+    if (cluster == 1) return launch_chained(kernel, grid, dim3(kBiasWarps * 32), 0, s, true, a, cluster);
+    return launch_clustered(kernel, cluster, grid, dim3(kBiasWarps * 32), 0, s, true, a, cluster);
 }
 
 // 16 bytes of outputs a lane where that still gives every SM a block
@@ -388,7 +428,7 @@ template <typename T, typename P>
 cudaError_t dense_gradient(int type, int param_type, const DenseGradArgs &a, cudaStream_t s) {
     cudaError_t e = dense_on_tensor_cores(type, a) ? launch_dense_tc(type, param_type, a, s) : cudaErrorNotSupported;
     if (e == cudaErrorNotSupported)
-        return launch_chained(a.n <= 16 ? dense_any_kernel<T, P, 16> : dense_any_kernel<T, P, 32>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
+        return launch_chained(a.n <= 16 ? dense_any_kernel<T, P, 16, false> : a.n <= kChain ? dense_any_kernel<T, P, 32, false> : dense_any_kernel<T, P, 32, true>, dim3((unsigned)((a.inputs + 63) / 64), (unsigned)((a.outputs + 63) / 64), a.m), dim3(256), 0, s, false, a);
     return e == cudaSuccess && a.db ? dense_bias<T, P>(a, s) : e;
 }
 

@@ -17,6 +17,7 @@ constexpr float kLogOfNothing = -200.f;
 // no 2^t overflows.  Entries below -kFar (masks) are kept at that, where they add nothing to such a row.  Other rows (masked
 // throughout, or not finite) are summed by the definition.
 constexpr float kFar = 134217728.f;
+constexpr int kChain = 4096;       // terms of a sum that one chain of additions may have
 constexpr float kUnset = -kFar * kLog2e;      // the reference of nothing
 constexpr float kSlack = 4.f;      // how far (in logits) the reference may fall behind the largest logit before it moves
 constexpr int kMaxTop = ZENO_MAX_TOP;
@@ -142,16 +143,22 @@ __device__ __noinline__ void sums_by_definition(const T *z, int64_t vocab, float
     __syncthreads();
     for (int k = 0; k < THREADS / 32; ++k) m = fmaxf(m, scratch[k]);
     if (m == -INFINITY) m = 0.f;
-    s = e = 0.f;
-    for (int64_t j = threadIdx.x; j < vocab; j += THREADS) {
-        const float d = value_of(z + j) - m, p = exp2f(d * kLog2e);
-        s += p;
-        e = fmaf(p, fmaxf(d, kLogOfNothing), e);
+    LongSum all_s, all_e;
+    for (int64_t j = threadIdx.x; j < vocab;) {
+        const int64_t end = min(vocab, j + kShortSum * THREADS);
+        s = e = 0.f;
+        for (; j < end; j += THREADS) {
+            const float d = value_of(z + j) - m, p = exp2f(d * kLog2e);
+            s += p;
+            e = fmaf(p, fmaxf(d, kLogOfNothing), e);
+        }
+        all_s.add(s);
+        all_e.add(e);
     }
     __syncthreads();
-    s = block_sum<THREADS>(s, scratch);
+    s = block_sum<THREADS>(all_s.sum, scratch);
     __syncthreads();
-    e = block_sum<THREADS>(e, scratch);
+    e = block_sum<THREADS>(all_e.sum, scratch);
 }
 
 // Places the better of `count` keys, which differ but for zeros (none), in their order: a key's place is the number of better ones.
@@ -449,7 +456,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 6 : THREADS == 128 ?
     }
     q = {sums[0], sums[1], sums[2]};
 
-    const bool plain = !(fabsf(q.M) <= 0.99f * kFar * kLog2e);
+    const bool plain = a.long_sums || !(fabsf(q.M) <= 0.99f * kFar * kLog2e);
     float m, log_s, mean_t;
     if (plain) {
         float s, e;
@@ -501,8 +508,8 @@ __device__ __noinline__ float sum_beside(const T *z, int64_t vocab, float lse, f
     using V = Vec<T>;
     const int64_t head = head_of(z, vocab), vecs = (vocab - head) / V::N, rest = vocab - vecs * V::N;
     const uint4 *zv = reinterpret_cast<const uint4 *>(z + head);
-    float s = 0.f;
-    if (threadIdx.x < rest) s = exp2_fast((value_of(z + (threadIdx.x < head ? threadIdx.x : vecs * V::N + threadIdx.x)) - lse) * kLog2e);
+    LongSum s;
+    if (threadIdx.x < rest) s.sum = exp2_fast((value_of(z + (threadIdx.x < head ? threadIdx.x : vecs * V::N + threadIdx.x)) - lse) * kLog2e);
     for (int64_t base = threadIdx.x; base < vecs; base += kGradThreads * kGradBatch) {
         uint4 raw[kGradBatch];
 #pragma unroll
@@ -515,9 +522,9 @@ __device__ __noinline__ float sum_beside(const T *z, int64_t vocab, float lse, f
 #pragma unroll
             for (int k = 0; k < V::N; ++k) part += exp2_fast((value_of(e + k) - lse) * kLog2e);
         }
-        s += part;
+        s.add(part);
     }
-    return block_sum<kGradThreads>(s, scratch);
+    return block_sum<kGradThreads>(s.sum, scratch);
 }
 
 // One element: what the row's sums say and the upstream gradients ask for; the target's own term is added apart.  `beside`: log of the above.
@@ -596,7 +603,8 @@ __global__ void __launch_bounds__(kGradThreads) token_gradient_kernel(TokenGradA
 }
 
 template <typename T, int THREADS>
-cudaError_t launch_logprobs(const LogprobArgs &a, int parts, cudaStream_t s) {
+cudaError_t launch_logprobs(LogprobArgs a, int parts, cudaStream_t s) {
+    a.long_sums = a.vocab > (int64_t)kChain * THREADS * 2 * parts;       // more than kChain terms to each of a thread's sums
     auto *kernel = a.top ? logprobs_kernel<T, THREADS, true> : logprobs_kernel<T, THREADS, false>;
     const dim3 grid((unsigned)(a.m * a.n * parts));
     return parts > 1 ? launch_clustered(kernel, parts, grid, dim3(THREADS), 0, s, false, a, parts) : launch_chained(kernel, grid, dim3(THREADS), 0, s, false, a, parts);

@@ -155,3 +155,106 @@ def test_token_gradient_of_logits_far_from_zero(vocab, act, with_entropy):
             total = got.double().sum(-1).abs()
             assert (total <= gl.double().abs() * (off + 2 * R.U) + vocab * 2.0 ** -120).all(), total
     assert torch.isnan(base[:, :3]).all()
+
+
+# Long sums.  Chains of additions have at most 64 terms along a row (then sums of sums lose next to nothing), and 18 additions join a block's: k = 96.
+# A single chain over such a row adds equal terms with the same rounding each time.
+@pytest.mark.parametrize("cols", [(1 << 20) - 3, 1 << 20, (1 << 26) + 1])
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_layer_norm_of_very_long_rows(cols, act):
+    g = _gen(cols)
+    x = torch.rand(2, cols, generator=g, device="cuda").to(act)
+    x[0] = 0.1
+    w, b = torch.full((cols,), 1.25, device="cuda"), torch.full((cols,), 0.5, device="cuda")
+    y, mean, rstd = zeno.layer_norm(x, w, b, eps=1e-5)
+    k, eps = 96 * R.U, float(np.float32(1e-5))
+    for r in range(2):
+        v = x[r].double()
+        m = v.mean()
+        want = ((v - m).square().mean() + eps) ** -0.5
+        mean_off = k * v.abs().mean()
+        rstd_off = want * (k + (mean_off * want) ** 2 + 4 * R.U)
+        R.assert_near(mean[r], m, mean_off, "mean")
+        R.assert_near(rstd[r], want, rstd_off, "rstd")
+        y_off = 1.25 * ((mean_off + 2 * R.U) * want + 4 * (rstd_off + 4 * R.U * want)) + 4 * R.U * 4
+        R.assert_near(y[r], 1.25 * (v - m) * want + 0.5, y_off, "y")
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_layer_norm_gradient_of_very_long_rows(act):
+    """Constant rows have h = 0: dx = rstd (g - avg(g)), zero where dy is constant too."""
+    cols = (1 << 20) - 1
+    x = torch.full((2, cols), 0.25, device="cuda", dtype=act)
+    dy = torch.full((2, cols), 0.1, device="cuda", dtype=act)
+    dy[1] = torch.rand(cols, generator=_gen(1), device="cuda").to(act)
+    w = torch.ones(cols, device="cuda")
+    mean, rstd = torch.full((2,), 0.25, device="cuda"), torch.full((2,), 300.0, device="cuda")
+    dx = zeno.layer_norm_gradient(dy, x, w, mean, rstd)
+    d = dy.double()
+    R.assert_near(dx, 300 * (d - d.mean(-1, keepdim=True)), 300 * (96 + 8) * R.U * (d.abs() + d.mean(-1, keepdim=True)), "dx")
+
+
+@pytest.mark.parametrize("cols,rows_side_by_side", [(5, 1), (8, 8)])
+def test_layer_norm_weight_gradients_over_many_rows(cols, rows_side_by_side):
+    """600 groups leave a block to each; 4,096 rows at most make a chain."""
+    m, n = 600, 131072
+    x = torch.full((1, n, cols), 0.3, device="cuda").expand(m, n, cols)
+    dy = torch.full((1, n, cols), 0.1, device="cuda").expand(m, n, cols)
+    mean, rstd = torch.zeros(m, n, device="cuda"), torch.ones(m, n, device="cuda")
+    dw, db = torch.full((m, cols), NAN, device="cuda"), torch.full((m, cols), NAN, device="cuda")
+    zeno.layer_norm_gradient(dy, x, torch.ones(cols, device="cuda"), mean, rstd, dw, db, want_dx=False)
+    a, b = float(np.float32(0.1)), float(np.float32(0.3))
+    k = (4096 / rows_side_by_side + 64) * R.U
+    R.assert_near(dw, torch.full((m, cols), n * a * b), n * a * b * (k + 3 * R.U), "dw")
+    R.assert_near(db, torch.full((m, cols), n * a), n * a * k, "db")
+
+
+def test_token_logprobs_and_gradient_of_very_long_rows():
+    """One largest entry and 2^26 equal ones: S = 1 + (vocab - 1) e^-0.35.  Besides the sums an exponential, 2^-21, and the logarithm."""
+    vocab = (1 << 26) + 3
+    d = float(np.float32(-0.3125))
+    for off in (0.0, 1024.0):
+        z = torch.full((1, vocab), off + d, device="cuda")
+        z[0, 7] = off
+        t = torch.full((1,), 7, device="cuda", dtype=torch.int32)
+        s = zeno.token_logprobs(z, t, top=2)
+        S = 1 + (vocab - 1) * np.exp(d)
+        lse = off + np.log(S)
+        S_off = 96 * R.U + 2.0 ** -20
+        R.assert_near(s.lse, torch.tensor([lse]), S_off + 20 * R.U, "lse")
+        R.assert_near(s.logprobs, torch.tensor([-np.log(S)]), S_off + 40 * R.U, "log probability")
+        H = np.log(S) - (vocab - 1) * np.exp(d) * d / S
+        R.assert_near(s.entropy, torch.tensor([H]), 4 * S_off + 60 * R.U, "entropy")
+        assert s.top_idx.tolist() == [[7, 0]]
+        grad = zeno.token_gradient(z, t, s.lse, torch.ones(1, device="cuda"))
+        p = torch.full((1, vocab), np.exp(d) / S, device="cuda", dtype=torch.float64)
+        want = -p
+        want[0, 7] = 1 - 1 / S
+        R.assert_near(grad, want, p * 2.0 ** -16 + 4 * R.U * (want == want[0, 7]), "gradient")
+
+
+def test_dense_gradient_over_very_many_rows():
+    """One tile of 2^24 rows: on the tensor cores in 74 parts of 222 stretches (64 truncating additions), and the sums of dY in chains of 1,024."""
+    n, inputs, outputs = (1 << 24) + 5, 16, 8
+    saved = zeno.Saved(torch.full((n, inputs), 0x38, device="cuda", dtype=torch.uint8), torch.ones(n, 1, device="cuda"))     # ones
+    dy = torch.full((n, outputs), 0.1, device="cuda", dtype=BF16)
+    dw, db = torch.full((outputs, inputs), NAN, device="cuda"), torch.full((outputs,), NAN, device="cuda")
+    zeno.dense_gradient(dy, saved, dw, db)
+    zeno.check_operator_status()
+    want = n * float(dy[0, 0])
+    R.assert_near(dw, torch.full((outputs, inputs), want), want * (64 * 2.0 ** -23 + 320 * R.U), "dw")
+    R.assert_near(db, torch.full((outputs,), want), want * (1024 + 64) * R.U, "db")
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_dense_gradient_over_many_rows_of_codes_that_start_anywhere(act):
+    """On the CUDA cores: chains of 1,024 rows."""
+    n, inputs, outputs = (1 << 20) + 7, 19, 8
+    codes = torch.full((n, inputs + 2), 0x7f, device="cuda", dtype=torch.uint8)[:, 1:-1]
+    codes.fill_(0x38)
+    dy = torch.full((n, outputs), 0.1, device="cuda", dtype=act)
+    dw, db = torch.full((outputs, inputs), NAN, device="cuda"), torch.full((outputs,), NAN, device="cuda")
+    zeno.dense_gradient(dy, zeno.Saved(codes, torch.ones(n, 1, device="cuda")), dw, db)
+    want = n * float(dy[0, 0])
+    R.assert_near(dw, torch.full((outputs, inputs), want), want * (1024 + 16) * R.U, "dw")
+    R.assert_near(db, torch.full((outputs,), want), want * (1024 + 16) * R.U, "db")
