@@ -89,14 +89,14 @@ zeno_status zeno_layer_norm_gradient(int32_t device, int32_t type, int32_t param
     const zeno_status st = check_sizes(m, n, cols);
     if (st != ZENO_OK) return st;
     const bool rows = m > 0 && n > 0;
-    if (cols > kMaxWeights) return ZENO_ERR_UNSUPPORTED;
+    if (cols > kMaxWeights && (dw || db)) return ZENO_ERR_UNSUPPORTED;
     const int size = size_of(type), wsize = size_of(param_type);
     if (!rows_ok(dy, size, m, n, cols) || (x ? !rows_ok(x, size, m, n, cols) : !rows_ok(codes, 1, m, n, cols) || !rows_ok(scales, 4, m, n, blocks_of(cols))))
         return ZENO_ERR_INVALID_ARG;
     if (!placed(w, wsize) || !placed(dw, wsize) || !placed(db, wsize) || !placed(mean, 4) || !placed(rstd, 4)) return ZENO_ERR_INVALID_ARG;
     if ((rows && (!mean || !rstd)) || (dx && (!rows_ok(dx, size, m, n, cols, false) || !w || (ldw != 0 && ldw < cols)))) return ZENO_ERR_INVALID_ARG;
     if ((dw || db) && m > 1 && ldg < cols) return ZENO_ERR_INVALID_ARG;
-    if (!workspace_ok(workspace, workspace_bytes, zeno::norm_gradient_workspace(m, n, cols))) return ZENO_ERR_INVALID_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, zeno_layer_norm_gradient_workspace(m, n, cols))) return ZENO_ERR_INVALID_ARG;
     if (m == 0) return ZENO_OK;
     zeno::NormGradArgs a = {rows_of(dy, n), rows_of(x, n), rows_of(x ? nullptr : codes, n), rows_of(x ? nullptr : scales, n), rows_of(dx, n),
                             m, n, cols, w, ldw, mean, rstd, dw, db, ldg, static_cast<float *>(workspace)};

@@ -258,3 +258,27 @@ def test_dense_gradient_over_many_rows_of_codes_that_start_anywhere(act):
     want = n * float(dy[0, 0])
     R.assert_near(dw, torch.full((outputs, inputs), want), want * (1024 + 16) * R.U, "dw")
     R.assert_near(db, torch.full((outputs,), want), want * (1024 + 16) * R.U, "db")
+
+
+@pytest.mark.parametrize("cols", [(1 << 20) + 1, (1 << 20) + 8, (1 << 25) + 3])
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("saved", [False, True])
+def test_layer_norm_gradient_of_rows_too_long_for_weight_gradients(cols, act, saved):
+    g = _gen(cols)
+    x = torch.randn(1, 2, cols, generator=g, device="cuda").to(act)
+    dy = torch.randn(1, 2, cols, generator=g, device="cuda").to(act)
+    w = 1 + 0.2 * torch.randn(cols, generator=g, device="cuda")
+    mean, rstd = torch.full((1, 2), 0.125, device="cuda"), torch.full((1, 2), 0.75, device="cuda")
+    source, value = x, x
+    if saved:
+        source = zeno.pack_activations(x)
+        value = R.unpack(source.codes, source.scales)
+    dx = zeno.layer_norm_gradient(dy, source, w, mean, rstd)
+    k = 96 * R.U
+    d, h = dy.double() * w.double(), (value.double() - 0.125) * 0.75
+    want = 0.75 * (d - d.mean(-1, keepdim=True) - h * (d * h).mean(-1, keepdim=True))
+    slack = 0.75 * ((k + 8 * R.U) * (d.abs().mean(-1, keepdim=True) + h.abs() * (d * h).abs().mean(-1, keepdim=True)) + 8 * R.U * d.abs())
+    R.assert_near(dx, want, slack, "dx")
+    with pytest.raises(zeno.ZenoError) as e:
+        zeno.layer_norm_gradient(dy, source, w, mean, rstd, torch.empty(1, cols, device="cuda"))
+    assert e.value.status == zeno.ERR_UNSUPPORTED
