@@ -144,6 +144,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_state[kAbortWords];
     __shared__ int issued[kCodeStages + kStages];            // last round a copy was issued into a stage, plus one
+    __shared__ int scaled[kCodeStages];                      // and the lanes that copy the scales have arrived for
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)cluster_rank();
@@ -192,6 +193,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
             mbar_init(dempty(q), 2 * kEpiWarps);
         }
         for (int s = 0; s < kCodeStages + kStages; ++s) issued[s] = 0;
+        for (int s = 0; s < kCodeStages; ++s) scaled[s] = 0;
         mbar_init(smem_u32(&drain_bar), 1);
         mbar_init(smem_u32(&never_bar), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -208,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
     if (a.followed) pdl_launch_dependents();  // by a kernel of this call, never by the next call's: that one may read V
     const uint32_t tmem = tmem_base_slot;
     volatile int *abortp = &abort_state[0];
-    if (warp == 0) wait_for_nothing(smem_u32(&never_bar), abortp);
+    if (warp == 3) wait_for_nothing(smem_u32(&never_bar), abortp);        // the codes' copies are under way meanwhile
     if (warp == 0 || warp == 2) {
         // ------------------------------------------------------------------ copies: codes (warp 0), dY (warp 2)
         const bool is_codes = warp == 0;
@@ -264,6 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                     cp_async<4>(smem_u32(scale_ring + s * kScaleBytes + (j * 32 + lane) * 4), scales + (valid ? t * a.d.scales.row : 0), valid);
                 }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(cfull(s)) : "memory");
+                if (lane == 0) scaled[s] = (int)round + 1;
                 if (++in_term == a.nkb) in_term = 0;
                 if (++s == kCodeStages) {
                     s = 0;
@@ -493,6 +496,8 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
         for (int s = 0; s < kCodeStages + kStages; ++s)
             if (issued[s] > 0) {
                 const uint32_t b = s < kCodeStages ? cfull(s) : afull(s - kCodeStages);
+                // the scales' warp may have left before the codes' copy that the barrier is to tell of
+                if (s < kCodeStages && scaled[s] < issued[s]) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 32;" ::"r"(b) : "memory");
                 for (uint32_t i = 0; i < kSpinLimit; ++i) {
                     if (mbar_try_wait(b, (uint32_t)(issued[s] - 1) & 1)) break;
                     __nanosleep(64);

@@ -26,6 +26,10 @@ def _gen(seed):
     return torch.Generator(device="cuda").manual_seed(seed)
 
 
+def _rows(g, m, n, cols, dtype, scale=1.0):
+    return (torch.randn(m, n, cols, generator=g, device="cuda") * scale).to(dtype)
+
+
 @pytest.mark.parametrize("cols", [8, 132, 136, 520, 1032, 2056, 4104, 5000])
 @pytest.mark.parametrize("act", [F32, BF16])
 @pytest.mark.parametrize("saved", [False, True])
@@ -282,3 +286,30 @@ def test_layer_norm_gradient_of_rows_too_long_for_weight_gradients(cols, act, sa
     with pytest.raises(zeno.ZenoError) as e:
         zeno.layer_norm_gradient(dy, source, w, mean, rstd, torch.empty(1, cols, device="cuda"))
     assert e.value.status == zeno.ERR_UNSUPPORTED
+
+
+def test_a_call_that_gives_up_ends_soon():
+    """With a limit of zero the warp that copies the scales gives up while the codes' copies are under way: before it ends, a block waits for those copies
+    alone.  (A wait for an arrival that nobody makes any more would take a quarter of a second for every stage.)"""
+    g = _gen(1)
+    saved = zeno.pack_activations(_rows(g, 4, 1000, 512, BF16))
+    dy = _rows(g, 4, 1000, 768, BF16, 0.1)
+    dw, want = torch.empty(4, 768, 512, device="cuda"), torch.empty(4, 768, 512, device="cuda")
+    zeno.dense_gradient(dy, saved, want)
+    zeno.check_operator_status()
+    zeno.debug_set_operator_wait_limit(0)
+    try:
+        for _ in range(3):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            zeno.dense_gradient(dy, saved, dw)
+            end.record()
+            with pytest.raises(zeno.ZenoError) as e:
+                zeno.check_operator_status()
+            assert e.value.status == zeno.ERR_TIMEOUT
+            assert begin.elapsed_time(end) < 100
+    finally:
+        zeno.debug_set_operator_wait_limit(1 << 22)
+    zeno.dense_gradient(dy, saved, dw)
+    zeno.check_operator_status()
+    assert torch.equal(dw, want)
