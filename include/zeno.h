@@ -381,7 +381,9 @@ zeno_status zeno_dense_gradient(int32_t device, int32_t type, int32_t param_type
                                 int64_t ldw, void *db, int64_t ldb, void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Synchronises `stream` and reports whether a kernel of these calls on `device` gave up on a bounded device-side wait since the
- * last such report (its outputs are then undefined): ZENO_ERR_TIMEOUT if so, else ZENO_OK.
+ * last such report for this stream (its outputs are then undefined): ZENO_ERR_TIMEOUT if so, else ZENO_OK.  Every stream is
+ * told of every such kernel that has ended, whichever stream it ran on: a report may be of another stream's call (so may the
+ * first one for a stream, of any earlier call), but none takes another stream's report away.
  * zeno_debug_set_operator_wait_limit: test hook, as zeno_debug_set_wait_limit, for later calls of this process (default 2^22). */
 zeno_status zeno_operator_status(int32_t device, void *stream);
 zeno_status zeno_debug_set_operator_wait_limit(uint32_t polls);

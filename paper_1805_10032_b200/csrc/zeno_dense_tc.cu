@@ -10,6 +10,10 @@
 //   warp 0: copies of the codes;  warp 3: of their scales;  warp 2: of dY;  warp 1 of the pair's first block: the instructions;
 // binary32 dY is rewritten as three bfloat16 terms first, which hold it exactly; few tiles are cut along the tokens.
 //   warps 4 - 19: codes to bfloat16;  warps 20 - 23: a finished tile from TMEM to dW while the next one is summed.
+#include <map>
+#include <mutex>
+#include <utility>
+
 #include "zeno_saved.cuh"
 #include "zeno_tc.cuh"
 
@@ -34,9 +38,8 @@ constexpr int kSmem = kStages * (kABytes + kBBytes) + kCodeStages * (kCodeBytes 
 constexpr int kConvWarps = 16, kSets = 4, kSetWarps = kConvWarps / kSets, kEpiWarps = 4;
 constexpr int kThreads = 32 * (4 + kConvWarps + kEpiWarps);
 constexpr int kTmemCols = 512;                // two sets of 256 sums
-constexpr int kKernelId = 5;
 
-__device__ int g_status;                      // raised by a block whose bounded wait gave up, cleared by who reads it
+__device__ unsigned g_given_up;               // blocks whose bounded waits gave up since the process began
 
 // The tensor core adds with truncation towards zero, which takes about 1.4e-8 of a sum with every 16 tokens: of 2,048 tokens' all positive products
 // 1.8e-6, of 32,768 6.7e-5, and 1.2e-4 in three terms.  So no set of sums in TMEM takes more than a stretch of stages; between two stretches of a tile
@@ -503,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                     __nanosleep(64);
                 }
             }
-        atomicCAS(&g_status, 0, wait_code(kKernelId, abort_state[0], smem_u32(bars)));
+        atomicAdd(&g_given_up, 1u);
     }
     __syncthreads();
     cluster_barrier();                        // the other block's instructions, arrivals and reads have ended too
@@ -704,17 +707,23 @@ cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &d, cu
 
 void set_operator_wait_limit(uint32_t polls) { spin_limit = polls; }
 
-// reads and clears what a block that gave up left
-cudaError_t read_operator_status(cudaStream_t s, int *status) {
+// The count is never cleared, since a block of another stream may give up at any time; what differs is what a stream's last report knew of.
+cudaError_t read_operator_status(int device, cudaStream_t s, int *status) try {
+    static std::mutex mutex;
+    static std::map<std::pair<int, cudaStream_t>, unsigned> known;
     void *at = nullptr;
-    cudaError_t e = cudaGetSymbolAddress(&at, g_status);
-    if (e == cudaSuccess) e = cudaMemcpyAsync(status, at, sizeof(int), cudaMemcpyDeviceToHost, s);
+    unsigned count = 0;
+    cudaError_t e = cudaGetSymbolAddress(&at, g_given_up);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(&count, at, sizeof(count), cudaMemcpyDeviceToHost, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    if (e == cudaSuccess && *status) {
-        e = cudaMemsetAsync(at, 0, sizeof(int), s);
-        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    }
-    return e;
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(mutex);
+    unsigned &before = known[{device, s}];
+    *status = count != before;
+    before = count;
+    return cudaSuccess;
+} catch (...) {
+    return cudaErrorMemoryAllocation;
 }
 
 }  // namespace zeno

@@ -156,7 +156,7 @@ zeno_status zeno_dense_gradient(int32_t device, int32_t type, int32_t param_type
 zeno_status zeno_operator_status(int32_t device, void *stream) {
     DeviceGuard guard(device);
     int status = 0;
-    if (guard.err != cudaSuccess || zeno::read_operator_status(static_cast<cudaStream_t>(stream), &status) != cudaSuccess) return ZENO_ERR_CUDA;
+    if (guard.err != cudaSuccess || zeno::read_operator_status(device, static_cast<cudaStream_t>(stream), &status) != cudaSuccess) return ZENO_ERR_CUDA;
     return status ? ZENO_ERR_TIMEOUT : ZENO_OK;
 }
 

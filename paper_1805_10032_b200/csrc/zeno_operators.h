@@ -89,7 +89,7 @@ cudaError_t launch_dense_gradient(int type, int param_type, const DenseGradArgs 
 int64_t dense_tc_workspace(int type, const DenseGradArgs &a);
 cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &a, cudaStream_t s);
 void set_operator_wait_limit(uint32_t polls);
-cudaError_t read_operator_status(cudaStream_t s, int *status);
+cudaError_t read_operator_status(int device, cudaStream_t s, int *status);
 
 struct LogprobArgs {
     Rows logits;

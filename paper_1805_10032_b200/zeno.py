@@ -760,7 +760,8 @@ def token_gradient(logits, targets, lse, g_logprob, entropy=None, g_entropy=None
 
 
 def check_operator_status(device: int = 0, stream=None):
-    """Synchronises and raises if a kernel of the operators above gave up on a bounded device-side wait (dense_gradient on the tensor cores has them)."""
+    """Synchronises the stream and raises if a kernel of the operators above gave up on a bounded device-side wait (dense_gradient on the tensor
+    cores has them) since this stream was last asked: on this stream, or on another one of the device."""
     st = load_library().zeno_operator_status(device, _current(device, stream))
     if st != OK:
         _done(st, "zeno_operator_status")

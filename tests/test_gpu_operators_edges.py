@@ -313,3 +313,34 @@ def test_a_call_that_gives_up_ends_soon():
     zeno.dense_gradient(dy, saved, dw)
     zeno.check_operator_status()
     assert torch.equal(dw, want)
+
+
+def test_every_stream_is_told_of_a_wait_that_ran_out():
+    g = _gen(1)
+    saved = zeno.pack_activations(_rows(g, 2, 200, 512, BF16))
+    dy = _rows(g, 2, 200, 768, BF16, 0.1)
+    dw = torch.empty(2, 768, 512, device="cuda")
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def told(stream):
+        try:
+            zeno.check_operator_status(stream=stream)
+        except zeno.ZenoError as e:
+            assert e.status == zeno.ERR_TIMEOUT
+            return True
+        return False
+
+    for s in (a, b, None):                                       # whatever earlier calls left
+        told(s)
+    torch.cuda.synchronize()
+    zeno.debug_set_operator_wait_limit(0)
+    try:
+        zeno.dense_gradient(dy, saved, dw, stream=a)
+    finally:
+        zeno.debug_set_operator_wait_limit(1 << 22)
+    a.synchronize()
+    assert told(b)                                               # which must not take the report from the stream that the call ran on
+    assert told(a) and told(None)
+    assert not (told(a) or told(b) or told(None))
+    zeno.dense_gradient(dy, saved, dw, stream=b)
+    assert not (told(b) or told(a) or told(None))
