@@ -344,3 +344,37 @@ def test_every_stream_is_told_of_a_wait_that_ran_out():
     assert not (told(a) or told(b) or told(None))
     zeno.dense_gradient(dy, saved, dw, stream=b)
     assert not (told(b) or told(a) or told(None))
+
+
+@pytest.mark.parametrize("cols", [1, 127, 129, 777, 1024])
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_codes_in_rows_of_any_stride_through_the_c_abi(cols, act):
+    """The binding makes rows of multiples of 16 bytes; the C ABI takes any, without a byte written between them."""
+    g = _gen(cols)
+    m, n = 3, 7
+    x = _rows(g, m, n, cols, act, 30.0)
+    x[0, 1, cols // 2] = NAN
+    x[1, 2, cols - 1] = INF
+    x[2, 3] = 0.0
+    x[2, 4] *= 2.0 ** 100
+    want, want_scales = R.pack(x)
+    lib = zeno.load_library()
+    blocks = -(-cols // 128)
+    for first, row, group in ((1, cols, n * cols), (3, cols + 2, n * (cols + 2) + 5), (0, cols + 1, n * (cols + 1))):
+        codes = torch.full((first + m * group + 16,), 0xa5, device="cuda", dtype=torch.uint8)
+        scales = torch.full((m * n * (blocks + 1),), -1.0, device="cuda")
+        st = lib.zeno_pack_activations(0, zeno.F32 if act == F32 else zeno.BF16, zeno.RowsDesc(x.data_ptr(), cols, n * cols), m, n, cols,
+                                       zeno.RowsDesc(codes.data_ptr() + first, row, group), zeno.RowsDesc(scales.data_ptr(), blocks + 1, n * (blocks + 1)),
+                                       torch.cuda.current_stream().cuda_stream)
+        assert st == zeno.OK
+        got = codes[first:].as_strided((m, n, cols), (group, row, 1))
+        got_scales = scales.as_strided((m, n, blocks), (n * (blocks + 1), blocks + 1, 1))
+        assert torch.equal(got_scales.double().cpu(), want_scales)
+        value = got.clone().view(torch.float8_e4m3fn).double() * got_scales.double().repeat_interleave(128, -1)[..., :cols]
+        want_value = want * want_scales.repeat_interleave(128, -1)[..., :cols]
+        assert torch.equal(value.cpu().nan_to_num(nan=-7.0), want_value.nan_to_num(nan=-7.0))
+        # the bits of the binding's codes
+        packed = zeno.pack_activations(x)
+        assert torch.equal(got, packed.codes.view(torch.uint8))
+        got.fill_(0xa5)
+        assert (codes == 0xa5).all() and (scales.as_strided((m, n), (n * (blocks + 1), blocks + 1), blocks) == -1.0).all()
