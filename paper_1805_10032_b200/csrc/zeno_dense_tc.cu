@@ -357,7 +357,8 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    // Not before the stores: they need what the loads bring.  An arrival right behind the loads let the next codes overtake them.
+                    // Behind the fence: it orders the loads of the codes, too, ahead of the next copy's writes, and an arrival alone does not (right behind
+                    // the loads, without a fence, it gave wrong sums).
                     mbar_arrive(cempty(sc));
                     if (rank == 0) mbar_arrive(bready(s));
                     else mbar_arrive_cluster(remote_bready + s * 8);

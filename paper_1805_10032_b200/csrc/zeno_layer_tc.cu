@@ -463,8 +463,7 @@ layer_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll
                     for (int c = 0; c < 8; ++c) vq[c] = make_uint4(0u, 0u, 0u, 0u);
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar_empty(s));       // this set is done with the stage's weight tiles
+                release_read_stage(bar_empty(s), lane);         // this set is done with the stage's weight tiles
                 uint32_t wa[32], wb[32];                        // bf16: wa = packed pairs; fp32: wa = hi, wb = lo
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {

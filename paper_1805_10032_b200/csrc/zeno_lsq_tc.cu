@@ -262,8 +262,7 @@ lsq_tc_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__
                 const int piece = a.wide ? 2 * j + h : h * n_pad + j;        // where row j of this warp's k-block landed
                 if (4 * u < n_pad) v[u] = *reinterpret_cast<const float4 *>(st + off_raw + piece * 128 + ((c ^ (piece & 7)) << 4));
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_empty(s));
+            release_read_stage(bar_empty(s), lane);
             ok = mbar_wait(bar_free(gb), (bround & 1) ^ 1, abortp);        // the MMAs that read this operand last are done
             if (!ok) break;
             tc_fence_after();
@@ -317,8 +316,6 @@ lsq_tc_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__
             uint32_t hi[32], lo[32];
 #pragma unroll
             for (int c = 0; c < 8; ++c) v[c] = *reinterpret_cast<const float4 *>(src + ((c ^ flip ^ (piece & 7)) << 4));
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_empty(s));
             if (flip) {
 #pragma unroll
                 for (int c = 0; c < 8; c += 2) {
@@ -338,6 +335,7 @@ lsq_tc_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__
                     lo[4 * c + u] = __float_as_uint(e[u] - h);
                 }
             }
+            release_read_stage(bar_empty(s), lane);
             if (!mbar_wait(bar_free(g), (around & 1) ^ 1, abortp)) break;
             tc_fence_after();
             tc_st32(a_bufs + g * 64, hi);

@@ -317,8 +317,7 @@ stream_tf32x3_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_con
                 uint32_t hi[32], lo[32];
 #pragma unroll
                 for (int c = 0; c < 8; ++c) v[c] = *reinterpret_cast<const float4 *>(src + ((c ^ (row & 7)) << 4));
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar_empty(p, s));    // the stage may be refilled
+                release_read_stage(bar_empty(p, s), lane);      // the stage may be refilled
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     const float e[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
