@@ -368,7 +368,8 @@ zeno_status zeno_pack_activations(int32_t device, int32_t type, const zeno_rows 
 /* A dense layer's weight gradient for every group, from the gradient dy at its output and its input as
  * zeno_pack_activations kept it:  dw[i][o][k] = sum over group i's rows of dy_o x_k,  db[i][o] = sum of dy_o.
  * dw: per group outputs x inputs entries, row-major, ldw elements after the previous group's; db (or NULL) likewise with ldb:
- * slices of V in the layout of the parameter vector.  The products are exact, their sums binary32.  (The tensor cores add with truncation
+ * slices of V in the layout of the parameter vector.  The products are exact, their sums binary32.  (Of binary32 dy the tensor cores take three
+ * bfloat16 terms, which hold an entry of 2^-110 or more as it is and a smaller one to within 2^-134.  They add with truncation
  * towards zero; their sums go on in additions to nearest after every 1,024 tokens, 4,096 for a bfloat16 result: all positive terms come out
  * too small by about 7e-7.)
  * The scales have to be powers of two, as zeno_pack_activations writes them.  Codes in rows and groups of multiples of 16 bytes, one

@@ -515,7 +515,8 @@ __global__ void __launch_bounds__(kThreads, 1) dense_tc_kernel(const __grid_cons
 }
 
 // dY as bfloat16 terms in [group][term][token][outputs, rounded up to 8]: one term (of bfloat16 in rows that no tensor map can step through) or
-// three, which hold a binary32 number exactly: each takes the leading 8 bits of what is left.  An infinity or NaN is its first term.
+// three, which hold a binary32 number exactly (from 2^-110 on; a smaller one has bits under bfloat16's smallest step, 2^-133, and is off by half of that): each
+// takes the leading 8 bits of what is left.  An infinity or NaN is its first term.
 template <typename T, int TERMS>
 __global__ void __launch_bounds__(256) dense_terms_kernel(Rows dy, int64_t rows, int64_t n, int64_t outputs, int64_t pitch, __nv_bfloat16 *out, int vectors) {
     const int64_t per_row = pitch / 8, total = rows * per_row;

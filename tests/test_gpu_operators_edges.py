@@ -346,6 +346,23 @@ def test_every_stream_is_told_of_a_wait_that_ran_out():
     assert not (told(b) or told(a) or told(None))
 
 
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_dense_gradient_of_the_smallest_entries(act):
+    """One token of a row that is not zero, under codes of 256: no additions.  Three bfloat16 terms hold 24 bits from 2^-110 on; below, half of bfloat16's smallest step
+    is missing at most."""
+    m, n, cols = 16, 64, 512
+    saved = zeno.pack_activations(torch.full((m, n, cols), 256.0, device="cuda", dtype=BF16))
+    dw = torch.empty(m, cols, cols, device="cuda")
+    e = torch.linspace(-148, -90, cols, device="cuda").round()
+    for part in (2.0 ** -7, 2.0 ** -7 + 2.0 ** -15 + 2.0 ** -23, 1 - 2.0 ** -23):
+        dy = torch.zeros(m, n, cols, device="cuda", dtype=act)
+        dy[:, 17] = (torch.exp2(e.double()) * (1 + part)).to(act)
+        zeno.dense_gradient(dy, saved, dw)
+        value = dy[:, 17].double()
+        off = torch.where((act == F32) & (value < 2.0 ** -110), 2.0 ** -134, 0.0)
+        R.assert_near(dw, (256 * value).unsqueeze(-1).expand(m, cols, cols), 256 * off.unsqueeze(-1), "dw")
+
+
 @pytest.mark.parametrize("cols", [1, 127, 129, 777, 1024])
 @pytest.mark.parametrize("act", [F32, BF16])
 def test_codes_in_rows_of_any_stride_through_the_c_abi(cols, act):
