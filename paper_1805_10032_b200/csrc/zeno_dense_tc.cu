@@ -600,7 +600,9 @@ struct Plan {
     int64_t pitch, part_at, kept_at, bytes;
 };
 
-// Parts: with fewer tiles than half the pairs of SMs, as many as the pairs take, each of eight stages and more.  The count of SMs is this
+// Parts: with fewer tiles than half the pairs of SMs, as many as the pairs take, each of eight stages and more (bfloat16: 4 x 8192 tokens, 512 x 1024,
+// 53 us, 80 in one part; 1 x 8192, 512 x 512, 27 and 72).  More tiles are not cut: in four parts 54 of them take 53 us and not 55 (6 x 4843, 640 x 560), 40
+// take 39 and not 29 (10 x 2048, 512 x 512).  The count of SMs is this
 // design's, so that the workspace's size needs no device.
 constexpr int kPairs = 74;
 
