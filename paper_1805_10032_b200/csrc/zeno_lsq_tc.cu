@@ -31,8 +31,8 @@
 //   warps 4-11   two converter sets on alternate k-blocks: thread = TMEM lane; reads its 128 bytes of V,
 //                accumulates v^2, stores v_hi / v_lo to TMEM as the A operand
 //   warps 12-15  drain the accumulator sets into registers; at the end write the slab
-// A stage of the load ring is free again as soon as the converters and the splitters have read it into
-// registers; only the operand slots wait for the MMAs.  An operand slot is a TMEM buffer (A: the
+// A stage of the load ring is free again when the converters and the splitters have read it and split what they read;
+// only the operand slots wait for the MMAs.  An operand slot is a TMEM buffer (A: the
 // candidates' entries) and a shared-memory buffer (B: the split rows of A) with ONE pair of barriers:
 // the issuing warp is the slowest link of the chain (cycle stamps: every barrier probe costs it 100 to
 // 500 cycles of shared-memory latency even when the phase has long completed), so it waits for one barrier
@@ -241,7 +241,8 @@ lsq_tc_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__
         // ------------------------------------------------------------------ rows of A: split for the MMA, and A x
         // Warp 2 takes the even k-block's rows of every stage, warp 3 the odd one's.  All of a lane's rows
         // are loaded before the first store (loads placed after stores to the same shared array would wait
-        // for them), and the stage is released as soon as they are in registers.
+        // for them).  The stage is released behind the one fence of the turn (as soon as the rows are in
+        // registers, behind a fence of its own, the step took 1 % longer).
         const int sset = warp >= 18 ? 1 : 0;          // set 0 takes the even stages, set 1 the odd
         const int h = warp & 1;
         float accx[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};    // rows 4 u + lane / 8 (u < n_pad / 4)
@@ -262,7 +263,6 @@ lsq_tc_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__
                 const int piece = a.wide ? 2 * j + h : h * n_pad + j;        // where row j of this warp's k-block landed
                 if (4 * u < n_pad) v[u] = *reinterpret_cast<const float4 *>(st + off_raw + piece * 128 + ((c ^ (piece & 7)) << 4));
             }
-            release_read_stage(bar_empty(s), lane);
             ok = mbar_wait(bar_free(gb), (bround & 1) ^ 1, abortp);        // the MMAs that read this operand last are done
             if (!ok) break;
             tc_fence_after();
@@ -279,9 +279,12 @@ lsq_tc_kernel(const __grid_constant__ CUtensorMap map_v, const __grid_constant__
                 *reinterpret_cast<float4 *>(bop + (2 + h) * n_pad * 128 + sw) =
                     make_float4(v[u].x - hi.x, v[u].y - hi.y, v[u].z - hi.z, v[u].w - hi.w);
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // generic writes -> tensor-core reads
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // generic writes -> tensor-core reads, and the stage's reads -> the next copy
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar_ready(gb));
+            if (lane == 0) {
+                mbar_arrive(bar_empty(s));
+                mbar_arrive(bar_ready(gb));
+            }
         }
         // A x: the eight lanes of a row add up
 #pragma unroll
