@@ -414,6 +414,54 @@ zeno_status zeno_token_gradient(int32_t device, int32_t type, const zeno_rows *l
                                 const int32_t *targets, const float *lse, const float *entropy, const float *g_logprob,
                                 const float *g_entropy, const zeno_rows *grad, void *stream);
 
+/* A language model's embedding:  y_t = scale table[id_t].  tokens: int32[m][n]; one outside [0, vocab) gets a row of zeros.
+ * table: vocab rows of cols entries, one after the other; a group's begins ldt entries after the previous group's (0: one table
+ * for all groups), as slices of parameter vectors do.  y: in `type`, rounded once.
+ * INVALID_ARG also: vocab < 1, cols < 1.  UNSUPPORTED also, here and in the next three calls: vocab > 2^24, cols > 2^20. */
+zeno_status zeno_embed(int32_t device, int32_t type, int32_t param_type, const int32_t *tokens, int32_t m, int64_t n,
+                       int64_t vocab, int64_t cols, const void *table, int64_t ldt, float scale, const zeno_rows *y, void *stream);
+
+/* The backward pass of zeno_embed from dy, the gradient at y, for every group:
+ *   dtable[i][v] = scale times the sum of dy over group i's tokens with id v        (add: that is added to what is there).
+ * dtable: laid out like the table, ldt entries from one group's to the next: a slice of V.  Every row of it is written, those
+ * that no token names with zeros; with `add` (tied weights: the output layer's gradient is there already) those are left alone,
+ * and a sum is added before the one rounding.  dy of tokens outside the vocabulary is not read.  A row's tokens are summed in
+ * their order, whatever the launch. */
+int64_t zeno_embed_gradient_workspace(int32_t m, int64_t n, int64_t vocab, int64_t cols);
+zeno_status zeno_embed_gradient(int32_t device, int32_t type, int32_t param_type, const int32_t *tokens, const zeno_rows *dy,
+                                int32_t m, int64_t n, int64_t vocab, int64_t cols, float scale, int32_t add, void *dtable,
+                                int64_t ldt, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Log probabilities of given tokens from the last hidden states x (rows of cols entries) and the output layer's weights w (vocab
+ * rows of cols entries, ldw entries from one group's to the next, 0: shared), without logits in memory:
+ *   z = scale x w^T,  lse = log sum_j exp(z_j),  logprob = z_target - lse.
+ * targets: int32[m][n]; a token whose target is outside [0, vocab) takes no part: logprob and lse 0, its x is not read.
+ * logprobs, lse: float[m][n] or NULL.  Products are exact, their sums binary32 (of binary32 x or w the tensor cores take three
+ * bfloat16 terms, which hold an entry of 2^-110 or more as it is; products under 2^-24 of the leading one are left out).  The
+ * tensor cores add with truncation towards zero; sums go on in additions to nearest after every stretch of the contraction.
+ * A row with a logit that is NaN or plus infinity gives NaN; in binary32 any infinity or NaN among its x or in w may.
+ * Weights that are bfloat16, aligned to 16 bytes, in rows and groups of multiples of 8 entries, are read as they lie; others are
+ * rewritten in the workspace, up to 256 MB of them at a time. */
+int64_t zeno_linear_logprobs_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols, int64_t vocab,
+                                       const void *w, int64_t ldw);
+zeno_status zeno_linear_logprobs(int32_t device, int32_t type, int32_t param_type, const zeno_rows *x, int32_t m, int64_t n,
+                                 int64_t cols, int64_t vocab, const void *w, int64_t ldw, const int32_t *targets, float scale,
+                                 float *logprobs, float *lse, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* The gradient of  sum over tokens of g_logprob logprob  at x and at w, from zeno_linear_logprobs's lse:
+ *   D_tj = g_logprob_t scale ([j = target_t] - exp(z_tj - lse_t)),  dx = D w,  dw[i] = D^T x over group i's tokens.
+ * lse, g_logprob: float[m][n].  dx or NULL: like x; zero for a token without a target.  dw or NULL: vocab x cols entries for every
+ * group, lddw entries from one group's to the next (a slice of V), also where w is shared.  The logits are computed again, a
+ * piece of the vocabulary at a time; D is kept for that piece, in bfloat16 (three terms of it, as above, if x or w is binary32).
+ * exp(z - lse) carries the rounding of lse, 2^-24 |lse|. */
+int64_t zeno_linear_logprobs_gradient_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols,
+                                                int64_t vocab, const void *w, int64_t ldw, int32_t want_dx);
+zeno_status zeno_linear_logprobs_gradient(int32_t device, int32_t type, int32_t param_type, const zeno_rows *x, int32_t m,
+                                          int64_t n, int64_t cols, int64_t vocab, const void *w, int64_t ldw,
+                                          const int32_t *targets, float scale, const float *lse, const float *g_logprob,
+                                          const zeno_rows *dx, void *dw, int64_t lddw, void *workspace, int64_t workspace_bytes,
+                                          void *stream);
+
 /* Synchronises `stream` and reports whether any kernel enqueued through this handle gave up on a
  * bounded device-side wait (its outputs are then undefined): ZENO_ERR_TIMEOUT if so, else
  * ZENO_OK.  The condition is sticky for the life of the handle. */

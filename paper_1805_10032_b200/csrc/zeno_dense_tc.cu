@@ -709,18 +709,23 @@ cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &d, cu
                           static_cast<float *>(d.dw), d.ldw, (int)(d.db != nullptr));
 }
 
-void set_operator_wait_limit(uint32_t polls) { spin_limit = polls; }
+void set_operator_wait_limit(uint32_t polls) {
+    spin_limit = polls;
+    set_head_wait_limit(polls);
+}
 
 // The count is never cleared, since a block of another stream may give up at any time; what differs is what a stream's last report knew of.
 cudaError_t read_operator_status(int device, cudaStream_t s, int *status) try {
     static std::mutex mutex;
     static std::map<std::pair<int, cudaStream_t>, unsigned> known;
     void *at = nullptr;
-    unsigned count = 0;
+    unsigned count = 0, others = 0;
     cudaError_t e = cudaGetSymbolAddress(&at, g_given_up);
     if (e == cudaSuccess) e = cudaMemcpyAsync(&count, at, sizeof(count), cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = head_given_up(&others, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     if (e != cudaSuccess) return e;
+    count += others;
     std::lock_guard<std::mutex> lock(mutex);
     unsigned &before = known[{device, s}];
     *status = count != before;

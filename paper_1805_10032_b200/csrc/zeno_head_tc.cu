@@ -1,0 +1,566 @@
+// The products around the output layer on the tensor cores: logits with the sums of their exponentials, the probabilities' gradient from
+// logits computed again, and its two products.
+//
+// A pair of blocks (a cluster of two SMs) takes a tile of 256 rows by kN columns: the pair's instruction (cta_group::2, M = 256) reads 128 rows of A and
+// half of the columns of B from each block's shared memory, so that a block copies half of what the tile needs, and leaves 128 rows of sums in either
+// block's TMEM.  Operands are bfloat16, in binary32 sums; a binary32 operand is three terms whose products are summed one pair of terms after the other, the
+// leading pair last.  X and W lie with the contraction's index contiguous for the logits ("K-major"); P W takes W, and P^T X both, with the index of the
+// result contiguous ("MN-major"), all in the 128-byte swizzled layouts that the tensor copies write.
+//   warp 0: copies;  warp 1: the pair's instructions in the first block, in the second the news that its copies have landed;
+//   warps 2 - 9: sums from TMEM, the next tile's being formed meanwhile: 32 rows and half of the columns each.
+//
+// The tensor core adds with truncation towards zero.  So no set of sums in TMEM takes more than a stretch of stages; what it holds is then added in
+// registers, to nearest.
+#include "zeno_head.h"
+#include "zeno_tc.cuh"
+
+namespace zeno {
+
+namespace {
+
+constexpr int kHalfRows = 128, kPairRows = 256;
+constexpr int kK = 64;                               // contraction indices of a stage: 128 bytes
+constexpr int kEpiWarps = 8, kThreads = 32 * (2 + kEpiWarps);
+constexpr int kABytes = kHalfRows * kK * 2;
+constexpr int kBox = 4096;                           // 32 rows of 128 bytes on their way out; each warp has two
+constexpr int kBand = 16;                            // tiles of rows that go together through the columns: their operand stays in L2
+
+template <int N>
+struct Shape {
+    static constexpr int kHalf = N / 2;
+    static constexpr int kBBytes = kHalf * kK * 2;
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = N == 256 ? 5 : 6;
+    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * 2 * kBox + 1024;
+};
+
+__device__ unsigned g_given_up;                      // blocks whose bounded waits gave up since the process began
+
+struct KernelArgs {
+    HeadTcArgs h;
+    int row_tiles, col_tiles;                        // row_tiles: at most, of a group
+    int drain, drain_small;                          // stages of a stretch
+    int manual_stores;                               // kWeights: rows that no tensor copy can write
+    uint32_t spin_limit;
+};
+
+__device__ __forceinline__ void remote_arrive(uint32_t addr) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+// an arrival on the barrier at this place in both blocks, once the instructions so far have ended
+__device__ __forceinline__ void commit_to_both(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// MN-major operand: rows of 64 contiguous entries, one for each value of the contraction index; eight of them make a group of 1024 bytes, the next 64
+// entries lie kK rows on.
+__device__ __forceinline__ uint64_t mn_major(uint32_t addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((addr & 0x3ffffu) >> 4);
+    d |= (uint64_t)((kK * 128) >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+__device__ __forceinline__ void store_box(const CUtensorMap *map, const void *smem, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(smem)), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void add_box(const CUtensorMap *map, const void *smem, int c0, int c1, int c2) {
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(smem)), "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
+__device__ __forceinline__ void boxes_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void boxes_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+__device__ __forceinline__ void boxes_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// One tile and the part of the contraction that goes into it.
+struct Item {
+    int group, row0, rows_end, col0, kb0, kb1, split;
+};
+
+template <HeadStep STEP, int N, typename P>
+__global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                              const __grid_constant__ CUtensorMap map_out, const KernelArgs args) {
+    using S = Shape<N>;
+    constexpr int HN = S::kHalf;
+    constexpr bool kAMn = STEP == HeadStep::kWeights, kBMn = STEP == HeadStep::kWeights || STEP == HeadStep::kInputs;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    // full, empty, landed [kStages]; dfull, dempty [2]
+    constexpr int kBars = 3 * S::kStages + 4;
+    __shared__ __align__(8) uint64_t bars[kBars];
+    __shared__ __align__(8) uint64_t drain_bar, never_bar;
+    __shared__ uint32_t tmem_base_slot;
+    __shared__ int abort_state[kAbortWords];
+    __shared__ int issued[S::kStages];                         // last round a copy was issued into a stage, plus one
+
+    const HeadTcArgs &h = args.h;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = (int)cluster_rank();
+    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *boxes = ring + S::kStages * S::kStageBytes;
+    auto full = [&](int s) { return smem_u32(&bars[s]); };
+    auto empty = [&](int s) { return smem_u32(&bars[S::kStages + s]); };
+    auto landed = [&](int s) { return smem_u32(&bars[2 * S::kStages + s]); };
+    auto dfull = [&](int q) { return smem_u32(&bars[3 * S::kStages + q]); };
+    auto dempty = [&](int q) { return smem_u32(&bars[3 * S::kStages + 2 + q]); };
+
+    if (tid == 0) {
+        abort_state[0] = 0;
+        abort_state[1] = (int)args.spin_limit;
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+            mbar_init(landed(s), 1);
+            issued[s] = 0;
+        }
+        for (int q = 0; q < 2; ++q) {
+            mbar_init(dfull(q), 1);
+            mbar_init(dempty(q), 2 * kEpiWarps);
+        }
+        mbar_init(smem_u32(&drain_bar), 1);
+        mbar_init(smem_u32(&never_bar), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(2 * N) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();                        // the other block's barriers are there
+    tc_fence_after();
+    pdl_wait();
+    if (!h.last) pdl_launch_dependents();     // by a kernel of this call, never by the next call's
+    const uint32_t tmem = tmem_base_slot;
+    volatile int *abortp = &abort_state[0];
+
+    const int pair = blockIdx.x >> 1, pairs_of_blocks = gridDim.x >> 1;
+    // The tiles in their order: rows first within a band of kBand tiles, then columns, so that pairs next to one another share the columns' operand and all
+    // of a band's rows stay in L2.
+    const int only_end = h.groups == 1 ? __ldcg(h.end) : 0;
+    const int row_tiles = STEP != HeadStep::kWeights && h.groups == 1 ? min(args.row_tiles, (only_end + kPairRows - 1) / kPairRows) : args.row_tiles;
+    const int64_t per_group = (int64_t)row_tiles * args.col_tiles, tiles = per_group * h.groups, items = tiles * (STEP == HeadStep::kInputs ? h.splits : 1);
+    // false: no further item
+    auto get_item = [&](int li, Item &it) {
+        int64_t item = pair + (int64_t)li * pairs_of_blocks;
+        if (item >= items) return false;
+        it.split = 0;
+        if (STEP == HeadStep::kInputs) {
+            it.split = (int)(item / tiles);
+            item -= it.split * tiles;
+        }
+        it.group = (int)(item / per_group);
+        int64_t in = item - it.group * per_group;
+        const int band = (int)(in / ((int64_t)kBand * args.col_tiles));
+        in -= (int64_t)band * kBand * args.col_tiles;
+        const int band_rows = min(kBand, row_tiles - band * kBand);
+        const int ct = (int)in / band_rows, rt = band * kBand + (int)in - ct * band_rows;
+        it.col0 = ct * N;
+        if (STEP == HeadStep::kWeights) {
+            it.row0 = rt * kPairRows;                                     // words of the piece
+            it.rows_end = (int)h.piece;
+            it.kb0 = __ldcg(h.begin + it.group) / kK;
+            it.kb1 = __ldcg(h.end + it.group) / kK;
+        } else {
+            it.rows_end = h.groups == 1 ? only_end : __ldcg(h.end + it.group);
+            it.row0 = (h.groups == 1 ? 0 : __ldcg(h.begin + it.group)) + rt * kPairRows;
+            const int nkb = (int)(((STEP == HeadStep::kInputs ? h.piece : h.cols) + kK - 1) / kK);
+            it.kb0 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * it.split / h.splits) : 0;
+            it.kb1 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * (it.split + 1) / h.splits) : nkb;
+            if (it.row0 >= it.rows_end) it.kb1 = it.kb0;                  // a group with fewer tokens
+        }
+        return true;
+    };
+    // Stretches of an item's stages: the smaller terms' in long ones, what is left of them with the first of the leading terms'.
+    struct Stretches {
+        int all, small, early, late, each;
+        __device__ Stretches(const KernelArgs &k, const Item &it) {
+            const int len = it.kb1 - it.kb0;
+            all = len * k.h.pairs;
+            small = all - len;
+            each = k.drain_small;
+            early = small / each;
+            late = (len + k.drain - 1) / k.drain;
+        }
+        __device__ int count() const { return early + late; }
+        __device__ int at(int part) const { return part <= early ? part * each : small + (int)((int64_t)(all - small) * (part - early) / late); }
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ copies
+        wait_for_nothing(smem_u32(&never_bar), abortp);
+        int s = 0;
+        uint32_t round = 0;
+        bool ok = true;
+        Item it;
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li)
+            for (int pr = 0; ok && pr < h.pairs; ++pr) {
+                const int plane_a = h.pair_a[pr], plane_b = (STEP == HeadStep::kWeights ? 0 : it.group * h.b_terms) + h.pair_b[pr];
+                for (int kb = it.kb0; kb < it.kb1; ++kb) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (round & 1) ^ 1, abortp));
+                    if (!ok) break;
+                    if (elect_one()) {
+                        uint8_t *to = ring + s * S::kStageBytes;
+                        mbar_expect_tx(full(s), S::kStageBytes);
+                        issued[s] = (int)round + 1;
+                        if (kAMn) {
+#pragma unroll 1
+                            for (int q = 0; q < 2; ++q) tma_load_3d(smem_u32(to + q * kK * 128), &map_a, it.row0 + rank * kHalfRows + q * 64, kb * kK, plane_a, full(s));
+                        } else {
+                            tma_load_3d(smem_u32(to), &map_a, kb * kK, it.row0 + rank * kHalfRows, plane_a, full(s));
+                        }
+                        to += kABytes;
+                        const int c0 = it.col0 + rank * HN;
+                        if (kBMn) {
+                            const int k0 = STEP == HeadStep::kInputs ? (int)h.b_row0 + kb * kK : kb * kK;
+#pragma unroll 1
+                            for (int q = 0; q < HN / 64; ++q) tma_load_3d(smem_u32(to + q * kK * 128), &map_b, c0 + q * 64, k0, plane_b, full(s));
+                        } else {
+                            tma_load_3d(smem_u32(to), &map_b, kb * kK, (int)h.b_row0 + c0, plane_b, full(s));
+                        }
+                    }
+                    __syncwarp();
+                    if (++s == S::kStages) {
+                        s = 0;
+                        ++round;
+                    }
+                }
+            }
+    } else if (warp == 1 && rank != 0) {
+        // ------------------------------------------------------------------ the second block's copies have landed
+        const uint32_t remote = cluster_addr(&bars[2 * S::kStages], 0);
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        Item it;
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li)
+            for (int j = 0, all = (it.kb1 - it.kb0) * h.pairs; j < all; ++j) {
+                ok = __all_sync(0xffffffffu, mbar_wait(full(s), ph, abortp));
+                if (!ok) break;
+                if (lane == 0) remote_arrive(remote + s * 8);
+                if (++s == S::kStages) {
+                    s = 0;
+                    ph ^= 1;
+                }
+            }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ instructions, by the first block for both
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kAMn ? 1u : 0u) << 15) | ((kBMn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kPairRows >> 4) << 24);
+        int s = 0;
+        uint32_t ph = 0, drain = 0;                                  // stretches so far
+        bool ok = true;
+        Item it;
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li) {
+            const Stretches st(args, it);
+            for (int part = 0, parts = st.count(); ok && part < parts; ++part, ++drain) {
+                const int set = (int)(drain & 1), from = st.at(part), to = st.at(part + 1);
+                ok = __all_sync(0xffffffffu, mbar_wait(dempty(set), ((drain >> 1) & 1) ^ 1, abortp));
+                if (!ok) break;
+                tc_fence_after();
+                for (int j = from; j < to; ++j) {
+                    ok = mbar_wait(full(s), ph, abortp) && mbar_wait(landed(s), ph, abortp);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t ab = smem_u32(ring + s * S::kStageBytes), bb = ab + kABytes;
+#pragma unroll
+                        for (int k = 0; k < kK / 16; ++k)        // 16 contraction indices: 32 bytes of a row, or 16 rows of 128 bytes
+                            mma_pair(tmem + set * N, kAMn ? mn_major(ab + k * 2048) : smem_desc_sw128(ab + k * 32), kBMn ? mn_major(bb + k * 2048) : smem_desc_sw128(bb + k * 32),
+                                     idesc, (uint32_t)((j - from) | k));
+                        commit_to_both(empty(s));
+                        if (j + 1 == to) commit_to_both(dfull(set));
+                    }
+                    __syncwarp();
+                    if (++s == S::kStages) {
+                        s = 0;
+                        ph ^= 1;
+                    }
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ sums
+        const int quad = warp & 3, half = (warp - 2) >> 2;         // TMEM lanes that this warp may access; its half of the columns
+        const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[3 * S::kStages + 2], 0);
+        uint8_t *box = boxes + (warp - 2) * 2 * kBox;
+        int turn = 0;
+        uint32_t drain = 0;
+        bool ok = true;
+        Item it;
+        // 16 bytes of this lane's row in the box that goes out next
+        auto put16 = [&](int chunk, uint4 v) { *reinterpret_cast<uint4 *>(box + turn * kBox + lane * 128 + ((chunk ^ (lane & 7)) << 4)) = v; };
+        auto open_box = [&] {                                      // the box's last store has been read
+            if (lane == 0) boxes_wait_read_but_one();
+            __syncwarp();
+        };
+        auto close_box = [&](bool add, int c0, int c1, int c2) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if (add) add_box(&map_out, box + turn * kBox, c0, c1, c2);
+                else store_box(&map_out, box + turn * kBox, c0, c1, c2);
+                boxes_commit();
+            }
+            turn ^= 1;
+        };
+        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li) {
+            float acc[HN];
+#pragma unroll
+            for (int c = 0; c < HN; ++c) acc[c] = 0.f;
+            const int parts = Stretches(args, it).count();
+            for (int part = 0; part < parts; ++part, ++drain) {
+                const int set = (int)(drain & 1);
+                ok = __all_sync(0xffffffffu, mbar_wait(dfull(set), (drain >> 1) & 1, abortp));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + set * N + half * HN;
+#pragma unroll
+                for (int c0 = 0; c0 < HN; c0 += 32) {
+                    uint32_t v[2][16];
+                    tc_ld16(from + c0, v[0]);
+                    tc_ld16(from + c0 + 16, v[1]);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) acc[c0 + k] += __uint_as_float(v[k / 16][k % 16]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (rank == 0) mbar_arrive(dempty(set));
+                    else remote_arrive(remote_dempty + set * 8);
+                }
+            }
+            if (!ok) break;
+            const int warp_row = it.row0 + rank * kHalfRows + quad * 32, row = warp_row + lane;
+            const int col = it.col0 + half * HN;                   // the first of this thread's columns
+            if (STEP != HeadStep::kWeights && it.row0 >= it.rows_end) continue;
+
+            if constexpr (STEP == HeadStep::kSums) {
+                const bool valid = row < it.rows_end;
+                const int have = (int)min((int64_t)HN, h.piece - col);          // words of this thread
+#pragma unroll
+                for (int c = 0; c < HN; ++c) acc[c] *= h.scale;
+                if (have < HN)
+#pragma unroll
+                    for (int c = 0; c < HN; ++c)
+                        if (c >= have) acc[c] = -INFINITY;
+                const int target = valid ? h.targets[row] - (int)(h.v0 + col) : -1;
+                if (__any_sync(0xffffffffu, target >= 0 && target < have)) {
+                    float z = 0.f;
+#pragma unroll
+                    for (int c = 0; c < HN; ++c) z = c == target ? acc[c] : z;
+                    if (target >= 0 && target < have) h.target_logit[row] = z;
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sum[4] = {};
+#pragma unroll
+                for (int c = 0; c < HN; ++c) top[c & 3] = fmaxf(top[c & 3], acc[c]);
+                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), beside = most == -INFINITY ? 0.f : most;
+#pragma unroll
+                for (int c = 0; c < HN; ++c) sum[c & 3] += exp2_fast((acc[c] - beside) * 1.4426950408889634f);
+                if (valid && have > 0) h.part[(int64_t)row * h.part_pitch + (h.v0 + col) / HN] = make_float2(most, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+            }
+            if constexpr (STEP == HeadStep::kProbs) {
+                const bool valid = row < it.rows_end;
+                const float lse = valid ? h.lse[row] : -INFINITY, g = valid ? h.g[row] : 0.f;
+                const bool none = lse == -INFINITY;                // no token, or nothing but logits of minus infinity
+                const int target = valid ? h.targets[row] - (int)(h.v0 + col) : -1;
+                const bool here = target >= 0 && target < HN;
+                // p - [the target], times -g
+#pragma unroll
+                for (int c = 0; c < HN; ++c) {
+                    float p = exp2_fast(fmaf(acc[c], h.scale, -lse) * 1.4426950408889634f);
+                    if (here && c == target) p -= 1.f;
+                    acc[c] = none ? 0.f : p * -g;
+                }
+                for (int t = 0; t < h.prob_terms; ++t) {
+#pragma unroll
+                    for (int c0 = 0; c0 < HN; c0 += 64) {
+                        if (col + c0 >= h.piece || warp_row >= h.slots) break;
+                        open_box();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float *f = &acc[c0 + q * 8 + e * 2];
+                                v[e] = two_bf16(f[0], f[1]);
+                                if (h.prob_terms > 1) {             // what the next term holds
+                                    f[0] -= __uint_as_float(v[e] << 16);
+                                    f[1] -= __uint_as_float(v[e] & 0xffff0000u);
+                                }
+                            }
+                            put16(q, make_uint4(v[0], v[1], v[2], v[3]));
+                        }
+                        close_box(false, col + c0, warp_row, t);
+                    }
+                }
+            }
+            if constexpr (STEP == HeadStep::kInputs) {
+#pragma unroll
+                for (int c0 = 0; c0 < HN; c0 += 32) {
+                    if (col + c0 >= h.cols || warp_row >= h.slots) break;
+                    open_box();
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        put16(q, make_uint4(__float_as_uint(acc[c0 + q * 4]), __float_as_uint(acc[c0 + q * 4 + 1]), __float_as_uint(acc[c0 + q * 4 + 2]), __float_as_uint(acc[c0 + q * 4 + 3])));
+                    close_box(h.accumulate, col + c0, warp_row, it.split);
+                }
+            }
+            if constexpr (STEP == HeadStep::kWeights) {
+                if (!args.manual_stores) {
+                    constexpr int kCols = 128 / sizeof(P), kPer = 16 / sizeof(P);
+#pragma unroll
+                    for (int c0 = 0; c0 < HN; c0 += kCols) {
+                        if (col + c0 >= h.cols || warp_row >= it.rows_end) break;
+                        open_box();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                v[e] = sizeof(P) == 4 ? __float_as_uint(acc[c0 + q * kPer + e]) : two_bf16(acc[c0 + q * kPer + e * 2], acc[c0 + q * kPer + (e * 2 + 1) % kPer]);
+                            put16(q, make_uint4(v[0], v[1], v[2], v[3]));
+                        }
+                        close_box(false, col + c0, (int)h.v0 + warp_row, it.group);
+                    }
+                } else {                                            // rows of any alignment, 32 columns of a row at a time
+                    float *turned = reinterpret_cast<float *>(box);
+                    const int rows = min(32, it.rows_end - warp_row);
+                    P *to = static_cast<P *>(h.dw) + it.group * h.lddw + (h.v0 + warp_row) * h.cols + col + lane;
+#pragma unroll
+                    for (int c0 = 0; c0 < HN; c0 += 32) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) turned[lane * 33 + k] = acc[c0 + k];
+                        __syncwarp();
+                        if (col + c0 + lane < h.cols)
+#pragma unroll 4
+                            for (int r = 0; r < rows; ++r) put(to + r * h.cols + c0, turned[r * 33 + lane]);
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+        if (lane == 0) boxes_wait_all();
+    }
+
+    // ---------------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1 && rank == 0 && abort_state[0]) {                 // instructions may still be running
+        if (elect_one()) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&drain_bar)) : "memory");
+        __syncwarp();
+        for (uint32_t i = 0; i < kSpinLimit; ++i) {
+            if (mbar_try_wait(smem_u32(&drain_bar), 0)) break;
+            __nanosleep(64);
+        }
+        __syncwarp();
+    }
+    if (tid == 0 && abort_state[0]) {
+        // copies still in flight must land before the block exits
+        for (int s = 0; s < S::kStages; ++s)
+            if (issued[s] > 0)
+                for (uint32_t i = 0; i < kSpinLimit; ++i) {
+                    if (mbar_try_wait(full(s), (uint32_t)(issued[s] - 1) & 1)) break;
+                    __nanosleep(64);
+                }
+        atomicAdd(&g_given_up, 1u);
+    }
+    __syncthreads();
+    cluster_barrier();                        // the other block's instructions, arrivals and reads have ended too
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * N) : "memory");
+}
+
+uint32_t spin_limit = kSpinLimit;
+
+bool encode(CUtensorMap *map, CUtensorMapDataType type, int size, const void *data, int64_t cols, int64_t rows, int64_t planes, int64_t row, int64_t plane, int box_cols,
+            int box_rows) {
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)row * size, (cuuint64_t)plane * size};
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
+    return enc(map, type, 3, const_cast<void *>(data), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool encode(CUtensorMap *map, const Operand &o, int box_cols, int box_rows) {
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, o.data, o.cols, o.rows, o.planes, o.row, o.plane, box_cols, box_rows);
+}
+
+template <HeadStep STEP, int N, typename P>
+cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const KernelArgs &k, int64_t items, cudaStream_t s) {
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return e;
+    static PerDeviceOnce once;
+    auto *kernel = head_tc_kernel<STEP, N, P>;
+    if (once.need(device)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<N>::kSmem);
+        if (e != cudaSuccess) return e;
+        once.mark(device);
+    }
+    const int64_t most = sms / 2, rounds = (items + most - 1) / most, pairs = (items + rounds - 1) / rounds;       // equal shares
+    return launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), Shape<N>::kSmem, s, true, a, b, out, k);
+}
+
+}  // namespace
+
+cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s) {
+    constexpr int N = 256, HN = N / 2;
+    KernelArgs k = {};
+    k.h = h;
+    const bool weights = h.step == HeadStep::kWeights, inputs = h.step == HeadStep::kInputs;
+    k.row_tiles = (int)(((weights ? h.piece : h.group_slots) + kPairRows - 1) / kPairRows);
+    k.col_tiles = (int)(((weights || inputs ? h.cols : h.piece) + N - 1) / N);
+    k.drain = 8;
+    k.drain_small = 64;
+    k.spin_limit = spin_limit;
+    const int64_t items = (int64_t)k.row_tiles * k.col_tiles * h.groups * (inputs ? h.splits : 1);
+    if (items == 0) return cudaSuccess;
+    CUtensorMap a, b, out = {};
+    if (!encode(&a, h.a, 64, weights ? kK : kHalfRows) || !encode(&b, h.b, 64, weights || inputs ? kK : HN)) return cudaErrorInvalidValue;
+    switch (h.step) {
+        case HeadStep::kSums:
+            return launch<HeadStep::kSums, N, float>(a, b, out, k, items, s);
+        case HeadStep::kProbs:
+            if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, h.probs, h.piece, h.slots, h.prob_terms, h.prob_pitch, h.slots * h.prob_pitch, 64, 32)) return cudaErrorInvalidValue;
+            return launch<HeadStep::kProbs, N, float>(a, b, out, k, items, s);
+        case HeadStep::kInputs:
+            if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.parts, h.cols, h.slots, h.splits, h.parts_pitch, h.slots * h.parts_pitch, 32, 32)) return cudaErrorInvalidValue;
+            return launch<HeadStep::kInputs, N, float>(a, b, out, k, items, s);
+        case HeadStep::kWeights: break;
+    }
+    const bool bf16 = h.param_type == ZENO_BF16;
+    const int size = bf16 ? 2 : 4;
+    const int64_t plane = h.groups > 1 ? h.lddw : h.cols, limit = (int64_t)1 << 40;
+    k.manual_stores = !(reinterpret_cast<uintptr_t>(h.dw) % 16 == 0 && h.cols * size % 16 == 0 && plane * size % 16 == 0 && plane * size < limit &&
+                        encode(&out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, size, h.dw, h.cols, h.vocab, h.groups, h.cols, plane, 128 / size, 32));
+    return bf16 ? launch<HeadStep::kWeights, N, __nv_bfloat16>(a, b, out, k, items, s) : launch<HeadStep::kWeights, N, float>(a, b, out, k, items, s);
+}
+
+void set_head_wait_limit(uint32_t polls) { spin_limit = polls; }
+
+cudaError_t head_given_up(unsigned *count, cudaStream_t s) {
+    void *at = nullptr;
+    const cudaError_t e = cudaGetSymbolAddress(&at, g_given_up);
+    return e == cudaSuccess ? cudaMemcpyAsync(count, at, sizeof(*count), cudaMemcpyDeviceToHost, s) : e;
+}
+
+}  // namespace zeno

@@ -10,7 +10,7 @@ using zeno::Rows;
 
 namespace {
 
-constexpr int64_t kMaxRows = 0x7fffffff, kMaxCols = (int64_t)1 << 30, kMaxWeights = (int64_t)1 << 20, kMaxStride = (int64_t)1 << 44;
+constexpr int64_t kMaxRows = 0x7fffffff, kMaxCols = (int64_t)1 << 30, kMaxWeights = (int64_t)1 << 20, kMaxStride = (int64_t)1 << 44, kMaxVocab = (int64_t)1 << 24;
 constexpr int kMaxGroups = 65535;
 
 bool type_ok(int32_t type) { return type == ZENO_F32 || type == ZENO_BF16; }
@@ -195,6 +195,138 @@ zeno_status zeno_token_gradient(int32_t device, int32_t type, const zeno_rows *l
     if (!targets || !lse || !g_logprob || (g_entropy && !entropy)) return ZENO_ERR_INVALID_ARG;
     zeno::TokenGradArgs a = {rows_of(logits, n), rows_of(grad, n), m, n, vocab, targets, lse, entropy, g_logprob, g_entropy};
     return on_device(device, [&] { return zeno::launch_token_gradient(type, a, static_cast<cudaStream_t>(stream)); });
+}
+
+// Rows of a table or of output weights, one after the other: a group's begin `ld` entries after the previous group's (0: one matrix for all of them).
+static zeno_status check_table(const void *w, int64_t ld, int size, int32_t m, int64_t vocab, int64_t cols, bool shared) {
+    if (!w || !placed(w, size)) return ZENO_ERR_INVALID_ARG;
+    if (m > 1 && !(shared && ld == 0) && ld < vocab * cols) return ZENO_ERR_INVALID_ARG;
+    return ZENO_OK;
+}
+
+static zeno_status check_vocab(int32_t m, int64_t n, int64_t vocab, int64_t cols) {
+    if (vocab < 1) return ZENO_ERR_INVALID_ARG;
+    const zeno_status st = check_sizes(m, n, cols);
+    if (st != ZENO_OK) return st;
+    return vocab > kMaxVocab || cols > kMaxWeights ? ZENO_ERR_UNSUPPORTED : ZENO_OK;
+}
+
+zeno_status zeno_embed(int32_t device, int32_t type, int32_t param_type, const int32_t *tokens, int32_t m, int64_t n, int64_t vocab, int64_t cols,
+                       const void *table, int64_t ldt, float scale, const zeno_rows *y, void *stream) {
+    Range range("zeno_embed");
+    if (!type_ok(type) || !type_ok(param_type) || !isfinite(scale)) return ZENO_ERR_INVALID_ARG;
+    zeno_status st = check_vocab(m, n, vocab, cols);
+    if (st == ZENO_OK) st = check_table(table, ldt, size_of(param_type), m, vocab, cols, true);
+    if (st != ZENO_OK) return st;
+    if (!rows_ok(y, size_of(type), m, n, cols, false) || !placed(tokens, 4)) return ZENO_ERR_INVALID_ARG;
+    if (m == 0 || n == 0) return ZENO_OK;
+    if (!tokens) return ZENO_ERR_INVALID_ARG;
+    zeno::EmbedArgs a = {tokens, m, n, vocab, cols, table, m > 1 ? ldt : 0, scale, rows_of(y, n)};
+    return on_device(device, [&] { return zeno::launch_embed(type, param_type, a, static_cast<cudaStream_t>(stream)); });
+}
+
+int64_t zeno_embed_gradient_workspace(int32_t m, int64_t n, int64_t vocab, int64_t cols) {
+    return check_vocab(m, n, vocab, cols) == ZENO_OK && m > 0 ? zeno::embed_gradient_workspace(m, n, vocab, cols) : 0;
+}
+
+zeno_status zeno_embed_gradient(int32_t device, int32_t type, int32_t param_type, const int32_t *tokens, const zeno_rows *dy, int32_t m, int64_t n,
+                                int64_t vocab, int64_t cols, float scale, int32_t add, void *dtable, int64_t ldt, void *workspace, int64_t workspace_bytes,
+                                void *stream) {
+    Range range("zeno_embed_gradient");
+    if (!type_ok(type) || !type_ok(param_type) || !isfinite(scale)) return ZENO_ERR_INVALID_ARG;
+    zeno_status st = check_vocab(m, n, vocab, cols);
+    if (st != ZENO_OK) return st;
+    if (!rows_ok(dy, size_of(type), m, n, cols) || !placed(tokens, 4) || (m > 0 && n > 0 && !tokens)) return ZENO_ERR_INVALID_ARG;
+    if (m == 0) return ZENO_OK;
+    st = check_table(dtable, ldt, size_of(param_type), m, vocab, cols, false);
+    if (st != ZENO_OK) return st;
+    if (!workspace_ok(workspace, workspace_bytes, zeno::embed_gradient_workspace(m, n, vocab, cols))) return ZENO_ERR_INVALID_ARG;
+    if (!zeno::embed_gradient_fits(m, vocab, cols)) return ZENO_ERR_UNSUPPORTED;
+    zeno::EmbedGradArgs a = {tokens, rows_of(dy, n), m, n, vocab, cols, scale, add != 0, dtable, ldt, workspace};
+    return on_device(device, [&] { return zeno::launch_embed_gradient(type, param_type, a, static_cast<cudaStream_t>(stream)); });
+}
+
+// The checks of the log probabilities from hidden states that the size of the workspace depends on; fills in what it goes by.
+static zeno_status check_head(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols, int64_t vocab, const void *w, int64_t ldw,
+                              zeno::HeadArgs *a) {
+    if (!type_ok(type) || !type_ok(param_type)) return ZENO_ERR_INVALID_ARG;
+    zeno_status st = check_vocab(m, n, vocab, cols);
+    if (st == ZENO_OK) st = check_table(w, ldw, size_of(param_type), m, vocab, cols, true);
+    if (st != ZENO_OK) return st;
+    if ((int64_t)m * ((n + 255) / 256 * 256) > kMaxRows - 256) return ZENO_ERR_UNSUPPORTED;
+    *a = {};
+    a->m = m;
+    a->n = n;
+    a->cols = cols;
+    a->vocab = vocab;
+    a->w = w;
+    a->ldw = m > 1 ? ldw : 0;
+    return ZENO_OK;
+}
+
+int64_t zeno_linear_logprobs_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols, int64_t vocab, const void *w, int64_t ldw) {
+    zeno::HeadArgs a;
+    return check_head(type, param_type, m, n, cols, vocab, w, ldw, &a) == ZENO_OK ? zeno::head_workspace(type, param_type, false, a) : 0;
+}
+
+zeno_status zeno_linear_logprobs(int32_t device, int32_t type, int32_t param_type, const zeno_rows *x, int32_t m, int64_t n, int64_t cols, int64_t vocab,
+                                 const void *w, int64_t ldw, const int32_t *targets, float scale, float *logprobs, float *lse, void *workspace,
+                                 int64_t workspace_bytes, void *stream) {
+    Range range("zeno_linear_logprobs");
+    if (!isfinite(scale)) return ZENO_ERR_INVALID_ARG;
+    zeno::HeadArgs a;
+    const zeno_status st = check_head(type, param_type, m, n, cols, vocab, w, ldw, &a);
+    if (st != ZENO_OK) return st;
+    if (!rows_ok(x, size_of(type), m, n, cols) || !placed(targets, 4) || !placed(logprobs, 4) || !placed(lse, 4)) return ZENO_ERR_INVALID_ARG;
+    if (m == 0 || n == 0) return ZENO_OK;
+    if (!targets || !workspace_ok(workspace, workspace_bytes, zeno::head_workspace(type, param_type, false, a))) return ZENO_ERR_INVALID_ARG;
+    a.x = rows_of(x, n);
+    a.targets = targets;
+    a.scale = scale;
+    a.logprobs = logprobs;
+    a.lse = lse;
+    a.workspace = workspace;
+    return on_device(device, [&] { return zeno::launch_head_logprobs(type, param_type, a, static_cast<cudaStream_t>(stream)); });
+}
+
+int64_t zeno_linear_logprobs_gradient_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols, int64_t vocab, const void *w,
+                                                int64_t ldw, int32_t want_dx) {
+    zeno::HeadArgs a;
+    if (check_head(type, param_type, m, n, cols, vocab, w, ldw, &a) != ZENO_OK) return 0;
+    a.dx.data = want_dx ? &a : nullptr;
+    return zeno::head_workspace(type, param_type, true, a);
+}
+
+zeno_status zeno_linear_logprobs_gradient(int32_t device, int32_t type, int32_t param_type, const zeno_rows *x, int32_t m, int64_t n, int64_t cols,
+                                          int64_t vocab, const void *w, int64_t ldw, const int32_t *targets, float scale, const float *lse,
+                                          const float *g_logprob, const zeno_rows *dx, void *dw, int64_t lddw, void *workspace, int64_t workspace_bytes,
+                                          void *stream) {
+    Range range("zeno_linear_logprobs_gradient");
+    if (!isfinite(scale)) return ZENO_ERR_INVALID_ARG;
+    zeno::HeadArgs a;
+    zeno_status st = check_head(type, param_type, m, n, cols, vocab, w, ldw, &a);
+    if (st != ZENO_OK) return st;
+    if (!rows_ok(x, size_of(type), m, n, cols) || (dx && !rows_ok(dx, size_of(type), m, n, cols, false))) return ZENO_ERR_INVALID_ARG;
+    if (!placed(targets, 4) || !placed(lse, 4) || !placed(g_logprob, 4)) return ZENO_ERR_INVALID_ARG;
+    if (m > 0 && n > 0 && (!targets || !lse || !g_logprob)) return ZENO_ERR_INVALID_ARG;
+    if (m == 0) return ZENO_OK;
+    if (dw) {
+        st = check_table(dw, lddw, size_of(param_type), m, vocab, cols, false);
+        if (st != ZENO_OK) return st;
+    }
+    a.dx.data = dx && n > 0 ? &a : nullptr;
+    if (!workspace_ok(workspace, workspace_bytes, zeno::head_workspace(type, param_type, true, a))) return ZENO_ERR_INVALID_ARG;
+    if (!dw && (!dx || n == 0)) return ZENO_OK;
+    a.x = rows_of(x, n);
+    a.dx = rows_of(dx, n);
+    a.targets = targets;
+    a.scale = scale;
+    a.lse_in = lse;
+    a.g = g_logprob;
+    a.dw = dw;
+    a.lddw = lddw;
+    a.workspace = workspace;
+    return on_device(device, [&] { return zeno::launch_head_gradient(type, param_type, a, static_cast<cudaStream_t>(stream)); });
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// Internal declarations of the language model operators (zeno_norm.cu, zeno_saved.cu, zeno_tokens.cu): arguments checked, the
+// Internal declarations of the language model operators (zeno_norm.cu, zeno_saved.cu, zeno_tokens.cu, zeno_embed.cu, zeno_head.cu): arguments checked, the
 // device current, at least one row unless noted.
 #pragma once
 
@@ -89,6 +89,8 @@ cudaError_t launch_dense_gradient(int type, int param_type, const DenseGradArgs 
 int64_t dense_tc_workspace(int type, const DenseGradArgs &a);
 cudaError_t launch_dense_tc(int type, int param_type, const DenseGradArgs &a, cudaStream_t s);
 void set_operator_wait_limit(uint32_t polls);
+void set_head_wait_limit(uint32_t polls);                       // zeno_head_tc.cu's waits, as part of the former
+cudaError_t head_given_up(unsigned *count, cudaStream_t s);     // its blocks whose waits gave up since the process began; copied on the stream
 cudaError_t read_operator_status(int device, cudaStream_t s, int *status);
 
 struct LogprobArgs {
@@ -112,6 +114,51 @@ struct TokenGradArgs {
     const float *lse, *entropy, *g_logprob, *g_entropy;
 };
 cudaError_t launch_token_gradient(int type, const TokenGradArgs &a, cudaStream_t s);
+
+struct EmbedArgs {
+    const int32_t *tokens;
+    int m;
+    int64_t n, vocab, cols;
+    const void *table;
+    int64_t ldt;                        // 0: one table for all groups
+    float scale;
+    Rows y;
+};
+cudaError_t launch_embed(int type, int param_type, const EmbedArgs &a, cudaStream_t s);
+
+struct EmbedGradArgs {
+    const int32_t *tokens;
+    Rows dy;
+    int m;
+    int64_t n, vocab, cols;
+    float scale;
+    int add;
+    void *dtable;
+    int64_t ldt;
+    void *workspace;
+};
+int64_t embed_gradient_workspace(int m, int64_t n, int64_t vocab, int64_t cols);
+bool embed_gradient_fits(int m, int64_t vocab, int64_t cols);           // one launch
+cudaError_t launch_embed_gradient(int type, int param_type, const EmbedGradArgs &a, cudaStream_t s);      // n may be 0
+
+struct HeadArgs {
+    Rows x;
+    int m;
+    int64_t n, cols, vocab;
+    const void *w;
+    int64_t ldw;                        // 0: one matrix for all groups
+    const int32_t *targets;
+    float scale;
+    float *logprobs, *lse;              // the log probabilities' call
+    const float *lse_in, *g;            // the gradient's
+    Rows dx;                            // data NULL: not wanted
+    void *dw;                           // or NULL
+    int64_t lddw;
+    void *workspace;
+};
+int64_t head_workspace(int type, int param_type, bool gradient, const HeadArgs &a);
+cudaError_t launch_head_logprobs(int type, int param_type, const HeadArgs &a, cudaStream_t s);
+cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cudaStream_t s);            // n may be 0
 
 #ifdef __CUDACC__
 

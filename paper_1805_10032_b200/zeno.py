@@ -33,6 +33,8 @@ EXPORTS = (
     "zeno_last_cuda_error", "zeno_last_wait_code", "zeno_status_string",
     "zeno_layer_norm", "zeno_layer_norm_gradient", "zeno_layer_norm_gradient_workspace", "zeno_pack_activations",
     "zeno_dense_gradient", "zeno_dense_gradient_workspace", "zeno_token_logprobs", "zeno_token_gradient",
+    "zeno_embed", "zeno_embed_gradient", "zeno_embed_gradient_workspace", "zeno_linear_logprobs", "zeno_linear_logprobs_workspace",
+    "zeno_linear_logprobs_gradient", "zeno_linear_logprobs_gradient_workspace",
     "zeno_operator_status", "zeno_debug_set_operator_wait_limit",
 )
 
@@ -145,6 +147,20 @@ def load_library() -> ctypes.CDLL:
     lib.zeno_token_logprobs.argtypes = [i32, i32, rows, i32, i64, i64, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.zeno_token_gradient.restype = i32
     lib.zeno_token_gradient.argtypes = [i32, i32, rows, i32, i64, i64, vp, vp, vp, vp, vp, rows, vp]
+    lib.zeno_embed.restype = i32
+    lib.zeno_embed.argtypes = [i32, i32, i32, vp, i32, i64, i64, i64, vp, i64, f32, rows, vp]
+    lib.zeno_embed_gradient.restype = i32
+    lib.zeno_embed_gradient.argtypes = [i32, i32, i32, vp, rows, i32, i64, i64, i64, f32, i32, vp, i64, vp, i64, vp]
+    lib.zeno_embed_gradient_workspace.restype = i64
+    lib.zeno_embed_gradient_workspace.argtypes = [i32, i64, i64, i64]
+    lib.zeno_linear_logprobs.restype = i32
+    lib.zeno_linear_logprobs.argtypes = [i32, i32, i32, rows, i32, i64, i64, i64, vp, i64, vp, f32, vp, vp, vp, i64, vp]
+    lib.zeno_linear_logprobs_workspace.restype = i64
+    lib.zeno_linear_logprobs_workspace.argtypes = [i32, i32, i32, i64, i64, i64, vp, i64]
+    lib.zeno_linear_logprobs_gradient.restype = i32
+    lib.zeno_linear_logprobs_gradient.argtypes = [i32, i32, i32, rows, i32, i64, i64, i64, vp, i64, vp, f32, vp, vp, rows, vp, i64, vp, i64, vp]
+    lib.zeno_linear_logprobs_gradient_workspace.restype = i64
+    lib.zeno_linear_logprobs_gradient_workspace.argtypes = [i32, i32, i32, i64, i64, i64, vp, i64, i32]
     _lib = lib
     return lib
 
@@ -483,6 +499,11 @@ class TokenLogprobs(NamedTuple):
     top_logprobs: Optional[torch.Tensor]
 
 
+class LinearLogprobs(NamedTuple):
+    logprobs: torch.Tensor
+    lse: torch.Tensor
+
+
 # Calls of a few tokens are over on the GPU in a few microseconds, so here too what the binding spends on a call shows: messages are built only for
 # a refusal, shapes and strides are read once, devices are compared by their index, empty_like and empty_strided (1.4 and 1.6 us) stand in for empty (2.4).
 _DEVICES = [torch.device("cuda", i) for i in range(64)]
@@ -757,6 +778,113 @@ def token_gradient(logits, targets, lse, g_logprob, entropy=None, g_entropy=None
     st = lib.zeno_token_gradient(dev, _type(logits, "logits"), _rows(logits, "logits"), m, n, vocab, targets.data_ptr(), lse.data_ptr(),
                                  _ptr(entropy), g_logprob.data_ptr(), _ptr(g_entropy), _rows(out, "out"), _current(dev, stream))
     return out if st == OK else _done(st, "zeno_token_gradient")
+
+
+def _matrix(w: torch.Tensor, m: int, rows: int, cols: int, name: str, shared: bool) -> int:
+    """Elements between the groups' matrices of contiguous rows: 0 if they share one."""
+    shape, strides = w.shape, w.stride()
+    if (shape == (rows, cols) and (shared or m == 1)) or shape == (m, rows, cols):
+        if (cols == 1 or strides[-1] == 1) and (rows == 1 or strides[-2] == cols):
+            return strides[0] if m > 1 and len(shape) == 3 else 0
+    _refuse(f"{name}: [{m}, {rows}, {cols}]{f' or [{rows}, {cols}]' if shared or m == 1 else ''}, contiguous for every group, is needed")
+
+
+def _group_sizes(tokens: torch.Tensor):
+    shape = tokens.shape
+    if len(shape) == 2:
+        return shape
+    if len(shape) != 1:
+        _refuse(f"tokens: [m, n] or [n] is needed, not {tuple(shape)}")
+    return 1, shape[0]
+
+
+def embed(tokens, table, scale=1.0, dtype=None, out=None, stream=None):
+    """zeno_embed: scale * table[tokens], [m, n, columns] of tokens [m, n] or [n, columns] of [n] (int32; one outside the vocabulary: zeros).  table:
+    [vocab, columns], or [m, vocab, columns] where every model has its own, for instance P[:, at:at + vocab * columns].unflatten(1, (vocab,
+    columns)).  The result's type is out's, dtype, or the table's."""
+    lib = load_library()
+    m, n = _group_sizes(tokens)
+    vocab, cols = table.shape[-2:]
+    dev = _device(tokens, table, out)
+    _per_token(tokens, tokens.shape, torch.int32, "tokens")
+    ldt = _matrix(table, m, vocab, cols, "table", True)
+    shape = (*tokens.shape, cols)
+    if out is None:
+        out = _empty(stream, dev, shape, dtype or table.dtype)
+    elif out.shape != shape or (dtype is not None and out.dtype != dtype):
+        _refuse(f"out: {dtype or out.dtype} {shape} is needed")
+    st = lib.zeno_embed(dev, _type(out, "out"), _type(table, "table"), tokens.data_ptr(), m, n, vocab, cols, table.data_ptr(), ldt, scale, _rows(out, "out"),
+                        _current(dev, stream))
+    return out if st == OK else _done(st, "zeno_embed")
+
+
+def embed_gradient(tokens, dy, dtable, scale=1.0, add=False, stream=None):
+    """zeno_embed_gradient: writes dtable ([m, vocab, columns], or without m; a slice of V as in embed) from dy, the gradient at embed's result; with
+    add, adds to it (tied weights, after linear_logprobs_gradient)."""
+    lib = load_library()
+    m, n = _group_sizes(tokens)
+    vocab, cols = dtable.shape[-2:]
+    dev = _device(tokens, dy, dtable)
+    _per_token(tokens, dy.shape[:-1], torch.int32, "tokens")
+    if dy.shape[-1] != cols:
+        _refuse(f"dy: rows of {cols} are needed, not {dy.shape[-1]}")
+    ldt = _matrix(dtable, m, vocab, cols, "dtable", False)
+    nbytes = lib.zeno_embed_gradient_workspace(m, n, vocab, cols)
+    ws = _empty(stream, dev, (nbytes,), torch.uint8) if nbytes else None
+    st = lib.zeno_embed_gradient(dev, _type(dy, "dy"), _type(dtable, "dtable"), tokens.data_ptr(), _rows(dy, "dy"), m, n, vocab, cols, scale, add,
+                                 dtable.data_ptr(), ldt, _ptr(ws), nbytes, _current(dev, stream))
+    return dtable if st == OK else _done(st, "zeno_embed_gradient")
+
+
+def linear_logprobs(x, weight, targets, scale=1.0, stream=None) -> LinearLogprobs:
+    """zeno_linear_logprobs: (logprobs, lse) of the targets (int32; one outside the vocabulary: 0 for both) under the logits scale * x @ weight.T, which
+    are not kept.  x: [m, n, columns] or [n, columns]; weight: [vocab, columns], or [m, vocab, columns] where every model has its own."""
+    lib = load_library()
+    shape = x.shape
+    m, n, cols = _sizes(shape)
+    vocab = weight.shape[-2]
+    dev = _device(x, weight, targets)
+    _per_token(targets, shape[:-1], torch.int32, "targets")
+    ldw = _matrix(weight, m, vocab, cols, "weight", True)
+    kind, wkind, w = _type(x, "x"), _type(weight, "weight"), weight.data_ptr()
+    logprobs = _empty(stream, dev, shape[:-1], torch.float32)
+    lse = _empty_like(stream, logprobs)
+    nbytes = lib.zeno_linear_logprobs_workspace(kind, wkind, m, n, cols, vocab, w, ldw)
+    ws = _empty(stream, dev, (nbytes,), torch.uint8) if nbytes else None
+    st = lib.zeno_linear_logprobs(dev, kind, wkind, _rows(x, "x"), m, n, cols, vocab, w, ldw, targets.data_ptr(), scale, logprobs.data_ptr(), lse.data_ptr(),
+                                  _ptr(ws), nbytes, _current(dev, stream))
+    return LinearLogprobs(logprobs, lse) if st == OK else _done(st, "zeno_linear_logprobs")
+
+
+def linear_logprobs_gradient(x, weight, targets, lse, g_logprob, dweight=None, dx=None, want_dx=True, scale=1.0, stream=None):
+    """zeno_linear_logprobs_gradient: from the gradient at linear_logprobs's logprobs, writes dweight ([m, vocab, columns], or without m; a slice of V
+    as in embed; every group its own, also where the weight is shared) and returns dx (None if not wanted)."""
+    lib = load_library()
+    shape = x.shape
+    lead = shape[:-1]
+    m, n, cols = _sizes(shape)
+    vocab = weight.shape[-2]
+    dev = _device(x, weight, targets, lse, g_logprob, dweight, dx)
+    _per_token(targets, lead, torch.int32, "targets")
+    _per_token(lse, lead, torch.float32, "lse")
+    _per_token(g_logprob, lead, torch.float32, "g_logprob")
+    ldw = _matrix(weight, m, vocab, cols, "weight", True)
+    lddw = 0
+    if dweight is not None:
+        if dweight.dtype != weight.dtype:
+            _refuse(f"dweight: {weight.dtype} is needed")
+        lddw = _matrix(dweight, m, vocab, cols, "dweight", False)
+    if dx is not None:
+        _alike(dx, x, "dx")
+    elif want_dx:
+        dx = _empty_like(stream, x)
+    kind, wkind, w = _type(x, "x"), _type(weight, "weight"), weight.data_ptr()
+    nbytes = lib.zeno_linear_logprobs_gradient_workspace(kind, wkind, m, n, cols, vocab, w, ldw, dx is not None)
+    ws = _empty(stream, dev, (nbytes,), torch.uint8) if nbytes else None
+    st = lib.zeno_linear_logprobs_gradient(dev, kind, wkind, _rows(x, "x"), m, n, cols, vocab, w, ldw, targets.data_ptr(), scale, lse.data_ptr(),
+                                           g_logprob.data_ptr(), None if dx is None else _rows(dx, "dx"), _ptr(dweight), lddw, _ptr(ws), nbytes,
+                                           _current(dev, stream))
+    return dx if st == OK else _done(st, "zeno_linear_logprobs_gradient")
 
 
 def check_operator_status(device: int = 0, stream=None):
