@@ -241,7 +241,7 @@ zeno_status zeno_embed_gradient(int32_t device, int32_t type, int32_t param_type
     st = check_table(dtable, ldt, size_of(param_type), m, vocab, cols, false);
     if (st != ZENO_OK) return st;
     if (!workspace_ok(workspace, workspace_bytes, zeno::embed_gradient_workspace(m, n, vocab, cols))) return ZENO_ERR_INVALID_ARG;
-    if (!zeno::embed_gradient_fits(m, vocab, cols)) return ZENO_ERR_UNSUPPORTED;
+    if (!zeno::embed_gradient_fits(n, vocab, cols)) return ZENO_ERR_UNSUPPORTED;
     zeno::EmbedGradArgs a = {tokens, rows_of(dy, n), m, n, vocab, cols, scale, add != 0, dtable, ldt, workspace};
     return on_device(device, [&] { return zeno::launch_embed_gradient(type, param_type, a, static_cast<cudaStream_t>(stream)); });
 }

@@ -138,7 +138,7 @@ struct EmbedGradArgs {
     void *workspace;
 };
 int64_t embed_gradient_workspace(int m, int64_t n, int64_t vocab, int64_t cols);
-bool embed_gradient_fits(int m, int64_t vocab, int64_t cols);           // one launch
+bool embed_gradient_fits(int64_t n, int64_t vocab, int64_t cols);
 cudaError_t launch_embed_gradient(int type, int param_type, const EmbedGradArgs &a, cudaStream_t s);      // n may be 0
 
 struct HeadArgs {
