@@ -16,9 +16,9 @@ constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.
 struct Plan {
-    int x_terms, w_terms, w_packed, prob_terms, groups, splits, pieces;
+    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, few, few_blocks;
     int64_t group_slots, slots, pitch, piece, parts_pitch, part_pitch;
-    int64_t counts, begin, end, total, list, rank, target, lse, g, target_logit, x, w, part, probs, parts, bytes;
+    int64_t counts, begin, end, total, list, rank, target, lse, g, target_logit, x, w, part, probs, parts, extra, bytes;
 };
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -28,9 +28,24 @@ bool mappable(const void *w, int64_t ldw, int64_t groups, int64_t cols) {
     return reinterpret_cast<uintptr_t>(w) % 16 == 0 && cols % 8 == 0 && (groups <= 1 || (ldw % 8 == 0 && ldw < limit));
 }
 
+// A group of at most so many tokens takes no tensor cores: the weights go by once whatever the number of tokens.
+constexpr int kFew = 8;
+constexpr int64_t kFewCols = 8192, kFewBytes = 128 << 10;
+
 Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     Plan p = {};
     p.groups = a.ldw != 0 && a.m > 1 ? a.m : 1;
+    const int64_t group_rows = p.groups > 1 ? a.n : a.m * a.n;
+    p.few = !gradient && group_rows <= kFew && a.cols <= kFewCols && (group_rows > 4 ? 8 : group_rows > 2 ? 4 : group_rows) * up(a.cols, 1024) * 4 <= kFewBytes;
+    if (p.few) {
+        const int64_t most = (a.vocab + 31) / 32, blocks = 2 * 2 * kHeadPairs / p.groups;       // two blocks an SM
+        p.few_blocks = (int)(blocks < 1 ? 1 : blocks < most ? blocks : most);
+        p.part_pitch = p.few_blocks;
+        p.target_logit = 0;
+        p.part = up(a.m * a.n * 4, 256);
+        p.bytes = p.part + a.m * a.n * p.part_pitch * 8;
+        return p;
+    }
     p.x_terms = type == ZENO_F32 ? 3 : 1;
     p.w_terms = param_type == ZENO_F32 ? 3 : 1;
     p.w_packed = p.w_terms > 1 || !mappable(a.w, a.ldw, p.groups, a.cols);
@@ -49,15 +64,14 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.pieces = (int)((a.vocab + most - 1) / most);
     p.piece = up((a.vocab + p.pieces - 1) / p.pieces, 256);
     p.pieces = (int)((a.vocab + p.piece - 1) / p.piece);
-    p.splits = 1;
-    if (gradient) {
-        // few tiles of dx: the words are cut, and the parts joined
-        const int64_t tiles = up(p.group_slots, 256) / 256 * (up(a.cols, 256) / 256) * p.groups, stages = p.piece / 64;
-        int64_t splits = 74 / (tiles > 0 ? tiles : 1);
-        if (splits > stages / 8) splits = stages / 8;
-        p.splits = splits < 1 ? 1 : (int)splits;
-    }
-    p.part_pitch = up(a.vocab, 256) / 128;
+    // a tile of 128 columns where there are fewer of 256 than pairs of SMs
+    const int64_t row_tiles = up(p.group_slots, kHeadRows) / kHeadRows * p.groups;
+    auto tile_for = [&](int64_t cols) { return row_tiles * (up(cols, 256) / 256) < kHeadPairs ? 128 : 256; };
+    p.sum_cols = tile_for(p.piece);
+    p.tile_cols = 256;                                                // its tiles are cut along the words instead
+    p.most_splits = (int)(p.piece / 64 / 8);                          // parts of eight stages and more
+    if (p.most_splits < 1) p.most_splits = 1;
+    p.part_pitch = up(a.vocab, 256) / (p.sum_cols / 2);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t from = at;
@@ -78,7 +92,8 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.w = take(per_word * p.piece);
     p.part = take(gradient ? 0 : p.slots * p.part_pitch * 8);
     p.probs = take(p.piece * per_prob);
-    p.parts = take(gradient && a.dx.data ? p.splits * p.slots * p.parts_pitch * 4 : 0);
+    p.parts = take(gradient && a.dx.data ? p.slots * p.parts_pitch * 4 : 0);
+    p.extra = take(gradient && a.dx.data ? (int64_t)kHeadPairs * kHeadRows * p.tile_cols * 4 : 0);
     p.bytes = at;
     return p;
 }
@@ -138,10 +153,10 @@ __device__ __forceinline__ void put_terms(float (&f)[8], __nv_bfloat16 *to, int6
     }
 }
 
-// A warp rewrites a row of cols entries (NULL: zeros), eight to a lane.
+// Some threads rewrite a row of cols entries (NULL: zeros), eight to each.
 template <typename T, int TERMS>
-__device__ __forceinline__ void row_terms(const T *from, int64_t cols, int64_t pitch, __nv_bfloat16 *to, int64_t plane, bool vectors) {
-    for (int64_t c = (threadIdx.x & 31) * 8; c < pitch; c += 256) {
+__device__ __forceinline__ void row_terms(const T *from, int64_t cols, int64_t pitch, __nv_bfloat16 *to, int64_t plane, bool vectors, int thread, int threads) {
+    for (int64_t c = thread * 8; c < pitch; c += threads * 8) {
         float f[8] = {};
         if (from && vectors) {
             alignas(16) T e[8];
@@ -149,19 +164,34 @@ __device__ __forceinline__ void row_terms(const T *from, int64_t cols, int64_t p
             for (int k = 0; k < (int)sizeof(e) / 16; ++k) reinterpret_cast<uint4 *>(e)[k] = reinterpret_cast<const uint4 *>(from + c)[k];
 #pragma unroll
             for (int k = 0; k < 8; ++k) f[k] = value_of(e + k);
-        } else if (from) {
+        } else if (from && c < cols) {                                 // by aligned loads and shifts, of words that hold an entry of the row
+            constexpr int kLoads = 8 * sizeof(T) / 16;
+            const uintptr_t at = reinterpret_cast<uintptr_t>(from + c), end = reinterpret_cast<uintptr_t>(from + cols);
+            const uint4 *words = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
+            uint4 q[kLoads + 1];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (c + k < cols) f[k] = value_of(from + c + k);
+            for (int k = 0; k <= kLoads; ++k) q[k] = reinterpret_cast<uintptr_t>(words + k) < end ? words[k] : make_uint4(0, 0, 0, 0);
+            alignas(16) T e[8];
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) reinterpret_cast<uint4 *>(e)[k] = shifted<sizeof(T)>(q[k], q[k + 1], (unsigned)(at & 15));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = c + k < cols ? value_of(e + k) : 0.f;
         }
         put_terms<TERMS>(f, to + c, plane);
     }
 }
 
+// Threads for a row: a power of two, a warp at least and a block at most.
+int threads_log2(int64_t pitch) {
+    int log2 = 5;
+    while (log2 < 8 && (8 << log2) < pitch) ++log2;
+    return log2;
+}
+
 struct SlotsArgs {
     HeadArgs a;
     Plan p;
-    int vectors;
+    int vectors, threads_log2;
 };
 
 template <typename V>
@@ -169,7 +199,7 @@ __host__ __device__ __forceinline__ V *at(const HeadArgs &a, int64_t offset) {
     return reinterpret_cast<V *>(static_cast<uint8_t *>(a.workspace) + offset);
 }
 
-// A warp per slot: blockIdx.y is the worker.
+// blockIdx.y is the worker.
 template <typename T, int TERMS>
 __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
     __shared__ int scratch[8];
@@ -200,10 +230,11 @@ __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
             at<int>(a, p.total)[1] = begin + filled;
         }
     }
-    for (int k = blockIdx.x * 8 + warp; k < filled; k += gridDim.x * 8) {
+    const int threads = 1 << args.threads_log2, thread = threadIdx.x & (threads - 1), rows_of_block = 256 >> args.threads_log2;
+    for (int k = blockIdx.x * rows_of_block + (threadIdx.x >> args.threads_log2); k < filled; k += gridDim.x * rows_of_block) {
         const int token = k < count ? at<int>(a, p.list)[worker * a.n + k] : -1;
         const int64_t slot = begin + k, row = worker * a.n + token;
-        if (lane == 0) {
+        if (thread == 0) {
             at<int>(a, p.target)[slot] = token >= 0 ? a.targets[row] : -1;
             if (a.g) {
                 at<float>(a, p.lse)[slot] = token >= 0 ? a.lse_in[row] : -INFINITY;
@@ -211,19 +242,148 @@ __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
             }
         }
         const T *from = token >= 0 ? static_cast<const T *>(a.x.data) + worker * a.x.group + token * a.x.row : nullptr;
-        row_terms<T, TERMS>(from, a.cols, p.pitch, at<__nv_bfloat16>(a, p.x) + slot * p.pitch, p.slots * p.pitch, args.vectors);
+        row_terms<T, TERMS>(from, a.cols, p.pitch, at<__nv_bfloat16>(a, p.x) + slot * p.pitch, p.slots * p.pitch, args.vectors, thread, threads);
     }
 }
 
-// Words v0 .. v0 + words - 1 of every group's weights: [group][term][piece][pitch].  A warp per word.
+// Words v0 .. v0 + words - 1 of every group's weights: [group][term][piece][pitch].  The first piece's are rewritten beside the tokens' kernels, which
+// touch none of them and started behind all that came before this call; the end is waited for all the same, for the sake of the kernel that comes next.
 template <typename T, int TERMS>
 __global__ void __launch_bounds__(256) head_words_kernel(const T *w, int64_t ldw, int64_t cols, int64_t pitch, int64_t v0, int words, int64_t piece, int64_t total,
-                                                         __nv_bfloat16 *out, int vectors) {
+                                                         __nv_bfloat16 *out, int vectors, int threads_log2, int beside) {
+    if (!beside) pdl_wait();
+    pdl_launch_dependents();
+    const int threads = 1 << threads_log2, rows_of_block = 256 >> threads_log2;
+    for (int64_t q = (int64_t)blockIdx.x * rows_of_block + (threadIdx.x >> threads_log2); q < total; q += (int64_t)gridDim.x * rows_of_block) {
+        const int64_t group = q / words, v = q - group * words;
+        row_terms<T, TERMS>(w + group * ldw + (v0 + v) * cols, cols, pitch, out + (group * TERMS * piece + v) * pitch, piece * pitch, vectors, threadIdx.x & (threads - 1), threads);
+    }
+    if (beside) pdl_wait();
+}
+
+// ---- few tokens
+
+// Log-sum-exp in parts: the largest so far and the sum of exponentials beside it.
+__device__ __forceinline__ void add_part(float2 &to, float top, float sum) {
+    const float most = fmaxf(to.x, top), beside = most == -INFINITY ? 0.f : most;
+    to.y = to.y * expf(to.x - beside) + sum * expf(top - beside);          // exp(-inf) of a part that has nothing yet; NaN stays in the sums
+    to.x = most;
+}
+
+// Every warp takes WORDS words at a time, its lanes eight columns of 256 (neighbours where all rows are aligned, else every 32nd), and asks for the next
+// AHEAD times 256 columns before it multiplies the last ones; hidden states are kept in shared memory in binary32.  Bound by the weights' way from memory.
+template <typename T, typename P, int R, bool VECTORS>
+__global__ void __launch_bounds__(256, 2) head_few_kernel(const HeadArgs a, const Plan p) {
+    constexpr int WORDS = 2, AHEAD = VECTORS && sizeof(P) == 2 && R <= 2 ? 4 : 2, kRegs = VECTORS ? (int)sizeof(P) * 2 : 8;
+    extern __shared__ __align__(16) float held[];            // [row][column]; of eight neighbours the latter four in a second half (VECTORS)
+    __shared__ float2 of_warp[8][R];
     pdl_wait();
     pdl_launch_dependents();
-    for (int64_t q = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); q < total; q += (int64_t)gridDim.x * 8) {
-        const int64_t group = q / words, v = q - group * words;
-        row_terms<T, TERMS>(w + group * ldw + (v0 + v) * cols, cols, pitch, out + (group * TERMS * piece + v) * pitch, piece * pitch, vectors);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t group_rows = p.groups > 1 ? a.n : a.m * a.n, row0 = blockIdx.y * group_rows;
+    const int cols = (int)a.cols, padded = (cols + 256 * AHEAD - 1) / (256 * AHEAD) * (256 * AHEAD);
+    const P *w = static_cast<const P *>(a.w) + blockIdx.y * a.ldw;
+    const int64_t step = (int64_t)gridDim.x * 8 * WORDS;
+    uint32_t next[AHEAD][WORDS][kRegs];
+    auto ask = [&](int64_t v0, int c0) {
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h)
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) {
+                const P *from = w + (v0 + k) * cols + c0 + h * 256;
+                const int left = v0 + k < a.vocab ? cols - c0 - h * 256 : 0;
+                if constexpr (VECTORS) {
+#pragma unroll
+                    for (int i = 0; i < kRegs / 4; ++i) {
+                        const uint4 q = lane * 8 < left ? __ldcs(reinterpret_cast<const uint4 *>(from + lane * 8) + i) : make_uint4(0, 0, 0, 0);
+                        next[h][k][4 * i] = q.x, next[h][k][4 * i + 1] = q.y, next[h][k][4 * i + 2] = q.z, next[h][k][4 * i + 3] = q.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) next[h][k][i] = lane + 32 * i < left ? __float_as_uint(value_of(from + lane + 32 * i)) : 0u;
+                }
+            }
+    };
+    int64_t v0 = ((int64_t)blockIdx.x * 8 + warp) * WORDS;
+    ask(v0, 0);
+    int target = -1;                                         // of the lane's row
+    if (lane < group_rows) target = a.targets[row0 + lane];
+    if ((uint32_t)target >= (uint64_t)a.vocab) target = -1;
+    const unsigned given = __ballot_sync(0xffffffffu, target >= 0);
+    for (int r = 0; r < R; ++r)
+        for (int c = threadIdx.x; c < padded; c += 256) {
+            float v = 0.f;
+            if (c < cols && (given >> r & 1)) {
+                const int64_t row = row0 + r, worker = row / a.n;
+                v = value_of(static_cast<const T *>(a.x.data) + worker * a.x.group + (row - worker * a.n) * a.x.row + c);
+            }
+            held[r * padded + (VECTORS ? (c & 4 ? padded / 2 : 0) + (c >> 3) * 4 + (c & 3) : c)] = v;
+        }
+    __syncthreads();
+    float2 mine = make_float2(-INFINITY, 0.f);               // of the lane's row
+    while (v0 < a.vocab) {
+        Two sum[2][WORDS][R] = {};                           // two chains of additions each
+        const int64_t following = v0 + step;
+        for (int c0 = 0; c0 < padded; c0 += 256 * AHEAD) {
+            uint32_t now[AHEAD][WORDS][kRegs];
+#pragma unroll
+            for (int h = 0; h < AHEAD; ++h)
+#pragma unroll
+                for (int k = 0; k < WORDS; ++k)
+#pragma unroll
+                    for (int i = 0; i < kRegs; ++i) now[h][k][i] = next[h][k][i];
+            const bool same = c0 + 256 * AHEAD < padded;
+            ask(same ? v0 : following, same ? c0 + 256 * AHEAD : 0);
+#pragma unroll
+            for (int h = 0; h < AHEAD; ++h) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float *x = held + r * padded;
+                    const int c = c0 + h * 256;
+                    float f[8];
+                    if constexpr (VECTORS) {
+                        const float4 lo = *reinterpret_cast<const float4 *>(x + (c >> 1) + lane * 4), hi = *reinterpret_cast<const float4 *>(x + padded / 2 + (c >> 1) + lane * 4);
+                        f[0] = lo.x, f[1] = lo.y, f[2] = lo.z, f[3] = lo.w, f[4] = hi.x, f[5] = hi.y, f[6] = hi.z, f[7] = hi.w;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = x[c + lane + 32 * i];
+                    }
+#pragma unroll
+                    for (int k = 0; k < WORDS; ++k)
+#pragma unroll
+                        for (int i = 0; i < 8; i += 2) {
+                            const uint32_t *q = now[h][k];
+                            const Two e = kRegs == 8 ? Two{__uint_as_float(q[i % kRegs]), __uint_as_float(q[(i + 1) % kRegs])}
+                                                     : Two{__uint_as_float(q[i / 2] << 16), __uint_as_float(q[i / 2] & 0xffff0000u)};
+                            Two &to = sum[h & 1][k][r];
+                            to = fma2(e, Two{f[i], f[i + 1]}, to);
+                        }
+                }
+            }
+        }
+        const int words = (int)min((int64_t)WORDS, a.vocab - v0);
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) {
+            float z = 0.f;                                   // of the lane's row
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float s = warp_sum((sum[0][k][r].x + sum[0][k][r].y) + (sum[1][k][r].x + sum[1][k][r].y));
+                if (lane == r) z = s;
+            }
+            z *= a.scale;
+            if (lane < group_rows && k < words) {
+                if (v0 + k == target) at<float>(a, p.target_logit)[row0 + lane] = z;
+                add_part(mine, z, 1.f);
+            }
+        }
+        v0 = following;
+    }
+    if (lane < R) of_warp[warp][lane] = mine;
+    __syncthreads();
+    if (threadIdx.x < group_rows) {
+        mine = of_warp[0][threadIdx.x];
+        for (int k = 1; k < 8; ++k) add_part(mine, of_warp[k][threadIdx.x].x, of_warp[k][threadIdx.x].y);
+        at<float2>(a, p.part)[(row0 + threadIdx.x) * p.part_pitch + blockIdx.x] = mine;
     }
 }
 
@@ -235,10 +395,10 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a, const 
     const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
     if (row >= a.m * a.n) return;
-    const int rank = at<int>(a, p.rank)[row];
+    const int rank = p.few ? ((uint32_t)a.targets[row] < (uint64_t)a.vocab ? 0 : -1) : at<int>(a, p.rank)[row];
     float lse = 0.f, logprob = 0.f;
     if (rank >= 0) {
-        const int64_t slot = at<int>(a, p.begin)[row / a.n] + rank;
+        const int64_t slot = p.few ? row : at<int>(a, p.begin)[row / a.n] + rank;
         const float2 *part = at<float2>(a, p.part) + slot * p.part_pitch;
         float most = -INFINITY;
         for (int i = lane; i < parts; i += 32) most = fmaxf(most, part[i].x);
@@ -262,21 +422,31 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a, const 
     }
 }
 
-// dx: the parts' sums, four neighbouring entries a thread, rounded once; zero without a target.
+// dx, four neighbouring entries a thread, rounded once; zero without a target.  Tiles that were cut have further parts.
 template <typename T>
-__global__ void __launch_bounds__(256) head_inputs_kernel(const HeadArgs a, const Plan p, int vectors) {
+__global__ void __launch_bounds__(256) head_inputs_kernel(const HeadArgs a, const Plan p, uint32_t pairs, int vectors) {
     pdl_wait();
-    const int64_t per_row = p.parts_pitch / 4, total = (int64_t)a.m * a.n * per_row, plane = p.slots * p.parts_pitch;
+    const int64_t per_row = p.parts_pitch / 4, total = (int64_t)a.m * a.n * per_row;
+    const uint32_t bound = (uint32_t)((p.group_slots + kHeadRows - 1) / kHeadRows), used = (uint32_t)((at<int>(a, p.total)[1] + kHeadRows - 1) / kHeadRows);
+    const uint32_t row_tiles = p.groups > 1 ? bound : min(bound, used), col_tiles = (uint32_t)((a.cols + p.tile_cols - 1) / p.tile_cols);
+    const uint32_t tiles = row_tiles * col_tiles * p.groups, whole = tiles / pairs * pairs;
+    const int splits = head_splits(tiles, pairs, p.most_splits);
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
         const int64_t row = q / per_row, c = (q - row * per_row) * 4, worker = row / a.n;
         const int rank = at<int>(a, p.rank)[row];
         float s[4] = {};
         if (rank >= 0) {
-            const float *from = at<float>(a, p.parts) + (at<int>(a, p.begin)[worker] + rank) * p.parts_pitch + c;
-            for (int i = 0; i < p.splits; ++i) {
-                const float4 v = *reinterpret_cast<const float4 *>(from + i * plane);
-                s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
-            }
+            const int slot = at<int>(a, p.begin)[worker] + rank;
+            const float4 v = *reinterpret_cast<const float4 *>(at<float>(a, p.parts) + slot * p.parts_pitch + c);
+            s[0] = v.x, s[1] = v.y, s[2] = v.z, s[3] = v.w;
+            const int in_group = p.groups > 1 ? rank : slot, col = (int)(c / p.tile_cols);
+            const uint32_t tile = (p.groups > 1 ? (uint32_t)worker * row_tiles * col_tiles : 0) + head_tile_number(in_group / kHeadRows, col, row_tiles, col_tiles);
+            if (tile >= whole)
+                for (int i = 1; i < splits; ++i) {
+                    const int64_t item = (int64_t)(tile - whole) * splits + i;
+                    const float4 u = *reinterpret_cast<const float4 *>(at<float>(a, p.extra) + (item * kHeadRows + in_group % kHeadRows) * p.tile_cols + (c - col * p.tile_cols));
+                    s[0] += u.x, s[1] += u.y, s[2] += u.z, s[3] += u.w;
+                }
         }
         T *to = static_cast<T *>(a.dx.data) + worker * a.dx.group + (row - worker * a.n) * a.dx.row + c;
         alignas(16) T e[4];
@@ -319,8 +489,8 @@ cudaError_t fill_slots(int type, const HeadArgs &a, const Plan &p, cudaStream_t 
     cudaError_t e = launch_chained(head_order_kernel, dim3(a.m), dim3(kOrderThreads), 0, s, true, a.targets, a.n, a.vocab, at<int>(a, p.counts), at<int>(a, p.list), at<int>(a, p.rank));
     if (e != cudaSuccess) return e;
     const int elem = type == ZENO_F32 ? 4 : 2;
-    const SlotsArgs args = {a, p, a.cols % 8 == 0 && aligned_to(a.x, a.m, a.n, elem, 16)};
-    const int64_t blocks = up(a.n, kSlots) / 8;
+    const SlotsArgs args = {a, p, a.cols % 8 == 0 && aligned_to(a.x, a.m, a.n, elem, 16), threads_log2(p.pitch)};
+    const int64_t blocks = up(a.n, kSlots) / (256 >> args.threads_log2);
     const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048), a.m);
     return type == ZENO_F32 ? launch_chained(head_slots_kernel<float, 3>, grid, dim3(256), 0, s, true, args)
                             : launch_chained(head_slots_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, s, true, args);
@@ -339,10 +509,12 @@ cudaError_t piece_weights(int param_type, const HeadArgs &a, const Plan &p, int6
     const int64_t total = p.groups * words;
     const int vectors = a.cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.w) % 16 == 0 && (p.groups <= 1 || a.ldw * size % 16 == 0);
     auto *out = at<__nv_bfloat16>(a, p.w);
-    return param_type == ZENO_F32 ? launch_chained(head_words_kernel<float, 3>, grid_for((total + 7) / 8), dim3(256), 0, s, true, static_cast<const float *>(a.w), a.ldw, a.cols, p.pitch, v0,
-                                                   (int)words, p.piece, total, out, vectors)
-                                  : launch_chained(head_words_kernel<__nv_bfloat16, 1>, grid_for((total + 7) / 8), dim3(256), 0, s, true, static_cast<const __nv_bfloat16 *>(a.w), a.ldw, a.cols,
-                                                   p.pitch, v0, (int)words, p.piece, total, out, vectors);
+    const int log2 = threads_log2(p.pitch), rows_of_block = 256 >> log2;
+    const dim3 grid = grid_for((total + rows_of_block - 1) / rows_of_block);
+    return param_type == ZENO_F32 ? launch_chained(head_words_kernel<float, 3>, grid, dim3(256), 0, s, true, static_cast<const float *>(a.w), a.ldw, a.cols, p.pitch, v0,
+                                                   (int)words, p.piece, total, out, vectors, log2, (int)(v0 == 0))
+                                  : launch_chained(head_words_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, s, true, static_cast<const __nv_bfloat16 *>(a.w), a.ldw, a.cols,
+                                                   p.pitch, v0, (int)words, p.piece, total, out, vectors, log2, (int)(v0 == 0));
 }
 
 HeadTcArgs common(const HeadArgs &a, const Plan &p, HeadStep step) {
@@ -358,10 +530,34 @@ HeadTcArgs common(const HeadArgs &a, const Plan &p, HeadStep step) {
     h.b_terms = p.w_terms;
     h.scale = a.scale;
     h.targets = at<int>(a, p.target);
+    h.tile_cols = p.sum_cols;
     return h;
 }
 
 Operand slots_operand(const HeadArgs &a, const Plan &p) { return Operand{at<void>(a, p.x), a.cols, p.slots, p.pitch, p.slots * p.pitch, p.x_terms}; }
+
+template <typename T, typename P, int R, bool VECTORS>
+cudaError_t few(const HeadArgs &a, const Plan &p, cudaStream_t s) {
+    auto *kernel = head_few_kernel<T, P, R, VECTORS>;
+    static PerDeviceOnce once;
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess && once.need(device)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewBytes);
+        if (e == cudaSuccess) once.mark(device);
+    }
+    return e == cudaSuccess ? launch_chained(kernel, dim3(p.few_blocks, p.groups), dim3(256), (size_t)(R * up(a.cols, 1024) * 4), s, true, a, p) : e;
+}
+
+template <typename T, typename P>
+cudaError_t few_rows(const HeadArgs &a, const Plan &p, cudaStream_t s) {
+    const int64_t rows = p.groups > 1 ? a.n : a.m * a.n;
+    const bool vectors = a.cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.w) % 16 == 0 && (p.groups == 1 || a.ldw * sizeof(P) % 16 == 0);
+    if (rows <= 1) return vectors ? few<T, P, 1, true>(a, p, s) : few<T, P, 1, false>(a, p, s);
+    if (rows <= 2) return vectors ? few<T, P, 2, true>(a, p, s) : few<T, P, 2, false>(a, p, s);
+    if (rows <= 4) return vectors ? few<T, P, 4, true>(a, p, s) : few<T, P, 4, false>(a, p, s);
+    return vectors ? few<T, P, 8, true>(a, p, s) : few<T, P, 8, false>(a, p, s);
+}
 
 }  // namespace
 
@@ -369,6 +565,12 @@ int64_t head_workspace(int type, int param_type, bool gradient, const HeadArgs &
 
 cudaError_t launch_head_logprobs(int type, int param_type, const HeadArgs &a, cudaStream_t s) {
     const Plan p = plan_head(type, param_type, false, a);
+    if (p.few) {
+        const cudaError_t e = type == ZENO_F32 ? (param_type == ZENO_F32 ? few_rows<float, float>(a, p, s) : few_rows<float, __nv_bfloat16>(a, p, s))
+                                               : (param_type == ZENO_F32 ? few_rows<__nv_bfloat16, float>(a, p, s) : few_rows<__nv_bfloat16, __nv_bfloat16>(a, p, s));
+        if (e != cudaSuccess) return e;
+        return launch_chained(head_join_kernel, dim3((unsigned)((a.m * a.n + 7) / 8)), dim3(256), 0, s, true, a, p, p.few_blocks);
+    }
     cudaError_t e = fill_slots(type, a, p, s);
     for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
         HeadTcArgs h = common(a, p, HeadStep::kSums);
@@ -384,7 +586,7 @@ cudaError_t launch_head_logprobs(int type, int param_type, const HeadArgs &a, cu
         e = launch_head_tc(h, s);
     }
     if (e != cudaSuccess) return e;
-    return launch_chained(head_join_kernel, dim3((unsigned)((a.m * a.n + 7) / 8)), dim3(256), 0, s, true, a, p, (int)(up(a.vocab, 128) / 128));
+    return launch_chained(head_join_kernel, dim3((unsigned)((a.m * a.n + 7) / 8)), dim3(256), 0, s, true, a, p, (int)(up(a.vocab, p.sum_cols / 2) / (p.sum_cols / 2)));
 }
 
 cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cudaStream_t s) {
@@ -422,13 +624,16 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
             set_pairs(&h, p.prob_terms, p.w_terms);
             h.parts = at<float>(a, p.parts);
             h.parts_pitch = p.parts_pitch;
-            h.splits = p.splits;
+            h.extra = at<float>(a, p.extra);
+            h.most_splits = p.most_splits;
+            h.tile_cols = p.tile_cols;
             h.accumulate = i > 0;
             e = launch_head_tc(h, s);
             if (e != cudaSuccess) break;
         }
         if (a.dw) {
             h.step = HeadStep::kWeights;
+            h.tile_cols = 256;
             h.a = probs;
             h.b = slots_operand(a, p);
             h.b_row0 = 0;
@@ -447,8 +652,9 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
     const int size = type == ZENO_F32 ? 4 : 2;
     const int vectors = a.cols % 4 == 0 && aligned_to(a.dx, a.m, a.n, size, 4 * size);
     const int64_t blocks = (a.m * a.n * (p.parts_pitch / 4) + 255) / 256;
-    return type == ZENO_F32 ? launch_chained(head_inputs_kernel<float>, grid_for(blocks), dim3(256), 0, s, true, a, p, vectors)
-                            : launch_chained(head_inputs_kernel<__nv_bfloat16>, grid_for(blocks), dim3(256), 0, s, true, a, p, vectors);
+    const uint32_t pairs = head_pairs();
+    return type == ZENO_F32 ? launch_chained(head_inputs_kernel<float>, grid_for(blocks), dim3(256), 0, s, true, a, p, pairs, vectors)
+                            : launch_chained(head_inputs_kernel<__nv_bfloat16>, grid_for(blocks), dim3(256), 0, s, true, a, p, pairs, vectors);
 }
 
 }  // namespace zeno

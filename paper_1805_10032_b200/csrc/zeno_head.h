@@ -43,17 +43,41 @@ struct HeadTcArgs {
     int64_t prob_pitch;
     int prob_terms;
     // kInputs
-    float *parts;                       // [split][slots][parts_pitch]
+    float *parts;                       // [slots][parts_pitch]
     int64_t parts_pitch;
-    int splits, accumulate;
+    float *extra;                       // [item behind the whole rounds][256][tile_cols]: parts of tiles that are cut, but for their first ones
+    int most_splits, accumulate;
     // kWeights
     void *dw;
     int64_t lddw;
     int param_type;
+    int tile_cols;                      // columns of a tile: 256 or 128
     int last;                           // no kernel of the same call comes after this one
 };
 
-int head_tile_cols(int64_t rows_bound, int64_t groups, int64_t cols);
-cudaError_t launch_head_tc(const HeadTcArgs &a, cudaStream_t s);
+cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s);
+
+constexpr int kHeadRows = 256;          // rows of a tile
+constexpr int kHeadPairs = 74;          // pairs of SMs of this design
+int head_pairs();                       // that the current device has, of those
+
+// Tile number t of a group: rows first within a band of kHeadBand tiles of them, then columns.
+constexpr uint32_t kHeadBand = 16;
+struct HeadTile { int row, col; };
+__host__ __device__ inline HeadTile head_tile(uint32_t t, uint32_t row_tiles, uint32_t col_tiles) {
+    const uint32_t band = t / (kHeadBand * col_tiles), in = t - band * kHeadBand * col_tiles, left = row_tiles - band * kHeadBand, rows = left < kHeadBand ? left : kHeadBand;
+    const uint32_t col = in / rows;
+    return HeadTile{(int)(band * kHeadBand + in - col * rows), (int)col};
+}
+__host__ __device__ inline uint32_t head_tile_number(int row, int col, uint32_t row_tiles, uint32_t col_tiles) {
+    const uint32_t band = row / kHeadBand, left = row_tiles - band * kHeadBand, rows = left < kHeadBand ? left : kHeadBand;
+    return band * kHeadBand * col_tiles + col * rows + (row - band * kHeadBand);
+}
+// Parts that the tiles behind the whole rounds of all pairs are cut into.
+__host__ __device__ inline int head_splits(uint32_t tiles, uint32_t pairs, int most) {
+    const uint32_t rest = tiles % pairs;
+    const int fit = rest ? (int)(pairs / rest) : 1;
+    return fit < most ? fit : most;
+}
 
 }  // namespace zeno

@@ -6,8 +6,10 @@
 // block's TMEM.  Operands are bfloat16, in binary32 sums; a binary32 operand is three terms whose products are summed one pair of terms after the other, the
 // leading pair last.  X and W lie with the contraction's index contiguous for the logits ("K-major"); P W takes W, and P^T X both, with the index of the
 // result contiguous ("MN-major"), all in the 128-byte swizzled layouts that the tensor copies write.
-//   warp 0: copies;  warp 1: the pair's instructions in the first block, in the second the news that its copies have landed;
+//   warp 0: copies, both blocks' counted on the first one's barriers;  warp 1 of the first block: the pair's instructions;
 //   warps 2 - 9: sums from TMEM, the next tile's being formed meanwhile: 32 rows and half of the columns each.
+// One lane each loops over the copies and the instructions: by whole warps that elect a lane for every stage, a stage takes 500 cycles whatever its size
+// (256 by 128 tiles: 400), and with the second block's copies counted on its own barriers and reported to the first, 580.
 //
 // The tensor core adds with truncation towards zero.  So no set of sums in TMEM takes more than a stretch of stages; what it holds is then added in
 // registers, to nearest.
@@ -22,16 +24,20 @@ constexpr int kHalfRows = 128, kPairRows = 256;
 constexpr int kK = 64;                               // contraction indices of a stage: 128 bytes
 constexpr int kEpiWarps = 8, kThreads = 32 * (2 + kEpiWarps);
 constexpr int kABytes = kHalfRows * kK * 2;
-constexpr int kBox = 4096;                           // 32 rows of 128 bytes on their way out; each warp has two
-constexpr int kBand = 16;                            // tiles of rows that go together through the columns: their operand stays in L2
+constexpr int kBox = 4096;                           // 32 rows of 128 bytes of a warp on their way out (where little is summed, two of them: 61 tokens of 16 workers, 32003 x 1024: 208 us, 224)
+constexpr int kTurnBytes = 32 * 33 * 4;              // or 32 rows of 32 sums that lanes along the rows will write
+constexpr int kBoundsKept = 48;                      // groups whose bounds are kept in shared memory
 
-template <int N>
+template <HeadStep STEP, int N>
 struct Shape {
     static constexpr int kHalf = N / 2;
     static constexpr int kBBytes = kHalf * kK * 2;
     static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = N == 256 ? 5 : 6;
-    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * 2 * kBox + 1024;
+    static constexpr int kBoxes = STEP == HeadStep::kSums ? 0 : STEP == HeadStep::kWeights ? 2 : 1;      // of a warp
+    static constexpr int kBoxBytes = kEpiWarps * kBoxes * kBox;
+    static_assert(STEP != HeadStep::kWeights || kTurnBytes <= kBoxes * kBox, "either fits");
+    static constexpr int kStages = (225 * 1024 - kBoxBytes) / kStageBytes;
+    static constexpr int kSmem = kStages * kStageBytes + kBoxBytes + 1024;
 };
 
 __device__ unsigned g_given_up;                      // blocks whose bounded waits gave up since the process began
@@ -68,6 +74,12 @@ __device__ __forceinline__ uint64_t mn_major(uint32_t addr) {
     d |= (uint64_t)2 << 61;
     return d;
 }
+// A copy into this block's shared memory whose bytes are counted on a barrier of the pair's first block.
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void store_box(const CUtensorMap *map, const void *smem, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(smem)), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
@@ -76,7 +88,10 @@ __device__ __forceinline__ void add_box(const CUtensorMap *map, const void *smem
                  : "memory");
 }
 __device__ __forceinline__ void boxes_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void boxes_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void boxes_wait_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT < 0 ? 0 : LEFT) : "memory");
+}
 __device__ __forceinline__ void boxes_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -91,23 +106,26 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
 
 // One tile and the part of the contraction that goes into it.
 struct Item {
-    int group, row0, rows_end, col0, kb0, kb1, split;
+    int group, row0, rows_end, col0, kb0, kb1, split, splits, extra;
 };
 
 template <HeadStep STEP, int N, typename P>
 __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                              const __grid_constant__ CUtensorMap map_out, const KernelArgs args) {
-    using S = Shape<N>;
+                                                              const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_extra, const KernelArgs args) {
+    using S = Shape<STEP, N>;
     constexpr int HN = S::kHalf;
     constexpr bool kAMn = STEP == HeadStep::kWeights, kBMn = STEP == HeadStep::kWeights || STEP == HeadStep::kInputs;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    // full, empty, landed [kStages]; dfull, dempty [2]
-    constexpr int kBars = 3 * S::kStages + 4;
+    // full, empty [kStages]; dfull, dempty [2]
+    constexpr int kBars = 2 * S::kStages + 4;
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ __align__(8) uint64_t drain_bar, never_bar;
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_state[kAbortWords];
-    __shared__ int issued[S::kStages];                         // last round a copy was issued into a stage, plus one
+    __shared__ uint32_t issued[2][S::kStages];                 // of each block (the first one knows both at the end): last round that copies were issued into a stage
+                                                               // in, plus one, times four; whether they were of this block's rows (1), and of the other's (2)
+    __shared__ int other_gave_up;
+    __shared__ int bounds[2 * kBoundsKept];                    // begin and end of each group
 
     const HeadTcArgs &h = args.h;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -116,9 +134,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
     uint8_t *boxes = ring + S::kStages * S::kStageBytes;
     auto full = [&](int s) { return smem_u32(&bars[s]); };
     auto empty = [&](int s) { return smem_u32(&bars[S::kStages + s]); };
-    auto landed = [&](int s) { return smem_u32(&bars[2 * S::kStages + s]); };
-    auto dfull = [&](int q) { return smem_u32(&bars[3 * S::kStages + q]); };
-    auto dempty = [&](int q) { return smem_u32(&bars[3 * S::kStages + 2 + q]); };
+    auto dfull = [&](int q) { return smem_u32(&bars[2 * S::kStages + q]); };
+    auto dempty = [&](int q) { return smem_u32(&bars[2 * S::kStages + 2 + q]); };
 
     if (tid == 0) {
         abort_state[0] = 0;
@@ -126,8 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
         for (int s = 0; s < S::kStages; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
-            mbar_init(landed(s), 1);
-            issued[s] = 0;
+            issued[0][s] = issued[1][s] = 0;
         }
         for (int q = 0; q < 2; ++q) {
             mbar_init(dfull(q), 1);
@@ -150,39 +166,47 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
     const uint32_t tmem = tmem_base_slot;
     volatile int *abortp = &abort_state[0];
 
-    const int pair = blockIdx.x >> 1, pairs_of_blocks = gridDim.x >> 1;
+    const uint32_t pair = blockIdx.x >> 1, pairs_of_blocks = gridDim.x >> 1;
     // The tiles in their order: rows first within a band of kBand tiles, then columns, so that pairs next to one another share the columns' operand and all
     // of a band's rows stay in L2.
-    const int only_end = h.groups == 1 ? __ldcg(h.end) : 0;
-    const int row_tiles = STEP != HeadStep::kWeights && h.groups == 1 ? min(args.row_tiles, (only_end + kPairRows - 1) / kPairRows) : args.row_tiles;
-    const int64_t per_group = (int64_t)row_tiles * args.col_tiles, tiles = per_group * h.groups, items = tiles * (STEP == HeadStep::kInputs ? h.splits : 1);
+    const bool in_smem = h.groups <= kBoundsKept;
+    if (in_smem && tid < 2 * h.groups) bounds[tid] = __ldcg((tid & 1 ? h.end : h.begin) + (tid >> 1));
+    __syncthreads();
+    auto begin_of = [&](int group) { return in_smem ? bounds[2 * group] : __ldcg(h.begin + group); };
+    auto end_of = [&](int group) { return in_smem ? bounds[2 * group + 1] : __ldcg(h.end + group); };
+    const uint32_t row_tiles = STEP != HeadStep::kWeights && h.groups == 1 ? min(args.row_tiles, (bounds[1] + kPairRows - 1) / kPairRows) : args.row_tiles;
+    const uint32_t per_group = row_tiles * args.col_tiles, tiles = per_group * h.groups;
+    // kInputs: whole rounds of tiles, then the rest of them, cut along the words so that it takes all pairs
+    const uint32_t whole = STEP == HeadStep::kInputs ? tiles / pairs_of_blocks * pairs_of_blocks : tiles;
+    const int splits = STEP == HeadStep::kInputs ? head_splits(tiles, pairs_of_blocks, h.most_splits) : 1;
+    const uint32_t items = whole + (tiles - whole) * splits;
     // false: no further item
     auto get_item = [&](int li, Item &it) {
-        int64_t item = pair + (int64_t)li * pairs_of_blocks;
+        const uint32_t item = pair + li * pairs_of_blocks;
         if (item >= items) return false;
+        uint32_t tile = item;
         it.split = 0;
-        if (STEP == HeadStep::kInputs) {
-            it.split = (int)(item / tiles);
-            item -= it.split * tiles;
+        it.splits = 1;
+        if (STEP == HeadStep::kInputs && item >= whole) {
+            tile = whole + (item - whole) / splits;
+            it.split = (int)(item - whole - (tile - whole) * splits);
+            it.splits = splits;
         }
-        it.group = (int)(item / per_group);
-        int64_t in = item - it.group * per_group;
-        const int band = (int)(in / ((int64_t)kBand * args.col_tiles));
-        in -= (int64_t)band * kBand * args.col_tiles;
-        const int band_rows = min(kBand, row_tiles - band * kBand);
-        const int ct = (int)in / band_rows, rt = band * kBand + (int)in - ct * band_rows;
-        it.col0 = ct * N;
+        it.extra = (int)(item - whole);
+        it.group = (int)(tile / per_group);
+        const HeadTile at = head_tile(tile - it.group * per_group, row_tiles, args.col_tiles);
+        it.col0 = at.col * N;
         if (STEP == HeadStep::kWeights) {
-            it.row0 = rt * kPairRows;                                     // words of the piece
+            it.row0 = at.row * kPairRows;                                 // words of the piece
             it.rows_end = (int)h.piece;
-            it.kb0 = __ldcg(h.begin + it.group) / kK;
-            it.kb1 = __ldcg(h.end + it.group) / kK;
+            it.kb0 = begin_of(it.group) / kK;
+            it.kb1 = end_of(it.group) / kK;
         } else {
-            it.rows_end = h.groups == 1 ? only_end : __ldcg(h.end + it.group);
-            it.row0 = (h.groups == 1 ? 0 : __ldcg(h.begin + it.group)) + rt * kPairRows;
+            it.rows_end = end_of(it.group);
+            it.row0 = begin_of(it.group) + at.row * kPairRows;
             const int nkb = (int)(((STEP == HeadStep::kInputs ? h.piece : h.cols) + kK - 1) / kK);
-            it.kb0 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * it.split / h.splits) : 0;
-            it.kb1 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * (it.split + 1) / h.splits) : nkb;
+            it.kb0 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * it.split / it.splits) : 0;
+            it.kb1 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * (it.split + 1) / it.splits) : nkb;
             if (it.row0 >= it.rows_end) it.kb1 = it.kb0;                  // a group with fewer tokens
         }
         return true;
@@ -203,103 +227,89 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
     };
 
     if (warp == 0) {
-        // ------------------------------------------------------------------ copies
+        // ------------------------------------------------------------------ copies, by one lane
         wait_for_nothing(smem_u32(&never_bar), abortp);
-        int s = 0;
-        uint32_t round = 0;
-        bool ok = true;
-        Item it;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li)
-            for (int pr = 0; ok && pr < h.pairs; ++pr) {
-                const int plane_a = h.pair_a[pr], plane_b = (STEP == HeadStep::kWeights ? 0 : it.group * h.b_terms) + h.pair_b[pr];
-                for (int kb = it.kb0; kb < it.kb1; ++kb) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (round & 1) ^ 1, abortp));
-                    if (!ok) break;
-                    if (elect_one()) {
-                        uint8_t *to = ring + s * S::kStageBytes;
-                        mbar_expect_tx(full(s), S::kStageBytes);
-                        issued[s] = (int)round + 1;
+        if (elect_one()) {
+            const uint32_t first_full = cluster_addr(&bars[0], 0);
+            int s = 0;
+            uint32_t round = 0;
+            bool ok = true;
+            Item it;
+            for (int li = 0; ok && get_item(li, it) && !*abortp; ++li) {
+                // (of rows that are not there the instructions may read anything)
+                const bool rows_here = kAMn || it.row0 + rank * kHalfRows < it.rows_end, rows_there = kAMn || it.row0 + (1 - rank) * kHalfRows < it.rows_end;
+                const uint32_t bytes = 2 * S::kBBytes + (rows_here ? kABytes : 0) + (rows_there ? kABytes : 0);
+                const int row = it.row0 + rank * kHalfRows, col = it.col0 + rank * HN;
+                for (int pr = 0; ok && pr < h.pairs; ++pr) {
+                    const int plane_a = h.pair_a[pr], plane_b = (STEP == HeadStep::kWeights ? 0 : it.group * h.b_terms) + h.pair_b[pr];
+                    for (int kb = it.kb0; kb < it.kb1; ++kb) {
+                        ok = mbar_wait(empty(s), (round & 1) ^ 1, abortp);
+                        if (!ok) break;
+                        const uint32_t to_a = smem_u32(ring) + s * S::kStageBytes, to_b = to_a + kABytes, bar = first_full + s * 8;
+                        if (rank == 0) mbar_expect_tx(full(s), bytes);
+                        issued[rank][s] = (round + 1) * 4 + rows_there * 2 + rows_here;
                         if (kAMn) {
-#pragma unroll 1
-                            for (int q = 0; q < 2; ++q) tma_load_3d(smem_u32(to + q * kK * 128), &map_a, it.row0 + rank * kHalfRows + q * 64, kb * kK, plane_a, full(s));
-                        } else {
-                            tma_load_3d(smem_u32(to), &map_a, kb * kK, it.row0 + rank * kHalfRows, plane_a, full(s));
+                            tma_load_pair(to_a, &map_a, row, kb * kK, plane_a, bar);
+                            tma_load_pair(to_a + kK * 128, &map_a, row + 64, kb * kK, plane_a, bar);
+                        } else if (rows_here) {
+                            tma_load_pair(to_a, &map_a, kb * kK, row, plane_a, bar);
                         }
-                        to += kABytes;
-                        const int c0 = it.col0 + rank * HN;
                         if (kBMn) {
                             const int k0 = STEP == HeadStep::kInputs ? (int)h.b_row0 + kb * kK : kb * kK;
-#pragma unroll 1
-                            for (int q = 0; q < HN / 64; ++q) tma_load_3d(smem_u32(to + q * kK * 128), &map_b, c0 + q * 64, k0, plane_b, full(s));
+                            tma_load_pair(to_b, &map_b, col, k0, plane_b, bar);
+                            if (HN > 64) tma_load_pair(to_b + kK * 128, &map_b, col + 64, k0, plane_b, bar);
                         } else {
-                            tma_load_3d(smem_u32(to), &map_b, kb * kK, (int)h.b_row0 + c0, plane_b, full(s));
+                            tma_load_pair(to_b, &map_b, kb * kK, (int)h.b_row0 + col, plane_b, bar);
                         }
-                    }
-                    __syncwarp();
-                    if (++s == S::kStages) {
-                        s = 0;
-                        ++round;
-                    }
-                }
-            }
-    } else if (warp == 1 && rank != 0) {
-        // ------------------------------------------------------------------ the second block's copies have landed
-        const uint32_t remote = cluster_addr(&bars[2 * S::kStages], 0);
-        int s = 0;
-        uint32_t ph = 0;
-        bool ok = true;
-        Item it;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li)
-            for (int j = 0, all = (it.kb1 - it.kb0) * h.pairs; j < all; ++j) {
-                ok = __all_sync(0xffffffffu, mbar_wait(full(s), ph, abortp));
-                if (!ok) break;
-                if (lane == 0) remote_arrive(remote + s * 8);
-                if (++s == S::kStages) {
-                    s = 0;
-                    ph ^= 1;
-                }
-            }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------------ instructions, by the first block for both
-        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kAMn ? 1u : 0u) << 15) | ((kBMn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kPairRows >> 4) << 24);
-        int s = 0;
-        uint32_t ph = 0, drain = 0;                                  // stretches so far
-        bool ok = true;
-        Item it;
-        for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li) {
-            const Stretches st(args, it);
-            for (int part = 0, parts = st.count(); ok && part < parts; ++part, ++drain) {
-                const int set = (int)(drain & 1), from = st.at(part), to = st.at(part + 1);
-                ok = __all_sync(0xffffffffu, mbar_wait(dempty(set), ((drain >> 1) & 1) ^ 1, abortp));
-                if (!ok) break;
-                tc_fence_after();
-                for (int j = from; j < to; ++j) {
-                    ok = mbar_wait(full(s), ph, abortp) && mbar_wait(landed(s), ph, abortp);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t ab = smem_u32(ring + s * S::kStageBytes), bb = ab + kABytes;
-#pragma unroll
-                        for (int k = 0; k < kK / 16; ++k)        // 16 contraction indices: 32 bytes of a row, or 16 rows of 128 bytes
-                            mma_pair(tmem + set * N, kAMn ? mn_major(ab + k * 2048) : smem_desc_sw128(ab + k * 32), kBMn ? mn_major(bb + k * 2048) : smem_desc_sw128(bb + k * 32),
-                                     idesc, (uint32_t)((j - from) | k));
-                        commit_to_both(empty(s));
-                        if (j + 1 == to) commit_to_both(dfull(set));
-                    }
-                    __syncwarp();
-                    if (++s == S::kStages) {
-                        s = 0;
-                        ph ^= 1;
+                        if (++s == S::kStages) {
+                            s = 0;
+                            ++round;
+                        }
                     }
                 }
             }
         }
-    } else {
+        __syncwarp();
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ instructions, by one lane of the first block for both
+        if (rank == 0 && elect_one()) {
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kAMn ? 1u : 0u) << 15) | ((kBMn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kPairRows >> 4) << 24);
+            int s = 0;
+            uint32_t ph = 0, drain = 0;                              // stretches so far
+            bool ok = true;
+            Item it;
+            for (int li = 0; ok && get_item(li, it) && !*abortp; ++li) {
+                const Stretches st(args, it);
+                for (int part = 0, parts = st.count(); ok && part < parts; ++part, ++drain) {
+                    const int set = (int)(drain & 1), from = st.at(part), to = st.at(part + 1);
+                    ok = mbar_wait(dempty(set), ((drain >> 1) & 1) ^ 1, abortp);
+                    if (!ok) break;
+                    tc_fence_after();
+                    for (int j = from; j < to; ++j) {
+                        ok = mbar_wait(full(s), ph, abortp);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t ab = smem_u32(ring) + s * S::kStageBytes, bb = ab + kABytes;
+                        const uint64_t a_desc = kAMn ? mn_major(ab) : smem_desc_sw128(ab), b_desc = kBMn ? mn_major(bb) : smem_desc_sw128(bb);
+#pragma unroll
+                        for (int k = 0; k < kK / 16; ++k)        // 16 contraction indices: 32 bytes of a row, or 16 rows of 128 bytes
+                            mma_pair(tmem + set * N, a_desc + k * (kAMn ? 2048 / 16 : 32 / 16), b_desc + k * (kBMn ? 2048 / 16 : 32 / 16), idesc, (uint32_t)((j - from) | k));
+                        commit_to_both(empty(s));
+                        if (j + 1 == to) commit_to_both(dfull(set));
+                        if (++s == S::kStages) {
+                            s = 0;
+                            ph ^= 1;
+                        }
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 2) {
         // ------------------------------------------------------------------ sums
         const int quad = warp & 3, half = (warp - 2) >> 2;         // TMEM lanes that this warp may access; its half of the columns
-        const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[3 * S::kStages + 2], 0);
-        uint8_t *box = boxes + (warp - 2) * 2 * kBox;
+        const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[2 * S::kStages + 2], 0);
+        uint8_t *box = boxes + (warp - 2) * S::kBoxes * kBox;
         int turn = 0;
         uint32_t drain = 0;
         bool ok = true;
@@ -307,18 +317,18 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
         // 16 bytes of this lane's row in the box that goes out next
         auto put16 = [&](int chunk, uint4 v) { *reinterpret_cast<uint4 *>(box + turn * kBox + lane * 128 + ((chunk ^ (lane & 7)) << 4)) = v; };
         auto open_box = [&] {                                      // the box's last store has been read
-            if (lane == 0) boxes_wait_read_but_one();
+            if (lane == 0) boxes_wait_read<S::kBoxes - 1>();
             __syncwarp();
         };
-        auto close_box = [&](bool add, int c0, int c1, int c2) {
+        auto close_box = [&](const CUtensorMap *map, bool add, int c0, int c1, int c2) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-                if (add) add_box(&map_out, box + turn * kBox, c0, c1, c2);
-                else store_box(&map_out, box + turn * kBox, c0, c1, c2);
+                if (add) add_box(map, box + turn * kBox, c0, c1, c2);
+                else store_box(map, box + turn * kBox, c0, c1, c2);
                 boxes_commit();
             }
-            turn ^= 1;
+            if (S::kBoxes > 1) turn ^= 1;
         };
         for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li) {
             float acc[HN];
@@ -408,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                             }
                             put16(q, make_uint4(v[0], v[1], v[2], v[3]));
                         }
-                        close_box(false, col + c0, warp_row, t);
+                        close_box(&map_out, false, col + c0, warp_row, t);
                     }
                 }
             }
@@ -420,7 +430,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
                         put16(q, make_uint4(__float_as_uint(acc[c0 + q * 4]), __float_as_uint(acc[c0 + q * 4 + 1]), __float_as_uint(acc[c0 + q * 4 + 2]), __float_as_uint(acc[c0 + q * 4 + 3])));
-                    close_box(h.accumulate, col + c0, warp_row, it.split);
+                    if (it.split == 0) close_box(&map_out, h.accumulate, col + c0, warp_row, 0);
+                    else close_box(&map_extra, h.accumulate, half * HN + c0, it.extra * kPairRows + rank * kHalfRows + quad * 32, 0);
                 }
             }
             if constexpr (STEP == HeadStep::kWeights) {
@@ -438,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                                 v[e] = sizeof(P) == 4 ? __float_as_uint(acc[c0 + q * kPer + e]) : two_bf16(acc[c0 + q * kPer + e * 2], acc[c0 + q * kPer + (e * 2 + 1) % kPer]);
                             put16(q, make_uint4(v[0], v[1], v[2], v[3]));
                         }
-                        close_box(false, col + c0, (int)h.v0 + warp_row, it.group);
+                        close_box(&map_out, false, col + c0, (int)h.v0 + warp_row, it.group);
                     }
                 } else {                                            // rows of any alignment, 32 columns of a row at a time
                     float *turned = reinterpret_cast<float *>(box);
@@ -473,18 +484,34 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
         }
         __syncwarp();
     }
-    if (tid == 0 && abort_state[0]) {
-        // copies still in flight must land before the block exits
-        for (int s = 0; s < S::kStages; ++s)
-            if (issued[s] > 0)
-                for (uint32_t i = 0; i < kSpinLimit; ++i) {
-                    if (mbar_try_wait(full(s), (uint32_t)(issued[s] - 1) & 1)) break;
-                    __nanosleep(64);
-                }
-        atomicAdd(&g_given_up, 1u);
+    if (tid == 0) {
+        // what the other block has to know
+        const uint32_t other = 1 - rank;
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(&other_gave_up, other)), "r"(abort_state[0]) : "memory");
+        if (rank != 0)
+            for (int s = 0; s < S::kStages; ++s) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(&issued[1][s], 0)), "r"(issued[1][s]) : "memory");
+        if (abort_state[0]) atomicAdd(&g_given_up, 1u);
     }
     __syncthreads();
     cluster_barrier();                        // the other block's instructions, arrivals and reads have ended too
+    if (abort_state[0] || other_gave_up) {
+        // Copies still in flight must land before a block exits.  The blocks are at most one round of a stage apart: bytes that the other one's copies were to
+        // bring are counted as here, or are now expected.
+        if (tid == 0 && rank == 0)
+            for (int s = 0; s < S::kStages; ++s) {
+                const uint32_t mine = issued[0][s] >> 2, theirs = issued[1][s] >> 2;
+                const auto bytes = [&](uint32_t of_rows) { return (uint32_t)(S::kBBytes + (of_rows ? kABytes : 0)); };
+                if (mine > theirs)
+                    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(full(s)), "r"(bytes(issued[0][s] & 2)) : "memory");
+                if (theirs > mine) mbar_expect_tx(full(s), bytes(issued[1][s] & 1));
+                for (uint32_t i = 0; (mine || theirs) && i < kSpinLimit; ++i) {
+                    if (mbar_try_wait(full(s), (max(mine, theirs) - 1) & 1)) break;
+                    __nanosleep(64);
+                }
+            }
+        __syncthreads();
+        cluster_barrier();
+    }
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * N) : "memory");
 }
 
@@ -504,26 +531,29 @@ bool encode(CUtensorMap *map, const Operand &o, int box_cols, int box_rows) {
 }
 
 template <HeadStep STEP, int N, typename P>
-cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const KernelArgs &k, int64_t items, cudaStream_t s) {
-    int device = 0, sms = 0;
+cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const CUtensorMap &extra, const KernelArgs &k, int64_t items, cudaStream_t s) {
+    int device = 0;
     cudaError_t e = cudaGetDevice(&device);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return e;
     static PerDeviceOnce once;
     auto *kernel = head_tc_kernel<STEP, N, P>;
     if (once.need(device)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<N>::kSmem);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (Shape<STEP, N>::kSmem));
         if (e != cudaSuccess) return e;
         once.mark(device);
     }
-    const int64_t most = sms / 2, rounds = (items + most - 1) / most, pairs = (items + rounds - 1) / rounds;       // equal shares
-    return launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), Shape<N>::kSmem, s, true, a, b, out, k);
+    // equal shares; kInputs cuts what is left over itself
+    int64_t pairs = head_pairs();
+    if (STEP != HeadStep::kInputs) {
+        const int64_t rounds = (items + pairs - 1) / pairs;
+        pairs = (items + rounds - 1) / rounds;
+    }
+    return launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), (Shape<STEP, N>::kSmem), s, true, a, b, out, extra, k);
 }
 
-}  // namespace
-
-cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s) {
-    constexpr int N = 256, HN = N / 2;
+template <int N>
+cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
+    constexpr int HN = N / 2;
     KernelArgs k = {};
     k.h = h;
     const bool weights = h.step == HeadStep::kWeights, inputs = h.step == HeadStep::kInputs;
@@ -532,19 +562,22 @@ cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s) {
     k.drain = 8;
     k.drain_small = 64;
     k.spin_limit = spin_limit;
-    const int64_t items = (int64_t)k.row_tiles * k.col_tiles * h.groups * (inputs ? h.splits : 1);
+    const int64_t items = (int64_t)k.row_tiles * k.col_tiles * h.groups;
     if (items == 0) return cudaSuccess;
-    CUtensorMap a, b, out = {};
+    if (items >= (int64_t)1 << 30) return cudaErrorInvalidValue;
+    CUtensorMap a, b, out = {}, extra = {};
     if (!encode(&a, h.a, 64, weights ? kK : kHalfRows) || !encode(&b, h.b, 64, weights || inputs ? kK : HN)) return cudaErrorInvalidValue;
     switch (h.step) {
         case HeadStep::kSums:
-            return launch<HeadStep::kSums, N, float>(a, b, out, k, items, s);
+            return launch<HeadStep::kSums, N, float>(a, b, out, extra, k, items, s);
         case HeadStep::kProbs:
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, h.probs, h.piece, h.slots, h.prob_terms, h.prob_pitch, h.slots * h.prob_pitch, 64, 32)) return cudaErrorInvalidValue;
-            return launch<HeadStep::kProbs, N, float>(a, b, out, k, items, s);
+            return launch<HeadStep::kProbs, N, float>(a, b, out, extra, k, items, s);
         case HeadStep::kInputs:
-            if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.parts, h.cols, h.slots, h.splits, h.parts_pitch, h.slots * h.parts_pitch, 32, 32)) return cudaErrorInvalidValue;
-            return launch<HeadStep::kInputs, N, float>(a, b, out, k, items, s);
+            if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.parts, h.cols, h.slots, 1, h.parts_pitch, h.slots * h.parts_pitch, 32, 32) ||
+                !encode(&extra, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.extra, N, kHeadPairs * kPairRows, 1, N, kHeadPairs * kPairRows * N, 32, 32))
+                return cudaErrorInvalidValue;
+            return launch<HeadStep::kInputs, N, float>(a, b, out, extra, k, items, s);
         case HeadStep::kWeights: break;
     }
     const bool bf16 = h.param_type == ZENO_BF16;
@@ -552,7 +585,17 @@ cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s) {
     const int64_t plane = h.groups > 1 ? h.lddw : h.cols, limit = (int64_t)1 << 40;
     k.manual_stores = !(reinterpret_cast<uintptr_t>(h.dw) % 16 == 0 && h.cols * size % 16 == 0 && plane * size % 16 == 0 && plane * size < limit &&
                         encode(&out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, size, h.dw, h.cols, h.vocab, h.groups, h.cols, plane, 128 / size, 32));
-    return bf16 ? launch<HeadStep::kWeights, N, __nv_bfloat16>(a, b, out, k, items, s) : launch<HeadStep::kWeights, N, float>(a, b, out, k, items, s);
+    return bf16 ? launch<HeadStep::kWeights, N, __nv_bfloat16>(a, b, out, extra, k, items, s) : launch<HeadStep::kWeights, N, float>(a, b, out, extra, k, items, s);
+}
+
+}  // namespace
+
+cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s) { return h.tile_cols == 128 ? launch_tiles<128>(h, s) : launch_tiles<256>(h, s); }
+
+int head_pairs() {
+    int device = 0, sms = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) sms = 2 * kHeadPairs;
+    return sms / 2 < kHeadPairs ? sms / 2 : kHeadPairs;
 }
 
 void set_head_wait_limit(uint32_t polls) { spin_limit = polls; }

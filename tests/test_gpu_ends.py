@@ -188,3 +188,33 @@ def test_linear_logprobs_gradient(m, n, cols, vocab, act, par):
         assert zeno.linear_logprobs_gradient(_rows(x, layout), w, targets, lse, gl, dweight=into, want_dx=False, scale=scale) is None
         assert torch.equal(first, into)
     zeno.check_operator_status()
+
+
+@pytest.mark.parametrize("act,par", [(F32, F32), (BF16, BF16)])
+def test_waits_that_run_out_are_reported(act, par):
+    """With no polls allowed every wait on the tensor cores' path that is not satisfied at once gives up; the next call is sound."""
+    g = _gen(5)
+    m, n, cols, vocab = 2, 150, 264, 700
+    targets = _tokens(g, m, n, vocab, 0.0)
+    x, w = _head(g, m, n, cols, vocab, act, par)
+    want = zeno.linear_logprobs(x, w, targets)
+    gl = torch.ones(m, n, device="cuda")
+    dw = torch.empty(m, vocab, cols, device="cuda", dtype=par)
+    dx = zeno.linear_logprobs_gradient(x, w, targets, want.lse, gl, dweight=dw)
+    kept = dw.clone()
+    zeno.check_operator_status()
+    zeno.debug_set_operator_wait_limit(0)
+    try:
+        zeno.linear_logprobs(x, w, targets)
+        with pytest.raises(zeno.ZenoError) as e:
+            zeno.check_operator_status()
+        assert e.value.status == zeno.ERR_TIMEOUT
+        zeno.linear_logprobs_gradient(x, w, targets, want.lse, gl, dweight=dw)
+        with pytest.raises(zeno.ZenoError):
+            zeno.check_operator_status()
+    finally:
+        zeno.debug_set_operator_wait_limit(1 << 22)
+    again = zeno.linear_logprobs(x, w, targets)
+    assert torch.equal(again.logprobs, want.logprobs) and torch.equal(again.lse, want.lse)
+    assert torch.equal(zeno.linear_logprobs_gradient(x, w, targets, want.lse, gl, dweight=dw), dx) and torch.equal(dw, kept)
+    zeno.check_operator_status()
