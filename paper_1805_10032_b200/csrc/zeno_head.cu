@@ -11,7 +11,7 @@ namespace zeno {
 
 namespace {
 
-constexpr int64_t kPieceBytes = (int64_t)128 << 20, kWeightBytes = (int64_t)256 << 20;
+constexpr int64_t kPieceBytes = (int64_t)128 << 20, kWeightBytes = (int64_t)512 << 20;
 constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.
@@ -28,17 +28,25 @@ bool mappable(const void *w, int64_t ldw, int64_t groups, int64_t cols) {
     return reinterpret_cast<uintptr_t>(w) % 16 == 0 && cols % 8 == 0 && (groups <= 1 || (ldw % 8 == 0 && ldw < limit));
 }
 
-// A group of at most so many tokens takes no tensor cores: the weights go by once whatever the number of tokens.
-constexpr int kFew = 8;
-constexpr int64_t kFewCols = 8192, kFewBytes = 128 << 10;
+// Few tokens take no tensor cores: the weights go by once for every kFew tokens.  32000 words by 4096 columns, tokens in brackets, here and on the tensor
+// cores: bfloat16 49 us (1), 69 (2), 87 (3), 79 for any number; binary32 101 (1), 128 (4), 697; bfloat16 words that are not aligned 114 (1) by 1023
+// columns, 66.
+constexpr int kFew = 4;
+constexpr int64_t kFewCols = 8192;                                    // their chains of additions are as long as the tensor cores' stretches
+
+// Tokens of a group that this way is quicker for.
+int64_t few_tokens(int type, int param_type, bool aligned) {
+    if (param_type == ZENO_F32) return 3 * kFew;
+    return !aligned ? 0 : type == ZENO_F32 ? kFew : 2;
+}
 
 Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     Plan p = {};
     p.groups = a.ldw != 0 && a.m > 1 ? a.m : 1;
     const int64_t group_rows = p.groups > 1 ? a.n : a.m * a.n;
-    p.few = !gradient && group_rows <= kFew && a.cols <= kFewCols && (group_rows > 4 ? 8 : group_rows > 2 ? 4 : group_rows) * up(a.cols, 1024) * 4 <= kFewBytes;
+    p.few = !gradient && a.cols <= kFewCols && group_rows <= few_tokens(type, param_type, mappable(a.w, a.ldw, p.groups, a.cols));
     if (p.few) {
-        const int64_t most = (a.vocab + 31) / 32, blocks = 2 * 2 * kHeadPairs / p.groups;       // two blocks an SM
+        const int64_t most = (a.vocab + 15) / 16, blocks = 2 * 2 * kHeadPairs / p.groups;       // two blocks an SM, a word's pair for each warp
         p.few_blocks = (int)(blocks < 1 ? 1 : blocks < most ? blocks : most);
         p.part_pitch = p.few_blocks;
         p.target_logit = 0;
@@ -49,11 +57,13 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.x_terms = type == ZENO_F32 ? 3 : 1;
     p.w_terms = param_type == ZENO_F32 ? 3 : 1;
     p.w_packed = p.w_terms > 1 || !mappable(a.w, a.ldw, p.groups, a.cols);
-    p.prob_terms = p.x_terms > 1 || p.w_terms > 1 ? 3 : 1;
     // groups whose tiles of rows are written whole must not share one
     const int64_t worker_slots = up(a.n, p.groups > 1 && gradient ? 256 : kSlots);
     p.slots = worker_slots * a.m;
     p.group_slots = p.groups > 1 ? worker_slots : p.slots;
+    // Of bfloat16 operands D is bfloat16, too: its rounding, as large as the results', makes them off by 1.4 times that.  A few tokens' results may hang on one
+    // of its entries, whose rounding is no average: they take two terms.
+    p.prob_terms = p.x_terms > 1 || p.w_terms > 1 ? 3 : p.slots <= 256 ? 2 : 1;
     p.pitch = up(a.cols, 8);
     p.parts_pitch = up(a.cols, 4);
     const int64_t per_word = p.w_packed ? p.groups * p.w_terms * p.pitch * 2 : 0, per_prob = gradient ? p.slots * p.prob_terms * 2 : 0;
@@ -63,9 +73,11 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     if (most < kMinPiece) most = kMinPiece;
     p.pieces = (int)((a.vocab + most - 1) / most);
     p.piece = up((a.vocab + p.pieces - 1) / p.pieces, 256);
+    // with few tiles of rows, pieces of as many tiles as make whole rounds
+    const int64_t row_tiles = up(p.group_slots, kHeadRows) / kHeadRows * p.groups, round = kHeadPairs / row_tiles * 256;
+    if (p.pieces > 1 && round > 0 && round <= most) p.piece = most / round * round;
     p.pieces = (int)((a.vocab + p.piece - 1) / p.piece);
     // a tile of 128 columns where there are fewer of 256 than pairs of SMs
-    const int64_t row_tiles = up(p.group_slots, kHeadRows) / kHeadRows * p.groups;
     auto tile_for = [&](int64_t cols) { return row_tiles * (up(cols, 256) / 256) < kHeadPairs ? 128 : 256; };
     p.sum_cols = tile_for(p.piece);
     p.tile_cols = 256;                                                // its tiles are cut along the words instead
@@ -280,7 +292,8 @@ __global__ void __launch_bounds__(256, 2) head_few_kernel(const HeadArgs a, cons
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t group_rows = p.groups > 1 ? a.n : a.m * a.n, row0 = blockIdx.y * group_rows;
+    const int64_t of_group = p.groups > 1 ? a.n : a.m * a.n, row0 = blockIdx.y * of_group + blockIdx.z * R;
+    const int group_rows = (int)min((int64_t)R, of_group - blockIdx.z * R);
     const int cols = (int)a.cols, padded = (cols + 256 * AHEAD - 1) / (256 * AHEAD) * (256 * AHEAD);
     const P *w = static_cast<const P *>(a.w) + blockIdx.y * a.ldw;
     const int64_t step = (int64_t)gridDim.x * 8 * WORDS;
@@ -380,7 +393,7 @@ __global__ void __launch_bounds__(256, 2) head_few_kernel(const HeadArgs a, cons
     }
     if (lane < R) of_warp[warp][lane] = mine;
     __syncthreads();
-    if (threadIdx.x < group_rows) {
+    if ((int)threadIdx.x < group_rows) {
         mine = of_warp[0][threadIdx.x];
         for (int k = 1; k < 8; ++k) add_part(mine, of_warp[k][threadIdx.x].x, of_warp[k][threadIdx.x].y);
         at<float2>(a, p.part)[(row0 + threadIdx.x) * p.part_pitch + blockIdx.x] = mine;
@@ -537,26 +550,25 @@ HeadTcArgs common(const HeadArgs &a, const Plan &p, HeadStep step) {
 Operand slots_operand(const HeadArgs &a, const Plan &p) { return Operand{at<void>(a, p.x), a.cols, p.slots, p.pitch, p.slots * p.pitch, p.x_terms}; }
 
 template <typename T, typename P, int R, bool VECTORS>
-cudaError_t few(const HeadArgs &a, const Plan &p, cudaStream_t s) {
+cudaError_t few(const HeadArgs &a, const Plan &p, int64_t rows, cudaStream_t s) {
     auto *kernel = head_few_kernel<T, P, R, VECTORS>;
     static PerDeviceOnce once;
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e == cudaSuccess && once.need(device)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewBytes);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R * (int)kFewCols * 4);
         if (e == cudaSuccess) once.mark(device);
     }
-    return e == cudaSuccess ? launch_chained(kernel, dim3(p.few_blocks, p.groups), dim3(256), (size_t)(R * up(a.cols, 1024) * 4), s, true, a, p) : e;
+    return e == cudaSuccess ? launch_chained(kernel, dim3(p.few_blocks, p.groups, (unsigned)((rows + R - 1) / R)), dim3(256), (size_t)(R * up(a.cols, 1024) * 4), s, true, a, p) : e;
 }
 
 template <typename T, typename P>
 cudaError_t few_rows(const HeadArgs &a, const Plan &p, cudaStream_t s) {
     const int64_t rows = p.groups > 1 ? a.n : a.m * a.n;
     const bool vectors = a.cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.w) % 16 == 0 && (p.groups == 1 || a.ldw * sizeof(P) % 16 == 0);
-    if (rows <= 1) return vectors ? few<T, P, 1, true>(a, p, s) : few<T, P, 1, false>(a, p, s);
-    if (rows <= 2) return vectors ? few<T, P, 2, true>(a, p, s) : few<T, P, 2, false>(a, p, s);
-    if (rows <= 4) return vectors ? few<T, P, 4, true>(a, p, s) : few<T, P, 4, false>(a, p, s);
-    return vectors ? few<T, P, 8, true>(a, p, s) : few<T, P, 8, false>(a, p, s);
+    if (rows <= 1) return vectors ? few<T, P, 1, true>(a, p, rows, s) : few<T, P, 1, false>(a, p, rows, s);
+    if (rows <= 2) return vectors ? few<T, P, 2, true>(a, p, rows, s) : few<T, P, 2, false>(a, p, rows, s);
+    return vectors ? few<T, P, kFew, true>(a, p, rows, s) : few<T, P, kFew, false>(a, p, rows, s);
 }
 
 }  // namespace
@@ -615,11 +627,13 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
         h.probs = at<__nv_bfloat16>(a, p.probs);
         h.prob_pitch = p.piece;
         h.prob_terms = p.prob_terms;
+        h.bf16_result = p.prob_terms < 3;
         e = launch_head_tc(h, s);
         if (e != cudaSuccess) break;
         const Operand probs = {h.probs, h.piece, p.slots, p.piece, p.slots * p.piece, p.prob_terms};
         if (a.dx.data) {
             h.step = HeadStep::kInputs;
+            h.bf16_result = type == ZENO_BF16;
             h.a = probs;
             set_pairs(&h, p.prob_terms, p.w_terms);
             h.parts = at<float>(a, p.parts);
@@ -633,6 +647,7 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
         }
         if (a.dw) {
             h.step = HeadStep::kWeights;
+            h.bf16_result = param_type == ZENO_BF16;
             h.tile_cols = 256;
             h.a = probs;
             h.b = slots_operand(a, p);

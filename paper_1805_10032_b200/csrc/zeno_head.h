@@ -51,6 +51,7 @@ struct HeadTcArgs {
     void *dw;
     int64_t lddw;
     int param_type;
+    int bf16_result;                    // what comes of the sums is bfloat16
     int tile_cols;                      // columns of a tile: 256 or 128
     int last;                           // no kernel of the same call comes after this one
 };

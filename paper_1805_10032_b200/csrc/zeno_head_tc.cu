@@ -11,8 +11,6 @@
 // One lane each loops over the copies and the instructions: by whole warps that elect a lane for every stage, a stage takes 500 cycles whatever its size
 // (256 by 128 tiles: 400), and with the second block's copies counted on its own barriers and reported to the first, 580.
 //
-// The tensor core adds with truncation towards zero.  So no set of sums in TMEM takes more than a stretch of stages; what it holds is then added in
-// registers, to nearest.
 #include "zeno_head.h"
 #include "zeno_tc.cuh"
 
@@ -42,10 +40,17 @@ struct Shape {
 
 __device__ unsigned g_given_up;                      // blocks whose bounded waits gave up since the process began
 
+// The tensor core adds with truncation towards zero, about 1.4e-8 of a sum with every 16 products (where all are positive).  So a set of sums in TMEM takes a
+// stretch of the contraction only, and goes on in registers, in additions to nearest.  Stretches of 256 where binary32 operands are multiplied (by 512,
+// gradients are off by 1.3 times as much as by plain products in binary32); of 512 for logits of bfloat16 operands, whose lse is binary32 (4096
+// tokens, 131072 words, 4096 columns: 2.50 ms, by 256 2.65); of 1,024 for what is rounded to bfloat16 anyway (D of the same: 333 us for 16384 words, by 256 360).
+// The terms' planes of a stretch stay in L2 for all pairs of terms.
+constexpr int kDrainTerms = 4, kDrain = 8, kDrainBf16 = 16;
+
 struct KernelArgs {
     HeadTcArgs h;
     int row_tiles, col_tiles;                        // row_tiles: at most, of a group
-    int drain, drain_small;                          // stages of a stretch
+    int drain;                                       // blocks of kK contraction indices of a stretch
     int manual_stores;                               // kWeights: rows that no tensor copy can write
     uint32_t spin_limit;
 };
@@ -99,6 +104,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = (float)(1.4426950408889634 - (double)kLog2e);
 __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&v);
@@ -211,20 +217,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
         }
         return true;
     };
-    // Stretches of an item's stages: the smaller terms' in long ones, what is left of them with the first of the leading terms'.
-    struct Stretches {
-        int all, small, early, late, each;
-        __device__ Stretches(const KernelArgs &k, const Item &it) {
-            const int len = it.kb1 - it.kb0;
-            all = len * k.h.pairs;
-            small = all - len;
-            each = k.drain_small;
-            early = small / each;
-            late = (len + k.drain - 1) / k.drain;
-        }
-        __device__ int count() const { return early + late; }
-        __device__ int at(int part) const { return part <= early ? part * each : small + (int)((int64_t)(all - small) * (part - early) / late); }
-    };
+    // An item's contraction goes in stretches of at most args.drain blocks of kK indices: of one, all pairs of terms, block by block, the leading pair last.
+    auto stretches = [&](const Item &it) { return (it.kb1 - it.kb0 + args.drain - 1) / args.drain; };
 
     if (warp == 0) {
         // ------------------------------------------------------------------ copies, by one lane
@@ -240,9 +234,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                 const bool rows_here = kAMn || it.row0 + rank * kHalfRows < it.rows_end, rows_there = kAMn || it.row0 + (1 - rank) * kHalfRows < it.rows_end;
                 const uint32_t bytes = 2 * S::kBBytes + (rows_here ? kABytes : 0) + (rows_there ? kABytes : 0);
                 const int row = it.row0 + rank * kHalfRows, col = it.col0 + rank * HN;
-                for (int pr = 0; ok && pr < h.pairs; ++pr) {
+                for (int from = it.kb0, pr = 0; ok && from < it.kb1; pr = pr + 1 == h.pairs ? 0 : pr + 1, from += pr == 0 ? args.drain : 0) {
                     const int plane_a = h.pair_a[pr], plane_b = (STEP == HeadStep::kWeights ? 0 : it.group * h.b_terms) + h.pair_b[pr];
-                    for (int kb = it.kb0; kb < it.kb1; ++kb) {
+                    for (int kb = from, to = min(it.kb1, from + args.drain); kb < to; ++kb) {
                         ok = mbar_wait(empty(s), (round & 1) ^ 1, abortp);
                         if (!ok) break;
                         const uint32_t to_a = smem_u32(ring) + s * S::kStageBytes, to_b = to_a + kABytes, bar = first_full + s * 8;
@@ -279,13 +273,12 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
             bool ok = true;
             Item it;
             for (int li = 0; ok && get_item(li, it) && !*abortp; ++li) {
-                const Stretches st(args, it);
-                for (int part = 0, parts = st.count(); ok && part < parts; ++part, ++drain) {
-                    const int set = (int)(drain & 1), from = st.at(part), to = st.at(part + 1);
+                for (int from = it.kb0; ok && from < it.kb1; from += args.drain, ++drain) {
+                    const int set = (int)(drain & 1), all = (min(it.kb1, from + args.drain) - from) * h.pairs;
                     ok = mbar_wait(dempty(set), ((drain >> 1) & 1) ^ 1, abortp);
                     if (!ok) break;
                     tc_fence_after();
-                    for (int j = from; j < to; ++j) {
+                    for (int j = 0; j < all; ++j) {
                         ok = mbar_wait(full(s), ph, abortp);
                         if (!ok) break;
                         tc_fence_after();
@@ -293,9 +286,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                         const uint64_t a_desc = kAMn ? mn_major(ab) : smem_desc_sw128(ab), b_desc = kBMn ? mn_major(bb) : smem_desc_sw128(bb);
 #pragma unroll
                         for (int k = 0; k < kK / 16; ++k)        // 16 contraction indices: 32 bytes of a row, or 16 rows of 128 bytes
-                            mma_pair(tmem + set * N, a_desc + k * (kAMn ? 2048 / 16 : 32 / 16), b_desc + k * (kBMn ? 2048 / 16 : 32 / 16), idesc, (uint32_t)((j - from) | k));
+                            mma_pair(tmem + set * N, a_desc + k * (kAMn ? 2048 / 16 : 32 / 16), b_desc + k * (kBMn ? 2048 / 16 : 32 / 16), idesc, (uint32_t)(j | k));
                         commit_to_both(empty(s));
-                        if (j + 1 == to) commit_to_both(dfull(set));
+                        if (j + 1 == all) commit_to_both(dfull(set));
                         if (++s == S::kStages) {
                             s = 0;
                             ph ^= 1;
@@ -334,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
             float acc[HN];
 #pragma unroll
             for (int c = 0; c < HN; ++c) acc[c] = 0.f;
-            const int parts = Stretches(args, it).count();
+            const int parts = stretches(it);
             for (int part = 0; part < parts; ++part, ++drain) {
                 const int set = (int)(drain & 1);
                 ok = __all_sync(0xffffffffu, mbar_wait(dfull(set), (drain >> 1) & 1, abortp));
@@ -383,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                 for (int c = 0; c < HN; ++c) top[c & 3] = fmaxf(top[c & 3], acc[c]);
                 const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), beside = most == -INFINITY ? 0.f : most;
 #pragma unroll
-                for (int c = 0; c < HN; ++c) sum[c & 3] += exp2_fast((acc[c] - beside) * 1.4426950408889634f);
+                for (int c = 0; c < HN; ++c) sum[c & 3] += exp2_fast((acc[c] - beside) * kLog2e);
                 if (valid && have > 0) h.part[(int64_t)row * h.part_pitch + (h.v0 + col) / HN] = make_float2(most, (sum[0] + sum[1]) + (sum[2] + sum[3]));
             }
             if constexpr (STEP == HeadStep::kProbs) {
@@ -395,7 +388,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                 // p - [the target], times -g
 #pragma unroll
                 for (int c = 0; c < HN; ++c) {
-                    float p = exp2_fast(fmaf(acc[c], h.scale, -lse) * 1.4426950408889634f);
+                    const float d = fmaf(acc[c], h.scale, -lse), t = d * kLog2e;
+                    float p = exp2_fast(t);
+                    if (h.prob_terms > 2) p = fmaf(p, (fmaf(d, kLog2e, -t) + d * kLog2eRest) * 0.69314718f, p);      // what t is off by
                     if (here && c == target) p -= 1.f;
                     acc[c] = none ? 0.f : p * -g;
                 }
@@ -559,8 +554,7 @@ cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
     const bool weights = h.step == HeadStep::kWeights, inputs = h.step == HeadStep::kInputs;
     k.row_tiles = (int)(((weights ? h.piece : h.group_slots) + kPairRows - 1) / kPairRows);
     k.col_tiles = (int)(((weights || inputs ? h.cols : h.piece) + N - 1) / N);
-    k.drain = 8;
-    k.drain_small = 64;
+    k.drain = h.bf16_result ? kDrainBf16 : h.pairs > 1 || inputs || weights ? kDrainTerms : kDrain;
     k.spin_limit = spin_limit;
     const int64_t items = (int64_t)k.row_tiles * k.col_tiles * h.groups;
     if (items == 0) return cudaSuccess;
