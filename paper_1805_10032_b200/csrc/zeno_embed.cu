@@ -109,7 +109,8 @@ constexpr int kOrderWarps = 16, kOrderThreads = 32 * kOrderWarps;
 constexpr int kClassRows = 1024;                     // rows of a class at most
 constexpr int kQueue = 512;                          // tokens of its class that a warp notes on its way: the row, and in 22 bits which of its stretch
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kZeroSlice = 4096, kZeroRows = 4;      // columns, and rows, of a warp that writes zeros
+constexpr int kZeroSlice = 4096;                     // columns of a warp that writes zeros, and about how many bytes in all: with 16 KB the ticket is what all
+constexpr int kZeroBytes = 48 << 10;                 // wait for (8 tables of 32000 x 4096 in bfloat16, 2.1 GB: 460 us, 320 with 32 KB)
 constexpr int kRun = 32;                             // sorted positions of a warp
 constexpr int kCopied = 8;                           // rows of dy that a warp asks for at a time; it has two such lots in shared memory
 constexpr int kSliceBytes = 512, kPitch = kSliceBytes + 16;        // of a row of dy: a warp's, and where it lies in shared memory
@@ -325,7 +326,7 @@ struct RowsArgs {
     float *parts;                                    // [worker][run][2][cols]: what the run has of the row it begins in the middle of, and of the one it ends in
     int64_t runs;                                    // of a worker, at most
     int followed;                                    // the third kernel comes after the second
-    int slices, zero_chunks, zero_slices;            // of a worker: slices of columns; groups of rows, and their slices
+    int slices, zero_rows, zero_chunks, zero_slices; // of a worker: slices of columns; groups of zero_rows rows, and their slices
 };
 
 // blockIdx.y: the worker.  Its warps take runs of sorted positions in turn, then, whoever is free, groups of rows to write zeros to.  The rows of dy are copied
@@ -442,12 +443,20 @@ __global__ void __launch_bounds__(kThreads, 3) embed_rows_kernel(const RowsArgs 
         if (lane == 0) task = atomicAdd(reinterpret_cast<unsigned *>(&r.count[worker].y), 1u);
         task = __shfl_sync(0xffffffffu, task, 0);
         if (task >= zeros) break;
-        const uint32_t chunk = task / (uint32_t)r.zero_slices, slice = task - chunk * r.zero_slices, id = chunk * kZeroRows + lane;
+        const uint32_t chunk = task / (uint32_t)r.zero_slices, slice = task - chunk * r.zero_slices, id = chunk * r.zero_rows + lane;
         const int64_t col0 = (int64_t)slice * kZeroSlice;
         const int cols = (int)min((int64_t)kZeroSlice, a.cols - col0);
         const int *s = start + c.cls(id) * c.starts() + c.row(id);
-        unsigned none = __ballot_sync(0xffffffffu, lane < kZeroRows && id < (uint32_t)a.vocab && __ldcg(s) == __ldcg(s + 1));
-        for (P *first = table + (int64_t)chunk * kZeroRows * a.cols + col0; none; none &= none - 1) zero_entries<VECTORS>(first + (__ffs(none) - 1) * a.cols, cols, lane);
+        unsigned none = __ballot_sync(0xffffffffu, lane < r.zero_rows && id < (uint32_t)a.vocab && __ldcg(s) == __ldcg(s + 1));
+        P *first = table + (int64_t)chunk * r.zero_rows * a.cols + col0;
+        while (none) {
+            const int at = __ffs(none) - 1;
+            const unsigned others = ~(none >> at);
+            // whole rows that follow one another are one stretch
+            const int together = r.zero_slices > 1 ? 1 : others ? __ffs(others) - 1 : 32;
+            zero_entries<VECTORS>(first + at * a.cols, together * cols, lane);
+            none &= together + at >= 32 ? 0u : ~0u << (at + together);
+        }
     }
 }
 
@@ -546,9 +555,13 @@ cudaError_t embed_gradient(const EmbedGradArgs &a, cudaStream_t s) {
     }
     e = launch_chained(embed_order_kernel, dim3(c.count(), a.m), dim3(kOrderThreads), (size_t)kOrderWarps * c.rows * 4, s, true, a.tokens, a.n, a.vocab, c, start, count, list);
     if (e != cudaSuccess) return e;
-    RowsArgs r = {a, c, start, count, list, reinterpret_cast<float *>(ws + p.parts), runs_of(a.n), a.n > kRun, 0, 0, 0};
-    r.zero_chunks = a.add ? 0 : (int)((a.vocab + kZeroRows - 1) / kZeroRows);
+    RowsArgs r = {a, c, start, count, list, reinterpret_cast<float *>(ws + p.parts), runs_of(a.n), a.n > kRun, 0, 0, 0, 0};
     r.zero_slices = (int)((a.cols + kZeroSlice - 1) / kZeroSlice);
+    const int64_t rows = kZeroBytes / ((a.cols < kZeroSlice ? a.cols : kZeroSlice) * (int)sizeof(P));
+    const int64_t shares = (int64_t)a.m * a.vocab * r.zero_slices / (148 * 3 * kWarps) + 1;           // so that every warp has some
+    r.zero_rows = (int)(rows < 1 ? 1 : rows < 32 ? rows : 32);
+    if (shares < r.zero_rows) r.zero_rows = (int)shares;
+    r.zero_chunks = a.add ? 0 : (int)((a.vocab + r.zero_rows - 1) / r.zero_rows);
     const bool vectors = a.cols % 8 == 0 && aligned_to(a.dy, a.m, a.n, sizeof(T), 16) && reinterpret_cast<uintptr_t>(a.dtable) % 16 == 0 && (a.m <= 1 || a.ldt * sizeof(P) % 16 == 0);
     return vectors ? sum_rows<T, P, true>(r, s) : sum_rows<T, P, false>(r, s);
 }
@@ -565,7 +578,7 @@ int64_t embed_gradient_workspace(int m, int64_t n, int64_t vocab, int64_t cols) 
 // A warp's tasks are counted in 32 bits.
 bool embed_gradient_fits(int64_t n, int64_t vocab, int64_t cols) {
     const int64_t limit = (int64_t)1 << 31;
-    return runs_of(n) * ((cols + 63) / 64) < limit && (vocab / kZeroRows + ((int64_t)1 << 16)) * ((cols + kZeroSlice - 1) / kZeroSlice) < limit;
+    return runs_of(n) * ((cols + 63) / 64) < limit && (vocab + 1) * ((cols + kZeroSlice - 1) / kZeroSlice) < limit;
 }
 
 cudaError_t launch_embed_gradient(int type, int param_type, const EmbedGradArgs &a, cudaStream_t s) {

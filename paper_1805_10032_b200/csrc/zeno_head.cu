@@ -16,12 +16,30 @@ constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.
 struct Plan {
-    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, few, few_blocks;
+    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, sum_words, few, few_blocks;
     int64_t group_slots, slots, pitch, piece, parts_pitch, part_pitch;
     int64_t counts, begin, end, total, list, rank, target, lse, g, target_logit, x, w, part, probs, parts, extra, bytes;
 };
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// Terms that are multiplied: those of the smallest products first.
+void set_pairs(HeadTcArgs *h, int a_terms, int b_terms) {
+    h->pairs = 0;
+    for (int order = 2; order >= 0; --order)
+        for (int i = 0; i <= order; ++i)
+            if (i < a_terms && order - i < b_terms) {
+                h->pair_a[h->pairs] = i;
+                h->pair_b[h->pairs++] = order - i;
+            }
+}
+
+// Words of a part of lse.
+int head_part_words(int tile_cols, int x_terms, int w_terms, int64_t cols) {
+    HeadTcArgs h = {};
+    set_pairs(&h, x_terms, w_terms);
+    return head_brief(h.pairs, cols) ? 64 : tile_cols / 2;
+}
 
 bool mappable(const void *w, int64_t ldw, int64_t groups, int64_t cols) {
     const int64_t limit = (int64_t)1 << 39;
@@ -46,7 +64,7 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     const int64_t group_rows = p.groups > 1 ? a.n : a.m * a.n;
     p.few = !gradient && a.cols <= kFewCols && group_rows <= few_tokens(type, param_type, mappable(a.w, a.ldw, p.groups, a.cols));
     if (p.few) {
-        const int64_t most = (a.vocab + 15) / 16, blocks = 2 * 2 * kHeadPairs / p.groups;       // two blocks an SM, a word's pair for each warp
+        const int64_t lots = (group_rows + kFew - 1) / kFew, most = (a.vocab + 15) / 16, blocks = 2 * 2 * kHeadPairs / (p.groups * lots);      // two blocks an SM
         p.few_blocks = (int)(blocks < 1 ? 1 : blocks < most ? blocks : most);
         p.part_pitch = p.few_blocks;
         p.target_logit = 0;
@@ -83,7 +101,8 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.tile_cols = 256;                                                // its tiles are cut along the words instead
     p.most_splits = (int)(p.piece / 64 / 8);                          // parts of eight stages and more
     if (p.most_splits < 1) p.most_splits = 1;
-    p.part_pitch = up(a.vocab, 256) / (p.sum_cols / 2);
+    p.sum_words = head_part_words(p.sum_cols, p.x_terms, p.w_terms, a.cols);
+    p.part_pitch = up(a.vocab, 256) / p.sum_words;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t from = at;
@@ -165,31 +184,50 @@ __device__ __forceinline__ void put_terms(float (&f)[8], __nv_bfloat16 *to, int6
     }
 }
 
-// Some threads rewrite a row of cols entries (NULL: zeros), eight to each.
-template <typename T, int TERMS>
-__device__ __forceinline__ void row_terms(const T *from, int64_t cols, int64_t pitch, __nv_bfloat16 *to, int64_t plane, bool vectors, int thread, int threads) {
-    for (int64_t c = thread * 8; c < pitch; c += threads * 8) {
-        float f[8] = {};
-        if (from && vectors) {
-            alignas(16) T e[8];
+// Eight entries of a row on their way: as they lie (VECTORS), or as the aligned words around them, of those that hold an entry of the row.
+template <typename T>
+struct Eight {
+    static constexpr int kLoads = 8 * sizeof(T) / 16;
+    uint4 q[kLoads + 1];
+    __device__ __forceinline__ void load(const T *row, int64_t c, int64_t cols, bool vectors) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(row + c), end = reinterpret_cast<uintptr_t>(row + cols);
+        const uint4 *words = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
 #pragma unroll
-            for (int k = 0; k < (int)sizeof(e) / 16; ++k) reinterpret_cast<uint4 *>(e)[k] = reinterpret_cast<const uint4 *>(from + c)[k];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = value_of(e + k);
-        } else if (from && c < cols) {                                 // by aligned loads and shifts, of words that hold an entry of the row
-            constexpr int kLoads = 8 * sizeof(T) / 16;
-            const uintptr_t at = reinterpret_cast<uintptr_t>(from + c), end = reinterpret_cast<uintptr_t>(from + cols);
-            const uint4 *words = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
-            uint4 q[kLoads + 1];
-#pragma unroll
-            for (int k = 0; k <= kLoads; ++k) q[k] = reinterpret_cast<uintptr_t>(words + k) < end ? words[k] : make_uint4(0, 0, 0, 0);
-            alignas(16) T e[8];
-#pragma unroll
-            for (int k = 0; k < kLoads; ++k) reinterpret_cast<uint4 *>(e)[k] = shifted<sizeof(T)>(q[k], q[k + 1], (unsigned)(at & 15));
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = c + k < cols ? value_of(e + k) : 0.f;
+        for (int k = 0; k < kLoads + 1; ++k) {
+            q[k] = make_uint4(0, 0, 0, 0);
+            if (row && c < cols && (k < kLoads || !vectors) && reinterpret_cast<uintptr_t>(words + k) < end) q[k] = words[k];
         }
-        put_terms<TERMS>(f, to + c, plane);
+    }
+    __device__ __forceinline__ void get(float (&f)[8], const T *row, int64_t c, int64_t cols, bool vectors) const {
+        const unsigned off = vectors ? 0u : (unsigned)(reinterpret_cast<uintptr_t>(row + c) & 15);
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const uint4 v = vectors ? q[k] : shifted<sizeof(T)>(q[k], q[k + 1], off);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 16 / (int)sizeof(T); ++i) {
+                const int at = k * (16 / (int)sizeof(T)) + i;
+                const float e = sizeof(T) == 4 ? __uint_as_float(w[i % 4]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+                f[at] = row && c + at < cols ? e : 0.f;
+            }
+        }
+    }
+};
+
+// Some threads rewrite ROWS rows of cols entries (NULL: zeros), eight of each to a thread and turn, all of a turn's rows asked for at once.
+template <typename T, int TERMS, int ROWS>
+__device__ __forceinline__ void rows_terms(const T *const (&from)[ROWS], __nv_bfloat16 *const (&to)[ROWS], int64_t cols, int64_t pitch, int64_t plane, bool vectors, int thread,
+                                           int threads) {
+    for (int64_t c = thread * 8; c < pitch; c += threads * 8) {
+        Eight<T> e[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) e[r].load(from[r], c, cols, vectors);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            float f[8];
+            e[r].get(f, from[r], c, cols, vectors);
+            if (to[r]) put_terms<TERMS>(f, to[r] + c, plane);
+        }
     }
 }
 
@@ -254,7 +292,9 @@ __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
             }
         }
         const T *from = token >= 0 ? static_cast<const T *>(a.x.data) + worker * a.x.group + token * a.x.row : nullptr;
-        row_terms<T, TERMS>(from, a.cols, p.pitch, at<__nv_bfloat16>(a, p.x) + slot * p.pitch, p.slots * p.pitch, args.vectors, thread, threads);
+        const T *const froms[1] = {from};
+        __nv_bfloat16 *const tos[1] = {at<__nv_bfloat16>(a, p.x) + slot * p.pitch};
+        rows_terms<T, TERMS, 1>(froms, tos, a.cols, p.pitch, p.slots * p.pitch, args.vectors, thread, threads);
     }
 }
 
@@ -265,10 +305,20 @@ __global__ void __launch_bounds__(256) head_words_kernel(const T *w, int64_t ldw
                                                          __nv_bfloat16 *out, int vectors, int threads_log2, int beside) {
     if (!beside) pdl_wait();
     pdl_launch_dependents();
+    constexpr int kRows = 1;
     const int threads = 1 << threads_log2, rows_of_block = 256 >> threads_log2;
-    for (int64_t q = (int64_t)blockIdx.x * rows_of_block + (threadIdx.x >> threads_log2); q < total; q += (int64_t)gridDim.x * rows_of_block) {
-        const int64_t group = q / words, v = q - group * words;
-        row_terms<T, TERMS>(w + group * ldw + (v0 + v) * cols, cols, pitch, out + (group * TERMS * piece + v) * pitch, piece * pitch, vectors, threadIdx.x & (threads - 1), threads);
+    const int64_t stride = (int64_t)gridDim.x * rows_of_block;
+    for (int64_t q0 = (int64_t)blockIdx.x * rows_of_block + (threadIdx.x >> threads_log2); q0 < total; q0 += kRows * stride) {
+        const T *from[kRows];
+        __nv_bfloat16 *to[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int64_t q = q0 + r * stride;
+            const uint32_t group = (uint32_t)(q < total ? q : 0) / (uint32_t)words, v = (uint32_t)(q < total ? q : 0) - group * words;
+            from[r] = q < total ? w + group * ldw + (v0 + v) * cols : nullptr;
+            to[r] = q < total ? out + ((int64_t)group * TERMS * piece + v) * pitch : nullptr;
+        }
+        rows_terms<T, TERMS, kRows>(from, to, cols, pitch, piece * pitch, vectors, threadIdx.x & (threads - 1), threads);
     }
     if (beside) pdl_wait();
 }
@@ -292,11 +342,14 @@ __global__ void __launch_bounds__(256, 2) head_few_kernel(const HeadArgs a, cons
     pdl_wait();
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t of_group = p.groups > 1 ? a.n : a.m * a.n, row0 = blockIdx.y * of_group + blockIdx.z * R;
-    const int group_rows = (int)min((int64_t)R, of_group - blockIdx.z * R);
+    // neighbouring blocks take the same words with R tokens each, so that all but one find the words in L2
+    const int64_t of_group = p.groups > 1 ? a.n : a.m * a.n;
+    const int lots = (int)((of_group + R - 1) / R), block = blockIdx.x / lots, lot = blockIdx.x - block * lots, blocks = gridDim.x / lots;
+    const int64_t row0 = blockIdx.y * of_group + lot * R;
+    const int group_rows = (int)min((int64_t)R, of_group - lot * R);
     const int cols = (int)a.cols, padded = (cols + 256 * AHEAD - 1) / (256 * AHEAD) * (256 * AHEAD);
     const P *w = static_cast<const P *>(a.w) + blockIdx.y * a.ldw;
-    const int64_t step = (int64_t)gridDim.x * 8 * WORDS;
+    const int64_t step = (int64_t)blocks * 8 * WORDS;
     uint32_t next[AHEAD][WORDS][kRegs];
     auto ask = [&](int64_t v0, int c0) {
 #pragma unroll
@@ -317,7 +370,7 @@ __global__ void __launch_bounds__(256, 2) head_few_kernel(const HeadArgs a, cons
                 }
             }
     };
-    int64_t v0 = ((int64_t)blockIdx.x * 8 + warp) * WORDS;
+    int64_t v0 = ((int64_t)block * 8 + warp) * WORDS;
     ask(v0, 0);
     int target = -1;                                         // of the lane's row
     if (lane < group_rows) target = a.targets[row0 + lane];
@@ -396,7 +449,7 @@ __global__ void __launch_bounds__(256, 2) head_few_kernel(const HeadArgs a, cons
     if ((int)threadIdx.x < group_rows) {
         mine = of_warp[0][threadIdx.x];
         for (int k = 1; k < 8; ++k) add_part(mine, of_warp[k][threadIdx.x].x, of_warp[k][threadIdx.x].y);
-        at<float2>(a, p.part)[(row0 + threadIdx.x) * p.part_pitch + blockIdx.x] = mine;
+        at<float2>(a, p.part)[(row0 + threadIdx.x) * p.part_pitch + block] = mine;
     }
 }
 
@@ -487,16 +540,6 @@ __global__ void __launch_bounds__(256) head_zero_kernel(P *dw, int64_t per_group
 
 dim3 grid_for(int64_t blocks) { return dim3((unsigned)(blocks < 148 * 16 ? blocks : 148 * 16)); }
 
-// Terms that are multiplied: those of the smallest products first.
-void set_pairs(HeadTcArgs *h, int a_terms, int b_terms) {
-    h->pairs = 0;
-    for (int order = 2; order >= 0; --order)
-        for (int i = 0; i <= order; ++i)
-            if (i < a_terms && order - i < b_terms) {
-                h->pair_a[h->pairs] = i;
-                h->pair_b[h->pairs++] = order - i;
-            }
-}
 
 cudaError_t fill_slots(int type, const HeadArgs &a, const Plan &p, cudaStream_t s) {
     cudaError_t e = launch_chained(head_order_kernel, dim3(a.m), dim3(kOrderThreads), 0, s, true, a.targets, a.n, a.vocab, at<int>(a, p.counts), at<int>(a, p.list), at<int>(a, p.rank));
@@ -559,7 +602,7 @@ cudaError_t few(const HeadArgs &a, const Plan &p, int64_t rows, cudaStream_t s) 
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R * (int)kFewCols * 4);
         if (e == cudaSuccess) once.mark(device);
     }
-    return e == cudaSuccess ? launch_chained(kernel, dim3(p.few_blocks, p.groups, (unsigned)((rows + R - 1) / R)), dim3(256), (size_t)(R * up(a.cols, 1024) * 4), s, true, a, p) : e;
+    return e == cudaSuccess ? launch_chained(kernel, dim3((unsigned)(p.few_blocks * ((rows + R - 1) / R)), p.groups), dim3(256), (size_t)(R * up(a.cols, 1024) * 4), s, true, a, p) : e;
 }
 
 template <typename T, typename P>
@@ -598,7 +641,7 @@ cudaError_t launch_head_logprobs(int type, int param_type, const HeadArgs &a, cu
         e = launch_head_tc(h, s);
     }
     if (e != cudaSuccess) return e;
-    return launch_chained(head_join_kernel, dim3((unsigned)((a.m * a.n + 7) / 8)), dim3(256), 0, s, true, a, p, (int)(up(a.vocab, p.sum_cols / 2) / (p.sum_cols / 2)));
+    return launch_chained(head_join_kernel, dim3((unsigned)((a.m * a.n + 7) / 8)), dim3(256), 0, s, true, a, p, (int)(up(a.vocab, p.sum_words) / p.sum_words));
 }
 
 cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cudaStream_t s) {

@@ -7,7 +7,7 @@
 // leading pair last.  X and W lie with the contraction's index contiguous for the logits ("K-major"); P W takes W, and P^T X both, with the index of the
 // result contiguous ("MN-major"), all in the 128-byte swizzled layouts that the tensor copies write.
 //   warp 0: copies, both blocks' counted on the first one's barriers;  warp 1 of the first block: the pair's instructions;
-//   warps 2 - 9: sums from TMEM, the next tile's being formed meanwhile: 32 rows and half of the columns each.
+//   the other warps: sums from TMEM, the next tile's being formed meanwhile: 32 rows and 64 columns each.
 // One lane each loops over the copies and the instructions: by whole warps that elect a lane for every stage, a stage takes 500 cycles whatever its size
 // (256 by 128 tiles: 400), and with the second block's copies counted on its own barriers and reported to the first, 580.
 //
@@ -20,20 +20,19 @@ namespace {
 
 constexpr int kHalfRows = 128, kPairRows = 256;
 constexpr int kK = 64;                               // contraction indices of a stage: 128 bytes
-constexpr int kEpiWarps = 8, kThreads = 32 * (2 + kEpiWarps);
 constexpr int kABytes = kHalfRows * kK * 2;
-constexpr int kBox = 4096;                           // 32 rows of 128 bytes of a warp on their way out (where little is summed, two of them: 61 tokens of 16 workers, 32003 x 1024: 208 us, 224)
-constexpr int kTurnBytes = 32 * 33 * 4;              // or 32 rows of 32 sums that lanes along the rows will write
+constexpr int kBox = 4096;                           // 32 rows of 128 bytes of a warp on their way out
 constexpr int kBoundsKept = 48;                      // groups whose bounds are kept in shared memory
 
-template <HeadStep STEP, int N>
+template <HeadStep STEP, int N, int COLS>
 struct Shape {
     static constexpr int kHalf = N / 2;
     static constexpr int kBBytes = kHalf * kK * 2;
     static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kCols = COLS;                                   // of a warp that takes sums
+    static constexpr int kEpiWarps = 4 * N / kCols, kThreads = 32 * (2 + kEpiWarps);
     static constexpr int kBoxes = STEP == HeadStep::kSums ? 0 : STEP == HeadStep::kWeights ? 2 : 1;      // of a warp
     static constexpr int kBoxBytes = kEpiWarps * kBoxes * kBox;
-    static_assert(STEP != HeadStep::kWeights || kTurnBytes <= kBoxes * kBox, "either fits");
     static constexpr int kStages = (225 * 1024 - kBoxBytes) / kStageBytes;
     static constexpr int kSmem = kStages * kStageBytes + kBoxBytes + 1024;
 };
@@ -115,11 +114,11 @@ struct Item {
     int group, row0, rows_end, col0, kb0, kb1, split, splits, extra;
 };
 
-template <HeadStep STEP, int N, typename P>
-__global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+template <HeadStep STEP, int N, int COLS, typename P>
+__global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                               const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_extra, const KernelArgs args) {
-    using S = Shape<STEP, N>;
-    constexpr int HN = S::kHalf;
+    using S = Shape<STEP, N, COLS>;
+    constexpr int HN = S::kHalf, kCols = COLS;
     constexpr bool kAMn = STEP == HeadStep::kWeights, kBMn = STEP == HeadStep::kWeights || STEP == HeadStep::kInputs;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // full, empty [kStages]; dfull, dempty [2]
@@ -153,7 +152,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
         }
         for (int q = 0; q < 2; ++q) {
             mbar_init(dfull(q), 1);
-            mbar_init(dempty(q), 2 * kEpiWarps);
+            mbar_init(dempty(q), 2 * S::kEpiWarps);
         }
         mbar_init(smem_u32(&drain_bar), 1);
         mbar_init(smem_u32(&never_bar), 1);
@@ -300,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
         __syncwarp();
     } else if (warp >= 2) {
         // ------------------------------------------------------------------ sums
-        const int quad = warp & 3, half = (warp - 2) >> 2;         // TMEM lanes that this warp may access; its half of the columns
+        const int quad = warp & 3, part_col = ((warp - 2) >> 2) * kCols;         // TMEM lanes that this warp may access; its columns
         const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[2 * S::kStages + 2], 0);
         uint8_t *box = boxes + (warp - 2) * S::kBoxes * kBox;
         int turn = 0;
@@ -324,18 +323,18 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
             if (S::kBoxes > 1) turn ^= 1;
         };
         for (int li = 0; ok && __all_sync(0xffffffffu, get_item(li, it) && !*abortp); ++li) {
-            float acc[HN];
+            float acc[kCols];
 #pragma unroll
-            for (int c = 0; c < HN; ++c) acc[c] = 0.f;
+            for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
             const int parts = stretches(it);
             for (int part = 0; part < parts; ++part, ++drain) {
                 const int set = (int)(drain & 1);
                 ok = __all_sync(0xffffffffu, mbar_wait(dfull(set), (drain >> 1) & 1, abortp));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + set * N + half * HN;
+                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + set * N + part_col;
 #pragma unroll
-                for (int c0 = 0; c0 < HN; c0 += 32) {
+                for (int c0 = 0; c0 < kCols; c0 += 32) {
                     uint32_t v[2][16];
                     tc_ld16(from + c0, v[0]);
                     tc_ld16(from + c0 + 16, v[1]);
@@ -352,42 +351,42 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
             }
             if (!ok) break;
             const int warp_row = it.row0 + rank * kHalfRows + quad * 32, row = warp_row + lane;
-            const int col = it.col0 + half * HN;                   // the first of this thread's columns
+            const int col = it.col0 + part_col;                   // the first of this thread's columns
             if (STEP != HeadStep::kWeights && it.row0 >= it.rows_end) continue;
 
             if constexpr (STEP == HeadStep::kSums) {
                 const bool valid = row < it.rows_end;
-                const int have = (int)min((int64_t)HN, h.piece - col);          // words of this thread
+                const int have = (int)min((int64_t)kCols, h.piece - col);          // words of this thread
 #pragma unroll
-                for (int c = 0; c < HN; ++c) acc[c] *= h.scale;
-                if (have < HN)
+                for (int c = 0; c < kCols; ++c) acc[c] *= h.scale;
+                if (have < kCols)
 #pragma unroll
-                    for (int c = 0; c < HN; ++c)
+                    for (int c = 0; c < kCols; ++c)
                         if (c >= have) acc[c] = -INFINITY;
                 const int target = valid ? h.targets[row] - (int)(h.v0 + col) : -1;
                 if (__any_sync(0xffffffffu, target >= 0 && target < have)) {
                     float z = 0.f;
 #pragma unroll
-                    for (int c = 0; c < HN; ++c) z = c == target ? acc[c] : z;
+                    for (int c = 0; c < kCols; ++c) z = c == target ? acc[c] : z;
                     if (target >= 0 && target < have) h.target_logit[row] = z;
                 }
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sum[4] = {};
 #pragma unroll
-                for (int c = 0; c < HN; ++c) top[c & 3] = fmaxf(top[c & 3], acc[c]);
+                for (int c = 0; c < kCols; ++c) top[c & 3] = fmaxf(top[c & 3], acc[c]);
                 const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), beside = most == -INFINITY ? 0.f : most;
 #pragma unroll
-                for (int c = 0; c < HN; ++c) sum[c & 3] += exp2_fast((acc[c] - beside) * kLog2e);
-                if (valid && have > 0) h.part[(int64_t)row * h.part_pitch + (h.v0 + col) / HN] = make_float2(most, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+                for (int c = 0; c < kCols; ++c) sum[c & 3] += exp2_fast((acc[c] - beside) * kLog2e);
+                if (valid && have > 0) h.part[(int64_t)row * h.part_pitch + (h.v0 + col) / kCols] = make_float2(most, (sum[0] + sum[1]) + (sum[2] + sum[3]));
             }
             if constexpr (STEP == HeadStep::kProbs) {
                 const bool valid = row < it.rows_end;
                 const float lse = valid ? h.lse[row] : -INFINITY, g = valid ? h.g[row] : 0.f;
                 const bool none = lse == -INFINITY;                // no token, or nothing but logits of minus infinity
                 const int target = valid ? h.targets[row] - (int)(h.v0 + col) : -1;
-                const bool here = target >= 0 && target < HN;
+                const bool here = target >= 0 && target < kCols;
                 // p - [the target], times -g
 #pragma unroll
-                for (int c = 0; c < HN; ++c) {
+                for (int c = 0; c < kCols; ++c) {
                     const float d = fmaf(acc[c], h.scale, -lse), t = d * kLog2e;
                     float p = exp2_fast(t);
                     if (h.prob_terms > 2) p = fmaf(p, (fmaf(d, kLog2e, -t) + d * kLog2eRest) * 0.69314718f, p);      // what t is off by
@@ -396,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                 }
                 for (int t = 0; t < h.prob_terms; ++t) {
 #pragma unroll
-                    for (int c0 = 0; c0 < HN; c0 += 64) {
+                    for (int c0 = 0; c0 < kCols; c0 += 64) {
                         if (col + c0 >= h.piece || warp_row >= h.slots) break;
                         open_box();
 #pragma unroll
@@ -419,21 +418,21 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
             }
             if constexpr (STEP == HeadStep::kInputs) {
 #pragma unroll
-                for (int c0 = 0; c0 < HN; c0 += 32) {
+                for (int c0 = 0; c0 < kCols; c0 += 32) {
                     if (col + c0 >= h.cols || warp_row >= h.slots) break;
                     open_box();
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
                         put16(q, make_uint4(__float_as_uint(acc[c0 + q * 4]), __float_as_uint(acc[c0 + q * 4 + 1]), __float_as_uint(acc[c0 + q * 4 + 2]), __float_as_uint(acc[c0 + q * 4 + 3])));
                     if (it.split == 0) close_box(&map_out, h.accumulate, col + c0, warp_row, 0);
-                    else close_box(&map_extra, h.accumulate, half * HN + c0, it.extra * kPairRows + rank * kHalfRows + quad * 32, 0);
+                    else close_box(&map_extra, h.accumulate, part_col + c0, it.extra * kPairRows + rank * kHalfRows + quad * 32, 0);
                 }
             }
             if constexpr (STEP == HeadStep::kWeights) {
                 if (!args.manual_stores) {
-                    constexpr int kCols = 128 / sizeof(P), kPer = 16 / sizeof(P);
+                    constexpr int kSpan = 128 / sizeof(P), kPer = 16 / sizeof(P);
 #pragma unroll
-                    for (int c0 = 0; c0 < HN; c0 += kCols) {
+                    for (int c0 = 0; c0 < kCols; c0 += kSpan) {
                         if (col + c0 >= h.cols || warp_row >= it.rows_end) break;
                         open_box();
 #pragma unroll
@@ -446,19 +445,60 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                         }
                         close_box(&map_out, false, col + c0, (int)h.v0 + warp_row, it.group);
                     }
-                } else {                                            // rows of any alignment, 32 columns of a row at a time
-                    float *turned = reinterpret_cast<float *>(box);
+                } else {
                     const int rows = min(32, it.rows_end - warp_row);
-                    P *to = static_cast<P *>(h.dw) + it.group * h.lddw + (h.v0 + warp_row) * h.cols + col + lane;
+                    if constexpr (sizeof(P) == 4) {                 // rows of any alignment: 32 columns of a row at a time
+                        static_assert(STEP != HeadStep::kWeights || 32 * 33 * 4 <= S::kBoxes * kBox, "32 rows of 32 sums, a word apart");
+                        float *turned = reinterpret_cast<float *>(box);
+                        P *to = static_cast<P *>(h.dw) + it.group * h.lddw + (h.v0 + warp_row) * h.cols + col + lane;
 #pragma unroll
-                    for (int c0 = 0; c0 < HN; c0 += 32) {
+                        for (int c0 = 0; c0 < kCols; c0 += 32) {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) turned[lane * 33 + k] = acc[c0 + k];
-                        __syncwarp();
-                        if (col + c0 + lane < h.cols)
+                            for (int k = 0; k < 32; ++k) turned[lane * 33 + k] = acc[c0 + k];
+                            __syncwarp();
+                            if (col + c0 + lane < h.cols)
 #pragma unroll 4
-                            for (int r = 0; r < rows; ++r) put(to + r * h.cols + c0, turned[r * 33 + lane]);
-                        __syncwarp();
+                                for (int r = 0; r < rows; ++r) put(to + r * h.cols + c0, turned[r * 33 + lane]);
+                            __syncwarp();
+                        }
+                    } else {
+                        // Rows of any alignment: 128 bytes of 32 rows by way of shared memory (a row's 16-byte pieces turned about by the row, so that neither lanes
+                        // along a row nor lanes along the rows meet in a bank), then 16 bytes at a time to where memory has such a boundary, put together from two
+                        // pieces, and single entries before the first and behind the last of them.  Eight lanes to a row.
+                        constexpr int kPer = 16 / sizeof(P), kLog = sizeof(P) == 2 ? 1 : 2, kSpan = 8 * kPer;
+                        const int l = lane & 7;
+#pragma unroll
+                        for (int c0 = 0; c0 < kCols; c0 += kSpan) {
+                            const int bytes = (int)min((int64_t)kSpan, h.cols - col - c0) << kLog;       // of a row
+                            if (bytes <= 0) break;
+                            __syncwarp();
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    v[e] = sizeof(P) == 4 ? __float_as_uint(acc[c0 + q * kPer + e]) : two_bf16(acc[c0 + q * kPer + e * 2], acc[c0 + q * kPer + (e * 2 + 1) % kPer]);
+                                put16(q, make_uint4(v[0], v[1], v[2], v[3]));
+                            }
+                            __syncwarp();
+                            uint8_t *to = reinterpret_cast<uint8_t *>(static_cast<P *>(h.dw) + it.group * h.lddw + (h.v0 + warp_row + (lane >> 3)) * h.cols + col + c0);
+#pragma unroll 4
+                            for (int r = lane >> 3; r < rows; r += 4, to += h.cols << (2 + kLog)) {
+                                const uint8_t *from = box + r * 128;
+                                const int off = (int)(reinterpret_cast<uintptr_t>(to) & 15);
+                                auto piece = [&](int q) { return *reinterpret_cast<const uint4 *>(from + (((q ^ r) & 7) << 4)); };
+                                // piece l of memory: bytes 16 l - off and on of the row
+                                const int at = 16 * l - off;
+                                const uint4 v = off == 0 ? piece(l) : shifted<sizeof(P)>(piece(l - 1), piece(l), (unsigned)(16 - off) & 15u);
+                                if (at >= 0 && at + 16 <= bytes) *reinterpret_cast<uint4 *>(to + at) = v;
+                                // what lies before the first whole piece, and behind the last one
+                                const int head = min(bytes, (16 - off) & 15), whole = (bytes - head) & ~15;
+                                for (int mine = l << kLog; mine < bytes - whole; mine += 8 << kLog) {
+                                    const int byte = mine < head ? mine : mine + whole;
+                                    *reinterpret_cast<P *>(to + byte) = *reinterpret_cast<const P *>(from + ((((byte >> 4) ^ r) & 7) << 4) + (byte & 15));
+                                }
+                            }
+                        }
                     }
                 }
             }
@@ -525,15 +565,15 @@ bool encode(CUtensorMap *map, const Operand &o, int box_cols, int box_rows) {
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, o.data, o.cols, o.rows, o.planes, o.row, o.plane, box_cols, box_rows);
 }
 
-template <HeadStep STEP, int N, typename P>
+template <HeadStep STEP, int N, int COLS, typename P>
 cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const CUtensorMap &extra, const KernelArgs &k, int64_t items, cudaStream_t s) {
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     static PerDeviceOnce once;
-    auto *kernel = head_tc_kernel<STEP, N, P>;
+    auto *kernel = head_tc_kernel<STEP, N, COLS, P>;
     if (once.need(device)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (Shape<STEP, N>::kSmem));
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (Shape<STEP, N, COLS>::kSmem));
         if (e != cudaSuccess) return e;
         once.mark(device);
     }
@@ -543,7 +583,7 @@ cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap
         const int64_t rounds = (items + pairs - 1) / pairs;
         pairs = (items + rounds - 1) / rounds;
     }
-    return launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(kThreads), (Shape<STEP, N>::kSmem), s, true, a, b, out, extra, k);
+    return launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(Shape<STEP, N, COLS>::kThreads), (Shape<STEP, N, COLS>::kSmem), s, true, a, b, out, extra, k);
 }
 
 template <int N>
@@ -561,17 +601,18 @@ cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
     if (items >= (int64_t)1 << 30) return cudaErrorInvalidValue;
     CUtensorMap a, b, out = {}, extra = {};
     if (!encode(&a, h.a, 64, weights ? kK : kHalfRows) || !encode(&b, h.b, 64, weights || inputs ? kK : HN)) return cudaErrorInvalidValue;
+    const bool brief = head_brief(h.pairs, h.cols);
     switch (h.step) {
         case HeadStep::kSums:
-            return launch<HeadStep::kSums, N, float>(a, b, out, extra, k, items, s);
+            return brief ? launch<HeadStep::kSums, N, 64, float>(a, b, out, extra, k, items, s) : launch<HeadStep::kSums, N, HN, float>(a, b, out, extra, k, items, s);
         case HeadStep::kProbs:
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, h.probs, h.piece, h.slots, h.prob_terms, h.prob_pitch, h.slots * h.prob_pitch, 64, 32)) return cudaErrorInvalidValue;
-            return launch<HeadStep::kProbs, N, float>(a, b, out, extra, k, items, s);
+            return brief ? launch<HeadStep::kProbs, N, 64, float>(a, b, out, extra, k, items, s) : launch<HeadStep::kProbs, N, HN, float>(a, b, out, extra, k, items, s);
         case HeadStep::kInputs:
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.parts, h.cols, h.slots, 1, h.parts_pitch, h.slots * h.parts_pitch, 32, 32) ||
                 !encode(&extra, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.extra, N, kHeadPairs * kPairRows, 1, N, kHeadPairs * kPairRows * N, 32, 32))
                 return cudaErrorInvalidValue;
-            return launch<HeadStep::kInputs, N, float>(a, b, out, extra, k, items, s);
+            return launch<HeadStep::kInputs, N, HN, float>(a, b, out, extra, k, items, s);
         case HeadStep::kWeights: break;
     }
     const bool bf16 = h.param_type == ZENO_BF16;
@@ -579,7 +620,7 @@ cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
     const int64_t plane = h.groups > 1 ? h.lddw : h.cols, limit = (int64_t)1 << 40;
     k.manual_stores = !(reinterpret_cast<uintptr_t>(h.dw) % 16 == 0 && h.cols * size % 16 == 0 && plane * size % 16 == 0 && plane * size < limit &&
                         encode(&out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, size, h.dw, h.cols, h.vocab, h.groups, h.cols, plane, 128 / size, 32));
-    return bf16 ? launch<HeadStep::kWeights, N, __nv_bfloat16>(a, b, out, extra, k, items, s) : launch<HeadStep::kWeights, N, float>(a, b, out, extra, k, items, s);
+    return bf16 ? launch<HeadStep::kWeights, N, HN, __nv_bfloat16>(a, b, out, extra, k, items, s) : launch<HeadStep::kWeights, N, HN, float>(a, b, out, extra, k, items, s);
 }
 
 }  // namespace
