@@ -218,3 +218,358 @@ def test_waits_that_run_out_are_reported(act, par):
     assert torch.equal(again.logprobs, want.logprobs) and torch.equal(again.lse, want.lse)
     assert torch.equal(zeno.linear_logprobs_gradient(x, w, targets, want.lse, gl, dweight=dw), dx) and torch.equal(dw, kept)
     zeno.check_operator_status()
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    m, n, cols, vocab = 2, 3, 8, 5
+    t = torch.zeros(m, n, device="cuda", dtype=torch.int32)
+    x, w = torch.zeros(m, n, cols, device="cuda"), torch.zeros(vocab, cols, device="cuda")
+    p = torch.zeros(m, n, device="cuda")
+    dw = torch.zeros(m, vocab, cols, device="cuda")
+    good = zeno.linear_logprobs(x, w, t)
+    assert torch.allclose(good.lse, torch.full_like(p, 5.0).log())
+    bad = [lambda: zeno.embed(t.long(), w), lambda: zeno.embed(t, w.half()), lambda: zeno.embed(t, w[:, ::2]), lambda: zeno.embed(t, w.expand(3, vocab, cols)),
+           lambda: zeno.embed(t.t(), w), lambda: zeno.embed(t, w, out=x[:, :2]), lambda: zeno.embed(t, w, dtype=BF16, out=x),
+           lambda: zeno.embed_gradient(t, x, w), lambda: zeno.embed_gradient(t, x[..., :7], dw), lambda: zeno.embed_gradient(t[:, :2], x, dw),
+           lambda: zeno.embed_gradient(t, x, dw.expand(m, vocab, cols)[:1]), lambda: zeno.linear_logprobs(x, w[:, :7], t), lambda: zeno.linear_logprobs(x, w, t.float()),
+           lambda: zeno.linear_logprobs(x, w.t().contiguous().t(), t), lambda: zeno.linear_logprobs(x, w, t.cpu()),
+           lambda: zeno.linear_logprobs_gradient(x, w, t, p.double(), p), lambda: zeno.linear_logprobs_gradient(x, w, t, p, p[:, :2]),
+           lambda: zeno.linear_logprobs_gradient(x, w, t, p, p, dweight=dw.to(BF16)), lambda: zeno.linear_logprobs_gradient(x, w, t, p, p, dweight=dw[0]),
+           lambda: zeno.linear_logprobs_gradient(x, w, t, p, p, dx=x[:, :2])]
+    for k, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            raise AssertionError(k)
+    # a gradient that all groups would write to the same place is the library's to refuse
+    with pytest.raises(zeno.ZenoError):
+        zeno.embed_gradient(t, x, dw[:1].expand(m, vocab, cols))
+
+
+def test_no_tokens_and_no_groups():
+    for act, par in TYPES:
+        V = torch.full((3, 70), NAN, device="cuda", dtype=par)
+        dw = V[:, 5:65].unflatten(1, (6, 10))
+        x, t = torch.zeros(3, 0, 10, device="cuda", dtype=act), torch.zeros(3, 0, device="cuda", dtype=torch.int32)
+        w = torch.ones(6, 10, device="cuda", dtype=par)
+        p = torch.zeros(3, 0, device="cuda")
+        assert zeno.embed(t, w).shape == (3, 0, 10) and zeno.linear_logprobs(x, w, t).lse.shape == (3, 0)
+        for write in (lambda: zeno.embed_gradient(t, x, dw), lambda: zeno.linear_logprobs_gradient(x, w, t, p, p, dweight=dw)):
+            V.fill_(NAN)
+            write()
+            assert (dw == 0).all() and torch.isnan(V[:, :5]).all() and torch.isnan(V[:, 65:]).all()
+        V.fill_(1.0)
+        zeno.embed_gradient(t, x, dw, add=True)
+        assert (V == 1).all()
+        empty = torch.zeros(0, 4, 10, device="cuda", dtype=act), torch.zeros(0, 4, device="cuda", dtype=torch.int32)
+        assert zeno.embed(empty[1], w).shape == (0, 4, 10) and zeno.linear_logprobs(empty[0], w, empty[1]).lse.shape == (0, 4)
+        # tokens, none of which carries anything: gradients are zero, nothing is read
+        x, t = torch.full((3, 70, 10), NAN, device="cuda", dtype=act), torch.full((3, 70), -1, device="cuda", dtype=torch.int32)
+        p = torch.full((3, 70), NAN, device="cuda")
+        s = zeno.linear_logprobs(x, w, t)
+        assert (s.lse == 0).all() and (s.logprobs == 0).all()
+        V.fill_(NAN)
+        assert (zeno.linear_logprobs_gradient(x, w, t, p, p, dweight=dw) == 0).all() and (dw == 0).all()
+
+
+@pytest.mark.parametrize("n", [2, 40])
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_values_that_are_not_finite(act, n):
+    """One row's infinity or NaN is that row's; a word whose logits are minus infinity has probability zero."""
+    g = _gen(n)
+    cols, vocab = 64, 300
+    x, w = _head(g, 1, n, cols, vocab, act, act)
+    t = torch.randint(1, vocab, (1, n), generator=g, device="cuda").int()
+    clean = zeno.linear_logprobs(x, w, t)
+    for value in (NAN, INF):
+        y = x.clone()
+        y[0, 1, 7] = value
+        got = zeno.linear_logprobs(y, w, t)
+        assert torch.isnan(got.lse[0, 1]) and torch.isnan(got.logprobs[0, 1])
+        assert torch.equal(got.lse[0, :1], clean.lse[0, :1]) and torch.equal(got.lse[0, 2:], clean.lse[0, 2:])
+        dx = zeno.linear_logprobs_gradient(y, w, t, got.lse, torch.ones(1, n, device="cuda"))
+        assert torch.isnan(dx[0, 1]).all() and torch.isfinite(dx[0, 0]).all() and torch.isfinite(dx[0, 2:]).all()
+    # hidden states with a positive first entry, and a word that only has minus a lot there
+    x = x.abs()
+    w = w.clone()
+    w[0] = 0.0
+    w[0, 0] = -3e38
+    x[..., 0] = 1.0
+    got = zeno.linear_logprobs(x, w, t)
+    want = E.logprobs(x, w[1:], t - 1, 1.0)                     # without that word
+    R.assert_near(got.logprobs, want[0], want[2], "logprobs")
+    R.assert_near(got.lse, want[1], want[3], "lse")
+    # and as the target
+    t[0, 0] = 0
+    got = zeno.linear_logprobs(x, w, t)
+    assert got.logprobs[0, 0] < -2.9e38 and torch.isfinite(got.lse).all()
+
+
+BIG = [(60, 5, 40, 300, True, F32, F32), (60, 70, 72, 200, True, BF16, BF16), (1, 5000, 72, 600, False, BF16, BF16), (2, 3000, 64, 9000, False, F32, F32),
+       (1, 2600, 2100, 3000, False, BF16, BF16), (1, 14, 8192, 12000, False, F32, F32), (3, 900, 100, 40000, False, BF16, F32)]
+
+
+@pytest.mark.parametrize("m,n,cols,vocab,models,act,par", BIG)
+def test_many_groups_tiles_and_pieces(m, n, cols, vocab, models, act, par):
+    """More groups than shared memory has room for, more rows than a band, a vocabulary of several pieces, tiles that are cut."""
+    g = _gen(m + n)
+    targets = _tokens(g, m, n, vocab)
+    x, w = _head(g, m, n, cols, vocab, act, par, models)
+    given = (targets >= 0) & (targets < vocab)
+    clean = torch.where(given.unsqueeze(-1), x, 0.0)
+    want = E.logprobs(clean, w, targets, 1.0)
+    got = zeno.linear_logprobs(x, w, targets)
+    R.assert_near(got.logprobs, want[0], want[2], "logprobs")
+    R.assert_near(got.lse, want[1], want[3], "lse")
+    gl = torch.randn(m, n, generator=g, device="cuda")
+    into, V = _slice(m, vocab * cols, par)
+    into = into.unflatten(1, (vocab, cols))
+    dx = zeno.linear_logprobs_gradient(x, w, targets, got.lse, gl, dweight=into)
+    for i in range(0, m, 1 if m < 5 else 13):
+        wi = w[i:i + 1] if models else w
+        ref = E.logprobs_gradient(clean[i:i + 1], wi, targets[i:i + 1], got.lse[i:i + 1], gl[i:i + 1], 1.0, F32 if F32 in (act, par) else BF16)
+        R.assert_near(dx[i:i + 1], ref[0], ref[2], "dx")
+        R.assert_near(into[i:i + 1], ref[1], ref[3], "dw")
+    _around_is_nan(V, vocab * cols)
+    zeno.check_operator_status()
+
+
+def test_gradients_against_differences():
+    """In binary32, the loss's slope along a direction against both gradients."""
+    g = _gen(9)
+    m, n, cols, vocab, scale = 1, 20, 48, 90, 0.7
+    x, w = _head(g, m, n, cols, vocab, F32, F32, scale=scale)
+    t = torch.randint(0, vocab, (m, n), generator=g, device="cuda").int()
+    gl = torch.randn(m, n, generator=g, device="cuda")
+    s = zeno.linear_logprobs(x, w, t, scale=scale)
+    dw = torch.empty(m, vocab, cols, device="cuda")
+    dx = zeno.linear_logprobs_gradient(x, w, t, s.lse, gl, dweight=dw, scale=scale)
+    ux, uw = torch.randn_like(x), torch.randn_like(w) * 0.1
+
+    def loss(h):
+        z = scale * ((x + h * ux).double() @ (w + h * uw).double().T)
+        return (torch.log_softmax(z, -1).gather(-1, t.long().unsqueeze(-1)).squeeze(-1) * gl).sum()
+
+    h = 2.0 ** -10
+    slope = (loss(h) - loss(-h)) / (2 * h)
+    along = (dx.double() * ux).sum() + (dw[0].double() * uw).sum()
+    # the third derivative's share is h^2/6 of a few units, x + h u rounds to 2^-24 of itself
+    assert abs(float(slope - along)) <= 2e-4 * float((dx * ux).abs().sum() + (dw[0] * uw).abs().sum())
+    # the embedding: linear, so that a difference is exact but for rounding
+    table, dy = torch.randn(vocab, cols, generator=g, device="cuda"), torch.randn(m, n, cols, generator=g, device="cuda")
+    de = zeno.embed_gradient(t, dy, torch.empty(1, vocab, cols, device="cuda"), scale=scale)
+    u = torch.randn_like(table)
+    change = ((zeno.embed(t, table + u, scale=scale).double() - zeno.embed(t, table - u, scale=scale).double()) / 2 * dy.double()).sum()
+    assert abs(float(change - (de[0].double() * u).sum())) <= 1e-5 * float((de[0] * u).abs().sum())
+
+
+def test_offsets_beyond_32_bits():
+    """Tables, gradients and rows of more than 2^31 entries."""
+    g = _gen(3)
+    cols, vocab = 4096, (1 << 19) + 77
+    table = torch.zeros(vocab, cols, device="cuda", dtype=BF16)
+    at = torch.tensor([[0, vocab - 1, 300000, vocab - 1, -1, (1 << 19) + 3]], device="cuda", dtype=torch.int32)
+    rows = at[0, [0, 1, 2, 5]].long()
+    table[rows] = torch.randn(4, cols, generator=g, device="cuda").to(BF16)
+    y = zeno.embed(at, table, scale=2.0)
+    R.assert_near(y, *E.embed(at, table, 2.0))
+    far = torch.empty((1 << 31) + 8 + 6 * cols, device="cuda", dtype=BF16).as_strided((2, 3, cols), ((1 << 31) + 8, cols, 1))
+    far.copy_(y.view(2, 3, cols))
+    two = torch.full((2 * vocab * cols + 8,), NAN, device="cuda", dtype=BF16)
+    dtable = two[8:].view(2, vocab, cols)
+    zeno.embed_gradient(at.view(2, 3), far, dtable)
+    for i in range(2):
+        ids = at.view(2, 3)[i]
+        want = torch.zeros(4, cols, device="cuda", dtype=torch.float64)
+        for k in range(3):
+            want += torch.where((rows == ids[k]).unsqueeze(1), far[i, k].double(), 0.0)
+        R.assert_near(dtable[i, rows], want, 4 * R.U * want.abs(), "row sums")
+        dtable[i, rows] = 0
+        assert not dtable[i].any()
+    # the same table as output weights: nearly all logits are zero
+    x = torch.randn(1, 2, cols, generator=g, device="cuda").to(BF16) / 64
+    t = torch.tensor([[vocab - 1, 5]], device="cuda", dtype=torch.int32)
+    for n in (2, 6):
+        xs, ts = x.repeat(1, n // 2, 1), t.repeat(1, n // 2)
+        got = zeno.linear_logprobs(xs, table, ts)
+        z = xs[0].double() @ table[rows].double().T
+        lse = torch.log((vocab - 4) + z.exp().sum(-1))
+        off = 200 * R.U * (1 + (xs[0].double().abs() @ table[rows].double().abs().T).amax(-1))
+        R.assert_near(got.lse[0], lse, off, "lse")
+        zt = torch.where(ts[0] == vocab - 1, z[:, 1], 0.0)
+        R.assert_near(got.logprobs[0], zt - lse, 2 * off, "logprobs")
+    gl = torch.ones(1, 2, device="cuda")
+    s = zeno.linear_logprobs(x, table, t)
+    two.fill_(NAN)
+    dx = zeno.linear_logprobs_gradient(x, table, t, s.lse, gl, dweight=dtable[:1])
+    p = torch.exp(-s.lse[0].double())
+    for word in (5, 12345, vocab - 2):
+        want = (((t[0] == word).double() - p).unsqueeze(1) * x[0].double()).sum(0)
+        R.assert_near(dtable[0, word], want, (2.0 ** -15 + 1e-5) * ((((t[0] == word).double() + p).unsqueeze(1)) * x[0].double().abs()).sum(0), "dw")
+    assert torch.isfinite(dtable[0]).all() and torch.isnan(two[:8]).all() and torch.isfinite(dx).all()
+
+
+def _every_call(seed, stream=None, act=BF16, m=3, n=65, cols=136, vocab=1000):
+    """Both ends once; returns their outputs, and the inputs that a later pass may change."""
+    g = _gen(seed)
+    t = _tokens(g, m, n, vocab)
+    x, w = _head(g, m, n, cols, vocab, act, act)
+    gl = torch.randn(m, n, generator=g, device="cuda")
+    V = torch.zeros(m, vocab * cols, device="cuda", dtype=act)
+    dw = V.unflatten(1, (vocab, cols))
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+
+    def run():
+        y = zeno.embed(t, w, scale=3.0, stream=stream)
+        s = zeno.linear_logprobs(x, w, t, stream=stream)
+        one = zeno.linear_logprobs(x[:, :1].contiguous() if stream is None else x, w, t[:, :1].contiguous() if stream is None else t, stream=stream)
+        dx = zeno.linear_logprobs_gradient(x, w, t, s.lse, gl, dweight=dw, stream=stream)
+        zeno.embed_gradient(t, dx, dw, scale=3.0, add=True, stream=stream)
+        return [y, *s, one.lse[:, :1], dx, V]
+    return run, (x, t, gl)
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_the_same_bits_again_and_on_another_stream(act):
+    run, _ = _every_call(1, act=act)
+    first = [v.clone() for v in run()]
+    assert all(torch.equal(p, q) for p, q in zip(first, run()))
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(20_000_000)                               # the default stream is busy: nothing may be waited for there
+    run, _ = _every_call(1, stream=side, act=act)
+    got = run()
+    side.synchronize()
+    for k, (p, q) in enumerate(zip(first, got)):
+        if k != 3:                                              # there all of the tokens, here one of each group
+            assert torch.equal(p, q), k
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_captured_and_replayed_on_other_values(act):
+    run, inputs = _every_call(4, act=act)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = run()
+    fresh, other = _every_call(5, act=act)
+    for p, q in zip(inputs, other):                             # other tokens, and other ones of them that carry nothing
+        p.copy_(q)
+    want = [v.clone() for v in run()]
+    for v in outs:
+        v.zero_()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(outs, want))
+    del fresh
+
+
+def test_two_graphs_replayed_side_by_side():
+    made = []
+    for seed in (6, 7):
+        run, _ = _every_call(seed)
+        want = [v.clone() for v in run()]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = run()
+        made.append((graph, outs, want, run))                   # run holds the inputs that the graph reads
+    streams = [torch.cuda.Stream() for _ in made]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (graph, *_), s in zip(made, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, outs, want, _ in made:
+        assert all(torch.equal(p, q) for p, q in zip(outs, want))
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_calls_that_follow_one_another(act):
+    """Calls of other sizes right behind each other, their workspaces in the same memory, on two streams at once."""
+    sizes = [(1, 1, 64, 500), (2, 300, 64, 500), (1, 40, 1031, 70), (3, 9, 264, 2000)]
+    made = []
+    for k, (m, n, cols, vocab) in enumerate(sizes):
+        g = _gen(k)
+        t = _tokens(g, m, n, vocab, 0.0)
+        x, w = _head(g, m, n, cols, vocab, act, act)
+        gl = torch.randn(m, n, generator=g, device="cuda")
+        s = zeno.linear_logprobs(x, w, t)
+        torch.cuda.synchronize()
+        dw = torch.empty(m, vocab, cols, device="cuda", dtype=act)
+        dx = zeno.linear_logprobs_gradient(x, w, t, s.lse, gl, dweight=dw)
+        torch.cuda.synchronize()
+        de = zeno.embed_gradient(t, x, torch.empty_like(dw))
+        torch.cuda.synchronize()
+        made.append((x, w, t, gl, s, dx, dw, de))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for turn in range(6):
+        for k, (x, w, t, gl, s, dx, dw, de) in enumerate(made):
+            with torch.cuda.stream(streams[(turn + k) % 2]):
+                a, b, c = zeno.linear_logprobs(x, w, t), torch.empty_like(dw), torch.empty_like(dw)
+                d = zeno.linear_logprobs_gradient(x, w, t, s.lse, gl, dweight=b)
+                zeno.embed_gradient(t, x, c)
+                got.append((k, a, d, b, c))
+    torch.cuda.synchronize()
+    for k, a, d, b, c in got:
+        _, _, _, _, s, dx, dw, de = made[k]
+        assert torch.equal(a.lse, s.lse) and torch.equal(a.logprobs, s.logprobs) and torch.equal(d, dx) and torch.equal(b, dw) and torch.equal(c, de), k
+
+
+def test_workers_gradients_of_a_tied_language_model_and_the_step_on_them():
+    """Workers' gradients of a small model whose embedding is its output layer (embedding, norm layer, token loss) through the operators into the rows of V,
+    against the derivatives in 64 bits; then a failure, the candidates' losses on the server's tokens, and the average of the best."""
+    m, n, cols, vocab, scale = 6, 33, 96, 250, 4.0
+    g = _gen(11)
+    d = vocab * cols + 2 * cols
+    params = torch.cat([0.3 * torch.randn(vocab * cols, generator=g, device="cuda"), torch.ones(cols, device="cuda"), torch.zeros(cols, device="cuda")])
+    text = torch.randint(0, vocab, (m, n + 1), generator=g, device="cuda").int()
+    t, nxt = text[:, :-1].contiguous(), text[:, 1:].contiguous()
+    t[:, -4:], nxt[:, -5:] = -1, -1                             # padding, and the last token has no next one
+
+    def split(v):
+        return v[..., :vocab * cols].unflatten(-1, (vocab, cols)), v[..., vocab * cols:vocab * cols + cols], v[..., vocab * cols + cols:d]
+
+    W, w, b = split(params)
+    V = torch.full((m, d + 32), NAN, device="cuda")
+    dW, dw, db = split(V[:, :d])
+    h = zeno.embed(t, W, scale=scale)
+    y, mean, rstd = zeno.layer_norm(h, w, b)
+    s = zeno.linear_logprobs(y, W, nxt, scale=0.2)
+    count = int((nxt[0] >= 0).sum())
+    dy = zeno.linear_logprobs_gradient(y, W, nxt, s.lse, torch.full((m, n), -1.0 / count, device="cuda"), dweight=dW, scale=0.2)
+    dh = zeno.layer_norm_gradient(dy, h, w, mean, rstd, dw, db)
+    zeno.embed_gradient(t, dh, dW, scale=scale, add=True)
+    leaves = [p.double().repeat(m, *([1] * p.dim())).requires_grad_(True) for p in (W, w, b)]
+    losses = []
+    for i in range(m):
+        hi = torch.where((t[i] >= 0).unsqueeze(-1), scale * leaves[0][i][t[i].clamp(min=0).long()], 0.0)
+        yi = torch.nn.functional.layer_norm(hi, (cols,), leaves[1][i], leaves[2][i], eps=1e-5)
+        lp = torch.log_softmax(0.2 * yi @ leaves[0][i].T, -1)
+        losses.append(-(lp.gather(-1, nxt[i].clamp(min=0).long().unsqueeze(-1)).squeeze(-1) * (nxt[i] >= 0)).sum() / count)
+    grads = torch.autograd.grad(sum(losses), leaves)
+    for i in range(m):
+        assert abs(float(-s.logprobs[i].sum() / count - losses[i].detach())) <= 1e-5
+    for got, want in zip((dW, dw, db), grads):
+        assert float((got.double() - want).norm() / want.norm()) <= 1e-5
+    assert torch.isnan(V[:, d:]).all()
+    with zeno.Zeno(zeno.LOSS_LEAST_SQUARES, zeno.F32, (d, 1), False, m_max=m, n_r_max=4) as z:
+        z.inject_faults(V, torch.tensor([2], device="cuda", dtype=torch.int32), zeno.FAULT_SCALE, -20.0)
+        models = torch.cat([params.unsqueeze(0), params - 0.5 * V[:, :d]])
+        mW, mw, mb = split(models)
+        batch = torch.randint(0, vocab, (1, 41), generator=g, device="cuda").int()
+        ids, following = batch[:, :-1].repeat(m + 1, 1), batch[:, 1:].repeat(m + 1, 1)
+        hidden, _, _ = zeno.layer_norm(zeno.embed(ids, mW, scale=scale), mw, mb)
+        loss = -zeno.linear_logprobs(hidden, mW, following, scale=0.2).logprobs.double().mean(-1)
+        scores = (loss[0] - loss[1:] - 1e-4 * (V[:, :d].double() ** 2).sum(-1)).float()
+        assert int(scores.argmin()) == 2                        # the failure
+        kept = z.select(scores, 2)
+        assert 2 not in kept.tolist()
+        average = z.aggregate(V, kept)
+        want = V[kept.long(), :d].double().mean(0)
+        assert float((average.double() - want).norm() / want.norm()) <= 1e-6
+    zeno.check_operator_status()
