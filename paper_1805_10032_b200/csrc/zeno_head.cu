@@ -16,7 +16,7 @@ constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.
 struct Plan {
-    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, sum_words, few, few_blocks;
+    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, sum_blocks, sum_words, few, few_blocks;
     int64_t group_slots, slots, pitch, piece, parts_pitch, part_pitch;
     int64_t counts, begin, end, total, list, rank, target, lse, g, target_logit, x, w, part, probs, parts, extra, bytes;
 };
@@ -92,12 +92,13 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.pieces = (int)((a.vocab + most - 1) / most);
     p.piece = up((a.vocab + p.pieces - 1) / p.pieces, 256);
     // with few tiles of rows, pieces of as many tiles as make whole rounds
-    const int64_t row_tiles = up(p.group_slots, kHeadRows) / kHeadRows * p.groups, round = kHeadPairs / row_tiles * 256;
+    p.sum_blocks = p.group_slots <= 128 ? 1 : 2;
+    const int64_t row_tiles = up(p.group_slots, p.sum_blocks * 128) / (p.sum_blocks * 128) * p.groups, units = 2 * kHeadPairs / p.sum_blocks, round = units / row_tiles * 256;
     if (p.pieces > 1 && round > 0 && round <= most) p.piece = most / round * round;
     p.pieces = (int)((a.vocab + p.piece - 1) / p.piece);
-    // a tile of 128 columns where there are fewer of 256 than pairs of SMs
-    auto tile_for = [&](int64_t cols) { return row_tiles * (up(cols, 256) / 256) < kHeadPairs ? 128 : 256; };
-    p.sum_cols = tile_for(p.piece);
+    // a tile of 128 columns where there are fewer of 256 than there are SMs, or pairs, for them
+    const int64_t sum_tiles = row_tiles * (p.piece / 256);
+    p.sum_cols = sum_tiles < units ? 128 : 256;
     p.tile_cols = 256;                                                // its tiles are cut along the words instead
     p.most_splits = (int)(p.piece / 64 / 8);                          // parts of eight stages and more
     if (p.most_splits < 1) p.most_splits = 1;
@@ -164,23 +165,44 @@ __global__ void __launch_bounds__(kOrderThreads) head_order_kernel(const int32_t
     if (threadIdx.x == 0) counts[worker] = base;
 }
 
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
 // The leading 8 bits of what is left of each number, TERMS times: three hold a binary32 number exactly (from 2^-110 on; a smaller one has bits under
 // bfloat16's smallest step, 2^-133).  An infinity or NaN is its first term.
 template <int TERMS>
 __device__ __forceinline__ void put_terms(float (&f)[8], __nv_bfloat16 *to, int64_t plane) {
+    float most = 0.f;
+    bool number = true;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(f[k])), number = number && f[k] == f[k];
+    const bool plain = number && most <= 3.3895314e38f;                // bfloat16's largest: nothing rounds to infinity
 #pragma unroll
     for (int t = 0; t < TERMS; ++t) {
-        alignas(16) __nv_bfloat16 v[8];
+        uint32_t v[4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            v[k] = __float2bfloat16_rn(f[k]);
-            if (TERMS > 1) {
-                // (a finite number may round to infinity: then the term is the largest finite one)
-                if (fabsf(f[k]) < INFINITY && !(fabsf(__bfloat162float(v[k])) < INFINITY)) v[k] = __ushort_as_bfloat16(f[k] < 0.f ? 0xff7f : 0x7f7f);
-                f[k] = fabsf(f[k]) < INFINITY ? f[k] - __bfloat162float(v[k]) : 0.f;
+        for (int k = 0; k < 4; ++k) {
+            if (TERMS > 1 && !plain) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float &e = f[2 * k + i];
+                    __nv_bfloat16 h = __float2bfloat16_rn(e);
+                    // (a finite number may round to infinity: then the term is the largest finite one)
+                    if (fabsf(e) < INFINITY && !(fabsf(__bfloat162float(h)) < INFINITY)) h = __ushort_as_bfloat16(e < 0.f ? 0xff7f : 0x7f7f);
+                    e = fabsf(e) < INFINITY ? e - __bfloat162float(h) : 0.f;
+                    v[k] = i ? v[k] | (uint32_t)__bfloat16_as_ushort(h) << 16 : __bfloat16_as_ushort(h);
+                }
+                continue;
+            }
+            v[k] = two_bf16(f[2 * k], f[2 * k + 1]);
+            if (t + 1 < TERMS) {
+                f[2 * k] -= __uint_as_float(v[k] << 16);
+                f[2 * k + 1] -= __uint_as_float(v[k] & 0xffff0000u);
             }
         }
-        *reinterpret_cast<uint4 *>(to + t * plane) = *reinterpret_cast<const uint4 *>(v);
+        *reinterpret_cast<uint4 *>(to + t * plane) = make_uint4(v[0], v[1], v[2], v[3]);
     }
 }
 
@@ -198,19 +220,27 @@ struct Eight {
             if (row && c < cols && (k < kLoads || !vectors) && reinterpret_cast<uintptr_t>(words + k) < end) q[k] = words[k];
         }
     }
+    // of bfloat16: as they are, zeros behind the row's end
+    __device__ __forceinline__ uint4 bits(const T *row, int64_t c, int64_t cols, bool vectors) const {
+        uint4 v = vectors ? q[0] : shifted<2>(q[0], q[1], (unsigned)(reinterpret_cast<uintptr_t>(row + c) & 15));
+        if (!row || c + 8 > cols) {
+            const int left = row && c < cols ? (int)(cols - c) : 0;
+            auto keep = [&](uint32_t w, int at) { return left >= at + 2 ? w : left == at + 1 ? w & 0xffffu : 0u; };
+            v = make_uint4(keep(v.x, 0), keep(v.y, 2), keep(v.z, 4), keep(v.w, 6));
+        }
+        return v;
+    }
+    // of binary32
     __device__ __forceinline__ void get(float (&f)[8], const T *row, int64_t c, int64_t cols, bool vectors) const {
         const unsigned off = vectors ? 0u : (unsigned)(reinterpret_cast<uintptr_t>(row + c) & 15);
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             const uint4 v = vectors ? q[k] : shifted<sizeof(T)>(q[k], q[k + 1], off);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int i = 0; i < 16 / (int)sizeof(T); ++i) {
-                const int at = k * (16 / (int)sizeof(T)) + i;
-                const float e = sizeof(T) == 4 ? __uint_as_float(w[i % 4]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-                f[at] = row && c + at < cols ? e : 0.f;
-            }
+            f[4 * k] = __uint_as_float(v.x), f[4 * k + 1] = __uint_as_float(v.y), f[4 * k + 2] = __uint_as_float(v.z), f[4 * k + 3] = __uint_as_float(v.w);
         }
+        if (!row || c + 8 > cols)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = row && c + i < cols ? f[i] : 0.f;
     }
 };
 
@@ -224,9 +254,13 @@ __device__ __forceinline__ void rows_terms(const T *const (&from)[ROWS], __nv_bf
         for (int r = 0; r < ROWS; ++r) e[r].load(from[r], c, cols, vectors);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            float f[8];
-            e[r].get(f, from[r], c, cols, vectors);
-            if (to[r]) put_terms<TERMS>(f, to[r] + c, plane);
+            if constexpr (sizeof(T) == 2) {
+                if (to[r]) *reinterpret_cast<uint4 *>(to[r] + c) = e[r].bits(from[r], c, cols, vectors);
+            } else {
+                float f[8];
+                e[r].get(f, from[r], c, cols, vectors);
+                if (to[r]) put_terms<TERMS>(f, to[r] + c, plane);
+            }
         }
     }
 }
@@ -587,6 +621,7 @@ HeadTcArgs common(const HeadArgs &a, const Plan &p, HeadStep step) {
     h.scale = a.scale;
     h.targets = at<int>(a, p.target);
     h.tile_cols = p.sum_cols;
+    h.blocks = p.sum_blocks;
     return h;
 }
 
@@ -684,6 +719,7 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
             h.extra = at<float>(a, p.extra);
             h.most_splits = p.most_splits;
             h.tile_cols = p.tile_cols;
+            h.blocks = 2;
             h.accumulate = i > 0;
             e = launch_head_tc(h, s);
             if (e != cudaSuccess) break;
@@ -692,6 +728,7 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
             h.step = HeadStep::kWeights;
             h.bf16_result = param_type == ZENO_BF16;
             h.tile_cols = 256;
+            h.blocks = 2;
             h.a = probs;
             h.b = slots_operand(a, p);
             h.b_row0 = 0;

@@ -53,6 +53,7 @@ struct HeadTcArgs {
     int param_type;
     int bf16_result;                    // what comes of the sums is bfloat16
     int tile_cols;                      // columns of a tile: 256 or 128
+    int blocks;                         // of a tile: two, or (kSums, kProbs) one
     int last;                           // no kernel of the same call comes after this one
 };
 

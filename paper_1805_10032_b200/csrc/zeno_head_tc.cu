@@ -1,7 +1,7 @@
 // The products around the output layer on the tensor cores: logits with the sums of their exponentials, the probabilities' gradient from
 // logits computed again, and its two products.
 //
-// A pair of blocks (a cluster of two SMs) takes a tile of 256 rows by kN columns: the pair's instruction (cta_group::2, M = 256) reads 128 rows of A and
+// A pair of blocks (a cluster of two SMs; a single one, with a tile of 128 rows, for the logits of groups that have no more) takes a tile of 256 rows by kN columns: the pair's instruction (cta_group::2, M = 256) reads 128 rows of A and
 // half of the columns of B from each block's shared memory, so that a block copies half of what the tile needs, and leaves 128 rows of sums in either
 // block's TMEM.  Operands are bfloat16, in binary32 sums; a binary32 operand is three terms whose products are summed one pair of terms after the other, the
 // leading pair last.  X and W lie with the contraction's index contiguous for the logits ("K-major"); P W takes W, and P^T X both, with the index of the
@@ -18,15 +18,16 @@ namespace zeno {
 
 namespace {
 
-constexpr int kHalfRows = 128, kPairRows = 256;
+constexpr int kBlockRows = 128;                     // rows of a tile that a block has
 constexpr int kK = 64;                               // contraction indices of a stage: 128 bytes
-constexpr int kABytes = kHalfRows * kK * 2;
+constexpr int kABytes = kBlockRows * kK * 2;
 constexpr int kBox = 4096;                           // 32 rows of 128 bytes of a warp on their way out
 constexpr int kBoundsKept = 48;                      // groups whose bounds are kept in shared memory
 
-template <HeadStep STEP, int N, int COLS>
+template <HeadStep STEP, int N, int COLS, int BLOCKS>
 struct Shape {
-    static constexpr int kHalf = N / 2;
+    static constexpr int kHalf = N / BLOCKS;                             // of the columns, in a block
+    static constexpr int kRows = BLOCKS * kBlockRows;
     static constexpr int kBBytes = kHalf * kK * 2;
     static constexpr int kStageBytes = kABytes + kBBytes;
     static constexpr int kCols = COLS;                                   // of a warp that takes sums
@@ -57,15 +58,24 @@ struct KernelArgs {
 __device__ __forceinline__ void remote_arrive(uint32_t addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
-// an arrival on the barrier at this place in both blocks, once the instructions so far have ended
-__device__ __forceinline__ void commit_to_both(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+// an arrival on the barrier at this place in all of a tile's blocks, once the instructions so far have ended
+template <int BLOCKS>
+__device__ __forceinline__ void commit_to_all(uint32_t bar) {
+    if constexpr (BLOCKS == 1) tc_commit(bar);
+    else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+template <int BLOCKS>
+__device__ __forceinline__ void mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (BLOCKS == 1)
+        asm volatile(
+            "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile(
+            "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 // MN-major operand: rows of 64 contiguous entries, one for each value of the contraction index; eight of them make a group of 1024 bytes, the next 64
 // entries lie kK rows on.
@@ -78,11 +88,15 @@ __device__ __forceinline__ uint64_t mn_major(uint32_t addr) {
     d |= (uint64_t)2 << 61;
     return d;
 }
-// A copy into this block's shared memory whose bytes are counted on a barrier of the pair's first block.
-__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
-        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+// A copy into this block's shared memory whose bytes are counted on a barrier of the tile's first block.
+template <int BLOCKS>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
+    if constexpr (BLOCKS == 1)
+        tma_load_3d(dst, map, c0, c1, c2, bar);
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
+            ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void store_box(const CUtensorMap *map, const void *smem, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(smem)), "r"(c0), "r"(c1), "r"(c2) : "memory");
@@ -114,11 +128,12 @@ struct Item {
     int group, row0, rows_end, col0, kb0, kb1, split, splits, extra;
 };
 
-template <HeadStep STEP, int N, int COLS, typename P>
-__global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+template <HeadStep STEP, int N, int COLS, int BLOCKS, typename P>
+__global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) head_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                               const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_extra, const KernelArgs args) {
-    using S = Shape<STEP, N, COLS>;
+    using S = Shape<STEP, N, COLS, BLOCKS>;
     constexpr int HN = S::kHalf, kCols = COLS;
+    static_assert(BLOCKS == 2 || STEP == HeadStep::kSums || STEP == HeadStep::kProbs, "few rows");
     constexpr bool kAMn = STEP == HeadStep::kWeights, kBMn = STEP == HeadStep::kWeights || STEP == HeadStep::kInputs;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // full, empty [kStages]; dfull, dempty [2]
@@ -134,7 +149,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
 
     const HeadTcArgs &h = args.h;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rank = (int)cluster_rank();
+    const int rank = BLOCKS == 1 ? 0 : (int)cluster_rank();
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *boxes = ring + S::kStages * S::kStageBytes;
     auto full = [&](int s) { return smem_u32(&bars[s]); };
@@ -152,26 +167,31 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
         }
         for (int q = 0; q < 2; ++q) {
             mbar_init(dfull(q), 1);
-            mbar_init(dempty(q), 2 * S::kEpiWarps);
+            mbar_init(dempty(q), BLOCKS * S::kEpiWarps);
         }
         mbar_init(smem_u32(&drain_bar), 1);
         mbar_init(smem_u32(&never_bar), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(2 * N) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        if constexpr (BLOCKS == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(2 * N) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(2 * N) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
     }
     tc_fence_before();
     __syncthreads();
-    cluster_barrier();                        // the other block's barriers are there
+    if (BLOCKS == 2) cluster_barrier();       // the other block's barriers are there
     tc_fence_after();
     pdl_wait();
     if (!h.last) pdl_launch_dependents();     // by a kernel of this call, never by the next call's
     const uint32_t tmem = tmem_base_slot;
     volatile int *abortp = &abort_state[0];
 
-    const uint32_t pair = blockIdx.x >> 1, pairs_of_blocks = gridDim.x >> 1;
+    const uint32_t pair = blockIdx.x / BLOCKS, pairs_of_blocks = gridDim.x / BLOCKS;
     // The tiles in their order: rows first within a band of kBand tiles, then columns, so that pairs next to one another share the columns' operand and all
     // of a band's rows stay in L2.
     const bool in_smem = h.groups <= kBoundsKept;
@@ -179,7 +199,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
     __syncthreads();
     auto begin_of = [&](int group) { return in_smem ? bounds[2 * group] : __ldcg(h.begin + group); };
     auto end_of = [&](int group) { return in_smem ? bounds[2 * group + 1] : __ldcg(h.end + group); };
-    const uint32_t row_tiles = STEP != HeadStep::kWeights && h.groups == 1 ? min(args.row_tiles, (bounds[1] + kPairRows - 1) / kPairRows) : args.row_tiles;
+    const uint32_t row_tiles = STEP != HeadStep::kWeights && h.groups == 1 ? min(args.row_tiles, (bounds[1] + S::kRows - 1) / S::kRows) : args.row_tiles;
     const uint32_t per_group = row_tiles * args.col_tiles, tiles = per_group * h.groups;
     // kInputs: whole rounds of tiles, then the rest of them, cut along the words so that it takes all pairs
     const uint32_t whole = STEP == HeadStep::kInputs ? tiles / pairs_of_blocks * pairs_of_blocks : tiles;
@@ -202,13 +222,13 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
         const HeadTile at = head_tile(tile - it.group * per_group, row_tiles, args.col_tiles);
         it.col0 = at.col * N;
         if (STEP == HeadStep::kWeights) {
-            it.row0 = at.row * kPairRows;                                 // words of the piece
+            it.row0 = at.row * S::kRows;                                 // words of the piece
             it.rows_end = (int)h.piece;
             it.kb0 = begin_of(it.group) / kK;
             it.kb1 = end_of(it.group) / kK;
         } else {
             it.rows_end = end_of(it.group);
-            it.row0 = begin_of(it.group) + at.row * kPairRows;
+            it.row0 = begin_of(it.group) + at.row * S::kRows;
             const int nkb = (int)(((STEP == HeadStep::kInputs ? h.piece : h.cols) + kK - 1) / kK);
             it.kb0 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * it.split / it.splits) : 0;
             it.kb1 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * (it.split + 1) / it.splits) : nkb;
@@ -223,16 +243,16 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
         // ------------------------------------------------------------------ copies, by one lane
         wait_for_nothing(smem_u32(&never_bar), abortp);
         if (elect_one()) {
-            const uint32_t first_full = cluster_addr(&bars[0], 0);
+            const uint32_t first_full = BLOCKS == 1 ? full(0) : cluster_addr(&bars[0], 0);
             int s = 0;
             uint32_t round = 0;
             bool ok = true;
             Item it;
             for (int li = 0; ok && get_item(li, it) && !*abortp; ++li) {
                 // (of rows that are not there the instructions may read anything)
-                const bool rows_here = kAMn || it.row0 + rank * kHalfRows < it.rows_end, rows_there = kAMn || it.row0 + (1 - rank) * kHalfRows < it.rows_end;
-                const uint32_t bytes = 2 * S::kBBytes + (rows_here ? kABytes : 0) + (rows_there ? kABytes : 0);
-                const int row = it.row0 + rank * kHalfRows, col = it.col0 + rank * HN;
+                const bool rows_here = kAMn || it.row0 + rank * kBlockRows < it.rows_end, rows_there = BLOCKS == 2 && (kAMn || it.row0 + (1 - rank) * kBlockRows < it.rows_end);
+                const uint32_t bytes = BLOCKS * S::kBBytes + (rows_here ? kABytes : 0) + (rows_there ? kABytes : 0);
+                const int row = it.row0 + rank * kBlockRows, col = it.col0 + rank * HN;
                 for (int from = it.kb0, pr = 0; ok && from < it.kb1; pr = pr + 1 == h.pairs ? 0 : pr + 1, from += pr == 0 ? args.drain : 0) {
                     const int plane_a = h.pair_a[pr], plane_b = (STEP == HeadStep::kWeights ? 0 : it.group * h.b_terms) + h.pair_b[pr];
                     for (int kb = from, to = min(it.kb1, from + args.drain); kb < to; ++kb) {
@@ -242,17 +262,17 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
                         if (rank == 0) mbar_expect_tx(full(s), bytes);
                         issued[rank][s] = (round + 1) * 4 + rows_there * 2 + rows_here;
                         if (kAMn) {
-                            tma_load_pair(to_a, &map_a, row, kb * kK, plane_a, bar);
-                            tma_load_pair(to_a + kK * 128, &map_a, row + 64, kb * kK, plane_a, bar);
+                            tma_load<BLOCKS>(to_a, &map_a, row, kb * kK, plane_a, bar);
+                            tma_load<BLOCKS>(to_a + kK * 128, &map_a, row + 64, kb * kK, plane_a, bar);
                         } else if (rows_here) {
-                            tma_load_pair(to_a, &map_a, kb * kK, row, plane_a, bar);
+                            tma_load<BLOCKS>(to_a, &map_a, kb * kK, row, plane_a, bar);
                         }
                         if (kBMn) {
                             const int k0 = STEP == HeadStep::kInputs ? (int)h.b_row0 + kb * kK : kb * kK;
-                            tma_load_pair(to_b, &map_b, col, k0, plane_b, bar);
-                            if (HN > 64) tma_load_pair(to_b + kK * 128, &map_b, col + 64, k0, plane_b, bar);
+                            tma_load<BLOCKS>(to_b, &map_b, col, k0, plane_b, bar);
+                            if (HN > 64) tma_load<BLOCKS>(to_b + kK * 128, &map_b, col + 64, k0, plane_b, bar);
                         } else {
-                            tma_load_pair(to_b, &map_b, kb * kK, (int)h.b_row0 + col, plane_b, bar);
+                            tma_load<BLOCKS>(to_b, &map_b, kb * kK, (int)h.b_row0 + col, plane_b, bar);
                         }
                         if (++s == S::kStages) {
                             s = 0;
@@ -266,7 +286,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
     } else if (warp == 1) {
         // ------------------------------------------------------------------ instructions, by one lane of the first block for both
         if (rank == 0 && elect_one()) {
-            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kAMn ? 1u : 0u) << 15) | ((kBMn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(kPairRows >> 4) << 24);
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kAMn ? 1u : 0u) << 15) | ((kBMn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(S::kRows >> 4) << 24);
             int s = 0;
             uint32_t ph = 0, drain = 0;                              // stretches so far
             bool ok = true;
@@ -285,9 +305,9 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
                         const uint64_t a_desc = kAMn ? mn_major(ab) : smem_desc_sw128(ab), b_desc = kBMn ? mn_major(bb) : smem_desc_sw128(bb);
 #pragma unroll
                         for (int k = 0; k < kK / 16; ++k)        // 16 contraction indices: 32 bytes of a row, or 16 rows of 128 bytes
-                            mma_pair(tmem + set * N, a_desc + k * (kAMn ? 2048 / 16 : 32 / 16), b_desc + k * (kBMn ? 2048 / 16 : 32 / 16), idesc, (uint32_t)(j | k));
-                        commit_to_both(empty(s));
-                        if (j + 1 == all) commit_to_both(dfull(set));
+                            mma<BLOCKS>(tmem + set * N, a_desc + k * (kAMn ? 2048 / 16 : 32 / 16), b_desc + k * (kBMn ? 2048 / 16 : 32 / 16), idesc, (uint32_t)(j | k));
+                        commit_to_all<BLOCKS>(empty(s));
+                        if (j + 1 == all) commit_to_all<BLOCKS>(dfull(set));
                         if (++s == S::kStages) {
                             s = 0;
                             ph ^= 1;
@@ -300,7 +320,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
     } else if (warp >= 2) {
         // ------------------------------------------------------------------ sums
         const int quad = warp & 3, part_col = ((warp - 2) >> 2) * kCols;         // TMEM lanes that this warp may access; its columns
-        const uint32_t remote_dempty = rank == 0 ? 0u : cluster_addr(&bars[2 * S::kStages + 2], 0);
+        const uint32_t remote_dempty = BLOCKS == 1 || rank == 0 ? 0u : cluster_addr(&bars[2 * S::kStages + 2], 0);
         uint8_t *box = boxes + (warp - 2) * S::kBoxes * kBox;
         int turn = 0;
         uint32_t drain = 0;
@@ -350,7 +370,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
                 }
             }
             if (!ok) break;
-            const int warp_row = it.row0 + rank * kHalfRows + quad * 32, row = warp_row + lane;
+            const int warp_row = it.row0 + rank * kBlockRows + quad * 32, row = warp_row + lane;
             const int col = it.col0 + part_col;                   // the first of this thread's columns
             if (STEP != HeadStep::kWeights && it.row0 >= it.rows_end) continue;
 
@@ -425,7 +445,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
                     for (int q = 0; q < 8; ++q)
                         put16(q, make_uint4(__float_as_uint(acc[c0 + q * 4]), __float_as_uint(acc[c0 + q * 4 + 1]), __float_as_uint(acc[c0 + q * 4 + 2]), __float_as_uint(acc[c0 + q * 4 + 3])));
                     if (it.split == 0) close_box(&map_out, h.accumulate, col + c0, warp_row, 0);
-                    else close_box(&map_extra, h.accumulate, part_col + c0, it.extra * kPairRows + rank * kHalfRows + quad * 32, 0);
+                    else close_box(&map_extra, h.accumulate, part_col + c0, it.extra * S::kRows + rank * kBlockRows + quad * 32, 0);
                 }
             }
             if constexpr (STEP == HeadStep::kWeights) {
@@ -511,7 +531,10 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
     __syncthreads();
     tc_fence_after();
     if (warp == 1 && rank == 0 && abort_state[0]) {                 // instructions may still be running
-        if (elect_one()) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&drain_bar)) : "memory");
+        if (elect_one()) {
+            if constexpr (BLOCKS == 1) tc_commit(smem_u32(&drain_bar));
+            else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&drain_bar)) : "memory");
+        }
         __syncwarp();
         for (uint32_t i = 0; i < kSpinLimit; ++i) {
             if (mbar_try_wait(smem_u32(&drain_bar), 0)) break;
@@ -521,20 +544,20 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
     }
     if (tid == 0) {
         // what the other block has to know
-        const uint32_t other = 1 - rank;
-        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(&other_gave_up, other)), "r"(abort_state[0]) : "memory");
+        if (BLOCKS == 1) other_gave_up = 0;
+        else asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(&other_gave_up, 1 - rank)), "r"(abort_state[0]) : "memory");
         if (rank != 0)
             for (int s = 0; s < S::kStages; ++s) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(&issued[1][s], 0)), "r"(issued[1][s]) : "memory");
         if (abort_state[0]) atomicAdd(&g_given_up, 1u);
     }
     __syncthreads();
-    cluster_barrier();                        // the other block's instructions, arrivals and reads have ended too
+    if (BLOCKS == 2) cluster_barrier();       // the other block's instructions, arrivals and reads have ended too
     if (abort_state[0] || other_gave_up) {
         // Copies still in flight must land before a block exits.  The blocks are at most one round of a stage apart: bytes that the other one's copies were to
         // bring are counted as here, or are now expected.
         if (tid == 0 && rank == 0)
             for (int s = 0; s < S::kStages; ++s) {
-                const uint32_t mine = issued[0][s] >> 2, theirs = issued[1][s] >> 2;
+                const uint32_t mine = issued[0][s] >> 2, theirs = BLOCKS == 1 ? mine : issued[1][s] >> 2;
                 const auto bytes = [&](uint32_t of_rows) { return (uint32_t)(S::kBBytes + (of_rows ? kABytes : 0)); };
                 if (mine > theirs)
                     asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(full(s)), "r"(bytes(issued[0][s] & 2)) : "memory");
@@ -545,9 +568,12 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS>::kThreads), 1) head_tc_k
                 }
             }
         __syncthreads();
-        cluster_barrier();
+        if (BLOCKS == 2) cluster_barrier();
     }
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * N) : "memory");
+    if (warp == 1) {
+        if constexpr (BLOCKS == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * N) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * N) : "memory");
+    }
 }
 
 uint32_t spin_limit = kSpinLimit;
@@ -565,34 +591,34 @@ bool encode(CUtensorMap *map, const Operand &o, int box_cols, int box_rows) {
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, o.data, o.cols, o.rows, o.planes, o.row, o.plane, box_cols, box_rows);
 }
 
-template <HeadStep STEP, int N, int COLS, typename P>
+template <HeadStep STEP, int N, int COLS, int BLOCKS, typename P>
 cudaError_t launch(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const CUtensorMap &extra, const KernelArgs &k, int64_t items, cudaStream_t s) {
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     static PerDeviceOnce once;
-    auto *kernel = head_tc_kernel<STEP, N, COLS, P>;
+    auto *kernel = head_tc_kernel<STEP, N, COLS, BLOCKS, P>;
     if (once.need(device)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (Shape<STEP, N, COLS>::kSmem));
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (Shape<STEP, N, COLS, BLOCKS>::kSmem));
         if (e != cudaSuccess) return e;
         once.mark(device);
     }
     // equal shares; kInputs cuts what is left over itself
-    int64_t pairs = head_pairs();
+    int64_t pairs = head_pairs() * (BLOCKS == 1 ? 2 : 1);
     if (STEP != HeadStep::kInputs) {
         const int64_t rounds = (items + pairs - 1) / pairs;
         pairs = (items + rounds - 1) / rounds;
     }
-    return launch_clustered(kernel, 2, dim3((unsigned)(2 * pairs)), dim3(Shape<STEP, N, COLS>::kThreads), (Shape<STEP, N, COLS>::kSmem), s, true, a, b, out, extra, k);
+    return launch_clustered(kernel, BLOCKS, dim3((unsigned)(BLOCKS * pairs)), dim3(Shape<STEP, N, COLS, BLOCKS>::kThreads), (Shape<STEP, N, COLS, BLOCKS>::kSmem), s, true, a, b, out, extra, k);
 }
 
-template <int N>
+template <int N, int BLOCKS>
 cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
-    constexpr int HN = N / 2;
+    constexpr int HN = N / 2, kRows = BLOCKS * kBlockRows;
     KernelArgs k = {};
     k.h = h;
     const bool weights = h.step == HeadStep::kWeights, inputs = h.step == HeadStep::kInputs;
-    k.row_tiles = (int)(((weights ? h.piece : h.group_slots) + kPairRows - 1) / kPairRows);
+    k.row_tiles = (int)(((weights ? h.piece : h.group_slots) + kRows - 1) / kRows);
     k.col_tiles = (int)(((weights || inputs ? h.cols : h.piece) + N - 1) / N);
     k.drain = h.bf16_result ? kDrainBf16 : h.pairs > 1 || inputs || weights ? kDrainTerms : kDrain;
     k.spin_limit = spin_limit;
@@ -600,19 +626,19 @@ cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
     if (items == 0) return cudaSuccess;
     if (items >= (int64_t)1 << 30) return cudaErrorInvalidValue;
     CUtensorMap a, b, out = {}, extra = {};
-    if (!encode(&a, h.a, 64, weights ? kK : kHalfRows) || !encode(&b, h.b, 64, weights || inputs ? kK : HN)) return cudaErrorInvalidValue;
+    if (!encode(&a, h.a, 64, weights ? kK : kBlockRows) || !encode(&b, h.b, 64, weights || inputs ? kK : N / BLOCKS)) return cudaErrorInvalidValue;
     const bool brief = head_brief(h.pairs, h.cols);
     switch (h.step) {
         case HeadStep::kSums:
-            return brief ? launch<HeadStep::kSums, N, 64, float>(a, b, out, extra, k, items, s) : launch<HeadStep::kSums, N, HN, float>(a, b, out, extra, k, items, s);
+            return brief ? launch<HeadStep::kSums, N, 64, BLOCKS, float>(a, b, out, extra, k, items, s) : launch<HeadStep::kSums, N, HN, BLOCKS, float>(a, b, out, extra, k, items, s);
         case HeadStep::kProbs:
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, h.probs, h.piece, h.slots, h.prob_terms, h.prob_pitch, h.slots * h.prob_pitch, 64, 32)) return cudaErrorInvalidValue;
-            return brief ? launch<HeadStep::kProbs, N, 64, float>(a, b, out, extra, k, items, s) : launch<HeadStep::kProbs, N, HN, float>(a, b, out, extra, k, items, s);
+            return brief ? launch<HeadStep::kProbs, N, 64, BLOCKS, float>(a, b, out, extra, k, items, s) : launch<HeadStep::kProbs, N, HN, BLOCKS, float>(a, b, out, extra, k, items, s);
         case HeadStep::kInputs:
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.parts, h.cols, h.slots, 1, h.parts_pitch, h.slots * h.parts_pitch, 32, 32) ||
-                !encode(&extra, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.extra, N, kHeadPairs * kPairRows, 1, N, kHeadPairs * kPairRows * N, 32, 32))
+                !encode(&extra, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.extra, N, kHeadPairs * kHeadRows, 1, N, kHeadPairs * kHeadRows * N, 32, 32))
                 return cudaErrorInvalidValue;
-            return launch<HeadStep::kInputs, N, HN, float>(a, b, out, extra, k, items, s);
+            return launch<HeadStep::kInputs, N, HN, 2, float>(a, b, out, extra, k, items, s);
         case HeadStep::kWeights: break;
     }
     const bool bf16 = h.param_type == ZENO_BF16;
@@ -620,12 +646,15 @@ cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
     const int64_t plane = h.groups > 1 ? h.lddw : h.cols, limit = (int64_t)1 << 40;
     k.manual_stores = !(reinterpret_cast<uintptr_t>(h.dw) % 16 == 0 && h.cols * size % 16 == 0 && plane * size % 16 == 0 && plane * size < limit &&
                         encode(&out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, size, h.dw, h.cols, h.vocab, h.groups, h.cols, plane, 128 / size, 32));
-    return bf16 ? launch<HeadStep::kWeights, N, HN, __nv_bfloat16>(a, b, out, extra, k, items, s) : launch<HeadStep::kWeights, N, HN, float>(a, b, out, extra, k, items, s);
+    return bf16 ? launch<HeadStep::kWeights, N, HN, 2, __nv_bfloat16>(a, b, out, extra, k, items, s) : launch<HeadStep::kWeights, N, HN, 2, float>(a, b, out, extra, k, items, s);
 }
 
 }  // namespace
 
-cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s) { return h.tile_cols == 128 ? launch_tiles<128>(h, s) : launch_tiles<256>(h, s); }
+cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s) {
+    if (h.blocks == 1) return h.tile_cols == 128 ? launch_tiles<128, 1>(h, s) : launch_tiles<256, 1>(h, s);
+    return h.tile_cols == 128 ? launch_tiles<128, 2>(h, s) : launch_tiles<256, 2>(h, s);
+}
 
 int head_pairs() {
     int device = 0, sms = 0;
