@@ -441,7 +441,7 @@ zeno_status zeno_embed_gradient(int32_t device, int32_t type, int32_t param_type
  * tensor cores add with truncation towards zero; sums go on in additions to nearest after every stretch of the contraction.
  * A row with a logit that is NaN or plus infinity gives NaN; in binary32 any infinity or NaN among its x or in w may.
  * Weights that are bfloat16, aligned to 16 bytes, in rows and groups of multiples of 8 entries, are read as they lie; others are
- * rewritten in the workspace, up to 512 MB of them at a time. */
+ * rewritten in the workspace, up to 768 MB of them at a time. */
 int64_t zeno_linear_logprobs_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols, int64_t vocab,
                                        const void *w, int64_t ldw);
 zeno_status zeno_linear_logprobs(int32_t device, int32_t type, int32_t param_type, const zeno_rows *x, int32_t m, int64_t n,

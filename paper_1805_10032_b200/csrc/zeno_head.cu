@@ -11,7 +11,7 @@ namespace zeno {
 
 namespace {
 
-constexpr int64_t kPieceBytes = (int64_t)128 << 20, kWeightBytes = (int64_t)512 << 20;
+constexpr int64_t kPieceBytes = (int64_t)128 << 20, kWeightBytes = (int64_t)768 << 20;
 constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.
@@ -91,9 +91,9 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     if (most < kMinPiece) most = kMinPiece;
     p.pieces = (int)((a.vocab + most - 1) / most);
     p.piece = up((a.vocab + p.pieces - 1) / p.pieces, 256);
-    // with few tiles of rows, pieces of as many tiles as make whole rounds
+    // with few tiles of rows, pieces of as many tiles as make whole rounds (however many of the tokens carry a target)
     p.sum_blocks = p.group_slots <= 128 ? 1 : 2;
-    const int64_t row_tiles = up(p.group_slots, p.sum_blocks * 128) / (p.sum_blocks * 128) * p.groups, units = 2 * kHeadPairs / p.sum_blocks, round = units / row_tiles * 256;
+    const int64_t row_tiles = up(p.group_slots, p.sum_blocks * 128) / (p.sum_blocks * 128) * p.groups, units = 2 * kHeadPairs / p.sum_blocks, round = (row_tiles <= 4 ? units : units / row_tiles) * 256;
     if (p.pieces > 1 && round > 0 && round <= most) p.piece = most / round * round;
     p.pieces = (int)((a.vocab + p.piece - 1) / p.piece);
     // a tile of 128 columns where there are fewer of 256 than there are SMs, or pairs, for them

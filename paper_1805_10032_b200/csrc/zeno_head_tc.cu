@@ -157,6 +157,10 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
     auto dfull = [&](int q) { return smem_u32(&bars[2 * S::kStages + q]); };
     auto dempty = [&](int q) { return smem_u32(&bars[2 * S::kStages + 2 + q]); };
 
+    if (tid == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+    }
     if (tid == 0) {
         abort_state[0] = 0;
         abort_state[1] = (int)args.spin_limit;
