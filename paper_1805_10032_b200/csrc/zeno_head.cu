@@ -99,7 +99,7 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     // a tile of 128 columns where there are fewer of 256 than there are SMs, or pairs, for them
     const int64_t sum_tiles = row_tiles * (p.piece / 256);
     p.sum_cols = sum_tiles < units ? 128 : 256;
-    p.tile_cols = 256;                                                // its tiles are cut along the words instead
+    p.tile_cols = a.cols <= 128 ? 128 : 256;                          // of the gradients: few tiles of dx are cut along the words instead
     p.most_splits = (int)(p.piece / 64 / 8);                          // parts of eight stages and more
     if (p.most_splits < 1) p.most_splits = 1;
     p.sum_words = head_part_words(p.sum_cols, p.x_terms, p.w_terms, a.cols);
@@ -727,7 +727,7 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
         if (a.dw) {
             h.step = HeadStep::kWeights;
             h.bf16_result = param_type == ZENO_BF16;
-            h.tile_cols = 256;
+            h.tile_cols = p.tile_cols;
             h.blocks = 2;
             h.a = probs;
             h.b = slots_operand(a, p);
