@@ -1,6 +1,6 @@
 // A language model's embedding, y_t = scale E[id_t], and its gradient for every worker, dE[v] = scale sum over the tokens with id v of dy_t.
 //
-// Forward: a lane gathers 16 bytes at a time (or an entry, of rows that start anywhere), two of four rows in flight; bound by memory.
+// Forward: a lane gathers 16 bytes at a time, two of four rows in flight; bound by memory.
 // Backward: every row of the table is written once, mostly zeros, and no row is summed by atomics.  A first kernel sorts each worker's token positions by
 // id: a block per class of ids counts what each of its warps finds in a stretch of the tokens, and places the positions, rows in order, positions
 // in order within a row.  The second one writes the rows without tokens, then walks over the sorted positions, a warp to 32 of them and 512 bytes of
@@ -50,7 +50,7 @@ struct Pack {
     }
 };
 
-// `lanes` (a power of two) lanes to a row, kRows rows and kPieces pieces of each in flight; blockIdx.y: which pieces of the rows.
+// 2^lanes_log2 lanes to a row, kRows rows and kPieces pieces of each in flight; blockIdx.y: which pieces of the rows.
 template <typename T, typename P, int N>
 __global__ void __launch_bounds__(256, 4) embed_kernel(const EmbedArgs a, int per_row, int rows, int lanes_log2) {
     constexpr int kRows = 4, kPieces = 2;
@@ -90,16 +90,76 @@ __global__ void __launch_bounds__(256, 4) embed_kernel(const EmbedArgs a, int pe
     }
 }
 
+// The same for rows that start anywhere: pieces of 16 bytes where the result's memory has such a boundary, put together from the aligned words around the
+// table's entries (of those that hold one of the row), entry by entry at a row's ends.
+template <typename T, typename P>
+__global__ void __launch_bounds__(256, 4) embed_ragged_kernel(const EmbedArgs a, int per_row, int rows, int lanes_log2) {
+    constexpr int kRows = 2, kPieces = 2, N = 16 / sizeof(T), kLoads = (N * (int)sizeof(P) + 15) / 16;
+    pdl_wait();
+    const int lane = threadIdx.x & 31, l = lane & ((1 << lanes_log2) - 1), sub = lane >> lanes_log2, at_once = 32 >> lanes_log2;
+    const int64_t row0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * kRows * at_once + sub;
+    const int piece0 = blockIdx.y * (kPieces << lanes_log2) + l;
+    uint4 in[kRows][kPieces][kLoads + 1];
+    int id[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) id[r] = row0 + r * at_once < rows ? a.tokens[row0 + r * at_once] : -1;
+    auto given = [&](int r) { return (uint32_t)id[r] < (uint64_t)a.vocab; };
+    auto to = [&](int r) { return static_cast<T *>(a.y.data) + a.y.at(row0 + r * at_once); };
+    auto table = [&](int r) { return static_cast<const P *>(a.table) + (a.ldt ? (uint32_t)(row0 + r * at_once) / (uint32_t)a.n * a.ldt : 0) + id[r] * a.cols; };
+    auto first = [&](int r, int k) { return (int64_t)(piece0 + (k << lanes_log2)) * N - (int)(reinterpret_cast<uintptr_t>(to(r)) % 16 / sizeof(T)); };      // entry of a piece
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k)
+#pragma unroll
+            for (int i = 0; i <= kLoads; ++i) {
+                in[r][k][i] = make_uint4(0, 0, 0, 0);
+                if (!given(r)) continue;
+                const uintptr_t begin = reinterpret_cast<uintptr_t>(table(r)), word = ((begin + first(r, k) * (int)sizeof(P)) & ~(uintptr_t)15) + i * 16;
+                if (word + 16 > begin && word < begin + a.cols * sizeof(P)) in[r][k][i] = *reinterpret_cast<const uint4 *>(word);
+            }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        if (row0 + r * at_once >= rows) break;
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            const int64_t c = first(r, k);
+            if (c >= a.cols || piece0 + (k << lanes_log2) >= per_row) continue;
+            const unsigned off = given(r) ? (unsigned)((reinterpret_cast<uintptr_t>(table(r)) + c * (int)sizeof(P)) & 15) : 0u;
+            Pack<P, N> e;
+            uint4 w[kLoads];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) w[i] = shifted<sizeof(P)>(in[r][k][i], in[r][k][i + 1], off);
+#pragma unroll
+            for (int i = 0; i < Pack<P, N>::kWords; ++i) {
+                const uint32_t q[4] = {w[i / 4].x, w[i / 4].y, w[i / 4].z, w[i / 4].w};
+                e.w[i] = q[i % 4];
+            }
+            Pack<T, N> out;
+#pragma unroll
+            for (int i = 0; i < N; ++i) out.set(i, given(r) ? a.scale * e.get(i) : 0.f);
+            T *at = to(r) + c;
+            if (c >= 0 && c + N <= a.cols) {
+                out.store(at);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (c + i >= 0 && c + i < a.cols) put(at + i, out.get(i));
+            }
+        }
+    }
+}
+
 template <typename T, typename P>
 cudaError_t embed(const EmbedArgs &a, cudaStream_t s) {
     constexpr int N = sizeof(T) + sizeof(P) == 4 ? 8 : 4;               // 16 bytes of the wider type
     const bool vectors = a.cols % N == 0 && aligned_to(a.y, a.m, a.n, sizeof(T), N * sizeof(T)) && reinterpret_cast<uintptr_t>(a.table) % (N * sizeof(P)) == 0 && a.ldt % N == 0;
-    const int64_t rows = a.m * a.n, per_row = vectors ? a.cols / N : a.cols;
+    const int64_t rows = a.m * a.n, per_row = vectors ? a.cols / N : a.cols / (16 / (int)sizeof(T)) + 2;
     int lanes_log2 = 0;
     while (lanes_log2 < 5 && (1 << lanes_log2) < per_row) ++lanes_log2;
-    const int64_t rows_per_block = 8 * 4 * (32 >> lanes_log2);
+    const int64_t rows_per_block = 8 * (vectors ? 4 : 2) * (32 >> lanes_log2);
     const dim3 grid((unsigned)((rows + rows_per_block - 1) / rows_per_block), (unsigned)((per_row + (2 << lanes_log2) - 1) / (2 << lanes_log2)));
-    auto *kernel = vectors ? embed_kernel<T, P, N> : embed_kernel<T, P, 1>;
+    auto *kernel = vectors ? embed_kernel<T, P, N> : embed_ragged_kernel<T, P>;
     return launch_chained(kernel, grid, dim3(256), 0, s, true, a, (int)per_row, (int)rows, lanes_log2);
 }
 

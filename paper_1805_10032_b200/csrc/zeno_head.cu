@@ -11,7 +11,7 @@ namespace zeno {
 
 namespace {
 
-constexpr int64_t kPieceBytes = (int64_t)128 << 20, kWeightBytes = (int64_t)768 << 20;
+constexpr int64_t kPieceBytes = (int64_t)256 << 20, kWeightBytes = (int64_t)768 << 20;
 constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.
