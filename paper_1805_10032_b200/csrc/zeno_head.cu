@@ -16,8 +16,8 @@ constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.
 struct Plan {
-    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, sum_blocks, sum_words, few, few_blocks;
-    int64_t group_slots, slots, pitch, piece, parts_pitch, part_pitch;
+    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, sum_blocks, sum_words, few, few_blocks, logits_parts;
+    int64_t group_slots, slots, pitch, piece, parts_pitch, part_pitch, logits_pitch;
     int64_t counts, begin, end, total, list, rank, target, lse, g, target_logit, x, w, part, probs, parts, extra, bytes;
 };
 
@@ -75,8 +75,8 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.x_terms = type == ZENO_F32 ? 3 : 1;
     p.w_terms = param_type == ZENO_F32 ? 3 : 1;
     p.w_packed = p.w_terms > 1 || !mappable(a.w, a.ldw, p.groups, a.cols);
-    // groups whose tiles of rows are written whole must not share one
-    const int64_t worker_slots = up(a.n, p.groups > 1 && gradient ? 256 : kSlots);
+    // groups whose tiles of rows are written whole must not share one (as the logits may be, and dx is)
+    const int64_t worker_slots = up(a.n, p.groups > 1 ? (gradient || a.n > 128 ? 256 : 128) : kSlots);
     p.slots = worker_slots * a.m;
     p.group_slots = p.groups > 1 ? worker_slots : p.slots;
     // Of bfloat16 operands D is bfloat16, too: its rounding, as large as the results', makes them off by 1.4 times that.  A few tokens' results may hang on one
@@ -99,6 +99,17 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     // a tile of 128 columns where there are fewer of 256 than there are SMs, or pairs, for them
     const int64_t sum_tiles = row_tiles * (p.piece / 256);
     p.sum_cols = sum_tiles < units ? 128 : 256;
+    // Few tiles of a long contraction: it is cut, the parts' logits are kept and joined by the kernel that needs them.  In one part a tile's stages follow one
+    // another on one SM or pair however idle the others are.
+    HeadTcArgs pairs = {};
+    set_pairs(&pairs, p.x_terms, p.w_terms);
+    const int64_t blocks_of_64 = (a.cols + 63) / 64, stages = blocks_of_64 * pairs.pairs;
+    int64_t logits_parts = units / sum_tiles;
+    if (logits_parts > stages / 8) logits_parts = stages / 8;
+    if (logits_parts > blocks_of_64) logits_parts = blocks_of_64;
+    // (A stage takes about a quarter of a microsecond, the parts' way through memory and the other kernel as much as some fifty.)
+    p.logits_parts = p.pieces == 1 && logits_parts > 1 && stages - stages / logits_parts >= 64 ? (int)logits_parts : 0;
+    p.logits_pitch = up(a.vocab, 4);
     p.tile_cols = a.cols <= 128 ? 128 : 256;                          // of the gradients: few tiles of dx are cut along the words instead
     p.most_splits = (int)(p.piece / 64 / 8);                          // parts of eight stages and more
     if (p.most_splits < 1) p.most_splits = 1;
@@ -122,7 +133,7 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.target_logit = take(gradient ? 0 : p.slots * 4);
     p.x = take(p.x_terms * p.slots * p.pitch * 2);
     p.w = take(per_word * p.piece);
-    p.part = take(gradient ? 0 : p.slots * p.part_pitch * 8);
+    p.part = take(p.logits_parts ? p.logits_parts * p.slots * p.logits_pitch * 4 : gradient ? 0 : p.slots * p.part_pitch * 8);
     p.probs = take(p.piece * per_prob);
     p.parts = take(gradient && a.dx.data ? p.slots * p.parts_pitch * 4 : 0);
     p.extra = take(gradient && a.dx.data ? (int64_t)kHeadPairs * kHeadRows * p.tile_cols * 4 : 0);
@@ -522,6 +533,91 @@ __global__ void __launch_bounds__(256) head_join_kernel(const HeadArgs a, const 
     }
 }
 
+// The sums of four neighbouring words' parts.
+__device__ __forceinline__ float4 four_logits(const float *parts, int count, int64_t plane) {
+    float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) {
+        const float4 v = *reinterpret_cast<const float4 *>(parts + i * plane);
+        z.x += v.x, z.y += v.y, z.z += v.z, z.w += v.w;
+    }
+    return z;
+}
+
+// lse and log probability of every token from its logits in parts: a block per token.
+__global__ void __launch_bounds__(256) head_logits_kernel(const HeadArgs a, const Plan p) {
+    __shared__ float2 of_warp[8];
+    __shared__ float target_logit;
+    pdl_wait();
+    const int64_t row = blockIdx.x;
+    const int rank = at<int>(a, p.rank)[row], lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (rank < 0) {
+        if (threadIdx.x == 0 && a.lse) a.lse[row] = 0.f;
+        if (threadIdx.x == 0 && a.logprobs) a.logprobs[row] = 0.f;
+        return;
+    }
+    const int64_t slot = at<int>(a, p.begin)[row / a.n] + rank, plane = p.slots * p.logits_pitch;
+    const float *logits = at<float>(a, p.part) + slot * p.logits_pitch;
+    const int target = a.targets[row];
+    float2 mine = make_float2(-INFINITY, 0.f);
+    for (int v0 = threadIdx.x * 4; v0 < (int)a.vocab; v0 += 1024) {
+        const float4 four = four_logits(logits + v0, p.logits_parts, plane);
+        float z[4] = {four.x * a.scale, four.y * a.scale, four.z * a.scale, four.w * a.scale};
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (v0 + k == target) target_logit = z[k];
+            if (v0 + k >= (int)a.vocab) z[k] = -INFINITY;
+            top = fmaxf(top, z[k]);
+        }
+        const float beside = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum += expf(z[k] - beside);
+        add_part(mine, top, sum);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const float top = __shfl_xor_sync(0xffffffffu, mine.x, d), sum = __shfl_xor_sync(0xffffffffu, mine.y, d);
+        add_part(mine, top, sum);
+    }
+    if (lane == 0) of_warp[warp] = mine;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < 8; ++w) add_part(mine, of_warp[w].x, of_warp[w].y);
+    const double beside = mine.x == -INFINITY ? 0. : mine.x, log_sum = log((double)mine.y);
+    if (a.lse) a.lse[row] = (float)(beside + log_sum);
+    if (a.logprobs) a.logprobs[row] = mine.y == 0.f ? -INFINITY : (float)((double)target_logit - beside - log_sum);
+}
+
+// D from logits in parts, eight words of a slot a thread: blockIdx.y is the group.
+template <int TERMS>
+__global__ void __launch_bounds__(256) head_probs_kernel(const HeadArgs a, const Plan p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int begin = p.groups > 1 ? at<int>(a, p.begin)[blockIdx.y] : 0, end = p.groups > 1 ? at<int>(a, p.end)[blockIdx.y] : at<int>(a, p.total)[1];
+    const int64_t per_row = p.piece / 8, total = (end - begin) * per_row, plane = p.slots * p.logits_pitch;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
+        const int64_t slot = begin + q / per_row, v0 = q % per_row * 8;
+        const float lse = at<float>(a, p.lse)[slot], g = at<float>(a, p.g)[slot];
+        const int target = at<int>(a, p.target)[slot];
+        const float *logits = at<float>(a, p.part) + slot * p.logits_pitch + v0;
+        float f[8] = {};
+        if (lse != -INFINITY)                              // else no token, or nothing but logits of minus infinity
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (v0 + 4 * h >= a.vocab) break;
+                const float4 four = four_logits(logits + 4 * h, p.logits_parts, plane);
+                const float z[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t v = v0 + 4 * h + k;
+                    f[4 * h + k] = v < a.vocab ? (expf(fmaf(z[k], a.scale, -lse)) - (v == target ? 1.f : 0.f)) * -g : 0.f;
+                }
+            }
+        put_terms<TERMS>(f, at<__nv_bfloat16>(a, p.probs) + slot * p.piece + v0, p.slots * p.piece);
+    }
+}
+
 // dx, four neighbouring entries a thread, rounded once; zero without a target.  Tiles that were cut have further parts.
 template <typename T>
 __global__ void __launch_bounds__(256) head_inputs_kernel(const HeadArgs a, const Plan p, uint32_t pairs, int vectors) {
@@ -625,6 +721,17 @@ HeadTcArgs common(const HeadArgs &a, const Plan &p, HeadStep step) {
     return h;
 }
 
+// Logits in parts.
+cudaError_t launch_logits(HeadTcArgs h, const HeadArgs &a, const Plan &p, cudaStream_t s) {
+    h.step = HeadStep::kLogits;
+    h.tile_cols = 256;
+    h.logits = at<float>(a, p.part);
+    h.logits_pitch = p.logits_pitch;
+    h.logits_parts = p.logits_parts;
+    h.bf16_result = 0;
+    return launch_head_tc(h, s);
+}
+
 Operand slots_operand(const HeadArgs &a, const Plan &p) { return Operand{at<void>(a, p.x), a.cols, p.slots, p.pitch, p.slots * p.pitch, p.x_terms}; }
 
 template <typename T, typename P, int R, bool VECTORS>
@@ -670,6 +777,10 @@ cudaError_t launch_head_logprobs(int type, int param_type, const HeadArgs &a, cu
         if (e != cudaSuccess) break;
         h.a = slots_operand(a, p);
         set_pairs(&h, p.x_terms, p.w_terms);
+        if (p.logits_parts) {
+            e = launch_logits(h, a, p, s);
+            return e == cudaSuccess ? launch_chained(head_logits_kernel, dim3((unsigned)(a.m * a.n)), dim3(256), 0, s, true, a, p) : e;
+        }
         h.part = at<float2>(a, p.part);
         h.part_pitch = p.part_pitch;
         h.target_logit = at<float>(a, p.target_logit);
@@ -706,7 +817,15 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
         h.prob_pitch = p.piece;
         h.prob_terms = p.prob_terms;
         h.bf16_result = p.prob_terms < 3;
-        e = launch_head_tc(h, s);
+        if (p.logits_parts) {
+            e = launch_logits(h, a, p, s);
+            if (e != cudaSuccess) break;
+            const int64_t blocks = (p.group_slots * (p.piece / 8) + 255) / 256;
+            const dim3 grid((unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), p.groups);
+            e = launch_chained(p.prob_terms == 1 ? head_probs_kernel<1> : p.prob_terms == 2 ? head_probs_kernel<2> : head_probs_kernel<3>, grid, dim3(256), 0, s, true, a, p);
+        } else {
+            e = launch_head_tc(h, s);
+        }
         if (e != cudaSuccess) break;
         const Operand probs = {h.probs, h.piece, p.slots, p.piece, p.slots * p.piece, p.prob_terms};
         if (a.dx.data) {

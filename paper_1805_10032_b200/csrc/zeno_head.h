@@ -17,11 +17,11 @@ struct Operand {
     int planes;
 };
 
-enum class HeadStep { kSums, kProbs, kInputs, kWeights };
+enum class HeadStep { kSums, kProbs, kLogits, kInputs, kWeights };
 
 struct HeadTcArgs {
     HeadStep step;
-    Operand a, b;                       // a: X (kSums, kProbs), P (kInputs, kWeights); b: W (kSums, kProbs, kInputs), X (kWeights)
+    Operand a, b;                       // a: X, P (kInputs, kWeights); b: W, X (kWeights)
     int pairs, pair_a[kMaxPairs], pair_b[kMaxPairs];        // terms that are multiplied, the last pair the leading ones
     int b_terms;                        // b's planes of a group
     int groups;                         // with weights of their own; kWeights: the workers
@@ -42,6 +42,10 @@ struct HeadTcArgs {
     __nv_bfloat16 *probs;               // [term][slots][prob_pitch]
     int64_t prob_pitch;
     int prob_terms;
+    // kLogits: unscaled, in parts of the contraction
+    float *logits;                      // [part][slots][logits_pitch]
+    int64_t logits_pitch;
+    int logits_parts;
     // kInputs
     float *parts;                       // [slots][parts_pitch]
     int64_t parts_pitch;
@@ -53,7 +57,7 @@ struct HeadTcArgs {
     int param_type;
     int bf16_result;                    // what comes of the sums is bfloat16
     int tile_cols;                      // columns of a tile: 256 or 128
-    int blocks;                         // of a tile: two, or (kSums, kProbs) one
+    int blocks;                         // of a tile: two, or (kSums, kProbs, kLogits) one
     int last;                           // no kernel of the same call comes after this one
 };
 

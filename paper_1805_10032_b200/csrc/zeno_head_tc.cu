@@ -133,7 +133,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                                                               const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_extra, const KernelArgs args) {
     using S = Shape<STEP, N, COLS, BLOCKS>;
     constexpr int HN = S::kHalf, kCols = COLS;
-    static_assert(BLOCKS == 2 || STEP == HeadStep::kSums || STEP == HeadStep::kProbs, "few rows");
+    static_assert(BLOCKS == 2 || STEP == HeadStep::kSums || STEP == HeadStep::kProbs || STEP == HeadStep::kLogits, "few rows");
     constexpr bool kAMn = STEP == HeadStep::kWeights, kBMn = STEP == HeadStep::kWeights || STEP == HeadStep::kInputs;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // full, empty [kStages]; dfull, dempty [2]
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
     // kInputs: whole rounds of tiles, then the rest of them, cut along the words so that it takes all pairs
     const uint32_t whole = STEP == HeadStep::kInputs ? tiles / pairs_of_blocks * pairs_of_blocks : tiles;
     const int splits = STEP == HeadStep::kInputs ? head_splits(tiles, pairs_of_blocks, h.most_splits) : 1;
-    const uint32_t items = whole + (tiles - whole) * splits;
+    const uint32_t items = STEP == HeadStep::kLogits ? tiles * h.logits_parts : whole + (tiles - whole) * splits;
     // false: no further item
     auto get_item = [&](int li, Item &it) {
         const uint32_t item = pair + li * pairs_of_blocks;
@@ -220,6 +220,11 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
             tile = whole + (item - whole) / splits;
             it.split = (int)(item - whole - (tile - whole) * splits);
             it.splits = splits;
+        }
+        if (STEP == HeadStep::kLogits) {
+            it.splits = h.logits_parts;
+            tile = item / it.splits;
+            it.split = (int)(item - tile * it.splits);
         }
         it.extra = (int)(item - whole);
         it.group = (int)(tile / per_group);
@@ -234,8 +239,9 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
             it.rows_end = end_of(it.group);
             it.row0 = begin_of(it.group) + at.row * S::kRows;
             const int nkb = (int)(((STEP == HeadStep::kInputs ? h.piece : h.cols) + kK - 1) / kK);
-            it.kb0 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * it.split / it.splits) : 0;
-            it.kb1 = STEP == HeadStep::kInputs ? (int)((int64_t)nkb * (it.split + 1) / it.splits) : nkb;
+            constexpr bool kCut = STEP == HeadStep::kInputs || STEP == HeadStep::kLogits;
+            it.kb0 = kCut ? (int)((int64_t)nkb * it.split / it.splits) : 0;
+            it.kb1 = kCut ? (int)((int64_t)nkb * (it.split + 1) / it.splits) : nkb;
             if (it.row0 >= it.rows_end) it.kb1 = it.kb0;                  // a group with fewer tokens
         }
         return true;
@@ -440,15 +446,16 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                     }
                 }
             }
-            if constexpr (STEP == HeadStep::kInputs) {
+            if constexpr (STEP == HeadStep::kInputs || STEP == HeadStep::kLogits) {
 #pragma unroll
                 for (int c0 = 0; c0 < kCols; c0 += 32) {
-                    if (col + c0 >= h.cols || warp_row >= h.slots) break;
+                    if (col + c0 >= (STEP == HeadStep::kLogits ? h.piece : h.cols) || warp_row >= h.slots) break;
                     open_box();
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
                         put16(q, make_uint4(__float_as_uint(acc[c0 + q * 4]), __float_as_uint(acc[c0 + q * 4 + 1]), __float_as_uint(acc[c0 + q * 4 + 2]), __float_as_uint(acc[c0 + q * 4 + 3])));
-                    if (it.split == 0) close_box(&map_out, h.accumulate, col + c0, warp_row, 0);
+                    if (STEP == HeadStep::kLogits) close_box(&map_out, false, col + c0, warp_row, it.split);
+                    else if (it.split == 0) close_box(&map_out, h.accumulate, col + c0, warp_row, 0);
                     else close_box(&map_extra, h.accumulate, part_col + c0, it.extra * S::kRows + rank * kBlockRows + quad * 32, 0);
                 }
             }
@@ -638,6 +645,9 @@ cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
         case HeadStep::kProbs:
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, h.probs, h.piece, h.slots, h.prob_terms, h.prob_pitch, h.slots * h.prob_pitch, 64, 32)) return cudaErrorInvalidValue;
             return brief ? launch<HeadStep::kProbs, N, 64, BLOCKS, float>(a, b, out, extra, k, items, s) : launch<HeadStep::kProbs, N, HN, BLOCKS, float>(a, b, out, extra, k, items, s);
+        case HeadStep::kLogits:
+            if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.logits, h.piece, h.slots, h.logits_parts, h.logits_pitch, h.slots * h.logits_pitch, 32, 32)) return cudaErrorInvalidValue;
+            return launch<HeadStep::kLogits, N, HN, BLOCKS, float>(a, b, out, extra, k, items * h.logits_parts, s);
         case HeadStep::kInputs:
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.parts, h.cols, h.slots, 1, h.parts_pitch, h.slots * h.parts_pitch, 32, 32) ||
                 !encode(&extra, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.extra, N, kHeadPairs * kHeadRows, 1, N, kHeadPairs * kHeadRows * N, 32, 32))
