@@ -309,9 +309,10 @@ zeno_status zeno_score_lsq_static(int32_t device, const float *x, const float *V
 /* ---- Operators of language models, on activations and logits that the caller's own model computes ----------------------
  *
  * A worker of Algorithm 1 that trains a language model, and a server that evaluates m + 1 of them (Definition 2), run most of
- * the model in a framework of their own.  These calls are the parts that belong next to the candidates: norm layers and
- * dense layers whose weight gradients go to every worker's own row of V (not summed over the workers), activations kept in
- * 8 bits for the backward pass, and the loss over a large vocabulary with its gradient.
+ * the model in a framework of their own.  These calls are the parts that belong next to the candidates: the embedding, norm
+ * layers and dense layers whose weight gradients go to every worker's own row of V (not summed over the workers), activations
+ * kept in 8 bits for the backward pass, and the loss over a large vocabulary with its gradient, from logits or, without them,
+ * from hidden states and the output layer's weights.
  *
  * Conventions besides those at the top of this file: no handle; `device` is the CUDA device of all pointers.  Activations
  * are m groups (workers, or models) of n rows (tokens) each, described by zeno_rows.  m or n may be zero: nothing is read,
@@ -450,9 +451,11 @@ zeno_status zeno_linear_logprobs(int32_t device, int32_t type, int32_t param_typ
 
 /* The gradient of  sum over tokens of g_logprob logprob  at x and at w, from zeno_linear_logprobs's lse:
  *   D_tj = g_logprob_t scale ([j = target_t] - exp(z_tj - lse_t)),  dx = D w,  dw[i] = D^T x over group i's tokens.
- * lse, g_logprob: float[m][n].  dx or NULL: like x; zero for a token without a target.  dw or NULL: vocab x cols entries for every
+ * lse, g_logprob: float[m][n]; a token whose lse is minus infinity has no gradient.  dx or NULL: like x; zero for a token
+ * without a target, whose lse and g_logprob are not read.  dw or NULL: vocab x cols entries for every
  * group, lddw entries from one group's to the next (a slice of V), also where w is shared.  The logits are computed again, a
- * piece of the vocabulary at a time; D is kept for that piece, in bfloat16 (three terms of it, as above, if x or w is binary32).
+ * piece of the vocabulary at a time; D is kept for that piece, in bfloat16 (two terms of it for a call of a few tokens, three, as
+ * above, if x or w is binary32).
  * exp(z - lse) carries the rounding of lse, 2^-24 |lse|. */
 int64_t zeno_linear_logprobs_gradient_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols,
                                                 int64_t vocab, const void *w, int64_t ldw, int32_t want_dx);

@@ -47,8 +47,8 @@ bool mappable(const void *w, int64_t ldw, int64_t groups, int64_t cols) {
 }
 
 // Few tokens take no tensor cores: the weights go by once for every kFew tokens.  32000 words by 4096 columns, tokens in brackets, here and on the tensor
-// cores: bfloat16 49 us (1), 69 (2), 87 (3), 79 for any number; binary32 101 (1), 128 (4), 697; bfloat16 words that are not aligned 114 (1) by 1023
-// columns, 66.
+// cores: bfloat16 60 us (1), 69 (2), 87 (3), there 75 for any number; binary32 101 (1), 128 (4), 181 (8), 316 (12), there 480; bfloat16 words that are not
+// aligned, by 1023 columns, 114 (1), there 66.
 constexpr int kFew = 4;
 constexpr int64_t kFewCols = 8192;                                    // their chains of additions are as long as the tensor cores' stretches
 
@@ -107,8 +107,8 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     int64_t logits_parts = units / sum_tiles;
     if (logits_parts > stages / 8) logits_parts = stages / 8;
     if (logits_parts > blocks_of_64) logits_parts = blocks_of_64;
-    // (A stage takes about a quarter of a microsecond, the parts' way through memory and the other kernel as much as some fifty.)
-    p.logits_parts = p.pieces == 1 && logits_parts > 1 && stages - stages / logits_parts >= 64 ? (int)logits_parts : 0;
+    // (A stage takes about a quarter of a microsecond, the parts' way through memory and the other kernel as much as some forty.)
+    p.logits_parts = p.pieces == 1 && logits_parts > 1 && stages - stages / logits_parts >= 40 ? (int)logits_parts : 0;
     p.logits_pitch = up(a.vocab, 4);
     p.tile_cols = a.cols <= 128 ? 128 : 256;                          // of the gradients: few tiles of dx are cut along the words instead
     p.most_splits = (int)(p.piece / 64 / 8);                          // parts of eight stages and more
@@ -294,22 +294,58 @@ __host__ __device__ __forceinline__ V *at(const HeadArgs &a, int64_t offset) {
     return reinterpret_cast<V *>(static_cast<uint8_t *>(a.workspace) + offset);
 }
 
-// blockIdx.y is the worker.
-template <typename T, int TERMS>
+// blockIdx.y is the worker.  ALONE: of a few tokens every block finds the order itself, which saves a launch (and 2 us of 22 for 1648 tokens, 449 words by 300 columns).
+constexpr int64_t kAloneTokens = 2048, kAloneAll = 8192;              // of a worker, and of all
+
+template <typename T, int TERMS, bool ALONE>
 __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
     __shared__ int scratch[8];
+    __shared__ short order[ALONE ? kAloneTokens : 1];
     const HeadArgs &a = args.a;
     const Plan &p = args.p;
     pdl_wait();
     pdl_launch_dependents();
     const int worker = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int *counts = at<int>(a, p.counts);
-    const int count = counts[worker], filled = (count + kSlots - 1) / kSlots * kSlots;
+    auto given = [&](int64_t row) { return (uint32_t)a.targets[row] < (uint64_t)a.vocab; };
+    int count = 0;
+    if constexpr (ALONE) {
+        for (int t0 = 0; t0 < (int)a.n; t0 += 256) {
+            const int t = t0 + threadIdx.x;
+            const bool mine = t < a.n && given(worker * a.n + t);
+            const unsigned votes = __ballot_sync(0xffffffffu, mine);
+            if (lane == 0) scratch[warp] = __popc(votes);
+            __syncthreads();
+            int before = count;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                if (w < warp) before += scratch[w];
+                count += scratch[w];
+            }
+            const int k = before + __popc(votes & ((1u << lane) - 1));
+            if (mine) order[k] = (short)t;
+            if (blockIdx.x == 0 && t < a.n) at<int>(a, p.rank)[worker * a.n + t] = mine ? k : -1;
+            __syncthreads();
+        }
+    } else {
+        count = counts[worker];
+    }
+    const int filled = (count + kSlots - 1) / kSlots * kSlots;
     int begin = 0;
     if (p.groups > 1) {
         begin = (int)(worker * p.group_slots);
     } else {                                                          // behind the workers before
-        for (int i = threadIdx.x; i < worker; i += 256) begin += (counts[i] + kSlots - 1) / kSlots * kSlots;
+        if constexpr (ALONE) {
+            for (int i = warp; i < worker; i += 8) {
+                int others = 0;
+#pragma unroll 4
+                for (int t = lane; t < (int)a.n; t += 32) others += given(i * a.n + t);
+                others = __reduce_add_sync(0xffffffffu, others);
+                if (lane == 0) begin += (others + kSlots - 1) / kSlots * kSlots;
+            }
+        } else {
+            for (int i = threadIdx.x; i < worker; i += 256) begin += (counts[i] + kSlots - 1) / kSlots * kSlots;
+        }
         begin = __reduce_add_sync(0xffffffffu, begin);
         if (lane == 0) scratch[warp] = begin;
         __syncthreads();
@@ -327,7 +363,7 @@ __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
     }
     const int threads = 1 << args.threads_log2, thread = threadIdx.x & (threads - 1), rows_of_block = 256 >> args.threads_log2;
     for (int k = blockIdx.x * rows_of_block + (threadIdx.x >> args.threads_log2); k < filled; k += gridDim.x * rows_of_block) {
-        const int token = k < count ? at<int>(a, p.list)[worker * a.n + k] : -1;
+        const int token = k >= count ? -1 : ALONE ? order[k] : at<int>(a, p.list)[worker * a.n + k];
         const int64_t slot = begin + k, row = worker * a.n + token;
         if (thread == 0) {
             at<int>(a, p.target)[slot] = token >= 0 ? a.targets[row] : -1;
@@ -672,14 +708,18 @@ dim3 grid_for(int64_t blocks) { return dim3((unsigned)(blocks < 148 * 16 ? block
 
 
 cudaError_t fill_slots(int type, const HeadArgs &a, const Plan &p, cudaStream_t s) {
-    cudaError_t e = launch_chained(head_order_kernel, dim3(a.m), dim3(kOrderThreads), 0, s, true, a.targets, a.n, a.vocab, at<int>(a, p.counts), at<int>(a, p.list), at<int>(a, p.rank));
-    if (e != cudaSuccess) return e;
+    const bool alone = a.n <= kAloneTokens && a.m * a.n <= kAloneAll;
+    if (!alone) {
+        const cudaError_t e = launch_chained(head_order_kernel, dim3(a.m), dim3(kOrderThreads), 0, s, true, a.targets, a.n, a.vocab, at<int>(a, p.counts), at<int>(a, p.list), at<int>(a, p.rank));
+        if (e != cudaSuccess) return e;
+    }
     const int elem = type == ZENO_F32 ? 4 : 2;
     const SlotsArgs args = {a, p, a.cols % 8 == 0 && aligned_to(a.x, a.m, a.n, elem, 16), threads_log2(p.pitch)};
     const int64_t blocks = up(a.n, kSlots) / (256 >> args.threads_log2);
     const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048), a.m);
-    return type == ZENO_F32 ? launch_chained(head_slots_kernel<float, 3>, grid, dim3(256), 0, s, true, args)
-                            : launch_chained(head_slots_kernel<__nv_bfloat16, 1>, grid, dim3(256), 0, s, true, args);
+    auto *kernel = type == ZENO_F32 ? (alone ? head_slots_kernel<float, 3, true> : head_slots_kernel<float, 3, false>)
+                                    : (alone ? head_slots_kernel<__nv_bfloat16, 1, true> : head_slots_kernel<__nv_bfloat16, 1, false>);
+    return launch_chained(kernel, grid, dim3(256), 0, s, true, args);
 }
 
 // The piece's weights as an operand; rewrites them if they have to be.

@@ -888,8 +888,8 @@ def linear_logprobs_gradient(x, weight, targets, lse, g_logprob, dweight=None, d
 
 
 def check_operator_status(device: int = 0, stream=None):
-    """Synchronises the stream and raises if a kernel of the operators above gave up on a bounded device-side wait (dense_gradient on the tensor
-    cores has them) since this stream was last asked: on this stream, or on another one of the device."""
+    """Synchronises the stream and raises if a kernel of the operators above gave up on a bounded device-side wait (dense_gradient and
+    linear_logprobs on the tensor cores, and the latter's gradient, have them) since this stream was last asked: on this stream, or on another one of the device."""
     st = load_library().zeno_operator_status(device, _current(device, stream))
     if st != OK:
         _done(st, "zeno_operator_status")

@@ -190,11 +190,12 @@ def test_linear_logprobs_gradient(m, n, cols, vocab, act, par):
     zeno.check_operator_status()
 
 
+@pytest.mark.parametrize("m,n,cols,vocab", [(2, 150, 264, 700), (1, 60, 264, 3000), (1, 60, 4096, 300), (1, 300, 4096, 300)])
 @pytest.mark.parametrize("act,par", [(F32, F32), (BF16, BF16)])
-def test_waits_that_run_out_are_reported(act, par):
-    """With no polls allowed every wait on the tensor cores' path that is not satisfied at once gives up; the next call is sound."""
+def test_waits_that_run_out_are_reported(m, n, cols, vocab, act, par):
+    """With no polls allowed every wait on the tensor cores' path that is not satisfied at once gives up, of pairs of blocks and single ones, of whole logits and
+    those in parts; the next call is sound."""
     g = _gen(5)
-    m, n, cols, vocab = 2, 150, 264, 700
     targets = _tokens(g, m, n, vocab, 0.0)
     x, w = _head(g, m, n, cols, vocab, act, par)
     want = zeno.linear_logprobs(x, w, targets)
@@ -305,12 +306,13 @@ def test_values_that_are_not_finite(act, n):
 
 
 BIG = [(60, 5, 40, 300, True, F32, F32), (60, 70, 72, 200, True, BF16, BF16), (1, 5000, 72, 600, False, BF16, BF16), (2, 3000, 64, 9000, False, F32, F32),
-       (1, 2600, 2100, 3000, False, BF16, BF16), (1, 14, 8192, 12000, False, F32, F32), (3, 900, 100, 40000, False, BF16, F32)]
+       (1, 2600, 2100, 3000, False, BF16, BF16), (1, 14, 8192, 12000, False, F32, F32), (3, 900, 100, 40000, False, BF16, F32),
+       (3, 70, 6000, 300, True, BF16, BF16), (2, 200, 5000, 513, True, F32, BF16), (1, 600, 7001, 255, False, BF16, F32), (9, 1, 4096, 90, False, BF16, BF16)]
 
 
 @pytest.mark.parametrize("m,n,cols,vocab,models,act,par", BIG)
 def test_many_groups_tiles_and_pieces(m, n, cols, vocab, models, act, par):
-    """More groups than shared memory has room for, more rows than a band, a vocabulary of several pieces, tiles that are cut."""
+    """More groups than shared memory has room for, more rows than a band, a vocabulary of several pieces, tiles that are cut, logits in parts."""
     g = _gen(m + n)
     targets = _tokens(g, m, n, vocab)
     x, w = _head(g, m, n, cols, vocab, act, par, models)
