@@ -3,7 +3,7 @@
 //   z = scale x W^T,  lse = log sum_j exp(z_j),  logprob = z_target - lse;
 //   D_tj = g_t scale ([j = target] - exp(z_tj - lse_t)),  dx = D W,  dW = D^T x (every worker's own).
 // Tokens without a target take no part: the others are gathered into slots first (their hidden states as bfloat16 terms, one of a bfloat16 number and three of a
-// binary32 one), each worker's in a run of its own that empty slots fill up to a multiple of kSlots, so that a worker's dW is a sum over whole stages.
+// binary32 one), each worker's in a run of its own; for the gradient empty slots fill it up to a multiple of kSlots, so that a worker's dW is a sum over whole instructions.
 // Weights that no tensor copy can step through, and binary32 ones, are rewritten in terms a piece at a time.
 #include "zeno_head.h"
 
@@ -16,7 +16,7 @@ constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.
 struct Plan {
-    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, sum_blocks, sum_words, few, few_blocks, logits_parts;
+    int x_terms, w_terms, w_packed, prob_terms, groups, most_splits, pieces, tile_cols, sum_cols, sum_blocks, sum_words, few, few_blocks, logits_parts, lot;
     int64_t group_slots, slots, pitch, piece, parts_pitch, part_pitch, logits_pitch;
     int64_t counts, begin, end, total, list, rank, target, lse, g, target_logit, x, w, part, probs, parts, extra, bytes;
 };
@@ -76,8 +76,9 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.w_terms = param_type == ZENO_F32 ? 3 : 1;
     p.w_packed = p.w_terms > 1 || !mappable(a.w, a.ldw, p.groups, a.cols);
     // groups whose tiles of rows are written whole must not share one (as the logits may be, and dx is)
-    const int64_t worker_slots = up(a.n, p.groups > 1 ? (gradient || a.n > 128 ? 256 : 128) : kSlots);
-    p.slots = worker_slots * a.m;
+    p.lot = p.groups > 1 || gradient ? kSlots : 1;
+    const int64_t worker_slots = up(a.n, p.groups > 1 ? (gradient || a.n > 128 ? 256 : 128) : p.lot);
+    p.slots = up(worker_slots * a.m, 64);
     p.group_slots = p.groups > 1 ? worker_slots : p.slots;
     // Of bfloat16 operands D is bfloat16, too: its rounding, as large as the results', makes them off by 1.4 times that.  A few tokens' results may hang on one
     // of its entries, whose rounding is no average: they take two terms.
@@ -330,7 +331,7 @@ __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
     } else {
         count = counts[worker];
     }
-    const int filled = (count + kSlots - 1) / kSlots * kSlots;
+    const int lot = p.lot, filled = (count + lot - 1) / lot * lot;
     int begin = 0;
     if (p.groups > 1) {
         begin = (int)(worker * p.group_slots);
@@ -341,10 +342,10 @@ __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
 #pragma unroll 4
                 for (int t = lane; t < (int)a.n; t += 32) others += given(i * a.n + t);
                 others = __reduce_add_sync(0xffffffffu, others);
-                if (lane == 0) begin += (others + kSlots - 1) / kSlots * kSlots;
+                if (lane == 0) begin += (others + lot - 1) / lot * lot;
             }
         } else {
-            for (int i = threadIdx.x; i < worker; i += 256) begin += (counts[i] + kSlots - 1) / kSlots * kSlots;
+            for (int i = threadIdx.x; i < worker; i += 256) begin += (counts[i] + lot - 1) / lot * lot;
         }
         begin = __reduce_add_sync(0xffffffffu, begin);
         if (lane == 0) scratch[warp] = begin;
@@ -715,7 +716,7 @@ cudaError_t fill_slots(int type, const HeadArgs &a, const Plan &p, cudaStream_t 
     }
     const int elem = type == ZENO_F32 ? 4 : 2;
     const SlotsArgs args = {a, p, a.cols % 8 == 0 && aligned_to(a.x, a.m, a.n, elem, 16), threads_log2(p.pitch)};
-    const int64_t blocks = up(a.n, kSlots) / (256 >> args.threads_log2);
+    const int64_t rows_of_block = 256 >> args.threads_log2, blocks = (up(a.n, p.lot) + rows_of_block - 1) / rows_of_block;
     const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048), a.m);
     auto *kernel = type == ZENO_F32 ? (alone ? head_slots_kernel<float, 3, true> : head_slots_kernel<float, 3, false>)
                                     : (alone ? head_slots_kernel<__nv_bfloat16, 1, true> : head_slots_kernel<__nv_bfloat16, 1, false>);

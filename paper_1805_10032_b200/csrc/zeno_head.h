@@ -5,8 +5,9 @@
 
 namespace zeno {
 
-// Tokens that carry a target lie in slots: worker i's in [begin[i], end[i]), both multiples of kSlots, those left over empty.
-constexpr int kSlots = 64;
+// Tokens that carry a target lie in slots: worker i's in [begin[i], end[i]), for the gradient both multiples of kSlots, the contraction indices of an
+// instruction; those left over are empty.
+constexpr int kSlots = 16;
 constexpr int kMaxPairs = 6;
 
 // Operands as bfloat16 terms: one of a bfloat16 number, three of a binary32 one, in planes of their own.

@@ -125,7 +125,7 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
 
 // One tile and the part of the contraction that goes into it.
 struct Item {
-    int group, row0, rows_end, col0, kb0, kb1, split, splits, extra;
+    int group, row0, rows_end, col0, k0, len, kb0, kb1, split, splits, extra;          // k0, len: the contraction's indices, kb0, kb1: blocks of kK of them
 };
 
 template <HeadStep STEP, int N, int COLS, int BLOCKS, typename P>
@@ -233,12 +233,16 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
         if (STEP == HeadStep::kWeights) {
             it.row0 = at.row * S::kRows;                                 // words of the piece
             it.rows_end = (int)h.piece;
-            it.kb0 = begin_of(it.group) / kK;
-            it.kb1 = end_of(it.group) / kK;
+            it.k0 = begin_of(it.group);
+            it.len = end_of(it.group) - it.k0;
+            it.kb0 = 0;
+            it.kb1 = (it.len + kK - 1) / kK;
         } else {
+            it.k0 = 0;
+            it.len = (int)(STEP == HeadStep::kInputs ? h.piece : h.cols);
             it.rows_end = end_of(it.group);
             it.row0 = begin_of(it.group) + at.row * S::kRows;
-            const int nkb = (int)(((STEP == HeadStep::kInputs ? h.piece : h.cols) + kK - 1) / kK);
+            const int nkb = (it.len + kK - 1) / kK;
             constexpr bool kCut = STEP == HeadStep::kInputs || STEP == HeadStep::kLogits;
             it.kb0 = kCut ? (int)((int64_t)nkb * it.split / it.splits) : 0;
             it.kb1 = kCut ? (int)((int64_t)nkb * (it.split + 1) / it.splits) : nkb;
@@ -272,13 +276,13 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                         if (rank == 0) mbar_expect_tx(full(s), bytes);
                         issued[rank][s] = (round + 1) * 4 + rows_there * 2 + rows_here;
                         if (kAMn) {
-                            tma_load<BLOCKS>(to_a, &map_a, row, kb * kK, plane_a, bar);
-                            tma_load<BLOCKS>(to_a + kK * 128, &map_a, row + 64, kb * kK, plane_a, bar);
+                            tma_load<BLOCKS>(to_a, &map_a, row, it.k0 + kb * kK, plane_a, bar);
+                            tma_load<BLOCKS>(to_a + kK * 128, &map_a, row + 64, it.k0 + kb * kK, plane_a, bar);
                         } else if (rows_here) {
                             tma_load<BLOCKS>(to_a, &map_a, kb * kK, row, plane_a, bar);
                         }
                         if (kBMn) {
-                            const int k0 = STEP == HeadStep::kInputs ? (int)h.b_row0 + kb * kK : kb * kK;
+                            const int k0 = STEP == HeadStep::kInputs ? (int)h.b_row0 + kb * kK : it.k0 + kb * kK;
                             tma_load<BLOCKS>(to_b, &map_b, col, k0, plane_b, bar);
                             if (HN > 64) tma_load<BLOCKS>(to_b + kK * 128, &map_b, col + 64, k0, plane_b, bar);
                         } else {
@@ -303,19 +307,27 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
             Item it;
             for (int li = 0; ok && get_item(li, it) && !*abortp; ++li) {
                 for (int from = it.kb0; ok && from < it.kb1; from += args.drain, ++drain) {
-                    const int set = (int)(drain & 1), all = (min(it.kb1, from + args.drain) - from) * h.pairs;
+                    const int set = (int)(drain & 1), to = min(it.kb1, from + args.drain), all = (to - from) * h.pairs;
                     ok = mbar_wait(dempty(set), ((drain >> 1) & 1) ^ 1, abortp);
                     if (!ok) break;
                     tc_fence_after();
-                    for (int j = 0; j < all; ++j) {
+                    for (int j = 0, kb = from; j < all; ++j, kb = kb + 1 == to ? from : kb + 1) {
                         ok = mbar_wait(full(s), ph, abortp);
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t ab = smem_u32(ring) + s * S::kStageBytes, bb = ab + kABytes;
                         const uint64_t a_desc = kAMn ? mn_major(ab) : smem_desc_sw128(ab), b_desc = kBMn ? mn_major(bb) : smem_desc_sw128(bb);
-#pragma unroll
-                        for (int k = 0; k < kK / 16; ++k)        // 16 contraction indices: 32 bytes of a row, or 16 rows of 128 bytes
+                        // 16 contraction indices: 32 bytes of a row, or 16 rows of 128 bytes.  Those behind the last one are left out: another worker's tokens.
+                        auto instruction = [&](int k) {
                             mma<BLOCKS>(tmem + set * N, a_desc + k * (kAMn ? 2048 / 16 : 32 / 16), b_desc + k * (kBMn ? 2048 / 16 : 32 / 16), idesc, (uint32_t)(j | k));
+                        };
+                        const int left = it.len - kb * kK;
+                        if (left >= kK) {
+#pragma unroll
+                            for (int k = 0; k < kK / 16; ++k) instruction(k);
+                        } else {
+                            for (int k = 0; k * 16 < left; ++k) instruction(k);
+                        }
                         commit_to_all<BLOCKS>(empty(s));
                         if (j + 1 == all) commit_to_all<BLOCKS>(dfull(set));
                         if (++s == S::kStages) {

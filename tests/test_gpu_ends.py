@@ -575,3 +575,40 @@ def test_workers_gradients_of_a_tied_language_model_and_the_step_on_them():
         want = V[kept.long(), :d].double().mean(0)
         assert float((average.double() - want).norm() / want.norm()) <= 1e-6
     zeno.check_operator_status()
+
+
+@pytest.mark.parametrize("m,n,cols,vocab,act,par", [(33, 5, 96, 700, F32, BF16), (17, 21, 200, 300, BF16, BF16), (50, 1, 264, 513, BF16, F32), (9, 33, 1100, 257, F32, F32),
+                                                    (5, 17, 4096, 300, BF16, BF16), (20, 130, 72, 90, BF16, BF16)])
+def test_workers_of_few_tokens_keep_to_themselves(m, n, cols, vocab, act, par):
+    """Workers that share weights and whose tokens lie next to one another: one worker's NaN reaches no other's gradient, nor does what memory held before."""
+    g = _gen(m * n)
+    targets = _tokens(g, m, n, vocab)
+    targets[1] = -1
+    targets[2, -1] = vocab - 1
+    x, w = _head(g, m, n, cols, vocab, act, par, False)
+    given = (targets >= 0) & (targets < vocab)
+    x = torch.where(given.unsqueeze(-1), x, NAN)
+    clean = torch.where(given.unsqueeze(-1), x, 0.0)
+    gl = torch.where(given, torch.randn(m, n, generator=g, device="cuda"), NAN)
+    for bad in (False, True):
+        if bad:
+            x[2, -1, cols // 2] = NAN
+        stale = torch.full((64 << 20,), NAN, device="cuda")
+        del stale
+        got = zeno.linear_logprobs(x, w, targets)
+        rest = [i for i in range(m) if i != 2 or not bad]
+        want = E.logprobs(clean, w, targets, 1.0)
+        R.assert_near(got.logprobs[rest], want[0][rest], want[2][rest], "logprobs")
+        R.assert_near(got.lse[rest], want[1][rest], want[3][rest], "lse")
+        stale = torch.full((64 << 20,), NAN, device="cuda")
+        del stale
+        dw = torch.full((m, vocab, cols), NAN, device="cuda", dtype=par)
+        dx = zeno.linear_logprobs_gradient(x, w, targets, torch.where(given, got.lse, NAN), gl, dweight=dw)
+        for i in rest[:: 1 if m < 10 else 5] + [1]:
+            ref = E.logprobs_gradient(clean[i:i + 1], w, targets[i:i + 1], got.lse[i:i + 1], torch.where(given, gl, 0.0)[i:i + 1], 1.0, F32 if F32 in (act, par) else BF16)
+            R.assert_near(dx[i:i + 1], ref[0], ref[2], "dx")
+            R.assert_near(dw[i:i + 1], ref[1], ref[3], "dw")
+        assert torch.isfinite(dw[rest]).all() and torch.isfinite(dx[rest]).all()
+        if bad:
+            assert torch.isnan(got.lse[2, -1]) and torch.isnan(dx[2, -1]).all() and torch.isnan(dw[2]).all()
+    zeno.check_operator_status()
