@@ -11,7 +11,9 @@ namespace zeno {
 
 namespace {
 
-constexpr int64_t kPieceBytes = (int64_t)256 << 20, kWeightBytes = (int64_t)768 << 20;
+// Of D, and of rewritten weights.  Every boundary between launches shows: 10 x 1778 tokens, 7744 words by 320 columns (binary32, weights bfloat16) take 1.19 ms,
+// in pieces of 256 MB 1.29, of 96 MB, which L2 would hold, 1.51.
+constexpr int64_t kPieceBytes = (int64_t)512 << 20, kWeightBytes = (int64_t)768 << 20;
 constexpr int kMinPiece = 2048;
 
 // What lies where in the workspace, and how the vocabulary is cut.

@@ -307,7 +307,8 @@ def test_values_that_are_not_finite(act, n):
 
 BIG = [(60, 5, 40, 300, True, F32, F32), (60, 70, 72, 200, True, BF16, BF16), (1, 5000, 72, 600, False, BF16, BF16), (2, 3000, 64, 9000, False, F32, F32),
        (1, 2600, 2100, 3000, False, BF16, BF16), (1, 14, 8192, 12000, False, F32, F32), (3, 900, 100, 40000, False, BF16, F32),
-       (3, 70, 6000, 300, True, BF16, BF16), (2, 200, 5000, 513, True, F32, BF16), (1, 600, 7001, 255, False, BF16, F32), (9, 1, 4096, 90, False, BF16, BF16)]
+       (3, 70, 6000, 300, True, BF16, BF16), (2, 200, 5000, 513, True, F32, BF16), (1, 600, 7001, 255, False, BF16, F32), (9, 1, 4096, 90, False, BF16, BF16),
+       (1, 4100, 64, 70000, False, BF16, BF16)]
 
 
 @pytest.mark.parametrize("m,n,cols,vocab,models,act,par", BIG)
