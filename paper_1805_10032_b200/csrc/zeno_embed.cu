@@ -520,23 +520,26 @@ __global__ void __launch_bounds__(kThreads, 3) embed_rows_kernel(const RowsArgs 
     }
 }
 
-// Rows of more than kRun positions: the warp of the run where such a row begins adds its parts, 64 columns of them.
-constexpr int kChecked = 8;                          // runs that a warp looks for such a beginning in
+// Rows of more than kRun positions: a block looks for those that begin in kChecked runs and adds their parts, 64 columns of them.  A warp takes a row, or, of more
+// than kOwnParts parts, all warps an equal share of it, joined in their order (65536 tokens, 131072 words by 2048 columns, a sixteenth of the tokens one word: 255 us
+// in all, by a warp for every row 272).
+constexpr int kChecked = 32, kOwnParts = 32;
 template <typename P>
 __global__ void __launch_bounds__(kThreads) embed_parts_kernel(const RowsArgs r, int slices) {
     constexpr int N = 2, kSlice = 32 * N, kAtOnce = 16;
+    __shared__ LongSum shares[kWarps][kSlice];
     pdl_wait();
     const EmbedGradArgs &a = r.a;
     const Classes c = r.c;
-    const int lane = threadIdx.x & 31, worker = blockIdx.y;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, worker = blockIdx.y;
     const Token *list = r.list + worker * a.n;
     const int *start = r.start + (int64_t)worker * c.count() * c.starts();
     const int count = r.count[worker].x;
     const uint32_t runs = (count + kRun - 1) / kRun, tasks = (runs + kChecked - 1) / kChecked * slices;
-    for (uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5); task < tasks; task += gridDim.x * kWarps) {
+    for (uint32_t task = blockIdx.x; task < tasks; task += gridDim.x) {
         const uint32_t group = task / (uint32_t)slices, slice = task - group * slices, mine = group * kChecked + lane;
         int id = -1, from = 0, of_row = 0;
-        if (lane < kChecked && mine < runs) {
+        if (mine < runs) {
             id = list[min(count, (int)(mine + 1) * kRun) - 1].id;
             const int *s = start + c.cls(id) * c.starts() + c.row(id);
             from = s[0], of_row = s[1] - s[0];
@@ -544,14 +547,9 @@ __global__ void __launch_bounds__(kThreads) embed_parts_kernel(const RowsArgs r,
         const int64_t col0 = (int64_t)slice * kSlice;
         const int cols = (int)min((int64_t)kSlice, a.cols - col0);
         const float *parts = r.parts + (int64_t)worker * r.runs * 2 * a.cols + col0;
-        for (unsigned found = __ballot_sync(0xffffffffu, of_row > kRun && from / kRun == (int)mine); found; found &= found - 1) {
-            const int at = __ffs(found) - 1, row = __shfl_sync(0xffffffffu, id, at);
-            const uint32_t run = group * kChecked + at, last = (__shfl_sync(0xffffffffu, from + of_row, at) - 1) / kRun;
-            LongSum total[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (lane + 32 * i < cols) total[i].sum = parts[((int64_t)run * 2 + 1) * a.cols + lane + 32 * i];
-            for (uint32_t k0 = run + 1; k0 <= last; k0 += kAtOnce) {
+        // the row's parts in runs k0 to last
+        auto add = [&](LongSum (&total)[N], uint32_t k0, uint32_t last) {
+            for (; k0 <= last; k0 += kAtOnce) {
                 float v[kAtOnce][N];
 #pragma unroll
                 for (int k = 0; k < kAtOnce; ++k)
@@ -562,10 +560,45 @@ __global__ void __launch_bounds__(kThreads) embed_parts_kernel(const RowsArgs r,
 #pragma unroll
                     for (int i = 0; i < N; ++i) total[i].add(v[k][i]);
             }
+        };
+        auto store = [&](const LongSum (&total)[N], int row) {
             float sum[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) sum[i] = total[i].sum;
             store_columns<N, false>(sum, static_cast<P *>(a.dtable) + worker * a.ldt + row * a.cols + col0, lane, cols, a.scale, a.add);
+        };
+        int turn = 0;
+        for (unsigned found = __ballot_sync(0xffffffffu, of_row > kRun && from / kRun == (int)mine); found; found &= found - 1, ++turn) {
+            const int at = __ffs(found) - 1, row = __shfl_sync(0xffffffffu, id, at);
+            const uint32_t run = group * kChecked + at, last = (__shfl_sync(0xffffffffu, from + of_row, at) - 1) / kRun, more = last - run;
+            const bool shared = more > kOwnParts, own = turn % kWarps == warp;
+            if (!shared && !own) continue;
+            LongSum total[N];
+            if (own)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (lane + 32 * i < cols) total[i].sum = parts[((int64_t)run * 2 + 1) * a.cols + lane + 32 * i];
+            if (!shared) {
+                add(total, run + 1, last);
+                store(total, row);
+                continue;
+            }
+            LongSum share[N];
+            add(share, run + 1 + (uint32_t)((uint64_t)more * warp / kWarps), run + (uint32_t)((uint64_t)more * (warp + 1) / kWarps));
+#pragma unroll
+            for (int i = 0; i < N; ++i) shares[warp][lane + 32 * i] = share[i];
+            __syncthreads();
+            if (own) {
+                for (int w = 0; w < kWarps; ++w)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const LongSum of_warp = shares[w][lane + 32 * i];
+                        total[i].add(of_warp.sum);
+                        total[i].add(-of_warp.lost);
+                    }
+                store(total, row);
+            }
+            __syncthreads();
         }
     }
 }
@@ -593,7 +626,7 @@ cudaError_t sum_rows(RowsArgs r, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     if (!r.followed) return cudaSuccess;                               // no row of more than a run
     const int slices = (int)((r.a.cols + 63) / 64);
-    return launch_chained(embed_parts_kernel<P>, dim3(blocks_for((runs_of(r.a.n) + kChecked - 1) / kChecked * slices, 6), r.a.m), dim3(kThreads), 0, s, true, r, slices);
+    return launch_chained(embed_parts_kernel<P>, dim3(blocks_for((runs_of(r.a.n) + kChecked - 1) / kChecked * slices * kWarps, 6), r.a.m), dim3(kThreads), 0, s, true, r, slices);
 }
 
 template <typename T, typename P>

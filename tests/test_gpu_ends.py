@@ -85,7 +85,7 @@ def test_embed(m, n, vocab, cols, act, par):
 
 
 GRADIENT = [(1, 1, 1, 1), (1, 1, 3000, 512), (2, 3, 5, 7), (3, 70, 50, 33), (2, 900, 11, 264), (4, 333, 777, 1025), (21, 40, 100, 64), (1, 5000, 4099, 520),
-            (2, 129, 17, 4096), (1, 20000, 40, 24), (3, 1, 2, 3), (2, 0, 70, 40)]
+            (2, 129, 17, 4096), (1, 20000, 40, 24), (2, 40000, 9, 100), (3, 1, 2, 3), (2, 0, 70, 40)]
 
 
 @pytest.mark.parametrize("m,n,vocab,cols", GRADIENT)
