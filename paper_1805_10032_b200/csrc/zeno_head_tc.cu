@@ -42,10 +42,11 @@ __device__ unsigned g_given_up;                      // blocks whose bounded wai
 
 // The tensor core adds with truncation towards zero, about 1.4e-8 of a sum with every 16 products (where all are positive).  So a set of sums in TMEM takes a
 // stretch of the contraction only, and goes on in registers, in additions to nearest.  Stretches of 256 where binary32 operands are multiplied (by 512,
-// gradients are off by 1.3 times as much as by plain products in binary32); of 512 for logits of bfloat16 operands, whose lse is binary32 (4096
+// gradients are off by 1.3 times as much as by plain products in binary32), of 128 for their logits, whose error a probability near one multiplies (2 x 332 tokens, 93
+// words by 667 columns: dx off by 0.7e-6, by 256 by 1.3e-6, in 1 % less time); of 512 for logits of bfloat16 operands, whose lse is binary32 (4096
 // tokens, 131072 words, 4096 columns: 2.50 ms, by 256 2.65); of 1,024 for what is rounded to bfloat16 anyway (D of the same: 333 us for 16384 words, by 256 360).
 // The terms' planes of a stretch stay in L2 for all pairs of terms.
-constexpr int kDrainTerms = 4, kDrain = 8, kDrainBf16 = 16;
+constexpr int kDrainTerms = 4, kDrainLogits = 2, kDrain = 8, kDrainBf16 = 16;
 
 struct KernelArgs {
     HeadTcArgs h;
@@ -709,7 +710,7 @@ cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
     const bool weights = h.step == HeadStep::kWeights, inputs = h.step == HeadStep::kInputs;
     k.row_tiles = (int)(((weights ? h.piece : h.group_slots) + kRows - 1) / kRows);
     k.col_tiles = (int)(((weights || inputs ? h.cols : h.piece) + N - 1) / N);
-    k.drain = h.bf16_result ? kDrainBf16 : h.pairs > 1 || inputs || weights ? kDrainTerms : kDrain;
+    k.drain = h.bf16_result ? kDrainBf16 : inputs || weights ? kDrainTerms : h.pairs > 1 ? kDrainLogits : kDrain;
     k.spin_limit = spin_limit;
     const int64_t items = (int64_t)k.row_tiles * k.col_tiles * h.groups;
     if (items == 0) return cudaSuccess;
