@@ -1,16 +1,15 @@
 // The products around the output layer on the tensor cores: logits with the sums of their exponentials, the probabilities' gradient from
 // logits computed again, and its two products.
 //
-// A pair of blocks (a cluster of two SMs; a single one, with a tile of 128 rows, for the logits of groups that have no more) takes a tile of 256 rows by kN columns: the pair's instruction (cta_group::2, M = 256) reads 128 rows of A and
-// half of the columns of B from each block's shared memory, so that a block copies half of what the tile needs, and leaves 128 rows of sums in either
+// A pair of blocks (a cluster of two SMs; a single one, with a tile of 128 rows, for the logits of groups that have no more) takes a tile of 256 rows by 256 or
+// 128 columns: the pair's instruction (cta_group::2, M = 256) reads 128 rows of A and half of the columns of B from each block's shared memory, so that a block copies half of what the tile needs, and leaves 128 rows of sums in either
 // block's TMEM.  Operands are bfloat16, in binary32 sums; a binary32 operand is three terms whose products are summed one pair of terms after the other, the
 // leading pair last.  X and W lie with the contraction's index contiguous for the logits ("K-major"); P W takes W, and P^T X both, with the index of the
 // result contiguous ("MN-major"), all in the 128-byte swizzled layouts that the tensor copies write.
 //   warp 0: copies, both blocks' counted on the first one's barriers;  warp 1 of the first block: the pair's instructions;
-//   the other warps: sums from TMEM, the next tile's being formed meanwhile: 32 rows and 64 columns each.
+//   the other warps: sums from TMEM, the next tile's being formed meanwhile: 32 rows and 64 or 128 columns each.
 // One lane each loops over the copies and the instructions: by whole warps that elect a lane for every stage, a stage takes 500 cycles whatever its size
 // (256 by 128 tiles: 400), and with the second block's copies counted on its own barriers and reported to the first, 580.
-//
 #include "zeno_head.h"
 #include "zeno_tc.cuh"
 
@@ -43,7 +42,7 @@ __device__ unsigned g_given_up;                      // blocks whose bounded wai
 // The tensor core adds with truncation towards zero, about 1.4e-8 of a sum with every 16 products (where all are positive).  So a set of sums in TMEM takes a
 // stretch of the contraction only, and goes on in registers, in additions to nearest.  Stretches of 256 where binary32 operands are multiplied (by 512,
 // gradients are off by 1.3 times as much as by plain products in binary32), of 128 for their logits, whose error a probability near one multiplies (2 x 332 tokens, 93
-// words by 667 columns: dx off by 0.7e-6, by 256 by 1.3e-6, in 1 % less time); of 512 for logits of bfloat16 operands, whose lse is binary32 (4096
+// words by 667 columns: dx off by less than 0.9e-6, by 256 by 1.3e-6, in 1 % less time); of 512 for logits of bfloat16 operands, whose lse is binary32 (4096
 // tokens, 131072 words, 4096 columns: 2.50 ms, by 256 2.65); of 1,024 for what is rounded to bfloat16 anyway (D of the same: 333 us for 16384 words, by 256 360).
 // The terms' planes of a stretch stay in L2 for all pairs of terms.
 constexpr int kDrainTerms = 4, kDrainLogits = 2, kDrain = 8, kDrainBf16 = 16;
