@@ -454,8 +454,7 @@ zeno_status zeno_linear_logprobs(int32_t device, int32_t type, int32_t param_typ
  * lse, g_logprob: float[m][n]; a token whose lse is minus infinity has no gradient.  dx or NULL: like x; zero for a token
  * without a target, whose lse and g_logprob are not read.  dw or NULL: vocab x cols entries for every
  * group, lddw entries from one group's to the next (a slice of V), also where w is shared.  The logits are computed again, a
- * piece of the vocabulary at a time; D is kept for that piece, in bfloat16 (two terms of it for a call of a few tokens, three, as
- * above, if x or w is binary32).
+ * piece of the vocabulary at a time; D is kept for that piece, in two bfloat16 terms (three, as above, if x or w is binary32).
  * exp(z - lse) carries the rounding of lse, 2^-24 |lse|. */
 int64_t zeno_linear_logprobs_gradient_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols,
                                                 int64_t vocab, const void *w, int64_t ldw, int32_t want_dx);

@@ -82,9 +82,9 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     const int64_t worker_slots = up(a.n, p.groups > 1 ? (gradient || a.n > 128 ? 256 : 128) : p.lot);
     p.slots = up(worker_slots * a.m, 64);
     p.group_slots = p.groups > 1 ? worker_slots : p.slots;
-    // Of bfloat16 operands D is bfloat16, too: its rounding, as large as the results', makes them off by 1.4 times that.  A few tokens' results may hang on one
-    // of its entries, whose rounding is no average: they take two terms.
-    p.prob_terms = p.x_terms > 1 || p.w_terms > 1 ? 3 : p.slots <= 256 ? 2 : 1;
+    // D of bfloat16 operands, 16 bits of it: by one term, as many bits as the results have, they would be off by 1.4 times their own rounding, and by up to twice it
+    // where they hang on one entry of D.
+    p.prob_terms = p.x_terms > 1 || p.w_terms > 1 ? 3 : 2;
     p.pitch = up(a.cols, 8);
     p.parts_pitch = up(a.cols, 4);
     const int64_t per_word = p.w_packed ? p.groups * p.w_terms * p.pitch * 2 : 0, per_prob = gradient ? p.slots * p.prob_terms * 2 : 0;
@@ -198,7 +198,7 @@ __device__ __forceinline__ void put_terms(float (&f)[8], __nv_bfloat16 *to, int6
         uint32_t v[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (TERMS > 1 && !plain) {
+            if (!plain) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     float &e = f[2 * k + i];
@@ -859,13 +859,12 @@ cudaError_t launch_head_gradient(int type, int param_type, const HeadArgs &a, cu
         h.probs = at<__nv_bfloat16>(a, p.probs);
         h.prob_pitch = p.piece;
         h.prob_terms = p.prob_terms;
-        h.bf16_result = p.prob_terms < 3;
         if (p.logits_parts) {
             e = launch_logits(h, a, p, s);
             if (e != cudaSuccess) break;
             const int64_t blocks = (p.group_slots * (p.piece / 8) + 255) / 256;
             const dim3 grid((unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), p.groups);
-            e = launch_chained(p.prob_terms == 1 ? head_probs_kernel<1> : p.prob_terms == 2 ? head_probs_kernel<2> : head_probs_kernel<3>, grid, dim3(256), 0, s, true, a, p);
+            e = launch_chained(p.prob_terms == 2 ? head_probs_kernel<2> : head_probs_kernel<3>, grid, dim3(256), 0, s, true, a, p);
         } else {
             e = launch_head_tc(h, s);
         }

@@ -42,8 +42,9 @@ __device__ unsigned g_given_up;                      // blocks whose bounded wai
 // The tensor core adds with truncation towards zero, about 1.4e-8 of a sum with every 16 products (where all are positive).  So a set of sums in TMEM takes a
 // stretch of the contraction only, and goes on in registers, in additions to nearest.  Stretches of 256 where binary32 operands are multiplied (by 512,
 // gradients are off by 1.3 times as much as by plain products in binary32), of 128 for their logits, whose error a probability near one multiplies (2 x 332 tokens, 93
-// words by 667 columns: dx off by less than 0.9e-6, by 256 by 1.3e-6, in 1 % less time); of 512 for logits of bfloat16 operands, whose lse is binary32 (4096
-// tokens, 131072 words, 4096 columns: 2.50 ms, by 256 2.65); of 1,024 for what is rounded to bfloat16 anyway (D of the same: 333 us for 16384 words, by 256 360).
+// words by 667 columns: dx off by less than 0.9e-6, by 256 by 1.3e-6, in 1 % less time); of 512 for logits of bfloat16 operands (4096 tokens, 131072 words, 4096
+// columns: 2.50 ms, by 256 2.65), for D's as for lse's, so that a row's probabilities are those that lse is the sum of; of 1,024 for gradients that are rounded
+// to bfloat16 anyway.
 // The terms' planes of a stretch stay in L2 for all pairs of terms.
 constexpr int kDrainTerms = 4, kDrainLogits = 2, kDrain = 8, kDrainBf16 = 16;
 
@@ -511,12 +512,10 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                             for (int e = 0; e < 4; ++e) {
                                 float *f = &acc[c0 + q * 8 + e * 2];
                                 v[e] = two_bf16(f[0], f[1]);
-                                if (h.prob_terms > 1) {             // what the next term holds
-                                    float hi0 = __uint_as_float(v[e] << 16), hi1 = __uint_as_float(v[e] & 0xffff0000u);
-                                    fma2(hi0, hi1, -1.f, -1.f, f[0], f[1]);
-                                    f[0] = hi0;
-                                    f[1] = hi1;
-                                }
+                                float hi0 = __uint_as_float(v[e] << 16), hi1 = __uint_as_float(v[e] & 0xffff0000u);
+                                fma2(hi0, hi1, -1.f, -1.f, f[0], f[1]);             // what the next term holds
+                                f[0] = hi0;
+                                f[1] = hi1;
                             }
                             put16(q, make_uint4(v[0], v[1], v[2], v[3]));
                         }

@@ -1,0 +1,67 @@
+"""How near the gradients of the log probabilities from hidden states come to their definitions in 64 bits: bounds that leave no room for more than the kernels'
+own roundings."""
+import pytest
+import torch
+
+from paper_1805_10032_b200 import zeno
+
+import ends_ref as E
+import operators_ref as R
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _library():
+    from paper_1805_10032_b200 import build as zbuild
+    zbuild.build()
+    assert torch.cuda.is_available(), "these tests need a CUDA device"
+    zeno.load_library()
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _head(g, m, n, cols, vocab, act, par, models):
+    w = torch.randn(*((m,) if models else ()), vocab, cols, generator=g, device="cuda") * (2.0 / cols ** 0.5)
+    return torch.randn(m, n, cols, generator=g, device="cuda").to(act), w.to(par)
+
+
+def _two_terms(x, w, t, lse, gl):
+    """One group's (dx, dw, their slacks) where D is held as two bfloat16 terms: the first is off by 2^-8 of D, the second by 2^-8 of that.  D's logits are summed
+    as lse's are (ends_ref); its products with w and x in stretches of at most 1,024 indices, 64 truncating steps of 2 U each (those of the second term, 2^-8 of
+    the sums, are 0.5 U together), stretches, tiles that are cut (80 parts at most) and pieces added to nearest."""
+    x, w = x.double(), w.double()
+    z, off = E.logits(x, w, 1.0)
+    L, gs = lse.double().unsqueeze(-1), gl.double().unsqueeze(-1)
+    hot = torch.zeros_like(z).scatter_(-1, t.long().unsqueeze(-1), 1.0)
+    p = torch.exp(z - L)
+    d = gs * (hot - p)
+    # the logits', the argument's roundings, the exponential's own error
+    p_off = p * (torch.expm1(off + R.U * L.abs() + 4 * R.U * (z - L).abs()) + 8 * R.U)
+    d_off = gs.abs() * p_off
+    d_off = d_off + (2.0 ** -16 + 2 * R.U) * (d.abs() + d_off)
+    size = d.abs() + d_off
+    products = lambda terms: (2 * 64 + 1 + terms / 1024 + 24 + 80) * R.U  # noqa: E731
+    return d @ w, d.T @ x, d_off @ w.abs() + products(len(w)) * (size @ w.abs()), d_off.T @ x.abs() + products(len(x)) * (size.T @ x.abs())
+
+
+# a token or a few of each worker, where a result hangs on one entry of D; workers with weights of their own; more tokens; long contractions of few tiles
+@pytest.mark.parametrize("m,n,cols,vocab,models", [(1, 1, 264, 700, False), (17, 1, 264, 700, False), (2, 1, 520, 300, True), (21, 5, 96, 513, True), (1, 300, 1032, 2000, False),
+                                                   (3, 333, 77, 1000, False), (16, 61, 136, 3003, False), (2, 40, 4096, 300, True), (1, 700, 4096, 130, False), (1, 2600, 64, 30000, False)])
+def test_bfloat16_operands_gradients_are_off_by_their_own_rounding(m, n, cols, vocab, models):
+    g = _gen(cols + vocab)
+    x, w = _head(g, m, n, cols, vocab, BF16, BF16, models)
+    t = torch.randint(0, vocab, (m, n), generator=g, device="cuda").int()
+    gl = torch.randn(m, n, generator=g, device="cuda")
+    lse = zeno.linear_logprobs(x, w, t).lse
+    dw = torch.empty(m, vocab, cols, device="cuda", dtype=BF16)
+    dx = zeno.linear_logprobs_gradient(x, w, t, lse, gl, dweight=dw)
+    for i in range(m):
+        want = _two_terms(x[i], w[i] if models else w, t[i], lse[i], gl[i])
+        R.assert_near(dx[i], want[0], want[2], "dx")
+        R.assert_near(dw[i], want[1], want[3], "dw")
+    zeno.check_operator_status()
