@@ -440,7 +440,9 @@ zeno_status zeno_embed_gradient(int32_t device, int32_t type, int32_t param_type
  * logprobs, lse: float[m][n] or NULL.  Products are exact, their sums binary32 (of binary32 x or w the tensor cores take three
  * bfloat16 terms, which hold an entry of 2^-110 or more as it is; products under 2^-24 of the leading one are left out).  The
  * tensor cores add with truncation towards zero; sums go on in additions to nearest after every stretch of the contraction.
- * A row with a logit that is NaN or plus infinity gives NaN; in binary32 any infinity or NaN among its x or in w may.
+ * A row with a logit that is NaN or plus infinity gives NaN; in binary32 any infinity or NaN among its x or in w may, and so may
+ * products whose magnitudes sum to 2^135 or more (the terms' own sums overflow then).  A logit of minus infinity, or as far below
+ * lse as binary32 goes, is a probability of zero, here and in the gradient.
  * Weights that are bfloat16, aligned to 16 bytes, in rows and groups of multiples of 8 entries, are read as they lie; others are
  * rewritten in the workspace, up to 768 MB of them at a time. */
 int64_t zeno_linear_logprobs_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols, int64_t vocab,

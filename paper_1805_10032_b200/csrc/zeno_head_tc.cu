@@ -485,8 +485,8 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                         fma2(f0, f1, kLog2eRest, kLog2eRest, e0, e1);
                         mul2(f0, f1, 0.69314718f);
                         fma2(f0, f1, p0, p1, p0, p1);
-                        p0 = f0;
-                        p1 = f1;
+                        p0 = p0 == 0.f ? 0.f : f0;              // of t beyond binary32 the correction is none (a NaN remains one)
+                        p1 = p1 == 0.f ? 0.f : f1;
                     }
                     acc[c] = p0;
                     acc[c + 1] = p1;

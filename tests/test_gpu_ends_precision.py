@@ -65,3 +65,42 @@ def test_bfloat16_operands_gradients_are_off_by_their_own_rounding(m, n, cols, v
         R.assert_near(dx[i], want[0], want[2], "dx")
         R.assert_near(dw[i], want[1], want[3], "dw")
     zeno.check_operator_status()
+
+
+# whole logits, of few and many tokens, a narrow and a wide layer, and (of 4096 columns) logits in parts of the contraction
+@pytest.mark.parametrize("n,cols", [(2, 64), (40, 64), (300, 1200), (2, 4096), (40, 4096)])
+@pytest.mark.parametrize("first", [1.0, 7.3])
+@pytest.mark.parametrize("act,par", [(F32, F32), (BF16, F32), (F32, BF16), (BF16, BF16)])
+def test_gradients_of_a_word_whose_logits_are_minus_a_lot(n, cols, first, act, par):
+    """A word whose weights are finite and whose logits are -3e38, or beyond binary32 and so minus infinity, has probability zero: its gradient is zero, and dx is
+    what it is without that word."""
+    g = _gen(n + cols)
+    vocab, m = 300, 1
+    x, w = _head(g, m, n, cols, vocab, act, par, False)
+    x[..., 0] = first
+    w[0] = 0.0
+    w[0, 0] = -3e38
+    t = torch.randint(1, vocab, (m, n), generator=g, device="cuda").int()
+    gl = torch.randn(m, n, generator=g, device="cuda")
+    got = zeno.linear_logprobs(x, w, t)
+    want = E.logprobs(x, w[1:], t - 1, 1.0)
+    R.assert_near(got.logprobs, want[0], want[2], "logprobs")
+    R.assert_near(got.lse, want[1], want[3], "lse")
+    dw = torch.full((m, vocab, cols), float("nan"), device="cuda", dtype=par)
+    dx = zeno.linear_logprobs_gradient(x, w, t, got.lse, gl, dweight=dw)
+    ref = E.logprobs_gradient(x, w[1:], t - 1, got.lse, gl, 1.0, BF16 if act == par == BF16 else F32)
+    R.assert_near(dx, ref[0], ref[2], "dx")
+    R.assert_near(dw[:, 1:], ref[1], ref[3], "dw")
+    assert (dw[:, 0] == 0).all()
+    # as the target of the first token: D of it is g, and that word's gradient g times the hidden states
+    t[0, 0] = 0
+    gl[0, 0] = 0.25
+    got = zeno.linear_logprobs(x, w, t)
+    assert torch.isfinite(got.lse).all() and (got.logprobs[0, 0] < -2.9e38)
+    dx = zeno.linear_logprobs_gradient(x, w, t, got.lse, gl, dweight=dw)
+    # g times the word's entry: the largest product of terms, each of three bfloat16 terms' products off by 4 U of the sum of their magnitudes
+    R.assert_near(dx[0, 0, 0], 0.25 * w[0, 0].double().cpu(), 100 * R.U * 0.25 * 3e38, "dx")
+    R.assert_near(dx[0, 1:], ref[0][0, 1:], ref[2][0, 1:], "dx of the others")
+    own = 0.25 * x[0, 0].double()
+    R.assert_near(dw[0, 0], own, 100 * R.U * own.abs(), "dw")
+    assert torch.isfinite(dw).all() and torch.isfinite(dx).all()
