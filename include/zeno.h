@@ -444,7 +444,10 @@ zeno_status zeno_embed_gradient(int32_t device, int32_t type, int32_t param_type
  * products whose magnitudes sum to 2^135 or more (the terms' own sums overflow then).  A logit of minus infinity, or as far below
  * lse as binary32 goes, is a probability of zero, here and in the gradient.
  * Weights that are bfloat16, aligned to 16 bytes, in rows and groups of multiples of 8 entries, are read as they lie; others are
- * rewritten in the workspace, up to 768 MB of them at a time. */
+ * rewritten in the workspace (2 bytes an entry, 6 of binary32), up to 768 MB at a time, or 2,048 words of every group where those
+ * take more.  Besides, the workspace holds x (2 bytes an entry, 6 of binary32), up to 8 bytes for every token and 64 words of the
+ * vocabulary, 16 bytes a token, 12 a group and up to 40 MB; where groups have weights of their own, every group's tokens count as
+ * a multiple of 256 (128 if they are no more). */
 int64_t zeno_linear_logprobs_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols, int64_t vocab,
                                        const void *w, int64_t ldw);
 zeno_status zeno_linear_logprobs(int32_t device, int32_t type, int32_t param_type, const zeno_rows *x, int32_t m, int64_t n,
@@ -456,7 +459,10 @@ zeno_status zeno_linear_logprobs(int32_t device, int32_t type, int32_t param_typ
  * lse, g_logprob: float[m][n]; a token whose lse is minus infinity has no gradient.  dx or NULL: like x; zero for a token
  * without a target, whose lse and g_logprob are not read.  dw or NULL: vocab x cols entries for every
  * group, lddw entries from one group's to the next (a slice of V), also where w is shared.  The logits are computed again, a
- * piece of the vocabulary at a time; D is kept for that piece, in two bfloat16 terms (three, as above, if x or w is binary32).
+ * piece of the vocabulary at a time; D is kept for that piece, in two bfloat16 terms (three, as above, if x or w is binary32):
+ * pieces are as long as D takes 512 MB and rewritten weights 768 MB, but 2,048 words at least.  Besides, the workspace holds x, as
+ * above, 4 bytes an entry for dx, 20 bytes a token, 12 a group and up to 40 MB; every group's tokens count as a multiple of 16, of
+ * 256 where groups have weights of their own.
  * exp(z - lse) carries the rounding of lse, 2^-24 |lse|. */
 int64_t zeno_linear_logprobs_gradient_workspace(int32_t type, int32_t param_type, int32_t m, int64_t n, int64_t cols,
                                                 int64_t vocab, const void *w, int64_t ldw, int32_t want_dx);

@@ -14,7 +14,7 @@ namespace {
 // Of D, and of rewritten weights.  Every boundary between launches shows: 10 x 1778 tokens, 7744 words by 320 columns (binary32, weights bfloat16) take 1.19 ms,
 // in pieces of 256 MB 1.29, of 96 MB, which L2 would hold, 1.51.
 constexpr int64_t kPieceBytes = (int64_t)512 << 20, kWeightBytes = (int64_t)768 << 20;
-constexpr int kMinPiece = 2048;
+constexpr int kMinPiece = 2048;                                       // words of a piece whatever its bytes: shorter ones would be all boundaries, and dx's sums in memory
 
 // What lies where in the workspace, and how the vocabulary is cut.
 struct Plan {
@@ -88,9 +88,9 @@ Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     p.pitch = up(a.cols, 8);
     p.parts_pitch = up(a.cols, 4);
     const int64_t per_word = p.w_packed ? p.groups * p.w_terms * p.pitch * 2 : 0, per_prob = gradient ? p.slots * p.prob_terms * 2 : 0;
-    int64_t most = a.vocab;
-    if (per_word && kWeightBytes / per_word < most) most = kWeightBytes / per_word;
-    if (per_prob && kPieceBytes / per_prob < most) most = kPieceBytes / per_prob;
+    int64_t most = up(a.vocab, 256);
+    if (per_word && kWeightBytes / per_word < most) most = kWeightBytes / per_word / 256 * 256;
+    if (per_prob && kPieceBytes / per_prob < most) most = kPieceBytes / per_prob / 256 * 256;
     if (most < kMinPiece) most = kMinPiece;
     p.pieces = (int)((a.vocab + most - 1) / most);
     p.piece = up((a.vocab + p.pieces - 1) / p.pieces, 256);
