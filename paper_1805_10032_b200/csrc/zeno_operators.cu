@@ -199,7 +199,7 @@ zeno_status zeno_token_gradient(int32_t device, int32_t type, const zeno_rows *l
 
 // Rows of a table or of output weights, one after the other: a group's begin `ld` entries after the previous group's (0: one matrix for all of them).
 static zeno_status check_table(const void *w, int64_t ld, int size, int32_t m, int64_t vocab, int64_t cols, bool shared) {
-    if (!w || !placed(w, size)) return ZENO_ERR_INVALID_ARG;
+    if ((!w && m > 0) || !placed(w, size)) return ZENO_ERR_INVALID_ARG;
     if (m > 1 && !(shared && ld == 0) && ld < vocab * cols) return ZENO_ERR_INVALID_ARG;
     return ZENO_OK;
 }

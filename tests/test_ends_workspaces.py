@@ -1,4 +1,4 @@
-"""The workspaces of the log probabilities from hidden states and of their gradient, against what the header says of them."""
+"""The workspaces of the log probabilities from hidden states and of their gradient, against what the header says of them; calls of no groups."""
 import pytest
 
 from paper_1805_10032_b200 import build as zbuild
@@ -44,3 +44,14 @@ def test_no_larger_than_the_header_says(lib, type, ptype, m, n, cols, vocab, mod
     for want_dx in (0, 1):
         gradient = weights + probs + tokens * (row * x_entry + want_dx * row * 4 + 20) + 12 * m
         assert 0 < lib.zeno_linear_logprobs_gradient_workspace(type, ptype, m, n, cols, vocab, P, ldw, want_dx) <= gradient + 40 * MB
+
+
+def test_no_groups_with_weights_of_their_own(lib):
+    """Of no groups there are no weights, nor an address of them."""
+    x = zeno.RowsDesc(None, 64, 640)
+    assert lib.zeno_embed(0, F32, F32, None, 0, 10, 100, 64, None, 6400, 1.0, x, None) == zeno.OK
+    assert lib.zeno_embed_gradient(0, F32, F32, None, x, 0, 10, 100, 64, 1.0, 0, None, 6400, None, 0, None) == zeno.OK
+    assert lib.zeno_linear_logprobs_workspace(F32, F32, 0, 10, 64, 100, None, 6400) == 0
+    assert lib.zeno_linear_logprobs(0, F32, F32, x, 0, 10, 64, 100, None, 6400, None, 1.0, None, None, None, 0, None) == zeno.OK
+    assert lib.zeno_linear_logprobs_gradient_workspace(F32, F32, 0, 10, 64, 100, None, 6400, 1) == 0
+    assert lib.zeno_linear_logprobs_gradient(0, F32, F32, x, 0, 10, 64, 100, None, 6400, None, 1.0, None, None, x, None, 6400, None, 0, None) == zeno.OK
