@@ -179,11 +179,6 @@ __global__ void __launch_bounds__(kOrderThreads) head_order_kernel(const int32_t
     if (threadIdx.x == 0) counts[worker] = base;
 }
 
-__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-
 // The leading 8 bits of what is left of each number, TERMS times: three hold a binary32 number exactly (from 2^-110 on; a smaller one has bits under
 // bfloat16's smallest step, 2^-133).  An infinity or NaN is its first term.
 template <int TERMS>
@@ -258,23 +253,18 @@ struct Eight {
     }
 };
 
-// Some threads rewrite ROWS rows of cols entries (NULL: zeros), eight of each to a thread and turn, all of a turn's rows asked for at once.
-template <typename T, int TERMS, int ROWS>
-__device__ __forceinline__ void rows_terms(const T *const (&from)[ROWS], __nv_bfloat16 *const (&to)[ROWS], int64_t cols, int64_t pitch, int64_t plane, bool vectors, int thread,
-                                           int threads) {
+// Some threads rewrite a row of cols entries (NULL: zeros), eight to a thread and turn.
+template <typename T, int TERMS>
+__device__ __forceinline__ void row_terms(const T *from, __nv_bfloat16 *to, int64_t cols, int64_t pitch, int64_t plane, bool vectors, int thread, int threads) {
     for (int64_t c = thread * 8; c < pitch; c += threads * 8) {
-        Eight<T> e[ROWS];
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) e[r].load(from[r], c, cols, vectors);
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            if constexpr (sizeof(T) == 2) {
-                if (to[r]) *reinterpret_cast<uint4 *>(to[r] + c) = e[r].bits(from[r], c, cols, vectors);
-            } else {
-                float f[8];
-                e[r].get(f, from[r], c, cols, vectors);
-                if (to[r]) put_terms<TERMS>(f, to[r] + c, plane);
-            }
+        Eight<T> e;
+        e.load(from, c, cols, vectors);
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint4 *>(to + c) = e.bits(from, c, cols, vectors);
+        } else {
+            float f[8];
+            e.get(f, from, c, cols, vectors);
+            put_terms<TERMS>(f, to + c, plane);
         }
     }
 }
@@ -376,9 +366,7 @@ __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
             }
         }
         const T *from = token >= 0 ? static_cast<const T *>(a.x.data) + worker * a.x.group + token * a.x.row : nullptr;
-        const T *const froms[1] = {from};
-        __nv_bfloat16 *const tos[1] = {at<__nv_bfloat16>(a, p.x) + slot * p.pitch};
-        rows_terms<T, TERMS, 1>(froms, tos, a.cols, p.pitch, p.slots * p.pitch, args.vectors, thread, threads);
+        row_terms<T, TERMS>(from, at<__nv_bfloat16>(a, p.x) + slot * p.pitch, a.cols, p.pitch, p.slots * p.pitch, args.vectors, thread, threads);
     }
 }
 
@@ -389,20 +377,10 @@ __global__ void __launch_bounds__(256) head_words_kernel(const T *w, int64_t ldw
                                                          __nv_bfloat16 *out, int vectors, int threads_log2, int beside) {
     if (!beside) pdl_wait();
     pdl_launch_dependents();
-    constexpr int kRows = 1;
     const int threads = 1 << threads_log2, rows_of_block = 256 >> threads_log2;
-    const int64_t stride = (int64_t)gridDim.x * rows_of_block;
-    for (int64_t q0 = (int64_t)blockIdx.x * rows_of_block + (threadIdx.x >> threads_log2); q0 < total; q0 += kRows * stride) {
-        const T *from[kRows];
-        __nv_bfloat16 *to[kRows];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const int64_t q = q0 + r * stride;
-            const uint32_t group = (uint32_t)(q < total ? q : 0) / (uint32_t)words, v = (uint32_t)(q < total ? q : 0) - group * words;
-            from[r] = q < total ? w + group * ldw + (v0 + v) * cols : nullptr;
-            to[r] = q < total ? out + ((int64_t)group * TERMS * piece + v) * pitch : nullptr;
-        }
-        rows_terms<T, TERMS, kRows>(from, to, cols, pitch, piece * pitch, vectors, threadIdx.x & (threads - 1), threads);
+    for (int64_t q = (int64_t)blockIdx.x * rows_of_block + (threadIdx.x >> threads_log2); q < total; q += (int64_t)gridDim.x * rows_of_block) {
+        const uint32_t group = (uint32_t)q / (uint32_t)words, v = (uint32_t)q - group * words;
+        row_terms<T, TERMS>(w + group * ldw + (v0 + v) * cols, out + ((int64_t)group * TERMS * piece + v) * pitch, cols, pitch, piece * pitch, vectors, threadIdx.x & (threads - 1), threads);
     }
     if (beside) pdl_wait();
 }

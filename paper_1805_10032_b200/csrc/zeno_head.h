@@ -92,4 +92,11 @@ __host__ __device__ inline int head_splits(uint32_t tiles, uint32_t pairs, int m
     return fit < most ? fit : most;
 }
 
+#ifdef __CUDACC__
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+#endif
+
 }  // namespace zeno

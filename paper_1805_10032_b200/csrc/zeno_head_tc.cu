@@ -118,24 +118,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Two sums, products at a time: half the instructions of what follows a narrow layer's logits (7168 tokens, 60000 words by 64 columns: 261 us, so 248; 17 x 390
+// What follows a narrow layer's logits takes two sums, or products, at a time, half the instructions (7168 tokens, 60000 words by 64 columns: 261 us, so 248; 17 x 390
 // tokens, 29736 words by 28, gradient: 387, 341).
-__device__ __forceinline__ void add2(float &x, float &y, float a, float b) {
-    asm("{\n.reg .b64 u, v;\nmov.b64 u, {%0, %1};\nmov.b64 v, {%2, %3};\nadd.rn.f32x2 u, u, v;\nmov.b64 {%0, %1}, u;\n}" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
-}
-__device__ __forceinline__ void mul2(float &x, float &y, float a) {
-    asm("{\n.reg .b64 u, v;\nmov.b64 u, {%0, %1};\nmov.b64 v, {%2, %2};\nmul.rn.f32x2 u, u, v;\nmov.b64 {%0, %1}, u;\n}" : "+f"(x), "+f"(y) : "f"(a));
-}
-// x = x a + b
-__device__ __forceinline__ void fma2(float &x, float &y, float a, float b, float to_x, float to_y) {
-    asm("{\n.reg .b64 u, v, w;\nmov.b64 u, {%0, %1};\nmov.b64 v, {%2, %3};\nmov.b64 w, {%4, %5};\nfma.rn.f32x2 u, u, v, w;\nmov.b64 {%0, %1}, u;\n}"
-        : "+f"(x), "+f"(y) : "f"(a), "f"(b), "f"(to_x), "f"(to_y));
-}
+__device__ __forceinline__ Two two_at(const float *f) { return Two{f[0], f[1]}; }
+__device__ __forceinline__ void put_two(float *f, Two v) { f[0] = v.x, f[1] = v.y; }
 constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = (float)(1.4426950408889634 - (double)kLog2e);
-__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
 
 // Division by the same number again and again: a multiplication by its reciprocal, rounded down, whose quotient is at most two too small.
 struct Divisor {
@@ -441,7 +428,7 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                 const bool valid = row < it.rows_end;
                 const int have = (int)min((int64_t)kCols, h.piece - col);          // words of this thread
 #pragma unroll
-                for (int c = 0; c < kCols; c += 2) mul2(acc[c], acc[c + 1], h.scale);
+                for (int c = 0; c < kCols; c += 2) put_two(acc + c, mul2(two_at(acc + c), both(h.scale)));
                 if (have < kCols)
 #pragma unroll
                     for (int c = 0; c < kCols; ++c)
@@ -453,18 +440,17 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                     for (int c = 0; c < kCols; ++c) z = c == target ? acc[c] : z;
                     if (target >= 0 && target < have) h.target_logit[row] = z;
                 }
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sum[4] = {};
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                Two sum[2] = {};
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) top[c & 3] = fmaxf(top[c & 3], acc[c]);
                 const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), beside = most == -INFINITY ? 0.f : most;
 #pragma unroll
                 for (int c = 0; c < kCols; c += 2) {
-                    float x = acc[c], y = acc[c + 1];
-                    add2(x, y, -beside, -beside);
-                    mul2(x, y, kLog2e);
-                    add2(sum[c & 2], sum[(c & 2) + 1], exp2_fast(x), exp2_fast(y));
+                    const Two t = mul2(add2(two_at(acc + c), both(-beside)), both(kLog2e));
+                    sum[c >> 1 & 1] = add2(sum[c >> 1 & 1], Two{exp2_fast(t.x), exp2_fast(t.y)});
                 }
-                if (valid && have > 0) h.part[(int64_t)row * h.part_pitch + (h.v0 + col) / kCols] = make_float2(most, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+                if (valid && have > 0) h.part[(int64_t)row * h.part_pitch + (h.v0 + col) / kCols] = make_float2(most, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
             }
             if constexpr (STEP == HeadStep::kProbs) {
                 const bool valid = row < it.rows_end;
@@ -475,28 +461,22 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                 // p - [the target], times -g
 #pragma unroll
                 for (int c = 0; c < kCols; c += 2) {
-                    fma2(acc[c], acc[c + 1], h.scale, h.scale, -lse, -lse);
-                    float t0 = acc[c], t1 = acc[c + 1];
-                    mul2(t0, t1, kLog2e);
-                    float p0 = exp2_fast(t0), p1 = exp2_fast(t1);
+                    const Two z = fma2(two_at(acc + c), both(h.scale), both(-lse)), t = mul2(z, both(kLog2e));
+                    Two q = {exp2_fast(t.x), exp2_fast(t.y)};
                     if (h.prob_terms > 2) {                         // what t is off by
-                        float e0 = acc[c], e1 = acc[c + 1], f0 = acc[c], f1 = acc[c + 1];
-                        fma2(e0, e1, kLog2e, kLog2e, -t0, -t1);
-                        fma2(f0, f1, kLog2eRest, kLog2eRest, e0, e1);
-                        mul2(f0, f1, 0.69314718f);
-                        fma2(f0, f1, p0, p1, p0, p1);
-                        p0 = p0 == 0.f ? 0.f : f0;              // of t beyond binary32 the correction is none (a NaN remains one)
-                        p1 = p1 == 0.f ? 0.f : f1;
+                        const Two off = fma2(z, both(kLog2eRest), fma2(z, both(kLog2e), Two{-t.x, -t.y}));
+                        const Two full = fma2(mul2(off, both(0.69314718f)), q, q);
+                        q.x = q.x == 0.f ? 0.f : full.x;            // of t beyond binary32 the correction is none (a NaN remains one)
+                        q.y = q.y == 0.f ? 0.f : full.y;
                     }
-                    acc[c] = p0;
-                    acc[c + 1] = p1;
+                    put_two(acc + c, q);
                 }
                 if (__any_sync(0xffffffffu, here))
 #pragma unroll
                     for (int c = 0; c < kCols; ++c)
                         if (here && c == target) acc[c] -= 1.f;
 #pragma unroll
-                for (int c = 0; c < kCols; c += 2) mul2(acc[c], acc[c + 1], -g);
+                for (int c = 0; c < kCols; c += 2) put_two(acc + c, mul2(two_at(acc + c), both(-g)));
                 if (__any_sync(0xffffffffu, none))
 #pragma unroll
                     for (int c = 0; c < kCols; ++c) acc[c] = none ? 0.f : acc[c];
@@ -512,10 +492,8 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                             for (int e = 0; e < 4; ++e) {
                                 float *f = &acc[c0 + q * 8 + e * 2];
                                 v[e] = two_bf16(f[0], f[1]);
-                                float hi0 = __uint_as_float(v[e] << 16), hi1 = __uint_as_float(v[e] & 0xffff0000u);
-                                fma2(hi0, hi1, -1.f, -1.f, f[0], f[1]);             // what the next term holds
-                                f[0] = hi0;
-                                f[1] = hi1;
+                                // what the next term holds
+                                put_two(f, fma2(Two{__uint_as_float(v[e] << 16), __uint_as_float(v[e] & 0xffff0000u)}, both(-1.f), two_at(f)));
                             }
                             put16(q, make_uint4(v[0], v[1], v[2], v[3]));
                         }
@@ -573,35 +551,34 @@ __global__ void __launch_bounds__((Shape<STEP, N, COLS, BLOCKS>::kThreads), 1) h
                         // Rows of any alignment: 128 bytes of 32 rows by way of shared memory (a row's 16-byte pieces turned about by the row, so that neither lanes
                         // along a row nor lanes along the rows meet in a bank), then 16 bytes at a time to where memory has such a boundary, put together from two
                         // pieces, and single entries before the first and behind the last of them.  Eight lanes to a row.
-                        constexpr int kPer = 16 / sizeof(P), kLog = sizeof(P) == 2 ? 1 : 2, kSpan = 8 * kPer;
+                        constexpr int kSpan = 64;
                         const int l = lane & 7;
 #pragma unroll
                         for (int c0 = 0; c0 < kCols; c0 += kSpan) {
-                            const int bytes = (int)min((int64_t)kSpan, h.cols - col - c0) << kLog;       // of a row
+                            const int bytes = (int)min((int64_t)kSpan, h.cols - col - c0) * 2;           // of a row
                             if (bytes <= 0) break;
                             __syncwarp();
 #pragma unroll
                             for (int q = 0; q < 8; ++q) {
                                 uint32_t v[4];
 #pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    v[e] = sizeof(P) == 4 ? __float_as_uint(acc[c0 + q * kPer + e]) : two_bf16(acc[c0 + q * kPer + e * 2], acc[c0 + q * kPer + (e * 2 + 1) % kPer]);
+                                for (int e = 0; e < 4; ++e) v[e] = two_bf16(acc[c0 + q * 8 + e * 2], acc[c0 + q * 8 + e * 2 + 1]);
                                 put16(q, make_uint4(v[0], v[1], v[2], v[3]));
                             }
                             __syncwarp();
                             uint8_t *to = reinterpret_cast<uint8_t *>(static_cast<P *>(h.dw) + it.group * h.lddw + (h.v0 + warp_row + (lane >> 3)) * h.cols + col + c0);
 #pragma unroll 4
-                            for (int r = lane >> 3; r < rows; r += 4, to += h.cols << (2 + kLog)) {
+                            for (int r = lane >> 3; r < rows; r += 4, to += h.cols * 8) {
                                 const uint8_t *from = box + r * 128;
                                 const int off = (int)(reinterpret_cast<uintptr_t>(to) & 15);
                                 auto piece = [&](int q) { return *reinterpret_cast<const uint4 *>(from + (((q ^ r) & 7) << 4)); };
                                 // piece l of memory: bytes 16 l - off and on of the row
                                 const int at = 16 * l - off;
-                                const uint4 v = off == 0 ? piece(l) : shifted<sizeof(P)>(piece(l - 1), piece(l), (unsigned)(16 - off) & 15u);
+                                const uint4 v = off == 0 ? piece(l) : shifted<2>(piece(l - 1), piece(l), (unsigned)(16 - off) & 15u);
                                 if (at >= 0 && at + 16 <= bytes) *reinterpret_cast<uint4 *>(to + at) = v;
                                 // what lies before the first whole piece, and behind the last one
                                 const int head = min(bytes, (16 - off) & 15), whole = (bytes - head) & ~15;
-                                for (int mine = l << kLog; mine < bytes - whole; mine += 8 << kLog) {
+                                for (int mine = l * 2; mine < bytes - whole; mine += 16) {
                                     const int byte = mine < head ? mine : mine + whole;
                                     *reinterpret_cast<P *>(to + byte) = *reinterpret_cast<const P *>(from + ((((byte >> 4) ^ r) & 7) << 4) + (byte & 15));
                                 }
@@ -725,19 +702,23 @@ cudaError_t launch_tiles(const HeadTcArgs &h, cudaStream_t s) {
         case HeadStep::kLogits:
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.logits, h.piece, h.slots, h.logits_parts, h.logits_pitch, h.slots * h.logits_pitch, 32, 32)) return cudaErrorInvalidValue;
             return launch<HeadStep::kLogits, N, HN, BLOCKS, float>(a, b, out, extra, k, items * h.logits_parts, s);
-        case HeadStep::kInputs:
+        default: break;
+    }
+    if constexpr (BLOCKS == 2) {
+        if (inputs) {
             if (!encode(&out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.parts, h.cols, h.slots, 1, h.parts_pitch, h.slots * h.parts_pitch, 32, 32) ||
                 !encode(&extra, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, h.extra, N, kHeadPairs * kHeadRows, 1, N, kHeadPairs * kHeadRows * N, 32, 32))
                 return cudaErrorInvalidValue;
             return launch<HeadStep::kInputs, N, HN, 2, float>(a, b, out, extra, k, items, s);
-        case HeadStep::kWeights: break;
+        }
+        const bool bf16 = h.param_type == ZENO_BF16;
+        const int size = bf16 ? 2 : 4;
+        const int64_t plane = h.groups > 1 ? h.lddw : h.cols, limit = (int64_t)1 << 40;
+        k.manual_stores = !(reinterpret_cast<uintptr_t>(h.dw) % 16 == 0 && h.cols * size % 16 == 0 && plane * size % 16 == 0 && plane * size < limit &&
+                            encode(&out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, size, h.dw, h.cols, h.vocab, h.groups, h.cols, plane, 128 / size, 32));
+        return bf16 ? launch<HeadStep::kWeights, N, HN, 2, __nv_bfloat16>(a, b, out, extra, k, items, s) : launch<HeadStep::kWeights, N, HN, 2, float>(a, b, out, extra, k, items, s);
     }
-    const bool bf16 = h.param_type == ZENO_BF16;
-    const int size = bf16 ? 2 : 4;
-    const int64_t plane = h.groups > 1 ? h.lddw : h.cols, limit = (int64_t)1 << 40;
-    k.manual_stores = !(reinterpret_cast<uintptr_t>(h.dw) % 16 == 0 && h.cols * size % 16 == 0 && plane * size % 16 == 0 && plane * size < limit &&
-                        encode(&out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, size, h.dw, h.cols, h.vocab, h.groups, h.cols, plane, 128 / size, 32));
-    return bf16 ? launch<HeadStep::kWeights, N, HN, 2, __nv_bfloat16>(a, b, out, extra, k, items, s) : launch<HeadStep::kWeights, N, HN, 2, float>(a, b, out, extra, k, items, s);
+    return cudaErrorInvalidValue;                                    // a single block's tiles are of logits
 }
 
 }  // namespace
