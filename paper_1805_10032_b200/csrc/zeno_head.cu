@@ -49,22 +49,28 @@ bool mappable(const void *w, int64_t ldw, int64_t groups, int64_t cols) {
 }
 
 // Few tokens take no tensor cores: the weights go by once for every kFew tokens.  32000 words by 4096 columns, tokens in brackets, here and on the tensor
-// cores: bfloat16 60 us (1), 69 (2), 87 (3), there 75 for any number; binary32 101 (1), 128 (4), 181 (8), 316 (12), there 480; bfloat16 words that are not
-// aligned, by 1023 columns, 114 (1), there 66.
+// cores: bfloat16 62 us (1), 73 (2), 87 (3), there 75 for any number; binary32 hidden states 62 (1), 93 (4), 138 (6), there 128; binary32 weights 101 (1), 128 (4),
+// 183 (8), 247 (12), there 452; bfloat16 words that are not aligned, by 4095 columns, 372 (1), there 168.
 constexpr int kFew = 4;
 constexpr int64_t kFewCols = 8192;                                    // their chains of additions are as long as the tensor cores' stretches
+// A warp takes as long for a word of a few columns as for one of 256, some 0.28 ns a word in all, and bfloat16 rows of 1,024 columns as much on their way from
+// memory: of many narrow words the tensor cores are quicker once that outweighs their launches (one token of 8 models of 50000 words by 64 columns: 110 us, there
+// 46; by 384 116, 81; but of one model by 64 24, 24; by 768 28, 38; 131072 words by 2048 97, 118).  Binary32 weights, four and eight tokens of 8 models of 50000
+// words: by 64 columns 153 and 294 us, there 217; by 256 157 and 302, there 332; of 512 by 64 13 and 13, there 18.
+constexpr int64_t kNarrow = 1024, kNarrowTimesWords = (int64_t)50 << 20, kNarrowF32 = 256, kManyWordsF32 = 40960;
 
-// Tokens of a group that this way is quicker for.
-int64_t few_tokens(int type, int param_type, bool aligned) {
-    if (param_type == ZENO_F32) return 3 * kFew;
-    return !aligned ? 0 : type == ZENO_F32 ? kFew : 2;
+// Tokens of a group that this way is quicker for; words: of all groups.
+int64_t few_tokens(int type, int param_type, bool aligned, int64_t cols, int64_t words) {
+    if (param_type == ZENO_F32) return cols < kNarrowF32 && words > kManyWordsF32 ? kFew : 3 * kFew;
+    if (!aligned || (cols < kNarrow && (kNarrow - cols) * words > kNarrowTimesWords)) return 0;
+    return type == ZENO_F32 ? kFew : 2;
 }
 
 Plan plan_head(int type, int param_type, bool gradient, const HeadArgs &a) {
     Plan p = {};
     p.groups = a.ldw != 0 && a.m > 1 ? a.m : 1;
     const int64_t group_rows = p.groups > 1 ? a.n : a.m * a.n;
-    p.few = !gradient && a.cols <= kFewCols && group_rows <= few_tokens(type, param_type, mappable(a.w, a.ldw, p.groups, a.cols));
+    p.few = !gradient && a.cols <= kFewCols && group_rows <= few_tokens(type, param_type, mappable(a.w, a.ldw, p.groups, a.cols), a.cols, p.groups * a.vocab);
     if (p.few) {
         const int64_t lots = (group_rows + kFew - 1) / kFew, most = (a.vocab + 15) / 16, blocks = 2 * 2 * kHeadPairs / (p.groups * lots);      // two blocks an SM
         p.few_blocks = (int)(blocks < 1 ? 1 : blocks < most ? blocks : most);
