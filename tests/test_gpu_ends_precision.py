@@ -104,3 +104,36 @@ def test_gradients_of_a_word_whose_logits_are_minus_a_lot(n, cols, first, act, p
     own = 0.25 * x[0, 0].double()
     R.assert_near(dw[0, 0], own, 100 * R.U * own.abs(), "dw")
     assert torch.isfinite(dw).all() and torch.isfinite(dx).all()
+
+
+@pytest.mark.parametrize("m,n,cols,vocab", [(2, 332, 667, 93), (3, 57, 777, 5001), (16, 61, 1024, 3203)])
+@pytest.mark.parametrize("act,par", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
+def test_gradients_are_as_near_to_64_bits_as_plain_products_in_binary32(m, n, cols, vocab, act, par):
+    """Of confident tokens (whose D is a small difference of a probability from one): the norm of what dx and dweight are off by is no larger than that of products
+    in binary32 whose results are rounded once; in bfloat16, where both are that rounding, by no more than a hundredth."""
+    g = _gen(cols)
+    w = (torch.randn(vocab, cols, generator=g, device="cuda") * (2.5 / cols ** 0.5)).to(par)
+    t = torch.randint(0, vocab, (m, n), generator=g, device="cuda").int()
+    x = (torch.randn(m, n, cols, generator=g, device="cuda") + w.float()[t.long()] * 0.96).to(act)
+    gl = torch.randn(m, n, generator=g, device="cuda") / n
+    hot = torch.nn.functional.one_hot(t.long(), vocab)
+
+    def gradients(kind):
+        xs, ws = x.to(kind), w.to(kind)
+        lse = torch.logsumexp(xs.double() @ ws.double().transpose(-1, -2), -1).float()        # the same for all
+        d = (hot - torch.exp(xs @ ws.T - lse.to(kind).unsqueeze(-1))) * gl.to(kind).unsqueeze(-1)
+        return lse, d @ ws, d.transpose(-1, -2) @ xs
+
+    allowed = torch.backends.cuda.matmul.allow_tf32
+    torch.backends.cuda.matmul.allow_tf32 = False
+    try:
+        lse, *want = gradients(torch.float64)
+        _, dx, dw = gradients(F32)
+    finally:
+        torch.backends.cuda.matmul.allow_tf32 = allowed
+    own_dw = torch.empty(m, vocab, cols, device="cuda", dtype=par)
+    own_dx = zeno.linear_logprobs_gradient(x, w, t, lse, gl, dweight=own_dw)
+    for got, plain, exact in ((own_dx, dx.to(act), want[0]), (own_dw, dw.to(par), want[1])):
+        off, plain_off = ((v.double() - exact).norm() for v in (got, plain))
+        assert off <= (1.01 if got.dtype == BF16 else 1.0) * plain_off, (float(off / plain_off))
+    zeno.check_operator_status()
