@@ -780,6 +780,13 @@ def token_gradient(logits, targets, lse, g_logprob, entropy=None, g_entropy=None
     return out if st == OK else _done(st, "zeno_token_gradient")
 
 
+def _vocabulary(w: torch.Tensor, name: str):
+    """(vocab, columns) of a table or of output weights."""
+    if len(w.shape) < 2:
+        _refuse(f"{name}: [vocab, columns] or [m, vocab, columns] is needed, not {tuple(w.shape)}")
+    return w.shape[-2:]
+
+
 def _matrix(w: torch.Tensor, m: int, rows: int, cols: int, name: str, shared: bool) -> int:
     """Elements between the groups' matrices of contiguous rows: 0 if they share one."""
     shape, strides = w.shape, w.stride()
@@ -804,7 +811,7 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, stream=None):
     columns)).  The result's type is out's, dtype, or the table's."""
     lib = load_library()
     m, n = _group_sizes(tokens)
-    vocab, cols = table.shape[-2:]
+    vocab, cols = _vocabulary(table, "table")
     dev = _device(tokens, table, out)
     _per_token(tokens, tokens.shape, torch.int32, "tokens")
     ldt = _matrix(table, m, vocab, cols, "table", True)
@@ -823,7 +830,7 @@ def embed_gradient(tokens, dy, dtable, scale=1.0, add=False, stream=None):
     add, adds to it (tied weights, after linear_logprobs_gradient)."""
     lib = load_library()
     m, n = _group_sizes(tokens)
-    vocab, cols = dtable.shape[-2:]
+    vocab, cols = _vocabulary(dtable, "dtable")
     dev = _device(tokens, dy, dtable)
     _per_token(tokens, dy.shape[:-1], torch.int32, "tokens")
     if dy.shape[-1] != cols:
@@ -842,7 +849,7 @@ def linear_logprobs(x, weight, targets, scale=1.0, stream=None) -> LinearLogprob
     lib = load_library()
     shape = x.shape
     m, n, cols = _sizes(shape)
-    vocab = weight.shape[-2]
+    vocab = _vocabulary(weight, "weight")[0]
     dev = _device(x, weight, targets)
     _per_token(targets, shape[:-1], torch.int32, "targets")
     ldw = _matrix(weight, m, vocab, cols, "weight", True)
@@ -863,7 +870,7 @@ def linear_logprobs_gradient(x, weight, targets, lse, g_logprob, dweight=None, d
     shape = x.shape
     lead = shape[:-1]
     m, n, cols = _sizes(shape)
-    vocab = weight.shape[-2]
+    vocab = _vocabulary(weight, "weight")[0]
     dev = _device(x, weight, targets, lse, g_logprob, dweight, dx)
     _per_token(targets, lead, torch.int32, "targets")
     _per_token(lse, lead, torch.float32, "lse")

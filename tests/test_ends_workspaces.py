@@ -1,5 +1,6 @@
-"""The workspaces of the log probabilities from hidden states and of their gradient, against what the header says of them; calls of no groups."""
+"""The workspaces of the log probabilities from hidden states and of their gradient, against what the header says of them; calls of no groups; weights that are no matrices."""
 import pytest
+import torch
 
 from paper_1805_10032_b200 import build as zbuild
 from paper_1805_10032_b200 import zeno
@@ -55,3 +56,10 @@ def test_no_groups_with_weights_of_their_own(lib):
     assert lib.zeno_linear_logprobs(0, F32, F32, x, 0, 10, 64, 100, None, 6400, None, 1.0, None, None, None, 0, None) == zeno.OK
     assert lib.zeno_linear_logprobs_gradient_workspace(F32, F32, 0, 10, 64, 100, None, 6400, 1) == 0
     assert lib.zeno_linear_logprobs_gradient(0, F32, F32, x, 0, 10, 64, 100, None, 6400, None, 1.0, None, None, x, None, 6400, None, 0, None) == zeno.OK
+
+
+def test_weights_of_one_dimension_are_refused():
+    t, x, p, w = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3, 8), torch.zeros(2, 3), torch.zeros(8)
+    for call in (lambda: zeno.embed(t, w), lambda: zeno.embed_gradient(t, x, w), lambda: zeno.linear_logprobs(x, w, t), lambda: zeno.linear_logprobs_gradient(x, w, t, p, p)):
+        with pytest.raises(ValueError, match="is needed"):
+            call()
