@@ -317,8 +317,8 @@ zeno_status zeno_score_lsq_static(int32_t device, const float *x, const float *V
  * Conventions besides those at the top of this file: no handle; `device` is the CUDA device of all pointers.  Activations
  * are m groups (workers, or models) of n rows (tokens) each, described by zeno_rows.  m or n may be zero: nothing is read,
  * per-token outputs are left alone and weight gradients become zero.  `type` is the storage type of activations and logits,
- * `param_type` that of weights and weight gradients; sums, statistics and products are kept in binary32, and results are
- * rounded once, when they are stored.  No output may overlap an input or another output unless the call says so.
+ * `param_type` that of weights and weight gradients; sums, statistics and products are kept in binary32 (where a call says
+ * so, as bfloat16 terms of 16 or 24 bits), and results are rounded once, when they are stored.  No output may overlap an input or another output unless the call says so.
  * Scratch is the caller's (`workspace`, 16-byte aligned, as many bytes as the call's _workspace function says, contents
  * irrelevant): calls that may overlap on the GPU need workspaces of their own.  Results do not depend on the order in which
  * blocks run.  The first call on a device makes the CUDA runtime load the library's code: make it before a stream capture.
@@ -439,7 +439,8 @@ zeno_status zeno_embed_gradient(int32_t device, int32_t type, int32_t param_type
  * targets: int32[m][n]; a token whose target is outside [0, vocab) takes no part: logprob and lse 0, its x is not read.
  * logprobs, lse: float[m][n] or NULL.  Products are exact, their sums binary32 (of binary32 x or w the tensor cores take three
  * bfloat16 terms, which hold an entry of 2^-110 or more as it is; products under 2^-24 of the leading one are left out).  The
- * tensor cores add with truncation towards zero; sums go on in additions to nearest after every stretch of the contraction.
+ * tensor cores add with truncation towards zero; sums go on in additions to nearest after every stretch of the contraction (of
+ * 512 indices for bfloat16 x and w: lse is off by up to 2^-22 of it).
  * A row with a logit that is NaN or plus infinity gives NaN; in binary32 any infinity or NaN among its x or in w may, and so may
  * products whose magnitudes sum to 2^135 or more (the terms' own sums overflow then).  A logit of minus infinity, or as far below
  * lse as binary32 goes, is a probability of zero, here and in the gradient.

@@ -67,7 +67,7 @@ cudaError_t launch_head_tc(const HeadTcArgs &h, cudaStream_t s);
 constexpr int kHeadRows = 256;          // rows of a tile
 
 // Tiles of fewer stages wait for the warps that take their sums, which sixteen with 64 columns each do sooner than eight with 128 (12 x 5555 tokens, 40103 words by
-// 84 columns: 1,457 us, 1,589); with more, the room that their boxes take is better spent on stages (132 tokens, 40576 words by 5568 columns in binary32:
+// 84 columns: 1,315 us, 1,490); with more, the room that their boxes take is better spent on stages (132 tokens, 40576 words by 5568 columns in binary32:
 // 168 us a piece with eight, 189).
 inline bool head_brief(int pairs, int64_t cols) { return pairs * ((cols + 63) / 64) < 16; }
 constexpr int kHeadPairs = 74;          // pairs of SMs of this design

@@ -41,10 +41,11 @@ __device__ unsigned g_given_up;                      // blocks whose bounded wai
 
 // The tensor core adds with truncation towards zero, about 1.4e-8 of a sum with every 16 products (where all are positive).  So a set of sums in TMEM takes a
 // stretch of the contraction only, and goes on in registers, in additions to nearest.  Stretches of 256 where binary32 operands are multiplied (by 512,
-// gradients are off by 1.3 times as much as by plain products in binary32), of 128 for their logits, whose error a probability near one multiplies (2 x 332 tokens, 93
-// words by 667 columns: dx off by less than 0.9e-6, by 256 by 1.3e-6, in 1 % less time); of 512 for logits of bfloat16 operands (4096 tokens, 131072 words, 4096
-// columns: 2.50 ms, by 256 2.65), for D's as for lse's, so that a row's probabilities are those that lse is the sum of; of 1,024 for gradients that are rounded
-// to bfloat16 anyway.
+// gradients are off by 1.3 times as much as by plain products in binary32), of 128 for their logits, whose error a probability near one multiplies (3 x 57 tokens, 5001
+// words by 777 columns: dx off by 4.4e-7, dW by 3.1e-7, by 256 by 7.5e-7 and 7.0e-7 in the same 96 us; 2048 tokens, 40576 words by 4096 9.7 ms, by 256 9.2); of 512
+// for logits of bfloat16 operands (4096 tokens, 131072 words by 4096 columns: 2.83 ms, by 256 2.94, by 128 3.28; lse of 32768 of the words off by 1.9e-7, 0.9e-7,
+// 0.5e-7, by plain products in binary32 0.6e-7), for D's as for lse's, so that a row's probabilities are those that lse is the sum of; of 1,024 for gradients that
+// are rounded to bfloat16 anyway.
 // The terms' planes of a stretch stay in L2 for all pairs of terms.
 constexpr int kDrainTerms = 4, kDrainLogits = 2, kDrain = 8, kDrainBf16 = 16;
 
@@ -118,8 +119,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// What follows a narrow layer's logits takes two sums, or products, at a time, half the instructions (7168 tokens, 60000 words by 64 columns: 261 us, so 248; 17 x 390
-// tokens, 29736 words by 28, gradient: 387, 341).
+// What follows a narrow layer's logits takes two sums, or products, at a time, half the instructions (7168 tokens, 60000 words by 64 columns: 261 us, so 248).
 __device__ __forceinline__ Two two_at(const float *f) { return Two{f[0], f[1]}; }
 __device__ __forceinline__ void put_two(float *f, Two v) { f[0] = v.x, f[1] = v.y; }
 constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = (float)(1.4426950408889634 - (double)kLog2e);
@@ -136,7 +136,7 @@ struct Divisor {
 };
 
 // head_tile() by reciprocals: of kHeadBand * col_tiles, and of the rows of the last band.  (Bound by the exponentials' unit, which divisions' conversions take
-// turns on: 7168 tokens, 60000 words by 64 columns: 228 us, by divisions 248.)
+// turns on: 7168 tokens, 60000 words by 64 columns: 235 us, by divisions 248.)
 __device__ __forceinline__ HeadTile head_tile(uint32_t t, uint32_t row_tiles, const Divisor &band_tiles, const Divisor &last_rows) {
     const uint32_t band = band_tiles(t), in = t - band * band_tiles.d;
     const bool whole = (band + 1) * kHeadBand <= row_tiles;
