@@ -294,8 +294,10 @@ __host__ __device__ __forceinline__ V *at(const HeadArgs &a, int64_t offset) {
     return reinterpret_cast<V *>(static_cast<uint8_t *>(a.workspace) + offset);
 }
 
-// blockIdx.y is the worker.  ALONE: of a few tokens every block finds the order itself, which saves a launch (and 2 us of 22 for 1648 tokens, 449 words by 300 columns).
-constexpr int64_t kAloneTokens = 2048, kAloneAll = 8192;              // of a worker, and of all
+// blockIdx.y is the worker.  ALONE: of a few tokens every block finds the order itself, which saves a launch (and 2 us of 25 for 1648 tokens, 449 words by 300
+// columns), but reads all workers' tokens before its own (8 x 1000 tokens, 200 words by 64 columns: 26 us, by the other kernel 24; 500 x 1 44, 19; 8000 x 1 2,290, 70).
+constexpr int64_t kAloneTokens = 2048;
+constexpr int kAloneWorkers = 32;
 
 template <typename T, int TERMS, bool ALONE>
 __global__ void __launch_bounds__(256) head_slots_kernel(const SlotsArgs args) {
@@ -696,7 +698,7 @@ dim3 grid_for(int64_t blocks) { return dim3((unsigned)(blocks < 148 * 16 ? block
 
 
 cudaError_t fill_slots(int type, const HeadArgs &a, const Plan &p, cudaStream_t s) {
-    const bool alone = a.n <= kAloneTokens && a.m * a.n <= kAloneAll;
+    const bool alone = a.m <= kAloneWorkers && a.m * a.n <= kAloneTokens;
     if (!alone) {
         const cudaError_t e = launch_chained(head_order_kernel, dim3(a.m), dim3(kOrderThreads), 0, s, true, a.targets, a.n, a.vocab, at<int>(a, p.counts), at<int>(a, p.list), at<int>(a, p.rank));
         if (e != cudaSuccess) return e;

@@ -137,3 +137,27 @@ def test_gradients_are_as_near_to_64_bits_as_plain_products_in_binary32(m, n, co
         off, plain_off = ((v.double() - exact).norm() for v in (got, plain))
         assert off <= (1.01 if got.dtype == BF16 else 1.0) * plain_off, (float(off / plain_off))
     zeno.check_operator_status()
+
+
+@pytest.mark.parametrize("m,n", [(32, 64), (33, 2), (500, 3), (4000, 1), (9, 250)])
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_many_workers_of_few_tokens(m, n, act):
+    """Workers that share weights, few tokens each, some without a target: every one's log probabilities, lse and gradient."""
+    g = _gen(m)
+    cols, vocab = 40, 70
+    x, w = _head(g, m, n, cols, vocab, act, act, False)
+    t = torch.randint(-20, vocab, (m, n), generator=g, device="cuda").int()
+    gl = torch.randn(m, n, generator=g, device="cuda")
+    got = zeno.linear_logprobs(x, w, t)
+    flat = lambda v: v.reshape(1, m * n, *v.shape[2:])  # noqa: E731
+    want = E.logprobs(flat(x), w, flat(t), 1.0)
+    R.assert_near(flat(got.logprobs), want[0], want[2], "logprobs")
+    R.assert_near(flat(got.lse), want[1], want[3], "lse")
+    dw = torch.full((m, vocab, cols), float("nan"), device="cuda", dtype=act)
+    dx = zeno.linear_logprobs_gradient(x, w, t, got.lse, gl, dweight=dw)
+    for i in range(0, m, max(1, m // 40)):
+        ref = E.logprobs_gradient(x[i:i + 1], w, t[i:i + 1], got.lse[i:i + 1], gl[i:i + 1], 1.0, act)
+        R.assert_near(dx[i:i + 1], ref[0], ref[2], "dx")
+        R.assert_near(dw[i:i + 1], ref[1], ref[3], "dw")
+    assert torch.isfinite(dw).all()
+    zeno.check_operator_status()
